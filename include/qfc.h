@@ -312,6 +312,103 @@ qfc_status_t qfc_attention(const void *q, const void *kcache, const void *vcache
                            const qfc_attn_shape_t *shape, void *workspace, size_t workspace_bytes,
                            void *out_f16, void *stream);
 
+/* ---- Batches of different requests: a paged cache held in 4 bits, attention over it, adapters ----
+ *
+ * A batch of `batch` requests, each with new tokens of its own behind positions of its own.  The new tokens lie one request behind
+ * the other: rows token_start[b] .. token_start[b + 1] - 1 of every [tokens, ...] array are request b's, and they are
+ * the last of its context[b] positions.  Position p of request b is place p % QFC_PAGE_POSITIONS of page
+ * page_table[b * table_width + p / QFC_PAGE_POSITIONS].
+ *   token_start  device, int32 [batch + 1], not descending, from 0 on; rows from token_start[batch] on belong to nobody: outputs are left as
+ *                they were there
+ *   context      device, int32 [batch]; 0 and more (a request without tokens may have any)
+ *   page_table   device, int32 [batch, table_width]; an entry outside [0, num_pages) is no page: nothing is stored there, and
+ *                attention does not see its positions
+ *   tokens       rows of the [tokens, ...] arrays (0: nothing to do)
+ *   max_tokens, max_context  no request has more; max_context <= table_width * QFC_PAGE_POSITIONS.  The launches and the workspace
+ *                are sized by them, so that the arrays may change from replay to replay of a captured graph.
+ * Where the arrays break these rules the calls stay inside every buffer; the results of the requests in question are not defined. */
+#define QFC_PAGE_POSITIONS 64
+typedef struct qfc_requests {
+    const int32_t *token_start, *context, *page_table; /* device */
+    int32_t batch, tokens, max_tokens, max_context, table_width;
+} qfc_requests_t;
+
+/* A cache of num_pages pages of 64 positions for h_kv heads of d_head (64, 128 or 256) values, keys and values in 4 bits: for each 32
+ * consecutive values of a position's head a binary16 step and a binary16 offset, value = offset + step * (code - 8), code 0 .. 15.
+ * From binary16 values x (operations rounded to 32 bits each):
+ *   step = fp16((max - min) / 15), offset = fp16(min + 8 step), code = clamp(rne((x - offset) * (1 / step)) + 8, 0, 15); step 0: code 8.
+ * pages: device, 16-byte aligned, qfc_q4_cache_size bytes (80 * d_head per page and head); need not be initialized.  Values have to be finite. */
+typedef struct qfc_q4_cache {
+    void *pages; /* device */
+    int32_t num_pages, h_kv, d_head;
+} qfc_q4_cache_t;
+/* Bytes of such a cache's pages (`cache` and `bytes` host pointers; the member `pages` is not read). */
+qfc_status_t qfc_q4_cache_size(const qfc_q4_cache_t *cache, size_t *bytes);
+
+/* Rotary embedding: the first rot_dim values (a multiple of 16, up to d_head) of a query or key head are rotated in pairs by the
+ * angle position * f_i, i < rot_dim / 2; the others stay.
+ *   layout  QFC_ROPE_HALF: pairs (i, i + rot_dim / 2);  QFC_ROPE_INTERLEAVED: pairs (2 i, 2 i + 1)
+ *   f_i     base^(-2 i / rot_dim), scaled for contexts beyond the trained ones: divided by `factor` (1 and more) where original_positions is 0; with
+ *           original_positions > 0 by parts: r = original_positions * f_i / (2 pi) turns; kept where r >= high_turns, divided by factor where
+ *           r <= low_turns, and between them keep * f_i + (1 - keep) * f_i / factor with keep = (r - low_turns) / (high_turns - low_turns)
+ *           (0 <= low_turns < high_turns)
+ *   amplitude  what cosines and sines are multiplied with (1: a rotation)
+ * base > 1. */
+enum { QFC_ROPE_HALF = 0, QFC_ROPE_INTERLEAVED = 1 };
+typedef struct qfc_rotary {
+    int32_t rot_dim, layout;
+    float base, factor;
+    int32_t original_positions;
+    float low_turns, high_turns, amplitude;
+} qfc_rotary_t;
+
+/* Cosines and sines of the first `positions` positions, evaluated in fp64 and rounded once: table (device, 8-byte aligned) float
+ * [positions][rot_dim / 2][2].  (For the half layout, all of the head and factor 1 these are qfc_rope_table's.) */
+qfc_status_t qfc_rotary_table(const qfc_rotary_t *rotary, int32_t positions, float *table, void *stream);
+
+/* Rotation and append for a batch of requests: qkv_f16 [tokens, (h_q + 2 h_kv) * d_head] is the QKV layer's output (query heads,
+ * key heads, value heads).  Queries and keys are rotated by their positions' angles (products and sum exact, rounded once to binary16); the
+ * queries go to q_out, binary16 [tokens, h_q * d_head]; keys and values are quantized into the cache, values as they are.
+ * rotary: host, or null for no rotation (rope_table is not read then); rope_table: from qfc_rotary_table with at least max_context
+ * positions (table_positions says how many).  No two rows may have the same place in the cache.
+ * Errors: QFC_ERR_INVALID_ARG (null pointers, sizes, h_q not a multiple of h_kv, max_context beyond the page table or the
+ * rotary table, rotary members out of range), QFC_ERR_UNSUPPORTED (d_head other than 64, 128, 256; rot_dim not a multiple of 16 or above
+ * d_head; more than 65535 heads or KV heads of all requests), QFC_ERR_ALIGNMENT (16 bytes; int32 arrays 4, the table 8). */
+qfc_status_t qfc_append_q4(const void *qkv_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_rotary_t *rotary,
+                           const float *rope_table, int32_t table_positions, const qfc_q4_cache_t *cache, void *q_out, void *stream);
+
+/* The values that the cache holds for the batch's new tokens: k, v binary16 [tokens, h_kv, d_head]; zeros for a token
+ * without a page.  Errors as qfc_append_q4. */
+qfc_status_t qfc_read_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, void *k, void *v, void *stream);
+
+/* Bytes of scratch qfc_attention_q4 needs for a batch of this size (batch, max_tokens and max_context are read; host pointers). */
+qfc_status_t qfc_attention_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
+
+/* Attention of a batch of requests over the cache: out = softmax(q K^T / sqrt(d_head)) V for each row and head, q and out binary16
+ * [tokens, h_q * d_head].  New token s of S of a request with n positions sees positions 0 .. n - S + s; a row that sees none
+ * (no positions, or no pages) gets zeros.  One token or many per request, in any mixture.
+ * workspace: device scratch of at least qfc_attention_q4_workspace_size bytes.  Errors as qfc_append_q4, QFC_ERR_BUFFER_TOO_SMALL. */
+qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache,
+                              void *workspace, size_t workspace_bytes, void *out_f16, void *stream);
+
+/* Low-rank adapters, `count` of them for one layer of K inputs and N outputs, all of rank `rank` (a multiple of 8, up to 128;
+ * adapters of a smaller rank are filled up with zeros): a binary16 [count, rank, K], b binary16 [count, N, rank], scale fp32 [count]. */
+typedef struct qfc_adapters {
+    const void *a, *b;  /* device */
+    const float *scale; /* device */
+    int32_t count, rank, K, N;
+} qfc_adapters_t;
+
+/* Bytes of scratch qfc_add_adapters needs for M rows (host pointers; of the adapters the sizes are read). */
+qfc_status_t qfc_adapters_workspace_size(const qfc_adapters_t *adapters, int32_t M, size_t *bytes);
+
+/* out[m] = fp16(y[m] + scale[a] B[a] (A[a] x[m])), a = ids[m], beside a shared layer whose output y is: every row (token) may have an
+ * adapter of its own; an id outside [0, count) has none, and out[m] = y[m].
+ *   x binary16 [M, K]; ids device, int32 [M]; y, out binary16 [M, N] (out may be y); K a multiple of 32.
+ * workspace: device scratch of at least qfc_adapters_workspace_size bytes. */
+qfc_status_t qfc_add_adapters(const void *x_f16, int32_t M, const int32_t *ids, const qfc_adapters_t *adapters, const void *y_f16,
+                              void *workspace, size_t workspace_bytes, void *out_f16, void *stream);
+
 /* Embedding lookup from a packed layer (section 4.2: the schemes quantize the
  * embedding table like the layers, and models tie it to the LM head, so the
  * table is the LM head's handle): y[m, k] = fp16(s * Wq[ids[m], k]) with the

@@ -24,10 +24,13 @@ QFC_SCALE_F32, QFC_SCALE_F16 = 0, 1
 QFC_COMPUTE_FP16_DEQUANT, QFC_COMPUTE_INT8_ACT, QFC_COMPUTE_INT8_ACT_DECODE = 0, 1, 2
 QFC_ACT_SILU, QFC_ACT_GELU_TANH = 0, 1
 QFC_PACK_GATED_PAIRS = 1
+QFC_PAGE_POSITIONS = 64
+QFC_ROPE_HALF, QFC_ROPE_INTERLEAVED = 0, 1
 
 EXPORTS = ["qfc_packed_size", "qfc_pack_weights", "qfc_unpack_weights", "qfc_workspace_size",
            "qfc_bind_workspace", "qfc_quantize_activations", "qfc_forward", "qfc_forward_fused", "qfc_forward_static", "qfc_rmsnorm", "qfc_rope_qkv", "qfc_rope_table", "qfc_forward_qkv_rope", "qfc_attention_workspace_size", "qfc_attention", "qfc_forward_q8",
-           "qfc_forward_acc_i32", "qfc_embedding", "qfc_forward_batch", "qfc_destroy", "qfc_status_string"]
+           "qfc_forward_acc_i32", "qfc_embedding", "qfc_q4_cache_size", "qfc_rotary_table", "qfc_append_q4", "qfc_read_q4", "qfc_attention_q4_workspace_size", "qfc_attention_q4",
+           "qfc_adapters_workspace_size", "qfc_add_adapters", "qfc_forward_batch", "qfc_destroy", "qfc_status_string"]
 
 
 class Desc(ctypes.Structure):
@@ -55,6 +58,29 @@ class AttnShape(ctypes.Structure):
     """qfc_attn_shape_t."""
     _fields_ = [("batch", ctypes.c_int32), ("h_q", ctypes.c_int32), ("h_kv", ctypes.c_int32),
                 ("d_head", ctypes.c_int32), ("cache_size", ctypes.c_int32)]
+
+
+class RequestsDesc(ctypes.Structure):
+    """qfc_requests_t."""
+    _fields_ = [("token_start", ctypes.c_void_p), ("context", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("batch", ctypes.c_int32),
+                ("tokens", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("max_context", ctypes.c_int32), ("table_width", ctypes.c_int32)]
+
+
+class CacheDesc(ctypes.Structure):
+    """qfc_q4_cache_t."""
+    _fields_ = [("pages", ctypes.c_void_p), ("num_pages", ctypes.c_int32), ("h_kv", ctypes.c_int32), ("d_head", ctypes.c_int32)]
+
+
+class Rotary(ctypes.Structure):
+    """qfc_rotary_t; see make_rotary."""
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("base", ctypes.c_float), ("factor", ctypes.c_float),
+                ("original_positions", ctypes.c_int32), ("low_turns", ctypes.c_float), ("high_turns", ctypes.c_float), ("amplitude", ctypes.c_float)]
+
+
+class AdaptersDesc(ctypes.Structure):
+    """qfc_adapters_t."""
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("count", ctypes.c_int32), ("rank", ctypes.c_int32),
+                ("K", ctypes.c_int32), ("N", ctypes.c_int32)]
 
 
 class QfcError(RuntimeError):
@@ -111,6 +137,15 @@ def lib() -> ctypes.CDLL:
         L.qfc_forward_q8.argtypes = [vp, vp, vp, i32, vp, vp]
         L.qfc_forward_acc_i32.argtypes = [vp, vp, i32, vp, vp]
         L.qfc_embedding.argtypes = [vp, vp, i32, vp, vp]
+        req, cache, adapters = ctypes.POINTER(RequestsDesc), ctypes.POINTER(CacheDesc), ctypes.POINTER(AdaptersDesc)
+        L.qfc_q4_cache_size.argtypes = [cache, ctypes.POINTER(sz)]
+        L.qfc_rotary_table.argtypes = [ctypes.POINTER(Rotary), i32, vp, vp]
+        L.qfc_append_q4.argtypes = [vp, req, i32, ctypes.POINTER(Rotary), vp, i32, cache, vp, vp]
+        L.qfc_read_q4.argtypes = [req, cache, vp, vp, vp]
+        L.qfc_attention_q4_workspace_size.argtypes = [req, i32, cache, ctypes.POINTER(sz)]
+        L.qfc_attention_q4.argtypes = [vp, req, i32, cache, vp, sz, vp, vp]
+        L.qfc_adapters_workspace_size.argtypes = [adapters, i32, ctypes.POINTER(sz)]
+        L.qfc_add_adapters.argtypes = [vp, i32, vp, adapters, vp, vp, sz, vp, vp]
         L.qfc_forward_batch.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(vp), i32, ctypes.POINTER(vp), i32, vp]
         L.qfc_destroy.argtypes = [vp]
         L.qfc_status_string.argtypes = [ctypes.c_int]
@@ -417,6 +452,147 @@ def qfc_embedding(h, ids: torch.Tensor, y: torch.Tensor):
     _want(ids, torch.int32, (None,), "ids")
     _want(y, torch.float16, (ids.shape[0], K), "y")
     _check(lib().qfc_embedding(h, _ptr(ids), ids.shape[0], _ptr(y), _stream()), "qfc_embedding")
+
+
+_u8, _i32 = torch.uint8, torch.int32
+
+
+def _here(*tensors):
+    """The calls below launch on the current device: their tensors have to be there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t.device.index != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+class PagedCache:
+    """Owner of a 4-bit cache: `num_pages` pages of 64 positions for h_kv heads of d_head values (qfc_q4_cache_t)."""
+
+    def __init__(self, num_pages: int, h_kv: int, d_head: int, device="cuda", pages: torch.Tensor | None = None):
+        self.num_pages, self.h_kv, self.d_head = num_pages, h_kv, d_head
+        self.desc = CacheDesc(None, num_pages, h_kv, d_head)
+        need = qfc_q4_cache_size(self.desc)
+        self.pages = torch.empty(need, dtype=_u8, device=device) if pages is None else pages
+        _want(self.pages, _u8, None, "pages")
+        if self.pages.numel() < need:
+            raise ValueError(f"pages: {self.pages.numel()} bytes, {need} are needed")
+        self.desc.pages = self.pages.data_ptr()
+
+
+class Requests:
+    """A batch of requests (qfc_requests_t): int32 tensors token_start [batch + 1], context [batch], page_table [batch, width], whose contents may change
+    between calls, and the sizes that may not: rows, most new tokens and most positions of a request."""
+
+    def __init__(self, token_start: torch.Tensor, context: torch.Tensor, page_table: torch.Tensor, tokens: int, max_tokens: int, max_context: int):
+        _want(context, _i32, None, "context")
+        batch = context.numel()
+        _want(context, _i32, (batch,), "context")
+        _want(token_start, _i32, (batch + 1,), "token_start")
+        if not (isinstance(page_table, _Tensor) and page_table.dim() == 2):
+            raise ValueError("page_table: a matrix is required")
+        _want(page_table, _i32, (batch, page_table.shape[1]), "page_table")
+        self.token_start, self.context, self.page_table = token_start, context, page_table
+        self.tokens, self.device = tokens, context.device
+        if token_start.device != self.device or page_table.device != self.device:
+            raise ValueError("token_start, context and page_table: on different devices")
+        self.desc = RequestsDesc(token_start.data_ptr(), context.data_ptr(), page_table.data_ptr(), batch, tokens, max_tokens, max_context, page_table.shape[1])
+
+
+def make_rotary(rot_dim: int, base: float, layout: int = QFC_ROPE_HALF, factor: float = 1.0, original_positions: int = 0, low_turns: float = 1.0,
+                high_turns: float = 4.0, amplitude: float = 1.0) -> Rotary:
+    return Rotary(rot_dim, layout, base, factor, original_positions, low_turns, high_turns, amplitude)
+
+
+def qfc_q4_cache_size(desc: CacheDesc) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().qfc_q4_cache_size(ctypes.byref(desc), ctypes.byref(out)), "qfc_q4_cache_size")
+    return out.value
+
+
+def qfc_rotary_table(rotary: Rotary, positions: int, device="cuda") -> torch.Tensor:
+    """cos and sin of the rotary angles of the first `positions` positions: float32 [positions, rot_dim / 2, 2]."""
+    if positions < 1 or rotary.rot_dim < 2:
+        raise ValueError("positions and rot_dim: at least one pair of one position")
+    table = torch.empty((positions, rotary.rot_dim // 2, 2), dtype=_f32, device=device)
+    _here(table)
+    _check(lib().qfc_rotary_table(ctypes.byref(rotary), positions, table.data_ptr(), _stream()), "qfc_rotary_table")
+    return table
+
+
+def qfc_append_q4(qkv: torch.Tensor, requests: Requests, h_q: int, rotary: Rotary | None, rope_table: torch.Tensor | None, cache: PagedCache,
+                  q_out: torch.Tensor):
+    """Rotation of queries and keys, append of keys and values to the cache.  rotary None: no rotation."""
+    T, d = requests.tokens, cache.d_head
+    _want(qkv, _f16, (T, (h_q + 2 * cache.h_kv) * d), "qkv")
+    _want(q_out, _f16, (T, h_q * d), "q_out")
+    rows = 0
+    if rotary is not None:
+        if not isinstance(rope_table, _Tensor):
+            raise ValueError("rope_table: a CUDA tensor is required")
+        rows = rope_table.shape[0]
+        _want(rope_table, _f32, (rows, rotary.rot_dim // 2, 2), "rope_table")
+        _here(rope_table)
+    _here(qkv, q_out, cache.pages, requests)
+    _check(lib().qfc_append_q4(qkv.data_ptr(), ctypes.byref(requests.desc), h_q, ctypes.byref(rotary) if rotary is not None else None,
+                               rope_table.data_ptr() if rotary is not None else None, rows, ctypes.byref(cache.desc), q_out.data_ptr(), _stream()), "qfc_append_q4")
+
+
+def qfc_read_q4(requests: Requests, cache: PagedCache, k: torch.Tensor, v: torch.Tensor):
+    """The values the cache holds for the requests' new tokens: k, v float16 [tokens, h_kv, d_head]."""
+    _want(k, _f16, (requests.tokens, cache.h_kv, cache.d_head), "k")
+    _want(v, _f16, (requests.tokens, cache.h_kv, cache.d_head), "v")
+    _here(k, v, cache.pages, requests)
+    _check(lib().qfc_read_q4(ctypes.byref(requests.desc), ctypes.byref(cache.desc), k.data_ptr(), v.data_ptr(), _stream()), "qfc_read_q4")
+
+
+def qfc_attention_q4_workspace_size(requests: Requests, h_q: int, cache: PagedCache) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().qfc_attention_q4_workspace_size(ctypes.byref(requests.desc), h_q, ctypes.byref(cache.desc), ctypes.byref(out)), "qfc_attention_q4_workspace_size")
+    return out.value
+
+
+def qfc_attention_q4(q: torch.Tensor, requests: Requests, h_q: int, cache: PagedCache, workspace: torch.Tensor, out: torch.Tensor):
+    shape = (requests.tokens, h_q * cache.d_head)
+    _want(q, _f16, shape, "q")
+    _want(out, _f16, shape, "out")
+    _want(workspace, _u8, None, "workspace")
+    _here(q, out, workspace, cache.pages, requests)
+    _check(lib().qfc_attention_q4(q.data_ptr(), ctypes.byref(requests.desc), h_q, ctypes.byref(cache.desc), workspace.data_ptr(), workspace.numel(), out.data_ptr(),
+                                  _stream()), "qfc_attention_q4")
+
+
+class Adapters:
+    """The adapters of one layer (qfc_adapters_t): a float16 [count, rank, K], b float16 [count, N, rank], scale float32 [count]."""
+
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: torch.Tensor):
+        for t, what in ((a, "a"), (b, "b")):
+            if not (isinstance(t, _Tensor) and t.dim() == 3):
+                raise ValueError(f"{what}: three dimensions are required")
+        count, rank, K = a.shape
+        N = b.shape[1]
+        _want(a, _f16, (count, rank, K), "a")
+        _want(b, _f16, (count, N, rank), "b")
+        _want(scale, _f32, (count,), "scale")
+        self.a, self.b, self.scale, self.count, self.rank, self.K, self.N = a, b, scale, count, rank, K, N
+        self.desc = AdaptersDesc(a.data_ptr(), b.data_ptr(), scale.data_ptr(), count, rank, K, N)
+
+
+def qfc_adapters_workspace_size(adapters: Adapters, M: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().qfc_adapters_workspace_size(ctypes.byref(adapters.desc), M, ctypes.byref(out)), "qfc_adapters_workspace_size")
+    return out.value
+
+
+def qfc_add_adapters(x: torch.Tensor, ids: torch.Tensor, adapters: Adapters, y: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor):
+    """out = y + scale[a] B[a] (A[a] x), row by row with a = ids[row]; out may be y."""
+    M = _rows(x, _f16, adapters.K, "x")
+    _want(ids, _i32, (M,), "ids")
+    _want(y, _f16, (M, adapters.N), "y")
+    _want(out, _f16, (M, adapters.N), "out")
+    _want(workspace, _u8, None, "workspace")
+    _here(x, ids, y, out, workspace, adapters.a, adapters.b, adapters.scale)
+    _check(lib().qfc_add_adapters(x.data_ptr(), M, ids.data_ptr(), ctypes.byref(adapters.desc), y.data_ptr(), workspace.data_ptr(), workspace.numel(), out.data_ptr(),
+                                  _stream()), "qfc_add_adapters")
 
 
 class ForwardBatch:

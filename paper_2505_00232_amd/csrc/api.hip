@@ -4,6 +4,7 @@
 #include <new>
 
 #include "../../include/qfc_experimental.h"
+#include "paged_q4.h"
 #include "qfc_internal.h"
 
 using namespace qfc;
@@ -416,6 +417,131 @@ qfc_status_t qfc_attention(const void *q, const void *kcache, const void *vcache
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return QFC_ERR_HIP;
     return hip_status(launch_attention(q, kcache, vcache, a->batch * a->h_kv, S, g, a->d_head, a->cache_size, n_ctx,
                                        workspace, out_f16, cus, static_cast<hipStream_t>(stream)));
+}
+
+// ---- batches of requests
+static bool aligned(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+static qfc_status_t check_q4_cache(const qfc_q4_cache_t *c) {
+    if (!c || c->num_pages < 1 || c->h_kv < 1) return QFC_ERR_INVALID_ARG;
+    if (c->d_head != 64 && c->d_head != 128 && c->d_head != 256) return QFC_ERR_UNSUPPORTED;
+    return QFC_OK;
+}
+
+// Sizes only: what the workspace depends on
+static qfc_status_t check_batch(const qfc_requests_t *r, int32_t h_q, const qfc_q4_cache_t *c) {
+    if (const qfc_status_t s = check_q4_cache(c); s != QFC_OK) return s;
+    if (!r || r->batch < 1 || r->max_tokens < 1 || r->max_context < 1 || h_q < 1 || h_q % c->h_kv != 0) return QFC_ERR_INVALID_ARG;
+    if ((long)h_q + 2L * c->h_kv > 65535 || (long)r->batch * c->h_kv > 65535 || (long)r->max_tokens * h_q > 1L << 26 || r->max_context > 1 << 26) return QFC_ERR_UNSUPPORTED;
+    return QFC_OK;
+}
+
+static qfc_status_t check_requests(const qfc_requests_t *r, int32_t h_q, const qfc_q4_cache_t *c) {
+    if (const qfc_status_t s = check_batch(r, h_q, c); s != QFC_OK) return s;
+    if (!r->token_start || !r->context || !r->page_table || !c->pages || r->tokens < 0 || r->table_width < 1) return QFC_ERR_INVALID_ARG;
+    if ((long)r->table_width * QFC_PAGE_POSITIONS < r->max_context) return QFC_ERR_INVALID_ARG;
+    if (!aligned(r->token_start, 4) || !aligned(r->context, 4) || !aligned(r->page_table, 4) || !aligned16(c->pages)) return QFC_ERR_ALIGNMENT;
+    return QFC_OK;
+}
+
+static Requests on_device(const qfc_requests_t *r, const qfc_q4_cache_t *c) {
+    return Requests{r->token_start, r->context, r->page_table, r->batch, r->tokens, r->max_tokens, r->max_context, r->table_width, c->num_pages};
+}
+
+qfc_status_t qfc_q4_cache_size(const qfc_q4_cache_t *cache, size_t *bytes) {
+    if (!bytes) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_q4_cache(cache); s != QFC_OK) return s;
+    *bytes = (size_t)cache->num_pages * cache->h_kv * 80 * cache->d_head;
+    return QFC_OK;
+}
+
+static qfc_status_t check_rotary(const qfc_rotary_t *r) {
+    if (!r || r->rot_dim < 1 || (r->layout != QFC_ROPE_HALF && r->layout != QFC_ROPE_INTERLEAVED)) return QFC_ERR_INVALID_ARG;
+    if (!(r->base > 1.0f && r->base < INFINITY) || !(r->factor >= 1.0f && r->factor < INFINITY) || !(r->amplitude > 0.0f && r->amplitude < INFINITY) || r->original_positions < 0)
+        return QFC_ERR_INVALID_ARG;
+    if (r->original_positions > 0 && !(r->low_turns >= 0.0f && r->low_turns < r->high_turns && r->high_turns < INFINITY)) return QFC_ERR_INVALID_ARG;
+    return r->rot_dim % 16 == 0 && r->rot_dim <= 256 ? QFC_OK : QFC_ERR_UNSUPPORTED;
+}
+
+qfc_status_t qfc_rotary_table(const qfc_rotary_t *rotary, int32_t positions, float *table, void *stream) {
+    if (const qfc_status_t s = check_rotary(rotary); s != QFC_OK) return s;
+    if (!table || positions < 1) return QFC_ERR_INVALID_ARG;
+    if (!aligned(table, 8)) return QFC_ERR_ALIGNMENT;
+    return hip_status(launch_rotary_table(rotary->rot_dim, rotary->base, rotary->factor, rotary->original_positions, rotary->low_turns, rotary->high_turns, rotary->amplitude,
+                                          positions, table, static_cast<hipStream_t>(stream)));
+}
+
+qfc_status_t qfc_append_q4(const void *qkv_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_rotary_t *rotary, const float *rope_table, int32_t table_positions,
+                           const qfc_q4_cache_t *cache, void *q_out, void *stream) {
+    if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
+    if (!qkv_f16 || !q_out) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(qkv_f16) || !aligned16(q_out)) return QFC_ERR_ALIGNMENT;
+    if (rotary) {
+        if (const qfc_status_t s = check_rotary(rotary); s != QFC_OK) return s;
+        if (rotary->rot_dim > cache->d_head) return QFC_ERR_UNSUPPORTED;
+        if (!rope_table || table_positions < requests->max_context) return QFC_ERR_INVALID_ARG;
+        if (!aligned(rope_table, 8)) return QFC_ERR_ALIGNMENT;
+    }
+    if (requests->tokens == 0) return QFC_OK;
+    const int cus = device_cus();
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_append_q4(qkv_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, rotary ? rotary->rot_dim : 0,
+                                       rotary && rotary->layout == QFC_ROPE_INTERLEAVED, rope_table, cache->pages, q_out, cus, static_cast<hipStream_t>(stream)));
+}
+
+qfc_status_t qfc_read_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, void *k, void *v, void *stream) {
+    if (const qfc_status_t s = check_requests(requests, cache ? cache->h_kv : 0, cache); s != QFC_OK) return s;
+    if (!k || !v) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(k) || !aligned16(v)) return QFC_ERR_ALIGNMENT;
+    if (requests->tokens == 0) return QFC_OK;
+    return hip_status(launch_read_q4(on_device(requests, cache), cache->h_kv, cache->d_head, cache->pages, k, v, static_cast<hipStream_t>(stream)));
+}
+
+qfc_status_t qfc_attention_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes) {
+    if (!bytes) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_batch(requests, h_q, cache); s != QFC_OK) return s;
+    *bytes = attention_q4_workspace(plan_attention_q4(requests->batch, cache->h_kv, h_q / cache->h_kv, requests->max_tokens, requests->max_context, device_cus()), requests->batch,
+                                    cache->h_kv, cache->d_head);
+    return QFC_OK;
+}
+
+qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, void *workspace, size_t workspace_bytes,
+                              void *out_f16, void *stream) {
+    if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
+    if (!q_f16 || !workspace || !out_f16) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(q_f16) || !aligned16(workspace) || !aligned16(out_f16)) return QFC_ERR_ALIGNMENT;
+    const AttnQ4Plan p = plan_attention_q4(requests->batch, cache->h_kv, h_q / cache->h_kv, requests->max_tokens, requests->max_context, device_cus());
+    if (workspace_bytes < attention_q4_workspace(p, requests->batch, cache->h_kv, cache->d_head)) return QFC_ERR_BUFFER_TOO_SMALL;
+    if ((long)p.chunks * requests->batch * cache->h_kv * p.blocks > INT32_MAX) return QFC_ERR_UNSUPPORTED;
+    if (requests->tokens == 0) return QFC_OK;
+    return hip_status(launch_attention_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, p, workspace, out_f16,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+static qfc_status_t check_adapters(const qfc_adapters_t *a, int32_t M) {
+    if (!a || M < 1 || a->count < 1 || a->K < 32 || a->K % 32 != 0 || a->N < 1 || a->rank < 1) return QFC_ERR_INVALID_ARG;
+    // (the launches' second dimensions)
+    return a->rank % 8 == 0 && a->rank <= 128 && a->N <= 65535 * 128 ? QFC_OK : QFC_ERR_UNSUPPORTED;
+}
+
+qfc_status_t qfc_adapters_workspace_size(const qfc_adapters_t *adapters, int32_t M, size_t *bytes) {
+    if (!bytes) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_adapters(adapters, M); s != QFC_OK) return s;
+    *bytes = adapters_workspace(plan_adapters(M, adapters->K, device_cus()), adapters->rank);
+    return QFC_OK;
+}
+
+qfc_status_t qfc_add_adapters(const void *x_f16, int32_t M, const int32_t *ids, const qfc_adapters_t *adapters, const void *y_f16, void *workspace, size_t workspace_bytes,
+                              void *out_f16, void *stream) {
+    if (const qfc_status_t s = check_adapters(adapters, M); s != QFC_OK) return s;
+    if (!x_f16 || !ids || !y_f16 || !workspace || !out_f16 || !adapters->a || !adapters->b || !adapters->scale) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(x_f16) || !aligned16(y_f16) || !aligned16(out_f16) || !aligned16(workspace) || !aligned16(adapters->a) || !aligned16(adapters->b) ||
+        !aligned(ids, 4) || !aligned(adapters->scale, 4))
+        return QFC_ERR_ALIGNMENT;
+    const AdapterPlan p = plan_adapters(M, adapters->K, device_cus());
+    if (workspace_bytes < adapters_workspace(p, adapters->rank)) return QFC_ERR_BUFFER_TOO_SMALL;
+    return hip_status(launch_adapters(x_f16, M, adapters->K, adapters->N, adapters->rank, adapters->count, adapters->a, adapters->b, adapters->scale, ids, y_f16, p, workspace,
+                                      out_f16, static_cast<hipStream_t>(stream)));
 }
 
 qfc_status_t qfc_forward_q8(qfc_handle_t h, const int8_t *xq, const float *sx, int32_t M, void *y_f16,

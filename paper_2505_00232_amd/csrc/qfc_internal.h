@@ -381,4 +381,31 @@ hipError_t launch_skinny_f16(const Geometry &g, const void *packed, const void *
 hipError_t launch_skinny_i8(const Geometry &g, const void *packed, const int8_t *xq_tiled, const float *sx, int M,
                             void *y, const void *residual, int gated_act, int num_cus, hipStream_t st);
 
+// The operators that serve a batch of requests.  Requests (device side): paged_q4.h.
+struct Requests;
+// cos and sin of pos * f_i in 32 bits, [positions][rot / 2][2]; see qfc_rotary_t
+hipError_t launch_rotary_table(int rot, double base, double factor, int original, double low, double high, double amplitude, int positions, float *table, hipStream_t st);
+// rot 0: no rotation, table unused
+hipError_t launch_append_q4(const void *qkv, const Requests &req, int h_q, int h_kv, int d, int rot, bool interleaved, const float *table, void *pages, void *q_out,
+                            int num_cus, hipStream_t st);
+hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, hipStream_t st);
+struct AttnQ4Plan {
+    int rows;         // query rows of a KV head at most
+    int blocks;       // blocks of 16 of them
+    int chunk_pages;  // pages a workgroup takes
+    int chunks;       // workgroups that share the longest request's pages
+};
+AttnQ4Plan plan_attention_q4(int batch, int h_kv, int g, int max_tokens, int max_context, int num_cus);
+size_t attention_q4_workspace(const AttnQ4Plan &p, int batch, int h_kv, int d);
+hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out,
+                               hipStream_t st);
+struct AdapterPlan {
+    int rows;           // M rounded up to whole blocks of 16
+    int parts, part_k;  // K in `parts` parts of `part_k`
+};
+AdapterPlan plan_adapters(int M, int K, int num_cus);
+size_t adapters_workspace(const AdapterPlan &p, int rank);
+hipError_t launch_adapters(const void *x, int M, int K, int N, int rank, int count, const void *a, const void *b, const float *scale, const int *ids, const void *y,
+                           const AdapterPlan &p, void *workspace, void *out, hipStream_t st);
+
 }  // namespace qfc
