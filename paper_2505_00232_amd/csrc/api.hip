@@ -645,6 +645,7 @@ void qfc_tune(int32_t key, int32_t value) {
     if (key == 11) t.skinny_blocks = value;
     if (key == 13) t.attn_few = value;
     if (key == 14) t.attn_shares = value;
+    if (key == 15) t.attn_q4_chunks = value < 0 ? 0 : value;
     if (key == 12) t.attn_splits = value < 0 ? 0 : value > kAttnMaxSplits ? kAttnMaxSplits : value;
 }
 

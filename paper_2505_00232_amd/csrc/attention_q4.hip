@@ -47,13 +47,30 @@ __device__ __forceinline__ RowBlock row_block(const AttnQ4Args &a, int b, int ro
     return k;
 }
 
-// Workgroup = four wavefronts and up to 16 query rows of a KV head; the wavefronts take the pages of the workgroup's chunk in turn.
+// What a wavefront has on its way: DEPTH pages, keys and values each in a place of PART bytes of LDS of its own.
 template <int D>
-__global__ __launch_bounds__(256, 1) void attn_q4_kernel(AttnQ4Args a) {
+struct Ring {
+    static constexpr int kHalf = 40 * D;                      // bytes of a page's keys or values
+    static constexpr int PART = (kHalf + 1023) / 1024 * 1024;  // copied in pieces of a KiB
+    static constexpr int COPIES = PART / 1024;
+    static constexpr int DEPTH = D == 64 ? 3 : 2;
+    static constexpr int PITCH = D + 4;  // floats per row of the wavefronts' results
+    static constexpr int WAVE = 2 * DEPTH * PART;
+    static constexpr int MERGE = 4 * 16 * PITCH * 4;
+    static constexpr int LDS = 4 * WAVE > MERGE ? 4 * WAVE : MERGE;
+    static constexpr int FLYING = (2 * DEPTH - 1) * COPIES;  // copies behind the ones waited for
+    static_assert(LDS <= (D <= 128 ? 80 : 160) * 1024 && FLYING <= 63, "LDS, and the 6-bit counter of outstanding copies");
+};
+
+// Workgroup = four wavefronts and up to 16 query rows of a KV head; the wavefronts take the pages of the workgroup's chunk in turn, each with
+// copies of its own on the way (no barrier before the end).
+template <int D>
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Args a) {
     typedef PageLayout<D> L;
+    typedef Ring<D> R;
     constexpr int G = L::G, DT = D / 16, W = L::W;
-    constexpr int PITCH = D + 4;
-    extern __shared__ float lds[];  // [4][16][PITCH]
+    constexpr int PITCH = R::PITCH;
+    extern __shared__ float lds[];  // the rings; then [4][16][PITCH]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, r = lane >> 4;
     int w = blockIdx.x;
@@ -116,10 +133,41 @@ __global__ __launch_bounds__(256, 1) void attn_q4_kernel(AttnQ4Args a) {
     for (int e = 0; e < 8; ++e) eight[e] = __builtin_bit_cast(_Float16, (uint16_t)8);
     const uint32_t mask_lo = 0x000F000Fu, mask_hi = 0x00F000F0u;
 
-    for (int pg = chunk * a.chunk_pages + wave; pg < pages; pg += 4) {
-        const int k0 = pg * kPage;
-        const int page = __builtin_amdgcn_readfirstlane(page_of(a.req, b, k0));
-        const char *src = a.pages + ((size_t)max(page, 0) * a.h_kv + kv) * L::kBytes;
+    // ---- copies.  The wavefront's i-th page is first + 4 i; lane i holds the place of page i (of 64 at a time)
+    const int first = chunk * a.chunk_pages + wave;
+    const int count = first < pages ? (pages - first + 3) / 4 : 0;
+    char *const ring = reinterpret_cast<char *>(lds) + wave * R::WAVE;
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * R::WAVE);
+    auto places = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (first + 4 * (i + lane)) * kPage) : -1; };
+    int ahead = places(0), now = ahead;  // of the pages that are requested, and of those that are worked on
+    auto copy = [&](int i, int slot, int part) __attribute__((always_inline)) {  // part 0: keys, 1: values
+        const int page = __builtin_amdgcn_readlane(ahead, i & 63);
+        const char *src = a.pages + ((size_t)max(page, 0) * a.h_kv + kv) * L::kBytes + part * R::kHalf;
+#pragma unroll
+        for (int c = 0; c < R::COPIES; ++c)  // (the last piece's lanes behind the part copy its end again)
+            copy16_to_lds(src, (uint32_t)min(c * 1024 + lane * 16, R::kHalf - 16), ring_at + (2 * slot + part) * R::PART + c * 1024);
+    };
+#pragma unroll
+    for (int i = 0; i < R::DEPTH; ++i)
+        if (i < count) {
+            copy(i, i, 0);
+            copy(i, i, 1);
+        }
+    // The copies of page i are there: as many as ever are behind them while DEPTH pages follow, none later.  In front of a copy into a place all reads of it are done.
+    auto wait_for = [&](int i) __attribute__((always_inline)) {
+        if (i + R::DEPTH < count)
+            wait_copies<R::FLYING>();
+        else
+            wait_copies<0>();
+    };
+
+    for (int i = 0, slot = 0; i < count; ++i, slot = slot + 1 == R::DEPTH ? 0 : slot + 1) {
+        const int k0 = (first + 4 * i) * kPage;
+        if (i > 0 && (i & 63) == 0) now = places(i);
+        if (i + R::DEPTH < count && ((i + R::DEPTH) & 63) == 0) ahead = places(i + R::DEPTH);
+        const int page = __builtin_amdgcn_readlane(now, i & 63);
+        const char *src = ring + 2 * slot * R::PART;
+        wait_for(i);
         const int seen = page >= 0 ? lim - k0 : 0, valid = page >= 0 ? n - k0 : 0;  // of this page, by the lane's row and by anyone
 
         // ---- scores; lane (m, r), element 4 t + i: position 16 r + 4 t + i, in units of log 2
@@ -131,7 +179,7 @@ __global__ __launch_bounds__(256, 1) void attn_q4_kernel(AttnQ4Args a) {
                 h8 off = {};
                 if (r < 2) {
 #pragma unroll
-                    for (int j = 0; j < G; ++j) off[j] = *reinterpret_cast<const _Float16 *>(src + L::kOffsetK + ((16 * t + m) * G + j) * 2);
+                    for (int j = 0; j < G; ++j) off[j] = reinterpret_cast<const _Float16 *>(src + L::kOffsetK + (16 * t + m) * G * 2)[j];
                 }
                 const v4f zero = {};
                 part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, sums, zero, 0, 0, 0);
@@ -161,6 +209,8 @@ __global__ __launch_bounds__(256, 1) void attn_q4_kernel(AttnQ4Args a) {
                     bmax = fmaxf(bmax, sc[4 * t + i]);
                 }
         }
+        wait_copies<63>();  // (the keys have been read)
+        if (i + R::DEPTH < count) copy(i + R::DEPTH, slot, 0);
         bmax = fmaxf(bmax, __shfl_xor(bmax, 16, 64));
         bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64));
         const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max);
@@ -183,6 +233,8 @@ __global__ __launch_bounds__(256, 1) void attn_q4_kernel(AttnQ4Args a) {
         }
 
         // ---- second product.  Positions that nobody has may hold anything: their steps and offsets are taken as 0
+        wait_for(i);
+        src += R::PART - R::kHalf;  // (the layout counts from the page's start)
         h8 step[G][2];
         uint32_t large = 0;
 #pragma unroll
@@ -243,9 +295,12 @@ __global__ __launch_bounds__(256, 1) void attn_q4_kernel(AttnQ4Args a) {
                 eights[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight, p, eights[j], 0, 0, 0);
             }
         }
+        wait_copies<63>();
+        if (i + R::DEPTH < count) copy(i + R::DEPTH, slot, 1);
     }
 
     // ---- the four wavefronts meet in LDS: [wave][m][PITCH] = output row m (2^14 times, unnormalized), then (maximum, sum)
+    __syncthreads();  // (all are done with their rings)
     float *mine = lds + ((size_t)wave * 16 + m) * PITCH;
     const float back = 16777216.0f / lower;
 #pragma unroll
@@ -330,7 +385,7 @@ __global__ __launch_bounds__(64) void attn_q4_combine_kernel(AttnQ4Args a) {
 
 template <int D>
 hipError_t launch(const AttnQ4Args &a, hipStream_t st) {
-    const size_t lds = (size_t)4 * 16 * (D + 4) * sizeof(float);
+    constexpr size_t lds = Ring<D>::LDS;
     if (const hipError_t e = allow_dynamic_lds<attn_q4_kernel<D>>(lds); e != hipSuccess) return e;
     attn_q4_kernel<D><<<(unsigned)((long)a.chunks * a.req.batch * a.h_kv * a.blocks), 256, lds, st>>>(a);
     const hipError_t e = hipGetLastError();
@@ -348,7 +403,8 @@ AttnQ4Plan plan_attention_q4(int batch, int h_kv, int g, int max_tokens, int max
     p.blocks = (p.rows + 15) / 16;
     const long work = (long)batch * h_kv * p.blocks, want = 4L * num_cus;
     long chunks = work >= want ? 1 : want / work;
-    if (chunks > (pages + 3) / 4) chunks = (pages + 3) / 4;
+    if (const int forced = tuning().attn_q4_chunks; forced > 0) chunks = forced < pages ? forced : pages;
+    else if (chunks > (pages + 3) / 4) chunks = (pages + 3) / 4;
     if (chunks > kAttnMaxSplits) chunks = kAttnMaxSplits;
     if (chunks < 1) chunks = 1;
     p.chunk_pages = (int)((pages + chunks - 1) / chunks);

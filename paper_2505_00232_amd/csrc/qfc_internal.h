@@ -140,6 +140,7 @@ struct Tuning {
     Tunable skinny_blocks{0};   // blocks the token rows are cut into at least (0: automatic)
     Tunable attn_few{-1};       // attention, blocks of 16 query rows: -1 automatic, 0 above 16 rows never, 1 always
     Tunable attn_splits{0};     // decode attention: workgroups per KV head (0: automatic)
+    Tunable attn_q4_chunks{0};  // attention over the 4-bit cache: workgroups that share a request's pages (0: automatic)
     Tunable gemv_half{-1};      // half-unit items of the decode kernel: -1 automatic, 0 never, 1 where possible
 };
 Tuning &tuning();
