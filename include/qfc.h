@@ -381,7 +381,8 @@ qfc_status_t qfc_append_q4(const void *qkv_f16, const qfc_requests_t *requests, 
  * without a page.  Errors as qfc_append_q4. */
 qfc_status_t qfc_read_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, void *k, void *v, void *stream);
 
-/* Bytes of scratch qfc_attention_q4 needs for a batch of this size (batch, max_tokens and max_context are read; host pointers). */
+/* Bytes of scratch qfc_attention_q4 needs for a batch of this size (batch, tokens, max_tokens and max_context are read; host
+ * pointers).  Where a request may have many query rows (max_tokens * h_q / h_kv above 256) they include binary16 copies of such requests' keys and values. */
 qfc_status_t qfc_attention_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
 
 /* Attention of a batch of requests over the cache: out = softmax(q K^T / sqrt(d_head)) V for each row and head, q and out binary16

@@ -431,14 +431,14 @@ static qfc_status_t check_q4_cache(const qfc_q4_cache_t *c) {
 // Sizes only: what the workspace depends on
 static qfc_status_t check_batch(const qfc_requests_t *r, int32_t h_q, const qfc_q4_cache_t *c) {
     if (const qfc_status_t s = check_q4_cache(c); s != QFC_OK) return s;
-    if (!r || r->batch < 1 || r->max_tokens < 1 || r->max_context < 1 || h_q < 1 || h_q % c->h_kv != 0) return QFC_ERR_INVALID_ARG;
-    if ((long)h_q + 2L * c->h_kv > 65535 || (long)r->batch * c->h_kv > 65535 || (long)r->max_tokens * h_q > 1L << 26 || r->max_context > 1 << 26) return QFC_ERR_UNSUPPORTED;
+    if (!r || r->batch < 1 || r->tokens < 0 || r->max_tokens < 1 || r->max_context < 1 || h_q < 1 || h_q % c->h_kv != 0) return QFC_ERR_INVALID_ARG;
+    if ((long)h_q + 2L * c->h_kv > 65535 || (long)r->batch * c->h_kv > 65535 || (long)r->max_tokens * h_q > 1L << 26 || (long)r->tokens * h_q > 1L << 30 || r->max_context > 1 << 26) return QFC_ERR_UNSUPPORTED;
     return QFC_OK;
 }
 
 static qfc_status_t check_requests(const qfc_requests_t *r, int32_t h_q, const qfc_q4_cache_t *c) {
     if (const qfc_status_t s = check_batch(r, h_q, c); s != QFC_OK) return s;
-    if (!r->token_start || !r->context || !r->page_table || !c->pages || r->tokens < 0 || r->table_width < 1) return QFC_ERR_INVALID_ARG;
+    if (!r->token_start || !r->context || !r->page_table || !c->pages || r->table_width < 1) return QFC_ERR_INVALID_ARG;
     if ((long)r->table_width * QFC_PAGE_POSITIONS < r->max_context) return QFC_ERR_INVALID_ARG;
     if (!aligned(r->token_start, 4) || !aligned(r->context, 4) || !aligned(r->page_table, 4) || !aligned16(c->pages)) return QFC_ERR_ALIGNMENT;
     return QFC_OK;
@@ -497,11 +497,14 @@ qfc_status_t qfc_read_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *c
     return hip_status(launch_read_q4(on_device(requests, cache), cache->h_kv, cache->d_head, cache->pages, k, v, static_cast<hipStream_t>(stream)));
 }
 
+static AttnQ4Plan attention_plan(const qfc_requests_t *r, int32_t h_q, const qfc_q4_cache_t *c, int cus) {
+    return plan_attention_q4(r->batch, r->tokens, c->h_kv, h_q / c->h_kv, c->d_head, r->max_tokens, r->max_context, cus);
+}
+
 qfc_status_t qfc_attention_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes) {
     if (!bytes) return QFC_ERR_INVALID_ARG;
     if (const qfc_status_t s = check_batch(requests, h_q, cache); s != QFC_OK) return s;
-    *bytes = attention_q4_workspace(plan_attention_q4(requests->batch, cache->h_kv, h_q / cache->h_kv, requests->max_tokens, requests->max_context, device_cus()), requests->batch,
-                                    cache->h_kv, cache->d_head);
+    *bytes = attention_plan(requests, h_q, cache, device_cus()).total;
     return QFC_OK;
 }
 
@@ -510,11 +513,13 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
     if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
     if (!q_f16 || !workspace || !out_f16) return QFC_ERR_INVALID_ARG;
     if (!aligned16(q_f16) || !aligned16(workspace) || !aligned16(out_f16)) return QFC_ERR_ALIGNMENT;
-    const AttnQ4Plan p = plan_attention_q4(requests->batch, cache->h_kv, h_q / cache->h_kv, requests->max_tokens, requests->max_context, device_cus());
-    if (workspace_bytes < attention_q4_workspace(p, requests->batch, cache->h_kv, cache->d_head)) return QFC_ERR_BUFFER_TOO_SMALL;
-    if ((long)p.chunks * requests->batch * cache->h_kv * p.blocks > INT32_MAX) return QFC_ERR_UNSUPPORTED;
+    const int cus = device_cus();
+    const AttnQ4Plan p = attention_plan(requests, h_q, cache, cus);
+    if (workspace_bytes < p.total) return QFC_ERR_BUFFER_TOO_SMALL;
+    if (p.blocks * p.chunks * cache->h_kv > INT32_MAX || (long)p.slots * cache->h_kv * p.pages > INT32_MAX) return QFC_ERR_UNSUPPORTED;
     if (requests->tokens == 0) return QFC_OK;
-    return hip_status(launch_attention_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, p, workspace, out_f16,
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_attention_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, p, workspace, out_f16, cus,
                                           static_cast<hipStream_t>(stream)));
 }
 

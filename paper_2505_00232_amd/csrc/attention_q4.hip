@@ -8,6 +8,10 @@
 //   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
 // P is multiplied with the step in 32 bits and rounded to binary16 once per group; the -8 is taken off with the same rounded values (an MFMA against a
 // constant), so that what the rounding leaves is relative to a centred code, and the offsets are again one MFMA, whose last row, ones, gives the sum of P.
+//
+// Few query rows of a request (up to kFewRows per KV head: tokens, short chunks) go through that kernel in blocks of 16.  Many rows would take the same
+// codes apart again and again: for them the pages are first turned into binary16 copies in the workspace, once, and the kernel for prompts (attention.hip) walks
+// those.  Which request is which is known on the device only, where a first small kernel finds it.
 // P is taken 2^14 times as large: with steps below 2 every product is below 2^15, and binary16 keeps its 11 bits down to 2^-28.  A
 // step of 2 or more (values some 30 apart and more) lowers that factor to 2^2 from there on, for which every step is small enough.
 #include "paged_q4.h"
@@ -23,28 +27,60 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kMasked = -1.0e30f;
 constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: above every masked score, below every real one
 
+constexpr int kFewRows = 256;
+constexpr int kMaxSlots = 256;  // requests of many rows at most, the others go through the blocks of 16
+
 struct AttnQ4Args {
     const _Float16 *q;  // [tokens, h_q, D]
     _Float16 *out;
     const char *pages;
     Requests req;
-    float *ws_o, *ws_ml;  // [batch h_kv, chunks, rows, D] partial outputs, [.., 2] (maximum, sum)
-    int h_q, h_kv, g, chunks, chunk_pages, blocks, max_rows;
+    float *ws_o, *ws_ml;  // [chunks, h_kv, ws_rows, D] partial outputs, [.., 2] (maximum, sum)
+    int *plan;            // ManyRows, or null
+    int h_q, h_kv, g, chunks, chunk_pages, few_rows, by_request;
+    int one_block;  // every request has one block of 16 rows at most
+    long ws_rows;
     float scale;
 };
 
-// How many pages the rows row0 .. row0 + 15 of a request see between them, and how many rows there are
+// The rows row0 .. row0 + 15 of a request: how many rows there are, how many pages they see between them, and into how many chunks those are cut
 struct RowBlock {
     Span span;
-    int rows, pages, end;  // end: positions the last row sees
+    int rows, pages, end, chunk_pages;  // end: positions the last row sees
 };
+__device__ __forceinline__ bool has_many(const AttnQ4Args &a, int b) { return a.plan && a.plan[ManyRows::kSlots + b] >= 0; }
 __device__ __forceinline__ RowBlock row_block(const AttnQ4Args &a, int b, int row0) {
     RowBlock k;
     k.span = span_of(a.req, b);
     k.rows = k.span.count * a.g;
     k.end = max(0, k.span.positions - k.span.count + min(row0 + 15, k.rows - 1) / a.g + 1);
     k.pages = (k.end + kPage - 1) / kPage;
+    k.chunk_pages = k.rows > a.few_rows ? max(k.pages, 1) : a.chunk_pages;  // (no room for more partial results)
     return k;
+}
+__device__ __forceinline__ size_t partial_row(const AttnQ4Args &a, int b, const RowBlock &k, int row, int kv, int chunk) {
+    return ((size_t)chunk * a.h_kv + kv) * a.ws_rows + (a.by_request ? (size_t)b * a.few_rows : (size_t)k.span.first * a.g) + row;
+}
+// Request and first row of the i-th block of 16 rows of all requests (those of many rows left out); -1 behind the last
+__device__ __forceinline__ int block_of(const AttnQ4Args &a, int i, int lane, int &row0) {
+    for (int b0 = 0; b0 < a.req.batch; b0 += 64) {
+        const int b = b0 + lane;
+        int upto = b < a.req.batch && !has_many(a, b) ? (span_of(a.req, b).count * a.g + 15) / 16 : 0;
+        const int own = upto;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int below = __shfl_up(upto, off, 64);
+            upto += lane >= off ? below : 0;
+        }
+        const uint64_t at = __ballot(upto > i);
+        if (at) {
+            const int l = __ffsll((unsigned long long)at) - 1;
+            row0 = __builtin_amdgcn_readfirstlane(16 * (i - __shfl(upto - own, l, 64)));
+            return b0 + __builtin_amdgcn_readfirstlane(l);
+        }
+        i -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return -1;
 }
 
 // What a wavefront has on its way: DEPTH pages, keys and values each in a place of PART bytes of LDS of its own.
@@ -73,15 +109,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     extern __shared__ float lds[];  // the rings; then [4][16][PITCH]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, r = lane >> 4;
-    int w = blockIdx.x;
-    const int chunk = w % a.chunks;
-    w /= a.chunks;
-    const int group = w % (a.req.batch * a.h_kv), row0 = w / (a.req.batch * a.h_kv) * 16;
-    const int b = group / a.h_kv, kv = group % a.h_kv;
+    const int chunk = (int)blockIdx.x % a.chunks, work = (int)blockIdx.x / a.chunks;
+    const int kv = work % a.h_kv;
+    int row0 = 0, b = work / a.h_kv;
+    if (!a.one_block) b = block_of(a, b, lane, row0);
+    if (b < 0) return;
     const RowBlock blk = row_block(a, b, row0);
     if (row0 >= blk.rows) return;
-    if (chunk > 0 && chunk * a.chunk_pages >= blk.pages) return;
-    const int pages = __builtin_amdgcn_readfirstlane(min(blk.pages, (chunk + 1) * a.chunk_pages));
+    if (chunk > 0 && chunk * blk.chunk_pages >= blk.pages) return;
+    const int pages = __builtin_amdgcn_readfirstlane(chunk == 0 ? min(blk.pages, blk.chunk_pages) : min(blk.pages, (chunk + 1) * blk.chunk_pages));
     const int n = blk.span.positions;
 
     // ---- queries: lane (m, r) holds q[row0 + m][32 j + 8 r .. + 7], scaled by a power of two
@@ -134,7 +170,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     const uint32_t mask_lo = 0x000F000Fu, mask_hi = 0x00F000F0u;
 
     // ---- copies.  The wavefront's i-th page is first + 4 i; lane i holds the place of page i (of 64 at a time)
-    const int first = chunk * a.chunk_pages + wave;
+    const int first = chunk * blk.chunk_pages + wave;
     const int count = first < pages ? (pages - first + 3) / 4 : 0;
     char *const ring = reinterpret_cast<char *>(lds) + wave * R::WAVE;
     const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * R::WAVE);
@@ -320,7 +356,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
         mine[D + 1] = rest[3];
     }
     __syncthreads();
-    const int rows = min(16, blk.rows - row0), chunks = max(1, (blk.pages + a.chunk_pages - 1) / a.chunk_pages);
+    const int rows = min(16, blk.rows - row0), chunks = max(1, (blk.pages + blk.chunk_pages - 1) / blk.chunk_pages);
     for (int e = threadIdx.x; e < rows * (D / 4); e += 256) {
         const int mm = e / (D / 4), dd = 4 * (e % (D / 4));
         const float *row = lds + (size_t)mm * PITCH;
@@ -345,7 +381,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
             *reinterpret_cast<h4 *>(a.out + ((size_t)(blk.span.first + s) * a.h_q + kv * a.g + j) * D + dd) =
                 h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
         } else {
-            const size_t p = ((size_t)group * a.chunks + chunk) * a.max_rows + row0 + mm;
+            const size_t p = partial_row(a, b, blk, row0 + mm, kv, chunk);
             *reinterpret_cast<v4f *>(a.ws_o + p * D + dd) = o;
             if (dd == 0) {
                 a.ws_ml[p * 2] = mx;
@@ -355,20 +391,33 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     }
 }
 
-// One wavefront per query row and 64 columns: lane c takes the (maximum, sum) of chunk c (at most 64).
+// One wavefront per query row and 64 columns: lane c takes the (maximum, sum) of chunk c (at most 64).  grid = (rows, KV heads, D / 64): rows of a request's one
+// block, 16 for each, or of all requests' tokens.
 template <int D>
 __global__ __launch_bounds__(64) void attn_q4_combine_kernel(AttnQ4Args a) {
-    const int lane = threadIdx.x, row = blockIdx.x, group = blockIdx.y;
-    const int b = group / a.h_kv, kv = group % a.h_kv;
+    const int lane = threadIdx.x, kv = blockIdx.y;
+    int b, row = blockIdx.x;
+    if (a.one_block) {
+        b = row / 16;
+        row %= 16;
+    } else {
+        const int token = row / a.g;
+        int ended = 0;
+        for (int b0 = 0; b0 < a.req.batch; b0 += 64) ended += __popcll(__ballot(b0 + lane < a.req.batch && a.req.start[b0 + lane + 1] <= token));
+        b = __builtin_amdgcn_readfirstlane(ended);
+        if (b >= a.req.batch || has_many(a, b)) return;
+        row -= span_of(a.req, b).first * a.g;
+        if (row < 0) return;
+    }
     const RowBlock blk = row_block(a, b, row & ~15);
-    const int chunks = (blk.pages + a.chunk_pages - 1) / a.chunk_pages;
+    const int chunks = (blk.pages + blk.chunk_pages - 1) / blk.chunk_pages;
     if (row >= blk.rows || chunks <= 1) return;  // (one chunk: written by the first kernel)
-    const size_t slot = (size_t)group * a.chunks * a.max_rows + row;
+    const size_t slot = partial_row(a, b, blk, row, kv, 0), per_chunk = (size_t)a.h_kv * a.ws_rows;
     const int col = 64 * blockIdx.z + lane;
     float mx = kNothingYet, l = 0.0f;
     if (lane < chunks) {
-        mx = a.ws_ml[(slot + (size_t)lane * a.max_rows) * 2];
-        l = a.ws_ml[(slot + (size_t)lane * a.max_rows) * 2 + 1];
+        mx = a.ws_ml[(slot + lane * per_chunk) * 2];
+        l = a.ws_ml[(slot + lane * per_chunk) * 2 + 1];
     }
     float top = mx;
 #pragma unroll
@@ -378,65 +427,265 @@ __global__ __launch_bounds__(64) void attn_q4_combine_kernel(AttnQ4Args a) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
     float o = 0.0f;
-    for (int c = 0; c < chunks; ++c) o = fmaf(__shfl(f, c, 64), a.ws_o[(slot + (size_t)c * a.max_rows) * D + col], o);
+    for (int c = 0; c < chunks; ++c) o = fmaf(__shfl(f, c, 64), a.ws_o[(slot + c * per_chunk) * D + col], o);
     const int s = row / a.g, j = row % a.g;
     a.out[((size_t)(blk.span.first + s) * a.h_q + kv * a.g + j) * D + col] = (_Float16)(sum > 0.0f ? o / sum : 0.0f);
 }
 
+// ---------------------------------------------------------------- many query rows
+struct ManyArgs {
+    Requests req;
+    int *plan;
+    const char *pages;
+    _Float16 *kc, *vc;  // [slots, h_kv, positions, D], [slots, h_kv, positions / 64, D, 64]
+    int g, h_kv, slots, records, block_rows, unit, items, target, max_pages;
+};
+
+// One workgroup: the list of the requests with more than kFewRows rows.  A request with a missing page, or with fewer positions than tokens, is none of them: the kernel for few rows
+// takes it.  Walks (steps of 32 positions) are cut where that leaves `target` workgroups more even shares, into eight at most.
+__global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
+    __shared__ uint64_t wanted[4];
+    __shared__ int rec[kMaxSlots][4], item[kMaxSlots];
+    __shared__ int longest, total_items;
+    __shared__ unsigned long long total_steps;  // twice, about
+    const int tid = threadIdx.x;
+    if (tid == 0) longest = 0, total_steps = 0;
+    int count = 0;  // (the same in every thread)
+    for (int b0 = 0; b0 < a.req.batch; b0 += 256) {
+        const int b = b0 + tid;
+        bool many = false;
+        if (b < a.req.batch) {
+            const Span s = span_of(a.req, b);
+            many = s.count * a.g > kFewRows && s.positions >= s.count;
+            if (!many) a.plan[ManyRows::kSlots + b] = -1;
+        }
+        const uint64_t mask = __ballot(many);
+        if ((tid & 63) == 0) wanted[tid >> 6] = mask;
+        __syncthreads();
+        for (int w = 0; w < 4; ++w) {
+            for (uint64_t m = wanted[w]; m; m &= m - 1) {
+                const int bb = b0 + 64 * w + __ffsll((unsigned long long)m) - 1;
+                const Span s = span_of(a.req, bb);
+                bool missing = false;
+                for (int p = tid; p * kPage < s.positions; p += 256) missing = missing || page_of(a.req, bb, p * kPage) < 0;
+                const bool taken = !__syncthreads_or(missing) && count < a.slots;
+                if (tid == 0) {
+                    if (taken) rec[count][0] = s.first, rec[count][1] = s.count, rec[count][2] = s.positions, rec[count][3] = bb;
+                    a.plan[ManyRows::kSlots + bb] = taken ? count : -1;
+                }
+                count += taken;
+            }
+        }
+        __syncthreads();
+    }
+    // steps of the last row of block j of a request's rows
+    auto steps = [&](int slot, int j) {
+        const int S = rec[slot][1], last = min((j + 1) * a.block_rows, S * a.g) - 1;
+        return (rec[slot][2] - S + last / a.g + 1 + 31) / 32;
+    };
+    const int blocks = tid < count ? (rec[tid][1] * a.g + a.block_rows - 1) / a.block_rows : 0;
+    if (tid < count) {
+        atomicMax(&longest, steps(tid, blocks - 1));
+        atomicAdd(&total_steps, (unsigned long long)blocks * (unsigned)(steps(tid, 0) + steps(tid, blocks - 1)));
+    }
+    __syncthreads();
+    int len = 0;
+    if (a.target > 0) {
+        len = (int)(total_steps * a.h_kv / (2ull * a.target)) + 1;
+        len = max(max(len, (longest + kPrefillMaxChunks - 1) / kPrefillMaxChunks), 16);
+        len = (len + a.unit - 1) / a.unit * a.unit;
+        if (len >= longest) len = 0;
+    }
+    for (int attempt = 0; attempt < 2; ++attempt) {
+        if (tid < count) {
+            int n = blocks;
+            if (len > 0) {
+                n = 0;
+                for (int j = 0; j < blocks; ++j) n += (steps(tid, j) + len - 1) / len;
+            }
+            item[tid] = n;
+        }
+        __syncthreads();
+        if (tid == 0) {
+            int sum = 0;
+            for (int i = 0; i < count; ++i) {
+                const int n = item[i];
+                item[i] = sum;
+                sum += n;
+            }
+            total_items = sum;
+        }
+        __syncthreads();
+        if (total_items <= a.items || len == 0) break;
+        len = 0;
+        __syncthreads();
+    }
+    if (tid < count) {
+        int *r = a.plan + a.records + tid * ManyRows::kRecord;
+        r[ManyRows::kRow] = rec[tid][0];
+        r[ManyRows::kTokens] = rec[tid][1];
+        r[ManyRows::kPositions] = rec[tid][2];
+        r[ManyRows::kItem] = item[tid];
+        r[ManyRows::kChunkSteps] = len;
+        r[ManyRows::kRequest] = rec[tid][3];
+    }
+    if (tid == 0) {
+        a.plan[ManyRows::kCount] = count;
+        a.plan[ManyRows::kItems] = total_items;
+    }
+}
+
+// grid = (pages of the longest request x KV heads, slots): a page's block of one head as binary16, fp16(offset + step (code - 8)).  Bound: memory.
 template <int D>
-hipError_t launch(const AttnQ4Args &a, hipStream_t st) {
+__global__ __launch_bounds__(256) void attn_q4_copy_kernel(ManyArgs a) {
+    typedef PageLayout<D> L;
+    constexpr int G = L::G;
+    const int slot = blockIdx.y, kv = (int)blockIdx.x % a.h_kv, pg = (int)blockIdx.x / a.h_kv;
+    if (slot >= a.plan[ManyRows::kCount]) return;
+    const int *r = a.plan + a.records + slot * ManyRows::kRecord;
+    if (pg * kPage >= r[ManyRows::kPositions]) return;
+    const int page = page_of(a.req, r[ManyRows::kRequest], pg * kPage);
+    if (page < 0) return;  // (none of the list's requests)
+    const char *src = a.pages + ((size_t)page * a.h_kv + kv) * L::kBytes;
+    const size_t dst = ((size_t)(slot * a.h_kv + kv) * a.max_pages + pg) * (kPage * D);
+    const int tid = threadIdx.x;
+    // keys: a thread per octet
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        const int o = (tid + 256 * i) % (D / 8), p = (tid + 256 * i) / (D / 8), j = o / 4;
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(src + L::code_k(p, j, o & 3));
+        const float step = (float)*reinterpret_cast<const _Float16 *>(src + L::step_k(p, j)), off = (float)*reinterpret_cast<const _Float16 *>(src + L::offset_k(p, j));
+        h8 x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (_Float16)fmaf((float)((w >> nibble(e)) & 15u) - 8.0f, step, off);
+        *reinterpret_cast<h8 *>(a.kc + dst + p * D + 8 * o) = x;
+    }
+    // values: a thread per 8 positions of the two values of a byte
+#pragma unroll
+    for (int i = 0; i < G * 128 / 256; ++i) {
+        const int t = tid + 256 * i, p0 = 8 * (t % 8), m = t / 8 % 16, j = t / 128;
+        const uint2 w = *reinterpret_cast<const uint2 *>(src + L::kCodesV + (j * 64 + (p0 >> 4) * 16 + m) * 16 + (p0 & 8));
+        const h8 step = *reinterpret_cast<const h8 *>(src + L::step_v(p0, j)), off = *reinterpret_cast<const h8 *>(src + L::offset_v(p0, j));
+        h8 lo, hi;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t byte = (e < 4 ? w.x : w.y) >> (8 * (((e & 1) << 1) | ((e >> 1) & 1)));
+            lo[e] = (_Float16)fmaf((float)(byte & 15u) - 8.0f, (float)step[e], (float)off[e]);
+            hi[e] = (_Float16)fmaf((float)((byte >> 4) & 15u) - 8.0f, (float)step[e], (float)off[e]);
+        }
+        *reinterpret_cast<h8 *>(a.vc + dst + (32 * j + m) * 64 + p0) = lo;
+        *reinterpret_cast<h8 *>(a.vc + dst + (32 * j + 16 + m) * 64 + p0) = hi;
+    }
+}
+
+template <int D>
+hipError_t launch(const AttnQ4Args &a, const ManyArgs &many, const AttnQ4Plan &p, hipStream_t st) {
+    if (p.slots > 0) {
+        attn_q4_list_kernel<<<1, 256, 0, st>>>(many);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
     constexpr size_t lds = Ring<D>::LDS;
     if (const hipError_t e = allow_dynamic_lds<attn_q4_kernel<D>>(lds); e != hipSuccess) return e;
-    attn_q4_kernel<D><<<(unsigned)((long)a.chunks * a.req.batch * a.h_kv * a.blocks), 256, lds, st>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.chunks == 1) return e;
-    attn_q4_combine_kernel<D><<<dim3((unsigned)a.max_rows, (unsigned)(a.req.batch * a.h_kv), D / 64), 64, 0, st>>>(a);
-    return hipGetLastError();
+    attn_q4_kernel<D><<<(unsigned)(p.blocks * p.chunks * a.h_kv), 256, lds, st>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (p.chunks > 1) {
+        const long rows = a.one_block ? 16L * a.req.batch : p.all_rows;
+        attn_q4_combine_kernel<D><<<dim3((unsigned)rows, (unsigned)a.h_kv, D / 64), 64, 0, st>>>(a);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    if (p.slots > 0) {
+        attn_q4_copy_kernel<D><<<dim3((unsigned)(p.pages * a.h_kv), (unsigned)p.slots), 256, 0, st>>>(many);
+        return hipGetLastError();
+    }
+    return hipSuccess;
 }
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
-AttnQ4Plan plan_attention_q4(int batch, int h_kv, int g, int max_tokens, int max_context, int num_cus) {
-    AttnQ4Plan p;
-    const int pages = (max_context + kPage - 1) / kPage;
+AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int max_tokens, int max_context, int num_cus) {
+    AttnQ4Plan p = {};
+    p.pages = (max_context + kPage - 1) / kPage;
     p.rows = max_tokens * g;
-    p.blocks = (p.rows + 15) / 16;
-    const long work = (long)batch * h_kv * p.blocks, want = 4L * num_cus;
-    long chunks = work >= want ? 1 : want / work;
-    if (const int forced = tuning().attn_q4_chunks; forced > 0) chunks = forced < pages ? forced : pages;
-    else if (chunks > (pages + 3) / 4) chunks = (pages + 3) / 4;
+    p.all_rows = (long)tokens * g;
+    p.blocks = p.rows <= 16 ? batch : (p.all_rows + 15) / 16 + batch;
+    // few rows: a workgroup for a chunk of a request's pages, four per compute unit where there are pages enough for its four wavefronts
+    long chunks = 4L * num_cus / ((long)batch * h_kv);
+    if (const int forced = tuning().attn_q4_chunks; forced > 0)
+        chunks = forced < p.pages ? forced : p.pages;
+    else if (chunks > (p.pages + 3) / 4)
+        chunks = (p.pages + 3) / 4;
     if (chunks > kAttnMaxSplits) chunks = kAttnMaxSplits;
     if (chunks < 1) chunks = 1;
-    p.chunk_pages = (int)((pages + chunks - 1) / chunks);
-    if (p.chunk_pages < 1) p.chunk_pages = 1;
-    p.chunks = (pages + p.chunk_pages - 1) / p.chunk_pages;
-    if (p.chunks < 1) p.chunks = 1;
+    p.chunk_pages = (int)((p.pages + chunks - 1) / chunks);
+    p.chunks = (p.pages + p.chunk_pages - 1) / p.chunk_pages;
+    p.few_rows = p.rows < kFewRows ? p.rows : kFewRows;
+    const long by_request = (long)batch * p.few_rows, ws_rows = by_request < p.all_rows ? by_request : p.all_rows;
+    p.total = 256;
+    p.partial = 0;
+    if (p.chunks > 1) p.total += up256((size_t)p.chunks * h_kv * ws_rows * (d + 2) * sizeof(float));
+    // many rows
+    if (p.rows <= kFewRows) return p;
+    const long most = p.all_rows / (kFewRows + 1);
+    p.slots = (int)(most < batch ? most : batch);
+    if (p.slots > kMaxSlots) p.slots = kMaxSlots;
+    if (p.slots == 0) return p;
+    const long on_card = (long)num_cus * (d <= 128 ? 2 : 1);  // workgroups the card holds at once
+    p.shares = p.all_rows * h_kv / 128 >= 2 * on_card ? 1 : 2;
+    const int block_rows = 128 / p.shares;
+    const long blocks = p.all_rows / block_rows + p.slots;
+    p.cut = p.all_rows * h_kv / block_rows < 2 * on_card;
+    p.items = (int)(p.cut ? 2 * blocks + on_card / h_kv + 1 : blocks);
+    p.records = (ManyRows::kSlots + batch + 7) / 8 * 8;
+    p.plan = p.total;
+    p.total += up256((size_t)(p.records + p.slots * ManyRows::kRecord) * sizeof(int));
+    p.copies = p.total;
+    p.total += up256((size_t)p.slots * h_kv * p.pages * kPage * d * 2 * 2);
+    p.many_partial = p.total;
+    if (p.cut) p.total += up256((size_t)kPrefillMaxChunks * h_kv * p.all_rows * (d + 2) * sizeof(float));
     return p;
 }
 
-size_t attention_q4_workspace(const AttnQ4Plan &p, int batch, int h_kv, int d) {
-    if (p.chunks == 1) return 256;
-    return (size_t)batch * h_kv * p.chunks * p.rows * (d + 2) * sizeof(float);
-}
-
-hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out,
+hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out, int num_cus,
                                hipStream_t st) {
-    AttnQ4Args a;
+    char *ws = static_cast<char *>(workspace);
+    AttnQ4Args a = {};
     a.q = static_cast<const _Float16 *>(q);
     a.out = static_cast<_Float16 *>(out);
     a.pages = static_cast<const char *>(pages);
     a.req = req;
     a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv;
-    a.chunks = p.chunks, a.chunk_pages = p.chunk_pages, a.blocks = p.blocks, a.max_rows = p.rows;
-    a.ws_o = static_cast<float *>(workspace);
-    a.ws_ml = a.ws_o + (size_t)req.batch * h_kv * p.chunks * p.rows * d;
+    a.chunks = p.chunks, a.chunk_pages = p.chunk_pages, a.few_rows = p.few_rows;
+    a.one_block = p.rows <= 16;
+    a.by_request = (long)req.batch * p.few_rows < p.all_rows;
+    a.ws_rows = a.by_request ? (long)req.batch * p.few_rows : p.all_rows;
+    a.ws_o = reinterpret_cast<float *>(ws + p.partial);
+    a.ws_ml = a.ws_o + (size_t)p.chunks * h_kv * a.ws_rows * d;
     a.scale = 1.4426950408889634f / sqrtf((float)d);
-    switch (d) {
-        case 64: return launch<64>(a, st);
-        case 128: return launch<128>(a, st);
-        case 256: return launch<256>(a, st);
-        default: return hipErrorInvalidValue;
+    ManyArgs many = {};
+    _Float16 *kc = nullptr, *vc = nullptr;
+    if (p.slots > 0) {
+        a.plan = reinterpret_cast<int *>(ws + p.plan);
+        kc = reinterpret_cast<_Float16 *>(ws + p.copies);
+        vc = kc + (size_t)p.slots * h_kv * p.pages * kPage * d;
+        many.req = req;
+        many.plan = a.plan;
+        many.pages = a.pages;
+        many.kc = kc, many.vc = vc;
+        many.g = a.g, many.h_kv = h_kv, many.slots = p.slots, many.records = p.records, many.block_rows = 128 / p.shares, many.unit = p.shares, many.items = p.items;
+        many.target = p.cut ? num_cus * (d <= 128 ? 2 : 1) : 0;
+        many.max_pages = p.pages;
     }
+    hipError_t e = hipErrorInvalidValue;
+    switch (d) {
+        case 64: e = launch<64>(a, many, p, st); break;
+        case 128: e = launch<128>(a, many, p, st); break;
+        case 256: e = launch<256>(a, many, p, st); break;
+    }
+    if (e != hipSuccess || p.slots == 0) return e;
+    return launch_attention_many(q, kc, vc, h_q, h_kv, d, p.pages * kPage, a.plan, p.records, p.shares, p.items, p.all_rows,
+                                 p.cut ? reinterpret_cast<float *>(ws + p.many_partial) : nullptr, out, st);
 }
 
 }  // namespace qfc

@@ -390,16 +390,34 @@ hipError_t launch_rotary_table(int rot, double base, double factor, int original
 hipError_t launch_append_q4(const void *qkv, const Requests &req, int h_q, int h_kv, int d, int rot, bool interleaved, const float *table, void *pages, void *q_out,
                             int num_cus, hipStream_t st);
 hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, hipStream_t st);
+// Attention of requests with many query rows: which they are, and how their walks are cut, is found on the device (attention_q4.hip) and left as a list of int32.
+struct ManyRows {
+    static constexpr int kCount = 0, kItems = 1, kSlots = 4;  // requests, workgroups per KV head; from kSlots on each request's place in the list or -1
+    static constexpr int kRecord = 8;                         // ints per request in the list:
+    static constexpr int kRow = 0, kTokens = 1, kPositions = 2, kItem = 3, kChunkSteps = 4, kRequest = 5;
+};
 struct AttnQ4Plan {
-    int rows;         // query rows of a KV head at most
-    int blocks;       // blocks of 16 of them
+    int rows;         // query rows of a KV head and request at most
+    long blocks;      // blocks of 16 rows of all requests at most
     int chunk_pages;  // pages a workgroup takes
     int chunks;       // workgroups that share the longest request's pages
+    int few_rows;     // rows per request with partial results
+    // requests of many rows (slots 0: there are none)
+    int slots;        // at most so many
+    int shares;       // wavefronts that share a walk
+    int items;        // workgroups per KV head at most
+    bool cut;         // walks may be cut into chunks
+    long all_rows;    // query rows of a KV head of all requests
+    // bytes from the workspace's start
+    size_t partial, plan, copies, many_partial, total;
+    int records;      // ints from the plan's start to its list
+    int pages;        // of the longest request
 };
-AttnQ4Plan plan_attention_q4(int batch, int h_kv, int g, int max_tokens, int max_context, int num_cus);
-size_t attention_q4_workspace(const AttnQ4Plan &p, int batch, int h_kv, int d);
-hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out,
+AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int max_tokens, int max_context, int num_cus);
+hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out, int num_cus,
                                hipStream_t st);
+hipError_t launch_attention_many(const void *q, const void *kc, const void *vc, int h_q, int h_kv, int d, int C, const int *plan, int records, int shares, int items,
+                                 long rows, float *partial, void *out, hipStream_t st);
 struct AdapterPlan {
     int rows;           // M rounded up to whole blocks of 16
     int parts, part_k;  // K in `parts` parts of `part_k`

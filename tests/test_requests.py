@@ -281,6 +281,11 @@ ATTENDS = [  # S, n, h_q, h_kv, d
     ([130, 1, 0, 33], [130, 257, 9, 1000], 4, 2, 128),
     ([100, 65], [163, 65], 2, 1, 256),
     ([257], [300], 8, 2, 64),
+    ([200, 1, 3], [3000, 2000, 70], 8, 2, 64),  # a prompt's walks in pieces, beside single tokens
+    ([1, 90, 300, 2], [700, 90, 811, 2], 4, 1, 128),
+    ([150, 260], [150, 700], 4, 2, 256),
+    ([600, 17], [601, 900], 1, 1, 128),
+    ([100] * 5, [100, 163, 164, 500, 228], 6, 2, 64),
 ]
 
 
@@ -312,7 +317,7 @@ def test_attention_far_from_zero():
 
 
 @gpu
-@pytest.mark.parametrize("S", [1, 40])
+@pytest.mark.parametrize("S", [1, 40, 150])
 def test_attention_rows_that_see_nothing_and_missing_pages(S):
     rng = np.random.default_rng(24)
     h_q, h_kv, d, n = 4, 2, 128, [300, 0, 200, 130, 64]
@@ -550,3 +555,33 @@ def test_layer_of_a_batch_of_requests(S, n):
     assert out.shape == (T, hidden) and np.all(np.isfinite(out))
     for l in layers:
         l.close()
+
+
+@gpu
+def test_prompts_in_a_replayed_graph():
+    """Which requests have many rows, and how long their walks are, may change from replay to replay."""
+    rng = np.random.default_rng(29)
+    h_q, h_kv, d, T, longest = 8, 2, 64, 400, 1024
+    table, num = _pages(rng, [longest] * 3)
+    cache, _, _, _ = _filled(rng, [longest] * 3, h_kv, d, table, num)
+    start, context = torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    req = B.Requests(start, context, _t(table), T, T, longest)
+    q = _t(_normal(rng, T, h_q * d))
+    ws, ws2 = (torch.empty(B.qfc_attention_q4_workspace_size(req, h_q, cache), dtype=torch.uint8, device=DEV) for _ in range(2))
+    out, out2 = torch.zeros_like(q), torch.zeros_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    B.qfc_attention_q4(q, req, h_q, cache, ws2, out2)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        B.qfc_attention_q4(q, req, h_q, cache, ws, out)
+    for cuts, n in (([0, 300, 301, 400], [1000, 5, 1024]), ([0, 1, 2, 3], [64, 65, 1]), ([0, 65, 400, 400], [65, 1023, 0]), ([0, 0, 200, 399], [9, 200, 1024])):
+        start.copy_(torch.tensor(cuts, dtype=torch.int32))
+        context.copy_(torch.tensor(n, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        out2.zero_()
+        B.qfc_attention_q4(q, req, h_q, cache, ws2, out2)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:cuts[-1]], out2[:cuts[-1]]) and bool(torch.isfinite(out2).all())
