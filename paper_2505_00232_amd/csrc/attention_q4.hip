@@ -24,8 +24,7 @@ typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kMasked = -1.0e30f;
-constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: above every masked score, below every real one
+constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: below every score
 
 constexpr int kFewRows = 256;
 constexpr int kMaxSlots = 256;  // requests of many rows at most, the others go through the blocks of 16
@@ -39,6 +38,7 @@ struct AttnQ4Args {
     int *plan;            // ManyRows, or null
     int h_q, h_kv, g, chunks, chunk_pages, few_rows, by_request;
     int one_block;  // every request has one block of 16 rows at most
+    int blocks;     // of 16 rows (with a plan: it says how many)
     long ws_rows;
     float scale;
 };
@@ -61,8 +61,11 @@ __device__ __forceinline__ RowBlock row_block(const AttnQ4Args &a, int b, int ro
 __device__ __forceinline__ size_t partial_row(const AttnQ4Args &a, int b, const RowBlock &k, int row, int kv, int chunk) {
     return ((size_t)chunk * a.h_kv + kv) * a.ws_rows + (a.by_request ? (size_t)b * a.few_rows : (size_t)k.span.first * a.g) + row;
 }
+__device__ __forceinline__ int block_count(const AttnQ4Args &a) { return a.plan ? a.plan[ManyRows::kFewBlocks] : a.blocks; }
 // Request and first row of the i-th block of 16 rows of all requests (those of many rows left out); -1 behind the last
 __device__ __forceinline__ int block_of(const AttnQ4Args &a, int i, int lane, int &row0) {
+    row0 = 0;
+    if (a.one_block) return i;
     for (int b0 = 0; b0 < a.req.batch; b0 += 64) {
         const int b = b0 + lane;
         int upto = b < a.req.batch && !has_many(a, b) ? (span_of(a.req, b).count * a.g + 15) / 16 : 0;
@@ -99,7 +102,7 @@ struct Ring {
 };
 
 // Workgroup = four wavefronts and up to 16 query rows of a KV head; the wavefronts take the pages of the workgroup's chunk in turn, each with
-// copies of its own on the way (no barrier before the end).
+// copies of its own on the way (no barrier before the end).  Where the number of blocks is only known on the device, workgroups take one after the other.
 template <int D>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Args a) {
     typedef PageLayout<D> L;
@@ -109,14 +112,15 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     extern __shared__ float lds[];  // the rings; then [4][16][PITCH]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, r = lane >> 4;
-    const int chunk = (int)blockIdx.x % a.chunks, work = (int)blockIdx.x / a.chunks;
-    const int kv = work % a.h_kv;
-    int row0 = 0, b = work / a.h_kv;
-    if (!a.one_block) b = block_of(a, b, lane, row0);
-    if (b < 0) return;
+    const int total = block_count(a) * a.h_kv * a.chunks;
+    for (int work = blockIdx.x; work < total; work += gridDim.x) {
+    const int chunk = work % a.chunks, kv = work / a.chunks % a.h_kv;
+    int row0;
+    const int b = block_of(a, work / a.chunks / a.h_kv, lane, row0);
+    if (b < 0) continue;
     const RowBlock blk = row_block(a, b, row0);
-    if (row0 >= blk.rows) return;
-    if (chunk > 0 && chunk * blk.chunk_pages >= blk.pages) return;
+    if (row0 >= blk.rows || (chunk > 0 && chunk * blk.chunk_pages >= blk.pages)) continue;
+    __syncthreads();  // (all are done with the work before)
     const int pages = __builtin_amdgcn_readfirstlane(chunk == 0 ? min(blk.pages, blk.chunk_pages) : min(blk.pages, (chunk + 1) * blk.chunk_pages));
     const int n = blk.span.positions;
 
@@ -206,55 +210,67 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
         wait_for(i);
         const int seen = page >= 0 ? lim - k0 : 0, valid = page >= 0 ? n - k0 : 0;  // of this page, by the lane's row and by anyone
 
-        // ---- scores; lane (m, r), element 4 t + i: position 16 r + 4 t + i, in units of log 2
-        float sc[16], bmax = kMasked;
+        // ---- scores; lane (m, r), element 4 t + i: position 16 r + 4 t + i, times 2^-24 and the queries' power of two
+        float sc[16];
         {
+            h8 off[4] = {};
+            if (r < 2) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int j = 0; j < G; ++j) off[t][j] = reinterpret_cast<const _Float16 *>(src + L::kOffsetK + (16 * t + m) * G * 2)[j];
+            }
             v4f part[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                h8 off = {};
-                if (r < 2) {
-#pragma unroll
-                    for (int j = 0; j < G; ++j) off[j] = reinterpret_cast<const _Float16 *>(src + L::kOffsetK + (16 * t + m) * G * 2)[j];
-                }
                 const v4f zero = {};
-                part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, sums, zero, 0, 0, 0);
+                part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off[t], sums, zero, 0, 0, 0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) part[t][i] *= 1.0f / 1048576.0f;
             }
 #pragma unroll
-            for (int j = 0; j < G; ++j) {
-                h8 st[2];
-                st[0] = *reinterpret_cast<const h8 *>(src + L::kStepK + (j * kPage + 16 * r) * 2);
-                st[1] = *reinterpret_cast<const h8 *>(src + L::kStepK + (j * kPage + 16 * r + 8) * 2);
+            for (int jj = 0; jj < G / W; ++jj) {
+                typedef uint32_t words __attribute__((ext_vector_type(W)));
+                words c[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const uint32_t c = *reinterpret_cast<const uint32_t *>(src + L::kCodesK + ((t * (G / W) + j / W) * 64 + lane) * (4 * W) + (j % W) * 4);
-                    const u32x4 op = {c & mask_lo, c & mask_hi, (c >> 8) & mask_lo, (c >> 8) & mask_hi};
-                    const v4f from = {start[j], start[j], start[j], start[j]};
-                    const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, op), qf[j], from, 0, 0, 0);
+                for (int t = 0; t < 4; ++t) c[t] = *reinterpret_cast<const words *>(src + L::kCodesK + ((t * (G / W) + jj) * 64 + lane) * (4 * W));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) part[t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[t][i]);
+                for (int jw = 0; jw < W; ++jw) {
+                    const int j = jj * W + jw;
+                    h8 st[2];
+                    st[0] = *reinterpret_cast<const h8 *>(src + L::kStepK + (j * kPage + 16 * r) * 2);
+                    st[1] = *reinterpret_cast<const h8 *>(src + L::kStepK + (j * kPage + 16 * r + 8) * 2);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const uint32_t w = c[t][jw];
+                        const u32x4 op = {w & mask_lo, w & mask_hi, (w >> 8) & mask_lo, (w >> 8) & mask_hi};
+                        const v4f from = {start[j], start[j], start[j], start[j]};
+                        const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, op), qf[j], from, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) part[t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[t][i]);
+                    }
                 }
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sc[4 * t + i] = 16 * r + 4 * t + i < seen ? part[t][i] * to_score : kMasked;
-                    bmax = fmaxf(bmax, sc[4 * t + i]);
-                }
+            for (int e = 0; e < 16; ++e) sc[e] = part[e >> 2][e & 3];
         }
+        if (__any(seen < kPage)) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[e] = 16 * r + e < seen ? sc[e] : -INFINITY;
+        }
+        float bmax = fmaxf(sc[0], sc[1]);
+#pragma unroll
+        for (int e = 2; e < 16; e += 2) bmax = fmaxf(fmaxf(bmax, sc[e]), sc[e + 1]);
         wait_copies<63>();  // (the keys have been read)
         if (i + R::DEPTH < count) copy(i + R::DEPTH, slot, 0);
         bmax = fmaxf(bmax, __shfl_xor(bmax, 16, 64));
-        bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64));
-        const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max);
+        bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64)) * to_score;  // (in units of log 2 from here on)
+        const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max), from14 = 14.0f - new_max;
         run_max = new_max;
         h8 pv[2];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            sc[e] = __builtin_amdgcn_exp2f(sc[e] - new_max + 14.0f);
+            sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], to_score, from14));
             pv[e >> 3][e & 7] = (_Float16)sc[e];
         }
         if (__any(corr != 1.0f)) {
@@ -271,19 +287,30 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
         // ---- second product.  Positions that nobody has may hold anything: their steps and offsets are taken as 0
         wait_for(i);
         src += R::PART - R::kHalf;  // (the layout counts from the page's start)
-        h8 step[G][2];
+        h8 step[G][2], off[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            off[u] = *reinterpret_cast<const h8 *>(src + L::kOffsetV + (min(m, G - 1) * kPage + 16 * r + 8 * u) * 2);
+#pragma unroll
+            for (int j = 0; j < G; ++j) step[j][u] = *reinterpret_cast<const h8 *>(src + L::kStepV + (j * kPage + 16 * r + 8 * u) * 2);
+        }
+        if (valid < kPage) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool none = 16 * r + 8 * u + e >= valid;
+                    off[u][e] = none ? (_Float16)0.0f : off[u][e];
+#pragma unroll
+                    for (int j = 0; j < G; ++j) step[j][u][e] = none ? (_Float16)0.0f : step[j][u][e];
+                }
+        }
         uint32_t large = 0;
 #pragma unroll
         for (int j = 0; j < G; ++j)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                h8 s = *reinterpret_cast<const h8 *>(src + L::kStepV + (j * kPage + 16 * r + 8 * u) * 2);
-                if (valid < kPage) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s[e] = 16 * r + 8 * u + e < valid ? s[e] : (_Float16)0.0f;
-                }
-                step[j][u] = s;
-                const u32x4 bits = __builtin_bit_cast(u32x4, s);
+                const u32x4 bits = __builtin_bit_cast(u32x4, step[j][u]);
                 large |= bits.x | bits.y | bits.z | bits.w;
             }
         if (lower == 1.0f && __any((large & 0x40004000u) != 0)) {  // a step of 2 or more
@@ -301,19 +328,10 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
             for (int e = 0; e < 16; ++e) sc[e] *= lower;
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            h8 off = {};
-            if (m < G) {
-                off = *reinterpret_cast<const h8 *>(src + L::kOffsetV + (m * kPage + 16 * r + 8 * u) * 2);
-                if (valid < kPage) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) off[e] = 16 * r + 8 * u + e < valid ? off[e] : (_Float16)0.0f;
-                }
-            } else if (m == 15) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) off[e] = (_Float16)1.0f;
-            }
-            rest = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, pv[u], rest, 0, 0, 0);
+        for (int u = 0; u < 2; ++u) {  // rows 0 .. G - 1: offsets; row 15: ones; the others are not used
+            const u32x4 w = __builtin_bit_cast(u32x4, off[u]);
+            const u32x4 rows = {m == 15 ? 0x3C003C00u : w.x, m == 15 ? 0x3C003C00u : w.y, m == 15 ? 0x3C003C00u : w.z, m == 15 ? 0x3C003C00u : w.w};
+            rest = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, rows), pv[u], rest, 0, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < G; ++j) {
@@ -322,7 +340,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
             for (int u = 0; u < 2; ++u) {
                 h8 p;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = (_Float16)(sc[8 * u + e] * (float)step[j][u][e]);
+                for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[8 * u + e], (float)step[j][u][e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits to 16)
                 const uint32_t c0 = c[2 * u], c1 = c[2 * u + 1];
                 const u32x4 lo = {c0 & mask_lo, (c0 >> 8) & mask_lo, c1 & mask_lo, (c1 >> 8) & mask_lo};
                 const u32x4 hi = {c0 & mask_hi, (c0 >> 8) & mask_hi, c1 & mask_hi, (c1 >> 8) & mask_hi};
@@ -389,47 +407,63 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
             }
         }
     }
+    }
 }
 
-// One wavefront per query row and 64 columns: lane c takes the (maximum, sum) of chunk c (at most 64).  grid = (rows, KV heads, D / 64): rows of a request's one
-// block, 16 for each, or of all requests' tokens.
+// One wavefront per query row, four rows of a block per workgroup: grid = (blocks x KV heads, 4).  Lane c takes the (maximum, sum) of chunk c (at most 64), and
+// D / 64 columns of the partial outputs.
 template <int D>
-__global__ __launch_bounds__(64) void attn_q4_combine_kernel(AttnQ4Args a) {
-    const int lane = threadIdx.x, kv = blockIdx.y;
-    int b, row = blockIdx.x;
-    if (a.one_block) {
-        b = row / 16;
-        row %= 16;
-    } else {
-        const int token = row / a.g;
-        int ended = 0;
-        for (int b0 = 0; b0 < a.req.batch; b0 += 64) ended += __popcll(__ballot(b0 + lane < a.req.batch && a.req.start[b0 + lane + 1] <= token));
-        b = __builtin_amdgcn_readfirstlane(ended);
-        if (b >= a.req.batch || has_many(a, b)) return;
-        row -= span_of(a.req, b).first * a.g;
-        if (row < 0) return;
-    }
-    const RowBlock blk = row_block(a, b, row & ~15);
-    const int chunks = (blk.pages + blk.chunk_pages - 1) / blk.chunk_pages;
-    if (row >= blk.rows || chunks <= 1) return;  // (one chunk: written by the first kernel)
-    const size_t slot = partial_row(a, b, blk, row, kv, 0), per_chunk = (size_t)a.h_kv * a.ws_rows;
-    const int col = 64 * blockIdx.z + lane;
-    float mx = kNothingYet, l = 0.0f;
-    if (lane < chunks) {
-        mx = a.ws_ml[(slot + lane * per_chunk) * 2];
-        l = a.ws_ml[(slot + lane * per_chunk) * 2 + 1];
-    }
-    float top = mx;
+__global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a) {
+    constexpr int PER = D / 64;
+    typedef float cols __attribute__((ext_vector_type(PER)));
+    typedef _Float16 out_cols __attribute__((ext_vector_type(PER)));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int total = block_count(a) * a.h_kv;
+    for (int work = blockIdx.x; work < total; work += gridDim.x) {
+        const int kv = work % a.h_kv;
+        int row0;
+        const int b = block_of(a, work / a.h_kv, lane, row0);
+        if (b < 0) continue;
+        const RowBlock blk = row_block(a, b, row0);
+        const int chunks = (blk.pages + blk.chunk_pages - 1) / blk.chunk_pages, row = row0 + 4 * (int)blockIdx.y + wave;
+        if (row >= blk.rows || chunks <= 1) continue;  // (one chunk: written by the first kernel)
+        const size_t slot = partial_row(a, b, blk, row, kv, 0), per_chunk = (size_t)a.h_kv * a.ws_rows;
+        float mx = kNothingYet, l = 0.0f;
+        if (lane < chunks) {
+            mx = a.ws_ml[(slot + lane * per_chunk) * 2];
+            l = a.ws_ml[(slot + lane * per_chunk) * 2 + 1];
+        }
+        // (eight chunks' columns at a time are on their way before the factors are known; chunks behind the last read it again and count as nothing)
+        const float *src = a.ws_o + slot * D + PER * lane;
+        cols part[8];
+        auto fetch = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    const float f = lane < chunks ? __builtin_amdgcn_exp2f(mx - top) : 0.0f;
-    float sum = f * l;
+            for (int c = 0; c < 8; ++c) part[c] = *reinterpret_cast<const cols *>(src + min(c0 + c, chunks - 1) * per_chunk * D);
+        };
+        fetch(0);
+        float top = mx;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    float o = 0.0f;
-    for (int c = 0; c < chunks; ++c) o = fmaf(__shfl(f, c, 64), a.ws_o[(slot + c * per_chunk) * D + col], o);
-    const int s = row / a.g, j = row % a.g;
-    a.out[((size_t)(blk.span.first + s) * a.h_q + kv * a.g + j) * D + col] = (_Float16)(sum > 0.0f ? o / sum : 0.0f);
+        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+        const float f = lane < chunks ? __builtin_amdgcn_exp2f(mx - top) : 0.0f;
+        float sum = f * l;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+        cols o = {};
+        for (int c0 = 0; c0 < chunks; c0 += 8) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const float fc = c0 + c < chunks ? __shfl(f, (c0 + c) & 63, 64) : 0.0f;
+#pragma unroll
+                for (int e = 0; e < PER; ++e) o[e] = c0 + c < chunks ? fmaf(fc, part[c][e], o[e]) : o[e];
+            }
+            if (c0 + 8 < chunks) fetch(c0 + 8);
+        }
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        out_cols y;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) y[e] = (_Float16)(o[e] * inv);
+        *reinterpret_cast<out_cols *>(a.out + ((size_t)(blk.span.first + row / a.g) * a.h_q + kv * a.g + row % a.g) * D + PER * lane) = y;
+    }
 }
 
 // ---------------------------------------------------------------- many query rows
@@ -446,10 +480,11 @@ struct ManyArgs {
 __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
     __shared__ uint64_t wanted[4];
     __shared__ int rec[kMaxSlots][4], item[kMaxSlots];
-    __shared__ int longest, total_items;
+    __shared__ int longest, total_items, few_blocks;
     __shared__ unsigned long long total_steps;  // twice, about
     const int tid = threadIdx.x;
-    if (tid == 0) longest = 0, total_steps = 0;
+    if (tid == 0) longest = 0, total_steps = 0, few_blocks = 0;
+    __syncthreads();
     int count = 0;  // (the same in every thread)
     for (int b0 = 0; b0 < a.req.batch; b0 += 256) {
         const int b = b0 + tid;
@@ -457,7 +492,10 @@ __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
         if (b < a.req.batch) {
             const Span s = span_of(a.req, b);
             many = s.count * a.g > kFewRows && s.positions >= s.count;
-            if (!many) a.plan[ManyRows::kSlots + b] = -1;
+            if (!many) {
+                a.plan[ManyRows::kSlots + b] = -1;
+                atomicAdd(&few_blocks, (s.count * a.g + 15) / 16);
+            }
         }
         const uint64_t mask = __ballot(many);
         if ((tid & 63) == 0) wanted[tid >> 6] = mask;
@@ -472,6 +510,7 @@ __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
                 if (tid == 0) {
                     if (taken) rec[count][0] = s.first, rec[count][1] = s.count, rec[count][2] = s.positions, rec[count][3] = bb;
                     a.plan[ManyRows::kSlots + bb] = taken ? count : -1;
+                    if (!taken) atomicAdd(&few_blocks, (s.count * a.g + 15) / 16);
                 }
                 count += taken;
             }
@@ -532,6 +571,7 @@ __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
     if (tid == 0) {
         a.plan[ManyRows::kCount] = count;
         a.plan[ManyRows::kItems] = total_items;
+        a.plan[ManyRows::kFewBlocks] = few_blocks;
     }
 }
 
@@ -579,18 +619,19 @@ __global__ __launch_bounds__(256) void attn_q4_copy_kernel(ManyArgs a) {
 }
 
 template <int D>
-hipError_t launch(const AttnQ4Args &a, const ManyArgs &many, const AttnQ4Plan &p, hipStream_t st) {
+hipError_t launch(const AttnQ4Args &a, const ManyArgs &many, const AttnQ4Plan &p, int num_cus, hipStream_t st) {
     if (p.slots > 0) {
         attn_q4_list_kernel<<<1, 256, 0, st>>>(many);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     constexpr size_t lds = Ring<D>::LDS;
     if (const hipError_t e = allow_dynamic_lds<attn_q4_kernel<D>>(lds); e != hipSuccess) return e;
-    attn_q4_kernel<D><<<(unsigned)(p.blocks * p.chunks * a.h_kv), 256, lds, st>>>(a);
+    // (with a plan only the device knows how many blocks there are: as many workgroups as the card holds at once, twice over)
+    const long most = p.slots > 0 ? 4L * num_cus : INT32_MAX, works = p.blocks * p.chunks * a.h_kv, rows = p.blocks * a.h_kv;
+    attn_q4_kernel<D><<<(unsigned)(works < most ? works : most), 256, lds, st>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p.chunks > 1) {
-        const long rows = a.one_block ? 16L * a.req.batch : p.all_rows;
-        attn_q4_combine_kernel<D><<<dim3((unsigned)rows, (unsigned)a.h_kv, D / 64), 64, 0, st>>>(a);
+        attn_q4_combine_kernel<D><<<dim3((unsigned)(rows < most ? rows : most), a.few_rows < 16 ? (unsigned)(a.few_rows + 3) / 4 : 4u), 256, 0, st>>>(a);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.slots > 0) {
@@ -658,6 +699,7 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
     a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv;
     a.chunks = p.chunks, a.chunk_pages = p.chunk_pages, a.few_rows = p.few_rows;
     a.one_block = p.rows <= 16;
+    a.blocks = (int)p.blocks;
     a.by_request = (long)req.batch * p.few_rows < p.all_rows;
     a.ws_rows = a.by_request ? (long)req.batch * p.few_rows : p.all_rows;
     a.ws_o = reinterpret_cast<float *>(ws + p.partial);
@@ -679,9 +721,9 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
     }
     hipError_t e = hipErrorInvalidValue;
     switch (d) {
-        case 64: e = launch<64>(a, many, p, st); break;
-        case 128: e = launch<128>(a, many, p, st); break;
-        case 256: e = launch<256>(a, many, p, st); break;
+        case 64: e = launch<64>(a, many, p, num_cus, st); break;
+        case 128: e = launch<128>(a, many, p, num_cus, st); break;
+        case 256: e = launch<256>(a, many, p, num_cus, st); break;
     }
     if (e != hipSuccess || p.slots == 0) return e;
     return launch_attention_many(q, kc, vc, h_q, h_kv, d, p.pages * kPage, a.plan, p.records, p.shares, p.items, p.all_rows,

@@ -392,7 +392,7 @@ hipError_t launch_append_q4(const void *qkv, const Requests &req, int h_q, int h
 hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, hipStream_t st);
 // Attention of requests with many query rows: which they are, and how their walks are cut, is found on the device (attention_q4.hip) and left as a list of int32.
 struct ManyRows {
-    static constexpr int kCount = 0, kItems = 1, kSlots = 4;  // requests, workgroups per KV head; from kSlots on each request's place in the list or -1
+    static constexpr int kCount = 0, kItems = 1, kFewBlocks = 2, kSlots = 4;  // requests, their workgroups per KV head, the other requests' blocks of 16 rows; from kSlots on each request's place in the list or -1
     static constexpr int kRecord = 8;                         // ints per request in the list:
     static constexpr int kRow = 0, kTokens = 1, kPositions = 2, kItem = 3, kChunkSteps = 4, kRequest = 5;
 };
