@@ -516,7 +516,8 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
     const int cus = device_cus();
     const AttnQ4Plan p = attention_plan(requests, h_q, cache, cus);
     if (workspace_bytes < p.total) return QFC_ERR_BUFFER_TOO_SMALL;
-    if (p.blocks * p.chunks * cache->h_kv > INT32_MAX || (long)p.slots * cache->h_kv * p.pages > INT32_MAX) return QFC_ERR_UNSUPPORTED;
+    // (places in the run of all pages, two more for each unit of 16 rows)
+    if ((long)p.slots * cache->h_kv * p.pages > INT32_MAX || p.blocks * cache->h_kv * (p.pages + 2) > INT32_MAX - (1 << 24)) return QFC_ERR_UNSUPPORTED;
     if (requests->tokens == 0) return QFC_OK;
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_attention_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, p, workspace, out_f16, cus,
@@ -650,7 +651,7 @@ void qfc_tune(int32_t key, int32_t value) {
     if (key == 11) t.skinny_blocks = value;
     if (key == 13) t.attn_few = value;
     if (key == 14) t.attn_shares = value;
-    if (key == 15) t.attn_q4_chunks = value < 0 ? 0 : value;
+    if (key == 15) t.attn_q4_pages = value < 0 ? 0 : value;
     if (key == 12) t.attn_splits = value < 0 ? 0 : value > kAttnMaxSplits ? kAttnMaxSplits : value;
 }
 

@@ -34,57 +34,101 @@ struct AttnQ4Args {
     _Float16 *out;
     const char *pages;
     Requests req;
-    float *ws_o, *ws_ml;  // [chunks, h_kv, ws_rows, D] partial outputs, [.., 2] (maximum, sum)
+    float *ws_o, *ws_ml;  // [workers, 2, 16, D] partial outputs, [.., 2] (maximum, sum)
     int *plan;            // ManyRows, or null
-    int h_q, h_kv, g, chunks, chunk_pages, few_rows, by_request;
-    int one_block;  // every request has one block of 16 rows at most
-    int blocks;     // of 16 rows (with a plan: it says how many)
-    long ws_rows;
+    int h_q, h_kv, g, workers, least;
     float scale;
 };
 
-// The rows row0 .. row0 + 15 of a request: how many rows there are, how many pages they see between them, and into how many chunks those are cut
-struct RowBlock {
-    Span span;
-    int rows, pages, end, chunk_pages;  // end: positions the last row sees
-};
+// The work: units of a KV head and a block of 16 query rows of a request, one behind the other (a request's blocks, in each all heads), each with the request's
+// pages.  The pages are dealt to the wavefronts in equal shares (at least `least`), whatever the requests' lengths: each has one run of pages, across units.  A
+// unit is done by one wavefront where it is short (half a share, or `least`), by that in whose share it begins; of a longer one a wavefront does the pages of its share, and
+// leaves partial results where others have the rest: two per wavefront at most, of the unit that its share begins inside of (or with), and of
+// the one that it ends inside of.  A unit's beginning costs about as much as two pages (its requests' arrays, queries and first page one after the other): where a share
+// is some pages, units are that much longer.
 __device__ __forceinline__ bool has_many(const AttnQ4Args &a, int b) { return a.plan && a.plan[ManyRows::kSlots + b] >= 0; }
-__device__ __forceinline__ RowBlock row_block(const AttnQ4Args &a, int b, int row0) {
-    RowBlock k;
-    k.span = span_of(a.req, b);
-    k.rows = k.span.count * a.g;
-    k.end = max(0, k.span.positions - k.span.count + min(row0 + 15, k.rows - 1) / a.g + 1);
-    k.pages = (k.end + kPage - 1) / kPage;
-    k.chunk_pages = k.rows > a.few_rows ? max(k.pages, 1) : a.chunk_pages;  // (no room for more partial results)
-    return k;
+// sum over the lanes up to this one
+__device__ __forceinline__ int sum_upto(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast 15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    return x;
 }
-__device__ __forceinline__ size_t partial_row(const AttnQ4Args &a, int b, const RowBlock &k, int row, int kv, int chunk) {
-    return ((size_t)chunk * a.h_kv + kv) * a.ws_rows + (a.by_request ? (size_t)b * a.few_rows : (size_t)k.span.first * a.g) + row;
-}
-__device__ __forceinline__ int block_count(const AttnQ4Args &a) { return a.plan ? a.plan[ManyRows::kFewBlocks] : a.blocks; }
-// Request and first row of the i-th block of 16 rows of all requests (those of many rows left out); -1 behind the last
-__device__ __forceinline__ int block_of(const AttnQ4Args &a, int i, int lane, int &row0) {
-    row0 = 0;
-    if (a.one_block) return i;
-    for (int b0 = 0; b0 < a.req.batch; b0 += 64) {
-        const int b = b0 + lane;
-        int upto = b < a.req.batch && !has_many(a, b) ? (span_of(a.req, b).count * a.g + 15) / 16 : 0;
-        const int own = upto;
+struct Unit {
+    int b, kv, row0;  // b < 0: behind the last
+    int begin, end;   // places in the run of all units
+};
+struct Units {
+    const AttnQ4Args a;
+    const int lane;
+    int share, over;           // pages of a wavefront, and what a unit has on top of its own
+    int b0, before, before_u;  // 64 requests at a time: the first, and places and units before them
+    int count, pages, upto, upto_u;  // of this lane's request: units, pages of each; places and units up to its end
+    __device__ __forceinline__ Units(const AttnQ4Args &args, int l) : a(args), lane(l), share(0), over(0), b0(0), before(0), before_u(0) {
+        int all = 0, units = 0, longest = 0;
+        for (int c = 0; c < a.req.batch; c += 64) {
+            load(c);
+            all += count * pages;
+            units += count;
+            longest = max(longest, count > 0 ? pages : 0);
+        }
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int below = __shfl_up(upto, off, 64);
-            upto += lane >= off ? below : 0;
-        }
-        const uint64_t at = __ballot(upto > i);
-        if (at) {
-            const int l = __ffsll((unsigned long long)at) - 1;
-            row0 = __builtin_amdgcn_readfirstlane(16 * (i - __shfl(upto - own, l, 64)));
-            return b0 + __builtin_amdgcn_readfirstlane(l);
-        }
-        i -= __builtin_amdgcn_readlane(upto, 63);
+        for (int off = 32; off > 0; off >>= 1) longest = max(longest, __shfl_xor(longest, off, 64));
+        all = last(sum_upto(all)), units = last(sum_upto(units)), longest = __builtin_amdgcn_readfirstlane(longest);
+        over = all / a.workers >= 4 ? 2 : 0;
+        // (a unit is cut into 254 whole shares and two ends at most: the combination's four wavefronts take 64 each)
+        share = max(max(a.least, (longest + over + 253) / 254), (all + over * units + a.workers - 1) / a.workers);
+        if (a.req.batch > 64) load(0);
+        sum();
     }
-    return -1;
-}
+    __device__ static __forceinline__ int last(int x) { return __builtin_amdgcn_readlane(x, 63); }
+    __device__ __forceinline__ void load(int c) {
+        b0 = c;
+        count = 0, pages = 1;  // (a unit without positions counts as one page: its rows are written)
+        const int b = c + lane;
+        if (b < a.req.batch && !has_many(a, b)) {
+            const Span s = span_of(a.req, b);
+            count = (s.count * a.g + 15) / 16 * a.h_kv;
+            pages = max(1, (s.positions + kPage - 1) / kPage);
+        }
+    }
+    __device__ __forceinline__ void sum() {
+        upto = sum_upto(count * (pages + over));
+        upto_u = sum_upto(count);
+    }
+    // The unit of place x or, by_index, the x-th; x does not descend from call to call
+    template <bool BY_INDEX>
+    __device__ __forceinline__ Unit at(int x) {
+        Unit u = {-1, 0, 0, 0, 0};
+        for (;;) {
+            const int of = BY_INDEX ? upto_u : upto, base = BY_INDEX ? before_u : before;
+            const uint64_t past = __ballot(of > x - base);
+            if (past) {
+                const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+                const int n = __builtin_amdgcn_readlane(count, l), len = __builtin_amdgcn_readlane(pages, l) + over;
+                const int first = before + __builtin_amdgcn_readlane(upto, l) - n * len;
+                const int index = BY_INDEX ? x - (before_u + __builtin_amdgcn_readlane(upto_u, l) - n) : (x - first) / len;
+                u.b = b0 + l;
+                u.kv = index % a.h_kv;
+                u.row0 = index / a.h_kv * 16;
+                u.begin = first + index * len;
+                u.end = u.begin + len;
+                return u;
+            }
+            if (b0 + 64 >= a.req.batch) return u;
+            before += last(upto);
+            before_u += last(upto_u);
+            load(b0 + 64);
+            sum();
+        }
+    }
+    __device__ __forceinline__ bool may_cut(const Unit &u) const { return u.end - u.begin > max(a.least + over, share / 2); }
+};
+// Place of the partial results that worker w leaves of a unit
+__device__ __forceinline__ size_t partial_of(const Unit &u, int w, int share) { return (size_t)w * 2 + (u.begin > w * share ? 1 : 0); }
 
 // What a wavefront has on its way: DEPTH pages, keys and values each in a place of PART bytes of LDS of its own.
 template <int D>
@@ -93,42 +137,49 @@ struct Ring {
     static constexpr int PART = (kHalf + 1023) / 1024 * 1024;  // copied in pieces of a KiB
     static constexpr int COPIES = PART / 1024;
     static constexpr int DEPTH = D == 64 ? 3 : 2;
-    static constexpr int PITCH = D + 4;  // floats per row of the wavefronts' results
     static constexpr int WAVE = 2 * DEPTH * PART;
-    static constexpr int MERGE = 4 * 16 * PITCH * 4;
-    static constexpr int LDS = 4 * WAVE > MERGE ? 4 * WAVE : MERGE;
+    static constexpr int LDS = 4 * WAVE;
     static constexpr int FLYING = (2 * DEPTH - 1) * COPIES;  // copies behind the ones waited for
     static_assert(LDS <= (D <= 128 ? 80 : 160) * 1024 && FLYING <= 63, "LDS, and the 6-bit counter of outstanding copies");
 };
 
-// Workgroup = four wavefronts and up to 16 query rows of a KV head; the wavefronts take the pages of the workgroup's chunk in turn, each with
-// copies of its own on the way (no barrier before the end).  Where the number of blocks is only known on the device, workgroups take one after the other.
+// Up to 16 query rows of a KV head at a time.  The wavefronts work for themselves, each with copies of its own on the way.
 template <int D>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Args a) {
     typedef PageLayout<D> L;
     typedef Ring<D> R;
     constexpr int G = L::G, DT = D / 16, W = L::W;
-    constexpr int PITCH = R::PITCH;
-    extern __shared__ float lds[];  // the rings; then [4][16][PITCH]
+    extern __shared__ float lds[];  // the rings
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, r = lane >> 4;
-    const int total = block_count(a) * a.h_kv * a.chunks;
-    for (int work = blockIdx.x; work < total; work += gridDim.x) {
-    const int chunk = work % a.chunks, kv = work / a.chunks % a.h_kv;
-    int row0;
-    const int b = block_of(a, work / a.chunks / a.h_kv, lane, row0);
-    if (b < 0) continue;
-    const RowBlock blk = row_block(a, b, row0);
-    if (row0 >= blk.rows || (chunk > 0 && chunk * blk.chunk_pages >= blk.pages)) continue;
-    __syncthreads();  // (all are done with the work before)
-    const int pages = __builtin_amdgcn_readfirstlane(chunk == 0 ? min(blk.pages, blk.chunk_pages) : min(blk.pages, (chunk + 1) * blk.chunk_pages));
-    const int n = blk.span.positions;
+    char *const ring = reinterpret_cast<char *>(lds) + wave * R::WAVE;
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * R::WAVE);
+    const int worker = (int)blockIdx.x * 4 + wave;
+    if (worker >= a.workers) return;
+    Units units(a, lane);
+    const int from = worker * units.share, stop = from + units.share;
+    for (int x = from; x < stop;) {
+    const Unit unit = units.at<false>(x);
+    if (unit.b < 0) return;
+    const bool cut = units.may_cut(unit);
+    if (!cut && unit.begin < x) {  // (another wavefront has it)
+        x = unit.end;
+        continue;
+    }
+    const int b = unit.b, kv = unit.kv, row0 = unit.row0;
+    const Span span = span_of(a.req, b);
+    const int rows = __builtin_amdgcn_readfirstlane(span.count * a.g), n = __builtin_amdgcn_readfirstlane(span.positions);
+    const int sees = max(0, n - rows / a.g + min(row0 + 15, rows - 1) / a.g + 1);  // positions the unit's last row sees
+    const int last = cut ? min(stop, unit.end) : unit.end;
+    const bool whole = unit.begin >= from && last == unit.end;  // no other wavefront has a page of the unit
+    const int page0 = max(x - unit.begin - units.over, 0), pages = min(last - unit.begin - units.over, (sees + kPage - 1) / kPage);  // the unit's pages that are taken here
+    x = last;
 
     // ---- queries: lane (m, r) holds q[row0 + m][32 j + 8 r .. + 7], scaled by a power of two
-    const bool real = row0 + m < blk.rows;
+    const bool real = row0 + m < rows;
     const int token = real ? (row0 + m) / a.g : 0, head = kv * a.g + (real ? (row0 + m) % a.g : 0);
-    const size_t at = ((size_t)(blk.span.first + token) * a.h_q + head) * D;
-    const int lim = real ? n - blk.span.count + token + 1 : 0;  // positions the lane's row sees (none where 0 or less)
+    const size_t at = ((size_t)(span.first + token) * a.h_q + head) * D;
+    const int lim = real ? n - span.count + token + 1 : 0;  // positions the lane's row sees (none where 0 or less)
     h8 qf[G];
     float top = 0.0f;
 #pragma unroll
@@ -173,16 +224,13 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     for (int e = 0; e < 8; ++e) eight[e] = __builtin_bit_cast(_Float16, (uint16_t)8);
     const uint32_t mask_lo = 0x000F000Fu, mask_hi = 0x00F000F0u;
 
-    // ---- copies.  The wavefront's i-th page is first + 4 i; lane i holds the place of page i (of 64 at a time)
-    const int first = chunk * blk.chunk_pages + wave;
-    const int count = first < pages ? (pages - first + 3) / 4 : 0;
-    char *const ring = reinterpret_cast<char *>(lds) + wave * R::WAVE;
-    const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * R::WAVE);
-    auto places = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (first + 4 * (i + lane)) * kPage) : -1; };
+    // ---- copies.  Lane i holds the place of the wavefront's i-th page (of 64 at a time)
+    const int count = pages - page0;
+    auto places = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (page0 + i + lane) * kPage) : -1; };
     int ahead = places(0), now = ahead;  // of the pages that are requested, and of those that are worked on
     auto copy = [&](int i, int slot, int part) __attribute__((always_inline)) {  // part 0: keys, 1: values
         const int page = __builtin_amdgcn_readlane(ahead, i & 63);
-        const char *src = a.pages + ((size_t)max(page, 0) * a.h_kv + kv) * L::kBytes + part * R::kHalf;
+        const char *src = a.pages + ((size_t)max(page, 0) * a.h_kv + __builtin_amdgcn_readfirstlane(kv)) * L::kBytes + part * R::kHalf;
 #pragma unroll
         for (int c = 0; c < R::COPIES; ++c)  // (the last piece's lanes behind the part copy its end again)
             copy16_to_lds(src, (uint32_t)min(c * 1024 + lane * 16, R::kHalf - 16), ring_at + (2 * slot + part) * R::PART + c * 1024);
@@ -202,7 +250,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     };
 
     for (int i = 0, slot = 0; i < count; ++i, slot = slot + 1 == R::DEPTH ? 0 : slot + 1) {
-        const int k0 = (first + 4 * i) * kPage;
+        const int k0 = (page0 + i) * kPage;
         if (i > 0 && (i & 63) == 0) now = places(i);
         if (i + R::DEPTH < count && ((i + R::DEPTH) & 63) == 0) ahead = places(i + R::DEPTH);
         const int page = __builtin_amdgcn_readlane(now, i & 63);
@@ -353,116 +401,102 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
         if (i + R::DEPTH < count) copy(i + R::DEPTH, slot, 1);
     }
 
-    // ---- the four wavefronts meet in LDS: [wave][m][PITCH] = output row m (2^14 times, unnormalized), then (maximum, sum)
-    __syncthreads();  // (all are done with their rings)
-    float *mine = lds + ((size_t)wave * 16 + m) * PITCH;
-    const float back = 16777216.0f / lower;
+    // ---- output row m (2^14 times, unnormalized), its maximum and sum
+    const float back = 16777216.0f / lower, sum = __shfl(rest[3], 48 + m, 64), inv = sum > 0.0f ? 1.0f / sum : 0.0f;  // (a row that sees nothing: 0)
+    const size_t part = partial_of(unit, worker, units.share) * 16 + m;
 #pragma unroll
     for (int j = 0; j < G; ++j) {
         const float off = __shfl(rest[j & 3], (j >> 2) * 16 + m, 64);
-        v4f lo, hi;
+        v4f o[2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            lo[i] = fmaf(acc[2 * j][i] - eights[j][i], back, off);
-            hi[i] = fmaf(acc[2 * j + 1][i] * 0.0625f - eights[j][i], back, off);
+            o[0][i] = fmaf(acc[2 * j][i] - eights[j][i], back, off);
+            o[1][i] = fmaf(acc[2 * j + 1][i] * 0.0625f - eights[j][i], back, off);
         }
-        *reinterpret_cast<v4f *>(mine + 32 * j + 4 * r) = lo;
-        *reinterpret_cast<v4f *>(mine + 32 * j + 16 + 4 * r) = hi;
+        if (!real) continue;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int d = 32 * j + 16 * k + 4 * r;
+            if (whole)
+                *reinterpret_cast<h4 *>(a.out + at + d) = h4{(_Float16)(o[k][0] * inv), (_Float16)(o[k][1] * inv), (_Float16)(o[k][2] * inv), (_Float16)(o[k][3] * inv)};
+            else
+                *reinterpret_cast<v4f *>(a.ws_o + part * D + d) = o[k];
+        }
     }
-    if (r == 3) {
-        mine[D] = run_max;
-        mine[D + 1] = rest[3];
-    }
-    __syncthreads();
-    const int rows = min(16, blk.rows - row0), chunks = max(1, (blk.pages + blk.chunk_pages - 1) / blk.chunk_pages);
-    for (int e = threadIdx.x; e < rows * (D / 4); e += 256) {
-        const int mm = e / (D / 4), dd = 4 * (e % (D / 4));
-        const float *row = lds + (size_t)mm * PITCH;
-        float f[4], mx = kNothingYet, l = 0.0f;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            f[x] = row[(size_t)x * 16 * PITCH + D];
-            mx = fmaxf(mx, f[x]);
-        }
-        v4f o = {};
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const v4f part = *reinterpret_cast<const v4f *>(row + (size_t)x * 16 * PITCH + dd);
-            f[x] = __builtin_amdgcn_exp2f(f[x] - mx);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += f[x] * part[i];
-            l += f[x] * row[(size_t)x * 16 * PITCH + D + 1];
-        }
-        if (chunks == 1) {
-            const int s = (row0 + mm) / a.g, j = (row0 + mm) % a.g;
-            const float inv = l > 0.0f ? 1.0f / l : 0.0f;  // (a row that sees nothing: 0)
-            *reinterpret_cast<h4 *>(a.out + ((size_t)(blk.span.first + s) * a.h_q + kv * a.g + j) * D + dd) =
-                h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
-        } else {
-            const size_t p = partial_row(a, b, blk, row0 + mm, kv, chunk);
-            *reinterpret_cast<v4f *>(a.ws_o + p * D + dd) = o;
-            if (dd == 0) {
-                a.ws_ml[p * 2] = mx;
-                a.ws_ml[p * 2 + 1] = l;
-            }
-        }
+    if (real && !whole && r == 0) {
+        a.ws_ml[part * 2] = run_max;
+        a.ws_ml[part * 2 + 1] = sum;
     }
     }
 }
 
-// One wavefront per query row, four rows of a block per workgroup: grid = (blocks x KV heads, 4).  Lane c takes the (maximum, sum) of chunk c (at most 64), and
-// D / 64 columns of the partial outputs.
+// The units that several wavefronts share, a row of one per workgroup: grid = (units, rows), or workgroups that take one unit after the other.  Its four wavefronts take the
+// parts in turn, lane c the (maximum, sum) of its c-th and D / 64 columns of the partial outputs; they meet in LDS.
 template <int D>
 __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a) {
     constexpr int PER = D / 64;
     typedef float cols __attribute__((ext_vector_type(PER)));
-    typedef _Float16 out_cols __attribute__((ext_vector_type(PER)));
+    __shared__ float outs[4][D], maxima[4], sums[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int total = block_count(a) * a.h_kv;
-    for (int work = blockIdx.x; work < total; work += gridDim.x) {
-        const int kv = work % a.h_kv;
-        int row0;
-        const int b = block_of(a, work / a.h_kv, lane, row0);
-        if (b < 0) continue;
-        const RowBlock blk = row_block(a, b, row0);
-        const int chunks = (blk.pages + blk.chunk_pages - 1) / blk.chunk_pages, row = row0 + 4 * (int)blockIdx.y + wave;
-        if (row >= blk.rows || chunks <= 1) continue;  // (one chunk: written by the first kernel)
-        const size_t slot = partial_row(a, b, blk, row, kv, 0), per_chunk = (size_t)a.h_kv * a.ws_rows;
+    Units units(a, lane);
+    for (int i = blockIdx.x;; i += gridDim.x) {
+        const Unit unit = units.at<true>(i);
+        if (unit.b < 0) return;
+        if (!units.may_cut(unit)) continue;
+        const int w0 = unit.begin / units.share, parts = (unit.end - 1) / units.share - w0 + 1;
+        if (parts == 1) continue;  // (written by the first kernel)
+        const Span span = span_of(a.req, unit.b);
+        const int row = unit.row0 + (int)blockIdx.y;
+        if (row >= span.count * a.g) continue;
+        const size_t slot0 = partial_of(unit, w0, units.share) * 16 + blockIdx.y;  // of the first; the others begin inside the unit
+        auto place = [&](int c) __attribute__((always_inline)) { return c == 0 ? slot0 : (size_t)(w0 + c) * 32 + blockIdx.y; };
+        const int own = (parts - wave + 3) / 4;  // of this wavefront: wave, wave + 4, ...
         float mx = kNothingYet, l = 0.0f;
-        if (lane < chunks) {
-            mx = a.ws_ml[(slot + lane * per_chunk) * 2];
-            l = a.ws_ml[(slot + lane * per_chunk) * 2 + 1];
+        if (lane < own) {
+            mx = a.ws_ml[place(wave + 4 * lane) * 2];
+            l = a.ws_ml[place(wave + 4 * lane) * 2 + 1];
         }
-        // (eight chunks' columns at a time are on their way before the factors are known; chunks behind the last read it again and count as nothing)
-        const float *src = a.ws_o + slot * D + PER * lane;
+        // (eight parts' columns at a time are on their way before the factors are known; parts behind the last read it again and count as nothing)
+        const float *src = a.ws_o + PER * lane;
         cols part[8];
         auto fetch = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) part[c] = *reinterpret_cast<const cols *>(src + min(c0 + c, chunks - 1) * per_chunk * D);
+            for (int c = 0; c < 8; ++c) part[c] = *reinterpret_cast<const cols *>(src + place(min(wave + 4 * (c0 + c), parts - 1)) * D);
         };
         fetch(0);
         float top = mx;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-        const float f = lane < chunks ? __builtin_amdgcn_exp2f(mx - top) : 0.0f;
+        const float f = lane < own ? __builtin_amdgcn_exp2f(mx - top) : 0.0f;
         float sum = f * l;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
         cols o = {};
-        for (int c0 = 0; c0 < chunks; c0 += 8) {
+        for (int c0 = 0; c0 < own; c0 += 8) {
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-                const float fc = c0 + c < chunks ? __shfl(f, (c0 + c) & 63, 64) : 0.0f;
+                const float fc = c0 + c < own ? __shfl(f, (c0 + c) & 63, 64) : 0.0f;
 #pragma unroll
-                for (int e = 0; e < PER; ++e) o[e] = c0 + c < chunks ? fmaf(fc, part[c][e], o[e]) : o[e];
+                for (int e = 0; e < PER; ++e) o[e] = c0 + c < own ? fmaf(fc, part[c][e], o[e]) : o[e];
             }
-            if (c0 + 8 < chunks) fetch(c0 + 8);
+            if (c0 + 8 < own) fetch(c0 + 8);
         }
-        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-        out_cols y;
+        __syncthreads();  // (the row before has been written)
 #pragma unroll
-        for (int e = 0; e < PER; ++e) y[e] = (_Float16)(o[e] * inv);
-        *reinterpret_cast<out_cols *>(a.out + ((size_t)(blk.span.first + row / a.g) * a.h_q + kv * a.g + row % a.g) * D + PER * lane) = y;
+        for (int e = 0; e < PER; ++e) outs[wave][PER * lane + e] = o[e];
+        if (lane == 0) maxima[wave] = top, sums[wave] = sum;
+        __syncthreads();
+        if (threadIdx.x < D) {
+            const float high = fmaxf(fmaxf(maxima[0], maxima[1]), fmaxf(maxima[2], maxima[3]));
+            float total = 0.0f, y = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float fw = __builtin_amdgcn_exp2f(maxima[w] - high);
+                total = fmaf(fw, sums[w], total);
+                y = fmaf(fw, outs[w][threadIdx.x], y);
+            }
+            a.out[((size_t)(span.first + row / a.g) * a.h_q + unit.kv * a.g + row % a.g) * D + threadIdx.x] = (_Float16)(total > 0.0f ? y / total : 0.0f);
+        }
     }
 }
 
@@ -480,10 +514,10 @@ struct ManyArgs {
 __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
     __shared__ uint64_t wanted[4];
     __shared__ int rec[kMaxSlots][4], item[kMaxSlots];
-    __shared__ int longest, total_items, few_blocks;
+    __shared__ int longest, total_items;
     __shared__ unsigned long long total_steps;  // twice, about
     const int tid = threadIdx.x;
-    if (tid == 0) longest = 0, total_steps = 0, few_blocks = 0;
+    if (tid == 0) longest = 0, total_steps = 0;
     __syncthreads();
     int count = 0;  // (the same in every thread)
     for (int b0 = 0; b0 < a.req.batch; b0 += 256) {
@@ -492,10 +526,7 @@ __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
         if (b < a.req.batch) {
             const Span s = span_of(a.req, b);
             many = s.count * a.g > kFewRows && s.positions >= s.count;
-            if (!many) {
-                a.plan[ManyRows::kSlots + b] = -1;
-                atomicAdd(&few_blocks, (s.count * a.g + 15) / 16);
-            }
+            if (!many) a.plan[ManyRows::kSlots + b] = -1;
         }
         const uint64_t mask = __ballot(many);
         if ((tid & 63) == 0) wanted[tid >> 6] = mask;
@@ -510,7 +541,6 @@ __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
                 if (tid == 0) {
                     if (taken) rec[count][0] = s.first, rec[count][1] = s.count, rec[count][2] = s.positions, rec[count][3] = bb;
                     a.plan[ManyRows::kSlots + bb] = taken ? count : -1;
-                    if (!taken) atomicAdd(&few_blocks, (s.count * a.g + 15) / 16);
                 }
                 count += taken;
             }
@@ -571,7 +601,6 @@ __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
     if (tid == 0) {
         a.plan[ManyRows::kCount] = count;
         a.plan[ManyRows::kItems] = total_items;
-        a.plan[ManyRows::kFewBlocks] = few_blocks;
     }
 }
 
@@ -626,12 +655,11 @@ hipError_t launch(const AttnQ4Args &a, const ManyArgs &many, const AttnQ4Plan &p
     }
     constexpr size_t lds = Ring<D>::LDS;
     if (const hipError_t e = allow_dynamic_lds<attn_q4_kernel<D>>(lds); e != hipSuccess) return e;
-    // (with a plan only the device knows how many blocks there are: as many workgroups as the card holds at once, twice over)
-    const long most = p.slots > 0 ? 4L * num_cus : INT32_MAX, works = p.blocks * p.chunks * a.h_kv, rows = p.blocks * a.h_kv;
-    attn_q4_kernel<D><<<(unsigned)(works < most ? works : most), 256, lds, st>>>(a);
+    attn_q4_kernel<D><<<(unsigned)((a.workers + 3) / 4), 256, lds, st>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (p.chunks > 1) {
-        attn_q4_combine_kernel<D><<<dim3((unsigned)(rows < most ? rows : most), a.few_rows < 16 ? (unsigned)(a.few_rows + 3) / 4 : 4u), 256, 0, st>>>(a);
+    if (p.shared) {
+        const long units = p.blocks * a.h_kv, most = 4L * num_cus;
+        attn_q4_combine_kernel<D><<<dim3((unsigned)(units < most ? units : most), p.rows < 16 ? (unsigned)p.rows : 16u), 256, 0, st>>>(a);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.slots > 0) {
@@ -651,28 +679,23 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     p.rows = max_tokens * g;
     p.all_rows = (long)tokens * g;
     p.blocks = p.rows <= 16 ? batch : (p.all_rows + 15) / 16 + batch;
-    // few rows: a workgroup for a chunk of a request's pages, four per compute unit where there are pages enough for its four wavefronts
-    long chunks = 4L * num_cus / ((long)batch * h_kv);
-    if (const int forced = tuning().attn_q4_chunks; forced > 0)
-        chunks = forced < p.pages ? forced : p.pages;
-    else if (chunks > (p.pages + 3) / 4)
-        chunks = (p.pages + 3) / 4;
-    if (chunks > kAttnMaxSplits) chunks = kAttnMaxSplits;
-    if (chunks < 1) chunks = 1;
-    p.chunk_pages = (int)((p.pages + chunks - 1) / chunks);
-    p.chunks = (p.pages + p.chunk_pages - 1) / p.chunk_pages;
-    p.few_rows = p.rows < kFewRows ? p.rows : kFewRows;
-    const long by_request = (long)batch * p.few_rows, ws_rows = by_request < p.all_rows ? by_request : p.all_rows;
+    // few rows: as many wavefronts as the card holds at once
+    const long on_card = (long)num_cus * (d <= 128 ? 2 : 1), most_pages = p.blocks * h_kv * p.pages;
+    p.least = 1;
+    if (const int forced = tuning().attn_q4_pages; forced > 0) p.least = forced;
+    const long shares = (most_pages + p.least - 1) / p.least;
+    p.workers = (int)(shares < 4 * on_card ? shares : 4 * on_card);
+    if (p.workers < 1) p.workers = 1;
+    p.shared = p.pages > p.least;
     p.total = 256;
     p.partial = 0;
-    if (p.chunks > 1) p.total += up256((size_t)p.chunks * h_kv * ws_rows * (d + 2) * sizeof(float));
+    if (p.shared) p.total += up256((size_t)p.workers * 2 * 16 * (d + 2) * sizeof(float));
     // many rows
     if (p.rows <= kFewRows) return p;
     const long most = p.all_rows / (kFewRows + 1);
     p.slots = (int)(most < batch ? most : batch);
     if (p.slots > kMaxSlots) p.slots = kMaxSlots;
     if (p.slots == 0) return p;
-    const long on_card = (long)num_cus * (d <= 128 ? 2 : 1);  // workgroups the card holds at once
     p.shares = p.all_rows * h_kv / 128 >= 2 * on_card ? 1 : 2;
     const int block_rows = 128 / p.shares;
     const long blocks = p.all_rows / block_rows + p.slots;
@@ -697,13 +720,9 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
     a.pages = static_cast<const char *>(pages);
     a.req = req;
     a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv;
-    a.chunks = p.chunks, a.chunk_pages = p.chunk_pages, a.few_rows = p.few_rows;
-    a.one_block = p.rows <= 16;
-    a.blocks = (int)p.blocks;
-    a.by_request = (long)req.batch * p.few_rows < p.all_rows;
-    a.ws_rows = a.by_request ? (long)req.batch * p.few_rows : p.all_rows;
+    a.workers = p.workers, a.least = p.least;
     a.ws_o = reinterpret_cast<float *>(ws + p.partial);
-    a.ws_ml = a.ws_o + (size_t)p.chunks * h_kv * a.ws_rows * d;
+    a.ws_ml = a.ws_o + (size_t)p.workers * 2 * 16 * d;
     a.scale = 1.4426950408889634f / sqrtf((float)d);
     ManyArgs many = {};
     _Float16 *kc = nullptr, *vc = nullptr;

@@ -140,7 +140,7 @@ struct Tuning {
     Tunable skinny_blocks{0};   // blocks the token rows are cut into at least (0: automatic)
     Tunable attn_few{-1};       // attention, blocks of 16 query rows: -1 automatic, 0 above 16 rows never, 1 always
     Tunable attn_splits{0};     // decode attention: workgroups per KV head (0: automatic)
-    Tunable attn_q4_chunks{0};  // attention over the 4-bit cache: workgroups that share a request's pages (0: automatic)
+    Tunable attn_q4_pages{0};   // attention over the 4-bit cache: pages a wavefront takes at least (0: automatic)
     Tunable gemv_half{-1};      // half-unit items of the decode kernel: -1 automatic, 0 never, 1 where possible
 };
 Tuning &tuning();
@@ -392,16 +392,16 @@ hipError_t launch_append_q4(const void *qkv, const Requests &req, int h_q, int h
 hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, hipStream_t st);
 // Attention of requests with many query rows: which they are, and how their walks are cut, is found on the device (attention_q4.hip) and left as a list of int32.
 struct ManyRows {
-    static constexpr int kCount = 0, kItems = 1, kFewBlocks = 2, kSlots = 4;  // requests, their workgroups per KV head, the other requests' blocks of 16 rows; from kSlots on each request's place in the list or -1
+    static constexpr int kCount = 0, kItems = 1, kSlots = 4;  // requests, their workgroups per KV head; from kSlots on each request's place in the list or -1
     static constexpr int kRecord = 8;                         // ints per request in the list:
     static constexpr int kRow = 0, kTokens = 1, kPositions = 2, kItem = 3, kChunkSteps = 4, kRequest = 5;
 };
 struct AttnQ4Plan {
     int rows;         // query rows of a KV head and request at most
     long blocks;      // blocks of 16 rows of all requests at most
-    int chunk_pages;  // pages a workgroup takes
-    int chunks;       // workgroups that share the longest request's pages
-    int few_rows;     // rows per request with partial results
+    int workers;      // wavefronts that share the pages of all requests of few rows
+    int least;        // pages a wavefront takes at least
+    bool shared;      // a request's pages may be shared by several
     // requests of many rows (slots 0: there are none)
     int slots;        // at most so many
     int shares;       // wavefronts that share a walk
