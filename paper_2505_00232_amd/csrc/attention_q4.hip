@@ -6,14 +6,14 @@
 // times as high meet queries divided by 16, and the accumulator starts at -8 sum q_j.  The steps multiply the 32-bit result; the offsets come in by one more MFMA, against the sums of
 // q in two binary16 parts (2^-22).  For the second product
 //   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
-// P is multiplied with the step in 32 bits and rounded to binary16 once per group; the -8 is taken off with the same rounded values (an MFMA against a
-// constant), so that what the rounding leaves is relative to a centred code, and the offsets are again one MFMA, whose last row, ones, gives the sum of P.
+// P is multiplied with the step in 32 bits and rounded to binary16 once per group; the -8 is taken off with the same rounded values (an MFMA with a
+// constant into the same sums), so that what the rounding leaves is relative to a centred code, and the offsets are again one MFMA, whose last row, ones, gives the sum of P.
 //
 // Few query rows of a request (up to kFewRows per KV head: tokens, short chunks) go through that kernel in blocks of 16.  Many rows would take the same
 // codes apart again and again: for them the pages are first turned into binary16 copies in the workspace, once, and the kernel for prompts (attention.hip) walks
 // those.  Which request is which is known on the device only, where a first small kernel finds it.
-// P is taken 2^14 times as large: with steps below 2 every product is below 2^15, and binary16 keeps its 11 bits down to 2^-28.  A
-// step of 2 or more (values some 30 apart and more) lowers that factor to 2^2 from there on, for which every step is small enough.
+// P is taken against a maximum that may be 2^4 too small (so that sums are seldom rescaled) and 2^10 times as large: with steps below 2 every product is below 2^15, and binary16
+// keeps its 11 bits down to 2^-24.  A step of 2 or more (values some 30 apart and more) lowers that factor to 2^-2 from there on, for which every step is small enough.
 #include "paged_q4.h"
 
 namespace qfc {
@@ -24,6 +24,7 @@ typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr float kFactor = 10.0f, kLag = 4.0f, kLower = 12.0f;  // log 2 of what P is multiplied with, of what the maximum may lag behind, of what large steps divide P by
 constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: below every score
 
 constexpr int kFewRows = 256;
@@ -60,6 +61,7 @@ __device__ __forceinline__ int sum_upto(int x) {
 struct Unit {
     int b, kv, row0;  // b < 0: behind the last
     int begin, end;   // places in the run of all units
+    Span span;
 };
 struct Units {
     const AttnQ4Args a;
@@ -67,32 +69,29 @@ struct Units {
     int share, over;           // pages of a wavefront, and what a unit has on top of its own
     int b0, before, before_u;  // 64 requests at a time: the first, and places and units before them
     int count, pages, upto, upto_u;  // of this lane's request: units, pages of each; places and units up to its end
+    Span span;
     __device__ __forceinline__ Units(const AttnQ4Args &args, int l) : a(args), lane(l), share(0), over(0), b0(0), before(0), before_u(0) {
-        int all = 0, units = 0, longest = 0;
+        int all = 0, units = 0;
         for (int c = 0; c < a.req.batch; c += 64) {
             load(c);
             all += count * pages;
             units += count;
-            longest = max(longest, count > 0 ? pages : 0);
         }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) longest = max(longest, __shfl_xor(longest, off, 64));
-        all = last(sum_upto(all)), units = last(sum_upto(units)), longest = __builtin_amdgcn_readfirstlane(longest);
-        over = all / a.workers >= 4 ? 2 : 0;
-        // (a unit is cut into 254 whole shares and two ends at most: the combination's four wavefronts take 64 each)
-        share = max(max(a.least, (longest + over + 253) / 254), (all + over * units + a.workers - 1) / a.workers);
+        all = last(sum_upto(all)), units = last(sum_upto(units));
+        over = all / 4 >= a.workers ? 2 : 0;
+        share = max(a.least, (all + over * units + a.workers - 1) / a.workers);
         if (a.req.batch > 64) load(0);
         sum();
     }
     __device__ static __forceinline__ int last(int x) { return __builtin_amdgcn_readlane(x, 63); }
     __device__ __forceinline__ void load(int c) {
         b0 = c;
-        count = 0, pages = 1;  // (a unit without positions counts as one page: its rows are written)
+        count = 0, pages = 1, span = Span{0, 0, 0};  // (a unit without positions counts as one page: its rows are written)
         const int b = c + lane;
         if (b < a.req.batch && !has_many(a, b)) {
-            const Span s = span_of(a.req, b);
-            count = (s.count * a.g + 15) / 16 * a.h_kv;
-            pages = max(1, (s.positions + kPage - 1) / kPage);
+            span = span_of(a.req, b);
+            count = (span.count * a.g + 15) / 16 * a.h_kv;
+            pages = max(1, (span.positions + kPage - 1) / kPage);
         }
     }
     __device__ __forceinline__ void sum() {
@@ -102,7 +101,7 @@ struct Units {
     // The unit of place x or, by_index, the x-th; x does not descend from call to call
     template <bool BY_INDEX>
     __device__ __forceinline__ Unit at(int x) {
-        Unit u = {-1, 0, 0, 0, 0};
+        Unit u = {-1, 0, 0, 0, 0, {0, 0, 0}};
         for (;;) {
             const int of = BY_INDEX ? upto_u : upto, base = BY_INDEX ? before_u : before;
             const uint64_t past = __ballot(of > x - base);
@@ -111,11 +110,13 @@ struct Units {
                 const int n = __builtin_amdgcn_readlane(count, l), len = __builtin_amdgcn_readlane(pages, l) + over;
                 const int first = before + __builtin_amdgcn_readlane(upto, l) - n * len;
                 const int index = BY_INDEX ? x - (before_u + __builtin_amdgcn_readlane(upto_u, l) - n) : (x - first) / len;
-                u.b = b0 + l;
-                u.kv = index % a.h_kv;
-                u.row0 = index / a.h_kv * 16;
-                u.begin = first + index * len;
-                u.end = u.begin + len;
+                // (the same in every lane: said explicitly, it stays in scalar registers)
+                u.b = __builtin_amdgcn_readfirstlane(b0 + l);
+                u.kv = __builtin_amdgcn_readfirstlane(index % a.h_kv);
+                u.row0 = __builtin_amdgcn_readfirstlane(index / a.h_kv * 16);
+                u.begin = __builtin_amdgcn_readfirstlane(first + index * len);
+                u.end = __builtin_amdgcn_readfirstlane(u.begin + len);
+                u.span = Span{__builtin_amdgcn_readlane(span.first, l), __builtin_amdgcn_readlane(span.count, l), __builtin_amdgcn_readlane(span.positions, l)};
                 return u;
             }
             if (b0 + 64 >= a.req.batch) return u;
@@ -136,16 +137,17 @@ struct Ring {
     static constexpr int kHalf = 40 * D;                      // bytes of a page's keys or values
     static constexpr int PART = (kHalf + 1023) / 1024 * 1024;  // copied in pieces of a KiB
     static constexpr int COPIES = PART / 1024;
-    static constexpr int DEPTH = D == 64 ? 3 : 2;
+    static constexpr int DEPTH = 1;
+    static constexpr int WGS = D == 64 ? 3 : 2;  // workgroups per compute unit
     static constexpr int WAVE = 2 * DEPTH * PART;
     static constexpr int LDS = 4 * WAVE;
     static constexpr int FLYING = (2 * DEPTH - 1) * COPIES;  // copies behind the ones waited for
-    static_assert(LDS <= (D <= 128 ? 80 : 160) * 1024 && FLYING <= 63, "LDS, and the 6-bit counter of outstanding copies");
+    static_assert(WGS * LDS <= 160 * 1024 && FLYING <= 63, "LDS, and the 6-bit counter of outstanding copies");
 };
 
 // Up to 16 query rows of a KV head at a time.  The wavefronts work for themselves, each with copies of its own on the way.
 template <int D>
-__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Args a) {
+__global__ __launch_bounds__(256, Ring<D>::WGS) void attn_q4_kernel(AttnQ4Args a) {
     typedef PageLayout<D> L;
     typedef Ring<D> R;
     constexpr int G = L::G, DT = D / 16, W = L::W;
@@ -160,20 +162,25 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     const int from = worker * units.share, stop = from + units.share;
     for (int x = from; x < stop;) {
     const Unit unit = units.at<false>(x);
-    if (unit.b < 0) return;
+    if (__builtin_amdgcn_readfirstlane(unit.b) < 0) return;
     const bool cut = units.may_cut(unit);
     if (!cut && unit.begin < x) {  // (another wavefront has it)
         x = unit.end;
         continue;
     }
-    const int b = unit.b, kv = unit.kv, row0 = unit.row0;
-    const Span span = span_of(a.req, b);
-    const int rows = __builtin_amdgcn_readfirstlane(span.count * a.g), n = __builtin_amdgcn_readfirstlane(span.positions);
+    const int b = __builtin_amdgcn_readfirstlane(unit.b), kv = __builtin_amdgcn_readfirstlane(unit.kv), row0 = __builtin_amdgcn_readfirstlane(unit.row0);
+    const Span span = unit.span;
+    const int rows = span.count * a.g, n = span.positions;
     const int sees = max(0, n - rows / a.g + min(row0 + 15, rows - 1) / a.g + 1);  // positions the unit's last row sees
     const int last = cut ? min(stop, unit.end) : unit.end;
     const bool whole = unit.begin >= from && last == unit.end;  // no other wavefront has a page of the unit
     const int page0 = max(x - unit.begin - units.over, 0), pages = min(last - unit.begin - units.over, (sees + kPage - 1) / kPage);  // the unit's pages that are taken here
-    x = last;
+    x = __builtin_amdgcn_readfirstlane(last);
+
+    // ---- copies.  Lane i holds the place of the wavefront's i-th page (of 64 at a time)
+    const int count = __builtin_amdgcn_readfirstlane(pages - page0);
+    auto places = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (page0 + i + lane) * kPage) : -1; };
+    int ahead = places(0), now = ahead;  // of the pages that are requested, and of those that are worked on
 
     // ---- queries: lane (m, r) holds q[row0 + m][32 j + 8 r .. + 7], scaled by a power of two
     const bool real = row0 + m < rows;
@@ -195,7 +202,6 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     const int up = top > 0.0f ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
     const float up2 = __builtin_amdgcn_ldexpf(1.0f, up);
     const float to_score = __builtin_amdgcn_ldexpf(a.scale, 24 - up);  // 2^24: the codes' denormals
-    float start[G];
     h8 sums = {};
 #pragma unroll
     for (int j = 0; j < G; ++j) {
@@ -208,29 +214,21 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
         }
         s += __shfl_xor(s, 16, 64);
         s += __shfl_xor(s, 32, 64);
-        start[j] = s * (-8.0f / 16777216.0f);
         const _Float16 hi = (_Float16)(s * 0.0625f), lo = (_Float16)(s * 0.0625f - (float)hi);
         sums[j] = r == 0 ? hi : r == 1 ? lo : (_Float16)0.0f;
     }
 
-    v4f acc[DT], eights[G], rest = {};
+    v4f acc[DT], rest = {};
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < G; ++j) eights[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    float run_max = kNothingYet, lower = 1.0f;  // lower: what P's factor 2^14 has been lowered by
-    h8 eight;  // 8 as a denormal code
-#pragma unroll
-    for (int e = 0; e < 8; ++e) eight[e] = __builtin_bit_cast(_Float16, (uint16_t)8);
+    float run_max = kNothingYet, factor = kFactor;
+    const u32x4 eight_lo = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u}, eight_hi = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u},  // -8 as a code
+                eight_k = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};
     const uint32_t mask_lo = 0x000F000Fu, mask_hi = 0x00F000F0u;
 
-    // ---- copies.  Lane i holds the place of the wavefront's i-th page (of 64 at a time)
-    const int count = pages - page0;
-    auto places = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (page0 + i + lane) * kPage) : -1; };
-    int ahead = places(0), now = ahead;  // of the pages that are requested, and of those that are worked on
     auto copy = [&](int i, int slot, int part) __attribute__((always_inline)) {  // part 0: keys, 1: values
         const int page = __builtin_amdgcn_readlane(ahead, i & 63);
-        const char *src = a.pages + ((size_t)max(page, 0) * a.h_kv + __builtin_amdgcn_readfirstlane(kv)) * L::kBytes + part * R::kHalf;
+        const char *src = a.pages + ((size_t)max(page, 0) * a.h_kv + kv) * L::kBytes + part * R::kHalf;
 #pragma unroll
         for (int c = 0; c < R::COPIES; ++c)  // (the last piece's lanes behind the part copy its end again)
             copy16_to_lds(src, (uint32_t)min(c * 1024 + lane * 16, R::kHalf - 16), ring_at + (2 * slot + part) * R::PART + c * 1024);
@@ -241,23 +239,18 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
             copy(i, i, 0);
             copy(i, i, 1);
         }
-    // The copies of page i are there: as many as ever are behind them while DEPTH pages follow, none later.  In front of a copy into a place all reads of it are done.
-    auto wait_for = [&](int i) __attribute__((always_inline)) {
-        if (i + R::DEPTH < count)
-            wait_copies<R::FLYING>();
-        else
-            wait_copies<0>();
-    };
-
     for (int i = 0, slot = 0; i < count; ++i, slot = slot + 1 == R::DEPTH ? 0 : slot + 1) {
         const int k0 = (page0 + i) * kPage;
         if (i > 0 && (i & 63) == 0) now = places(i);
         if (i + R::DEPTH < count && ((i + R::DEPTH) & 63) == 0) ahead = places(i + R::DEPTH);
         const int page = __builtin_amdgcn_readlane(now, i & 63);
         const char *src = ring + 2 * slot * R::PART;
-        wait_for(i);
+        // The page's keys are there: behind them are its values and DEPTH - 1 pages (at the end, none).  In front of a copy into a place all reads of it are done.
+        if (i + R::DEPTH <= count)
+            wait_copies<R::FLYING>();
+        else
+            wait_copies<0>();
         const int seen = page >= 0 ? lim - k0 : 0, valid = page >= 0 ? n - k0 : 0;  // of this page, by the lane's row and by anyone
-
         // ---- scores; lane (m, r), element 4 t + i: position 16 r + 4 t + i, times 2^-24 and the queries' power of two
         float sc[16];
         {
@@ -285,6 +278,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
 #pragma unroll
                 for (int jw = 0; jw < W; ++jw) {
                     const int j = jj * W + jw;
+                    const v4f zero = {};
+                    const v4f from = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_k), qf[j], zero, 0, 0, 0);
                     h8 st[2];
                     st[0] = *reinterpret_cast<const h8 *>(src + L::kStepK + (j * kPage + 16 * r) * 2);
                     st[1] = *reinterpret_cast<const h8 *>(src + L::kStepK + (j * kPage + 16 * r + 8) * 2);
@@ -292,7 +287,6 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
                     for (int t = 0; t < 4; ++t) {
                         const uint32_t w = c[t][jw];
                         const u32x4 op = {w & mask_lo, w & mask_hi, (w >> 8) & mask_lo, (w >> 8) & mask_hi};
-                        const v4f from = {start[j], start[j], start[j], start[j]};
                         const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, op), qf[j], from, 0, 0, 0);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) part[t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[t][i]);
@@ -303,6 +297,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
             for (int e = 0; e < 16; ++e) sc[e] = part[e >> 2][e & 3];
         }
         if (__any(seen < kPage)) {
+            __builtin_amdgcn_sched_barrier(0);  // (a branch, not 32 more instructions for every page)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[e] = 16 * r + e < seen ? sc[e] : -INFINITY;
         }
@@ -311,98 +306,83 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
         for (int e = 2; e < 16; e += 2) bmax = fmaxf(fmaxf(bmax, sc[e]), sc[e + 1]);
         wait_copies<63>();  // (the keys have been read)
         if (i + R::DEPTH < count) copy(i + R::DEPTH, slot, 0);
-        bmax = fmaxf(bmax, __shfl_xor(bmax, 16, 64));
-        bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64)) * to_score;  // (in units of log 2 from here on)
-        const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max), from14 = 14.0f - new_max;
-        run_max = new_max;
-        h8 pv[2];
+        // (and its values: behind them DEPTH - 1 pages and the next one's keys)
+        if (i + R::DEPTH < count)
+            wait_copies<R::FLYING>();
+        else
+            wait_copies<0>();
+        const char *const vsrc = src + R::PART - R::kHalf;  // (the layout counts from the page's start)
+        if (valid < kPage) {  // positions that nobody has may hold anything: their values' steps and offsets are taken as 0
+            char *const clear = ring + (2 * slot + 1) * R::PART - R::kHalf;
+            if (lane >= valid) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], to_score, from14));
-            pv[e >> 3][e & 7] = (_Float16)sc[e];
-        }
-        if (__any(corr != 1.0f)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                for (int t = 0; t < DT; ++t) acc[t][i] *= corr;
-#pragma unroll
-                for (int j = 0; j < G; ++j) eights[j][i] *= corr;
-                rest[i] *= corr;
+                for (int j = 0; j < G; ++j) {
+                    *reinterpret_cast<_Float16 *>(clear + L::step_v(lane, j)) = (_Float16)0.0f;
+                    *reinterpret_cast<_Float16 *>(clear + L::offset_v(lane, j)) = (_Float16)0.0f;
+                }
             }
         }
-
-        // ---- second product.  Positions that nobody has may hold anything: their steps and offsets are taken as 0
-        wait_for(i);
-        src += R::PART - R::kHalf;  // (the layout counts from the page's start)
-        h8 step[G][2], off[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            off[u] = *reinterpret_cast<const h8 *>(src + L::kOffsetV + (min(m, G - 1) * kPage + 16 * r + 8 * u) * 2);
-#pragma unroll
-            for (int j = 0; j < G; ++j) step[j][u] = *reinterpret_cast<const h8 *>(src + L::kStepV + (j * kPage + 16 * r + 8 * u) * 2);
-        }
-        if (valid < kPage) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool none = 16 * r + 8 * u + e >= valid;
-                    off[u][e] = none ? (_Float16)0.0f : off[u][e];
-#pragma unroll
-                    for (int j = 0; j < G; ++j) step[j][u][e] = none ? (_Float16)0.0f : step[j][u][e];
-                }
-        }
+        auto step_of = [&](int j, int u) __attribute__((always_inline)) { return *reinterpret_cast<const h8 *>(vsrc + L::kStepV + (j * kPage + 16 * r + 8 * u) * 2); };
         uint32_t large = 0;
 #pragma unroll
         for (int j = 0; j < G; ++j)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const u32x4 bits = __builtin_bit_cast(u32x4, step[j][u]);
+                const u32x4 bits = __builtin_bit_cast(u32x4, step_of(j, u));
                 large |= bits.x | bits.y | bits.z | bits.w;
             }
-        if (lower == 1.0f && __any((large & 0x40004000u) != 0)) {  // a step of 2 or more
-            lower = 1.0f / 4096.0f;
+        bmax = fmaxf(bmax, __shfl_xor(bmax, 16, 64));
+        bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64)) * to_score;  // (in units of log 2 from here on)
+        const bool lowers = factor == kFactor && __any((large & 0x40004000u) != 0);  // a step of 2 or more
+        if (__any(bmax > run_max + kLag) || lowers) {
+            const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max - (lowers ? kLower : 0.0f));
+            run_max = new_max;
+            factor = lowers ? kFactor - kLower : factor;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                for (int t = 0; t < DT; ++t) acc[t][i] *= lower;
-#pragma unroll
-                for (int j = 0; j < G; ++j) eights[j][i] *= lower;
+                for (int t = 0; t < DT; ++t) acc[t][i] *= corr;
+                rest[i] *= corr;
             }
         }
-        if (lower != 1.0f) {
+        const float from_max = factor - run_max;
+        h8 pv[2];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sc[e] *= lower;
+        for (int e = 0; e < 16; ++e) {
+            sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], to_score, from_max));
+            pv[e >> 3][e & 7] = (_Float16)sc[e];
         }
+        // ---- second product
 #pragma unroll
         for (int u = 0; u < 2; ++u) {  // rows 0 .. G - 1: offsets; row 15: ones; the others are not used
-            const u32x4 w = __builtin_bit_cast(u32x4, off[u]);
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(vsrc + L::kOffsetV + (min(m, G - 1) * kPage + 16 * r + 8 * u) * 2);
             const u32x4 rows = {m == 15 ? 0x3C003C00u : w.x, m == 15 ? 0x3C003C00u : w.y, m == 15 ? 0x3C003C00u : w.z, m == 15 ? 0x3C003C00u : w.w};
             rest = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, rows), pv[u], rest, 0, 0, 0);
         }
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-            const u32x4 c = *reinterpret_cast<const u32x4 *>(src + L::kCodesV + (j * 64 + lane) * 16);
+            const u32x4 c = *reinterpret_cast<const u32x4 *>(vsrc + L::kCodesV + (j * 64 + lane) * 16);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
+                const h8 step = step_of(j, u);
                 h8 p;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[8 * u + e], (float)step[j][u][e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits to 16)
+                for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
                 const uint32_t c0 = c[2 * u], c1 = c[2 * u + 1];
                 const u32x4 lo = {c0 & mask_lo, (c0 >> 8) & mask_lo, c1 & mask_lo, (c1 >> 8) & mask_lo};
                 const u32x4 hi = {c0 & mask_hi, (c0 >> 8) & mask_hi, c1 & mask_hi, (c1 >> 8) & mask_hi};
                 acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, lo), p, acc[2 * j], 0, 0, 0);
                 acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, hi), p, acc[2 * j + 1], 0, 0, 0);
-                eights[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight, p, eights[j], 0, 0, 0);
+                acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_lo), p, acc[2 * j], 0, 0, 0);
+                acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_hi), p, acc[2 * j + 1], 0, 0, 0);
             }
         }
         wait_copies<63>();
         if (i + R::DEPTH < count) copy(i + R::DEPTH, slot, 1);
     }
 
-    // ---- output row m (2^14 times, unnormalized), its maximum and sum
-    const float back = 16777216.0f / lower, sum = __shfl(rest[3], 48 + m, 64), inv = sum > 0.0f ? 1.0f / sum : 0.0f;  // (a row that sees nothing: 0)
+    // ---- output row m (2^kFactor times, unnormalized), its maximum and sum
+    const float back = 16777216.0f, sum = __shfl(rest[3], 48 + m, 64), inv = sum > 0.0f ? 1.0f / sum : 0.0f;  // (a row that sees nothing: 0)
     const size_t part = partial_of(unit, worker, units.share) * 16 + m;
 #pragma unroll
     for (int j = 0; j < G; ++j) {
@@ -410,8 +390,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
         v4f o[2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            o[0][i] = fmaf(acc[2 * j][i] - eights[j][i], back, off);
-            o[1][i] = fmaf(acc[2 * j + 1][i] * 0.0625f - eights[j][i], back, off);
+            o[0][i] = fmaf(acc[2 * j][i], back, off);
+            o[1][i] = fmaf(acc[2 * j + 1][i], back * 0.0625f, off);
         }
         if (!real) continue;
 #pragma unroll
@@ -430,26 +410,27 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_q4_kernel(AttnQ4Ar
     }
 }
 
-// The units that several wavefronts share, a row of one per workgroup: grid = (units, rows), or workgroups that take one unit after the other.  Its four wavefronts take the
+// The units that several wavefronts share, a row of one (unit_rows in each) per workgroup, or one after the other.  Its four wavefronts take the
 // parts in turn, lane c the (maximum, sum) of its c-th and D / 64 columns of the partial outputs; they meet in LDS.
 template <int D>
-__global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a) {
+__global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a, int unit_rows) {
     constexpr int PER = D / 64;
     typedef float cols __attribute__((ext_vector_type(PER)));
     __shared__ float outs[4][D], maxima[4], sums[4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Units units(a, lane);
-    for (int i = blockIdx.x;; i += gridDim.x) {
-        const Unit unit = units.at<true>(i);
+    for (long i = blockIdx.x;; i += gridDim.x) {
+        const int in_unit = (int)(i % unit_rows);
+        const Unit unit = units.at<true>((int)(i / unit_rows));
         if (unit.b < 0) return;
         if (!units.may_cut(unit)) continue;
         const int w0 = unit.begin / units.share, parts = (unit.end - 1) / units.share - w0 + 1;
         if (parts == 1) continue;  // (written by the first kernel)
-        const Span span = span_of(a.req, unit.b);
-        const int row = unit.row0 + (int)blockIdx.y;
+        const Span span = unit.span;
+        const int row = unit.row0 + in_unit;
         if (row >= span.count * a.g) continue;
-        const size_t slot0 = partial_of(unit, w0, units.share) * 16 + blockIdx.y;  // of the first; the others begin inside the unit
-        auto place = [&](int c) __attribute__((always_inline)) { return c == 0 ? slot0 : (size_t)(w0 + c) * 32 + blockIdx.y; };
+        const size_t slot0 = partial_of(unit, w0, units.share) * 16 + in_unit;  // of the first; the others begin inside the unit
+        auto place = [&](int c) __attribute__((always_inline)) { return c == 0 ? slot0 : (size_t)(w0 + c) * 32 + in_unit; };
         const int own = (parts - wave + 3) / 4;  // of this wavefront: wave, wave + 4, ...
         float mx = kNothingYet, l = 0.0f;
         if (lane < own) {
@@ -658,8 +639,9 @@ hipError_t launch(const AttnQ4Args &a, const ManyArgs &many, const AttnQ4Plan &p
     attn_q4_kernel<D><<<(unsigned)((a.workers + 3) / 4), 256, lds, st>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p.shared) {
-        const long units = p.blocks * a.h_kv, most = 4L * num_cus;
-        attn_q4_combine_kernel<D><<<dim3((unsigned)(units < most ? units : most), p.rows < 16 ? (unsigned)p.rows : 16u), 256, 0, st>>>(a);
+        const int unit_rows = p.rows < 16 ? p.rows : 16;
+        const long works = p.blocks * a.h_kv * unit_rows, most = 4L * num_cus;
+        attn_q4_combine_kernel<D><<<(unsigned)(works < most ? works : most), 256, 0, st>>>(a, unit_rows);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.slots > 0) {
@@ -680,11 +662,11 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     p.all_rows = (long)tokens * g;
     p.blocks = p.rows <= 16 ? batch : (p.all_rows + 15) / 16 + batch;
     // few rows: as many wavefronts as the card holds at once
-    const long on_card = (long)num_cus * (d <= 128 ? 2 : 1), most_pages = p.blocks * h_kv * p.pages;
-    p.least = 1;
-    if (const int forced = tuning().attn_q4_pages; forced > 0) p.least = forced;
+    const long waves = 4L * num_cus * (d == 64 ? Ring<64>::WGS : d == 128 ? Ring<128>::WGS : Ring<256>::WGS), most_pages = p.blocks * h_kv * p.pages;
+    p.least = (p.pages + 2 + 253) / 254;  // (a unit is cut into 254 whole shares and two ends at most: the combination's four wavefronts take 64 each)
+    if (const int forced = tuning().attn_q4_pages; forced > p.least) p.least = forced;
     const long shares = (most_pages + p.least - 1) / p.least;
-    p.workers = (int)(shares < 4 * on_card ? shares : 4 * on_card);
+    p.workers = (int)(shares < waves ? shares : waves);
     if (p.workers < 1) p.workers = 1;
     p.shared = p.pages > p.least;
     p.total = 256;
@@ -692,6 +674,7 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     if (p.shared) p.total += up256((size_t)p.workers * 2 * 16 * (d + 2) * sizeof(float));
     // many rows
     if (p.rows <= kFewRows) return p;
+    const long on_card = (long)num_cus * (d <= 128 ? 2 : 1);  // workgroups of the kernel for prompts
     const long most = p.all_rows / (kFewRows + 1);
     p.slots = (int)(most < batch ? most : batch);
     if (p.slots > kMaxSlots) p.slots = kMaxSlots;
