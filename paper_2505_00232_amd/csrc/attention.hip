@@ -1203,6 +1203,15 @@ hipError_t launch_attention(const void *q, const void *kc, const void *vc, int G
     }
 }
 
+// The plan for requests of up to S tokens and n_ctx positions, `groups` times a KV head: wavefronts that share a walk (returned), steps of a chunk (0: walks are whole).
+int plan_attention_many(int groups, int S, int g, int d, int n_ctx, int num_cus, int *chunk_steps) {
+    AttnArgs a = {};
+    a.M = S * g, a.g = g, a.S = S, a.n_ctx = n_ctx < S ? S : n_ctx, a.groups = groups;
+    const int shares = plan_prefill(a, d, num_cus);
+    *chunk_steps = a.chunk_steps;
+    return shares;
+}
+
 // The prompts of a batch of requests over binary16 copies of their caches (attention_q4.hip); shares: wavefronts that share a walk.
 hipError_t launch_attention_many(const void *q, const void *kc, const void *vc, int h_q, int h_kv, int d, int C, const int *plan, int records, int shares, int items,
                                  long rows, float *partial, void *out, hipStream_t st) {

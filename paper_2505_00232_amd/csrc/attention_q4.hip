@@ -30,6 +30,8 @@ constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no po
 constexpr int kFewRows = 256;
 constexpr int kMaxSlots = 256;  // requests of many rows at most, the others go through the blocks of 16
 
+constexpr int kWhole = 4;
+
 struct AttnQ4Args {
     const _Float16 *q;  // [tokens, h_q, D]
     _Float16 *out;
@@ -37,13 +39,13 @@ struct AttnQ4Args {
     Requests req;
     float *ws_o, *ws_ml;  // [workers, 2, 16, D] partial outputs, [.., 2] (maximum, sum)
     int *plan;            // ManyRows, or null
-    int h_q, h_kv, g, workers, least;
+    int h_q, h_kv, g, workers, least, whole;
     float scale;
 };
 
 // The work: units of a KV head and a block of 16 query rows of a request, one behind the other (a request's blocks, in each all heads), each with the request's
 // pages.  The pages are dealt to the wavefronts in equal shares (at least `least`), whatever the requests' lengths: each has one run of pages, across units.  A
-// unit is done by one wavefront where it is short (half a share, or `least`), by that in whose share it begins; of a longer one a wavefront does the pages of its share, and
+// unit is done by one wavefront where it is short (half a share, or, of small shares, kWhole pages: less work than a second launch), by that in whose share it begins; of a longer one a wavefront does the pages of its share, and
 // leaves partial results where others have the rest: two per wavefront at most, of the unit that its share begins inside of (or with), and of
 // the one that it ends inside of.  A unit's beginning costs about as much as two pages (its requests' arrays, queries and first page one after the other): where a share
 // is some pages, units are that much longer.
@@ -126,7 +128,7 @@ struct Units {
             sum();
         }
     }
-    __device__ __forceinline__ bool may_cut(const Unit &u) const { return u.end - u.begin > max(a.least + over, share / 2); }
+    __device__ __forceinline__ bool may_cut(const Unit &u) const { return u.end - u.begin - over > max(over ? share / 2 : kWhole, a.whole); }
 };
 // Place of the partial results that worker w leaves of a unit
 __device__ __forceinline__ size_t partial_of(const Unit &u, int w, int share) { return (size_t)w * 2 + (u.begin > w * share ? 1 : 0); }
@@ -297,7 +299,6 @@ __global__ __launch_bounds__(256, Ring<D>::WGS) void attn_q4_kernel(AttnQ4Args a
             for (int e = 0; e < 16; ++e) sc[e] = part[e >> 2][e & 3];
         }
         if (__any(seen < kPage)) {
-            __builtin_amdgcn_sched_barrier(0);  // (a branch, not 32 more instructions for every page)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[e] = 16 * r + e < seen ? sc[e] : -INFINITY;
         }
@@ -323,14 +324,14 @@ __global__ __launch_bounds__(256, Ring<D>::WGS) void attn_q4_kernel(AttnQ4Args a
             }
         }
         auto step_of = [&](int j, int u) __attribute__((always_inline)) { return *reinterpret_cast<const h8 *>(vsrc + L::kStepV + (j * kPage + 16 * r + 8 * u) * 2); };
-        uint32_t large = 0;
+        uint32_t large;  // some of the page's steps; all of them in the wavefront
+        {
+            typedef uint32_t words __attribute__((ext_vector_type(G / 2)));
+            const words w = *reinterpret_cast<const words *>(vsrc + L::kStepV + lane * (2 * G));
+            large = w[0];
 #pragma unroll
-        for (int j = 0; j < G; ++j)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const u32x4 bits = __builtin_bit_cast(u32x4, step_of(j, u));
-                large |= bits.x | bits.y | bits.z | bits.w;
-            }
+            for (int j = 1; j < G / 2; ++j) large |= w[j];
+        }
         bmax = fmaxf(bmax, __shfl_xor(bmax, 16, 64));
         bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64)) * to_score;  // (in units of log 2 from here on)
         const bool lowers = factor == kFactor && __any((large & 0x40004000u) != 0);  // a step of 2 or more
@@ -487,19 +488,15 @@ struct ManyArgs {
     int *plan;
     const char *pages;
     _Float16 *kc, *vc;  // [slots, h_kv, positions, D], [slots, h_kv, positions / 64, D, 64]
-    int g, h_kv, slots, records, block_rows, unit, items, target, max_pages;
+    int g, h_kv, slots, records, block_rows, chunk_steps, max_pages;
 };
 
-// One workgroup: the list of the requests with more than kFewRows rows.  A request with a missing page, or with fewer positions than tokens, is none of them: the kernel for few rows
-// takes it.  Walks (steps of 32 positions) are cut where that leaves `target` workgroups more even shares, into eight at most.
+// One workgroup: the list of the requests with more than kFewRows rows, and how many workgroups each takes (per block of rows one for a chunk of its steps).  A request with a missing
+// page, or with fewer positions than tokens, is none of them: the kernel for few rows takes it.
 __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
     __shared__ uint64_t wanted[4];
     __shared__ int rec[kMaxSlots][4], item[kMaxSlots];
-    __shared__ int longest, total_items;
-    __shared__ unsigned long long total_steps;  // twice, about
     const int tid = threadIdx.x;
-    if (tid == 0) longest = 0, total_steps = 0;
-    __syncthreads();
     int count = 0;  // (the same in every thread)
     for (int b0 = 0; b0 < a.req.batch; b0 += 256) {
         const int b = b0 + tid;
@@ -533,55 +530,35 @@ __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
         const int S = rec[slot][1], last = min((j + 1) * a.block_rows, S * a.g) - 1;
         return (rec[slot][2] - S + last / a.g + 1 + 31) / 32;
     };
-    const int blocks = tid < count ? (rec[tid][1] * a.g + a.block_rows - 1) / a.block_rows : 0;
     if (tid < count) {
-        atomicMax(&longest, steps(tid, blocks - 1));
-        atomicAdd(&total_steps, (unsigned long long)blocks * (unsigned)(steps(tid, 0) + steps(tid, blocks - 1)));
+        const int blocks = (rec[tid][1] * a.g + a.block_rows - 1) / a.block_rows;
+        int n = blocks;
+        if (a.chunk_steps > 0) {
+            n = 0;
+            for (int j = 0; j < blocks; ++j) n += (steps(tid, j) + a.chunk_steps - 1) / a.chunk_steps;
+        }
+        item[tid] = n;
     }
     __syncthreads();
-    int len = 0;
-    if (a.target > 0) {
-        len = (int)(total_steps * a.h_kv / (2ull * a.target)) + 1;
-        len = max(max(len, (longest + kPrefillMaxChunks - 1) / kPrefillMaxChunks), 16);
-        len = (len + a.unit - 1) / a.unit * a.unit;
-        if (len >= longest) len = 0;
-    }
-    for (int attempt = 0; attempt < 2; ++attempt) {
-        if (tid < count) {
-            int n = blocks;
-            if (len > 0) {
-                n = 0;
-                for (int j = 0; j < blocks; ++j) n += (steps(tid, j) + len - 1) / len;
-            }
-            item[tid] = n;
+    if (tid == 0) {
+        int sum = 0;
+        for (int i = 0; i < count; ++i) {
+            const int n = item[i];
+            item[i] = sum;
+            sum += n;
         }
-        __syncthreads();
-        if (tid == 0) {
-            int sum = 0;
-            for (int i = 0; i < count; ++i) {
-                const int n = item[i];
-                item[i] = sum;
-                sum += n;
-            }
-            total_items = sum;
-        }
-        __syncthreads();
-        if (total_items <= a.items || len == 0) break;
-        len = 0;
-        __syncthreads();
+        a.plan[ManyRows::kCount] = count;
+        a.plan[ManyRows::kItems] = sum;
     }
+    __syncthreads();
     if (tid < count) {
         int *r = a.plan + a.records + tid * ManyRows::kRecord;
         r[ManyRows::kRow] = rec[tid][0];
         r[ManyRows::kTokens] = rec[tid][1];
         r[ManyRows::kPositions] = rec[tid][2];
         r[ManyRows::kItem] = item[tid];
-        r[ManyRows::kChunkSteps] = len;
+        r[ManyRows::kChunkSteps] = a.chunk_steps;
         r[ManyRows::kRequest] = rec[tid][3];
-    }
-    if (tid == 0) {
-        a.plan[ManyRows::kCount] = count;
-        a.plan[ManyRows::kItems] = total_items;
     }
 }
 
@@ -668,29 +645,28 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     const long shares = (most_pages + p.least - 1) / p.least;
     p.workers = (int)(shares < waves ? shares : waves);
     if (p.workers < 1) p.workers = 1;
-    p.shared = p.pages > p.least;
+    p.shared = p.pages > kWhole;
     p.total = 256;
     p.partial = 0;
     if (p.shared) p.total += up256((size_t)p.workers * 2 * 16 * (d + 2) * sizeof(float));
     // many rows
     if (p.rows <= kFewRows) return p;
-    const long on_card = (long)num_cus * (d <= 128 ? 2 : 1);  // workgroups of the kernel for prompts
     const long most = p.all_rows / (kFewRows + 1);
     p.slots = (int)(most < batch ? most : batch);
     if (p.slots > kMaxSlots) p.slots = kMaxSlots;
     if (p.slots == 0) return p;
-    p.shares = p.all_rows * h_kv / 128 >= 2 * on_card ? 1 : 2;
-    const int block_rows = 128 / p.shares;
-    const long blocks = p.all_rows / block_rows + p.slots;
-    p.cut = p.all_rows * h_kv / block_rows < 2 * on_card;
-    p.items = (int)(p.cut ? 2 * blocks + on_card / h_kv + 1 : blocks);
+    // (as for equal requests of the most tokens and positions, as many as make up the rows)
+    const long alike = (p.all_rows + p.rows / 2) / p.rows;
+    p.shares = plan_attention_many((int)((alike < 1 ? 1 : alike) * h_kv), max_tokens, g, d, max_context, num_cus, &p.chunk_steps);
+    const int steps = (max_context + 31) / 32, chunks = p.chunk_steps > 0 ? (steps + p.chunk_steps - 1) / p.chunk_steps : 1;
+    p.items = (int)((p.all_rows / (128 / p.shares) + p.slots) * chunks);
     p.records = (ManyRows::kSlots + batch + 7) / 8 * 8;
     p.plan = p.total;
     p.total += up256((size_t)(p.records + p.slots * ManyRows::kRecord) * sizeof(int));
     p.copies = p.total;
     p.total += up256((size_t)p.slots * h_kv * p.pages * kPage * d * 2 * 2);
     p.many_partial = p.total;
-    if (p.cut) p.total += up256((size_t)kPrefillMaxChunks * h_kv * p.all_rows * (d + 2) * sizeof(float));
+    if (p.chunk_steps > 0) p.total += up256((size_t)kPrefillMaxChunks * h_kv * p.all_rows * (d + 2) * sizeof(float));
     return p;
 }
 
@@ -703,7 +679,7 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
     a.pages = static_cast<const char *>(pages);
     a.req = req;
     a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv;
-    a.workers = p.workers, a.least = p.least;
+    a.workers = p.workers, a.least = p.least, a.whole = p.shared ? 0 : kWhole;  // (no second launch: nothing is cut)
     a.ws_o = reinterpret_cast<float *>(ws + p.partial);
     a.ws_ml = a.ws_o + (size_t)p.workers * 2 * 16 * d;
     a.scale = 1.4426950408889634f / sqrtf((float)d);
@@ -717,8 +693,7 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
         many.plan = a.plan;
         many.pages = a.pages;
         many.kc = kc, many.vc = vc;
-        many.g = a.g, many.h_kv = h_kv, many.slots = p.slots, many.records = p.records, many.block_rows = 128 / p.shares, many.unit = p.shares, many.items = p.items;
-        many.target = p.cut ? num_cus * (d <= 128 ? 2 : 1) : 0;
+        many.g = a.g, many.h_kv = h_kv, many.slots = p.slots, many.records = p.records, many.block_rows = 128 / p.shares, many.chunk_steps = p.chunk_steps;
         many.max_pages = p.pages;
     }
     hipError_t e = hipErrorInvalidValue;
@@ -729,7 +704,7 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
     }
     if (e != hipSuccess || p.slots == 0) return e;
     return launch_attention_many(q, kc, vc, h_q, h_kv, d, p.pages * kPage, a.plan, p.records, p.shares, p.items, p.all_rows,
-                                 p.cut ? reinterpret_cast<float *>(ws + p.many_partial) : nullptr, out, st);
+                                 p.chunk_steps > 0 ? reinterpret_cast<float *>(ws + p.many_partial) : nullptr, out, st);
 }
 
 }  // namespace qfc

@@ -406,7 +406,7 @@ struct AttnQ4Plan {
     int slots;        // at most so many
     int shares;       // wavefronts that share a walk
     int items;        // workgroups per KV head at most
-    bool cut;         // walks may be cut into chunks
+    int chunk_steps;  // steps of 32 positions of the chunks walks are cut into (0: whole)
     long all_rows;    // query rows of a KV head of all requests
     // bytes from the workspace's start
     size_t partial, plan, copies, many_partial, total;
@@ -416,6 +416,7 @@ struct AttnQ4Plan {
 AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int max_tokens, int max_context, int num_cus);
 hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out, int num_cus,
                                hipStream_t st);
+int plan_attention_many(int groups, int S, int g, int d, int n_ctx, int num_cus, int *chunk_steps);
 hipError_t launch_attention_many(const void *q, const void *kc, const void *vc, int h_q, int h_kv, int d, int C, const int *plan, int records, int shares, int items,
                                  long rows, float *partial, void *out, hipStream_t st);
 struct AdapterPlan {
