@@ -1,9 +1,11 @@
 // Low-rank adapters of many requests beside a shared layer: out[m] = fp16(y[m] + scale[a] B[a] (A[a] x[m])), a = ids[m].
 //
-// Two kernels over blocks of 16 rows.  The first multiplies a block's rows with the A of every adapter that occurs among them (v_mfma_f32_16x16x32_f16; an
-// adapter's result is kept for its own rows only, so that nothing of one adapter, infinities included, reaches another one's rows) and leaves
-// the sums over a part of K in the workspace; the second adds the parts up, multiplies with B and adds the shared layer's output.
-// The low-rank values are rounded to binary16 between the two (relative to their row's largest: 2^-12 of what the adapter adds).
+// Two kernels.  The first multiplies blocks of 16 rows with the A of every adapter that occurs among them (v_mfma_f32_16x16x32_f16) and leaves
+// the sums over a part of K in the workspace, in 32 bits; the second adds the parts up, multiplies with B and adds the shared layer's output.  An adapter's results are kept for its
+// own rows only, so that nothing of one adapter, infinities included, reaches another one's rows.  Where every row has an adapter of its own (a decode step), the adapters of a
+// block of rows are dealt to several workgroups.
+// The low-rank values are rounded to binary16 between the two, scaled by a power of two to their row's largest (2^-11 of a value, 2^-25 of the largest), for the matrix product;
+// the output is rounded once.  Bound: memory (A and B of the adapters in use, x, y and out), for few rows the latency of two launches.
 #include "qfc_internal.h"
 
 namespace qfc {
@@ -16,55 +18,71 @@ struct AdapterArgs {
     const _Float16 *x, *a, *b, *y;  // [M, K], [count, rank, K], [count, N, rank], [M, N]
     const float *scale;             // [count]
     const int *ids;                 // [M]
-    float *low;                     // [parts, 16 blocks, rank]
+    float *low;                     // [parts, rows, rank]
     _Float16 *out;
-    int M, K, N, rank, count, parts, part_k, rows;  // rows: M rounded up to 16
+    int M, K, N, rank, count, parts, part_k, rows, dealt, tiles;  // rows: M rounded up; dealt: workgroups that share a block's adapters; tiles: of 32 columns per wavefront
 };
 
-// Smallest id above `last` among the 16 rows of a block (id in lane m of each quarter), INT32_MAX if there is none
-__device__ __forceinline__ int next_id(int id, int last) {
-    int next = id > last ? id : INT32_MAX;
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) next = min(next, __shfl_xor(next, off, 64));
-    return __builtin_amdgcn_readfirstlane(next);
-}
-__device__ __forceinline__ int row_id(const AdapterArgs &a, int row) {
-    const int id = row < a.M ? a.ids[row] : -1;
+// Adapter of row row0 + lane of a block of ROWS, -1 for none
+template <int ROWS>
+__device__ __forceinline__ int row_id(const AdapterArgs &a, int row0, int lane) {
+    const int id = lane < ROWS && row0 + lane < a.M ? a.ids[row0 + lane] : -1;
     return id >= 0 && id < a.count ? id : -1;
 }
+// f(adapter, its rows' bits) for the adapters of the block that are this workgroup's, in the order of their first rows
+template <class F>
+__device__ __forceinline__ void for_adapters(int id, int mine, int dealt, const F &f) {
+    uint64_t left = __ballot(id >= 0);
+    for (int k = 0; left; ++k) {
+        const int one = __builtin_amdgcn_readlane(id, __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)left) - 1));
+        const uint64_t rows = __ballot(id == one);
+        left &= ~rows;
+        if (k % dealt == mine) f(one, rows);
+    }
+}
 
-// grid = (blocks of 16 rows, parts of K); the four wavefronts of a workgroup take the part's pieces of 32 k in turn.  RT: tiles of 16 low-rank values.
+// grid = (blocks of 16 rows, parts of K, workgroups that share a block's adapters); the four wavefronts of a workgroup take the part's pieces of 32 k in turn.  RT: tiles of 16
+// low-rank values.
 template <int RT>
 __global__ __launch_bounds__(256) void adapters_shrink_kernel(AdapterArgs a) {
     __shared__ float sums[4][RT][64][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, r = lane >> 4;
+    constexpr int U = RT <= 2 ? 4 : RT == 4 ? 2 : 1;  // pieces on their way at once
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, r = lane >> 4;
     const int row0 = (int)blockIdx.x * 16, k0 = (int)blockIdx.y * a.part_k, k1 = min(k0 + a.part_k, a.K);
-    const int id = row_id(a, row0 + m);
-    int ids4[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) ids4[i] = __shfl(id, 4 * r + i, 64);
+    const int id = row_id<16>(a, row0, lane);
     const _Float16 *x = a.x + (size_t)min(row0 + m, a.M - 1) * a.K + 8 * r;
     v4f kept[RT];
+    uint64_t done = 0;
 #pragma unroll
     for (int t = 0; t < RT; ++t) kept[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int one = next_id(id, -1); one != INT32_MAX; one = next_id(id, one)) {
+    for_adapters(id, blockIdx.z, a.dealt, [&](int one, uint64_t rows) __attribute__((always_inline)) {
+        done |= rows;
+        const _Float16 *w = a.a + (size_t)one * a.rank * a.K + (size_t)m * a.K + 8 * r;
         v4f acc[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int k = k0 + 32 * wave; k < k1; k += 128) {
-            const h8 xv = *reinterpret_cast<const h8 *>(x + k);
+        for (int k = k0 + 32 * wave; k < k1; k += 128 * U) {
+            h8 xv[U], wv[U][RT];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                h8 w = {};
-                if (16 * t + m < a.rank) w = *reinterpret_cast<const h8 *>(a.a + ((size_t)one * a.rank + 16 * t + m) * a.K + k + 8 * r);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv, w, acc[t], 0, 0, 0);
+            for (int u = 0; u < U; ++u) {
+                const h8 zero = {};
+                const bool there = k + 128 * u < k1;
+                xv[u] = there ? *reinterpret_cast<const h8 *>(x + k + 128 * u) : zero;
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+                    wv[u][t] = there && 16 * t + m < a.rank ? *reinterpret_cast<const h8 *>(w + (size_t)16 * t * a.K + k + 128 * u) : zero;
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(xv[u], wv[u][t], acc[t], 0, 0, 0);
         }
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) kept[t][i] = ids4[i] == one ? acc[t][i] : kept[t][i];
-    }
+            for (int i = 0; i < 4; ++i) kept[t][i] = rows >> (4 * r + i) & 1 ? acc[t][i] : kept[t][i];
+    });
+    if (!done) return;  // (the same in all four wavefronts)
 #pragma unroll
     for (int t = 0; t < RT; ++t) *reinterpret_cast<v4f *>(sums[wave][t][lane]) = kept[t];
     __syncthreads();
@@ -74,106 +92,180 @@ __global__ __launch_bounds__(256) void adapters_shrink_kernel(AdapterArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float v = (sums[0][t][lane][i] + sums[1][t][lane][i]) + (sums[2][t][lane][i] + sums[3][t][lane][i]);
-            a.low[((size_t)blockIdx.y * a.rows + row0 + 4 * r + i) * a.rank + 16 * t + m] = v;
+            if (done >> (4 * r + i) & 1) a.low[((size_t)blockIdx.y * a.rows + row0 + 4 * r + i) * a.rank + 16 * t + m] = v;
         }
     }
 }
 
-// grid = (blocks of 16 rows, pieces of 128 columns): a wavefront takes 32 columns.  The low-rank values are the second operand (rows as columns of the result), so that a lane
+// grid = (blocks of 16 MT rows, pieces of 128 `tiles` columns, workgroups that share a block's adapters).  The workgroup adds up its rows' low-rank values once, into LDS; then a
+// wavefront takes 32 columns at a time, each of B's tiles for all of the block's rows.  The low-rank values are the second operand (rows as columns of the result), so that a lane
 // ends up with 8 consecutive columns of a row: row i of tile t of B is column 8 (i / 4) + 4 t + i % 4.  KT: steps of 32 low-rank values.
-template <int KT>
+template <int KT, int MT>
 __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, r = lane >> 4;
-    const int row = (int)blockIdx.x * 16 + m, n0 = ((int)blockIdx.y * 4 + wave) * 32;
-    if (n0 >= a.N) return;
-    const int id = row_id(a, row);
-    // lane (m, r): low-rank values 32 t + 8 r .. + 7 of its row, the row's largest scaled to 2^13 .. 2^14
-    float low[KT][8], top = 0.0f;
+    constexpr int ROWS = 16 * MT, PITCH = 32 * KT + 8;
+    __shared__ _Float16 low[ROWS][PITCH];
+    __shared__ uint32_t top[ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, r = lane >> 4;
+    const int row0 = (int)blockIdx.x * ROWS;
+    const int id = row_id<ROWS>(a, row0, lane);
+    uint64_t own = 0;
+    for_adapters(id, blockIdx.z, a.dealt, [&](int, uint64_t rows) __attribute__((always_inline)) { own |= rows; });
+    // rows without an adapter: the first of the workgroups copies them
+    const uint64_t plain = blockIdx.z == 0 ? __ballot(id < 0 && lane < ROWS && row0 + lane < a.M) : 0;
+    if (!(own | plain)) return;
+
+    if (own) {
+        constexpr int MOST = ROWS * KT * 4 / 256 > 0 ? ROWS * KT * 4 / 256 : 1;  // octets per thread
+        const int octets = a.rank / 8;
+        float v[MOST][8];
+        if (threadIdx.x < ROWS) top[threadIdx.x] = 0;
+        __syncthreads();
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+        for (int q = 0; q < MOST; ++q) {
+            const int e = threadIdx.x + 256 * q, row = e / octets, o = e % octets;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) low[t][e] = 0.0f;
-    for (int p = 0; p < a.parts; ++p) {
-        const float *src = a.low + ((size_t)p * a.rows + row) * a.rank;
+            for (int i = 0; i < 8; ++i) v[q][i] = 0.0f;
+            if (row < ROWS && (own >> row & 1)) {
+                const float *src = a.low + (size_t)(row0 + row) * a.rank + 8 * o;
+                for (int p = 0; p < a.parts; ++p) {
+                    const v4f l0 = *reinterpret_cast<const v4f *>(src + (size_t)p * a.rows * a.rank), l1 = *reinterpret_cast<const v4f *>(src + (size_t)p * a.rows * a.rank + 4);
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
-            if (32 * t + 8 * r < a.rank) {
-                const v4f l0 = *reinterpret_cast<const v4f *>(src + 32 * t + 8 * r), l1 = *reinterpret_cast<const v4f *>(src + 32 * t + 8 * r + 4);
+                    for (int i = 0; i < 4; ++i) {
+                        v[q][i] += l0[i];
+                        v[q][4 + i] += l1[i];
+                    }
+                }
+                float big = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    low[t][e] += l0[e];
-                    low[t][4 + e] += l1[e];
+                for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(v[q][i]));
+                atomicMax(&top[row], __float_as_uint(big));  // (a maximum: whatever the order)
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < MOST; ++q) {
+            const int e = threadIdx.x + 256 * q, row = e / octets, o = e % octets;
+            if (row >= ROWS) continue;
+            const float big = __uint_as_float(top[row]);
+            const int up = big > 0.0f && big < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(big) : 0;  // the row's largest to 2^13 .. 2^14
+            h8 x;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (_Float16)__builtin_amdgcn_ldexpf(v[q][i], up);
+            *reinterpret_cast<h8 *>(&low[row][8 * o]) = x;
+        }
+        for (int e = threadIdx.x; e < ROWS * (4 * KT - octets); e += 256) {
+            const h8 zero = {};
+            *reinterpret_cast<h8 *>(&low[e / (4 * KT - octets)][8 * (octets + e % (4 * KT - octets))]) = zero;
+        }
+        __syncthreads();
+    }
+    h8 v[MT][KT];
+    float back[MT];  // the scale and the power of two taken back
+    bool real[MT], has[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int row = 16 * t + m;
+        has[t] = own >> row & 1;
+        real[t] = (own | plain) >> row & 1;
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+            const h8 zero = {};
+            v[t][k] = own ? *reinterpret_cast<const h8 *>(&low[row][32 * k + 8 * r]) : zero;
+        }
+        const float big = own ? __uint_as_float(top[row]) : 0.0f;
+        const int up = big > 0.0f && big < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(big) : 0;
+        const int of_row = __shfl(id, row, 64);
+        back[t] = has[t] ? __builtin_amdgcn_ldexpf(a.scale[of_row], -up) : 0.0f;
+    }
+    for (int c = 0; c < a.tiles; ++c) {
+        const int n0 = (((int)blockIdx.y * a.tiles + c) * 4 + wave) * 32, n = n0 + 8 * r;
+        if (n0 >= a.N) return;
+        h8 y[MT];
+        if (a.N % 8 == 0 && n < a.N) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                if (real[t]) y[t] = *reinterpret_cast<const h8 *>(a.y + (size_t)(row0 + 16 * t + m) * a.N + n);
+        }
+        v4f kept[MT][2];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) kept[t][0] = kept[t][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        for_adapters(id, blockIdx.z, a.dealt, [&](int one, uint64_t rows) __attribute__((always_inline)) {
+            h8 w[2][KT];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int col = n0 + 8 * (m >> 2) + 4 * u + (m & 3);
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    const h8 zero = {};
+                    w[u][k] = col < a.N && 32 * k + 8 * r < a.rank ? *reinterpret_cast<const h8 *>(a.b + ((size_t)one * a.N + col) * a.rank + 32 * k + 8 * r) : zero;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                if (!(rows >> (16 * t) & 0xFFFF)) continue;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int k = 0; k < KT; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[u][k], v[t][k], acc, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) kept[t][u][i] = rows >> (16 * t + m) & 1 ? acc[i] : kept[t][u][i];
+                }
+            }
+        });
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            if (!real[t]) continue;
+            const size_t at = (size_t)(row0 + 16 * t + m) * a.N + n;
+            if (a.N % 8 == 0) {
+                if (n >= a.N) continue;
+                if (has[t]) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[t][e] = (_Float16)((float)y[t][e] + kept[t][e >> 2][e & 3] * back[t]);
+                }
+                *reinterpret_cast<h8 *>(a.out + at) = y[t];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (n + e >= a.N) break;
+                    const _Float16 old = a.y[at + e];
+                    a.out[at + e] = has[t] ? (_Float16)((float)old + kept[t][e >> 2][e & 3] * back[t]) : old;
                 }
             }
         }
     }
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(low[t][e]));
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const int up = top > 0.0f && top < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
-    h8 v[KT];
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[t][e] = (_Float16)__builtin_amdgcn_ldexpf(low[t][e], up);
-    const float scale = id >= 0 ? a.scale[id] : 0.0f;
+}
 
-    v4f kept[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}};
-    for (int one = next_id(id, -1); one != INT32_MAX; one = next_id(id, one)) {
-        const bool own = id == one;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int n = n0 + 8 * (m >> 2) + 4 * t + (m & 3);
-            v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < KT; ++k) {
-                h8 w = {};
-                if (n < a.N && 32 * k + 8 * r < a.rank) w = *reinterpret_cast<const h8 *>(a.b + ((size_t)one * a.N + n) * a.rank + 32 * k + 8 * r);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w, v[k], acc, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) kept[t][i] = own ? acc[i] : kept[t][i];
-        }
-    }
-    if (row >= a.M) return;
-    const int n = n0 + 8 * r;
-    const size_t at = (size_t)row * a.N + n;
-    float add[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) add[e] = __builtin_amdgcn_ldexpf(kept[e >> 2][e & 3], -up) * scale;
-    if (a.N % 8 == 0) {
-        if (n >= a.N) return;
-        h8 y = *reinterpret_cast<const h8 *>(a.y + at);
-        if (id >= 0) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = (_Float16)((float)y[e] + add[e]);
-        }
-        *reinterpret_cast<h8 *>(a.out + at) = y;
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (n + e >= a.N) break;
-        const _Float16 y = a.y[at + e];
-        a.out[at + e] = id >= 0 ? (_Float16)((float)y + add[e]) : y;
-    }
+template <int KT>
+void launch_expand(const AdapterArgs &g, int block_rows, hipStream_t st) {
+    const dim3 grid((unsigned)((g.M + block_rows - 1) / block_rows), (unsigned)((g.N + 128 * g.tiles - 1) / (128 * g.tiles)), (unsigned)g.dealt);
+    if (block_rows == 16)
+        adapters_expand_kernel<KT, 1><<<grid, 256, 0, st>>>(g);
+    else
+        adapters_expand_kernel<KT, 4><<<grid, 256, 0, st>>>(g);
 }
 
 }  // namespace
 
-AdapterPlan plan_adapters(int M, int K, int num_cus) {
+AdapterPlan plan_adapters(int M, int K, int N, int num_cus) {
     AdapterPlan p;
-    p.rows = round_up(M, 16);
-    const int blocks = p.rows / 16, pieces = (K + 127) / 128;
-    int parts = (2 * num_cus + blocks - 1) / blocks;
+    if (num_cus < 1) num_cus = 1;
+    p.rows = round_up(M, 64);
+    const int blocks = (M + 15) / 16, pieces = (K + 127) / 128, pieces_n = (N + 127) / 128;
+    // few rows: up to an adapter for every row, dealt to as many workgroups
+    p.dealt = M <= 16 ? M : M <= 128 ? 16 : M <= 512 ? 4 : 1;
+    int parts = 2 * num_cus / (blocks * p.dealt);
     if (parts > 16) parts = 16;
     if (parts > pieces) parts = pieces;
     if (parts < 1) parts = 1;
     p.part_k = (pieces + parts - 1) / parts * 128;
     p.parts = (K + p.part_k - 1) / p.part_k;
+    // many rows: blocks of 64 share B's tiles; columns per workgroup as long as there are four workgroups per compute unit
+    p.block_rows = M > 512 ? 64 : 16;
+    const long works = (long)((M + p.block_rows - 1) / p.block_rows) * pieces_n * (p.dealt > 4 ? 4 : 1);
+    p.tiles = (int)(works / (4L * num_cus));
+    if (p.tiles > 8) p.tiles = 8;
+    if (p.tiles < 1) p.tiles = 1;
     return p;
 }
 
@@ -191,8 +283,8 @@ hipError_t launch_adapters(const void *x, int M, int K, int N, int rank, int cou
     g.low = static_cast<float *>(workspace);
     g.out = static_cast<_Float16 *>(out);
     g.M = M, g.K = K, g.N = N, g.rank = rank, g.count = count;
-    g.parts = p.parts, g.part_k = p.part_k, g.rows = p.rows;
-    const dim3 shrink((unsigned)(p.rows / 16), (unsigned)p.parts), expand((unsigned)(p.rows / 16), (unsigned)((N + 127) / 128));
+    g.parts = p.parts, g.part_k = p.part_k, g.rows = p.rows, g.dealt = p.dealt, g.tiles = p.tiles;
+    const dim3 shrink((unsigned)((M + 15) / 16), (unsigned)p.parts, (unsigned)p.dealt);
     if (rank <= 16)
         adapters_shrink_kernel<1><<<shrink, 256, 0, st>>>(g);
     else if (rank <= 32)
@@ -203,11 +295,11 @@ hipError_t launch_adapters(const void *x, int M, int K, int N, int rank, int cou
         adapters_shrink_kernel<8><<<shrink, 256, 0, st>>>(g);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (rank <= 32)
-        adapters_expand_kernel<1><<<expand, 256, 0, st>>>(g);
+        launch_expand<1>(g, p.block_rows, st);
     else if (rank <= 64)
-        adapters_expand_kernel<2><<<expand, 256, 0, st>>>(g);
+        launch_expand<2>(g, p.block_rows, st);
     else
-        adapters_expand_kernel<4><<<expand, 256, 0, st>>>(g);
+        launch_expand<4>(g, p.block_rows, st);
     return hipGetLastError();
 }
 

@@ -533,7 +533,7 @@ static qfc_status_t check_adapters(const qfc_adapters_t *a, int32_t M) {
 qfc_status_t qfc_adapters_workspace_size(const qfc_adapters_t *adapters, int32_t M, size_t *bytes) {
     if (!bytes) return QFC_ERR_INVALID_ARG;
     if (const qfc_status_t s = check_adapters(adapters, M); s != QFC_OK) return s;
-    *bytes = adapters_workspace(plan_adapters(M, adapters->K, device_cus()), adapters->rank);
+    *bytes = adapters_workspace(plan_adapters(M, adapters->K, adapters->N, device_cus()), adapters->rank);
     return QFC_OK;
 }
 
@@ -544,7 +544,7 @@ qfc_status_t qfc_add_adapters(const void *x_f16, int32_t M, const int32_t *ids, 
     if (!aligned16(x_f16) || !aligned16(y_f16) || !aligned16(out_f16) || !aligned16(workspace) || !aligned16(adapters->a) || !aligned16(adapters->b) ||
         !aligned(ids, 4) || !aligned(adapters->scale, 4))
         return QFC_ERR_ALIGNMENT;
-    const AdapterPlan p = plan_adapters(M, adapters->K, device_cus());
+    const AdapterPlan p = plan_adapters(M, adapters->K, adapters->N, device_cus());
     if (workspace_bytes < adapters_workspace(p, adapters->rank)) return QFC_ERR_BUFFER_TOO_SMALL;
     return hip_status(launch_adapters(x_f16, M, adapters->K, adapters->N, adapters->rank, adapters->count, adapters->a, adapters->b, adapters->scale, ids, y_f16, p, workspace,
                                       out_f16, static_cast<hipStream_t>(stream)));

@@ -420,10 +420,13 @@ int plan_attention_many(int groups, int S, int g, int d, int n_ctx, int num_cus,
 hipError_t launch_attention_many(const void *q, const void *kc, const void *vc, int h_q, int h_kv, int d, int C, const int *plan, int records, int shares, int items,
                                  long rows, float *partial, void *out, hipStream_t st);
 struct AdapterPlan {
-    int rows;           // M rounded up to whole blocks of 16
+    int rows;           // M rounded up
     int parts, part_k;  // K in `parts` parts of `part_k`
+    int dealt;          // workgroups that share the adapters of a block of rows
+    int block_rows;     // second kernel: 16 or 64 rows per workgroup, 128 `tiles` columns
+    int tiles;
 };
-AdapterPlan plan_adapters(int M, int K, int num_cus);
+AdapterPlan plan_adapters(int M, int K, int N, int num_cus);
 size_t adapters_workspace(const AdapterPlan &p, int rank);
 hipError_t launch_adapters(const void *x, int M, int K, int N, int rank, int count, const void *a, const void *b, const float *scale, const int *ids, const void *y,
                            const AdapterPlan &p, void *workspace, void *out, hipStream_t st);
