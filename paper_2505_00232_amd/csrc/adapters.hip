@@ -33,20 +33,20 @@ __device__ __forceinline__ int row_id(const AdapterArgs &a, int row0, int lane) 
 template <class F>
 __device__ __forceinline__ void for_adapters(int id, int mine, int dealt, const F &f) {
     uint64_t left = __ballot(id >= 0);
-    for (int k = 0; left; ++k) {
+    for (int turn = 0; left; turn = turn + 1 == dealt ? 0 : turn + 1) {
         const int one = __builtin_amdgcn_readlane(id, __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)left) - 1));
         const uint64_t rows = __ballot(id == one);
         left &= ~rows;
-        if (k % dealt == mine) f(one, rows);
+        if (turn == mine) f(one, rows);
     }
 }
 
-// grid = (blocks of 16 rows, parts of K, workgroups that share a block's adapters); the four wavefronts of a workgroup take the part's pieces of 32 k in turn.  RT: tiles of 16
+// grid = (blocks of 16 rows, parts of K, workgroups that share a block's adapters); the four wavefronts of a workgroup take the part's pieces of 64 k in turn.  RT: tiles of 16
 // low-rank values.
 template <int RT>
 __global__ __launch_bounds__(256) void adapters_shrink_kernel(AdapterArgs a) {
     __shared__ float sums[4][RT][64][4];
-    constexpr int U = RT <= 2 ? 4 : RT == 4 ? 2 : 1;  // pieces on their way at once
+    constexpr int U = RT <= 4 ? 4 : 2;  // pieces on their way at once
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, r = lane >> 4;
     const int row0 = (int)blockIdx.x * 16, k0 = (int)blockIdx.y * a.part_k, k1 = min(k0 + a.part_k, a.K);
     const int id = row_id<16>(a, row0, lane);
@@ -61,16 +61,16 @@ __global__ __launch_bounds__(256) void adapters_shrink_kernel(AdapterArgs a) {
         v4f acc[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int k = k0 + 32 * wave; k < k1; k += 128 * U) {
+        for (int k = k0 + 64 * wave; k < k1; k += 128 * U) {
             h8 xv[U], wv[U][RT];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const h8 zero = {};
-                const bool there = k + 128 * u < k1;
-                xv[u] = there ? *reinterpret_cast<const h8 *>(x + k + 128 * u) : zero;
+                const int ku = k + 32 * (u & 1) + 256 * (u >> 1);
+                const bool there = ku < k1;
+                xv[u] = there ? *reinterpret_cast<const h8 *>(x + ku) : zero;
 #pragma unroll
-                for (int t = 0; t < RT; ++t)
-                    wv[u][t] = there && 16 * t + m < a.rank ? *reinterpret_cast<const h8 *>(w + (size_t)16 * t * a.K + k + 128 * u) : zero;
+                for (int t = 0; t < RT; ++t) wv[u][t] = there && 16 * t + m < a.rank ? *reinterpret_cast<const h8 *>(w + (size_t)16 * t * a.K + ku) : zero;
             }
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -97,7 +97,8 @@ __global__ __launch_bounds__(256) void adapters_shrink_kernel(AdapterArgs a) {
     }
 }
 
-// grid = (blocks of 16 MT rows, pieces of 128 `tiles` columns, workgroups that share a block's adapters).  The workgroup adds up its rows' low-rank values once, into LDS; then a
+// grid = (blocks of 16 MT rows x pieces of 128 `tiles` columns, workgroups that share a block's adapters): the blocks of a piece side by side on one XCD, whose L2 then
+// has the piece of B.  The workgroup adds up its rows' low-rank values once, into LDS; then a
 // wavefront takes 32 columns at a time, each of B's tiles for all of the block's rows.  The low-rank values are the second operand (rows as columns of the result), so that a lane
 // ends up with 8 consecutive columns of a row: row i of tile t of B is column 8 (i / 4) + 4 t + i % 4.  KT: steps of 32 low-rank values.
 template <int KT, int MT>
@@ -106,13 +107,40 @@ __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
     __shared__ _Float16 low[ROWS][PITCH];
     __shared__ uint32_t top[ROWS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, r = lane >> 4;
-    const int row0 = (int)blockIdx.x * ROWS;
+    const int blocks = (a.M + ROWS - 1) / ROWS, turn = (int)blockIdx.x / 8;
+    const int piece = (int)blockIdx.x % 8 + 8 * (turn / blocks), row0 = turn % blocks * ROWS;
+    if (piece * a.tiles * 128 >= a.N) return;
     const int id = row_id<ROWS>(a, row0, lane);
     uint64_t own = 0;
-    for_adapters(id, blockIdx.z, a.dealt, [&](int, uint64_t rows) __attribute__((always_inline)) { own |= rows; });
+    for_adapters(id, blockIdx.y, a.dealt, [&](int, uint64_t rows) __attribute__((always_inline)) { own |= rows; });
     // rows without an adapter: the first of the workgroups copies them
-    const uint64_t plain = blockIdx.z == 0 ? __ballot(id < 0 && lane < ROWS && row0 + lane < a.M) : 0;
+    const uint64_t plain = blockIdx.y == 0 ? __ballot(id < 0 && lane < ROWS && row0 + lane < a.M) : 0;
     if (!(own | plain)) return;
+
+    // What does not depend on the low-rank values is requested before they are read: the first columns' outputs and the first adapter's tile
+    auto columns = [&](int c) __attribute__((always_inline)) { return ((piece * a.tiles + c) * 4 + wave) * 32; };
+    auto load_y = [&](int c, h8 (&y)[MT]) __attribute__((always_inline)) {
+        const int n = columns(c) + 8 * r;
+        if (a.N % 8 != 0 || n >= a.N || c >= a.tiles) return;
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            if ((own | plain) >> (16 * t + m) & 1) y[t] = *reinterpret_cast<const h8 *>(a.y + (size_t)(row0 + 16 * t + m) * a.N + n);
+    };
+    auto load_w = [&](int c, int one, h8 (&w)[2][KT]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int col = columns(c) + 8 * (m >> 2) + 4 * u + (m & 3);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) {
+                const h8 zero = {};
+                w[u][k] = col < a.N && 32 * k + 8 * r < a.rank ? *reinterpret_cast<const h8 *>(a.b + ((size_t)one * a.N + col) * a.rank + 32 * k + 8 * r) : zero;
+            }
+        }
+    };
+    const int first = own ? __builtin_amdgcn_readlane(id, __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)own) - 1)) : -1;
+    h8 y[MT], w0[2][KT];
+    load_y(0, y);
+    if (first >= 0) load_w(0, first, w0);
 
     if (own) {
         constexpr int MOST = ROWS * KT * 4 / 256 > 0 ? ROWS * KT * 4 / 256 : 1;  // octets per thread
@@ -127,13 +155,18 @@ __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
             for (int i = 0; i < 8; ++i) v[q][i] = 0.0f;
             if (row < ROWS && (own >> row & 1)) {
                 const float *src = a.low + (size_t)(row0 + row) * a.rank + 8 * o;
-                for (int p = 0; p < a.parts; ++p) {
-                    const v4f l0 = *reinterpret_cast<const v4f *>(src + (size_t)p * a.rows * a.rank), l1 = *reinterpret_cast<const v4f *>(src + (size_t)p * a.rows * a.rank + 4);
+                for (int p0 = 0; p0 < a.parts; p0 += 8) {  // (eight parts on their way at once; those behind the last read it again and are left out)
+                    v4f l[8][2];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[q][i] += l0[i];
-                        v[q][4 + i] += l1[i];
+                    for (int p = 0; p < 8; ++p) {
+                        const float *part = src + (size_t)min(p0 + p, a.parts - 1) * a.rows * a.rank;
+                        l[p][0] = *reinterpret_cast<const v4f *>(part);
+                        l[p][1] = *reinterpret_cast<const v4f *>(part + 4);
                     }
+#pragma unroll
+                    for (int p = 0; p < 8; ++p)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[q][i] = p0 + p < a.parts ? v[q][i] + l[p][i >> 2][i & 3] : v[q][i];
                 }
                 float big = 0.0f;
 #pragma unroll
@@ -178,27 +211,23 @@ __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
         back[t] = has[t] ? __builtin_amdgcn_ldexpf(a.scale[of_row], -up) : 0.0f;
     }
     for (int c = 0; c < a.tiles; ++c) {
-        const int n0 = (((int)blockIdx.y * a.tiles + c) * 4 + wave) * 32, n = n0 + 8 * r;
+        const int n0 = columns(c), n = n0 + 8 * r;
         if (n0 >= a.N) return;
-        h8 y[MT];
-        if (a.N % 8 == 0 && n < a.N) {
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-                if (real[t]) y[t] = *reinterpret_cast<const h8 *>(a.y + (size_t)(row0 + 16 * t + m) * a.N + n);
-        }
+        h8 y_next[MT];
+        load_y(c + 1, y_next);
         v4f kept[MT][2];
 #pragma unroll
         for (int t = 0; t < MT; ++t) kept[t][0] = kept[t][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        for_adapters(id, blockIdx.z, a.dealt, [&](int one, uint64_t rows) __attribute__((always_inline)) {
+        for_adapters(id, blockIdx.y, a.dealt, [&](int one, uint64_t rows) __attribute__((always_inline)) {
             h8 w[2][KT];
+            if (one == first) {  // (requested during the columns before)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int col = n0 + 8 * (m >> 2) + 4 * u + (m & 3);
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int k = 0; k < KT; ++k) {
-                    const h8 zero = {};
-                    w[u][k] = col < a.N && 32 * k + 8 * r < a.rank ? *reinterpret_cast<const h8 *>(a.b + ((size_t)one * a.N + col) * a.rank + 32 * k + 8 * r) : zero;
-                }
+                    for (int k = 0; k < KT; ++k) w[u][k] = w0[u][k];
+                if (c + 1 < a.tiles) load_w(c + 1, first, w0);
+            } else {
+                load_w(c, one, w);
             }
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
@@ -233,12 +262,15 @@ __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
                 }
             }
         }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) y[t] = y_next[t];
     }
 }
 
 template <int KT>
 void launch_expand(const AdapterArgs &g, int block_rows, hipStream_t st) {
-    const dim3 grid((unsigned)((g.M + block_rows - 1) / block_rows), (unsigned)((g.N + 128 * g.tiles - 1) / (128 * g.tiles)), (unsigned)g.dealt);
+    const int pieces = (g.N + 128 * g.tiles - 1) / (128 * g.tiles);
+    const dim3 grid((unsigned)((g.M + block_rows - 1) / block_rows * round_up(pieces, 8)), (unsigned)g.dealt);
     if (block_rows == 16)
         adapters_expand_kernel<KT, 1><<<grid, 256, 0, st>>>(g);
     else
