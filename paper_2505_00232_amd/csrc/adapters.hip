@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
         }
         __syncthreads();
     }
-    h8 v[MT][KT];
+    auto low_at = [&](int t, int k) __attribute__((always_inline)) { return *reinterpret_cast<const h8 *>(&low[16 * t + m][32 * k + 8 * r]); };  // (in LDS: registers are for what is on its way)
     float back[MT];  // the scale and the power of two taken back
     bool real[MT], has[MT];
 #pragma unroll
@@ -200,17 +200,99 @@ __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
         const int row = 16 * t + m;
         has[t] = own >> row & 1;
         real[t] = (own | plain) >> row & 1;
-#pragma unroll
-        for (int k = 0; k < KT; ++k) {
-            const h8 zero = {};
-            v[t][k] = own ? *reinterpret_cast<const h8 *>(&low[row][32 * k + 8 * r]) : zero;
-        }
         const float big = own ? __uint_as_float(top[row]) : 0.0f;
         const int up = big > 0.0f && big < INFINITY ? 14 - __builtin_amdgcn_frexp_expf(big) : 0;
         const int of_row = __shfl(id, row, 64);
         back[t] = has[t] ? __builtin_amdgcn_ldexpf(a.scale[of_row], -up) : 0.0f;
     }
-    for (int c = 0; c < a.tiles; ++c) {
+    int c = 0;
+    // Every row there and this workgroup's, whole tiles: no branches but the loop over the adapters, so that the loads of the next columns are not waited for.
+    if (own && (own | plain) == (ROWS == 64 ? ~0ull : (1ull << ROWS) - 1) && a.N % 8 == 0) {
+        const _Float16 *yp[MT];
+        _Float16 *op[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            yp[t] = a.y + (size_t)(row0 + 16 * t + m) * a.N + columns(0) + 8 * r;
+            op[t] = a.out + (size_t)(row0 + 16 * t + m) * a.N + columns(0) + 8 * r;
+        }
+        const int whole = a.N > columns(0) ? min(a.tiles, ((a.N - columns(0)) / 32 + 3) / 4) : 0;  // tiles of 32 columns of this wavefront, four apart
+        const uint64_t firsts = __ballot(id == first), others = own & ~firsts;
+        // (every address is one to read from, and what is not wanted is dropped: no branches around the loads)
+        const _Float16 *wp[2][KT];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int k = 0; k < KT; ++k) wp[u][k] = a.b + ((size_t)columns(0) + 8 * (m >> 2) + 4 * u + (m & 3)) * a.rank + min(32 * k + 8 * r, a.rank - 8);
+        auto load_whole = [&](int tile, int one, h8 (&w)[2][KT]) __attribute__((always_inline)) {
+            const size_t off = ((size_t)one * a.N + tile * 128) * a.rank;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < KT; ++k) w[u][k] = *reinterpret_cast<const h8 *>(wp[u][k] + off);
+        };
+        auto cut = [&](h8 (&w)[2][KT]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    const h8 zero = {};
+                    w[u][k] = 32 * k + 8 * r < a.rank ? w[u][k] : zero;
+                }
+        };
+        auto work = [&](h8 (&yc)[MT], h8 (&wc)[2][KT], h8 (&yn)[MT], h8 (&wn)[2][KT]) __attribute__((always_inline)) {
+            const int next = min(c + 1, whole - 1) * 128;
+#pragma unroll
+            for (int t = 0; t < MT; ++t) yn[t] = *reinterpret_cast<const h8 *>(yp[t] + next);
+            load_whole(min(c + 1, whole - 1), first, wn);
+            cut(wc);
+            v4f kept[MT][2];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                kept[t][0] = kept[t][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) kept[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wc[u][k], low_at(t, k), kept[t][u], 0, 0, 0);
+            }
+            for (uint64_t left = others; left;) {
+                const int one = __builtin_amdgcn_readlane(id, __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)left) - 1));
+                const uint64_t rows = __ballot(id == one);
+                left &= ~rows;
+                h8 w[2][KT];
+                load_whole(c, one, w);
+                cut(w);
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int k = 0; k < KT; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[u][k], low_at(t, k), acc, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) kept[t][u][i] = rows >> (16 * t + m) & 1 ? acc[i] : kept[t][u][i];
+                    }
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                h8 o;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = has[t] ? (_Float16)((float)yc[t][e] + kept[t][e >> 2][e & 3] * back[t]) : yc[t][e];
+                *reinterpret_cast<h8 *>(op[t] + c * 128) = o;
+            }
+            ++c;
+        };
+        h8 y1[MT], w1[2][KT];
+        while (c + 1 < whole) {
+            work(y, w0, y1, w1);
+            work(y1, w1, y, w0);
+        }
+        if (c < whole) work(y, w0, y1, w1);
+        if (c < a.tiles && columns(c) < a.N) {
+            load_y(c, y);
+            load_w(c, first, w0);
+        }
+    }
+    for (; c < a.tiles; ++c) {
         const int n0 = columns(c), n = n0 + 8 * r;
         if (n0 >= a.N) return;
         h8 y_next[MT];
@@ -236,7 +318,7 @@ __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
                 for (int u = 0; u < 2; ++u) {
                     v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int k = 0; k < KT; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[u][k], v[t][k], acc, 0, 0, 0);
+                    for (int k = 0; k < KT; ++k) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[u][k], low_at(t, k), acc, 0, 0, 0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) kept[t][u][i] = rows >> (16 * t + m) & 1 ? acc[i] : kept[t][u][i];
                 }
@@ -285,18 +367,22 @@ AdapterPlan plan_adapters(int M, int K, int N, int num_cus) {
     p.rows = round_up(M, 64);
     const int blocks = (M + 15) / 16, pieces = (K + 127) / 128, pieces_n = (N + 127) / 128;
     // few rows: up to an adapter for every row, dealt to as many workgroups
-    p.dealt = M <= 16 ? M : M <= 128 ? 16 : M <= 512 ? 4 : 1;
+    // (64 rows of 40 adapters, 4096 x 4096, 16 / 8 / 4 workgroups per block: 17.1 / 13.3 / 13.8 us; 128 rows 27.5 / 19.3 / 15.4; 16 rows 11.2 / 11.0 / 11.9)
+    p.dealt = 4 * num_cus / (blocks * pieces_n);
+    if (p.dealt > 16) p.dealt = 16;
+    if (p.dealt > M) p.dealt = M;
+    if (p.dealt < 1) p.dealt = 1;
     int parts = 2 * num_cus / (blocks * p.dealt);
     if (parts > 16) parts = 16;
     if (parts > pieces) parts = pieces;
     if (parts < 1) parts = 1;
     p.part_k = (pieces + parts - 1) / parts * 128;
     p.parts = (K + p.part_k - 1) / p.part_k;
-    // many rows: blocks of 64 share B's tiles; columns per workgroup as long as there are four workgroups per compute unit
+    // many rows: blocks of 64 share B's tiles; columns per workgroup so that the card holds all workgroups at once
     p.block_rows = M > 512 ? 64 : 16;
-    const long works = (long)((M + p.block_rows - 1) / p.block_rows) * pieces_n * (p.dealt > 4 ? 4 : 1);
-    p.tiles = (int)(works / (4L * num_cus));
-    if (p.tiles > 8) p.tiles = 8;
+    const long works = (long)((M + p.block_rows - 1) / p.block_rows) * pieces_n;
+    p.tiles = (int)((works + 2L * num_cus - 1) / (2L * num_cus));
+    if (p.tiles > 16) p.tiles = 16;
     if (p.tiles < 1) p.tiles = 1;
     return p;
 }
