@@ -9,11 +9,11 @@
 // P is multiplied with the step in 32 bits and rounded to binary16 once per group; the -8 is taken off with the same rounded values (an MFMA with a
 // constant into the same sums), so that what the rounding leaves is relative to a centred code, and the offsets are again one MFMA, whose last row, ones, gives the sum of P.
 //
-// Few query rows of a request (up to kFewRows per KV head: tokens, short chunks) go through that kernel in blocks of 16.  Many rows would take the same
+// Few query rows of a request (up to few_rows per KV head: tokens, short chunks) go through that kernel in blocks of 16.  Many rows would take the same
 // codes apart again and again: for them the pages are first turned into binary16 copies in the workspace, once, and the kernel for prompts (attention.hip) walks
 // those.  Which request is which is known on the device only, where a first small kernel finds it.
-// P is taken against a maximum that may be 2^4 too small (so that sums are seldom rescaled) and 2^10 times as large: with steps below 2 every product is below 2^15, and binary16
-// keeps its 11 bits down to 2^-24.  A step of 2 or more (values some 30 apart and more) lowers that factor to 2^-2 from there on, for which every step is small enough.
+// P is taken 2^14 times as large: with steps below 2 every product is below 2^15, and binary16 keeps its 11 bits down to a product of 2^-28.  A step of 2 or more (values some 30
+// apart and more) lowers that factor to 2^2 from there on, for which every step (8734 at most) is small enough.
 #include "paged_q4.h"
 
 namespace qfc {
@@ -24,13 +24,16 @@ typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kFactor = 10.0f, kLag = 4.0f, kLower = 12.0f;  // log 2 of what P is multiplied with, of what the maximum may lag behind, of what large steps divide P by
+constexpr float kFactor = 14.0f, kLower = 12.0f;  // log 2 of what P is multiplied with, of what large steps divide that by
 constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: below every score
 
-constexpr int kFewRows = 256;
+// Rows of a request per KV head that the blocks of 16 take.  Heads 32 on 8 of 128 values, us with blocks of 16 / with copies: one request at 512 positions 128 rows 15 / 23,
+// 256 rows 18 / 23, 512 rows 26 / 23, at 4096 positions 256 rows 31 / 33, 512 rows 46 / 39; eight requests, which keep the card busy, at 512 positions 128 rows 40 / 31, 192 rows
+// 54 / 32, at 4096 positions 72 rows 54 / 87, 128 rows 77 / 92, 192 rows 113 / 122, 256 rows 136 / 121.
+int few_rows(long all_rows) { return all_rows > 1024 ? 128 : 256; }
 constexpr int kMaxSlots = 256;  // requests of many rows at most, the others go through the blocks of 16
 
-constexpr int kWhole = 4;
+constexpr int kWhole = 4;  // pages of a unit that is not cut, of small shares
 
 struct AttnQ4Args {
     const _Float16 *q;  // [tokens, h_q, D]
@@ -133,281 +136,272 @@ struct Units {
 // Place of the partial results that worker w leaves of a unit
 __device__ __forceinline__ size_t partial_of(const Unit &u, int w, int share) { return (size_t)w * 2 + (u.begin > w * share ? 1 : 0); }
 
-// What a wavefront has on its way: DEPTH pages, keys and values each in a place of PART bytes of LDS of its own.
+// Workgroups per compute unit.  More would fit the LDS with heads of 128 and 64 values and were slower: 32 requests of up to 8192 positions 47 us, with three 51; 16 requests of 3000
+// to 6000, heads of 64, 19.0, with three 21.7, with four 20.4.
+constexpr int kWgs = 2;
+
+// What a wavefront has on its way: a page's keys and its values, each in a place of PART bytes of LDS of its own, which the next page's take as soon as they are read.
 template <int D>
-struct Ring {
+struct Place {
     static constexpr int kHalf = 40 * D;                      // bytes of a page's keys or values
     static constexpr int PART = (kHalf + 1023) / 1024 * 1024;  // copied in pieces of a KiB
     static constexpr int COPIES = PART / 1024;
-    static constexpr int DEPTH = 1;
-    static constexpr int WGS = D == 64 ? 3 : 2;  // workgroups per compute unit
-    static constexpr int WAVE = 2 * DEPTH * PART;
-    static constexpr int LDS = 4 * WAVE;
-    static constexpr int FLYING = (2 * DEPTH - 1) * COPIES;  // copies behind the ones waited for
-    static_assert(WGS * LDS <= 160 * 1024 && FLYING <= 63, "LDS, and the 6-bit counter of outstanding copies");
+    static constexpr int LDS = 4 * 2 * PART;
+    static_assert(kWgs * LDS <= 160 * 1024 && COPIES <= 63, "LDS, and the 6-bit counter of outstanding copies");
 };
 
 // Up to 16 query rows of a KV head at a time.  The wavefronts work for themselves, each with copies of its own on the way.
 template <int D>
-__global__ __launch_bounds__(256, Ring<D>::WGS) void attn_q4_kernel(AttnQ4Args a) {
+__global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
     typedef PageLayout<D> L;
-    typedef Ring<D> R;
+    typedef Place<D> R;
     constexpr int G = L::G, DT = D / 16, W = L::W;
-    extern __shared__ float lds[];  // the rings
+    extern __shared__ float lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane & 15, r = lane >> 4;
-    char *const ring = reinterpret_cast<char *>(lds) + wave * R::WAVE;
-    const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * R::WAVE);
+    char *const keys = reinterpret_cast<char *>(lds) + wave * (2 * R::PART), *const values = keys + R::PART - R::kHalf;  // (the layout counts from the page's start)
+    const uint32_t lds_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * (2 * R::PART));
     const int worker = (int)blockIdx.x * 4 + wave;
     if (worker >= a.workers) return;
     Units units(a, lane);
     const int from = worker * units.share, stop = from + units.share;
     for (int x = from; x < stop;) {
-    const Unit unit = units.at<false>(x);
-    if (__builtin_amdgcn_readfirstlane(unit.b) < 0) return;
-    const bool cut = units.may_cut(unit);
-    if (!cut && unit.begin < x) {  // (another wavefront has it)
-        x = unit.end;
-        continue;
-    }
-    const int b = __builtin_amdgcn_readfirstlane(unit.b), kv = __builtin_amdgcn_readfirstlane(unit.kv), row0 = __builtin_amdgcn_readfirstlane(unit.row0);
-    const Span span = unit.span;
-    const int rows = span.count * a.g, n = span.positions;
-    const int sees = max(0, n - rows / a.g + min(row0 + 15, rows - 1) / a.g + 1);  // positions the unit's last row sees
-    const int last = cut ? min(stop, unit.end) : unit.end;
-    const bool whole = unit.begin >= from && last == unit.end;  // no other wavefront has a page of the unit
-    const int page0 = max(x - unit.begin - units.over, 0), pages = min(last - unit.begin - units.over, (sees + kPage - 1) / kPage);  // the unit's pages that are taken here
-    x = __builtin_amdgcn_readfirstlane(last);
-
-    // ---- copies.  Lane i holds the place of the wavefront's i-th page (of 64 at a time)
-    const int count = __builtin_amdgcn_readfirstlane(pages - page0);
-    auto places = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (page0 + i + lane) * kPage) : -1; };
-    int ahead = places(0), now = ahead;  // of the pages that are requested, and of those that are worked on
-
-    // ---- queries: lane (m, r) holds q[row0 + m][32 j + 8 r .. + 7], scaled by a power of two
-    const bool real = row0 + m < rows;
-    const int token = real ? (row0 + m) / a.g : 0, head = kv * a.g + (real ? (row0 + m) % a.g : 0);
-    const size_t at = ((size_t)(span.first + token) * a.h_q + head) * D;
-    const int lim = real ? n - span.count + token + 1 : 0;  // positions the lane's row sees (none where 0 or less)
-    h8 qf[G];
-    float top = 0.0f;
-#pragma unroll
-    for (int j = 0; j < G; ++j) {
-        const h8 zero = {};
-        qf[j] = real ? *reinterpret_cast<const h8 *>(a.q + at + 32 * j + 8 * r) : zero;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qf[j][e]));
-    }
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    // the largest to 2^13 .. 2^14: what the division by 16 below loses is 2^-24 of it and less
-    const int up = top > 0.0f ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
-    const float up2 = __builtin_amdgcn_ldexpf(1.0f, up);
-    const float to_score = __builtin_amdgcn_ldexpf(a.scale, 24 - up);  // 2^24: the codes' denormals
-    h8 sums = {};
-#pragma unroll
-    for (int j = 0; j < G; ++j) {
-        float s = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = (float)qf[j][e] * up2;
-            s += x;
-            qf[j][e] = (_Float16)(e & 2 ? x * 0.0625f : x);  // (values 2, 3, 6, 7 of an octet: the high nibbles of their bytes)
+        const Unit unit = units.at<false>(x);
+        if (__builtin_amdgcn_readfirstlane(unit.b) < 0) return;
+        const bool cut = units.may_cut(unit);
+        if (!cut && unit.begin < x) {  // (another wavefront has it)
+            x = unit.end;
+            continue;
         }
-        s += __shfl_xor(s, 16, 64);
-        s += __shfl_xor(s, 32, 64);
-        const _Float16 hi = (_Float16)(s * 0.0625f), lo = (_Float16)(s * 0.0625f - (float)hi);
-        sums[j] = r == 0 ? hi : r == 1 ? lo : (_Float16)0.0f;
-    }
+        const int b = __builtin_amdgcn_readfirstlane(unit.b), kv = __builtin_amdgcn_readfirstlane(unit.kv), row0 = __builtin_amdgcn_readfirstlane(unit.row0);
+        const Span span = unit.span;
+        const int rows = span.count * a.g, n = span.positions;
+        const int sees = max(0, n - rows / a.g + min(row0 + 15, rows - 1) / a.g + 1);  // positions the unit's last row sees
+        const int last = cut ? min(stop, unit.end) : unit.end;
+        const bool whole = unit.begin >= from && last == unit.end;  // no other wavefront has a page of the unit
+        const int page0 = max(x - unit.begin - units.over, 0), pages = min(last - unit.begin - units.over, (sees + kPage - 1) / kPage);  // the unit's pages that are taken here
+        x = __builtin_amdgcn_readfirstlane(last);
 
-    v4f acc[DT], rest = {};
-#pragma unroll
-    for (int t = 0; t < DT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    float run_max = kNothingYet, factor = kFactor;
-    const u32x4 eight_lo = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u}, eight_hi = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u},  // -8 as a code
-                eight_k = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};
-    const uint32_t mask_lo = 0x000F000Fu, mask_hi = 0x00F000F0u;
+        // ---- copies.  Lane i holds the number of the wavefront's i-th page (of 64 at a time)
+        const int count = __builtin_amdgcn_readfirstlane(pages - page0);
+        auto numbers = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (page0 + i + lane) * kPage) : -1; };
+        int ahead = numbers(0), page = __builtin_amdgcn_readlane(ahead, 0);
 
-    auto copy = [&](int i, int slot, int part) __attribute__((always_inline)) {  // part 0: keys, 1: values
-        const int page = __builtin_amdgcn_readlane(ahead, i & 63);
-        const char *src = a.pages + ((size_t)max(page, 0) * a.h_kv + kv) * L::kBytes + part * R::kHalf;
+        // ---- queries: lane (m, r) holds q[row0 + m][32 j + 8 r .. + 7], scaled by a power of two
+        const bool real = row0 + m < rows;
+        const int token = real ? (row0 + m) / a.g : 0, head = kv * a.g + (real ? (row0 + m) % a.g : 0);
+        const size_t at = ((size_t)(span.first + token) * a.h_q + head) * D;
+        const int lim = real ? n - span.count + token + 1 : 0;  // positions the lane's row sees (none where 0 or less)
+        h8 qf[G];
+        float top = 0.0f;
 #pragma unroll
-        for (int c = 0; c < R::COPIES; ++c)  // (the last piece's lanes behind the part copy its end again)
-            copy16_to_lds(src, (uint32_t)min(c * 1024 + lane * 16, R::kHalf - 16), ring_at + (2 * slot + part) * R::PART + c * 1024);
-    };
+        for (int j = 0; j < G; ++j) {
+            const h8 zero = {};
+            qf[j] = real ? *reinterpret_cast<const h8 *>(a.q + at + 32 * j + 8 * r) : zero;
 #pragma unroll
-    for (int i = 0; i < R::DEPTH; ++i)
-        if (i < count) {
-            copy(i, i, 0);
-            copy(i, i, 1);
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qf[j][e]));
         }
-    for (int i = 0, slot = 0; i < count; ++i, slot = slot + 1 == R::DEPTH ? 0 : slot + 1) {
-        const int k0 = (page0 + i) * kPage;
-        if (i > 0 && (i & 63) == 0) now = places(i);
-        if (i + R::DEPTH < count && ((i + R::DEPTH) & 63) == 0) ahead = places(i + R::DEPTH);
-        const int page = __builtin_amdgcn_readlane(now, i & 63);
-        const char *src = ring + 2 * slot * R::PART;
-        // The page's keys are there: behind them are its values and DEPTH - 1 pages (at the end, none).  In front of a copy into a place all reads of it are done.
-        if (i + R::DEPTH <= count)
-            wait_copies<R::FLYING>();
-        else
-            wait_copies<0>();
-        const int seen = page >= 0 ? lim - k0 : 0, valid = page >= 0 ? n - k0 : 0;  // of this page, by the lane's row and by anyone
-        // ---- scores; lane (m, r), element 4 t + i: position 16 r + 4 t + i, times 2^-24 and the queries' power of two
-        float sc[16];
-        {
-            h8 off[4] = {};
-            if (r < 2) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        // the largest to 2^13 .. 2^14: what the division by 16 below loses is 2^-24 of it and less
+        const int up = top > 0.0f ? 14 - __builtin_amdgcn_frexp_expf(top) : 0;
+        const float up2 = __builtin_amdgcn_ldexpf(1.0f, up);
+        const float to_score = __builtin_amdgcn_ldexpf(a.scale, 24 - up);  // 2^24: the codes' denormals
+        h8 sums = {};
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
+        for (int j = 0; j < G; ++j) {
+            float s = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < G; ++j) off[t][j] = reinterpret_cast<const _Float16 *>(src + L::kOffsetK + (16 * t + m) * G * 2)[j];
+            for (int e = 0; e < 8; ++e) {
+                const float x = (float)qf[j][e] * up2;
+                s += x;
+                qf[j][e] = (_Float16)(e & 2 ? x * 0.0625f : x);  // (values 2, 3, 6, 7 of an octet: the high nibbles of their bytes)
             }
-            v4f part[4];
+            s += __shfl_xor(s, 16, 64);
+            s += __shfl_xor(s, 32, 64);
+            const _Float16 hi = (_Float16)(s * 0.0625f), lo = (_Float16)(s * 0.0625f - (float)hi);
+            sums[j] = r == 0 ? hi : r == 1 ? lo : (_Float16)0.0f;
+        }
+
+        v4f acc[DT], rest = {};
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const v4f zero = {};
-                part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off[t], sums, zero, 0, 0, 0);
+        for (int t = 0; t < DT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        float run_max = kNothingYet, factor = kFactor;
+        const u32x4 eight_lo = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u}, eight_hi = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u},  // -8 as a code
+                    eight_k = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};
+        const uint32_t mask_lo = 0x000F000Fu, mask_hi = 0x00F000F0u;
+
+        auto copy = [&](int of, int part) __attribute__((always_inline)) {  // part 0: keys, 1: values
+            const char *src = a.pages + ((size_t)max(of, 0) * a.h_kv + kv) * L::kBytes + part * R::kHalf;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) part[t][i] *= 1.0f / 1048576.0f;
-            }
+            for (int c = 0; c < R::COPIES; ++c)  // (the last piece's lanes behind the part copy its end again)
+                copy16_to_lds(src, (uint32_t)min(c * 1024 + lane * 16, R::kHalf - 16), lds_at + part * R::PART + c * 1024);
+        };
+        if (count > 0) {
+            copy(page, 0);
+            copy(page, 1);
+        }
+        for (int i = 0; i < count; ++i) {
+            const int k0 = (page0 + i) * kPage;
+            const bool more = i + 1 < count;
+            if (more && ((i + 1) & 63) == 0) ahead = numbers(i + 1);
+            const int next = __builtin_amdgcn_readlane(ahead, (i + 1) & 63);
+            wait_copies<R::COPIES>();  // the page's keys are there: behind them are its values
+            const int seen = page >= 0 ? lim - k0 : 0, valid = page >= 0 ? n - k0 : 0;  // of this page, by the lane's row and by anyone
+            // ---- scores; lane (m, r), element 4 t + i: position 16 r + 4 t + i, times 2^-24 and the queries' power of two
+            float sc[16];
+            {
+                h8 off[4] = {};
+                if (r < 2) {
 #pragma unroll
-            for (int jj = 0; jj < G / W; ++jj) {
-                typedef uint32_t words __attribute__((ext_vector_type(W)));
-                words c[4];
+                    for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) c[t] = *reinterpret_cast<const words *>(src + L::kCodesK + ((t * (G / W) + jj) * 64 + lane) * (4 * W));
+                        for (int j = 0; j < G; ++j) off[t][j] = reinterpret_cast<const _Float16 *>(keys + L::kOffsetK + (16 * t + m) * G * 2)[j];
+                }
+                v4f part[4];
 #pragma unroll
-                for (int jw = 0; jw < W; ++jw) {
-                    const int j = jj * W + jw;
+                for (int t = 0; t < 4; ++t) {
                     const v4f zero = {};
-                    const v4f from = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_k), qf[j], zero, 0, 0, 0);
-                    h8 st[2];
-                    st[0] = *reinterpret_cast<const h8 *>(src + L::kStepK + (j * kPage + 16 * r) * 2);
-                    st[1] = *reinterpret_cast<const h8 *>(src + L::kStepK + (j * kPage + 16 * r + 8) * 2);
+                    part[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off[t], sums, zero, 0, 0, 0);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const uint32_t w = c[t][jw];
-                        const u32x4 op = {w & mask_lo, w & mask_hi, (w >> 8) & mask_lo, (w >> 8) & mask_hi};
-                        const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, op), qf[j], from, 0, 0, 0);
+                    for (int i = 0; i < 4; ++i) part[t][i] *= 1.0f / 1048576.0f;
+                }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) part[t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[t][i]);
+                for (int jj = 0; jj < G / W; ++jj) {
+                    typedef uint32_t words __attribute__((ext_vector_type(W)));
+                    words c[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) c[t] = *reinterpret_cast<const words *>(keys + L::kCodesK + ((t * (G / W) + jj) * 64 + lane) * (4 * W));
+#pragma unroll
+                    for (int jw = 0; jw < W; ++jw) {
+                        const int j = jj * W + jw;
+                        const v4f zero = {};
+                        const v4f from = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_k), qf[j], zero, 0, 0, 0);
+                        h8 st[2];
+                        st[0] = *reinterpret_cast<const h8 *>(keys + L::kStepK + (j * kPage + 16 * r) * 2);
+                        st[1] = *reinterpret_cast<const h8 *>(keys + L::kStepK + (j * kPage + 16 * r + 8) * 2);
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            const uint32_t w = c[t][jw];
+                            const u32x4 op = {w & mask_lo, w & mask_hi, (w >> 8) & mask_lo, (w >> 8) & mask_hi};
+                            const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, op), qf[j], from, 0, 0, 0);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) part[t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[t][i]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[e] = part[e >> 2][e & 3];
+            }
+            if (__any(seen < kPage)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[e] = 16 * r + e < seen ? sc[e] : -INFINITY;
+            }
+            float bmax = fmaxf(sc[0], sc[1]);
+#pragma unroll
+            for (int e = 2; e < 16; e += 2) bmax = fmaxf(fmaxf(bmax, sc[e]), sc[e + 1]);
+            wait_copies<63>();  // (in front of a copy into a place all reads of it are done)
+            if (more) {
+                copy(next, 0);
+                wait_copies<R::COPIES>();  // the values: behind them are the next page's keys
+            } else {
+                wait_copies<0>();
+            }
+            if (valid < kPage) {  // positions that nobody has may hold anything: their values' steps and offsets are taken as 0
+                if (lane >= valid) {
+#pragma unroll
+                    for (int j = 0; j < G; ++j) {
+                        *reinterpret_cast<_Float16 *>(values + L::step_v(lane, j)) = (_Float16)0.0f;
+                        *reinterpret_cast<_Float16 *>(values + L::offset_v(lane, j)) = (_Float16)0.0f;
                     }
                 }
             }
+            auto step_of = [&](int j, int u) __attribute__((always_inline)) { return *reinterpret_cast<const h8 *>(values + L::kStepV + (j * kPage + 16 * r + 8 * u) * 2); };
+            uint32_t large;  // some of the page's steps; all of them in the wavefront
+            {
+                typedef uint32_t words __attribute__((ext_vector_type(G / 2)));
+                const words w = *reinterpret_cast<const words *>(values + L::kStepV + lane * (2 * G));
+                large = w[0];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sc[e] = part[e >> 2][e & 3];
-        }
-        if (__any(seen < kPage)) {
+                for (int j = 1; j < G / 2; ++j) large |= w[j];
+            }
+            bmax = fmaxf(bmax, __shfl_xor(bmax, 16, 64));
+            bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64)) * to_score;  // (in units of log 2 from here on)
+            const bool lowers = factor == kFactor && __any((large & 0x40004000u) != 0);  // a step of 2 or more
+            if (__any(bmax > run_max) || lowers) {
+                const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max - (lowers ? kLower : 0.0f));
+                run_max = new_max;
+                factor = lowers ? kFactor - kLower : factor;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sc[e] = 16 * r + e < seen ? sc[e] : -INFINITY;
-        }
-        float bmax = fmaxf(sc[0], sc[1]);
+                for (int i = 0; i < 4; ++i) {
 #pragma unroll
-        for (int e = 2; e < 16; e += 2) bmax = fmaxf(fmaxf(bmax, sc[e]), sc[e + 1]);
-        wait_copies<63>();  // (the keys have been read)
-        if (i + R::DEPTH < count) copy(i + R::DEPTH, slot, 0);
-        // (and its values: behind them DEPTH - 1 pages and the next one's keys)
-        if (i + R::DEPTH < count)
-            wait_copies<R::FLYING>();
-        else
-            wait_copies<0>();
-        const char *const vsrc = src + R::PART - R::kHalf;  // (the layout counts from the page's start)
-        if (valid < kPage) {  // positions that nobody has may hold anything: their values' steps and offsets are taken as 0
-            char *const clear = ring + (2 * slot + 1) * R::PART - R::kHalf;
-            if (lane >= valid) {
-#pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    *reinterpret_cast<_Float16 *>(clear + L::step_v(lane, j)) = (_Float16)0.0f;
-                    *reinterpret_cast<_Float16 *>(clear + L::offset_v(lane, j)) = (_Float16)0.0f;
+                    for (int t = 0; t < DT; ++t) acc[t][i] *= corr;
+                    rest[i] *= corr;
                 }
             }
-        }
-        auto step_of = [&](int j, int u) __attribute__((always_inline)) { return *reinterpret_cast<const h8 *>(vsrc + L::kStepV + (j * kPage + 16 * r + 8 * u) * 2); };
-        uint32_t large;  // some of the page's steps; all of them in the wavefront
-        {
-            typedef uint32_t words __attribute__((ext_vector_type(G / 2)));
-            const words w = *reinterpret_cast<const words *>(vsrc + L::kStepV + lane * (2 * G));
-            large = w[0];
+            const float from_max = factor - run_max;
+            h8 pv[2];
 #pragma unroll
-            for (int j = 1; j < G / 2; ++j) large |= w[j];
-        }
-        bmax = fmaxf(bmax, __shfl_xor(bmax, 16, 64));
-        bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64)) * to_score;  // (in units of log 2 from here on)
-        const bool lowers = factor == kFactor && __any((large & 0x40004000u) != 0);  // a step of 2 or more
-        if (__any(bmax > run_max + kLag) || lowers) {
-            const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max - (lowers ? kLower : 0.0f));
-            run_max = new_max;
-            factor = lowers ? kFactor - kLower : factor;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                for (int t = 0; t < DT; ++t) acc[t][i] *= corr;
-                rest[i] *= corr;
+            for (int e = 0; e < 16; ++e) {
+                sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], to_score, from_max));
+                pv[e >> 3][e & 7] = (_Float16)sc[e];
             }
-        }
-        const float from_max = factor - run_max;
-        h8 pv[2];
+            // ---- second product
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], to_score, from_max));
-            pv[e >> 3][e & 7] = (_Float16)sc[e];
-        }
-        // ---- second product
+            for (int u = 0; u < 2; ++u) {  // rows 0 .. G - 1: offsets; row 15: ones; the others are not used
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(values + L::kOffsetV + (min(m, G - 1) * kPage + 16 * r + 8 * u) * 2);
+                const u32x4 rows = {m == 15 ? 0x3C003C00u : w.x, m == 15 ? 0x3C003C00u : w.y, m == 15 ? 0x3C003C00u : w.z, m == 15 ? 0x3C003C00u : w.w};
+                rest = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, rows), pv[u], rest, 0, 0, 0);
+            }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {  // rows 0 .. G - 1: offsets; row 15: ones; the others are not used
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(vsrc + L::kOffsetV + (min(m, G - 1) * kPage + 16 * r + 8 * u) * 2);
-            const u32x4 rows = {m == 15 ? 0x3C003C00u : w.x, m == 15 ? 0x3C003C00u : w.y, m == 15 ? 0x3C003C00u : w.z, m == 15 ? 0x3C003C00u : w.w};
-            rest = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, rows), pv[u], rest, 0, 0, 0);
+            for (int j = 0; j < G; ++j) {
+                const u32x4 c = *reinterpret_cast<const u32x4 *>(values + L::kCodesV + (j * 64 + lane) * 16);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const h8 step = step_of(j, u);
+                    h8 p;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
+                    const uint32_t c0 = c[2 * u], c1 = c[2 * u + 1];
+                    const u32x4 lo = {c0 & mask_lo, (c0 >> 8) & mask_lo, c1 & mask_lo, (c1 >> 8) & mask_lo};
+                    const u32x4 hi = {c0 & mask_hi, (c0 >> 8) & mask_hi, c1 & mask_hi, (c1 >> 8) & mask_hi};
+                    acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, lo), p, acc[2 * j], 0, 0, 0);
+                    acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, hi), p, acc[2 * j + 1], 0, 0, 0);
+                    acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_lo), p, acc[2 * j], 0, 0, 0);
+                    acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_hi), p, acc[2 * j + 1], 0, 0, 0);
+                }
+            }
+            wait_copies<63>();
+            if (more) copy(next, 1);
+            page = next;
         }
+
+        // ---- output row m (2^kFactor times, unnormalized), its maximum and sum
+        const float back = 16777216.0f, sum = __shfl(rest[3], 48 + m, 64), inv = sum > 0.0f ? 1.0f / sum : 0.0f;  // (a row that sees nothing: 0)
+        const size_t part = partial_of(unit, worker, units.share) * 16 + m;
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-            const u32x4 c = *reinterpret_cast<const u32x4 *>(vsrc + L::kCodesV + (j * 64 + lane) * 16);
+            const float off = __shfl(rest[j & 3], (j >> 2) * 16 + m, 64);
+            v4f o[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const h8 step = step_of(j, u);
-                h8 p;
+            for (int i = 0; i < 4; ++i) {
+                o[0][i] = fmaf(acc[2 * j][i], back, off);
+                o[1][i] = fmaf(acc[2 * j + 1][i], back * 0.0625f, off);
+            }
+            if (!real) continue;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
-                const uint32_t c0 = c[2 * u], c1 = c[2 * u + 1];
-                const u32x4 lo = {c0 & mask_lo, (c0 >> 8) & mask_lo, c1 & mask_lo, (c1 >> 8) & mask_lo};
-                const u32x4 hi = {c0 & mask_hi, (c0 >> 8) & mask_hi, c1 & mask_hi, (c1 >> 8) & mask_hi};
-                acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, lo), p, acc[2 * j], 0, 0, 0);
-                acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, hi), p, acc[2 * j + 1], 0, 0, 0);
-                acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_lo), p, acc[2 * j], 0, 0, 0);
-                acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_hi), p, acc[2 * j + 1], 0, 0, 0);
+            for (int k = 0; k < 2; ++k) {
+                const int d = 32 * j + 16 * k + 4 * r;
+                if (whole)
+                    *reinterpret_cast<h4 *>(a.out + at + d) = h4{(_Float16)(o[k][0] * inv), (_Float16)(o[k][1] * inv), (_Float16)(o[k][2] * inv), (_Float16)(o[k][3] * inv)};
+                else
+                    *reinterpret_cast<v4f *>(a.ws_o + part * D + d) = o[k];
             }
         }
-        wait_copies<63>();
-        if (i + R::DEPTH < count) copy(i + R::DEPTH, slot, 1);
-    }
-
-    // ---- output row m (2^kFactor times, unnormalized), its maximum and sum
-    const float back = 16777216.0f, sum = __shfl(rest[3], 48 + m, 64), inv = sum > 0.0f ? 1.0f / sum : 0.0f;  // (a row that sees nothing: 0)
-    const size_t part = partial_of(unit, worker, units.share) * 16 + m;
-#pragma unroll
-    for (int j = 0; j < G; ++j) {
-        const float off = __shfl(rest[j & 3], (j >> 2) * 16 + m, 64);
-        v4f o[2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            o[0][i] = fmaf(acc[2 * j][i], back, off);
-            o[1][i] = fmaf(acc[2 * j + 1][i], back * 0.0625f, off);
+        if (real && !whole && r == 0) {
+            a.ws_ml[part * 2] = run_max;
+            a.ws_ml[part * 2 + 1] = sum;
         }
-        if (!real) continue;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int d = 32 * j + 16 * k + 4 * r;
-            if (whole)
-                *reinterpret_cast<h4 *>(a.out + at + d) = h4{(_Float16)(o[k][0] * inv), (_Float16)(o[k][1] * inv), (_Float16)(o[k][2] * inv), (_Float16)(o[k][3] * inv)};
-            else
-                *reinterpret_cast<v4f *>(a.ws_o + part * D + d) = o[k];
-        }
-    }
-    if (real && !whole && r == 0) {
-        a.ws_ml[part * 2] = run_max;
-        a.ws_ml[part * 2 + 1] = sum;
-    }
     }
 }
 
@@ -488,10 +482,10 @@ struct ManyArgs {
     int *plan;
     const char *pages;
     _Float16 *kc, *vc;  // [slots, h_kv, positions, D], [slots, h_kv, positions / 64, D, 64]
-    int g, h_kv, slots, records, block_rows, chunk_steps, max_pages;
+    int g, h_kv, slots, records, block_rows, chunk_steps, max_pages, few;
 };
 
-// One workgroup: the list of the requests with more than kFewRows rows, and how many workgroups each takes (per block of rows one for a chunk of its steps).  A request with a missing
+// One workgroup: the list of the requests with more than `few` rows, and how many workgroups each takes (per block of rows one for a chunk of its steps).  A request with a missing
 // page, or with fewer positions than tokens, is none of them: the kernel for few rows takes it.
 __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
     __shared__ uint64_t wanted[4];
@@ -503,7 +497,7 @@ __global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
         bool many = false;
         if (b < a.req.batch) {
             const Span s = span_of(a.req, b);
-            many = s.count * a.g > kFewRows && s.positions >= s.count;
+            many = s.count * a.g > a.few && s.positions >= s.count;
             if (!many) a.plan[ManyRows::kSlots + b] = -1;
         }
         const uint64_t mask = __ballot(many);
@@ -611,7 +605,7 @@ hipError_t launch(const AttnQ4Args &a, const ManyArgs &many, const AttnQ4Plan &p
         attn_q4_list_kernel<<<1, 256, 0, st>>>(many);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    constexpr size_t lds = Ring<D>::LDS;
+    constexpr size_t lds = Place<D>::LDS;
     if (const hipError_t e = allow_dynamic_lds<attn_q4_kernel<D>>(lds); e != hipSuccess) return e;
     attn_q4_kernel<D><<<(unsigned)((a.workers + 3) / 4), 256, lds, st>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -639,7 +633,7 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     p.all_rows = (long)tokens * g;
     p.blocks = p.rows <= 16 ? batch : (p.all_rows + 15) / 16 + batch;
     // few rows: as many wavefronts as the card holds at once
-    const long waves = 4L * num_cus * (d == 64 ? Ring<64>::WGS : d == 128 ? Ring<128>::WGS : Ring<256>::WGS), most_pages = p.blocks * h_kv * p.pages;
+    const long waves = 4L * num_cus * kWgs, most_pages = p.blocks * h_kv * p.pages;
     p.least = (p.pages + 2 + 253) / 254;  // (a unit is cut into 254 whole shares and two ends at most: the combination's four wavefronts take 64 each)
     if (const int forced = tuning().attn_q4_pages; forced > p.least) p.least = forced;
     const long shares = (most_pages + p.least - 1) / p.least;
@@ -650,8 +644,9 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     p.partial = 0;
     if (p.shared) p.total += up256((size_t)p.workers * 2 * 16 * (d + 2) * sizeof(float));
     // many rows
-    if (p.rows <= kFewRows) return p;
-    const long most = p.all_rows / (kFewRows + 1);
+    const int few = few_rows(p.all_rows);
+    if (p.rows <= few) return p;
+    const long most = p.all_rows / (few + 1);
     p.slots = (int)(most < batch ? most : batch);
     if (p.slots > kMaxSlots) p.slots = kMaxSlots;
     if (p.slots == 0) return p;
@@ -694,7 +689,7 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
         many.pages = a.pages;
         many.kc = kc, many.vc = vc;
         many.g = a.g, many.h_kv = h_kv, many.slots = p.slots, many.records = p.records, many.block_rows = 128 / p.shares, many.chunk_steps = p.chunk_steps;
-        many.max_pages = p.pages;
+        many.max_pages = p.pages, many.few = few_rows(p.all_rows);
     }
     hipError_t e = hipErrorInvalidValue;
     switch (d) {
