@@ -474,6 +474,7 @@ qfc_status_t qfc_rotary_table(const qfc_rotary_t *rotary, int32_t positions, flo
 qfc_status_t qfc_append_q4(const void *qkv_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_rotary_t *rotary, const float *rope_table, int32_t table_positions,
                            const qfc_q4_cache_t *cache, void *q_out, void *stream) {
     if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
+    if (requests->tokens == 0) return QFC_OK;
     if (!qkv_f16 || !q_out) return QFC_ERR_INVALID_ARG;
     if (!aligned16(qkv_f16) || !aligned16(q_out)) return QFC_ERR_ALIGNMENT;
     if (rotary) {
@@ -482,7 +483,6 @@ qfc_status_t qfc_append_q4(const void *qkv_f16, const qfc_requests_t *requests, 
         if (!rope_table || table_positions < requests->max_context) return QFC_ERR_INVALID_ARG;
         if (!aligned(rope_table, 8)) return QFC_ERR_ALIGNMENT;
     }
-    if (requests->tokens == 0) return QFC_OK;
     const int cus = device_cus();
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_append_q4(qkv_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, rotary ? rotary->rot_dim : 0,
@@ -491,10 +491,12 @@ qfc_status_t qfc_append_q4(const void *qkv_f16, const qfc_requests_t *requests, 
 
 qfc_status_t qfc_read_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, void *k, void *v, void *stream) {
     if (const qfc_status_t s = check_requests(requests, cache ? cache->h_kv : 0, cache); s != QFC_OK) return s;
+    if (requests->tokens == 0) return QFC_OK;
     if (!k || !v) return QFC_ERR_INVALID_ARG;
     if (!aligned16(k) || !aligned16(v)) return QFC_ERR_ALIGNMENT;
-    if (requests->tokens == 0) return QFC_OK;
-    return hip_status(launch_read_q4(on_device(requests, cache), cache->h_kv, cache->d_head, cache->pages, k, v, static_cast<hipStream_t>(stream)));
+    const int cus = device_cus();
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_read_q4(on_device(requests, cache), cache->h_kv, cache->d_head, cache->pages, k, v, cus, static_cast<hipStream_t>(stream)));
 }
 
 static AttnQ4Plan attention_plan(const qfc_requests_t *r, int32_t h_q, const qfc_q4_cache_t *c, int cus) {
@@ -511,6 +513,7 @@ qfc_status_t qfc_attention_q4_workspace_size(const qfc_requests_t *requests, int
 qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, void *workspace, size_t workspace_bytes,
                               void *out_f16, void *stream) {
     if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
+    if (requests->tokens == 0) return QFC_OK;
     if (!q_f16 || !workspace || !out_f16) return QFC_ERR_INVALID_ARG;
     if (!aligned16(q_f16) || !aligned16(workspace) || !aligned16(out_f16)) return QFC_ERR_ALIGNMENT;
     const int cus = device_cus();
@@ -518,7 +521,6 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
     if (workspace_bytes < p.total) return QFC_ERR_BUFFER_TOO_SMALL;
     // (places in the run of all pages, two more for each unit of 16 rows)
     if ((long)p.slots * cache->h_kv * p.pages > INT32_MAX || p.blocks * cache->h_kv * (p.pages + 2) > INT32_MAX - (1 << 24)) return QFC_ERR_UNSUPPORTED;
-    if (requests->tokens == 0) return QFC_OK;
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_attention_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, p, workspace, out_f16, cus,
                                           static_cast<hipStream_t>(stream)));
@@ -526,8 +528,8 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
 
 static qfc_status_t check_adapters(const qfc_adapters_t *a, int32_t M) {
     if (!a || M < 1 || a->count < 1 || a->K < 32 || a->K % 32 != 0 || a->N < 1 || a->rank < 1) return QFC_ERR_INVALID_ARG;
-    // (the launches' second dimensions)
-    return a->rank % 8 == 0 && a->rank <= 128 && a->N <= 65535 * 128 ? QFC_OK : QFC_ERR_UNSUPPORTED;
+    // (M / 64 blocks of rows times N / 2048 pieces of columns are one dimension of a launch)
+    return a->rank % 8 == 0 && a->rank <= 128 && a->N <= 1 << 23 && M <= 1 << 24 ? QFC_OK : QFC_ERR_UNSUPPORTED;
 }
 
 qfc_status_t qfc_adapters_workspace_size(const qfc_adapters_t *adapters, int32_t M, size_t *bytes) {

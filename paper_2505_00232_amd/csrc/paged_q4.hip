@@ -29,6 +29,17 @@ __device__ __forceinline__ int request_of(const Requests &q, int first, int mine
     return b;
 }
 
+// Tiles of tokens are dealt four by four to the XCDs (workgroup i runs on XCD i % 8): a page's lines, of which each tile has a part, then meet in one L2 (4096 tokens appended and read
+// 38.6 us, dealt one by one 39.5).
+constexpr int kTiles = 4;
+__device__ __forceinline__ int tile_of_block(unsigned x) { return (int)((x / (8 * kTiles) * 8 + x % 8) * kTiles + x / 8 % kTiles); }
+// Heads one workgroup takes: as few as still fit the card at once, `fit` workgroups per compute unit
+int heads_of_workgroup(long tiles, int heads, long fit) {
+    const long per = fit > 0 ? tiles * heads / fit : 1;
+    return (int)(per < 1 ? 1 : per > heads ? heads : per);
+}
+unsigned blocks_of_tiles(long tiles) { return (unsigned)((tiles + 8 * kTiles - 1) / (8 * kTiles) * (8 * kTiles)); }
+
 // x0 c + x1 s, rounded to binary16 once: both products with their rounding errors (fma), their sum with its own (Knuth's two-sum); what the last sum
 // rounds off decides its lowest bit (rounding to odd), so that the conversion to binary16 rounds the real result.  Without a correction the plain sum stands
 // (a zero keeps its sign, an infinite x gives what it gives).
@@ -41,16 +52,29 @@ __device__ __forceinline__ _Float16 rotated(float x0, float c, float x1, float s
     return (_Float16)(low < 0.0f || low > 0.0f ? (off != 0.0f ? __int_as_float(odd) : r) : sum);
 }
 
+// An octet of them.  x0 c + x1 s with two roundings is off by 2^-24 (|x0 c| + 2 |sum|) at most; where the values that far to both sides of it round to the same binary16,
+// that is the result, and only the others (one in some 700) are worked out as above.
+__device__ __forceinline__ h8 rotated8(const h8 &x, const h8 &other, const float (&c)[8], const float (&s)[8]) {
+    constexpr float off = 1.25f / 8388608.0f;
+    h8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float p = (float)x[e] * c[e], sum = fmaf((float)other[e], s[e], p), size = fabsf(p) + fabsf(sum);
+        const _Float16 low = (_Float16)fmaf(-off, size, sum), high = (_Float16)fmaf(off, size, sum);
+        y[e] = low;
+        if (__builtin_expect(__any(bits16(low) != bits16(high)), 0)) y[e] = rotated((float)x[e], c[e], (float)other[e], s[e]);
+    }
+    return y;
+}
+
 // Eight of the 32 values of a group, the others in the three neighbours of this lane's quad: their codes (value e in bits 4 e .. + 3), and the group's step and offset.
 __device__ __forceinline__ uint32_t quantize8(const h8 &x, _Float16 &step, _Float16 &offset) {
 #pragma clang fp contract(off)
-    float v[8], lo, hi;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        v[e] = (float)x[e];
-        lo = e == 0 ? v[0] : fminf(lo, v[e]);
-        hi = e == 0 ? v[0] : fmaxf(hi, v[e]);
-    }
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    const h4 lo4 = __builtin_elementwise_min(x.lo, x.hi), hi4 = __builtin_elementwise_max(x.lo, x.hi);
+    const h2 lo2 = __builtin_elementwise_min(lo4.lo, lo4.hi), hi2 = __builtin_elementwise_max(hi4.lo, hi4.hi);
+    float lo = fminf((float)lo2.x, (float)lo2.y), hi = fmaxf((float)hi2.x, (float)hi2.y);
 #pragma unroll
     for (int off = 1; off < 4; off <<= 1) {
         lo = fminf(lo, __shfl_xor(lo, off, 64));
@@ -62,7 +86,7 @@ __device__ __forceinline__ uint32_t quantize8(const h8 &x, _Float16 &step, _Floa
     uint32_t codes = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float u = (v[e] - zero) * inv;
+        const float u = ((float)x[e] - zero) * inv;
         codes |= (uint32_t)(int)fminf(fmaxf(rintf(u) + 8.0f, 0.0f), 15.0f) << (4 * e);
     }
     return codes;
@@ -78,7 +102,8 @@ struct AppendArgs {
 };
 
 // A workgroup takes 2048 / D consecutive token rows and heads_per_wg heads, one after the other; a thread one octet of a token's head.  The angles stay in its registers from
-// head to head.
+// head to head, the next head's octets are on their way.  Bound: the latency of arrays, page table, angles and stores one behind the other where tokens are few (64 requests 7 us), memory
+// and instructions about alike where they are many: 4096 tokens, 32 heads on 8 of 128 values, 25 us for 89 MB (3.5 TB/s).
 template <int D>
 __global__ __launch_bounds__(256) void append_q4_kernel(AppendArgs a) {
     typedef PageLayout<D> L;
@@ -86,8 +111,16 @@ __global__ __launch_bounds__(256) void append_q4_kernel(AppendArgs a) {
     __shared__ uint32_t vbytes[TT][D / 8];  // values of a token, a byte for every two
     __shared__ int at[TT][2];               // page (-1: none) and position of each token
     const int o = threadIdx.x % OCT, tt = threadIdx.x / OCT, lane = threadIdx.x & 63;
-    const int tok0 = (int)blockIdx.x * TT, tok = tok0 + tt;
+    const int tok0 = tile_of_block(blockIdx.x) * TT, tok = tok0 + tt;
+    if (tok0 >= a.req.tokens) return;
     const int heads = a.h_q + 2 * a.h_kv, head0 = (int)blockIdx.y * a.heads_per_wg, head1 = min(head0 + a.heads_per_wg, heads);
+
+    // An octet and what it is rotated with, a head ahead, the first before anything is known of the requests
+    const int half = a.rot / 2;
+    const bool turns = 8 * o < a.rot, first = 8 * o < half;
+    const int partner = !turns || a.interleaved ? o : first ? o + half / 8 : o - half / 8;
+    const _Float16 *src = a.qkv + ((size_t)min(tok, a.req.tokens - 1) * heads + head0) * D;
+    h8 x_next = *reinterpret_cast<const h8 *>(src + 8 * o), other_next = *reinterpret_cast<const h8 *>(src + 8 * partner);
 
     const int b = request_of<PER>(a.req, tok0 + tt / PER * PER, tt % PER, lane);
     bool mine = tok < a.req.tokens && b < a.req.batch;
@@ -102,10 +135,7 @@ __global__ __launch_bounds__(256) void append_q4_kernel(AppendArgs a) {
         at[tt][0] = page;
         at[tt][1] = pos;
     }
-    // cosine and signed sine of the octet's values; a value's partner: the octet `partner`, or its neighbour
-    const int half = a.rot / 2;
-    const bool turns = 8 * o < a.rot;
-    int partner = o;
+    // cosine and signed sine of the octet's values
     float c[8], s[8];
     if (turns && mine && head0 < a.h_q + a.h_kv) {
         const float2 *row = a.table + (size_t)max(pos, 0) * half;
@@ -117,8 +147,6 @@ __global__ __launch_bounds__(256) void append_q4_kernel(AppendArgs a) {
                 s[e] = e & 1 ? t.y : -t.y;
             }
         } else {
-            const bool first = 8 * o < half;
-            partner = first ? o + half / 8 : o - half / 8;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float2 t = row[(first ? 8 * o : 8 * o - half) + e];
@@ -128,16 +156,12 @@ __global__ __launch_bounds__(256) void append_q4_kernel(AppendArgs a) {
         }
     }
     for (int head = head0; head < head1; ++head) {
-        const _Float16 *src = a.qkv + ((size_t)(mine ? tok : 0) * heads + head) * D;
-        h8 x = {};
-        if (mine) x = *reinterpret_cast<const h8 *>(src + 8 * o);
-        if (head < a.h_q + a.h_kv && turns && mine) {
-            const h8 other = *reinterpret_cast<const h8 *>(src + 8 * partner);
-            h8 y;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = rotated((float)x[e], c[e], (float)(a.interleaved ? x[e ^ 1] : other[e]), s[e]);
-            x = y;
-        }
+        h8 x = x_next;
+        const h8 other = a.interleaved ? __builtin_shufflevector(x, x, 1, 0, 3, 2, 5, 4, 7, 6) : other_next;
+        src += head + 1 < head1 ? D : 0;
+        x_next = *reinterpret_cast<const h8 *>(src + 8 * o);
+        other_next = *reinterpret_cast<const h8 *>(src + 8 * partner);
+        if (head < a.h_q + a.h_kv && turns && mine) x = rotated8(x, other, c, s);
         if (head < a.h_q) {
             if (mine) *reinterpret_cast<h8 *>(a.q_out + ((size_t)tok * a.h_q + head) * D + 8 * o) = x;
             continue;
@@ -201,38 +225,42 @@ struct ReadArgs {
     const char *pages;
     _Float16 *k, *v;  // [tokens, h_kv, D]
     Requests req;
-    int h_kv;
+    int h_kv, heads_per_wg;
 };
 
-// The values the cache holds for the requests' new tokens; zeros where a token has no page
+// The values the cache holds for the requests' new tokens; zeros where a token has no page.  Bound: latency, arrays, table, codes and stores one behind the other (64 requests 4 us, 4096
+// tokens on 8 heads of 128 values 13 us for 22 MB).
 template <int D>
 __global__ __launch_bounds__(256) void read_q4_kernel(ReadArgs a) {
     typedef PageLayout<D> L;
     constexpr int OCT = D / 8, TT = 256 / OCT, PER = 64 / OCT;
     const int o = threadIdx.x % OCT, tt = threadIdx.x / OCT, lane = threadIdx.x & 63;
-    const int tok0 = (int)blockIdx.x * TT, tok = tok0 + tt, kv = blockIdx.y;
+    const int tok0 = tile_of_block(blockIdx.x) * TT, tok = tok0 + tt;
     const int b = request_of<PER>(a.req, tok0 + tt / PER * PER, tt % PER, lane);
     if (tok >= a.req.tokens || b >= a.req.batch) return;
     const Span s = span_of(a.req, b);
     if (tok < s.first || tok - s.first >= s.count) return;
     const int pos = s.positions - s.count + tok - s.first, page = pos >= 0 ? page_of(a.req, b, pos) : -1;
-    h8 k = {}, v = {};
-    if (page >= 0) {
-        const char *src = a.pages + ((size_t)page * a.h_kv + kv) * L::kBytes;
-        const int p = pos & (kPage - 1), j = o / 4;
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(src + L::code_k(p, j, o & 3));
-        const float sk = (float)*reinterpret_cast<const _Float16 *>(src + L::step_k(p, j)), ok = (float)*reinterpret_cast<const _Float16 *>(src + L::offset_k(p, j));
-        const float sv = (float)*reinterpret_cast<const _Float16 *>(src + L::step_v(p, j)), ov = (float)*reinterpret_cast<const _Float16 *>(src + L::offset_v(p, j));
+    const int p = pos & (kPage - 1), j = o / 4, kv1 = min(((int)blockIdx.y + 1) * a.heads_per_wg, a.h_kv);
+#pragma unroll 2
+    for (int kv = (int)blockIdx.y * a.heads_per_wg; kv < kv1; ++kv) {
+        h8 k = {}, v = {};
+        if (page >= 0) {
+            const char *src = a.pages + ((size_t)page * a.h_kv + kv) * L::kBytes;
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(src + L::code_k(p, j, o & 3));
+            const float sk = (float)*reinterpret_cast<const _Float16 *>(src + L::step_k(p, j)), ok = (float)*reinterpret_cast<const _Float16 *>(src + L::offset_k(p, j));
+            const float sv = (float)*reinterpret_cast<const _Float16 *>(src + L::step_v(p, j)), ov = (float)*reinterpret_cast<const _Float16 *>(src + L::offset_v(p, j));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            k[e] = (_Float16)fmaf((float)((w >> nibble(e)) & 15u) - 8.0f, sk, ok);
-            const uint32_t byte = (uint8_t)src[L::code_v(p, j, 8 * (o & 1) + e)];
-            v[e] = (_Float16)fmaf((float)((o & 2 ? byte >> 4 : byte) & 15u) - 8.0f, sv, ov);
+            for (int e = 0; e < 8; ++e) {
+                k[e] = (_Float16)fmaf((float)((w >> nibble(e)) & 15u) - 8.0f, sk, ok);
+                const uint32_t byte = (uint8_t)src[L::code_v(p, j, 8 * (o & 1) + e)];
+                v[e] = (_Float16)fmaf((float)((o & 2 ? byte >> 4 : byte) & 15u) - 8.0f, sv, ov);
+            }
         }
+        const size_t dst = ((size_t)tok * a.h_kv + kv) * D + 8 * o;
+        *reinterpret_cast<h8 *>(a.k + dst) = k;
+        *reinterpret_cast<h8 *>(a.v + dst) = v;
     }
-    const size_t dst = ((size_t)tok * a.h_kv + kv) * D + 8 * o;
-    *reinterpret_cast<h8 *>(a.k + dst) = k;
-    *reinterpret_cast<h8 *>(a.v + dst) = v;
 }
 
 // table[p][i] = amplitude (cos, sin) of p f_i, in fp64 as far as the rounding to 32 bits
@@ -270,9 +298,9 @@ hipError_t launch_append_q4(const void *qkv, const Requests &req, int h_q, int h
     a.h_q = h_q, a.h_kv = h_kv, a.rot = rot, a.interleaved = interleaved;
     const int tt = 2048 / d, heads = h_q + 2 * h_kv;
     const long tiles = (req.tokens + tt - 1) / tt;
-    long per = tiles * heads / (8L * num_cus);
-    a.heads_per_wg = (int)(per < 1 ? 1 : per > heads ? heads : per);
-    const dim3 grid((unsigned)tiles, (unsigned)((heads + a.heads_per_wg - 1) / a.heads_per_wg));
+    // (70 registers: seven fit.  4096 tokens, 32 heads on 8 of 128 values, with 4 / 5 / 6 / 7 / 8 of them: 28 / 25 / 25 / 30 / 30 us)
+    a.heads_per_wg = heads_of_workgroup(tiles, heads, 6L * num_cus);
+    const dim3 grid(blocks_of_tiles(tiles), (unsigned)((heads + a.heads_per_wg - 1) / a.heads_per_wg));
     if (d == 64)
         append_q4_kernel<64><<<grid, 256, 0, st>>>(a);
     else if (d == 128)
@@ -282,15 +310,16 @@ hipError_t launch_append_q4(const void *qkv, const Requests &req, int h_q, int h
     return hipGetLastError();
 }
 
-hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, hipStream_t st) {
+hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, int num_cus, hipStream_t st) {
     ReadArgs a;
     a.pages = static_cast<const char *>(pages);
     a.k = static_cast<_Float16 *>(k);
     a.v = static_cast<_Float16 *>(v);
     a.req = req;
-    a.h_kv = h_kv;
     const int tt = 2048 / d;
-    const dim3 grid((unsigned)((req.tokens + tt - 1) / tt), (unsigned)h_kv);
+    const long tiles = (req.tokens + tt - 1) / tt;
+    a.h_kv = h_kv, a.heads_per_wg = heads_of_workgroup(tiles, h_kv, 8L * num_cus);
+    const dim3 grid(blocks_of_tiles(tiles), (unsigned)((h_kv + a.heads_per_wg - 1) / a.heads_per_wg));
     if (d == 64)
         read_q4_kernel<64><<<grid, 256, 0, st>>>(a);
     else if (d == 128)

@@ -389,7 +389,7 @@ hipError_t launch_rotary_table(int rot, double base, double factor, int original
 // rot 0: no rotation, table unused
 hipError_t launch_append_q4(const void *qkv, const Requests &req, int h_q, int h_kv, int d, int rot, bool interleaved, const float *table, void *pages, void *q_out,
                             int num_cus, hipStream_t st);
-hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, hipStream_t st);
+hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, int num_cus, hipStream_t st);
 // Attention of requests with many query rows: which they are, and how their walks are cut, is found on the device (attention_q4.hip) and left as a list of int32.
 struct ManyRows {
     static constexpr int kCount = 0, kItems = 1, kSlots = 4;  // requests, their workgroups per KV head; from kSlots on each request's place in the list or -1
