@@ -457,12 +457,12 @@ def qfc_embedding(h, ids: torch.Tensor, y: torch.Tensor):
 _u8, _i32 = torch.uint8, torch.int32
 
 
-def _here(*tensors):
-    """The calls below launch on the current device: their tensors have to be there."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t.device.index != dev:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+def _here(*devices):
+    """The calls below launch on the current device: their tensors (given by their devices' numbers) have to be there."""
+    dev = _device() if _device is not None else torch.cuda.current_device()
+    for d in devices:
+        if d != dev:
+            raise ValueError(f"a tensor is on cuda:{d}, the current device is cuda:{dev}")
 
 
 class PagedCache:
@@ -477,6 +477,7 @@ class PagedCache:
         if self.pages.numel() < need:
             raise ValueError(f"pages: {self.pages.numel()} bytes, {need} are needed")
         self.desc.pages = self.pages.data_ptr()
+        self.ref, self.device = ctypes.byref(self.desc), self.pages.get_device()
 
 
 class Requests:
@@ -492,10 +493,11 @@ class Requests:
             raise ValueError("page_table: a matrix is required")
         _want(page_table, _i32, (batch, page_table.shape[1]), "page_table")
         self.token_start, self.context, self.page_table = token_start, context, page_table
-        self.tokens, self.device = tokens, context.device
-        if token_start.device != self.device or page_table.device != self.device:
+        self.tokens, self.device = tokens, context.get_device()
+        if token_start.get_device() != self.device or page_table.get_device() != self.device:
             raise ValueError("token_start, context and page_table: on different devices")
         self.desc = RequestsDesc(token_start.data_ptr(), context.data_ptr(), page_table.data_ptr(), batch, tokens, max_tokens, max_context, page_table.shape[1])
+        self.ref = ctypes.byref(self.desc)
 
 
 def make_rotary(rot_dim: int, base: float, layout: int = QFC_ROPE_HALF, factor: float = 1.0, original_positions: int = 0, low_turns: float = 1.0,
@@ -514,8 +516,8 @@ def qfc_rotary_table(rotary: Rotary, positions: int, device="cuda") -> torch.Ten
     if positions < 1 or rotary.rot_dim < 2:
         raise ValueError("positions and rot_dim: at least one pair of one position")
     table = torch.empty((positions, rotary.rot_dim // 2, 2), dtype=_f32, device=device)
-    _here(table)
-    _check(lib().qfc_rotary_table(ctypes.byref(rotary), positions, table.data_ptr(), _stream()), "qfc_rotary_table")
+    _here(table.get_device())
+    _check(lib().qfc_rotary_table(rotary, positions, table.data_ptr(), _stream()), "qfc_rotary_table")
     return table
 
 
@@ -525,29 +527,31 @@ def qfc_append_q4(qkv: torch.Tensor, requests: Requests, h_q: int, rotary: Rotar
     T, d = requests.tokens, cache.d_head
     _want(qkv, _f16, (T, (h_q + 2 * cache.h_kv) * d), "qkv")
     _want(q_out, _f16, (T, h_q * d), "q_out")
-    rows = 0
-    if rotary is not None:
+    if rotary is None:
+        _here(qkv.get_device(), q_out.get_device(), cache.device, requests.device)
+        status = lib().qfc_append_q4(qkv.data_ptr(), requests.ref, h_q, None, None, 0, cache.ref, q_out.data_ptr(), _stream())
+    else:
         if not isinstance(rope_table, _Tensor):
             raise ValueError("rope_table: a CUDA tensor is required")
         rows = rope_table.shape[0]
         _want(rope_table, _f32, (rows, rotary.rot_dim // 2, 2), "rope_table")
-        _here(rope_table)
-    _here(qkv, q_out, cache.pages, requests)
-    _check(lib().qfc_append_q4(qkv.data_ptr(), ctypes.byref(requests.desc), h_q, ctypes.byref(rotary) if rotary is not None else None,
-                               rope_table.data_ptr() if rotary is not None else None, rows, ctypes.byref(cache.desc), q_out.data_ptr(), _stream()), "qfc_append_q4")
+        _here(qkv.get_device(), q_out.get_device(), rope_table.get_device(), cache.device, requests.device)
+        status = lib().qfc_append_q4(qkv.data_ptr(), requests.ref, h_q, rotary, rope_table.data_ptr(), rows, cache.ref, q_out.data_ptr(), _stream())
+    _check(status, "qfc_append_q4")
 
 
 def qfc_read_q4(requests: Requests, cache: PagedCache, k: torch.Tensor, v: torch.Tensor):
     """The values the cache holds for the requests' new tokens: k, v float16 [tokens, h_kv, d_head]."""
-    _want(k, _f16, (requests.tokens, cache.h_kv, cache.d_head), "k")
-    _want(v, _f16, (requests.tokens, cache.h_kv, cache.d_head), "v")
-    _here(k, v, cache.pages, requests)
-    _check(lib().qfc_read_q4(ctypes.byref(requests.desc), ctypes.byref(cache.desc), k.data_ptr(), v.data_ptr(), _stream()), "qfc_read_q4")
+    shape = (requests.tokens, cache.h_kv, cache.d_head)
+    _want(k, _f16, shape, "k")
+    _want(v, _f16, shape, "v")
+    _here(k.get_device(), v.get_device(), cache.device, requests.device)
+    _check(lib().qfc_read_q4(requests.ref, cache.ref, k.data_ptr(), v.data_ptr(), _stream()), "qfc_read_q4")
 
 
 def qfc_attention_q4_workspace_size(requests: Requests, h_q: int, cache: PagedCache) -> int:
     out = ctypes.c_size_t(0)
-    _check(lib().qfc_attention_q4_workspace_size(ctypes.byref(requests.desc), h_q, ctypes.byref(cache.desc), ctypes.byref(out)), "qfc_attention_q4_workspace_size")
+    _check(lib().qfc_attention_q4_workspace_size(requests.ref, h_q, cache.ref, ctypes.byref(out)), "qfc_attention_q4_workspace_size")
     return out.value
 
 
@@ -556,9 +560,8 @@ def qfc_attention_q4(q: torch.Tensor, requests: Requests, h_q: int, cache: Paged
     _want(q, _f16, shape, "q")
     _want(out, _f16, shape, "out")
     _want(workspace, _u8, None, "workspace")
-    _here(q, out, workspace, cache.pages, requests)
-    _check(lib().qfc_attention_q4(q.data_ptr(), ctypes.byref(requests.desc), h_q, ctypes.byref(cache.desc), workspace.data_ptr(), workspace.numel(), out.data_ptr(),
-                                  _stream()), "qfc_attention_q4")
+    _here(q.get_device(), out.get_device(), workspace.get_device(), cache.device, requests.device)
+    _check(lib().qfc_attention_q4(q.data_ptr(), requests.ref, h_q, cache.ref, workspace.data_ptr(), workspace.numel(), out.data_ptr(), _stream()), "qfc_attention_q4")
 
 
 class Adapters:
@@ -574,12 +577,16 @@ class Adapters:
         _want(b, _f16, (count, N, rank), "b")
         _want(scale, _f32, (count,), "scale")
         self.a, self.b, self.scale, self.count, self.rank, self.K, self.N = a, b, scale, count, rank, K, N
+        self.device = a.get_device()
+        if b.get_device() != self.device or scale.get_device() != self.device:
+            raise ValueError("a, b and scale: on different devices")
         self.desc = AdaptersDesc(a.data_ptr(), b.data_ptr(), scale.data_ptr(), count, rank, K, N)
+        self.ref = ctypes.byref(self.desc)
 
 
 def qfc_adapters_workspace_size(adapters: Adapters, M: int) -> int:
     out = ctypes.c_size_t(0)
-    _check(lib().qfc_adapters_workspace_size(ctypes.byref(adapters.desc), M, ctypes.byref(out)), "qfc_adapters_workspace_size")
+    _check(lib().qfc_adapters_workspace_size(adapters.ref, M, ctypes.byref(out)), "qfc_adapters_workspace_size")
     return out.value
 
 
@@ -587,12 +594,13 @@ def qfc_add_adapters(x: torch.Tensor, ids: torch.Tensor, adapters: Adapters, y: 
     """out = y + scale[a] B[a] (A[a] x), row by row with a = ids[row]; out may be y."""
     M = _rows(x, _f16, adapters.K, "x")
     _want(ids, _i32, (M,), "ids")
-    _want(y, _f16, (M, adapters.N), "y")
-    _want(out, _f16, (M, adapters.N), "out")
+    shape = (M, adapters.N)
+    _want(y, _f16, shape, "y")
+    _want(out, _f16, shape, "out")
     _want(workspace, _u8, None, "workspace")
-    _here(x, ids, y, out, workspace, adapters.a, adapters.b, adapters.scale)
-    _check(lib().qfc_add_adapters(x.data_ptr(), M, ids.data_ptr(), ctypes.byref(adapters.desc), y.data_ptr(), workspace.data_ptr(), workspace.numel(), out.data_ptr(),
-                                  _stream()), "qfc_add_adapters")
+    _here(x.get_device(), ids.get_device(), y.get_device(), out.get_device(), workspace.get_device(), adapters.device)
+    _check(lib().qfc_add_adapters(x.data_ptr(), M, ids.data_ptr(), adapters.ref, y.data_ptr(), workspace.data_ptr(), workspace.numel(), out.data_ptr(), _stream()),
+           "qfc_add_adapters")
 
 
 class ForwardBatch:

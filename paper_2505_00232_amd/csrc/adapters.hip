@@ -368,7 +368,7 @@ AdapterPlan plan_adapters(int M, int K, int N, int num_cus) {
     const int blocks = (M + 15) / 16, pieces = (K + 127) / 128, pieces_n = (N + 127) / 128;
     // few rows: up to an adapter for every row, dealt to as many workgroups
     // (64 rows of 40 adapters, 4096 x 4096, 16 / 8 / 4 workgroups per block: 17.1 / 13.3 / 13.8 us; 128 rows 27.5 / 19.3 / 15.4; 16 rows 11.2 / 11.0 / 11.9)
-    p.dealt = 4 * num_cus / (blocks * pieces_n);
+    p.dealt = (int)(4L * num_cus / ((long)blocks * pieces_n));
     if (p.dealt > 16) p.dealt = 16;
     if (p.dealt > M) p.dealt = M;
     if (p.dealt < 1) p.dealt = 1;

@@ -140,6 +140,20 @@ def test_refusals_before_any_launch():
     assert add(ad(), n=16) == 3 and add(ad(), x=0x1008) == 4
 
 
+def test_refusals_of_the_largest_sizes_and_calls_without_tokens():
+    L = B.lib()
+    A, s, size = 0x1000, ctypes.c_void_p(0), ctypes.c_size_t(0)
+    ad = lambda N: ctypes.byref(B.AdaptersDesc(A, A, A, 2, 16, 64, N))
+    for M, N in (((1 << 24) + 1, 8), (1, (1 << 23) + 1), (2 ** 31 - 1, 2 ** 31 - 1)):
+        assert L.qfc_adapters_workspace_size(ad(N), M, ctypes.byref(size)) == 2
+        assert L.qfc_add_adapters(A, M, A, ad(N), A, A, 1 << 60, A, s) == 2
+    assert L.qfc_adapters_workspace_size(ad(1 << 23), 1 << 24, ctypes.byref(size)) == 0 and size.value >= (1 << 24) * 16 * 4
+    cache, none = ctypes.byref(B.CacheDesc(A, 4, 2, 64)), ctypes.byref(B.RequestsDesc(A, A, A, 2, 0, 1, 128, 2))
+    assert L.qfc_append_q4(None, none, 4, None, None, 0, cache, None, s) == 0 and L.qfc_read_q4(none, cache, None, None, s) == 0
+    assert L.qfc_attention_q4(None, none, 4, cache, None, 0, None, s) == 0
+    assert L.qfc_attention_q4(None, none, 3, cache, None, 0, None, s) == 1
+
+
 def test_binding_refuses_host_tensors():
     c = torch.zeros(2, dtype=torch.int32)
     with pytest.raises(ValueError):
@@ -585,3 +599,203 @@ def test_prompts_in_a_replayed_graph():
         B.qfc_attention_q4(q, req, h_q, cache, ws2, out2)
         torch.cuda.synchronize()
         assert torch.equal(out[:cuts[-1]], out2[:cuts[-1]]) and bool(torch.isfinite(out2).all())
+
+
+def _check_some(req, got, q, S, n, h_q, K, V, P, which):
+    """Requests `which` of an attention's result."""
+    first, d = np.concatenate([[0], np.cumsum(S)]), K[0].shape[-1]
+    for b in which:
+        rows = slice(first[b], first[b + 1])
+        want = ref.attention(q.reshape(-1, h_q, d)[rows], K[b], V[b], P[b])
+        _close(got.reshape(-1, h_q, d)[rows], *want, rows=S[b] * (h_q // K[b].shape[1]))
+
+
+@gpu
+@pytest.mark.parametrize("batch,longest,h_q,h_kv,d", [(130, 700, 4, 2, 64), (300, 200, 4, 1, 128), (100, 1500, 16, 8, 128), (90, 1900, 8, 8, 64)])
+def test_attention_of_more_requests_than_a_wavefront_has_lanes(batch, longest, h_q, h_kv, d):
+    """Single tokens, chunks and empty requests among them, few pages per wavefront and more than four; every request against the oracle."""
+    rng = np.random.default_rng(51)
+    n = [int(x) for x in rng.integers(1, longest + 1, batch)]
+    S = [int(min(rng.choice([1, 1, 1, 0, 3]), m)) for m in n]
+    S[5], n[5], n[64], S[64] = 1, 1, 1, 1
+    table, num = _pages(rng, n)
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num)
+    q, req = _normal(rng, sum(S), h_q * d), _requests(S, n, table)
+    got = _attend(req, q, h_q, cache)
+    _check_some(req, got, q, S, n, h_q, K, V, P, range(batch))
+
+
+@gpu
+def test_prompts_among_many_requests():
+    """More requests than the first kernel's threads, prompts before and behind the 256th."""
+    rng = np.random.default_rng(52)
+    batch, h_q, h_kv, d = 270, 4, 1, 64
+    n = [int(x) for x in rng.integers(1, 90, batch)]
+    S = [1] * batch
+    for b, s in ((0, 140), (3, 90), (200, 33), (255, 129), (256, 150), (269, 100)):
+        S[b], n[b] = s, s + b % 70
+    table, num = _pages(rng, n)
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num)
+    q, req = _normal(rng, sum(S), h_q * d), _requests(S, n, table)
+    _check_some(req, _attend(req, q, h_q, cache), q, S, n, h_q, K, V, P, range(batch))
+
+
+@gpu
+@pytest.mark.parametrize("least", [7, 70, 300])
+def test_attention_of_long_walks(least):
+    """Wavefronts that take more pages than a wavefront holds page numbers; the limits above the real lengths."""
+    rng = np.random.default_rng(53)
+    h_q, h_kv, d, n, S = 4, 1, 64, [9000, 4470, 64], [1, 2, 1]
+    table, num = _pages(rng, n, width=200)
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num)
+    q, req = _normal(rng, sum(S), h_q * d), _requests(S, n, table, max_tokens=4, max_context=200 * 64)
+    try:
+        B.lib().qfc_tune(15, least)
+        got = _attend(req, q, h_q, cache)
+    finally:
+        B.lib().qfc_tune(15, 0)
+    _check_some(req, got, q, S, n, h_q, K, V, P, range(3))
+
+
+@gpu
+def test_requests_that_share_pages():
+    """A common beginning held once: pages in several requests' rows of the table."""
+    rng = np.random.default_rng(54)
+    h_q, h_kv, d, common, n = 8, 2, 128, 256, [300, 420, 257]
+    table, num = _pages(rng, n)
+    table[:, :common // 64] = table[0, :common // 64]
+    k, v = _normal(rng, sum(n), h_kv, d), _normal(rng, sum(n), h_kv, d)
+    at = np.concatenate([[0], np.cumsum(n)])
+    for x in (k, v):
+        for b in (1, 2):
+            x[at[b]:at[b] + common] = x[:common]
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num, k, v)
+    q, req = _normal(rng, 3, h_q * d), _requests([1] * 3, n, table)
+    _check_some(req, _attend(req, q, h_q, cache), q, [1] * 3, n, h_q, K, V, P, range(3))
+
+
+@gpu
+def test_single_tokens_on_two_streams_at_once():
+    rng = np.random.default_rng(55)
+    h_q, h_kv, d, n = 8, 2, 128, [2000, 1500, 900]
+    table, num = _pages(rng, n)
+    cache, _, _, _ = _filled(rng, n, h_kv, d, table, num)
+    q, req = [_normal(rng, 3, h_q * d) for _ in range(2)], _requests([1] * 3, n, table)
+    alone = [_attend(req, x, h_q, cache) for x in q]
+    size = B.qfc_attention_q4_workspace_size(req, h_q, cache)
+    dev = [_t(x) for x in q]
+    out, ws, streams = [torch.zeros_like(x) for x in dev], [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in q], [torch.cuda.Stream() for _ in q]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                B.qfc_attention_q4(dev[i], req, h_q, cache, ws[i], out[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert np.array_equal(out[i].cpu().numpy().astype(np.float64), alone[i])
+
+
+@gpu
+def test_calls_without_tokens_and_with_wrong_tensors():
+    rng = np.random.default_rng(56)
+    table, num = _pages(rng, [64])
+    cache = B.PagedCache(num, 1, 64)
+    half = lambda *shape: torch.zeros(shape, dtype=torch.float16, device=DEV)
+    none = B.Requests(_t(np.zeros(2, dtype=np.int32)), _t(np.asarray([64], dtype=np.int32)), _t(table), 0, 1, 64)
+    B.qfc_append_q4(half(0, 4 * 64), none, 2, None, None, cache, half(0, 2 * 64))
+    B.qfc_read_q4(none, cache, half(0, 1, 64), half(0, 1, 64))
+    ws = torch.empty(max(B.qfc_attention_q4_workspace_size(none, 2, cache), 1), dtype=torch.uint8, device=DEV)
+    B.qfc_attention_q4(half(0, 2 * 64), none, 2, cache, ws, half(0, 2 * 64))
+    req = _requests([1], [64], table)
+    size = B.qfc_attention_q4_workspace_size(req, 2, cache)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    for q, w, out in ((half(1, 64), ws, half(1, 128)), (half(1, 128).float(), ws, half(1, 128)), (half(1, 128), ws, half(2, 128)), (half(1, 256)[:, ::2], ws, half(1, 128)),
+                      (torch.zeros((1, 128), dtype=torch.float16), ws, half(1, 128))):
+        with pytest.raises(ValueError):
+            B.qfc_attention_q4(q, req, 2, cache, w, out)
+    with pytest.raises(B.QfcError):
+        B.qfc_attention_q4(half(1, 128), req, 2, cache, ws[:size - 1], half(1, 128))
+    rotary = B.make_rotary(64, 10000.0)
+    with pytest.raises(B.QfcError):  # angles for fewer positions than the requests may have
+        B.qfc_append_q4(half(1, 4 * 64), req, 2, rotary, B.qfc_rotary_table(rotary, 63), cache, half(1, 128))
+    with pytest.raises(ValueError):
+        B.PagedCache(2, 1, 64, pages=torch.zeros(100, dtype=torch.uint8, device=DEV))
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N,rank,count", [(513, 128, 1000, 16, 6), (700, 160, 257, 64, 3), (640, 64, 6144, 8, 2), (1030, 96, 520, 128, 40), (2048, 256, 8200, 32, 5), (576, 64, 32, 40, 1)])
+def test_adapters_of_many_rows(M, K, N, rank, count):
+    """Blocks of many rows: whole and cut ones, one adapter and many in a block, none in some, tiles that the columns end inside of."""
+    rng = np.random.default_rng(34)
+    a, b, scale = _adapters(rng, count, rank, K, N)
+    x, y = _normal(rng, M, K), _normal(rng, M, N)
+    for ids in (np.full(M, count - 1), np.sort(rng.integers(-1, count, M)), rng.integers(0, count, M), rng.integers(-1, count + 1, M), np.repeat([0, -1, count - 1], [300, 100, M - 400])):
+        ids = ids.astype(np.int32)
+        got = _add(x, ids, a, b, scale, y)
+        _check_adapters(got, x, ids, a, b, scale, y)
+        assert np.array_equal(got, _add(x, ids, a, b, scale, y, alias=True))
+
+
+@gpu
+@pytest.mark.parametrize("M,N", [(700, 512), (700, 1000)])
+def test_adapters_of_many_rows_do_not_reach_other_rows(M, N):
+    rng = np.random.default_rng(35)
+    K, rank, count = 64, 16, 4
+    a, b, scale = _adapters(rng, count, rank, K, N)
+    x, y = _normal(rng, M, K), _normal(rng, M, N)
+    ids = (np.arange(M) // 7 % count).astype(np.int32)
+    clean = _add(x, ids, a, b, scale, y)
+    a[2], b[1, 5], scale[3] = np.inf, np.nan, np.inf
+    x[4], y[9] = np.nan, np.inf
+    got = _add(x, ids, a, b, scale, y)
+    same = (ids < 2)[:, None] & ~((ids == 1)[:, None] & (np.arange(N) == 5))
+    same[[4, 9]] = False
+    assert np.array_equal(got.view(np.uint16)[same], clean.view(np.uint16)[same])
+
+
+@gpu
+@pytest.mark.parametrize("M", [1, 48, 600])
+def test_adapters_in_a_replayed_graph(M):
+    """Rows and adapters that change from replay to replay; the output in place of the layer's."""
+    rng = np.random.default_rng(36)
+    K, N, rank, count = 512, 264, 16, 5
+    ad = B.Adapters(*(_t(t) for t in _adapters(rng, count, rank, K, N)))
+    x, y, ids = torch.zeros((M, K), dtype=torch.float16, device=DEV), torch.zeros((M, N), dtype=torch.float16, device=DEV), torch.zeros(M, dtype=torch.int32, device=DEV)
+    ws, ws2 = (torch.empty(B.qfc_adapters_workspace_size(ad, M), dtype=torch.uint8, device=DEV) for _ in range(2))
+    out = torch.empty_like(y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    B.qfc_add_adapters(x, ids, ad, y, ws2, out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        B.qfc_add_adapters(x, ids, ad, y, ws, y)
+    for _ in range(4):
+        x.copy_(_t(_normal(rng, M, K)))
+        y.copy_(_t(_normal(rng, M, N)))
+        ids.copy_(_t(rng.integers(-1, count + 1, M).astype(np.int32)))
+        B.qfc_add_adapters(x, ids, ad, y, ws2, out)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), y.view(torch.int16))
+
+
+@gpu
+def test_append_of_a_batch_is_append_one_by_one():
+    """Requests whose rows begin inside a tile, positions that begin inside a dword."""
+    rng = np.random.default_rng(57)
+    h_q, h_kv, d, S = 2, 1, 128, [5, 6, 1, 70]
+    n = [5, 70, 64, 133]
+    table, num = _pages(rng, n)
+    qkv = _normal(rng, sum(S), (h_q + 2 * h_kv) * d)
+    caches = [B.PagedCache(num, h_kv, d) for _ in range(2)]
+    for c in caches:
+        c.pages.fill_(0x5A)
+    out = torch.empty((sum(S), h_q * d), dtype=torch.float16, device=DEV)
+    B.qfc_append_q4(_t(qkv), _requests(S, n, table), h_q, None, None, caches[0], out)
+    at = 0
+    for b, s in enumerate(S):  # one request at a time
+        B.qfc_append_q4(_t(qkv[at:at + s]), _requests([s], [n[b]], table[b:b + 1]), h_q, None, None, caches[1], torch.empty((s, h_q * d), dtype=torch.float16, device=DEV))
+        at += s
+    assert torch.equal(caches[0].pages, caches[1].pages) and np.array_equal(out.cpu().numpy(), qkv[:, :h_q * d])
