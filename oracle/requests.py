@@ -57,13 +57,12 @@ def q4_values(codes, steps, offsets):
 
 def attention(q_f16, K, V, V_parts, there=None):
     """Attention of the last S of n positions: q [S, h_q, d]; K, V, V_parts [n, h_kv, d] fp64; there [n] (None: all): positions that are in the cache.
-    Returns (out, spread, slope), [S, h_q, d] each: out = softmax(q K^T / sqrt d) V (0 where nothing is seen), spread = sum p V_parts, slope =
-    (largest sum |q| |K| / sqrt d over the row's positions) sum p |V - out|: what a relative change of every key by 1 can move, to first order."""
+    Returns (out, spread), [S, h_q, d] each: out = softmax(q K^T / sqrt d) V (0 where nothing is seen), spread = sum p V_parts."""
     q = np.asarray(q_f16, dtype=np.float16).astype(np.float64)
     S, h_q, d = q.shape
     n, h_kv = K.shape[:2]
     g = h_q // h_kv
-    out, spread, slope = (np.zeros((S, h_q, d)) for _ in range(3))
+    out, spread = np.zeros((S, h_q, d)), np.zeros((S, h_q, d))
     for s in range(S):
         lim = n - S + s + 1
         if lim <= 0:
@@ -78,8 +77,7 @@ def attention(q_f16, K, V, V_parts, there=None):
             p /= p.sum()
             out[s, h] = p @ v
             spread[s, h] = p @ V_parts[see, h // g]
-            slope[s, h] = (np.abs(k) @ np.abs(q[s, h])).max() / np.sqrt(d) * (p @ np.abs(v - out[s, h]))
-    return out, spread, slope
+    return out, spread
 
 
 def adapters(x_f16, ids, a_f16, b_f16, scale, y_f16):

@@ -25,7 +25,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # Prefill attention holds the sums of the second product in accumulation registers, but its scores are vector operands at once:
 # with every MFMA writing accumulation registers they would be moved over one by one (us with / without: head size 256, 2048 tokens
 # 50.6 / 62.0; 128 and 64 level, and so is the kernel for few query rows in the same file, within the 1 % of two runs).
-SOURCE_FLAGS = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("attention.hip", "attention_q4.hip")}
+SOURCE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 # Kernels that load MFMA operands into registers with hand-written asynchronous loads and place the

@@ -506,7 +506,7 @@ static AttnQ4Plan attention_plan(const qfc_requests_t *r, int32_t h_q, const qfc
 qfc_status_t qfc_attention_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes) {
     if (!bytes) return QFC_ERR_INVALID_ARG;
     if (const qfc_status_t s = check_batch(requests, h_q, cache); s != QFC_OK) return s;
-    *bytes = attention_plan(requests, h_q, cache, device_cus()).total;
+    *bytes = attention_plan(requests, h_q, cache, device_cus()).bytes;
     return QFC_OK;
 }
 
@@ -518,9 +518,9 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
     if (!aligned16(q_f16) || !aligned16(workspace) || !aligned16(out_f16)) return QFC_ERR_ALIGNMENT;
     const int cus = device_cus();
     const AttnQ4Plan p = attention_plan(requests, h_q, cache, cus);
-    if (workspace_bytes < p.total) return QFC_ERR_BUFFER_TOO_SMALL;
-    // (places in the run of all pages, two more for each unit of 16 rows)
-    if ((long)p.slots * cache->h_kv * p.pages > INT32_MAX || p.blocks * cache->h_kv * (p.pages + 2) > INT32_MAX - (1 << 24)) return QFC_ERR_UNSUPPORTED;
+    if (workspace_bytes < p.bytes) return QFC_ERR_BUFFER_TOO_SMALL;
+    // (places in the run of all blocks' pages, some more for each)
+    if (p.blocks * cache->h_kv * (p.pages + 4) > INT32_MAX - (1 << 24)) return QFC_ERR_UNSUPPORTED;
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_attention_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, p, workspace, out_f16, cus,
                                           static_cast<hipStream_t>(stream)));

@@ -244,10 +244,6 @@ struct AttnArgs {
     int chunk_steps;  // prefill: > 0 = walks are cut into chunks of this many steps (one workgroup each)
     int max_chunks;   // prefill: chunk slots per query row in the workspace
     float scale;
-    // a batch of requests (prefill; groups = KV heads): what is known on the device only, see ManyRows
-    const int *plan;
-    int records, h_q;
-    long ws_rows;     // query rows of a KV head of all requests
 };
 // prefill: steps of 32 positions that the walk of block j of `rows` query rows takes (the last row of the block sees most)
 __host__ __device__ inline int prefill_steps(const AttnArgs &a, int j, int rows) {
@@ -566,26 +562,7 @@ __device__ __forceinline__ float both_halves_max(float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Of the requests in the plan (`field` ascending from record to record) the last whose field is at most x; -1 if there is none
-__device__ __forceinline__ int record_of(const AttnArgs &a, int field, int x) {
-    const int count = a.plan[ManyRows::kCount], lane = threadIdx.x & 63;
-    int below = 0;
-    for (int s0 = 0; s0 < count; s0 += 64)
-        below += __popcll(__ballot(s0 + lane < count && a.plan[a.records + (s0 + lane) * ManyRows::kRecord + field] <= x));
-    return __builtin_amdgcn_readfirstlane(below) - 1;
-}
-// ... and what `a` is for that request; row0: its first token row
-__device__ __forceinline__ void take_record(AttnArgs &a, int slot, int &row0) {
-    const int *r = a.plan + a.records + slot * ManyRows::kRecord;
-    row0 = __builtin_amdgcn_readfirstlane(r[ManyRows::kRow]);
-    a.S = __builtin_amdgcn_readfirstlane(r[ManyRows::kTokens]);
-    a.n_ctx = __builtin_amdgcn_readfirstlane(r[ManyRows::kPositions]);
-    a.chunk_steps = __builtin_amdgcn_readfirstlane(r[ManyRows::kChunkSteps]);
-    a.M = a.S * a.g;
-}
-
-// BATCH: requests of different lengths, token rows [tokens, h_q, D] (queries and output), a workgroup's request and work from the plan
-template <int D, int PS, bool BATCH = false>
+template <int D, int PS>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_prefill_kernel(AttnArgs a) {
     typedef float v16f __attribute__((ext_vector_type(16)));
     typedef PrefillCfg<D, PS> Cfg;
@@ -600,16 +577,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_prefill_kernel(Att
     const int rw = wave % RW, ps = wave / RW;
     const int q = lane & 31, h = lane >> 5;
     // (groups side by side: where 8 divides their number, the workgroups of one share the L2 of one XCD)
-    int G = (int)blockIdx.x % a.groups, item = (int)blockIdx.x / a.groups;
-    const int kv = G;
-    int row0 = 0;
-    if constexpr (BATCH) {
-        const int slot = item < a.plan[ManyRows::kItems] ? record_of(a, ManyRows::kItem, item) : -1;
-        if (slot < 0) return;
-        item -= __builtin_amdgcn_readfirstlane(a.plan[a.records + slot * ManyRows::kRecord + ManyRows::kItem]);
-        take_record(a, slot, row0);
-        G += slot * a.groups;
-    }
+    const int G = (int)blockIdx.x % a.groups, item = (int)blockIdx.x / a.groups;
     const int nblocks = (a.M + Cfg::ROWS - 1) / Cfg::ROWS;
     // Longest walks first: the compute units that finish theirs take the shorter ones.  a.chunk_steps > 0 (a multiple of
     // PS; few blocks): the walk of a block is cut into chunks of that many steps, one workgroup
@@ -637,13 +605,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_prefill_kernel(Att
     const int nb = chunks > 1 ? min(nb_all, sb + a.chunk_steps) : nb_all;
     const int lim = min(real ? a.n_ctx - a.S + m / a.g + 1 : a.n_ctx, 32 * nb);  // end of the positions the lane's row sees in them
 
-    const size_t row_at = BATCH ? (size_t)(row0 + m / a.g) * a.h_q + kv * a.g + m % a.g : (size_t)G * a.M + m;  // of queries and output
     // Q^T operand: lane (q, h) holds Q[m][16 j + 8 h .. + 7]
     h8 qf[DJ];
 #pragma unroll
     for (int j = 0; j < DJ; ++j) {
         const h8 zero = {0};
-        qf[j] = real ? *reinterpret_cast<const h8 *>(a.q + row_at * D + 16 * j + 8 * h) : zero;
+        qf[j] = real ? *reinterpret_cast<const h8 *>(a.q + ((size_t)G * a.M + m) * D + 16 * j + 8 * h) : zero;
     }
 
     // ---- copies: the KiB pieces of a step are dealt to the wavefronts in turn
@@ -860,8 +827,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_prefill_kernel(Att
     }
     if (!real) return;
     // lane (q, h) holds O^T rows d = 32 dt + 8 b + 4 h + r of column q: four consecutive d per b
-    const size_t slot = BATCH ? ((size_t)chunk * a.groups + kv) * a.ws_rows + (size_t)row0 * a.g + m
-                              : ((size_t)G * a.max_chunks + chunk) * a.M + m;  // (rows side by side: 4 KiB apart they meet in one memory channel)
+    const size_t slot = ((size_t)G * a.max_chunks + chunk) * a.M + m;  // (rows side by side: 4 KiB apart they meet in one memory channel)
     const float inv = 1.0f / run_sum;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -873,7 +839,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_prefill_kernel(Att
             if (chunks > 1)  // partial result: unnormalized O^T column, maximum (in units of log 2) and sum
                 *reinterpret_cast<v4f *>(a.ws_o + slot * D + d) = o;
             else
-                *reinterpret_cast<h4 *>(a.out + row_at * D + d) =
+                *reinterpret_cast<h4 *>(a.out + ((size_t)G * a.M + m) * D + d) =
                     h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
         }
     }
@@ -885,32 +851,22 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attn_prefill_kernel(Att
 
 // Chunked walks: the rows of blocks with more than one chunk.  One wavefront per query row; lane l
 // takes the D / 64 consecutive values from d = l D / 64.
-template <int D, bool BATCH = false>
+template <int D>
 __global__ __launch_bounds__(256) void attn_prefill_combine_kernel(AttnArgs a) {
     constexpr int PER = D / 64;
     const int lane = threadIdx.x & 63;
-    int m = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    const int m = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     const int G = blockIdx.y;
-    const int row = m;  // (BATCH: of all requests)
-    if constexpr (BATCH) {
-        if (m >= a.ws_rows) return;
-        int row0 = 0;
-        const int slot = record_of(a, ManyRows::kRow, m / a.g);
-        if (slot < 0) return;
-        take_record(a, slot, row0);
-        m -= row0 * a.g;
-    }
-    if (m >= a.M || (BATCH && a.chunk_steps == 0)) return;
+    if (m >= a.M) return;
     const int chunks = (prefill_steps(a, m / a.block_rows, a.block_rows) + a.chunk_steps - 1) / a.chunk_steps;
     if (chunks <= 1) return;  // written by the first kernel
-    const size_t slot0 = BATCH ? (size_t)G * a.ws_rows + row : (size_t)G * a.max_chunks * a.M + m;  // chunk c's: slot0 + c * per_chunk
-    const size_t per_chunk = BATCH ? (size_t)a.groups * a.ws_rows : (size_t)a.M;
+    const size_t slot0 = (size_t)G * a.max_chunks * a.M + m;  // chunk c's: slot0 + c * M
     // lane c < chunks holds chunk c's (maximum, sum); all loads of the row are requested at once
     static_assert(kPrefillMaxChunks == 8, "the reductions below cover eight lanes");
     float mx = kNegBig, l = 0.0f;
     if (lane < chunks) {
-        mx = a.ws_ml[(slot0 + lane * per_chunk) * 2];
-        l = a.ws_ml[(slot0 + lane * per_chunk) * 2 + 1];
+        mx = a.ws_ml[(slot0 + (size_t)lane * a.M) * 2];
+        l = a.ws_ml[(slot0 + (size_t)lane * a.M) * 2 + 1];
     }
     float part[kPrefillMaxChunks][PER];
 #pragma unroll
@@ -918,7 +874,7 @@ __global__ __launch_bounds__(256) void attn_prefill_combine_kernel(AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < PER; ++e) part[c][e] = 0.0f;
         if (c >= chunks) continue;  // (the same for the whole wavefront)
-        const float *src = a.ws_o + (slot0 + c * per_chunk) * D + lane * PER;
+        const float *src = a.ws_o + (slot0 + (size_t)c * a.M) * D + lane * PER;
 #pragma unroll
         for (int e = 0; e < PER; ++e) part[c][e] = src[e];
     }
@@ -941,7 +897,7 @@ __global__ __launch_bounds__(256) void attn_prefill_combine_kernel(AttnArgs a) {
         for (int e = 0; e < PER; ++e) o[e] = fmaf(fc, part[c][e], o[e]);
     }
     const float inv = 1.0f / den;
-    _Float16 *dst = a.out + (BATCH ? (size_t)(row / a.g) * a.h_q + G * a.g + row % a.g : (size_t)G * a.M + m) * D + lane * PER;
+    _Float16 *dst = a.out + ((size_t)G * a.M + m) * D + lane * PER;
 #pragma unroll
     for (int e = 0; e < PER; ++e) dst[e] = (_Float16)(o[e] * inv);
 }
@@ -961,18 +917,6 @@ hipError_t launch_attn_prefill(const AttnArgs &a, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.chunk_steps == 0) return e;
     attn_prefill_combine_kernel<D><<<dim3((unsigned)((a.M + 3) / 4), (unsigned)a.groups), 256, 0, st>>>(a);
-    return hipGetLastError();
-}
-
-template <int D, int PS>
-hipError_t launch_attn_many(AttnArgs a, int items, hipStream_t st) {
-    constexpr int lds = PrefillCfg<D, PS>::LDS;
-    if (const hipError_t e = allow_dynamic_lds<attn_prefill_kernel<D, PS, true>>(lds); e != hipSuccess) return e;
-    a.block_rows = PrefillCfg<D, PS>::ROWS;
-    attn_prefill_kernel<D, PS, true><<<dim3((unsigned)(items * a.groups)), 256, lds, st>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !a.ws_o) return e;
-    attn_prefill_combine_kernel<D, true><<<dim3((unsigned)((a.ws_rows + 3) / 4), (unsigned)a.groups), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -1199,36 +1143,6 @@ hipError_t launch_attention(const void *q, const void *kc, const void *vc, int G
         case 64: return launch_attn<64>(a, G, st);
         case 128: return launch_attn<128>(a, G, st);
         case 256: return launch_attn<256>(a, G, st);
-        default: return hipErrorInvalidValue;
-    }
-}
-
-// The plan for requests of up to S tokens and n_ctx positions, `groups` times a KV head: wavefronts that share a walk (returned), steps of a chunk (0: walks are whole).
-int plan_attention_many(int groups, int S, int g, int d, int n_ctx, int num_cus, int *chunk_steps) {
-    AttnArgs a = {};
-    a.M = S * g, a.g = g, a.S = S, a.n_ctx = n_ctx < S ? S : n_ctx, a.groups = groups;
-    const int shares = plan_prefill(a, d, num_cus);
-    *chunk_steps = a.chunk_steps;
-    return shares;
-}
-
-// The prompts of a batch of requests over binary16 copies of their caches (attention_q4.hip); shares: wavefronts that share a walk.
-hipError_t launch_attention_many(const void *q, const void *kc, const void *vc, int h_q, int h_kv, int d, int C, const int *plan, int records, int shares, int items,
-                                 long rows, float *partial, void *out, hipStream_t st) {
-    AttnArgs a = {};
-    a.q = static_cast<const _Float16 *>(q);
-    a.kc = static_cast<const _Float16 *>(kc);
-    a.vc = static_cast<const _Float16 *>(vc);
-    a.out = static_cast<_Float16 *>(out);
-    a.g = h_q / h_kv, a.h_q = h_q, a.groups = h_kv, a.C = C;
-    a.scale = 1.4426950408889634f / sqrtf((float)d);
-    a.plan = plan, a.records = records, a.ws_rows = rows, a.max_chunks = kPrefillMaxChunks;
-    a.ws_o = partial;
-    a.ws_ml = partial ? partial + (size_t)kPrefillMaxChunks * h_kv * rows * d : nullptr;
-    switch (d) {
-        case 64: return shares == 1 ? launch_attn_many<64, 1>(a, items, st) : launch_attn_many<64, 2>(a, items, st);
-        case 128: return shares == 1 ? launch_attn_many<128, 1>(a, items, st) : launch_attn_many<128, 2>(a, items, st);
-        case 256: return shares == 1 ? launch_attn_many<256, 1>(a, items, st) : launch_attn_many<256, 2>(a, items, st);
         default: return hipErrorInvalidValue;
     }
 }

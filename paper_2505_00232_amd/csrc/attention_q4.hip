@@ -7,11 +7,11 @@
 // q in two binary16 parts (2^-22).  For the second product
 //   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
 // P is multiplied with the step in 32 bits and rounded to binary16 once per group; the -8 is taken off with the same rounded values (an MFMA with a
-// constant into the same sums), so that what the rounding leaves is relative to a centred code, and the offsets are again one MFMA, whose last row, ones, gives the sum of P.
+// constant into the same sums: taken off at the end, from sums of their own, it left errors of 2^-15 of 8 steps where one position has nearly all of P), so that what the rounding
+// leaves is relative to a centred code, and the offsets are again one MFMA, whose last row, ones, gives the sum of P.
+// Cached values are never rounded: as binary16 copies, with the kernel for prompts over a 16-bit cache (attention.hip), prompts of 1024 and 601 tokens took 48 us instead of 78, with
+// twice the error (relative to the result's norm 4.0e-4 instead of 2.8e-4, where the output's own rounding is 2.1e-4).
 //
-// Few query rows of a request (up to few_rows per KV head: tokens, short chunks) go through that kernel in blocks of 16.  Many rows would take the same
-// codes apart again and again: for them the pages are first turned into binary16 copies in the workspace, once, and the kernel for prompts (attention.hip) walks
-// those.  Which request is which is known on the device only, where a first small kernel finds it.
 // P is taken 2^14 times as large: with steps below 2 every product is below 2^15, and binary16 keeps its 11 bits down to a product of 2^-28.  A step of 2 or more (values some 30
 // apart and more) lowers that factor to 2^2 from there on, for which every step (8734 at most) is small enough.
 #include "paged_q4.h"
@@ -27,12 +27,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kFactor = 14.0f, kLower = 12.0f;  // log 2 of what P is multiplied with, of what large steps divide that by
 constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: below every score
 
-// Rows of a request per KV head that the blocks of 16 take.  Heads 32 on 8 of 128 values, us with blocks of 16 / with copies: one request at 512 positions 128 rows 15 / 23,
-// 256 rows 18 / 23, 512 rows 26 / 23, at 4096 positions 256 rows 31 / 33, 512 rows 46 / 39; eight requests, which keep the card busy, at 512 positions 128 rows 40 / 31, 192 rows
-// 54 / 32, at 4096 positions 72 rows 54 / 87, 128 rows 77 / 92, 192 rows 113 / 122, 256 rows 136 / 121.
-int few_rows(long all_rows) { return all_rows > 1024 ? 128 : 256; }
-constexpr int kMaxSlots = 256;  // requests of many rows at most, the others go through the blocks of 16
-
 constexpr int kWhole = 4;  // pages of a unit that is not cut, of small shares
 
 struct AttnQ4Args {
@@ -41,18 +35,10 @@ struct AttnQ4Args {
     const char *pages;
     Requests req;
     float *ws_o, *ws_ml;  // [workers, 2, 16, D] partial outputs, [.., 2] (maximum, sum)
-    int *plan;            // ManyRows, or null
     int h_q, h_kv, g, workers, least, whole;
     float scale;
 };
 
-// The work: units of a KV head and a block of 16 query rows of a request, one behind the other (a request's blocks, in each all heads), each with the request's
-// pages.  The pages are dealt to the wavefronts in equal shares (at least `least`), whatever the requests' lengths: each has one run of pages, across units.  A
-// unit is done by one wavefront where it is short (half a share, or, of small shares, kWhole pages: less work than a second launch), by that in whose share it begins; of a longer one a wavefront does the pages of its share, and
-// leaves partial results where others have the rest: two per wavefront at most, of the unit that its share begins inside of (or with), and of
-// the one that it ends inside of.  A unit's beginning costs about as much as two pages (its requests' arrays, queries and first page one after the other): where a share
-// is some pages, units are that much longer.
-__device__ __forceinline__ bool has_many(const AttnQ4Args &a, int b) { return a.plan && a.plan[ManyRows::kSlots + b] >= 0; }
 // sum over the lanes up to this one
 __device__ __forceinline__ int sum_upto(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
@@ -63,9 +49,16 @@ __device__ __forceinline__ int sum_upto(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
     return x;
 }
+// The work: units of a KV head and a block of 16 query rows of a request, one behind the other, each with the pages that its last row sees.  A request's blocks come in pairs, the
+// first with the last and so on, all heads of a pair in turn: every pair of a request has about as many pages, so that a place in the run of all is found without a list.
+// The pages are dealt to the wavefronts in equal shares (at least `least`), whatever the requests' lengths: each has one run of pages, across units.  A
+// unit is done by one wavefront where it is short (half a share, or, of small shares, kWhole pages: less work than a second launch), by that in whose share it begins; of a longer
+// one a wavefront does the pages of its share, and leaves partial results where others have the rest: two per wavefront at most, of the unit that its share begins inside of (or
+// with), and of the one that it ends inside of.  A unit's beginning costs about as much as two pages (its requests' arrays, queries and first page one after the other): where a share
+// is some pages, units are that much longer (32 requests of up to 8192 positions 46.8 us, without 49.6).
 struct Unit {
     int b, kv, row0;  // b < 0: behind the last
-    int begin, end;   // places in the run of all units
+    int begin, end;   // places in the run of all units; a unit without rows: places that are nobody's
     Span span;
 };
 struct Units {
@@ -73,35 +66,46 @@ struct Units {
     const int lane;
     int share, over;           // pages of a wavefront, and what a unit has on top of its own
     int b0, before, before_u;  // 64 requests at a time: the first, and places and units before them
-    int count, pages, upto, upto_u;  // of this lane's request: units, pages of each; places and units up to its end
+    int blocks, pages, upto, upto_u;  // of this lane's request: blocks of 16 rows, pages of a pair (of the block, where it is the only one); places and units up to its end
     Span span;
     __device__ __forceinline__ Units(const AttnQ4Args &args, int l) : a(args), lane(l), share(0), over(0), b0(0), before(0), before_u(0) {
         int all = 0, units = 0;
         for (int c = 0; c < a.req.batch; c += 64) {
             load(c);
-            all += count * pages;
-            units += count;
+            all += pairs(blocks) * pages;
+            units += pairs(blocks) * of_pair(blocks);
         }
-        all = last(sum_upto(all)), units = last(sum_upto(units));
+        all = last(sum_upto(all * a.h_kv)), units = last(sum_upto(units * a.h_kv));
         over = all / 4 >= a.workers ? 2 : 0;
         share = max(a.least, (all + over * units + a.workers - 1) / a.workers);
         if (a.req.batch > 64) load(0);
         sum();
     }
     __device__ static __forceinline__ int last(int x) { return __builtin_amdgcn_readlane(x, 63); }
+    __device__ static __forceinline__ int pairs(int blocks) { return (blocks + 1) / 2; }
+    __device__ static __forceinline__ int of_pair(int blocks) { return blocks > 1 ? 2 : 1; }
+    // pages that the last row of block k sees (one at least: a unit without positions has its rows written)
+    __device__ __forceinline__ int pages_of(const Span &s, int k) const {
+        return max(1, (s.positions - s.count + min(16 * k + 15, s.count * a.g - 1) / a.g + kPage) / kPage);
+    }
     __device__ __forceinline__ void load(int c) {
         b0 = c;
-        count = 0, pages = 1, span = Span{0, 0, 0};  // (a unit without positions counts as one page: its rows are written)
+        blocks = 0, pages = 1, span = Span{0, 0, 0};
         const int b = c + lane;
-        if (b < a.req.batch && !has_many(a, b)) {
+        if (b < a.req.batch) {
             span = span_of(a.req, b);
-            count = (span.count * a.g + 15) / 16 * a.h_kv;
+            blocks = (span.count * a.g + 15) / 16;
             pages = max(1, (span.positions + kPage - 1) / kPage);
+            if (blocks > 1) {  // (of a block k and the one as far from the end, whatever k: their last tokens add up to (16 blocks + 14) / g at most)
+                const int past = span.positions - span.count;
+                pages += pages_of(span, (blocks - 1) / 2);
+                if (past >= 0) pages = min(pages, (2 * past + (16 * blocks + 14) / a.g) / kPage + 2);
+            }
         }
     }
     __device__ __forceinline__ void sum() {
-        upto = sum_upto(count * (pages + over));
-        upto_u = sum_upto(count);
+        upto = sum_upto(pairs(blocks) * a.h_kv * (pages + over * of_pair(blocks)));
+        upto_u = sum_upto(pairs(blocks) * a.h_kv * of_pair(blocks));
     }
     // The unit of place x or, by_index, the x-th; x does not descend from call to call
     template <bool BY_INDEX>
@@ -112,16 +116,24 @@ struct Units {
             const uint64_t past = __ballot(of > x - base);
             if (past) {
                 const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
-                const int n = __builtin_amdgcn_readlane(count, l), len = __builtin_amdgcn_readlane(pages, l) + over;
-                const int first = before + __builtin_amdgcn_readlane(upto, l) - n * len;
-                const int index = BY_INDEX ? x - (before_u + __builtin_amdgcn_readlane(upto_u, l) - n) : (x - first) / len;
-                // (the same in every lane: said explicitly, it stays in scalar registers)
-                u.b = __builtin_amdgcn_readfirstlane(b0 + l);
-                u.kv = __builtin_amdgcn_readfirstlane(index % a.h_kv);
-                u.row0 = __builtin_amdgcn_readfirstlane(index / a.h_kv * 16);
-                u.begin = __builtin_amdgcn_readfirstlane(first + index * len);
-                u.end = __builtin_amdgcn_readfirstlane(u.begin + len);
+                const int n = __builtin_amdgcn_readlane(blocks, l), units = of_pair(n), len = __builtin_amdgcn_readlane(pages, l) + over * units;
+                const int first = before + __builtin_amdgcn_readlane(upto, l) - pairs(n) * a.h_kv * len;
+                const int nth = x - (before_u + __builtin_amdgcn_readlane(upto_u, l) - pairs(n) * a.h_kv * units);
                 u.span = Span{__builtin_amdgcn_readlane(span.first, l), __builtin_amdgcn_readlane(span.count, l), __builtin_amdgcn_readlane(span.positions, l)};
+                // (the same in every lane: said explicitly, it stays in scalar registers)
+                const int pair = __builtin_amdgcn_readfirstlane(BY_INDEX ? nth / units : (x - first) / len), k = __builtin_amdgcn_readfirstlane(pair / a.h_kv);
+                const int begin = first + pair * len;
+                u.b = __builtin_amdgcn_readfirstlane(b0 + l);
+                u.kv = __builtin_amdgcn_readfirstlane(pair - k * a.h_kv);
+                u.begin = __builtin_amdgcn_readfirstlane(begin);
+                u.end = __builtin_amdgcn_readfirstlane(begin + len);
+                if (units == 2) {  // the pair's first block, its second one (the middle block has none), places that are nobody's
+                    const int cut = begin + over + pages_of(u.span, k), other = n - 1 - k, end = other > k ? cut + over + pages_of(u.span, other) : cut;
+                    const int which = BY_INDEX ? (nth % 2 == 0 ? 0 : other > k ? 1 : 2) : x < cut ? 0 : x < end ? 1 : 2;
+                    u.row0 = __builtin_amdgcn_readfirstlane(16 * (which == 0 ? k : which == 1 ? other : n));
+                    u.begin = __builtin_amdgcn_readfirstlane(which == 0 ? begin : which == 1 ? cut : end);
+                    u.end = __builtin_amdgcn_readfirstlane(which == 0 ? cut : which == 1 ? end : begin + len);
+                }
                 return u;
             }
             if (b0 + 64 >= a.req.batch) return u;
@@ -150,7 +162,10 @@ struct Place {
     static_assert(kWgs * LDS <= 160 * 1024 && COPIES <= 63, "LDS, and the 6-bit counter of outstanding copies");
 };
 
-// Up to 16 query rows of a KV head at a time.  The wavefronts work for themselves, each with copies of its own on the way.
+// Up to 16 query rows of a KV head at a time.  The wavefronts work for themselves, each with copies of its own on the way.  Bound: memory where rows are few (32 requests of up to 8192
+// positions, 32 heads on 8 of 128 values: 168 MB in 41 us, 4.1 TB/s), the some 450 vector instructions of a page and block, and little that runs beside them, where they are many
+// (prompts of 1024 and 601 tokens 67 us).  Two blocks that share the codes' taking apart need more registers than two wavefronts of a SIMD have, and were slower (prompts 187 us, 167
+// with one, both before blocks came in pairs).
 template <int D>
 __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
     typedef PageLayout<D> L;
@@ -169,7 +184,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
         const Unit unit = units.at<false>(x);
         if (__builtin_amdgcn_readfirstlane(unit.b) < 0) return;
         const bool cut = units.may_cut(unit);
-        if (!cut && unit.begin < x) {  // (another wavefront has it)
+        if ((!cut && unit.begin < x) || unit.row0 >= unit.span.count * a.g) {  // (another wavefront has it, or there is none)
             x = unit.end;
             continue;
         }
@@ -405,6 +420,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
     }
 }
 
+// Joining costs 4 to 12 us, most of it a launch and four reads one behind the other.
 // The units that several wavefronts share, a row of one (unit_rows in each) per workgroup, or one after the other.  Its four wavefronts take the
 // parts in turn, lane c the (maximum, sum) of its c-th and D / 64 columns of the partial outputs; they meet in LDS.
 template <int D>
@@ -476,153 +492,77 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a, int 
     }
 }
 
-// ---------------------------------------------------------------- many query rows
-struct ManyArgs {
-    Requests req;
-    int *plan;
-    const char *pages;
-    _Float16 *kc, *vc;  // [slots, h_kv, positions, D], [slots, h_kv, positions / 64, D, 64]
-    int g, h_kv, slots, records, block_rows, chunk_steps, max_pages, few;
-};
-
-// One workgroup: the list of the requests with more than `few` rows, and how many workgroups each takes (per block of rows one for a chunk of its steps).  A request with a missing
-// page, or with fewer positions than tokens, is none of them: the kernel for few rows takes it.
-__global__ __launch_bounds__(256) void attn_q4_list_kernel(ManyArgs a) {
-    __shared__ uint64_t wanted[4];
-    __shared__ int rec[kMaxSlots][4], item[kMaxSlots];
-    const int tid = threadIdx.x;
-    int count = 0;  // (the same in every thread)
-    for (int b0 = 0; b0 < a.req.batch; b0 += 256) {
-        const int b = b0 + tid;
-        bool many = false;
-        if (b < a.req.batch) {
-            const Span s = span_of(a.req, b);
-            many = s.count * a.g > a.few && s.positions >= s.count;
-            if (!many) a.plan[ManyRows::kSlots + b] = -1;
-        }
-        const uint64_t mask = __ballot(many);
-        if ((tid & 63) == 0) wanted[tid >> 6] = mask;
-        __syncthreads();
-        for (int w = 0; w < 4; ++w) {
-            for (uint64_t m = wanted[w]; m; m &= m - 1) {
-                const int bb = b0 + 64 * w + __ffsll((unsigned long long)m) - 1;
-                const Span s = span_of(a.req, bb);
-                bool missing = false;
-                for (int p = tid; p * kPage < s.positions; p += 256) missing = missing || page_of(a.req, bb, p * kPage) < 0;
-                const bool taken = !__syncthreads_or(missing) && count < a.slots;
-                if (tid == 0) {
-                    if (taken) rec[count][0] = s.first, rec[count][1] = s.count, rec[count][2] = s.positions, rec[count][3] = bb;
-                    a.plan[ManyRows::kSlots + bb] = taken ? count : -1;
-                }
-                count += taken;
+// The same where rows are many (few: chunks of 40 tokens of two requests 33 us, this kernel 39; many: a chunk of 300 tokens beside tokens 97 us, a workgroup per row 124): a workgroup per worker, for the unit that the worker's share begins inside of, if it is the first to do so; a wavefront per row
+template <int D>
+__global__ __launch_bounds__(256) void attn_q4_combine_rows_kernel(AttnQ4Args a) {
+    constexpr int PER = D / 64;
+    typedef float cols __attribute__((ext_vector_type(PER)));
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Units units(a, lane);
+    const int x = ((int)blockIdx.x + 1) * units.share;
+    const Unit unit = units.at<false>(x);
+    if (unit.b < 0 || unit.begin >= x || x - unit.begin > units.share || !units.may_cut(unit)) return;
+    const Span span = unit.span;
+    const int w0 = unit.begin / units.share, parts = (unit.end - 1) / units.share - w0 + 1, rows = min(16, span.count * a.g - unit.row0);
+    const size_t slot0 = partial_of(unit, w0, units.share) * 16;
+    // (four rows of a wavefront; everything's first parts are on their way at once, and those behind the last are read again and count as nothing)
+    auto place = [&](int row, int c) __attribute__((always_inline)) { return (c == 0 ? slot0 : (size_t)(w0 + c) * 32) + min(wave + 4 * row, rows - 1); };
+    float mx[4], l[4];
+    cols part[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        mx[i] = a.ws_ml[place(i, min(lane, parts - 1)) * 2];
+        l[i] = a.ws_ml[place(i, min(lane, parts - 1)) * 2 + 1];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) part[i][c] = *reinterpret_cast<const cols *>(a.ws_o + place(i, c) * D + PER * lane);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float top = mx[i];
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+        const float f = lane < parts ? __builtin_amdgcn_exp2f(mx[i] - top) : 0.0f;
+        float sum = f * l[i];
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+        cols o = {};
+        for (int c0 = 0; c0 < parts; c0 += 2) {
+            const cols now[2] = {part[i][0], part[i][1]};
+            if (c0 + 2 < parts) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) part[i][c] = *reinterpret_cast<const cols *>(a.ws_o + place(i, min(c0 + 2 + c, parts - 1)) * D + PER * lane);
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float fc = __shfl(f, (c0 + c) & 63, 64);
+#pragma unroll
+                for (int e = 0; e < PER; ++e) o[e] = c0 + c < parts ? fmaf(fc, now[c][e], o[e]) : o[e];
             }
         }
-        __syncthreads();
-    }
-    // steps of the last row of block j of a request's rows
-    auto steps = [&](int slot, int j) {
-        const int S = rec[slot][1], last = min((j + 1) * a.block_rows, S * a.g) - 1;
-        return (rec[slot][2] - S + last / a.g + 1 + 31) / 32;
-    };
-    if (tid < count) {
-        const int blocks = (rec[tid][1] * a.g + a.block_rows - 1) / a.block_rows;
-        int n = blocks;
-        if (a.chunk_steps > 0) {
-            n = 0;
-            for (int j = 0; j < blocks; ++j) n += (steps(tid, j) + a.chunk_steps - 1) / a.chunk_steps;
-        }
-        item[tid] = n;
-    }
-    __syncthreads();
-    if (tid == 0) {
-        int sum = 0;
-        for (int i = 0; i < count; ++i) {
-            const int n = item[i];
-            item[i] = sum;
-            sum += n;
-        }
-        a.plan[ManyRows::kCount] = count;
-        a.plan[ManyRows::kItems] = sum;
-    }
-    __syncthreads();
-    if (tid < count) {
-        int *r = a.plan + a.records + tid * ManyRows::kRecord;
-        r[ManyRows::kRow] = rec[tid][0];
-        r[ManyRows::kTokens] = rec[tid][1];
-        r[ManyRows::kPositions] = rec[tid][2];
-        r[ManyRows::kItem] = item[tid];
-        r[ManyRows::kChunkSteps] = a.chunk_steps;
-        r[ManyRows::kRequest] = rec[tid][3];
-    }
-}
-
-// grid = (pages of the longest request x KV heads, slots): a page's block of one head as binary16, fp16(offset + step (code - 8)).  Bound: memory.
-template <int D>
-__global__ __launch_bounds__(256) void attn_q4_copy_kernel(ManyArgs a) {
-    typedef PageLayout<D> L;
-    constexpr int G = L::G;
-    const int slot = blockIdx.y, kv = (int)blockIdx.x % a.h_kv, pg = (int)blockIdx.x / a.h_kv;
-    if (slot >= a.plan[ManyRows::kCount]) return;
-    const int *r = a.plan + a.records + slot * ManyRows::kRecord;
-    if (pg * kPage >= r[ManyRows::kPositions]) return;
-    const int page = page_of(a.req, r[ManyRows::kRequest], pg * kPage);
-    if (page < 0) return;  // (none of the list's requests)
-    const char *src = a.pages + ((size_t)page * a.h_kv + kv) * L::kBytes;
-    const size_t dst = ((size_t)(slot * a.h_kv + kv) * a.max_pages + pg) * (kPage * D);
-    const int tid = threadIdx.x;
-    // keys: a thread per octet
+        if (wave + 4 * i >= rows) return;
+        const int row = unit.row0 + wave + 4 * i;
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        _Float16 *out = a.out + ((size_t)(span.first + row / a.g) * a.h_q + unit.kv * a.g + row % a.g) * D + PER * lane;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const int o = (tid + 256 * i) % (D / 8), p = (tid + 256 * i) / (D / 8), j = o / 4;
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(src + L::code_k(p, j, o & 3));
-        const float step = (float)*reinterpret_cast<const _Float16 *>(src + L::step_k(p, j)), off = (float)*reinterpret_cast<const _Float16 *>(src + L::offset_k(p, j));
-        h8 x;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (_Float16)fmaf((float)((w >> nibble(e)) & 15u) - 8.0f, step, off);
-        *reinterpret_cast<h8 *>(a.kc + dst + p * D + 8 * o) = x;
-    }
-    // values: a thread per 8 positions of the two values of a byte
-#pragma unroll
-    for (int i = 0; i < G * 128 / 256; ++i) {
-        const int t = tid + 256 * i, p0 = 8 * (t % 8), m = t / 8 % 16, j = t / 128;
-        const uint2 w = *reinterpret_cast<const uint2 *>(src + L::kCodesV + (j * 64 + (p0 >> 4) * 16 + m) * 16 + (p0 & 8));
-        const h8 step = *reinterpret_cast<const h8 *>(src + L::step_v(p0, j)), off = *reinterpret_cast<const h8 *>(src + L::offset_v(p0, j));
-        h8 lo, hi;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t byte = (e < 4 ? w.x : w.y) >> (8 * (((e & 1) << 1) | ((e >> 1) & 1)));
-            lo[e] = (_Float16)fmaf((float)(byte & 15u) - 8.0f, (float)step[e], (float)off[e]);
-            hi[e] = (_Float16)fmaf((float)((byte >> 4) & 15u) - 8.0f, (float)step[e], (float)off[e]);
-        }
-        *reinterpret_cast<h8 *>(a.vc + dst + (32 * j + m) * 64 + p0) = lo;
-        *reinterpret_cast<h8 *>(a.vc + dst + (32 * j + 16 + m) * 64 + p0) = hi;
+        for (int e = 0; e < PER; ++e) out[e] = (_Float16)(o[e] * inv);
     }
 }
 
 template <int D>
-hipError_t launch(const AttnQ4Args &a, const ManyArgs &many, const AttnQ4Plan &p, int num_cus, hipStream_t st) {
-    if (p.slots > 0) {
-        attn_q4_list_kernel<<<1, 256, 0, st>>>(many);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
+hipError_t launch(const AttnQ4Args &a, const AttnQ4Plan &p, int num_cus, hipStream_t st) {
     constexpr size_t lds = Place<D>::LDS;
     if (const hipError_t e = allow_dynamic_lds<attn_q4_kernel<D>>(lds); e != hipSuccess) return e;
     attn_q4_kernel<D><<<(unsigned)((a.workers + 3) / 4), 256, lds, st>>>(a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (p.shared) {
-        const int unit_rows = p.rows < 16 ? p.rows : 16;
-        const long works = p.blocks * a.h_kv * unit_rows, most = 4L * num_cus;
-        attn_q4_combine_kernel<D><<<(unsigned)(works < most ? works : most), 256, 0, st>>>(a, unit_rows);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-    if (p.slots > 0) {
-        attn_q4_copy_kernel<D><<<dim3((unsigned)(p.pages * a.h_kv), (unsigned)p.slots), 256, 0, st>>>(many);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || !p.shared) return e;
+    if (p.many) {
+        if (a.workers > 1) attn_q4_combine_rows_kernel<D><<<(unsigned)(a.workers - 1), 256, 0, st>>>(a);
         return hipGetLastError();
     }
-    return hipSuccess;
+    const int unit_rows = p.rows < 16 ? p.rows : 16;
+    const long works = p.blocks * a.h_kv * unit_rows, most = 4L * num_cus;
+    attn_q4_combine_kernel<D><<<(unsigned)(works < most ? works : most), 256, 0, st>>>(a, unit_rows);
+    return hipGetLastError();
 }
-
-size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -630,76 +570,39 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     AttnQ4Plan p = {};
     p.pages = (max_context + kPage - 1) / kPage;
     p.rows = max_tokens * g;
-    p.all_rows = (long)tokens * g;
-    p.blocks = p.rows <= 16 ? batch : (p.all_rows + 15) / 16 + batch;
-    // few rows: as many wavefronts as the card holds at once
+    p.blocks = p.rows <= 16 ? batch : ((long)tokens * g + 15) / 16 + 2L * batch;  // (pairs: one more where a request's number is odd)
+    // as many wavefronts as the card holds at once
     const long waves = 4L * num_cus * kWgs, most_pages = p.blocks * h_kv * p.pages;
-    p.least = (p.pages + 2 + 253) / 254;  // (a unit is cut into 254 whole shares and two ends at most: the combination's four wavefronts take 64 each)
+    p.many = p.blocks * h_kv * (p.rows < 16 ? p.rows : 16) > 16L * num_cus;
+    const int most_shares = p.many ? 62 : 254;  // (and two ends: a lane of the combination's wavefront, or of its four, for each)
+    p.least = (p.pages + most_shares) / most_shares;
     if (const int forced = tuning().attn_q4_pages; forced > p.least) p.least = forced;
     const long shares = (most_pages + p.least - 1) / p.least;
     p.workers = (int)(shares < waves ? shares : waves);
     if (p.workers < 1) p.workers = 1;
     p.shared = p.pages > kWhole;
-    p.total = 256;
-    p.partial = 0;
-    if (p.shared) p.total += up256((size_t)p.workers * 2 * 16 * (d + 2) * sizeof(float));
-    // many rows
-    const int few = few_rows(p.all_rows);
-    if (p.rows <= few) return p;
-    const long most = p.all_rows / (few + 1);
-    p.slots = (int)(most < batch ? most : batch);
-    if (p.slots > kMaxSlots) p.slots = kMaxSlots;
-    if (p.slots == 0) return p;
-    // (as for equal requests of the most tokens and positions, as many as make up the rows)
-    const long alike = (p.all_rows + p.rows / 2) / p.rows;
-    p.shares = plan_attention_many((int)((alike < 1 ? 1 : alike) * h_kv), max_tokens, g, d, max_context, num_cus, &p.chunk_steps);
-    const int steps = (max_context + 31) / 32, chunks = p.chunk_steps > 0 ? (steps + p.chunk_steps - 1) / p.chunk_steps : 1;
-    p.items = (int)((p.all_rows / (128 / p.shares) + p.slots) * chunks);
-    p.records = (ManyRows::kSlots + batch + 7) / 8 * 8;
-    p.plan = p.total;
-    p.total += up256((size_t)(p.records + p.slots * ManyRows::kRecord) * sizeof(int));
-    p.copies = p.total;
-    p.total += up256((size_t)p.slots * h_kv * p.pages * kPage * d * 2 * 2);
-    p.many_partial = p.total;
-    if (p.chunk_steps > 0) p.total += up256((size_t)kPrefillMaxChunks * h_kv * p.all_rows * (d + 2) * sizeof(float));
+    p.bytes = 256 + (p.shared ? (size_t)p.workers * 2 * 16 * (d + 2) * sizeof(float) : 0);
     return p;
 }
 
 hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out, int num_cus,
                                hipStream_t st) {
-    char *ws = static_cast<char *>(workspace);
     AttnQ4Args a = {};
     a.q = static_cast<const _Float16 *>(q);
     a.out = static_cast<_Float16 *>(out);
     a.pages = static_cast<const char *>(pages);
     a.req = req;
     a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv;
-    a.workers = p.workers, a.least = p.least, a.whole = p.shared ? 0 : kWhole;  // (no second launch: nothing is cut)
-    a.ws_o = reinterpret_cast<float *>(ws + p.partial);
+    a.workers = p.workers, a.least = p.least, a.whole = p.shared ? 0 : INT32_MAX;  // (no second launch: nothing is cut)
+    a.ws_o = static_cast<float *>(workspace);
     a.ws_ml = a.ws_o + (size_t)p.workers * 2 * 16 * d;
     a.scale = 1.4426950408889634f / sqrtf((float)d);
-    ManyArgs many = {};
-    _Float16 *kc = nullptr, *vc = nullptr;
-    if (p.slots > 0) {
-        a.plan = reinterpret_cast<int *>(ws + p.plan);
-        kc = reinterpret_cast<_Float16 *>(ws + p.copies);
-        vc = kc + (size_t)p.slots * h_kv * p.pages * kPage * d;
-        many.req = req;
-        many.plan = a.plan;
-        many.pages = a.pages;
-        many.kc = kc, many.vc = vc;
-        many.g = a.g, many.h_kv = h_kv, many.slots = p.slots, many.records = p.records, many.block_rows = 128 / p.shares, many.chunk_steps = p.chunk_steps;
-        many.max_pages = p.pages, many.few = few_rows(p.all_rows);
-    }
-    hipError_t e = hipErrorInvalidValue;
     switch (d) {
-        case 64: e = launch<64>(a, many, p, num_cus, st); break;
-        case 128: e = launch<128>(a, many, p, num_cus, st); break;
-        case 256: e = launch<256>(a, many, p, num_cus, st); break;
+        case 64: return launch<64>(a, p, num_cus, st);
+        case 128: return launch<128>(a, p, num_cus, st);
+        case 256: return launch<256>(a, p, num_cus, st);
     }
-    if (e != hipSuccess || p.slots == 0) return e;
-    return launch_attention_many(q, kc, vc, h_q, h_kv, d, p.pages * kPage, a.plan, p.records, p.shares, p.items, p.all_rows,
-                                 p.chunk_steps > 0 ? reinterpret_cast<float *>(ws + p.many_partial) : nullptr, out, st);
+    return hipErrorInvalidValue;
 }
 
 }  // namespace qfc

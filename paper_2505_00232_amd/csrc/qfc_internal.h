@@ -390,35 +390,19 @@ hipError_t launch_rotary_table(int rot, double base, double factor, int original
 hipError_t launch_append_q4(const void *qkv, const Requests &req, int h_q, int h_kv, int d, int rot, bool interleaved, const float *table, void *pages, void *q_out,
                             int num_cus, hipStream_t st);
 hipError_t launch_read_q4(const Requests &req, int h_kv, int d, const void *pages, void *k, void *v, int num_cus, hipStream_t st);
-// Attention of requests with many query rows: which they are, and how their walks are cut, is found on the device (attention_q4.hip) and left as a list of int32.
-struct ManyRows {
-    static constexpr int kCount = 0, kItems = 1, kSlots = 4;  // requests, their workgroups per KV head; from kSlots on each request's place in the list or -1
-    static constexpr int kRecord = 8;                         // ints per request in the list:
-    static constexpr int kRow = 0, kTokens = 1, kPositions = 2, kItem = 3, kChunkSteps = 4, kRequest = 5;
-};
 struct AttnQ4Plan {
-    int rows;         // query rows of a KV head and request at most
-    long blocks;      // blocks of 16 rows of all requests at most
-    int workers;      // wavefronts that share the pages of all requests of few rows
-    int least;        // pages a wavefront takes at least
-    bool shared;      // a request's pages may be shared by several
-    // requests of many rows (slots 0: there are none)
-    int slots;        // at most so many
-    int shares;       // wavefronts that share a walk
-    int items;        // workgroups per KV head at most
-    int chunk_steps;  // steps of 32 positions of the chunks walks are cut into (0: whole)
-    long all_rows;    // query rows of a KV head of all requests
-    // bytes from the workspace's start
-    size_t partial, plan, copies, many_partial, total;
-    int records;      // ints from the plan's start to its list
-    int pages;        // of the longest request
+    int rows;      // query rows of a KV head and request at most
+    int pages;     // of the longest request
+    long blocks;   // blocks of 16 rows of all requests at most
+    int workers;   // wavefronts that share the pages of all blocks
+    int least;     // pages a wavefront takes at least
+    bool shared;   // a block's pages may be shared by several
+    bool many;     // rows enough for a wavefront of the combination each
+    size_t bytes;  // of the workspace
 };
 AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int max_tokens, int max_context, int num_cus);
 hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out, int num_cus,
                                hipStream_t st);
-int plan_attention_many(int groups, int S, int g, int d, int n_ctx, int num_cus, int *chunk_steps);
-hipError_t launch_attention_many(const void *q, const void *kc, const void *vc, int h_q, int h_kv, int d, int C, const int *plan, int records, int shares, int items,
-                                 long rows, float *partial, void *out, hipStream_t st);
 struct AdapterPlan {
     int rows;           // M rounded up
     int parts, part_k;  // K in `parts` parts of `part_k`
