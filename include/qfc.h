@@ -368,7 +368,7 @@ qfc_status_t qfc_rotary_table(const qfc_rotary_t *rotary, int32_t positions, flo
 
 /* Rotation and append for a batch of requests: qkv_f16 [tokens, (h_q + 2 h_kv) * d_head] is the QKV layer's output (query heads,
  * key heads, value heads).  Queries and keys are rotated by their positions' angles (products and sum exact, rounded once to binary16); the
- * queries go to q_out, binary16 [tokens, h_q * d_head]; keys and values are quantized into the cache, values as they are.
+ * queries go to q_out, binary16 [tokens, h_q * d_head], a buffer of its own; keys and values are quantized into the cache, values as they are.
  * rotary: host, or null for no rotation (rope_table is not read then); rope_table: from qfc_rotary_table with at least max_context
  * positions (table_positions says how many).  No two rows may have the same place in the cache.
  * Errors: QFC_ERR_INVALID_ARG (null pointers, sizes, h_q not a multiple of h_kv, max_context beyond the page table or the
@@ -381,14 +381,15 @@ qfc_status_t qfc_append_q4(const void *qkv_f16, const qfc_requests_t *requests, 
  * without a page.  Errors as qfc_append_q4. */
 qfc_status_t qfc_read_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, void *k, void *v, void *stream);
 
-/* Bytes of scratch qfc_attention_q4 needs for a batch of this size (batch, tokens, max_tokens and max_context are read; host
- * pointers).  Where a request may have many query rows (max_tokens * h_q / h_kv above 256) they include binary16 copies of such requests' keys and values. */
+/* Bytes of scratch qfc_attention_q4 needs for a batch of this size (batch, tokens, max_tokens and max_context are read; host pointers): partial
+ * results of requests whose positions several wavefronts share, 68 MB at most. */
 qfc_status_t qfc_attention_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
 
 /* Attention of a batch of requests over the cache: out = softmax(q K^T / sqrt(d_head)) V for each row and head, q and out binary16
  * [tokens, h_q * d_head].  New token s of S of a request with n positions sees positions 0 .. n - S + s; a row that sees none
  * (no positions, or no pages) gets zeros.  One token or many per request, in any mixture.
- * workspace: device scratch of at least qfc_attention_q4_workspace_size bytes.  Errors as qfc_append_q4, QFC_ERR_BUFFER_TOO_SMALL. */
+ * workspace: device scratch of at least qfc_attention_q4_workspace_size bytes, one call's at a time.  Errors as qfc_append_q4, QFC_ERR_BUFFER_TOO_SMALL,
+ * QFC_ERR_UNSUPPORTED also where all blocks of 16 query rows with the most pages make up 2^31 and more. */
 qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache,
                               void *workspace, size_t workspace_bytes, void *out_f16, void *stream);
 
@@ -406,7 +407,9 @@ qfc_status_t qfc_adapters_workspace_size(const qfc_adapters_t *adapters, int32_t
 /* out[m] = fp16(y[m] + scale[a] B[a] (A[a] x[m])), a = ids[m], beside a shared layer whose output y is: every row (token) may have an
  * adapter of its own; an id outside [0, count) has none, and out[m] = y[m].
  *   x binary16 [M, K]; ids device, int32 [M]; y, out binary16 [M, N] (out may be y); K a multiple of 32.
- * workspace: device scratch of at least qfc_adapters_workspace_size bytes. */
+ * workspace: device scratch of at least qfc_adapters_workspace_size bytes, one call's at a time.  Errors: QFC_ERR_INVALID_ARG (null pointers, sizes),
+ * QFC_ERR_UNSUPPORTED (rank not a multiple of 8 or above 128, N above 2^23, M above 2^24), QFC_ERR_ALIGNMENT (16 bytes; ids and scale 4),
+ * QFC_ERR_BUFFER_TOO_SMALL. */
 qfc_status_t qfc_add_adapters(const void *x_f16, int32_t M, const int32_t *ids, const qfc_adapters_t *adapters, const void *y_f16,
                               void *workspace, size_t workspace_bytes, void *out_f16, void *stream);
 

@@ -42,7 +42,8 @@ __device__ __forceinline__ void for_adapters(int id, int mine, int dealt, const 
 }
 
 // grid = (blocks of 16 rows, parts of K, workgroups that share a block's adapters); the four wavefronts of a workgroup take the part's pieces of 64 k in turn.  RT: tiles of 16
-// low-rank values.
+// low-rank values.  One row of 4096 values 2.7 us, 64 rows of 40 adapters of rank 16 4.8 us, 2048 rows of 5 adapters of rank 64 23 us (20 MB, each block of rows reads its adapters again
+// from L2).
 template <int RT>
 __global__ __launch_bounds__(256) void adapters_shrink_kernel(AdapterArgs a) {
     __shared__ float sums[4][RT][64][4];
@@ -101,6 +102,8 @@ __global__ __launch_bounds__(256) void adapters_shrink_kernel(AdapterArgs a) {
 // has the piece of B.  The workgroup adds up its rows' low-rank values once, into LDS; then a
 // wavefront takes 32 columns at a time, each of B's tiles for all of the block's rows.  The low-rank values are the second operand (rows as columns of the result), so that a lane
 // ends up with 8 consecutive columns of a row: row i of tile t of B is column 8 (i / 4) + 4 t + i % 4.  KT: steps of 32 low-rank values.
+// One row of 6144 columns 4.8 us, 64 rows of 40 adapters and 4096 columns 8.0 us, both latency; 2048 rows of 28672 columns 83 us for 252 MB (3.0 TB/s; the same loads and stores of y and
+// out without the products take 33 us: what is left is waiting, with two wavefronts on a SIMD, for loads and stores that share a counter).
 template <int KT, int MT>
 __global__ __launch_bounds__(256) void adapters_expand_kernel(AdapterArgs a) {
     constexpr int ROWS = 16 * MT, PITCH = 32 * KT + 8;
@@ -372,14 +375,15 @@ AdapterPlan plan_adapters(int M, int K, int N, int num_cus) {
     if (p.dealt > 16) p.dealt = 16;
     if (p.dealt > M) p.dealt = M;
     if (p.dealt < 1) p.dealt = 1;
-    int parts = 2 * num_cus / (blocks * p.dealt);
+    int parts = 2 * num_cus / (blocks * p.dealt);  // (of K, so that few rows reach every compute unit)
     if (parts > 16) parts = 16;
     if (parts > pieces) parts = pieces;
     if (parts < 1) parts = 1;
     p.part_k = (pieces + parts - 1) / parts * 128;
     p.parts = (K + p.part_k - 1) / p.part_k;
-    // many rows: blocks of 64 share B's tiles; columns per workgroup so that the card holds all workgroups at once
-    p.block_rows = M > 512 ? 64 : 16;
+    // many rows: blocks of 64 share B's tiles (us with 16 / 64: 300 x 28672 23.0 / 21.8, 520 x 6144 17.3 / 16.1, 1000 x 6144 19.5 / 20.9, 2048 x 6144 38 / 29, 1000 x 28672 76 / 58);
+    // columns per workgroup so that the card holds all workgroups at once, two to a compute unit (2048 x 28672: 107 us, with four 117 and 112 for blocks of 32)
+    p.block_rows = M > 256 ? 64 : 16;
     const long works = (long)((M + p.block_rows - 1) / p.block_rows) * pieces_n;
     p.tiles = (int)((works + 2L * num_cus - 1) / (2L * num_cus));
     if (p.tiles > 16) p.tiles = 16;

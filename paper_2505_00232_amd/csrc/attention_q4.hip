@@ -39,14 +39,16 @@ struct AttnQ4Args {
     float scale;
 };
 
+// Sums of places end at the largest int: requests whose arrays overlap have more than a call may have, and what lies behind is left out.
+__device__ __forceinline__ int add(int x, int y) { return __builtin_elementwise_add_sat(x, y); }
 // sum over the lanes up to this one
 __device__ __forceinline__ int sum_upto(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast 15, 31
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));  // row_shr 1, 2, 4, 8
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));  // row_bcast 15, 31
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
     return x;
 }
 // The work: units of a KV head and a block of 16 query rows of a request, one behind the other, each with the pages that its last row sees.  A request's blocks come in pairs, the
@@ -72,12 +74,12 @@ struct Units {
         int all = 0, units = 0;
         for (int c = 0; c < a.req.batch; c += 64) {
             load(c);
-            all += pairs(blocks) * pages;
-            units += pairs(blocks) * of_pair(blocks);
+            all = add(all, pairs(blocks) * a.h_kv * pages);
+            units = add(units, pairs(blocks) * a.h_kv * of_pair(blocks));
         }
-        all = last(sum_upto(all * a.h_kv)), units = last(sum_upto(units * a.h_kv));
+        all = last(sum_upto(all)), units = min(last(sum_upto(units)), INT32_MAX / 2);
         over = all / 4 >= a.workers ? 2 : 0;
-        share = max(a.least, (all + over * units + a.workers - 1) / a.workers);
+        share = max(a.least, add(add(all, over * units), a.workers - 1) / a.workers);
         if (a.req.batch > 64) load(0);
         sum();
     }
@@ -137,8 +139,8 @@ struct Units {
                 return u;
             }
             if (b0 + 64 >= a.req.batch) return u;
-            before += last(upto);
-            before_u += last(upto_u);
+            before = add(before, last(upto));
+            before_u = add(before_u, last(upto_u));
             load(b0 + 64);
             sum();
         }
