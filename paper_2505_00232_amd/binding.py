@@ -531,8 +531,8 @@ def qfc_append_q4(qkv: torch.Tensor, requests: Requests, h_q: int, rotary: Rotar
         _here(qkv.get_device(), q_out.get_device(), cache.device, requests.device)
         status = lib().qfc_append_q4(qkv.data_ptr(), requests.ref, h_q, None, None, 0, cache.ref, q_out.data_ptr(), _stream())
     else:
-        if not isinstance(rope_table, _Tensor):
-            raise ValueError("rope_table: a CUDA tensor is required")
+        if not (isinstance(rope_table, _Tensor) and rope_table.dim() == 3):
+            raise ValueError("rope_table: three dimensions are required")
         rows = rope_table.shape[0]
         _want(rope_table, _f32, (rows, rotary.rot_dim // 2, 2), "rope_table")
         _here(qkv.get_device(), q_out.get_device(), rope_table.get_device(), cache.device, requests.device)
