@@ -27,7 +27,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kFactor = 14.0f, kLower = 12.0f;  // log 2 of what P is multiplied with, of what large steps divide that by
 constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: below every score
 
-constexpr int kWhole = 4;  // pages of a unit that is not cut, of small shares
+constexpr int kWhole = 4;  // pages of a unit that is not cut, of small shares (256 requests of up to 150 positions 17 us, cut 33)
 
 struct AttnQ4Args {
     const _Float16 *q;  // [tokens, h_q, D]
@@ -494,7 +494,8 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a, int 
     }
 }
 
-// The same where rows are many (few: chunks of 40 tokens of two requests 33 us, this kernel 39; many: a chunk of 300 tokens beside tokens 97 us, a workgroup per row 124): a workgroup per worker, for the unit that the worker's share begins inside of, if it is the first to do so; a wavefront per row
+// The same where rows are many (few: chunks of 40 tokens of two requests 33 us, this kernel 39; many: a chunk of 300 tokens beside tokens 97 us, a workgroup per row 124): a workgroup
+// per worker, for the unit that the worker's share begins inside of, if it is the first to do so; a wavefront per row.
 template <int D>
 __global__ __launch_bounds__(256) void attn_q4_combine_rows_kernel(AttnQ4Args a) {
     constexpr int PER = D / 64;
