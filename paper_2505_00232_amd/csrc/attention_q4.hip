@@ -416,7 +416,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
             }
         }
         if (real && !whole && r == 0) {
-            a.ws_ml[part * 2] = run_max;
+            a.ws_ml[part * 2] = run_max + (kFactor - factor);  // (the maximum for which output and sum are taken 2^kFactor times, whatever this wavefront's factor)
             a.ws_ml[part * 2 + 1] = sum;
         }
     }

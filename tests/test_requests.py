@@ -318,6 +318,23 @@ def test_attention_sizes_of_values(d, k_size, v_size):
 
 
 @gpu
+@pytest.mark.parametrize("least", [0, 5, 300])  # pages a wavefront takes at least: wavefronts with and without large steps, and walks that meet them on the way
+@pytest.mark.parametrize("first,last", [(0, 64), (640, 704), (700, 701), (1280, 1399)])
+@pytest.mark.parametrize("S,h_q,h_kv,d", [([1, 1], 4, 2, 64), ([3, 1], 2, 1, 256), ([600], 8, 2, 64)])
+def test_attention_large_values_in_some_pages(S, h_q, h_kv, d, first, last, least):
+    """Steps of 2 and more in one page of a walk that several wavefronts share, in the middle of one wavefront's, and in the last page; other requests without any."""
+    rng = np.random.default_rng(58)
+    n = [1400, 1000][:len(S)]
+    k, v = (_normal(rng, sum(n), h_kv, d) for _ in range(2))
+    v[first:last] *= np.float16(100)
+    try:
+        B.lib().qfc_tune(15, least)
+        _check_attention(rng, S, n, h_q, h_kv, d, k=k, v=v)
+    finally:
+        B.lib().qfc_tune(15, 0)
+
+
+@gpu
 def test_attention_far_from_zero():
     """Keys and values with a mean far above their spread: offsets carry the result."""
     rng = np.random.default_rng(23)
