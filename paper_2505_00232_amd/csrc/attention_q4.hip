@@ -12,8 +12,11 @@
 // Cached values are never rounded: as binary16 copies, with the kernel for prompts over a 16-bit cache (attention.hip), prompts of 1024 and 601 tokens took 48 us instead of 78, with
 // twice the error (relative to the result's norm 4.0e-4 instead of 2.8e-4, where the output's own rounding is 2.1e-4).
 //
-// P is taken 2^14 times as large: with steps below 2 every product is below 2^15, and binary16 keeps its 11 bits down to a product of 2^-28.  A step of 2 or more (values some 30
-// apart and more) lowers that factor to 2^2 from there on, for which every step (8734 at most) is small enough.
+// P is taken 2^14 times as large: with steps below 2 every product is below 2^15, and binary16 keeps its 11 bits down to a product of 2^-28.  The steps of 2 and more (values some 30
+// apart and more) of a page are multiplied on their own, in a turn before the others' with each row's P lowered as far as that row's products need, so that what binary16 then loses is
+// little against a product that is in the row's sums; all others keep their bits.
+#include <type_traits>
+
 #include "paged_q4.h"
 
 namespace qfc {
@@ -24,7 +27,7 @@ typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kFactor = 14.0f, kLower = 12.0f;  // log 2 of what P is multiplied with, of what large steps divide that by
+constexpr float kFactor = 14.0f;  // log 2 of what P is multiplied with
 constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: below every score
 
 constexpr int kWhole = 4;  // pages of a unit that is not cut, of small shares (256 requests of up to 150 positions 17 us, cut 33)
@@ -243,7 +246,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
         v4f acc[DT], rest = {};
 #pragma unroll
         for (int t = 0; t < DT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        float run_max = kNothingYet, factor = kFactor;
+        float run_max = kNothingYet;
         const u32x4 eight_lo = {0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u}, eight_hi = {0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u},  // -8 as a code
                     eight_k = {0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u};
         const uint32_t mask_lo = 0x000F000Fu, mask_hi = 0x00F000F0u;
@@ -334,29 +337,78 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
                 }
             }
             auto step_of = [&](int j, int u) __attribute__((always_inline)) { return *reinterpret_cast<const h8 *>(values + L::kStepV + (j * kPage + 16 * r + 8 * u) * 2); };
-            uint32_t large;  // some of the page's steps; all of them in the wavefront
-            {
-                typedef uint32_t words __attribute__((ext_vector_type(G / 2)));
-                const words w = *reinterpret_cast<const words *>(values + L::kStepV + lane * (2 * G));
-                large = w[0];
+            typedef uint32_t words __attribute__((ext_vector_type(G / 2)));
+            words *const steps_at = reinterpret_cast<words *>(values + L::kStepV + lane * (2 * G));  // some of the page's steps; all of them in the wavefront
+            const words steps = *steps_at;
+            uint32_t any = steps[0];
 #pragma unroll
-                for (int j = 1; j < G / 2; ++j) large |= w[j];
-            }
+            for (int j = 1; j < G / 2; ++j) any |= steps[j];
+            const bool twice = __any((any & 0x40004000u) != 0);  // a step of 2 or more
+            auto large = [&]() __attribute__((always_inline)) { return (steps >> 14 & 0x00010001u) * 0xFFFFu; };  // the bits of those
             bmax = fmaxf(bmax, __shfl_xor(bmax, 16, 64));
             bmax = fmaxf(bmax, __shfl_xor(bmax, 32, 64)) * to_score;  // (in units of log 2 from here on)
-            const bool lowers = factor == kFactor && __any((large & 0x40004000u) != 0);  // a step of 2 or more
-            if (__any(bmax > run_max) || lowers) {
-                const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max - (lowers ? kLower : 0.0f));
+            auto product = [&](auto second, const float (&P)[16]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    if constexpr (decltype(second)::value) __builtin_amdgcn_sched_barrier(0);  // (a group after the other: registers)
+                    const u32x4 c = *reinterpret_cast<const u32x4 *>(values + L::kCodesV + (j * 64 + lane) * 16);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const h8 step = step_of(j, u);
+                        h8 p;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(P[8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
+                        const uint32_t c0 = c[2 * u], c1 = c[2 * u + 1];
+                        const u32x4 lo = {c0 & mask_lo, (c0 >> 8) & mask_lo, c1 & mask_lo, (c1 >> 8) & mask_lo};
+                        const u32x4 hi = {c0 & mask_hi, (c0 >> 8) & mask_hi, c1 & mask_hi, (c1 >> 8) & mask_hi};
+                        acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, lo), p, acc[2 * j], 0, 0, 0);
+                        acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, hi), p, acc[2 * j + 1], 0, 0, 0);
+                        acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_lo), p, acc[2 * j], 0, 0, 0);
+                        acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_hi), p, acc[2 * j + 1], 0, 0, 0);
+                    }
+                }
+            };
+            if (__any(bmax > run_max) || twice) {
+                const float new_max = fmaxf(run_max, bmax), corr = __builtin_amdgcn_exp2f(run_max - new_max);
                 run_max = new_max;
-                factor = lowers ? kFactor - kLower : factor;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
 #pragma unroll
                     for (int t = 0; t < DT; ++t) acc[t][i] *= corr;
                     rest[i] *= corr;
                 }
+                if (twice) {  // the large steps: the row's largest product to 2^14 .. 2^15 (by powers of two: exact in P and in sums of 32 bits)
+                    *steps_at = steps & large();
+                    float P[16], most = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], to_score, kFactor - run_max));
+#pragma unroll
+                    for (int j = 0; j < G; ++j)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            const h8 step = step_of(j, u);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) most = fmaxf(most, P[8 * u + e] * (float)step[e]);
+                        }
+                    most = fmaxf(most, __shfl_xor(most, 16, 64));
+                    most = fmaxf(most, __shfl_xor(most, 32, 64));
+                    const int down = most >= 32768.0f ? __builtin_amdgcn_frexp_expf(most) - 15 : 0;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) P[e] = __builtin_amdgcn_ldexpf(P[e], -down);
+#pragma unroll
+                    for (int t = 0; t < DT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_amdgcn_ldexpf(acc[t][i], -down);
+                    product(std::true_type(), P);
+#pragma unroll
+                    for (int t = 0; t < DT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_amdgcn_ldexpf(acc[t][i], down);
+                    *steps_at = steps & ~large();
+                }
             }
-            const float from_max = factor - run_max;
+            const float from_max = kFactor - run_max;
             h8 pv[2];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -370,24 +422,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
                 const u32x4 rows = {m == 15 ? 0x3C003C00u : w.x, m == 15 ? 0x3C003C00u : w.y, m == 15 ? 0x3C003C00u : w.z, m == 15 ? 0x3C003C00u : w.w};
                 rest = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, rows), pv[u], rest, 0, 0, 0);
             }
-#pragma unroll
-            for (int j = 0; j < G; ++j) {
-                const u32x4 c = *reinterpret_cast<const u32x4 *>(values + L::kCodesV + (j * 64 + lane) * 16);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const h8 step = step_of(j, u);
-                    h8 p;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
-                    const uint32_t c0 = c[2 * u], c1 = c[2 * u + 1];
-                    const u32x4 lo = {c0 & mask_lo, (c0 >> 8) & mask_lo, c1 & mask_lo, (c1 >> 8) & mask_lo};
-                    const u32x4 hi = {c0 & mask_hi, (c0 >> 8) & mask_hi, c1 & mask_hi, (c1 >> 8) & mask_hi};
-                    acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, lo), p, acc[2 * j], 0, 0, 0);
-                    acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, hi), p, acc[2 * j + 1], 0, 0, 0);
-                    acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_lo), p, acc[2 * j], 0, 0, 0);
-                    acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_hi), p, acc[2 * j + 1], 0, 0, 0);
-                }
-            }
+            product(std::false_type(), sc);
             wait_copies<63>();
             if (more) copy(next, 1);
             page = next;
@@ -416,7 +451,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
             }
         }
         if (real && !whole && r == 0) {
-            a.ws_ml[part * 2] = run_max + (kFactor - factor);  // (the maximum for which output and sum are taken 2^kFactor times, whatever this wavefront's factor)
+            a.ws_ml[part * 2] = run_max;
             a.ws_ml[part * 2 + 1] = sum;
         }
     }

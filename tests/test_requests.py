@@ -335,6 +335,29 @@ def test_attention_large_values_in_some_pages(S, h_q, h_kv, d, first, last, leas
 
 
 @gpu
+@pytest.mark.parametrize("least", [0, 300])
+@pytest.mark.parametrize("S,d,n,where,value,small,gap", [(1, 64, 1000, 100, 40, 0.05, 12), (1, 64, 1000, 100, 40, 0.005, 12), (1, 64, 8000, 100, 30.5, 0.01, 16), (1, 64, 8000, 70, 4000, 0.005, 12),
+                                                         (3, 128, 1000, 64, 60000, 0.01, 14), (3, 128, 1000, 999, 60000, 0.01, 14), (1, 256, 1000, 100, 40, 0.005, 12), (20, 256, 400, 0, 300, 0.02, 12)])
+def test_attention_large_value_beside_small_ones(S, d, n, where, value, small, gap, least):
+    """One large value in one group of 32, a group of small ones beside it, and a position with nearly all of P whose values are next to nothing: the others make up the result, with
+    products down to 2^-30 of the large value's.  (Products that are denormals of binary16 are off by 2^-25 of 2^14, times a code of 8: 2^-36, nothing against the bound's 2^-24.)"""
+    rng = np.random.default_rng(59)
+    q, k, v = _normal(rng, S, d), _normal(rng, n, 1, d), _normal(rng, n, 1, d)
+    k[5, 0] = q[0] * np.float16(gap * np.sqrt(d) / np.sum(q[0].astype(np.float64) ** 2))
+    v[:, :, 32:] *= np.float16(small)
+    v[5] *= np.float16(1e-3)
+    v[where, 0, 3] = value
+    table, num = _pages(rng, [n])
+    try:
+        B.lib().qfc_tune(15, least)
+        cache, K, V, P = _filled(rng, [n], 1, d, table, num, k=k, v=v)
+        got = _attend(_requests([S], [n], table), q, 1, cache).reshape(-1, 1, d)
+    finally:
+        B.lib().qfc_tune(15, 0)
+    _close(got, *ref.attention(q.reshape(-1, 1, d), K[0], V[0], P[0]))
+
+
+@gpu
 def test_attention_far_from_zero():
     """Keys and values with a mean far above their spread: offsets carry the result."""
     rng = np.random.default_rng(23)
