@@ -541,6 +541,7 @@ __global__ __launch_bounds__(256) void attn_q4_combine_rows_kernel(AttnQ4Args a)
     const Unit unit = units.at<false>(x);
     if (unit.b < 0 || unit.begin >= x || x - unit.begin > units.share || !units.may_cut(unit)) return;
     const Span span = unit.span;
+    if (unit.row0 >= span.count * a.g) return;  // (places that are nobody's)
     const int w0 = unit.begin / units.share, parts = (unit.end - 1) / units.share - w0 + 1, rows = min(16, span.count * a.g - unit.row0);
     const size_t slot0 = partial_of(unit, w0, units.share) * 16;
     // (four rows of a wavefront; everything's first parts are on their way at once, and those behind the last are read again and count as nothing)

@@ -476,6 +476,23 @@ def test_attention_repeats_bit_for_bit():
     assert np.array_equal(first, _attend(req, q, 8, cache))
 
 
+@gpu
+@pytest.mark.parametrize("S,n,h_q,h_kv", [([1, 1], [3000, 700], 4, 1), ([40, 3], [2500, 900], 4, 2), ([600], [1400], 8, 2), ([327, 300], [2000, 1700], 12, 4)])
+def test_attention_whatever_the_workspace_holds(S, n, h_q, h_kv):
+    """Partial results are read where a wavefront has left some: not in the places of blocks without a partner, of rows behind a block's last, of units that were not cut."""
+    rng = np.random.default_rng(60)
+    d = 64
+    table, num = _pages(rng, n)
+    cache, _, _, _ = _filled(rng, n, h_kv, d, table, num)
+    q, req = _t(_normal(rng, sum(S), h_q * d)), _requests(S, n, table)
+    out = []
+    for fill in (0, 0xFF, 0x7C):  # (NaN; large values)
+        ws = torch.full((B.qfc_attention_q4_workspace_size(req, h_q, cache),), fill, dtype=torch.uint8, device=DEV)
+        out.append(torch.zeros_like(q))
+        B.qfc_attention_q4(q, req, h_q, cache, ws, out[-1])
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2]) and bool(torch.isfinite(out[0]).all())
+
+
 # ---------------------------------------------------------------- adapters
 def _adapters(rng, count, rank, K, N):
     a = (_normal(rng, count, rank, K).astype(np.float32) / np.sqrt(K)).astype(np.float16)
