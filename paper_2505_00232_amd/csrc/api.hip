@@ -519,8 +519,7 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
     const int cus = device_cus();
     const AttnQ4Plan p = attention_plan(requests, h_q, cache, cus);
     if (workspace_bytes < p.bytes) return QFC_ERR_BUFFER_TOO_SMALL;
-    // (places in the run of all blocks' pages, some more for each)
-    if (p.blocks * cache->h_kv * (p.pages + 4) > INT32_MAX - (1 << 24)) return QFC_ERR_UNSUPPORTED;
+    if (most_places(p, cache->h_kv) > INT32_MAX - (1 << 24)) return QFC_ERR_UNSUPPORTED;
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_attention_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, p, workspace, out_f16, cus,
                                           static_cast<hipStream_t>(stream)));

@@ -39,10 +39,12 @@ struct AttnQ4Args {
     Requests req;
     float *ws_o, *ws_ml;  // [workers, 2, 16, D] partial outputs, [.., 2] (maximum, sum)
     int h_q, h_kv, g, workers, least, whole;
+    int most;  // places that requests within the call's limits have at most
     float scale;
 };
 
-// Sums of places end at the largest int: requests whose arrays overlap have more than a call may have, and what lies behind is left out.
+// Sums of places end at the largest int.  Requests whose arrays overlap may have more places than a call's limits allow: what lies behind those (AttnQ4Args::most, 2^24 and more below
+// the largest int, so that no place of a unit that is worked on passes it) is left out.
 __device__ __forceinline__ int add(int x, int y) { return __builtin_elementwise_add_sat(x, y); }
 // sum over the lanes up to this one
 __device__ __forceinline__ int sum_upto(int x) {
@@ -82,7 +84,7 @@ struct Units {
         }
         all = last(sum_upto(all)), units = min(last(sum_upto(units)), INT32_MAX / 2);
         over = all / 4 >= a.workers ? 2 : 0;
-        share = max(a.least, add(add(all, over * units), a.workers - 1) / a.workers);
+        share = max(a.least, (min(add(all, over * units), a.most) + a.workers - 1) / a.workers);
         if (a.req.batch > 64) load(0);
         sum();
     }
@@ -116,28 +118,29 @@ struct Units {
     template <bool BY_INDEX>
     __device__ __forceinline__ Unit at(int x) {
         Unit u = {-1, 0, 0, 0, 0, {0, 0, 0}};
+        auto plus = [](int p, int q) __attribute__((always_inline)) { return BY_INDEX ? add(p, q) : p + q; };  // (by place: at most x and a unit's length)
         for (;;) {
             const int of = BY_INDEX ? upto_u : upto, base = BY_INDEX ? before_u : before;
             const uint64_t past = __ballot(of > x - base);
             if (past) {
                 const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
                 const int n = __builtin_amdgcn_readlane(blocks, l), units = of_pair(n), len = __builtin_amdgcn_readlane(pages, l) + over * units;
-                const int first = before + __builtin_amdgcn_readlane(upto, l) - pairs(n) * a.h_kv * len;
+                const int first = plus(before, __builtin_amdgcn_readlane(upto, l) - pairs(n) * a.h_kv * len);
                 const int nth = x - (before_u + __builtin_amdgcn_readlane(upto_u, l) - pairs(n) * a.h_kv * units);
                 u.span = Span{__builtin_amdgcn_readlane(span.first, l), __builtin_amdgcn_readlane(span.count, l), __builtin_amdgcn_readlane(span.positions, l)};
                 // (the same in every lane: said explicitly, it stays in scalar registers)
                 const int pair = __builtin_amdgcn_readfirstlane(BY_INDEX ? nth / units : (x - first) / len), k = __builtin_amdgcn_readfirstlane(pair / a.h_kv);
-                const int begin = first + pair * len;
+                const int begin = plus(first, pair * len);
                 u.b = __builtin_amdgcn_readfirstlane(b0 + l);
                 u.kv = __builtin_amdgcn_readfirstlane(pair - k * a.h_kv);
                 u.begin = __builtin_amdgcn_readfirstlane(begin);
-                u.end = __builtin_amdgcn_readfirstlane(begin + len);
+                u.end = __builtin_amdgcn_readfirstlane(plus(begin, len));
                 if (units == 2) {  // the pair's first block, its second one (the middle block has none), places that are nobody's
-                    const int cut = begin + over + pages_of(u.span, k), other = n - 1 - k, end = other > k ? cut + over + pages_of(u.span, other) : cut;
+                    const int cut = plus(begin, over + pages_of(u.span, k)), other = n - 1 - k, end = other > k ? plus(cut, over + pages_of(u.span, other)) : cut;
                     const int which = BY_INDEX ? (nth % 2 == 0 ? 0 : other > k ? 1 : 2) : x < cut ? 0 : x < end ? 1 : 2;
                     u.row0 = __builtin_amdgcn_readfirstlane(16 * (which == 0 ? k : which == 1 ? other : n));
                     u.begin = __builtin_amdgcn_readfirstlane(which == 0 ? begin : which == 1 ? cut : end);
-                    u.end = __builtin_amdgcn_readfirstlane(which == 0 ? cut : which == 1 ? end : begin + len);
+                    u.end = __builtin_amdgcn_readfirstlane(which == 0 ? cut : which == 1 ? end : plus(begin, len));
                 }
                 return u;
             }
@@ -148,6 +151,8 @@ struct Units {
             sum();
         }
     }
+    // wavefronts that have places of a unit, from the w0-th on (the last one's share ends where the call's places end)
+    __device__ __forceinline__ int parts_of(const Unit &u, int w0) const { return min((u.end - 1) / share, a.workers - 1) - w0 + 1; }
     __device__ __forceinline__ bool may_cut(const Unit &u) const { return u.end - u.begin - over > max(over ? share / 2 : kWhole, a.whole); }
 };
 // Place of the partial results that worker w leaves of a unit
@@ -471,9 +476,9 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a, int 
         const int in_unit = (int)(i % unit_rows);
         const Unit unit = units.at<true>((int)(i / unit_rows));
         if (unit.b < 0) return;
-        if (!units.may_cut(unit)) continue;
-        const int w0 = unit.begin / units.share, parts = (unit.end - 1) / units.share - w0 + 1;
-        if (parts == 1) continue;  // (written by the first kernel)
+        const int w0 = unit.begin / units.share, parts = units.parts_of(unit, w0);
+        if (w0 >= a.workers) return;  // (behind the last wavefront's places)
+        if (!units.may_cut(unit) || parts <= 1) continue;  // (written by the first kernel, or without a place)
         const Span span = unit.span;
         const int row = unit.row0 + in_unit;
         if (row >= span.count * a.g) continue;
@@ -542,7 +547,7 @@ __global__ __launch_bounds__(256) void attn_q4_combine_rows_kernel(AttnQ4Args a)
     if (unit.b < 0 || unit.begin >= x || x - unit.begin > units.share || !units.may_cut(unit)) return;
     const Span span = unit.span;
     if (unit.row0 >= span.count * a.g) return;  // (places that are nobody's)
-    const int w0 = unit.begin / units.share, parts = (unit.end - 1) / units.share - w0 + 1, rows = min(16, span.count * a.g - unit.row0);
+    const int w0 = unit.begin / units.share, parts = units.parts_of(unit, w0), rows = min(16, span.count * a.g - unit.row0);
     const size_t slot0 = partial_of(unit, w0, units.share) * 16;
     // (four rows of a wavefront; everything's first parts are on their way at once, and those behind the last are read again and count as nothing)
     auto place = [&](int row, int c) __attribute__((always_inline)) { return (c == 0 ? slot0 : (size_t)(w0 + c) * 32) + min(wave + 4 * row, rows - 1); };
@@ -615,7 +620,7 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     p.many = p.blocks * h_kv * (p.rows < 16 ? p.rows : 16) > 16L * num_cus;
     const int most_shares = p.many ? 62 : 254;  // (and two ends: a lane of the combination's wavefront, or of its four, for each)
     p.least = (p.pages + most_shares) / most_shares;
-    if (const int forced = tuning().attn_q4_pages; forced > p.least) p.least = forced;
+    if (const int forced = tuning().attn_q4_pages; forced > p.least) p.least = forced < 1 << 20 ? forced : 1 << 20;
     const long shares = (most_pages + p.least - 1) / p.least;
     p.workers = (int)(shares < waves ? shares : waves);
     if (p.workers < 1) p.workers = 1;
@@ -623,6 +628,8 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
     p.bytes = 256 + (p.shared ? (size_t)p.workers * 2 * 16 * (d + 2) * sizeof(float) : 0);
     return p;
 }
+
+long most_places(const AttnQ4Plan &p, int h_kv) { return p.blocks * h_kv * (p.pages + 4); }
 
 hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out, int num_cus,
                                hipStream_t st) {
@@ -632,7 +639,7 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
     a.pages = static_cast<const char *>(pages);
     a.req = req;
     a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv;
-    a.workers = p.workers, a.least = p.least, a.whole = p.shared ? 0 : INT32_MAX;  // (no second launch: nothing is cut)
+    a.workers = p.workers, a.least = p.least, a.most = (int)most_places(p, h_kv), a.whole = p.shared ? 0 : INT32_MAX;  // (no second launch: nothing is cut)
     a.ws_o = static_cast<float *>(workspace);
     a.ws_ml = a.ws_o + (size_t)p.workers * 2 * 16 * d;
     a.scale = 1.4426950408889634f / sqrtf((float)d);

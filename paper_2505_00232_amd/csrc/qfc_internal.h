@@ -401,6 +401,7 @@ struct AttnQ4Plan {
     size_t bytes;  // of the workspace
 };
 AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int max_tokens, int max_context, int num_cus);
+long most_places(const AttnQ4Plan &p, int h_kv);  // in the run of all blocks' pages, some more for each; to be below INT32_MAX - 2^24
 hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out, int num_cus,
                                hipStream_t st);
 struct AdapterPlan {

@@ -414,6 +414,29 @@ def test_arrays_that_break_the_rules_stay_inside_the_buffers():
 
 
 @gpu
+def test_requests_that_overlap_until_their_places_pass_an_int():
+    """Thousands of requests that each claim all rows: the call ends, does no more than its limits allow, and writes nothing outside its rows."""
+    T, batch, longest, d = 16384, 4096, 131072, 64
+    start = np.zeros(batch + 1, dtype=np.int32)
+    start[1::2] = T  # 0, T, 0, T, ...
+    cache = B.PagedCache(4, 1, d)
+    cache.pages.zero_()
+    table = torch.zeros((batch, longest // 64), dtype=torch.int32, device=DEV)
+    req = B.Requests(_t(start), torch.full((batch,), longest, dtype=torch.int32, device=DEV), table, T, T, longest)
+    guard = torch.full((T + 32, d), 3.0, dtype=torch.float16, device=DEV)
+    ws = torch.empty(B.qfc_attention_q4_workspace_size(req, 1, cache) + 1024, dtype=torch.uint8, device=DEV)
+    ws[-1024:] = 0x5A
+    try:
+        for least in (0, 40):
+            B.lib().qfc_tune(15, least)
+            B.qfc_attention_q4(torch.ones((T, d), dtype=torch.float16, device=DEV), req, 1, cache, ws, guard[16:-16])
+            torch.cuda.synchronize()
+            assert bool((guard[:16] == 3.0).all()) and bool((guard[-16:] == 3.0).all()) and bool((ws[-1024:] == 0x5A).all())
+    finally:
+        B.lib().qfc_tune(15, 0)
+
+
+@gpu
 def test_pages_beyond_two_gigabytes():
     rng = np.random.default_rng(26)
     h_q, h_kv, d, n = 16, 8, 128, [130]
