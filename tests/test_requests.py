@@ -183,6 +183,19 @@ def test_rotary_table(rot, extra):
 
 
 @gpu
+def test_rotary_table_of_more_angles_than_a_launch_has_threads():
+    """2^26 positions (the most that a batch may have) of 64 pairs.  Bound: the rounding to 32 bits 2^-25; on either side the frequency's roundings, 3 (1 + x) e^-x 2^-53 <= 3 2^-53
+    for f = e^-x, at 2^26 positions 2^-25.4; together less than 2^-23."""
+    positions, rotary = 1 << 26, B.make_rotary(128, 500000.0)
+    table = B.qfc_rotary_table(rotary, positions)
+    few = B.qfc_rotary_table(rotary, 5000)
+    assert torch.equal(table[:5000], few)
+    at = np.unique(np.concatenate([np.random.default_rng(2).integers(0, positions, 300), np.arange(positions - 3, positions), (1 << 22) + np.arange(-2, 3), (1 << 25) + np.arange(-2, 3)]))
+    got = table[torch.from_numpy(at).to(DEV)].cpu().numpy()
+    assert np.max(np.abs(got - ref.rotary_table(128, at, 500000.0))) <= 2.0 ** -23
+
+
+@gpu
 def test_rotary_table_is_the_other_one_where_they_meet():
     a = B.qfc_rope_table(B.AttnShape(1, 2, 1, 128, 64), 10000.0, 5000)
     b = B.qfc_rotary_table(B.make_rotary(128, 10000.0), 5000)
