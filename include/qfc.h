@@ -373,16 +373,17 @@ qfc_status_t qfc_rotary_table(const qfc_rotary_t *rotary, int32_t positions, flo
  * positions (table_positions says how many).  No two rows may have the same place in the cache.
  * Errors: QFC_ERR_INVALID_ARG (null pointers, sizes, h_q not a multiple of h_kv, max_context beyond the page table or the
  * rotary table, rotary members out of range), QFC_ERR_UNSUPPORTED (d_head other than 64, 128, 256; rot_dim not a multiple of 16 or above
- * d_head; more than 65535 heads or KV heads of all requests), QFC_ERR_ALIGNMENT (16 bytes; int32 arrays 4, the table 8). */
+ * d_head; h_q + 2 h_kv or batch * h_kv above 65535, max_tokens * h_q above 2^26, tokens * h_q above 2^30, tokens * d_head above 2^34,
+ * max_context above 2^26), QFC_ERR_ALIGNMENT (16 bytes; int32 arrays 4, the table 8). */
 qfc_status_t qfc_append_q4(const void *qkv_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_rotary_t *rotary,
                            const float *rope_table, int32_t table_positions, const qfc_q4_cache_t *cache, void *q_out, void *stream);
 
 /* The values that the cache holds for the batch's new tokens: k, v binary16 [tokens, h_kv, d_head]; zeros for a token
- * without a page.  Errors as qfc_append_q4. */
+ * without a page.  Errors as qfc_append_q4, h_q taken as h_kv. */
 qfc_status_t qfc_read_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, void *k, void *v, void *stream);
 
 /* Bytes of scratch qfc_attention_q4 needs for a batch of this size (batch, tokens, max_tokens and max_context are read; host pointers): partial
- * results of requests whose positions several wavefronts share, 68 MB at most. */
+ * results of requests whose positions several wavefronts share, 68 MB at most.  Errors as qfc_append_q4's for sizes. */
 qfc_status_t qfc_attention_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
 
 /* Attention of a batch of requests over the cache: out = softmax(q K^T / sqrt(d_head)) V for each row and head, q and out binary16

@@ -432,7 +432,10 @@ static qfc_status_t check_q4_cache(const qfc_q4_cache_t *c) {
 static qfc_status_t check_batch(const qfc_requests_t *r, int32_t h_q, const qfc_q4_cache_t *c) {
     if (const qfc_status_t s = check_q4_cache(c); s != QFC_OK) return s;
     if (!r || r->batch < 1 || r->tokens < 0 || r->max_tokens < 1 || r->max_context < 1 || h_q < 1 || h_q % c->h_kv != 0) return QFC_ERR_INVALID_ARG;
-    if ((long)h_q + 2L * c->h_kv > 65535 || (long)r->batch * c->h_kv > 65535 || (long)r->max_tokens * h_q > 1L << 26 || (long)r->tokens * h_q > 1L << 30 || r->max_context > 1 << 26) return QFC_ERR_UNSUPPORTED;
+    // (a launch has fewer than 2^32 threads: eight values of a token each)
+    if ((long)h_q + 2L * c->h_kv > 65535 || (long)r->batch * c->h_kv > 65535 || (long)r->max_tokens * h_q > 1L << 26 || (long)r->tokens * h_q > 1L << 30 || (long)r->tokens * c->d_head > 1L << 34 ||
+        r->max_context > 1 << 26)
+        return QFC_ERR_UNSUPPORTED;
     return QFC_OK;
 }
 

@@ -150,6 +150,25 @@ def test_refusals_of_the_largest_sizes_and_calls_without_tokens():
     assert L.qfc_attention_q4(None, none, 3, cache, None, 0, None, s) == 1
 
 
+def test_refusals_of_batches_above_each_limit():
+    """At a limit the workspace's size is given; one more is refused by every call."""
+    L = B.lib()
+    A, s, size = 0x1000, ctypes.c_void_p(0), ctypes.c_size_t(0)
+    pairs = [  # (batch, tokens, max_tokens, max_context, h_q, h_kv, d) at the limit, and above it
+        ((2, 2, 1, 128, 65531, 1, 64), None), (None, (2, 2, 1, 128, 65534, 1, 64)), ((65535, 2, 1, 128, 1, 1, 64), (65536, 2, 1, 128, 1, 1, 64)),
+        ((2, 2, 1 << 25, 128, 2, 1, 64), (2, 2, (1 << 25) + 1, 128, 2, 1, 64)), ((16, 1 << 22, 1 << 18, 128, 256, 1, 64), (16, (1 << 22) + 1, 1 << 18, 128, 256, 1, 64)),
+        ((2, 1 << 28, 1 << 26, 128, 1, 1, 64), (2, (1 << 28) + 1, 1 << 26, 128, 1, 1, 64)), ((2, 1 << 26, 1 << 26, 128, 1, 1, 256), (2, (1 << 26) + 1, 1 << 26, 128, 1, 1, 256)),
+        ((2, 2, 1, 1 << 26, 2, 1, 64), (2, 2, 1, (1 << 26) + 1, 2, 1, 64))]
+    for case, want in [(c, w) for pair in pairs for c, w in zip(pair, (0, 2)) if c]:
+        batch, tokens, most, longest, h_q, h_kv, d = case
+        req = ctypes.byref(B.RequestsDesc(A, A, A, batch, tokens, most, longest, 1 << 21))
+        cache = ctypes.byref(B.CacheDesc(A, 4, h_kv, d))
+        assert L.qfc_attention_q4_workspace_size(req, h_q, cache, ctypes.byref(size)) == want, case
+        if want:
+            assert L.qfc_append_q4(A, req, h_q, None, None, 0, cache, A, s) == 2 and L.qfc_attention_q4(A, req, h_q, cache, A, 1 << 60, A, s) == 2
+            assert h_q != h_kv or L.qfc_read_q4(req, cache, A, A, s) == 2
+
+
 def test_binding_refuses_host_tensors():
     c = torch.zeros(2, dtype=torch.int32)
     with pytest.raises(ValueError):
