@@ -434,7 +434,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
         }
 
         // ---- output row m (2^kFactor times, unnormalized), its maximum and sum
-        const float back = 16777216.0f, sum = __shfl(rest[3], 48 + m, 64), inv = sum > 0.0f ? 1.0f / sum : 0.0f;  // (a row that sees nothing: 0)
+        const float back = 16777216.0f, sum = __shfl(rest[3], 48 + m, 64), inv = sum != 0.0f ? 1.0f / sum : 0.0f;  // (a row that sees nothing: 0; one of a NaN stays NaN)
         const size_t part = partial_of(unit, worker, units.share) * 16 + m;
 #pragma unroll
         for (int j = 0; j < G; ++j) {
@@ -529,7 +529,7 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a, int 
                 total = fmaf(fw, sums[w], total);
                 y = fmaf(fw, outs[w][threadIdx.x], y);
             }
-            a.out[((size_t)(span.first + row / a.g) * a.h_q + unit.kv * a.g + row % a.g) * D + threadIdx.x] = (_Float16)(total > 0.0f ? y / total : 0.0f);
+            a.out[((size_t)(span.first + row / a.g) * a.h_q + unit.kv * a.g + row % a.g) * D + threadIdx.x] = (_Float16)(total != 0.0f ? y / total : 0.0f);
         }
     }
 }
@@ -585,7 +585,7 @@ __global__ __launch_bounds__(256) void attn_q4_combine_rows_kernel(AttnQ4Args a)
         }
         if (wave + 4 * i >= rows) return;
         const int row = unit.row0 + wave + 4 * i;
-        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
         _Float16 *out = a.out + ((size_t)(span.first + row / a.g) * a.h_q + unit.kv * a.g + row % a.g) * D + PER * lane;
 #pragma unroll
         for (int e = 0; e < PER; ++e) out[e] = (_Float16)(o[e] * inv);

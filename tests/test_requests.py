@@ -532,6 +532,23 @@ def test_attention_repeats_bit_for_bit():
 
 
 @gpu
+@pytest.mark.parametrize("S,n,h_q,h_kv", [([1, 1, 1], [3000, 700, 40], 4, 1), ([3, 5], [250, 60], 4, 2), ([600], [1400], 8, 2)])
+def test_attention_of_queries_that_are_not_finite(S, n, h_q, h_kv):
+    """Walked by one wavefront and by several, joined by either kernel: their own row and head is NaN, the others keep their bits."""
+    rng = np.random.default_rng(61)
+    d = 64
+    table, num = _pages(rng, n)
+    cache, _, _, _ = _filled(rng, n, h_kv, d, table, num)
+    q, req = _normal(rng, sum(S), h_q * d), _requests(S, n, table)
+    clean = _attend(req, q, h_q, cache)
+    bad = np.zeros((sum(S), h_q), dtype=bool)
+    for row, head, value in ((0, 1, np.nan), (sum(S) - 1, 0, np.nan), (sum(S) // 2, 2, np.inf)):
+        q.reshape(-1, h_q, d)[row, head, 7], bad[row, head] = value, True
+    got = _attend(req, q, h_q, cache).reshape(-1, h_q, d)
+    assert np.array_equal(got[~bad], clean.reshape(-1, h_q, d)[~bad]) and np.all(np.isnan(got[bad]))
+
+
+@gpu
 @pytest.mark.parametrize("S,n,h_q,h_kv", [([1, 1], [3000, 700], 4, 1), ([40, 3], [2500, 900], 4, 2), ([600], [1400], 8, 2), ([327, 300], [2000, 1700], 12, 4)])
 def test_attention_whatever_the_workspace_holds(S, n, h_q, h_kv):
     """Partial results are read where a wavefront has left some: not in the places of blocks without a partner, of rows behind a block's last, of units that were not cut."""
