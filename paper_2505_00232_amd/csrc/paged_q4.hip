@@ -263,28 +263,28 @@ __global__ __launch_bounds__(256) void read_q4_kernel(ReadArgs a) {
     }
 }
 
-// table[p][i] = amplitude (cos, sin) of p f_i, in fp64 as far as the rounding to 32 bits
-__global__ __launch_bounds__(256) void rotary_table_kernel(int half, int positions, double log_base, double factor, double turns, double low, double high, double amplitude,
+// table[p][i] = amplitude (cos, sin) of p f_i, in fp64 as far as the rounding to 32 bits; the angles from `first` on
+__global__ __launch_bounds__(256) void rotary_table_kernel(long first, int half, int positions, double log_base, double factor, double turns, double low, double high, double amplitude,
                                                            float2 *__restrict__ table) {
-    const long total = (long)positions * half;
-    for (long idx = (long)blockIdx.x * 256 + threadIdx.x; idx < total; idx += (long)gridDim.x * 256) {
-        const int i = (int)(idx % half), pos = (int)(idx / half);
-        double f = exp(-(double)i / (double)half * log_base);
-        // a wave that turns often within `turns` 2 pi positions keeps its frequency, one that hardly turns has it divided
-        const double keep = turns > 0.0 ? fmin(fmax((turns * f - low) / (high - low), 0.0), 1.0) : 0.0;
-        f = keep * f + (1.0 - keep) * f / factor;
-        double sn, cs;
-        sincos((double)pos * f, &sn, &cs);
-        table[idx] = make_float2((float)(amplitude * cs), (float)(amplitude * sn));
-    }
+    const long idx = first + (long)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= (long)positions * half) return;
+    const int i = (int)(idx % half), pos = (int)(idx / half);
+    double f = exp(-(double)i / (double)half * log_base);
+    // a wave that turns often within `turns` 2 pi positions keeps its frequency, one that hardly turns has it divided
+    const double keep = turns > 0.0 ? fmin(fmax((turns * f - low) / (high - low), 0.0), 1.0) : 0.0;
+    f = keep * f + (1.0 - keep) * f / factor;
+    double sn, cs;
+    sincos((double)pos * f, &sn, &cs);
+    table[idx] = make_float2((float)(amplitude * cs), (float)(amplitude * sn));
 }
 
 }  // namespace
 
 hipError_t launch_rotary_table(int rot, double base, double factor, int original, double low, double high, double amplitude, int positions, float *table, hipStream_t st) {
-    const long blocks = ((long)positions * (rot / 2) + 255) / 256, most = 1L << 20;  // (a launch has fewer than 2^32 threads)
-    rotary_table_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, st>>>(rot / 2, positions, log(base), factor, (double)original / (2.0 * M_PI), low, high, amplitude,
-                                                                         reinterpret_cast<float2 *>(table));
+    const long total = (long)positions * (rot / 2), most = 1L << 28;  // (a launch has fewer than 2^32 threads)
+    for (long first = 0; first < total; first += most)
+        rotary_table_kernel<<<(unsigned)(((total - first < most ? total - first : most) + 255) / 256), 256, 0, st>>>(
+            first, rot / 2, positions, log(base), factor, (double)original / (2.0 * M_PI), low, high, amplitude, reinterpret_cast<float2 *>(table));
     return hipGetLastError();
 }
 
