@@ -337,7 +337,8 @@ typedef struct qfc_requests {
  * consecutive values of a position's head a binary16 step and a binary16 offset, value = offset + step * (code - 8), code 0 .. 15.
  * From binary16 values x (operations rounded to 32 bits each):
  *   step = fp16((max - min) / 15), offset = fp16(min + 8 step), code = clamp(rne((x - offset) * (1 / step)) + 8, 0, 15); step 0: code 8.
- * pages: device, 16-byte aligned, qfc_q4_cache_size bytes (80 * d_head per page and head); need not be initialized.  Values have to be finite. */
+ * pages: device, 16-byte aligned, qfc_q4_cache_size bytes (80 * d_head per page and head); need not be initialized.  Values have to be finite, rotated
+ * keys too. */
 typedef struct qfc_q4_cache {
     void *pages; /* device */
     int32_t num_pages, h_kv, d_head;
@@ -407,7 +408,7 @@ qfc_status_t qfc_adapters_workspace_size(const qfc_adapters_t *adapters, int32_t
 
 /* out[m] = fp16(y[m] + scale[a] B[a] (A[a] x[m])), a = ids[m], beside a shared layer whose output y is: every row (token) may have an
  * adapter of its own; an id outside [0, count) has none, and out[m] = y[m].
- *   x binary16 [M, K]; ids device, int32 [M]; y, out binary16 [M, N] (out may be y); K a multiple of 32.
+ *   x binary16 [M, K], M 1 and more; ids device, int32 [M]; y, out binary16 [M, N] (out may be y); K a multiple of 32.
  * workspace: device scratch of at least qfc_adapters_workspace_size bytes, one call's at a time.  Errors: QFC_ERR_INVALID_ARG (null pointers, sizes),
  * QFC_ERR_UNSUPPORTED (rank not a multiple of 8 or above 128, N above 2^23, M above 2^24), QFC_ERR_ALIGNMENT (16 bytes; ids and scale 4),
  * QFC_ERR_BUFFER_TOO_SMALL. */

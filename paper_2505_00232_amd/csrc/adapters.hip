@@ -4,7 +4,7 @@
 // the sums over a part of K in the workspace, in 32 bits; the second adds the parts up, multiplies with B and adds the shared layer's output.  An adapter's results are kept for its
 // own rows only, so that nothing of one adapter, infinities included, reaches another one's rows.  Where every row has an adapter of its own (a decode step), the adapters of a
 // block of rows are dealt to several workgroups.
-// The low-rank values are rounded to binary16 between the two, scaled by a power of two to their row's largest (2^-11 of a value, 2^-25 of the largest), for the matrix product;
+// The low-rank values are rounded to binary16 between the two, scaled by a power of two to their row's largest (2^-11 of a value, 2^-38 of the largest), for the matrix product;
 // the output is rounded once.  Bound: memory (A and B of the adapters in use, x, y and out), for few rows the latency of two launches.
 #include "qfc_internal.h"
 
@@ -381,8 +381,11 @@ AdapterPlan plan_adapters(int M, int K, int N, int num_cus) {
     if (parts < 1) parts = 1;
     p.part_k = (pieces + parts - 1) / parts * 128;
     p.parts = (K + p.part_k - 1) / p.part_k;
-    // many rows: blocks of 64 share B's tiles (us with 16 / 64: 300 x 28672 23.0 / 21.8, 520 x 6144 17.3 / 16.1, 1000 x 6144 19.5 / 20.9, 2048 x 6144 38 / 29, 1000 x 28672 76 / 58);
-    // columns per workgroup so that the card holds all workgroups at once, two to a compute unit (2048 x 28672: 107 us, with four 117 and 112 for blocks of 32)
+    // many rows: blocks of 64 share B's tiles.  (us with 16 / 64, rows of five requests one behind the other: 300 x 28672 21.2 / 19.8, 520 x 6144 17.2 / 16.2, 1000 x 6144 19.4 / 20.6,
+    // 2048 x 6144 38 / 29, 1000 x 28672 76 / 58.  Rows in turn with 40 adapters, which the host does not know, would want blocks of 16 up to some 1000 rows: 300 x 4096 30 / 40,
+    // 1000 x 6144 77 / 94, 2048 x 6144 183 / 154.)
+    // Columns per workgroup so that the card holds all workgroups at once, two to a compute unit (2048 x 28672: 107 us, with four 117 and 112 for blocks of 32; ranks above 64 have
+    // registers for one, and take two rounds)
     p.block_rows = M > 256 ? 64 : 16;
     const long works = (long)((M + p.block_rows - 1) / p.block_rows) * pieces_n;
     p.tiles = (int)((works + 2L * num_cus - 1) / (2L * num_cus));

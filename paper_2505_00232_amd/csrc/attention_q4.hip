@@ -9,12 +9,12 @@
 // P is multiplied with the step in 32 bits and rounded to binary16 once per group; the -8 is taken off with the same rounded values (an MFMA with a
 // constant into the same sums: taken off at the end, from sums of their own, it left errors of 2^-15 of 8 steps where one position has nearly all of P), so that what the rounding
 // leaves is relative to a centred code, and the offsets are again one MFMA, whose last row, ones, gives the sum of P.
-// Cached values are never rounded: as binary16 copies, with the kernel for prompts over a 16-bit cache (attention.hip), prompts of 1024 and 601 tokens took 48 us instead of 78, with
+// Cached values are never rounded: as binary16 copies, with the kernel for prompts over a 16-bit cache (attention.hip), prompts of 1024 and 601 tokens took 48 us instead of 76, with
 // twice the error (relative to the result's norm 4.0e-4 instead of 2.8e-4, where the output's own rounding is 2.1e-4).
 //
 // P is taken 2^14 times as large: with steps below 2 every product is below 2^15, and binary16 keeps its 11 bits down to a product of 2^-28.  The steps of 2 and more (values some 30
 // apart and more) of a page are multiplied on their own, in a turn before the others' with each row's P lowered as far as that row's products need, so that what binary16 then loses is
-// little against a product that is in the row's sums; all others keep their bits.
+// little against a product that is in the row's sums; all others keep their bits.  (Where every page has such steps: 32 requests of up to 8192 positions 48 -> 61 us, prompts 76 -> 124.)
 #include <type_traits>
 
 #include "paged_q4.h"
@@ -174,7 +174,7 @@ struct Place {
 
 // Up to 16 query rows of a KV head at a time.  The wavefronts work for themselves, each with copies of its own on the way.  Bound: memory where rows are few (32 requests of up to 8192
 // positions, 32 heads on 8 of 128 values: 168 MB in 41 us, 4.1 TB/s), the some 450 vector instructions of a page and block, and little that runs beside them, where they are many
-// (prompts of 1024 and 601 tokens 67 us).  Two blocks that share the codes' taking apart need more registers than two wavefronts of a SIMD have, and were slower (prompts 187 us, 167
+// (prompts of 1024 and 601 tokens 72 us).  Two blocks that share the codes' taking apart need more registers than two wavefronts of a SIMD have, and were slower (prompts 187 us, 167
 // with one, both before blocks came in pairs).
 template <int D>
 __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_kernel(AttnQ4Args a) {
     }
 }
 
-// Joining costs 4 to 12 us, most of it a launch and four reads one behind the other.
+// Joining costs 4 to 13 us, most of it a launch and four reads one behind the other.
 // The units that several wavefronts share, a row of one (unit_rows in each) per workgroup, or one after the other.  Its four wavefronts take the
 // parts in turn, lane c the (maximum, sum) of its c-th and D / 64 columns of the partial outputs; they meet in LDS.
 template <int D>
@@ -534,7 +534,7 @@ __global__ __launch_bounds__(256) void attn_q4_combine_kernel(AttnQ4Args a, int 
     }
 }
 
-// The same where rows are many (few: chunks of 40 tokens of two requests 33 us, this kernel 39; many: a chunk of 300 tokens beside tokens 97 us, a workgroup per row 124): a workgroup
+// The same where rows are many (a call: chunks of 40 tokens of two requests 35 us, with this kernel 40; a chunk of 300 tokens beside tokens 99 us, a workgroup per row 131): a workgroup
 // per worker, for the unit that the worker's share begins inside of, if it is the first to do so; a wavefront per row.
 template <int D>
 __global__ __launch_bounds__(256) void attn_q4_combine_rows_kernel(AttnQ4Args a) {
