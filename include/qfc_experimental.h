@@ -43,7 +43,7 @@ extern "C" {
  *   key 12 attention with at most 16 query rows per KV head: workgroups per KV head (0 = automatic; 1 .. 64)
  *   key 13 attention with more than 16 query rows per KV head: blocks of 16 (-1 automatic, 0 never, 1 always)
  *   key 14 prefill attention: wavefronts that share the walk of the same query rows (0 = automatic; 1, 2)
- *   key 15 attention over the 4-bit cache: pages a wavefront takes at least (0 = automatic); the workspace's size follows */
+ *   key 15 attention over the 4-bit cache: pages a wavefront takes at least (0 = automatic; up to 2^20); the workspace's size follows */
 void qfc_tune(int32_t key, int32_t value);
 
 /* Measurement probe (bench.py --probe-mfma): `workgroups` workgroups of four wavefronts each issue
