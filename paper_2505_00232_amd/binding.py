@@ -30,6 +30,8 @@ QFC_ROPE_HALF, QFC_ROPE_INTERLEAVED = 0, 1
 EXPORTS = ["qfc_packed_size", "qfc_pack_weights", "qfc_unpack_weights", "qfc_workspace_size",
            "qfc_bind_workspace", "qfc_quantize_activations", "qfc_forward", "qfc_forward_fused", "qfc_forward_static", "qfc_rmsnorm", "qfc_rope_qkv", "qfc_rope_table", "qfc_forward_qkv_rope", "qfc_attention_workspace_size", "qfc_attention", "qfc_forward_q8",
            "qfc_forward_acc_i32", "qfc_embedding", "qfc_q4_cache_size", "qfc_rotary_table", "qfc_append_q4", "qfc_read_q4", "qfc_attention_q4_workspace_size", "qfc_attention_q4",
+           "qfc_pages_workspace_size", "qfc_copy_pages", "qfc_take_pages", "qfc_fork_pages", "qfc_free_pages", "qfc_compact_pages", "qfc_attention_shared_q4_workspace_size", "qfc_attention_shared_q4",
+           "qfc_bound_pages_q4", "qfc_select_pages_q4_workspace_size", "qfc_select_pages_q4", "qfc_attention_selected_q4_workspace_size", "qfc_attention_selected_q4",
            "qfc_adapters_workspace_size", "qfc_add_adapters", "qfc_forward_batch", "qfc_destroy", "qfc_status_string"]
 
 
@@ -75,6 +77,16 @@ class Rotary(ctypes.Structure):
     """qfc_rotary_t; see make_rotary."""
     _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("base", ctypes.c_float), ("factor", ctypes.c_float),
                 ("original_positions", ctypes.c_int32), ("low_turns", ctypes.c_float), ("high_turns", ctypes.c_float), ("amplitude", ctypes.c_float)]
+
+
+class SharedDesc(ctypes.Structure):
+    """qfc_shared_t."""
+    _fields_ = [("group_start", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("groups", ctypes.c_int32), ("max_group_tokens", ctypes.c_int32), ("max_positions", ctypes.c_int32)]
+
+
+class BoundsDesc(ctypes.Structure):
+    """qfc_page_bounds_t."""
+    _fields_ = [("codes", ctypes.c_void_p), ("steps", ctypes.c_void_p)]
 
 
 class AdaptersDesc(ctypes.Structure):
@@ -144,6 +156,20 @@ def lib() -> ctypes.CDLL:
         L.qfc_read_q4.argtypes = [req, cache, vp, vp, vp]
         L.qfc_attention_q4_workspace_size.argtypes = [req, i32, cache, ctypes.POINTER(sz)]
         L.qfc_attention_q4.argtypes = [vp, req, i32, cache, vp, sz, vp, vp]
+        shared, bounds = ctypes.POINTER(SharedDesc), ctypes.POINTER(BoundsDesc)
+        L.qfc_pages_workspace_size.argtypes = [cache, i32, ctypes.POINTER(sz)]
+        L.qfc_copy_pages.argtypes = [cache, cache, vp, vp, i32, vp]
+        L.qfc_take_pages.argtypes = [cache, vp, vp, vp, i32, i32, vp, vp, sz, vp]
+        L.qfc_fork_pages.argtypes = [cache, vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]
+        L.qfc_free_pages.argtypes = [cache, vp, vp, vp, i32, i32, vp]
+        L.qfc_compact_pages.argtypes = [cache, vp, vp, i32, i32, vp, vp, sz, vp]
+        L.qfc_attention_shared_q4_workspace_size.argtypes = [req, shared, i32, cache, ctypes.POINTER(sz)]
+        L.qfc_attention_shared_q4.argtypes = [vp, req, shared, i32, cache, vp, sz, vp, vp]
+        L.qfc_bound_pages_q4.argtypes = [req, cache, bounds, vp]
+        L.qfc_select_pages_q4_workspace_size.argtypes = [req, i32, cache, ctypes.POINTER(sz)]
+        L.qfc_select_pages_q4.argtypes = [vp, req, i32, cache, bounds, i32, i32, i32, vp, sz, vp, vp]
+        L.qfc_attention_selected_q4_workspace_size.argtypes = [req, i32, cache, i32, ctypes.POINTER(sz)]
+        L.qfc_attention_selected_q4.argtypes = [vp, req, i32, cache, vp, i32, vp, sz, vp, vp]
         L.qfc_adapters_workspace_size.argtypes = [adapters, i32, ctypes.POINTER(sz)]
         L.qfc_add_adapters.argtypes = [vp, i32, vp, adapters, vp, vp, sz, vp, vp]
         L.qfc_forward_batch.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(vp), i32, ctypes.POINTER(vp), i32, vp]
@@ -562,6 +588,178 @@ def qfc_attention_q4(q: torch.Tensor, requests: Requests, h_q: int, cache: Paged
     _want(workspace, _u8, None, "workspace")
     _here(q.get_device(), out.get_device(), workspace.get_device(), cache.device, requests.device)
     _check(lib().qfc_attention_q4(q.data_ptr(), requests.ref, h_q, cache.ref, workspace.data_ptr(), workspace.numel(), out.data_ptr(), _stream()), "qfc_attention_q4")
+
+
+def _table(t: torch.Tensor, what: str):
+    """A matrix of page numbers: (rows, entries of a row)."""
+    if not (isinstance(t, _Tensor) and t.dim() == 2):
+        raise ValueError(f"{what}: a matrix is required")
+    batch, width = t.shape
+    _want(t, _i32, (batch, width), what)
+    return batch, width
+
+
+def _numbers(t: torch.Tensor | None, count: int, what: str, *devices):
+    """int32 [count] (or None, for an argument that may be left out) on the current device, like everything else of the call: its address."""
+    if t is not None:
+        _want(t, _i32, (count,), what)
+        devices += (t.get_device(),)
+    _here(*devices)
+    return t.data_ptr() if t is not None else None
+
+
+def qfc_pages_workspace_size(cache: PagedCache, batch: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().qfc_pages_workspace_size(cache.ref, batch, ctypes.byref(out)), "qfc_pages_workspace_size")
+    return out.value
+
+
+def qfc_copy_pages(source_cache: PagedCache, target_cache: PagedCache, source: torch.Tensor, target: torch.Tensor):
+    """Pages source[i] of one cache to pages target[i] of another (or the same)."""
+    if not (isinstance(source, _Tensor) and source.dim() == 1):
+        raise ValueError("source: a vector is required")
+    count = source.shape[0]
+    s = _numbers(source, count, "source", source_cache.device)
+    t = _numbers(target, count, "target", target_cache.device)
+    _check(lib().qfc_copy_pages(source_cache.ref, target_cache.ref, s, t, count, _stream()), "qfc_copy_pages")
+
+
+def qfc_take_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, positions: torch.Tensor, workspace: torch.Tensor, missing: torch.Tensor | None = None):
+    """Free pages for the first positions[b] positions of each row that lack one."""
+    batch, width = _table(page_table, "page_table")
+    _want(workspace, _u8, None, "workspace")
+    r = _numbers(references, cache.num_pages, "references", cache.device, page_table.get_device(), workspace.get_device())
+    p = _numbers(positions, batch, "positions")
+    m = _numbers(missing, 1, "missing")
+    _check(lib().qfc_take_pages(cache.ref, r, page_table.data_ptr(), p, batch, width, m, workspace.data_ptr(), workspace.numel(), _stream()), "qfc_take_pages")
+
+
+def qfc_fork_pages(cache: PagedCache, references: torch.Tensor, from_table: torch.Tensor, parents: torch.Tensor, positions: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor,
+                   missing: torch.Tensor | None = None):
+    """Row b of page_table continues the first positions[b] positions of row parents[b] of from_table: whole pages are shared, the one in part filled is copied."""
+    from_batch, from_width = _table(from_table, "from_table")
+    batch, width = _table(page_table, "page_table")
+    _want(workspace, _u8, None, "workspace")
+    r = _numbers(references, cache.num_pages, "references", cache.device, from_table.get_device(), page_table.get_device(), workspace.get_device())
+    f, p = _numbers(parents, batch, "parents"), _numbers(positions, batch, "positions")
+    m = _numbers(missing, 1, "missing")
+    _check(lib().qfc_fork_pages(cache.ref, r, from_table.data_ptr(), from_batch, from_width, f, p, page_table.data_ptr(), batch, width, m, workspace.data_ptr(), workspace.numel(), _stream()),
+           "qfc_fork_pages")
+
+
+def qfc_free_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, keep: torch.Tensor | None = None):
+    """Every row keeps the pages of its first keep[b] positions (None: of none) and lets the others go."""
+    batch, width = _table(page_table, "page_table")
+    r = _numbers(references, cache.num_pages, "references", cache.device, page_table.get_device())
+    k = _numbers(keep, batch, "keep")
+    _check(lib().qfc_free_pages(cache.ref, r, page_table.data_ptr(), k, batch, width, _stream()), "qfc_free_pages")
+
+
+def qfc_compact_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor, used: torch.Tensor | None = None):
+    """The pages in use get the numbers from 0 on; page_table holds all rows that name pages of the cache."""
+    batch, width = _table(page_table, "page_table")
+    _want(workspace, _u8, None, "workspace")
+    r = _numbers(references, cache.num_pages, "references", cache.device, page_table.get_device(), workspace.get_device())
+    u = _numbers(used, 1, "used")
+    _check(lib().qfc_compact_pages(cache.ref, r, page_table.data_ptr(), batch, width, u, workspace.data_ptr(), workspace.numel(), _stream()), "qfc_compact_pages")
+
+
+class SharedPrefixes:
+    """Groups of requests whose first positions are the same pages (qfc_shared_t): int32 tensors group_start [groups + 1], positions [groups], whose contents may change between
+    calls, and the sizes that may not: most new tokens of a group's requests together, most positions."""
+
+    def __init__(self, group_start: torch.Tensor, positions: torch.Tensor, max_group_tokens: int, max_positions: int):
+        _want(positions, _i32, None, "positions")
+        groups = positions.numel()
+        _want(positions, _i32, (groups,), "positions")
+        _want(group_start, _i32, (groups + 1,), "group_start")
+        self.group_start, self.positions, self.device = group_start, positions, positions.get_device()
+        if group_start.get_device() != self.device:
+            raise ValueError("group_start and positions: on different devices")
+        self.desc = SharedDesc(group_start.data_ptr(), positions.data_ptr(), groups, max_group_tokens, max_positions)
+        self.ref = ctypes.byref(self.desc)
+
+
+def qfc_attention_shared_q4_workspace_size(requests: Requests, shared: SharedPrefixes, h_q: int, cache: PagedCache) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().qfc_attention_shared_q4_workspace_size(requests.ref, shared.ref, h_q, cache.ref, ctypes.byref(out)), "qfc_attention_shared_q4_workspace_size")
+    return out.value
+
+
+def qfc_attention_shared_q4(q: torch.Tensor, requests: Requests, shared: SharedPrefixes, h_q: int, cache: PagedCache, workspace: torch.Tensor, out: torch.Tensor):
+    """qfc_attention_q4 with what groups of requests have in common read once for each group."""
+    shape = (requests.tokens, h_q * cache.d_head)
+    _want(q, _f16, shape, "q")
+    _want(out, _f16, shape, "out")
+    _want(workspace, _u8, None, "workspace")
+    _here(q.get_device(), out.get_device(), workspace.get_device(), cache.device, requests.device, shared.device)
+    _check(lib().qfc_attention_shared_q4(q.data_ptr(), requests.ref, shared.ref, h_q, cache.ref, workspace.data_ptr(), workspace.numel(), out.data_ptr(), _stream()),
+           "qfc_attention_shared_q4")
+
+
+class PageBounds:
+    """Bounds of the keys of a cache's pages (qfc_page_bounds_t): codes int8 [num_pages, h_kv, 2, d_head] (upper, lower), steps float32 [num_pages, h_kv]."""
+
+    def __init__(self, cache: PagedCache):
+        self.codes = torch.zeros((cache.num_pages, cache.h_kv, 2, cache.d_head), dtype=_i8, device=cache.pages.device)
+        self.steps = torch.zeros((cache.num_pages, cache.h_kv), dtype=_f32, device=cache.pages.device)
+        self.shape, self.device = (cache.num_pages, cache.h_kv, cache.d_head), cache.device
+        self.desc = BoundsDesc(self.codes.data_ptr(), self.steps.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+    def _of(self, cache: PagedCache):
+        if self.shape != (cache.num_pages, cache.h_kv, cache.d_head):
+            raise ValueError(f"bounds: of a cache of {self.shape} pages, heads and values, not {(cache.num_pages, cache.h_kv, cache.d_head)}")
+
+
+def qfc_bound_pages_q4(requests: Requests, cache: PagedCache, bounds: PageBounds):
+    """Bounds of the pages that the requests' new tokens are in."""
+    bounds._of(cache)
+    _here(cache.device, requests.device, bounds.device)
+    _check(lib().qfc_bound_pages_q4(requests.ref, cache.ref, bounds.ref, _stream()), "qfc_bound_pages_q4")
+
+
+def qfc_select_pages_q4_workspace_size(requests: Requests, h_q: int, cache: PagedCache) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().qfc_select_pages_q4_workspace_size(requests.ref, h_q, cache.ref, ctypes.byref(out)), "qfc_select_pages_q4_workspace_size")
+    return out.value
+
+
+def _selected(selected: torch.Tensor, requests: Requests, cache: PagedCache) -> int:
+    if not (isinstance(selected, _Tensor) and selected.dim() == 3):
+        raise ValueError("selected: three dimensions are required")
+    count = selected.shape[2]
+    _want(selected, _i32, (requests.tokens, cache.h_kv, count), "selected")
+    return count
+
+
+def qfc_select_pages_q4(q: torch.Tensor, requests: Requests, h_q: int, cache: PagedCache, bounds: PageBounds, first: int, last: int, selected: torch.Tensor, workspace: torch.Tensor):
+    """selected[t, kv] = numbers of the pages worth reading for token t and KV head kv, ascending: the first, the last, and the best of the others."""
+    bounds._of(cache)
+    _want(q, _f16, (requests.tokens, h_q * cache.d_head), "q")
+    _want(workspace, _u8, None, "workspace")
+    count = _selected(selected, requests, cache)
+    _here(q.get_device(), workspace.get_device(), selected.get_device(), cache.device, requests.device, bounds.device)
+    _check(lib().qfc_select_pages_q4(q.data_ptr(), requests.ref, h_q, cache.ref, bounds.ref, first, last, count, workspace.data_ptr(), workspace.numel(), selected.data_ptr(), _stream()),
+           "qfc_select_pages_q4")
+
+
+def qfc_attention_selected_q4_workspace_size(requests: Requests, h_q: int, cache: PagedCache, count: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().qfc_attention_selected_q4_workspace_size(requests.ref, h_q, cache.ref, count, ctypes.byref(out)), "qfc_attention_selected_q4_workspace_size")
+    return out.value
+
+
+def qfc_attention_selected_q4(q: torch.Tensor, requests: Requests, h_q: int, cache: PagedCache, selected: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor):
+    """Attention of each token and KV head over the pages that `selected` lists."""
+    shape = (requests.tokens, h_q * cache.d_head)
+    _want(q, _f16, shape, "q")
+    _want(out, _f16, shape, "out")
+    _want(workspace, _u8, None, "workspace")
+    count = _selected(selected, requests, cache)
+    _here(q.get_device(), out.get_device(), workspace.get_device(), selected.get_device(), cache.device, requests.device)
+    _check(lib().qfc_attention_selected_q4(q.data_ptr(), requests.ref, h_q, cache.ref, selected.data_ptr(), count, workspace.data_ptr(), workspace.numel(), out.data_ptr(), _stream()),
+           "qfc_attention_selected_q4")
 
 
 class Adapters:

@@ -528,6 +528,183 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
                                           static_cast<hipStream_t>(stream)));
 }
 
+// ---- pages that requests share
+static qfc_status_t check_pool(const qfc_q4_cache_t *c, const int32_t *references, const int32_t *table, int32_t batch, int32_t width) {
+    if (const qfc_status_t s = check_q4_cache(c); s != QFC_OK) return s;
+    if (!references || !table || batch < 1 || width < 1) return QFC_ERR_INVALID_ARG;
+    if (batch > 1 << 22 || (long)c->h_kv * 80 * c->d_head > INT32_MAX) return QFC_ERR_UNSUPPORTED;
+    if (!aligned(references, 4) || !aligned(table, 4)) return QFC_ERR_ALIGNMENT;
+    return QFC_OK;
+}
+
+// Behind check_pool: the cache's pages, the workspace and `missing` (or `used`)
+static qfc_status_t check_pool_work(const qfc_q4_cache_t *c, int32_t batch, const int32_t *number, const void *workspace, size_t workspace_bytes) {
+    if (!c->pages || !workspace) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(c->pages) || !aligned16(workspace) || !aligned(number, 4)) return QFC_ERR_ALIGNMENT;
+    return workspace_bytes < pages_workspace(c->num_pages, batch) ? QFC_ERR_BUFFER_TOO_SMALL : QFC_OK;
+}
+
+static PagePool pool_of(const qfc_q4_cache_t *c, int32_t *references) { return PagePool{c->pages, references, c->num_pages, c->h_kv * 80 * c->d_head}; }
+
+qfc_status_t qfc_pages_workspace_size(const qfc_q4_cache_t *cache, int32_t batch, size_t *bytes) {
+    if (!bytes) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_q4_cache(cache); s != QFC_OK) return s;
+    if (batch < 1) return QFC_ERR_INVALID_ARG;
+    if (batch > 1 << 22) return QFC_ERR_UNSUPPORTED;
+    *bytes = pages_workspace(cache->num_pages, batch);
+    return QFC_OK;
+}
+
+qfc_status_t qfc_copy_pages(const qfc_q4_cache_t *from, const qfc_q4_cache_t *to, const int32_t *source, const int32_t *target, int32_t count, void *stream) {
+    if (const qfc_status_t s = check_q4_cache(from); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_q4_cache(to); s != QFC_OK) return s;
+    if (from->h_kv != to->h_kv || from->d_head != to->d_head || count < 0) return QFC_ERR_INVALID_ARG;
+    if ((long)from->h_kv * 80 * from->d_head > INT32_MAX) return QFC_ERR_UNSUPPORTED;
+    if (count == 0) return QFC_OK;
+    if (!from->pages || !to->pages || !source || !target) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(from->pages) || !aligned16(to->pages) || !aligned(source, 4) || !aligned(target, 4)) return QFC_ERR_ALIGNMENT;
+    const int cus = device_cus();
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_copy_pages(from->pages, from->num_pages, to->pages, to->num_pages, from->h_kv * 80 * from->d_head, source, target, count, cus, static_cast<hipStream_t>(stream)));
+}
+
+qfc_status_t qfc_take_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, const int32_t *positions, int32_t batch, int32_t table_width, int32_t *missing,
+                            void *workspace, size_t workspace_bytes, void *stream) {
+    if (const qfc_status_t s = check_pool(cache, references, page_table, batch, table_width); s != QFC_OK) return s;
+    if (!positions) return QFC_ERR_INVALID_ARG;
+    if (!aligned(positions, 4)) return QFC_ERR_ALIGNMENT;
+    if (const qfc_status_t s = check_pool_work(cache, batch, missing, workspace, workspace_bytes); s != QFC_OK) return s;
+    return hip_status(launch_take_pages(pool_of(cache, references), page_table, positions, batch, table_width, missing, workspace, static_cast<hipStream_t>(stream)));
+}
+
+qfc_status_t qfc_fork_pages(const qfc_q4_cache_t *cache, int32_t *references, const int32_t *from, int32_t from_batch, int32_t from_width, const int32_t *parents, const int32_t *positions,
+                            int32_t *page_table, int32_t batch, int32_t table_width, int32_t *missing, void *workspace, size_t workspace_bytes, void *stream) {
+    if (const qfc_status_t s = check_pool(cache, references, page_table, batch, table_width); s != QFC_OK) return s;
+    if (!from || !parents || !positions || from_batch < 1 || from_width < 1) return QFC_ERR_INVALID_ARG;
+    if (!aligned(from, 4) || !aligned(parents, 4) || !aligned(positions, 4)) return QFC_ERR_ALIGNMENT;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(from), b = reinterpret_cast<uintptr_t>(page_table);
+    if (a < b + (size_t)batch * table_width * 4 && b < a + (size_t)from_batch * from_width * 4) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_pool_work(cache, batch, missing, workspace, workspace_bytes); s != QFC_OK) return s;
+    const int cus = device_cus();
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_fork_pages(pool_of(cache, references), from, from_batch, from_width, parents, positions, page_table, batch, table_width, missing, workspace, cus,
+                                        static_cast<hipStream_t>(stream)));
+}
+
+qfc_status_t qfc_free_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, const int32_t *keep, int32_t batch, int32_t table_width, void *stream) {
+    if (const qfc_status_t s = check_pool(cache, references, page_table, batch, table_width); s != QFC_OK) return s;
+    if (!aligned(keep, 4)) return QFC_ERR_ALIGNMENT;
+    const int cus = device_cus();
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_free_pages(references, cache->num_pages, page_table, keep, batch, table_width, cus, static_cast<hipStream_t>(stream)));
+}
+
+qfc_status_t qfc_compact_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, int32_t batch, int32_t table_width, int32_t *used, void *workspace,
+                               size_t workspace_bytes, void *stream) {
+    if (const qfc_status_t s = check_pool(cache, references, page_table, batch, table_width); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_pool_work(cache, batch, used, workspace, workspace_bytes); s != QFC_OK) return s;
+    const int cus = device_cus();
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_compact_pages(pool_of(cache, references), page_table, batch, table_width, used, workspace, cus, static_cast<hipStream_t>(stream)));
+}
+
+// ---- attention behind common pages, and over selected ones
+static qfc_status_t check_shared(const qfc_shared_t *s) {
+    return s && s->groups >= 1 && s->max_group_tokens >= 1 && s->max_positions >= 1 ? QFC_OK : QFC_ERR_INVALID_ARG;
+}
+
+static AttnPartsPlan shared_plan(const qfc_requests_t *r, const qfc_shared_t *s, int32_t h_q, const qfc_q4_cache_t *c, int cus) {
+    return plan_attention_shared_q4(r->batch, r->tokens, h_q, c->h_kv, c->d_head, r->max_tokens, r->max_context, s->groups, s->max_group_tokens, s->max_positions, cus);
+}
+
+qfc_status_t qfc_attention_shared_q4_workspace_size(const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes) {
+    if (!bytes) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_batch(requests, h_q, cache); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_shared(shared); s != QFC_OK) return s;
+    *bytes = shared_plan(requests, shared, h_q, cache, device_cus()).bytes;
+    return QFC_OK;
+}
+
+qfc_status_t qfc_attention_shared_q4(const void *q_f16, const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, void *workspace,
+                                     size_t workspace_bytes, void *out_f16, void *stream) {
+    if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_shared(shared); s != QFC_OK) return s;
+    if (!shared->group_start || !shared->positions) return QFC_ERR_INVALID_ARG;
+    if (!aligned(shared->group_start, 4) || !aligned(shared->positions, 4)) return QFC_ERR_ALIGNMENT;
+    if (requests->tokens == 0) return QFC_OK;
+    if (!q_f16 || !workspace || !out_f16) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(q_f16) || !aligned16(workspace) || !aligned16(out_f16)) return QFC_ERR_ALIGNMENT;
+    const int cus = device_cus();
+    const AttnPartsPlan p = shared_plan(requests, shared, h_q, cache, cus);
+    if (workspace_bytes < p.bytes) return QFC_ERR_BUFFER_TOO_SMALL;
+    if (p.prefix_blocks > INT32_MAX || p.blocks > INT32_MAX) return QFC_ERR_UNSUPPORTED;
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_attention_shared_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, shared->group_start, shared->positions, shared->groups,
+                                                 shared->max_group_tokens, shared->max_positions, p, workspace, out_f16, cus, static_cast<hipStream_t>(stream)));
+}
+
+static qfc_status_t check_bounds(const qfc_page_bounds_t *b) {
+    if (!b || !b->codes || !b->steps) return QFC_ERR_INVALID_ARG;
+    return aligned16(b->codes) && aligned(b->steps, 4) ? QFC_OK : QFC_ERR_ALIGNMENT;
+}
+
+qfc_status_t qfc_bound_pages_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, const qfc_page_bounds_t *bounds, void *stream) {
+    if (const qfc_status_t s = check_requests(requests, cache ? cache->h_kv : 0, cache); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_bounds(bounds); s != QFC_OK) return s;
+    if (requests->tokens == 0) return QFC_OK;
+    return hip_status(launch_bound_pages_q4(on_device(requests, cache), cache->h_kv, cache->d_head, cache->pages, bounds->codes, bounds->steps, static_cast<hipStream_t>(stream)));
+}
+
+constexpr int kMostSelected = 1 << 16;
+
+qfc_status_t qfc_select_pages_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes) {
+    if (!bytes) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_batch(requests, h_q, cache); s != QFC_OK) return s;
+    *bytes = select_workspace(requests->tokens, cache->h_kv, requests->max_context, device_cus());
+    return QFC_OK;
+}
+
+qfc_status_t qfc_select_pages_q4(const void *q_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, const qfc_page_bounds_t *bounds, int32_t first, int32_t last,
+                                 int32_t count, void *workspace, size_t workspace_bytes, int32_t *selected, void *stream) {
+    if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_bounds(bounds); s != QFC_OK) return s;
+    if (first < 0 || last < 0 || count < 1 || (long)first + last > count) return QFC_ERR_INVALID_ARG;
+    if (count > kMostSelected) return QFC_ERR_UNSUPPORTED;
+    if (requests->tokens == 0) return QFC_OK;
+    if (!q_f16 || !workspace || !selected) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(q_f16) || !aligned16(workspace) || !aligned(selected, 4)) return QFC_ERR_ALIGNMENT;
+    const int cus = device_cus();
+    if (workspace_bytes < select_workspace(requests->tokens, cache->h_kv, requests->max_context, cus)) return QFC_ERR_BUFFER_TOO_SMALL;
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_select_pages_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, bounds->codes, bounds->steps, first, last, count, workspace, selected, cus,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+qfc_status_t qfc_attention_selected_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, int32_t count, size_t *bytes) {
+    if (!bytes) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_batch(requests, h_q, cache); s != QFC_OK) return s;
+    if (count < 1) return QFC_ERR_INVALID_ARG;
+    if (count > kMostSelected) return QFC_ERR_UNSUPPORTED;
+    *bytes = plan_attention_selected_q4(requests->tokens, h_q, cache->h_kv, cache->d_head, count, device_cus()).bytes;
+    return QFC_OK;
+}
+
+qfc_status_t qfc_attention_selected_q4(const void *q_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, const int32_t *selected, int32_t count,
+                                       void *workspace, size_t workspace_bytes, void *out_f16, void *stream) {
+    if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
+    if (count < 1) return QFC_ERR_INVALID_ARG;
+    if (count > kMostSelected) return QFC_ERR_UNSUPPORTED;
+    if (requests->tokens == 0) return QFC_OK;
+    if (!q_f16 || !workspace || !out_f16 || !selected) return QFC_ERR_INVALID_ARG;
+    if (!aligned16(q_f16) || !aligned16(workspace) || !aligned16(out_f16) || !aligned(selected, 4)) return QFC_ERR_ALIGNMENT;
+    const int cus = device_cus();
+    const AttnPartsPlan p = plan_attention_selected_q4(requests->tokens, h_q, cache->h_kv, cache->d_head, count, cus);
+    if (workspace_bytes < p.bytes) return QFC_ERR_BUFFER_TOO_SMALL;
+    if (cus < 1) return QFC_ERR_HIP;
+    return hip_status(launch_attention_selected_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, selected, count, p, workspace, out_f16, cus,
+                                                   static_cast<hipStream_t>(stream)));
+}
+
 static qfc_status_t check_adapters(const qfc_adapters_t *a, int32_t M) {
     if (!a || M < 1 || a->count < 1 || a->K < 32 || a->K % 32 != 0 || a->N < 1 || a->rank < 1) return QFC_ERR_INVALID_ARG;
     // (M / 64 blocks of rows times N / 2048 pieces of columns are one dimension of a launch)

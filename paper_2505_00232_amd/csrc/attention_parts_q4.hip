@@ -1,0 +1,331 @@
+// Attention over the paged 4-bit cache in parts that are joined afterwards: of requests whose first positions are the same pages, and over selected pages.
+//
+// A part is a run of pages and 16 query rows of a KV head; it leaves unnormalized outputs o, a maximum m and a sum l, and
+//   out = sum_i e^(m_i - m) o_i / sum_i e^(m_i - m) l_i,   m = max_i m_i.
+// The rows of a group of requests meet their common pages as rows of one request do, whatever request they are of: what the pages cost is shared by 16 rows.  What a wavefront does with a
+// page, and in which precision: attention_q4_rows.h.
+#include "attention_q4_rows.h"
+
+namespace qfc {
+namespace {
+
+struct PartsArgs {
+    const _Float16 *q;  // [tokens, h_q, D]
+    _Float16 *out;
+    const char *pages;
+    Requests req;
+    const int *selected;  // [tokens, h_kv, count], or null
+    int count;
+    const int *group_start, *prefix;  // of groups with common pages
+    int groups, group_tokens, longest;
+    float *ws_o, *ws_ml;  // [slots][tokens * h_q][D] partial outputs, [..][2] (maximum, sum; 0: nothing was seen, no output)
+    int h_q, h_kv, g, head_blocks;
+    int prefix_parts, parts;  // slots: of common pages, and behind them of the others
+    long prefix_items, items;  // of workgroups; items: all of them
+    float scale;
+};
+
+// x among runs of len(i) places, i = 0, 1, .. count - 1: which run, and the place in it (-1: behind the last).  A lane looks at one run at a time.
+struct Found {
+    int run, place;
+};
+template <class Len>
+__device__ __forceinline__ Found find(int x, int count, int lane, const Len &len) {
+    for (int c = 0; c < count; c += 64) {
+        const int mine = c + lane < count ? len(c + lane) : 0, upto = sum_upto(mine);
+        const uint64_t past = __ballot(upto > x);
+        if (past) {
+            const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+            const int len_of = __builtin_amdgcn_readlane(mine, l), place = x - (__builtin_amdgcn_readlane(upto, l) - len_of);
+            return place < len_of ? Found{c + l, place} : Found{-1, 0};  // (sums that ended at the largest int)
+        }
+        x -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return Found{-1, 0};
+}
+
+// Requests of group i, their rows, and the pages in front of all their new tokens that they have in common
+struct Group {
+    int lead, pages;  // the first one with tokens: its table's row is read
+};
+__device__ __forceinline__ int group_end(const PartsArgs &a, int i) { return min(max(a.group_start[i], 0), a.req.batch); }
+__device__ __forceinline__ int token_at(const PartsArgs &a, int b) { return min(max(a.req.start[b], 0), a.req.tokens); }
+__device__ __forceinline__ int tokens_of_group(const PartsArgs &a, int i) {
+    return min(max(token_at(a, group_end(a, i + 1)) - token_at(a, group_end(a, i)), 0), a.group_tokens);
+}
+__device__ __forceinline__ Group group_of(const PartsArgs &a, int i, int lane) {
+    const int first = group_end(a, i), end = group_end(a, i + 1);
+    int least = min(max(a.prefix[i], 0), a.longest), lead = -1;
+    for (int b0 = first; b0 < end; b0 += 64) {
+        const int b = b0 + lane;
+        const Span s = b < end ? span_of(a.req, b) : Span{0, 0, 0};
+        const uint64_t some = __ballot(s.count > 0);
+        if (lead < 0 && some) lead = b0 + __ffsll((unsigned long long)some) - 1;
+        if (s.count > 0) least = min(least, max(s.positions - s.count, 0));
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) least = min(least, __shfl_xor(least, off, 64));
+    return Group{__builtin_amdgcn_readfirstlane(max(lead, 0)), __builtin_amdgcn_readfirstlane(lead < 0 ? 0 : least / kPage)};
+}
+
+// A workgroup per part: its four wavefronts have a quarter of the pages each and meet in LDS.
+template <int D, bool SELECTED>
+__global__ __launch_bounds__(256, kWgs) void attn_q4_parts_kernel(PartsArgs a) {
+    constexpr int STRIDE = D + 4;  // of a row of partial outputs in LDS (banks)
+    static_assert(16 * STRIDE * 4 <= 2 * Place<D>::PART, "a wavefront's partial outputs take its pages' places");
+    extern __shared__ float lds[];
+    __shared__ float sums[4][16][2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long all_rows = (long)a.req.tokens * a.h_q;
+    const bool direct = a.prefix_parts + a.parts == 1;
+    Rows<D> rows(lds, wave, lane);
+    const int m = rows.m, r = rows.r;
+    for (long item = blockIdx.x; item < a.items; item += gridDim.x) {
+        // ---- which rows, which pages: from .. to - 1 of request b (of its list, where SELECTED)
+        int b, slot, token = 0, head = 0, lim, n, from, to;
+        bool real;
+        const int *list = nullptr;
+        const bool common = !SELECTED && item < a.prefix_items;
+        const long x = SELECTED || common ? item : item - a.prefix_items;
+        const int parts = common ? a.prefix_parts : a.parts, kv = (int)(x % a.h_kv), part = (int)(x / a.h_kv % parts);
+        const long block = x / a.h_kv / parts;
+        if constexpr (SELECTED) {
+            const int heads0 = (int)(block % a.head_blocks) * 16;
+            token = (int)(block / a.head_blocks);
+            b = __builtin_amdgcn_readfirstlane(request_of<1>(a.req, token, 0, lane));
+            if (b >= a.req.batch) return;  // (so are all later tokens)
+            const Span s = span_of(a.req, b);
+            if (token < s.first || token - s.first >= s.count) continue;
+            n = s.positions, lim = n - s.count + token - s.first + 1;
+            real = heads0 + m < a.g, head = kv * a.g + min(heads0 + m, a.g - 1);
+            const int per = (a.count + parts - 1) / parts;
+            from = min(part * per, a.count), to = min(from + per, a.count), slot = part;
+            list = a.selected + ((size_t)token * a.h_kv + kv) * a.count;
+        } else {
+            int first, row, rows_all, pages;
+            if (common) {
+                const Found f = find((int)block, a.groups, lane, [&](int i) __attribute__((always_inline)) { return (int)(((long)tokens_of_group(a, i) * a.g + 15) / 16); });
+                if (f.run < 0) {  // (on to the items behind the groups')
+                    item += (a.prefix_items - 1 - item) / gridDim.x * gridDim.x;
+                    continue;
+                }
+                const Group group = group_of(a, f.run, lane);
+                b = group.lead, pages = group.pages;
+                first = token_at(a, group_end(a, f.run)), rows_all = tokens_of_group(a, f.run) * a.g, row = f.place * 16 + m;
+                n = pages * kPage, lim = n, from = 0;
+            } else {
+                Found f = {(int)block, 0};
+                if (a.req.max_tokens * a.g > 16)
+                    f = find((int)block, a.req.batch, lane, [&](int i) __attribute__((always_inline)) { return (span_of(a.req, i).count * a.g + 15) / 16; });
+                if (f.run < 0 || f.run >= a.req.batch) return;
+                b = f.run;
+                const Span s = span_of(a.req, b);
+                first = s.first, rows_all = s.count * a.g, row = f.place * 16 + m;
+                n = s.positions, lim = n - s.count + row / a.g + 1;
+                // its group, and the pages that are done with that
+                int before = 0;
+                for (int c = 0; c <= a.groups; c += 64) before += __popcll(__ballot(c + lane <= a.groups && group_end(a, min(c + lane, a.groups)) <= b));
+                from = before > 0 && before <= a.groups ? group_of(a, before - 1, lane).pages : 0;
+                // (the last row's positions are the most)
+                const int sees = max(0, n - s.count + min(f.place * 16 + 15, rows_all - 1) / a.g + 1);
+                pages = (sees + kPage - 1) / kPage;
+            }
+            if (rows_all <= 0) continue;
+            real = row < rows_all, row = min(row, rows_all - 1);
+            token = first + row / a.g, head = kv * a.g + row % a.g;
+            const int per = max(4, (max(pages - from, 0) + parts - 1) / parts);
+            from = min(from + part * per, max(pages, from)), to = min(from + per, max(pages, from)), slot = part + (common ? 0 : a.prefix_parts);
+        }
+        const size_t at = (size_t)token * a.h_q + head, out_row = (size_t)slot * all_rows + at;
+        if (from >= to && !direct) {
+            if (wave == 0 && r == 0 && real) a.ws_ml[out_row * 2 + 1] = 0.0f;
+            continue;
+        }
+        // ---- this wavefront's quarter
+        const int share = (to - from + 3) / 4, begin = min(from + wave * share, to), count = __builtin_amdgcn_readfirstlane(min(begin + share, to) - begin);
+        int place = -1;  // of the page in its request, a page per lane
+        auto numbers = [&](int i) __attribute__((always_inline)) {
+            if constexpr (SELECTED) {
+                place = i + lane < count ? list[begin + i + lane] : -1;
+                return place >= 0 && place < (a.req.max_context + kPage - 1) / kPage ? page_of(a.req, b, place * kPage) : -1;
+            } else {
+                return i + lane < count ? page_of(a.req, b, (begin + i + lane) * kPage) : -1;
+            }
+        };
+        auto start_of = [&](int i) __attribute__((always_inline)) {
+            if constexpr (SELECTED) return __builtin_amdgcn_readlane(place, i & 63) * kPage;
+            return (begin + i) * kPage;
+        };
+        const int ahead = numbers(0);
+        rows.load(a.q + at * D, real, a.scale);
+        rows.walk(count, real ? lim : 0, n, a.pages, a.h_kv, kv, ahead, numbers, start_of);
+        // ---- the four meet
+        float *const mine = lds + wave * (2 * Place<D>::PART / 4) + m * STRIDE;
+        rows.columns([&](int d, const v4f &o) __attribute__((always_inline)) { *reinterpret_cast<v4f *>(mine + d) = o; });
+        const float own_sum = rows.sum();
+        if (r == 0) sums[wave][m][0] = rows.run_max, sums[wave][m][1] = own_sum;
+        __syncthreads();
+        // thread: row threadIdx.x / 16, columns 4 (threadIdx.x % 16) and every 64th behind them.  (What a lane knows of row m the lanes of row threadIdx.x / 16 ask for.)
+        const int tr = threadIdx.x >> 4, from_lane = tr;
+        const size_t their_at = __shfl((unsigned long long)at, from_lane, 64);
+        const bool their_real = __shfl((int)real, from_lane, 64) != 0;
+        if (their_real) {
+            float f[4], top = sums[0][tr][0], l = 0.0f;
+#pragma unroll
+            for (int w = 1; w < 4; ++w) top = fmaxf(top, sums[w][tr][0]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                f[w] = __builtin_amdgcn_exp2f(sums[w][tr][0] - top);
+                l = fmaf(f[w], sums[w][tr][1], l);
+            }
+            const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+            const size_t to_row = (size_t)slot * all_rows + their_at;
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+                const int d = 64 * c + 4 * (threadIdx.x & 15);
+                v4f o = {};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const v4f x4 = *reinterpret_cast<const v4f *>(lds + w * (2 * Place<D>::PART / 4) + tr * STRIDE + d);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = fmaf(f[w], x4[i], o[i]);
+                }
+                if (direct)
+                    *reinterpret_cast<h4 *>(a.out + their_at * D + d) = h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
+                else
+                    *reinterpret_cast<v4f *>(a.ws_o + to_row * D + d) = o;
+            }
+            if (!direct && (threadIdx.x & 15) == 0) a.ws_ml[to_row * 2] = top, a.ws_ml[to_row * 2 + 1] = l;
+        }
+        __syncthreads();
+    }
+}
+
+// D / 4 threads per row: its parts, eight on their way at a time.  Rows of nobody stay as they are.
+template <int D>
+__global__ __launch_bounds__(256) void attn_q4_join_kernel(PartsArgs a) {
+    const long all_rows = (long)a.req.tokens * a.h_q, step = (long)gridDim.x * (1024 / D);
+    const int d = 4 * (threadIdx.x % (D / 4)), last = token_at(a, a.req.batch), slots = a.prefix_parts + a.parts;
+    int group0 = 0, group1 = 0;  // tokens of groups
+    if (a.prefix_parts) group0 = token_at(a, group_end(a, 0)), group1 = token_at(a, group_end(a, a.groups));
+    for (long row = (long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4); row < all_rows; row += step) {
+        const int token = (int)(row / a.h_q);
+        if (token >= last) return;
+        const int first = token >= group0 && token < group1 ? 0 : a.prefix_parts;
+        float top = kNothingYet, l = 0.0f;
+        v4f o = {};
+        for (int s0 = first; s0 < slots; s0 += 8) {
+            float ms[8], ls[8];
+            v4f os[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const size_t at = (size_t)min(s0 + i, slots - 1) * all_rows + row;
+                ms[i] = a.ws_ml[at * 2], ls[i] = a.ws_ml[at * 2 + 1];
+                os[i] = *reinterpret_cast<const v4f *>(a.ws_o + at * D + d);
+            }
+            float new_top = top;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (s0 + i >= slots) ls[i] = 0.0f;
+                new_top = ls[i] != 0.0f ? fmaxf(new_top, ms[i]) : new_top;
+            }
+            const float corr = __builtin_amdgcn_exp2f(top - new_top);
+            top = new_top, l *= corr;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] *= corr;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (ls[i] == 0.0f) continue;  // (nothing was seen: what stands there is not defined)
+                const float f = __builtin_amdgcn_exp2f(ms[i] - top);
+                l = fmaf(f, ls[i], l);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, os[i][e], o[e]);
+            }
+        }
+        const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+        *reinterpret_cast<h4 *>(a.out + row * D + d) = h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
+    }
+}
+
+template <int D, bool SELECTED>
+hipError_t launch(const PartsArgs &a, int num_cus, hipStream_t st) {
+    constexpr size_t lds = Place<D>::LDS;
+    if (const hipError_t e = allow_dynamic_lds<attn_q4_parts_kernel<D, SELECTED>>(lds); e != hipSuccess) return e;
+    const long most = 1L << 22;  // (a launch has fewer than 2^32 threads)
+    attn_q4_parts_kernel<D, SELECTED><<<(unsigned)(a.items < most ? a.items : most), 256, lds, st>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || a.prefix_parts + a.parts == 1) return e;
+    const long joins = ((long)a.req.tokens * a.h_q + 1024 / D - 1) / (1024 / D);
+    attn_q4_join_kernel<D><<<(unsigned)(joins < most ? joins : most), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <bool SELECTED>
+hipError_t launch(const PartsArgs &a, int d, int num_cus, hipStream_t st) {
+    switch (d) {
+        case 64: return launch<64, SELECTED>(a, num_cus, st);
+        case 128: return launch<128, SELECTED>(a, num_cus, st);
+        case 256: return launch<256, SELECTED>(a, num_cus, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+PartsArgs args_of(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnPartsPlan &p, void *workspace, void *out) {
+    PartsArgs a = {};
+    a.q = static_cast<const _Float16 *>(q);
+    a.out = static_cast<_Float16 *>(out);
+    a.pages = static_cast<const char *>(pages);
+    a.req = req;
+    a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv, a.head_blocks = (a.g + 15) / 16;
+    a.prefix_parts = p.prefix_parts, a.parts = p.parts;
+    a.prefix_items = p.prefix_blocks * h_kv * p.prefix_parts;
+    a.items = a.prefix_items + p.blocks * h_kv * p.parts;
+    a.ws_o = static_cast<float *>(workspace);
+    a.ws_ml = a.ws_o + (size_t)(p.prefix_parts + p.parts) * req.tokens * h_q * d;
+    a.scale = 1.4426950408889634f / sqrtf((float)d);
+    return a;
+}
+
+constexpr int kMostParts = 16;
+// Workgroups that share a block's pages: as many as fill the card, each with a page per wavefront at least
+int parts_of(long blocks, int pages, int num_cus) {
+    const long fill = ((long)kWgs * num_cus + blocks - 1) / (blocks > 0 ? blocks : 1), most = (pages + 3) / 4;
+    const long parts = fill < most ? fill : most;
+    return (int)(parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts);
+}
+
+}  // namespace
+
+AttnPartsPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, int count, int num_cus) {
+    AttnPartsPlan p = {};
+    p.blocks = (long)tokens * ((h_q / h_kv + 15) / 16);
+    p.parts = parts_of(p.blocks * h_kv, count, num_cus);
+    p.bytes = 256 + (p.parts > 1 ? (size_t)p.parts * tokens * h_q * (d + 2) * sizeof(float) : 0);
+    return p;
+}
+
+AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv, int d, int max_tokens, int max_context, int groups, int group_tokens, int longest, int num_cus) {
+    AttnPartsPlan p = {};
+    const int g = h_q / h_kv;
+    const long by_group = (long)groups * (((long)group_tokens * g + 15) / 16), by_token = ((long)tokens * g + 15) / 16 + groups;
+    p.prefix_blocks = by_group < by_token ? by_group : by_token;
+    p.blocks = max_tokens * g <= 16 ? batch : ((long)tokens * g + 15) / 16 + batch;
+    p.prefix_parts = parts_of(p.prefix_blocks * h_kv, (longest < max_context ? longest : max_context) / kPage, num_cus);
+    p.parts = parts_of(p.blocks * h_kv, (max_context + kPage - 1) / kPage, num_cus);
+    p.bytes = 256 + (size_t)(p.prefix_parts + p.parts) * tokens * h_q * (d + 2) * sizeof(float);
+    return p;
+}
+
+hipError_t launch_attention_selected_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *selected, int count, const AttnPartsPlan &p, void *workspace,
+                                        void *out, int num_cus, hipStream_t st) {
+    PartsArgs a = args_of(q, req, h_q, h_kv, d, pages, p, workspace, out);
+    a.selected = selected, a.count = count;
+    return launch<true>(a, d, num_cus, st);
+}
+
+hipError_t launch_attention_shared_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *group_start, const int *prefix, int groups, int group_tokens,
+                                      int longest, const AttnPartsPlan &p, void *workspace, void *out, int num_cus, hipStream_t st) {
+    PartsArgs a = args_of(q, req, h_q, h_kv, d, pages, p, workspace, out);
+    a.group_start = group_start, a.prefix = prefix, a.groups = groups, a.group_tokens = group_tokens, a.longest = longest;
+    return launch<false>(a, d, num_cus, st);
+}
+
+}  // namespace qfc

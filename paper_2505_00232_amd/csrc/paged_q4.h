@@ -63,5 +63,26 @@ __device__ __forceinline__ int page_of(const Requests &q, int b, int p) {
     const int page = q.table[(size_t)b * q.width + p / kPage];
     return page >= 0 && page < q.num_pages ? page : -1;
 }
+// Requests of the tokens of a wavefront, PER of them from `first` on: how many requests end at or before a token.  A lane looks at one request at a time.
+template <int PER>
+__device__ __forceinline__ int request_of(const Requests &q, int first, int mine, int lane) {
+    int count[PER] = {};
+    for (int b0 = 0; b0 < q.batch; b0 += 64) {
+        const int end = b0 + lane < q.batch ? q.start[b0 + lane + 1] : INT32_MAX;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) count[i] += __popcll(__ballot(end <= first + i));
+    }
+    int b = count[0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) b = mine == i ? count[i] : b;
+    return b;
+}
+
+// Pages and how often tables name them, on the device
+struct PagePool {
+    void *pages;
+    int *references;
+    int num_pages, page_bytes;
+};
 
 }  // namespace qfc

@@ -14,21 +14,6 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ uint16_t bits16(_Float16 x) { return __builtin_bit_cast(uint16_t, x); }
 
-// Requests of the tokens of a wavefront, PER of them from `first` on: how many requests end at or before a token.  A lane looks at one request at a time.
-template <int PER>
-__device__ __forceinline__ int request_of(const Requests &q, int first, int mine, int lane) {
-    int count[PER] = {};
-    for (int b0 = 0; b0 < q.batch; b0 += 64) {
-        const int end = b0 + lane < q.batch ? q.start[b0 + lane + 1] : INT32_MAX;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) count[i] += __popcll(__ballot(end <= first + i));
-    }
-    int b = count[0];
-#pragma unroll
-    for (int i = 1; i < PER; ++i) b = mine == i ? count[i] : b;
-    return b;
-}
-
 // Tiles of tokens are dealt four by four to the XCDs (workgroup i runs on XCD i % 8): a page's lines, of which each tile has a part, then meet in one L2 (4096 tokens appended and read
 // 38.6 us, dealt one by one 39.5).
 constexpr int kTiles = 4;

@@ -404,6 +404,33 @@ AttnQ4Plan plan_attention_q4(int batch, int tokens, int h_kv, int g, int d, int 
 long most_places(const AttnQ4Plan &p, int h_kv);  // in the run of all blocks' pages, some more for each; to be below INT32_MAX - 2^24
 hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnQ4Plan &p, void *workspace, void *out, int num_cus,
                                hipStream_t st);
+// Pages that requests share (paged_q4.h: PagePool)
+struct PagePool;
+size_t pages_workspace(int num_pages, int batch);
+hipError_t launch_copy_pages(const void *from, int from_pages, void *to, int to_pages, int page_bytes, const int *source, const int *target, int count, int num_cus, hipStream_t st);
+hipError_t launch_take_pages(const PagePool &pool, int *table, const int *positions, int batch, int width, int *missing, void *workspace, hipStream_t st);
+hipError_t launch_fork_pages(const PagePool &pool, const int *from, int from_batch, int from_width, const int *parents, const int *positions, int *table, int batch, int width, int *missing,
+                             void *workspace, int num_cus, hipStream_t st);
+hipError_t launch_free_pages(int *references, int num_pages, int *table, const int *keep, int batch, int width, int num_cus, hipStream_t st);
+hipError_t launch_compact_pages(const PagePool &pool, int *table, int batch, int width, int *used, void *workspace, int num_cus, hipStream_t st);
+// Bounds of pages' keys, pages selected by them
+constexpr int kSelectInLds = 32768;  // pages of a request whose scores fit the LDS
+hipError_t launch_bound_pages_q4(const Requests &req, int h_kv, int d, const void *pages, int8_t *codes, float *steps, hipStream_t st);
+size_t select_workspace(int tokens, int h_kv, int max_context, int num_cus);
+hipError_t launch_select_pages_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const int8_t *codes, const float *steps, int first, int last, int count, void *workspace,
+                                  int *selected, int num_cus, hipStream_t st);
+// Attention in parts that are joined: of selected pages, and of requests with common pages
+struct AttnPartsPlan {
+    long prefix_blocks, blocks;  // of 16 query rows of a KV head: of groups (common pages), of requests
+    int prefix_parts, parts;     // runs that their pages are cut into
+    size_t bytes;                // of the workspace
+};
+AttnPartsPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, int count, int num_cus);
+AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv, int d, int max_tokens, int max_context, int groups, int group_tokens, int longest, int num_cus);
+hipError_t launch_attention_selected_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *selected, int count, const AttnPartsPlan &p, void *workspace,
+                                        void *out, int num_cus, hipStream_t st);
+hipError_t launch_attention_shared_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *group_start, const int *prefix, int groups, int group_tokens,
+                                      int longest, const AttnPartsPlan &p, void *workspace, void *out, int num_cus, hipStream_t st);
 struct AdapterPlan {
     int rows;           // M rounded up
     int parts, part_k;  // K in `parts` parts of `part_k`

@@ -1,0 +1,317 @@
+// Which pages of a paged 4-bit cache are worth attention's while: bounds of each page's keys, and the pages whose bounds promise a query the largest scores.
+//
+// Bounds of a page and KV head: the largest and the smallest value hi_d, lo_d of each of its d components over the page's positions, as 8-bit codes rounded outward:
+//   a = max_d max(|hi_d|, |lo_d|), step = a / 127, codes ceil(hi_d (127 / a)) and floor(lo_d (127 / a)).
+// No key k of the page has q . k above sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d.  With q in 8 bits too (s_h = max |q| / 127, codes rounded to the nearest) that sum is one of whole numbers
+// below 2^24, two runs of v_mfma_i32_16x16x64_i8 (the positive codes against the upper bounds, the negative ones against the lower), and exact in whatever order; a page's score for a
+// token and KV head is the most any of the head's queries could reach, step max_h s_h sum_h, each product rounded to 32 bits.
+#include "paged_q4.h"
+
+namespace qfc {
+namespace {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+struct BoundArgs {
+    const char *pages;
+    Requests req;
+    int8_t *codes;  // [num_pages][h_kv][2][D]: upper, lower
+    float *steps;   // [num_pages][h_kv]
+    int h_kv, slots;  // pages that a request's new tokens are in, at most
+};
+
+// largest (or smallest, of negated values) over the 16 lanes of a row
+__device__ __forceinline__ float row_max(float x) {
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false)));  // row_ror 8, 4, 2, 1
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xF, 0xF, false)));
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xF, 0xF, false)));
+    return fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xF, 0xF, false)));
+}
+__device__ __forceinline__ int clamped(float x) { return (int)fminf(fmaxf(x, -127.0f), 127.0f); }
+
+// A wavefront per page and head.  Lane (m, r) reads what it reads in attention: of the positions of its slots the octets 32 j + 8 r.
+template <int D>
+__global__ __launch_bounds__(256) void bound_pages_kernel(BoundArgs a) {
+    typedef PageLayout<D> L;
+    constexpr int G = L::G, W = L::W;
+    const int lane = threadIdx.x & 63, m = lane & 15, r = lane >> 4;
+    const long all = (long)a.req.batch * a.slots * a.h_kv, step = (long)gridDim.x * 4;
+    for (long i = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < all; i += step) {
+        const int kv = (int)(i % a.h_kv), slot = (int)(i / a.h_kv % a.slots), b = (int)(i / a.h_kv / a.slots);
+        const Span s = span_of(a.req, b);
+        const int p0 = max(s.positions - s.count, 0) / kPage + slot;
+        if (s.count == 0 || p0 * (long)kPage >= s.positions) continue;
+        const int page = page_of(a.req, b, p0 * kPage), there = s.positions - p0 * kPage;
+        if (page < 0) continue;
+        const char *src = a.pages + ((size_t)page * a.h_kv + kv) * L::kBytes;
+        float hi[G][8], lo[G][8];  // (lo: negated)
+#pragma unroll
+        for (int j = 0; j < G; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) hi[j][e] = lo[j][e] = -INFINITY;
+        typedef uint32_t words __attribute__((ext_vector_type(W)));
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int p = 16 * (m >> 2) + 4 * t + (m & 3);
+#pragma unroll
+            for (int jj = 0; jj < G / W; ++jj) {
+                const words c = *reinterpret_cast<const words *>(src + L::kCodesK + ((t * (G / W) + jj) * 64 + lane) * (4 * W));
+#pragma unroll
+                for (int jw = 0; jw < W; ++jw) {
+                    const int j = jj * W + jw;
+                    const float by = (float)*reinterpret_cast<const _Float16 *>(src + L::step_k(p, j)), off = (float)*reinterpret_cast<const _Float16 *>(src + L::offset_k(p, j));
+                    if (p < there) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float x = fmaf((float)((c[jw] >> nibble(e)) & 15u) - 8.0f, by, off);
+                            hi[j][e] = fmaxf(hi[j][e], x), lo[j][e] = fmaxf(lo[j][e], -x);
+                        }
+                    }
+                }
+            }
+        }
+        float most = 0.0f;
+#pragma unroll
+        for (int j = 0; j < G; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                hi[j][e] = row_max(hi[j][e]), lo[j][e] = row_max(lo[j][e]);
+                most = fmaxf(most, fmaxf(fabsf(hi[j][e]), fabsf(lo[j][e])));
+            }
+        most = fmaxf(most, __shfl_xor(most, 16, 64));
+        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        const float f = most > 0.0f ? 127.0f / most : 0.0f;
+        int8_t *dst = a.codes + ((size_t)page * a.h_kv + kv) * (2 * D);
+#pragma unroll
+        for (int j = 0; j < G; ++j) {  // lane m: octet m % G of the upper bounds (m < G) or the lower ones
+            if (m % 8 != j) continue;
+            u32x2 up = {0, 0}, down = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                up[e / 4] |= (uint32_t)(clamped(ceilf(hi[j][e] * f)) & 255) << (8 * (e % 4));
+                down[e / 4] |= (uint32_t)(clamped(floorf(-lo[j][e] * f)) & 255) << (8 * (e % 4));
+            }
+            *reinterpret_cast<u32x2 *>(dst + (m < 8 ? 0 : D) + 32 * j + 8 * r) = m < 8 ? up : down;
+        }
+        if (lane == 0) a.steps[(size_t)page * a.h_kv + kv] = most / 127.0f;
+    }
+}
+
+struct SelectArgs {
+    const _Float16 *q;
+    Requests req;
+    const int8_t *codes;
+    const float *steps;
+    int *selected;  // [tokens][h_kv][count]
+    float *scores;  // of a workgroup [most_pages], where they do not fit the LDS
+    int h_q, h_kv, g, first, last, count, most_pages;
+    long items;
+};
+
+__device__ __forceinline__ uint32_t key_of(float x) {  // order of floats as one of whole numbers
+    const uint32_t u = __float_as_uint(x);
+    return u ^ ((int)u < 0 ? 0xFFFFFFFFu : 0x80000000u);
+}
+
+// A workgroup per token and KV head: scores of all pages it sees, the one that is the last to be taken (a byte of it at a time, by how many scores begin so), and the list in ascending order.
+template <int D, bool IN_LDS>
+__global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
+    constexpr int C = D / 64, AHEAD = 2;  // chunks of 64 components; groups of 16 pages on their way
+    extern __shared__ float lds_scores[];
+    __shared__ int counts[256], found[2], taken[16][2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, m = lane & 15, r = lane >> 4;
+    float *const scores = IN_LDS ? lds_scores : a.scores + (size_t)blockIdx.x * a.most_pages;
+    for (long item = blockIdx.x; item < a.items; item += gridDim.x) {
+        const int kv = (int)(item % a.h_kv), token = (int)(item / a.h_kv);
+        const int b = __builtin_amdgcn_readfirstlane(request_of<1>(a.req, token, 0, lane));
+        if (b >= a.req.batch) return;
+        const Span s = span_of(a.req, b);
+        if (token < s.first || token - s.first >= s.count) continue;
+        const int pos = s.positions - s.count + token - s.first, sees = pos < 0 ? 0 : pos / kPage + 1;
+        int *const out = a.selected + (size_t)item * a.count;
+        if (sees <= a.count) {
+            for (int i = threadIdx.x; i < a.count; i += blockDim.x) out[i] = i < sees ? i : -1;
+            continue;
+        }
+        const int k = a.count - a.first - a.last, mid0 = a.first, mid1 = sees - a.last;
+        if (k > 0) {
+            // ---- scores of the pages in between, 16 heads at a time
+            for (int h0 = 0; h0 < a.g; h0 += 16) {
+                const _Float16 *q = a.q + ((size_t)token * a.h_q + kv * a.g + min(h0 + m, a.g - 1)) * D;
+                float x[C][16], top = 0.0f;
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const h8 v = *reinterpret_cast<const h8 *>(q + 64 * c + 16 * r + 8 * u);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            x[c][8 * u + e] = (float)v[e];
+                            top = fmaxf(top, fabsf((float)v[e]));
+                        }
+                    }
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float f = top > 0.0f ? 127.0f / top : 0.0f, by = top / 127.0f;
+                i32x4 up[C], down[C];
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    up[c] = down[c] = i32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int code = clamped(rintf(x[c][e] * f));
+                        up[c][e / 4] |= (max(code, 0) & 255) << (8 * (e % 4));
+                        down[c][e / 4] |= (min(code, 0) & 255) << (8 * (e % 4));
+                    }
+                }
+                float of_row[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) of_row[i] = __shfl(by, 4 * r + i, 64);
+                for (int p0 = mid0 + wave * (16 * AHEAD); p0 < mid1; p0 += waves * (16 * AHEAD)) {
+                    int page[AHEAD];
+                    float step[AHEAD];
+                    i32x4 bound[AHEAD][2 * C];
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) page[u] = page_of(a.req, b, min(p0 + 16 * u + m, mid1 - 1) * kPage);
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        const size_t at = (size_t)max(page[u], 0) * a.h_kv + kv;
+#pragma unroll
+                        for (int c = 0; c < 2 * C; ++c) bound[u][c] = *reinterpret_cast<const i32x4 *>(a.codes + at * (2 * D) + 64 * c + 16 * r);
+                        step[u] = a.steps[at];
+                    }
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        i32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+                        for (int c = 0; c < C; ++c) {
+                            sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(up[c], bound[u][c], sum, 0, 0, 0);
+                            sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(down[c], bound[u][C + c], sum, 0, 0, 0);
+                        }
+                        float most = (float)sum[0] * of_row[0];  // rows 4 r .. + 3, page m
+#pragma unroll
+                        for (int i = 1; i < 4; ++i) most = fmaxf(most, (float)sum[i] * of_row[i]);
+                        most = fmaxf(most, __shfl_xor(most, 16, 64));
+                        most = fmaxf(most, __shfl_xor(most, 32, 64));
+                        most = page[u] < 0 ? -INFINITY : most * step[u];
+                        const int p = p0 + 16 * u + m;
+                        if (r == 0 && p < mid1) scores[p] = h0 == 0 ? most : fmaxf(scores[p], most);
+                    }
+                }
+            }
+            __syncthreads();
+            // ---- the k-th of them
+            uint32_t prefix = 0, mask = 0;
+            int left = k;
+            for (int shift = 24; shift >= 0; shift -= 8) {
+                for (int i = threadIdx.x; i < 256; i += blockDim.x) counts[i] = 0;
+                __syncthreads();
+                for (int p = mid0 + (int)threadIdx.x; p < mid1; p += blockDim.x) {
+                    const uint32_t key = key_of(scores[p]);
+                    if ((key & mask) == prefix) atomicAdd(counts + (key >> shift & 255u), 1);
+                }
+                __syncthreads();
+                if (wave == 0) {  // lane l: bytes 255 - 4 l and the three below
+                    int own[4], all = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) all += own[i] = counts[255 - 4 * lane - i];
+                    int upto = all;
+#pragma unroll
+                    for (int off = 1; off < 64; off <<= 1) {
+                        const int other = __shfl_up(upto, off, 64);
+                        upto += lane >= off ? other : 0;
+                    }
+                    if (upto >= left && upto - all < left) {
+                        int rest = left - (upto - all), byte = 255 - 4 * lane;
+#pragma unroll
+                        for (int i = 0; i < 3; ++i)
+                            if (rest > own[i] && byte == 255 - 4 * lane - i) rest -= own[i], --byte;
+                        found[0] = byte, found[1] = rest;
+                    }
+                }
+                __syncthreads();
+                prefix |= (uint32_t)found[0] << shift, mask |= 255u << shift, left = found[1];
+            }
+            // ---- the list: above it, and of those level with it the first `left`
+            int above = 0, level = 0;  // before this round
+            for (int base = mid0; base < mid1; base += blockDim.x) {
+                const int p = base + (int)threadIdx.x;
+                const uint32_t key = p < mid1 ? key_of(scores[p]) : 0;
+                const bool is_above = p < mid1 && key > prefix, is_level = p < mid1 && key == prefix;
+                const uint64_t above_bits = __ballot(is_above), level_bits = __ballot(is_level), lower = (1ull << lane) - 1;
+                __syncthreads();  // (the round before has been read)
+                if (lane == 0) taken[wave][0] = __popcll(above_bits), taken[wave][1] = __popcll(level_bits);
+                __syncthreads();
+                int above_here = above + __popcll(above_bits & lower), level_here = level + __popcll(level_bits & lower);
+                for (int w = 0; w < waves; ++w) {
+                    const int t0 = taken[w][0], t1 = taken[w][1];
+                    if (w < wave) above_here += t0, level_here += t1;
+                    above += t0, level += t1;
+                }
+                if (is_above || (is_level && level_here < left)) out[a.first + above_here + min(level_here, left)] = p;
+            }
+        }
+        for (int i = threadIdx.x; i < a.first + a.last; i += blockDim.x) out[i < a.first ? i : k + i] = i < a.first ? i : sees - (a.first + a.last) + i;
+        __syncthreads();
+    }
+}
+
+template <int D, bool IN_LDS>
+hipError_t launch_select(const SelectArgs &a, int threads, unsigned grid, hipStream_t st) {
+    const size_t lds = IN_LDS ? (size_t)a.most_pages * sizeof(float) : 0;
+    if constexpr (IN_LDS)
+        if (const hipError_t e = allow_dynamic_lds<select_pages_kernel<D, true>>((size_t)kSelectInLds * sizeof(float)); e != hipSuccess) return e;
+    select_pages_kernel<D, IN_LDS><<<grid, threads, lds, st>>>(a);
+    return hipGetLastError();
+}
+
+int pages_below(int max_context) { return (max_context + kPage - 1) / kPage; }
+
+}  // namespace
+
+hipError_t launch_bound_pages_q4(const Requests &req, int h_kv, int d, const void *pages, int8_t *codes, float *steps, hipStream_t st) {
+    BoundArgs a;
+    a.pages = static_cast<const char *>(pages);
+    a.req = req;
+    a.codes = codes, a.steps = steps, a.h_kv = h_kv;
+    a.slots = (req.max_tokens < req.max_context ? req.max_tokens : req.max_context) / kPage + 2;
+    const long wgs = ((long)req.batch * a.slots * h_kv + 3) / 4, most = 1L << 22;
+    const unsigned grid = (unsigned)(wgs < most ? wgs : most);
+    if (d == 64)
+        bound_pages_kernel<64><<<grid, 256, 0, st>>>(a);
+    else if (d == 128)
+        bound_pages_kernel<128><<<grid, 256, 0, st>>>(a);
+    else
+        bound_pages_kernel<256><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+size_t select_workspace(int tokens, int h_kv, int max_context, int num_cus) {
+    const int pages = pages_below(max_context);
+    const long items = (long)tokens * h_kv, wgs = items < num_cus ? items : num_cus;
+    return 256 + (pages > kSelectInLds ? (size_t)wgs * pages * sizeof(float) : 0);
+}
+
+hipError_t launch_select_pages_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const int8_t *codes, const float *steps, int first, int last, int count, void *workspace,
+                                  int *selected, int num_cus, hipStream_t st) {
+    SelectArgs a;
+    a.q = static_cast<const _Float16 *>(q);
+    a.req = req;
+    a.codes = codes, a.steps = steps, a.selected = selected, a.scores = static_cast<float *>(workspace);
+    a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv, a.first = first, a.last = last, a.count = count, a.most_pages = pages_below(req.max_context);
+    a.items = (long)req.tokens * h_kv;
+    const bool in_lds = a.most_pages <= kSelectInLds;
+    const long most = in_lds ? 1L << 20 : num_cus;
+    const unsigned grid = (unsigned)(a.items < most ? a.items : most);
+    const int threads = a.most_pages > 512 ? 1024 : 256;
+    switch (d) {
+        case 64: return in_lds ? launch_select<64, true>(a, threads, grid, st) : launch_select<64, false>(a, threads, grid, st);
+        case 128: return in_lds ? launch_select<128, true>(a, threads, grid, st) : launch_select<128, false>(a, threads, grid, st);
+        case 256: return in_lds ? launch_select<256, true>(a, threads, grid, st) : launch_select<256, false>(a, threads, grid, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace qfc

@@ -1,0 +1,807 @@
+"""Operators on pages of the 4-bit cache that requests share or pick from, against the oracle: tables and counts, attention behind common pages, bounds, selection, attention over selected pages,
+and runs of them as a server makes them."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as ref
+from oracle import requests as q4
+from paper_2505_00232_amd import binding as B
+from test_requests import DEV, _close, _filled, _normal, _pages, _requests, _t
+
+gpu = pytest.mark.gpu
+
+
+def _i(x):
+    return torch.tensor(np.asarray(x, dtype=np.int32)).to(DEV)
+
+
+def _space(n):
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=DEV)
+
+
+# ---------------------------------------------------------------- refusals, without a GPU
+def test_page_refusals_before_any_launch():
+    L, A, odd, s, size = B.lib(), 0x1000, 0x1002, ctypes.c_void_p(0), ctypes.c_size_t(0)
+    cache = lambda pages=A, num=4, h=2, d=64: ctypes.byref(B.CacheDesc(pages, num, h, d))
+    far, big = 0x100000, 1 << 40
+    assert L.qfc_pages_workspace_size(cache(None), 3, ctypes.byref(size)) == 0 and size.value > 0
+    assert L.qfc_pages_workspace_size(cache(), 0, ctypes.byref(size)) == 1 and L.qfc_pages_workspace_size(cache(), 3, None) == 1 and L.qfc_pages_workspace_size(None, 3, ctypes.byref(size)) == 1
+    assert L.qfc_pages_workspace_size(cache(d=96), 3, ctypes.byref(size)) == 2 and L.qfc_pages_workspace_size(cache(), (1 << 22) + 1, ctypes.byref(size)) == 2
+    take = lambda c=cache(), r=A, t=A, p=A, b=2, w=3, m=A, ws=A, n=big: L.qfc_take_pages(c, r, t, p, b, w, m, ws, n, s)
+    fork = lambda c=cache(), r=A, f=far, fb=2, fw=3, pa=A, p=A, t=A, b=2, w=3, m=A, ws=A, n=big: L.qfc_fork_pages(c, r, f, fb, fw, pa, p, t, b, w, m, ws, n, s)
+    free = lambda c=cache(), r=A, t=A, k=A, b=2, w=3: L.qfc_free_pages(c, r, t, k, b, w, s)
+    compact = lambda c=cache(), r=A, t=A, b=2, w=3, m=A, ws=A, n=big: L.qfc_compact_pages(c, r, t, b, w, m, ws, n, s)
+    for call in (take, fork, free, compact):
+        assert call(c=None) == 1 and call(c=cache(num=0)) == 1 and call(r=None) == 1 and call(t=None) == 1 and call(b=0) == 1 and call(w=0) == 1 and call(b=-1) == 1
+        assert call(c=cache(d=80)) == 2 and call(b=(1 << 22) + 1) == 2 and call(c=cache(h=1 << 20)) == 2
+        assert call(r=odd) == 4 and call(t=odd) == 4
+    for call in (take, fork, compact):
+        assert call(ws=None) == 1 and call(c=cache(None)) == 1 and call(n=8) == 3 and call(ws=0x1008) == 4 and call(m=odd) == 4 and call(c=cache(0x1008)) == 4
+    assert take(p=None) == 1 and take(p=odd) == 4 and free(k=odd) == 4
+    for name in ("f", "pa", "p"):
+        assert fork(**{name: None}) == 1 and fork(**{name: odd}) == 4
+    assert fork(fb=0) == 1 and fork(fw=0) == 1
+    assert fork(f=A) == 1 and fork(f=A + 20) == 1 and fork(f=A - 20) == 1  # tables that overlap
+    copy = lambda f=cache(), t=cache(num=9), a=A, b=A, n=2: L.qfc_copy_pages(f, t, a, b, n, s)
+    assert copy(f=None) == 1 and copy(t=None) == 1 and copy(t=cache(h=3)) == 1 and copy(t=cache(d=128)) == 1 and copy(n=-1) == 1 and copy(a=None) == 1 and copy(b=None) == 1
+    assert copy(f=cache(None)) == 1 and copy(f=cache(0x1008)) == 4 and copy(a=odd) == 4 and copy(b=odd) == 4 and copy(f=cache(d=32), t=cache(d=32)) == 2
+    assert copy(n=0) == 0 and copy(n=0, a=None, b=None) == 0  # nothing to do
+
+
+def test_attention_and_selection_refusals_before_any_launch():
+    L, A, odd, s, size, big = B.lib(), 0x1000, 0x1002, ctypes.c_void_p(0), ctypes.c_size_t(0), 1 << 60
+    cache = lambda pages=A, num=4, h=2, d=64: ctypes.byref(B.CacheDesc(pages, num, h, d))
+    req = lambda start=A, ctx=A, table=A, batch=2, tokens=2, most=1, longest=128, width=2: ctypes.byref(B.RequestsDesc(start, ctx, table, batch, tokens, most, longest, width))
+    shared = lambda g=A, p=A, n=1, tokens=2, longest=128: ctypes.byref(B.SharedDesc(g, p, n, tokens, longest))
+    bounds = lambda c=A, t=A: ctypes.byref(B.BoundsDesc(c, t))
+    common = lambda r=req(), c=cache(), h=4, sh=shared(), q=A, ws=A, n=big, o=A: L.qfc_attention_shared_q4(q, r, sh, h, c, ws, n, o, s)
+    bound = lambda r=req(), c=cache(), b=bounds(): L.qfc_bound_pages_q4(r, c, b, s)
+    select = lambda r=req(), c=cache(), h=4, b=bounds(), first=1, last=1, count=4, q=A, ws=A, n=big, o=A: L.qfc_select_pages_q4(q, r, h, c, b, first, last, count, ws, n, o, s)
+    some = lambda r=req(), c=cache(), h=4, sel=A, count=4, q=A, ws=A, n=big, o=A: L.qfc_attention_selected_q4(q, r, h, c, sel, count, ws, n, o, s)
+    for call in (common, bound, select, some):
+        for bad in (None, req(start=None), req(ctx=None), req(table=None), req(batch=0), req(tokens=-1), req(most=0), req(longest=0), req(longest=129), req(width=0)):
+            assert call(r=bad) == 1
+        for bad in (None, cache(None), cache(num=0), cache(h=0)):
+            assert call(c=bad) == 1
+        assert call(c=cache(d=80)) == 2 and call(c=cache(odd)) == 4 and call(r=req(start=odd)) == 4 and call(r=req(batch=40000)) == 2
+        assert call(r=req(tokens=0)) == 0  # nothing to do, nothing launched
+    for call in (common, select, some):
+        assert call(h=3) == 1 and call(h=0) == 1 and call(h=65534) == 2 and call(q=None) == 1 and call(ws=None) == 1 and call(o=None) == 1 and call(q=odd) == 4 and call(ws=odd) == 4
+        assert call(o=0x1001) == 4 and call(n=8) == 3
+    for bad in (None, shared(None), shared(p=None), shared(n=0), shared(tokens=0), shared(longest=0)):
+        assert common(sh=bad) == 1
+    assert common(sh=shared(odd)) == 4 and common(sh=shared(p=odd)) == 4 and common(o=0x1008) == 4
+    for call in (bound, select):
+        assert call(b=None) == 1 and call(b=bounds(None)) == 1 and call(b=bounds(t=None)) == 1 and call(b=bounds(0x1008)) == 4 and call(b=bounds(t=odd)) == 4
+    assert select(first=-1) == 1 and select(last=-1) == 1 and select(count=0) == 1 and select(first=3, last=2) == 1 and select(first=2 ** 31 - 1, last=2 ** 31 - 1) == 1 and select(count=65537) == 2
+    assert some(sel=None) == 1 and some(sel=0x1001) == 4 and some(count=0) == 1 and some(count=65537) == 2 and some(o=0x1008) == 4
+    q = ctypes.byref(size)
+    for f in (lambda r, h, c, o: L.qfc_attention_shared_q4_workspace_size(r, shared(None, None), h, c, o), L.qfc_select_pages_q4_workspace_size,
+              lambda r, h, c, o: L.qfc_attention_selected_q4_workspace_size(r, h, c, 5, o)):
+        assert f(req(None, None, None), 4, cache(None), q) == 0 and size.value >= 256
+        assert f(req(), 4, cache(), None) == 1 and f(None, 4, cache(), q) == 1 and f(req(), 3, cache(), q) == 1 and f(req(), 4, cache(d=96), q) == 2
+    assert L.qfc_attention_shared_q4_workspace_size(req(), None, 4, cache(), q) == 1 and L.qfc_attention_selected_q4_workspace_size(req(), 4, cache(), 0, q) == 1
+
+
+def test_binding_refuses_host_tensors_and_other_shapes():
+    c = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        B.SharedPrefixes(torch.zeros(3, dtype=torch.int32), c, 2, 64)
+    with pytest.raises(ValueError):
+        B._table(torch.zeros(3, dtype=torch.int32), "page_table")
+    with pytest.raises(ValueError):
+        B._table(torch.zeros((3, 2), dtype=torch.int32), "page_table")
+
+
+# ---------------------------------------------------------------- the oracle by hand
+def test_oracle_pages_by_hand():
+    table, refs, missing = ref.take(np.array([[3, -1, -1], [7, 9, -1]]), np.array([0, 1, 0, 1, 0]), [130, 64])
+    assert np.array_equal(table, [[3, 0, 2], [4, 9, -1]]) and np.array_equal(refs, [1, 1, 1, 1, 1]) and missing == 0
+    pages = np.arange(5)[:, None]
+    table, refs, pages, missing = ref.fork(np.array([[1, 3]]), np.array([0, 1, 0, 1, 0]), [0, 0, 2, 0], [100, 64, 64, 65], 2, pages)
+    assert np.array_equal(table, [[1, 0], [1, -1], [-1, -1], [1, 2]]) and np.array_equal(refs, [1, 4, 1, 1, 0]) and np.array_equal(pages[:, 0], [3, 1, 3, 3, 4]) and missing == 0
+    table, refs = ref.free(table, refs, [64, 0, 5, 128])
+    assert np.array_equal(table, [[1, -1], [-1, -1], [-1, -1], [1, 2]]) and np.array_equal(refs, [0, 3, 1, 1, 0])
+    table, refs, pages, used = ref.compact(np.array([[1, 2], [3, 1]]), np.array([0, 2, 1, 1, 0]), np.arange(5))
+    assert used == 3 and np.array_equal(table, [[1, 2], [0, 1]]) and np.array_equal(refs, [1, 2, 1, 0, 0]) and pages[0] == 3
+
+
+def test_oracle_selection_by_hand():
+    codes, step = ref.bounds(np.array([[1.0, -2.0], [127.0, 4.25], [-3.5, 0.0]]))
+    assert np.array_equal(codes, [[127, 5], [-4, -2]]) and step == 1
+    score = ref.scores(np.array([[127.0, -127.0]]), np.array([codes, codes]), np.array([1.0, 2.0]), np.array([True, True]))
+    assert score[0] == 127 * 127 + 127 * 2 and score[1] == 2 * score[0]
+    assert np.array_equal(ref.select(np.array([0, 5, 7, 5, 5, 0.0]), 6, 1, 1, 4), [0, 1, 2, 5])  # of equal ones the first
+    assert np.array_equal(ref.select(np.zeros(3), 3, 1, 1, 5), [0, 1, 2, -1, -1])
+
+
+# ---------------------------------------------------------------- pages
+class Pool:
+    """A cache with references and their copies on the host."""
+
+    def __init__(self, num, h_kv=1, d=64, rng=None):
+        self.cache = B.PagedCache(num, h_kv, d)
+        self.bytes = 80 * d * h_kv
+        self.pages = (rng or np.random.default_rng(3)).integers(0, 256, (num, self.bytes), dtype=np.uint8)
+        self.cache.pages.copy_(torch.from_numpy(self.pages.ravel()))
+
+    def now(self):
+        return self.cache.pages.cpu().numpy().reshape(-1, self.bytes)
+
+    def space(self, batch):
+        n = B.qfc_pages_workspace_size(self.cache, batch)
+        w = torch.full((n + 64,), 0xAB, dtype=torch.uint8, device=DEV)
+        return w[:n], w[n:]
+
+
+def _counts(rng, num, share):
+    """References of a pool of which a share is in use."""
+    return np.where(rng.random(num) < share, rng.integers(1, 4, num), 0).astype(np.int32)
+
+
+@gpu
+@pytest.mark.parametrize("num,batch,width,share", [(1, 1, 1, 0.0), (1, 2, 3, 1.0), (64, 3, 7, 0.5), (65, 1, 70, 0.1), (1023, 5, 130, 0.5), (1024, 4, 300, 0.9), (1025, 130, 9, 0.3), (5000, 37, 65, 0.7),
+                                                   (70000, 11, 200, 0.99), (4096, 1, 5000, 0.0)])
+def test_take_pages(num, batch, width, share):
+    rng = np.random.default_rng(num + batch)
+    pool, refs = Pool(num), _counts(rng, num, share)
+    table = np.where(rng.random((batch, width)) < 0.4, rng.integers(-5, num + 5, (batch, width)), -1).astype(np.int32)
+    positions = rng.integers(-3, width * 64 + 100, batch).astype(np.int32)
+    positions[0] = width * 64
+    want = ref.take(table, refs, positions)
+    t, r, missing, (space, behind) = _i(table), _i(refs), _i([77]), pool.space(batch)
+    B.qfc_take_pages(pool.cache, r, t, _i(positions), space, missing)
+    assert np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(r.cpu().numpy(), want[1]) and int(missing) == want[2]
+    assert np.array_equal(pool.now(), pool.pages) and bool((behind == 0xAB).all())
+    t, r = _i(table), _i(refs)
+    B.qfc_take_pages(pool.cache, r, t, _i(positions), space)
+    assert np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(r.cpu().numpy(), want[1])
+
+
+@gpu
+@pytest.mark.parametrize("num,parents,children,from_width,width,share,h_kv,d", [(4, 1, 1, 1, 1, 0.5, 1, 64), (70, 3, 5, 4, 6, 0.5, 3, 64), (1500, 20, 64, 30, 20, 0.4, 2, 128),
+                                                                                (3000, 7, 300, 9, 9, 0.95, 1, 256), (2100, 2, 3, 600, 700, 0.6, 8, 128)])
+def test_fork_pages(num, parents, children, from_width, width, share, h_kv, d):
+    rng = np.random.default_rng(num)
+    pool, refs = Pool(num, h_kv, d), _counts(rng, num, share)
+    used = np.flatnonzero(refs)
+    source = rng.choice(used, (parents, from_width)).astype(np.int32) if used.size else np.full((parents, from_width), -1, np.int32)
+    source[rng.random(source.shape) < 0.05] = rng.choice([-1, num, -7, 2 ** 30])
+    of = rng.integers(0, parents, children).astype(np.int32)
+    of[rng.random(children) < 0.1] = rng.choice([-1, parents])
+    positions = rng.integers(0, 64 * from_width + 30, children).astype(np.int32)
+    positions[rng.random(children) < 0.3] &= ~63
+    want = ref.fork(source, refs, of, positions, width, pool.pages)
+    f, r, missing, (space, behind) = _i(source), _i(refs), _i([77]), pool.space(children)
+    t = torch.full((children, width), 123456, dtype=torch.int32, device=DEV)
+    B.qfc_fork_pages(pool.cache, r, f, _i(of), _i(positions), t, space, missing)
+    assert np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(r.cpu().numpy(), want[1]) and int(missing) == want[3]
+    assert np.array_equal(pool.now(), want[2]) and np.array_equal(f.cpu().numpy(), source) and bool((behind == 0xAB).all())
+
+
+@gpu
+@pytest.mark.parametrize("num,batch,width", [(3, 1, 1), (100, 7, 33), (5000, 300, 100)])
+def test_free_pages(num, batch, width):
+    rng = np.random.default_rng(num)
+    pool = Pool(num)
+    table = np.where(rng.random((batch, width)) < 0.7, rng.integers(-2, num + 2, (batch, width)), -1).astype(np.int32)
+    refs = np.bincount(table[(table >= 0) & (table < num)], minlength=num).astype(np.int32)
+    keep = rng.integers(-5, 64 * width + 64, batch).astype(np.int32)
+    for k in (keep, None):
+        want = ref.free(table, refs, k)
+        t, r = _i(table), _i(refs)
+        B.qfc_free_pages(pool.cache, r, t, None if k is None else _i(k))
+        assert np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(r.cpu().numpy(), want[1])
+        assert k is not None or not r.any()
+
+
+@gpu
+@pytest.mark.parametrize("num,batch,width,share,h_kv,d", [(1, 1, 1, 0.0, 1, 64), (1, 1, 1, 1.0, 1, 64), (64, 3, 30, 0.5, 1, 64), (1024, 9, 200, 1.0, 1, 64), (1025, 9, 200, 0.5, 2, 64),
+                                                          (3001, 50, 40, 0.03, 1, 128), (2048, 3, 900, 0.5, 1, 256), (5000, 17, 300, 0.9, 3, 64)])
+def test_compact_pages(num, batch, width, share, h_kv, d):
+    rng = np.random.default_rng(num)
+    pool = Pool(num, h_kv, d)
+    used = np.flatnonzero(rng.random(num) < share)
+    table = rng.choice(used, (batch, width)).astype(np.int32) if used.size else np.full((batch, width), -1, np.int32)
+    table[rng.random(table.shape) < 0.2] = -1
+    table[0, 0] = num  # no page
+    refs = np.bincount(table[(table >= 0) & (table < num)], minlength=num).astype(np.int32)
+    want = ref.compact(table, refs, pool.pages)
+    t, r, count, (space, behind) = _i(table), _i(refs), _i([-1]), pool.space(batch)
+    B.qfc_compact_pages(pool.cache, r, t, space, count)
+    n = want[3]
+    assert int(count) == n and np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(r.cpu().numpy(), want[1]) and bool((behind == 0xAB).all())
+    assert np.array_equal(pool.now(), want[2])
+    assert bool((r[:n] > 0).all()) and not r[n:].any()
+    B.qfc_compact_pages(pool.cache, r, t, space, None)  # once more: nothing to do
+    assert np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(pool.now(), want[2])
+
+
+@gpu
+@pytest.mark.parametrize("count,h_kv,d", [(1, 1, 64), (5, 3, 64), (333, 2, 128), (40, 8, 256)])
+def test_copy_pages(count, h_kv, d):
+    rng = np.random.default_rng(count)
+    a, b = Pool(count + 7, h_kv, d, rng), Pool(count + 3, h_kv, d, rng)
+    source, target = rng.permutation(count + 7)[:count].astype(np.int32), rng.permutation(count + 3)[:count].astype(np.int32)
+    if count > 4:
+        source[1], target[2], source[3] = -1, count + 3, count + 7
+    want = b.pages.copy()
+    for x, y in zip(source, target):
+        if 0 <= x < count + 7 and 0 <= y < count + 3:
+            want[y] = a.pages[x]
+    B.qfc_copy_pages(a.cache, b.cache, _i(source), _i(target))
+    assert np.array_equal(b.now(), want) and np.array_equal(a.now(), a.pages)
+    one = a.now()
+    B.qfc_copy_pages(a.cache, a.cache, _i([count + 6]), _i([0]))
+    one[0] = one[count + 6]
+    assert np.array_equal(a.now(), one)
+    B.qfc_copy_pages(a.cache, a.cache, _i([]), _i([]))
+
+
+@gpu
+def test_pages_of_a_search_step_by_step():
+    """Forks, frees, new pages and compactions in turn, as a search over continuations makes them; the counts are those of the tables at every step."""
+    rng = np.random.default_rng(9)
+    num, batch, width = 400, 12, 20
+    pool = Pool(num)
+    pages, refs, table, positions = pool.pages, np.zeros(num, np.int32), np.full((batch, width), -1, np.int32), rng.integers(1, 300, batch).astype(np.int32)
+    r, t, (space, _) = _i(refs), _i(table), pool.space(batch)
+    other = torch.empty_like(t)
+    for step in range(25):
+        B.qfc_take_pages(pool.cache, r, t, _i(positions), space)
+        table, refs, missing = ref.take(table, refs, positions)
+        assert missing == 0
+        of = rng.integers(0, batch, batch).astype(np.int32)
+        B.qfc_fork_pages(pool.cache, r, t, _i(of), _i(positions[of]), other, space)
+        children, refs, pages, missing = ref.fork(table, refs, of, positions[of], width, pages)
+        assert missing == 0
+        B.qfc_free_pages(pool.cache, r, t)
+        _, refs = ref.free(table, refs)
+        t, other, table = other, t, children
+        if step % 5 == 4:
+            cut = (positions[of] // 2).astype(np.int32)  # tokens that are taken back
+            B.qfc_free_pages(pool.cache, r, t, _i(cut))
+            table, refs = ref.free(table, refs, cut)
+            positions = np.maximum(cut, 1)
+            B.qfc_compact_pages(pool.cache, r, t, space)
+            table, refs, pages, _ = ref.compact(table, refs, pages)
+        else:
+            positions = np.minimum(positions[of] + rng.integers(1, 90, batch), width * 64).astype(np.int32)
+        assert np.array_equal(t.cpu().numpy(), table) and np.array_equal(r.cpu().numpy(), refs)
+        assert np.array_equal(refs, np.bincount(table[table >= 0], minlength=num))
+        assert np.array_equal(pool.now(), pages)
+
+
+@gpu
+def test_pages_captured_and_replayed():
+    rng = np.random.default_rng(10)
+    num, batch, width = 300, 6, 9
+    pool, refs = Pool(num), np.zeros(num, np.int32)
+    start, refs, _ = ref.take(np.full((batch, width), -1, np.int32), refs, [300, 64, 1, 130, 500, 65])
+    space, _ = pool.space(batch)
+    r, t, kids = _i(refs), _i(start), _i(np.zeros((batch, width)))
+    of, positions, grown = _i(np.zeros(batch)), _i(np.zeros(batch)), _i(np.zeros(batch))
+    counts, tables = r.clone(), t.clone()
+
+    def step():
+        r.copy_(counts)
+        t.copy_(tables)
+        B.qfc_fork_pages(pool.cache, r, t, of, positions, kids, space)
+        B.qfc_free_pages(pool.cache, r, t)
+        B.qfc_take_pages(pool.cache, r, kids, grown, space)
+        B.qfc_compact_pages(pool.cache, r, kids, space)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    torch.cuda.synchronize()
+    for k in range(4):
+        parents = rng.integers(0, batch, batch).astype(np.int32)
+        n = np.array([300, 64, 1, 130, 500, 65], np.int32)[parents]
+        pool.cache.pages.copy_(torch.from_numpy(pool.pages.ravel()))
+        of.copy_(_i(parents)), positions.copy_(_i(n)), grown.copy_(_i(n + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        table, want, pages, _ = ref.fork(start, refs, parents, n, width, pool.pages)
+        _, want = ref.free(start, want)
+        table, want, _ = ref.take(table, want, n + k)
+        table, want, pages, _ = ref.compact(table, want, pages)
+        assert np.array_equal(kids.cpu().numpy(), table) and np.array_equal(r.cpu().numpy(), want) and np.array_equal(pool.now(), pages)
+
+
+# ---------------------------------------------------------------- attention behind common pages
+def _attend_shared(req, shared, q, h_q, cache, fill=0.0):
+    out = torch.full((q.shape[0], h_q * cache.d_head), fill, dtype=torch.float16, device=DEV)
+    n = B.qfc_attention_shared_q4_workspace_size(req, shared, h_q, cache)
+    ws = torch.full((n + 64,), 0xFF, dtype=torch.uint8, device=DEV)  # (NaN in what is read without having been written)
+    B.qfc_attention_shared_q4(_t(q), req, shared, h_q, cache, ws[:n], out)
+    torch.cuda.synchronize()
+    assert bool((ws[n:] == 0xFF).all())
+    return out.cpu().numpy().astype(np.float64)
+
+
+def _shared_batch(rng, group, prefix, S, n, h_kv, d):
+    """A cache and a table in which the requests of each group share prefix // 64 pages; K, V and V's parts per request."""
+    lead = np.arange(len(S))
+    whole = np.zeros(len(S), int)
+    for i, p in enumerate(prefix):
+        first = group[i]
+        for b in range(group[i], group[i + 1]):
+            lead[b], whole[b] = first, p // 64
+    for b in range(len(S)):
+        whole[b] = min(whole[b], (n[b] - S[b]) // 64 if S[b] else n[b] // 64, n[lead[b]] // 64)
+    table, num = _pages(rng, n)
+    k, v = [_normal(rng, x, h_kv, d) for x in n], [_normal(rng, x, h_kv, d) for x in n]
+    for b in range(len(S)):
+        if lead[b] != b:
+            table[b, :whole[b]] = table[lead[b], :whole[b]]
+            k[b][:64 * whole[b]], v[b][:64 * whole[b]] = k[lead[b]][:64 * whole[b]], v[lead[b]][:64 * whole[b]]
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num, np.concatenate(k), np.concatenate(v))
+    return cache, table, K, V, P
+
+
+SHARED = [  # group_start, positions, S, n, h_q, h_kv, d
+    ([0, 1], [64], [1], [65], 1, 1, 64),
+    ([0, 2], [128], [1, 1], [129, 300], 4, 1, 128),
+    ([0, 3], [700], [1, 1, 1], [701, 800, 1000], 8, 2, 64),
+    ([0, 2, 5], [200, 64], [1, 2, 1, 4, 1], [300, 202, 70, 100, 65], 8, 4, 256),
+    ([1, 3], [130], [1, 1, 1, 2], [40, 131, 200, 500], 4, 2, 128),           # requests in front of the groups and behind them
+    ([0, 0, 2, 2, 4], [64, 320, 640, 70], [1, 1, 1, 1], [400, 321, 71, 200], 2, 2, 128),  # groups without requests
+    ([0, 4], [256], [0, 1, 0, 3], [256, 300, 900, 260], 6, 2, 64),           # a first request without tokens
+    ([0, 3], [1000], [1, 1, 1], [1100, 200, 64], 4, 1, 128),                 # more positions than two of the requests have: cut
+    ([0, 2], [50], [1, 1], [100, 90], 4, 4, 64),                             # less than a page
+    ([0, 40], [2000], [1] * 40, [2001 + 3 * i for i in range(40)], 8, 2, 128),
+    ([0, 3], [512], [30, 1, 70], [600, 513, 800], 4, 2, 128),                # prompts
+    ([0, 2], [320], [1, 1], [400, 333], 40, 2, 64),                          # 20 heads on one
+    ([0, 100], [192], [1] * 100, [193 + i for i in range(100)], 4, 1, 256),
+    ([0, 70], [3000], [1] * 70, [3001] * 70, 16, 2, 64),
+    ([0, 7, 80, 81], [640, 1300, 70], [1 + i % 3 for i in range(81)], [1310 + i for i in range(81)], 3, 1, 128),
+]
+
+
+@gpu
+@pytest.mark.parametrize("group,prefix,S,n,h_q,h_kv,d", SHARED)
+def test_attention_shared(group, prefix, S, n, h_q, h_kv, d):
+    rng = np.random.default_rng(21)
+    cache, table, K, V, P = _shared_batch(rng, group, prefix, S, n, h_kv, d)
+    T, behind = sum(S), 3
+    q = _normal(rng, T + behind, h_q * d)
+    req = _requests(S, n, table, rows=T + behind)
+    sizes = np.concatenate([[0], np.cumsum(S)])
+    most = max(max(int(sizes[group[i + 1]] - sizes[group[i]]) for i in range(len(prefix))), 1)
+    shared = B.SharedPrefixes(_i(group), _i(prefix), most, max(prefix))
+    got = _attend_shared(req, shared, q, h_q, cache, fill=7.0)
+    assert np.all(got[T:] == 7.0)
+    got, at = got.reshape(-1, h_q, d), 0
+    for b, s in enumerate(S):
+        _close(got[at:at + s], *q4.attention(q.reshape(-1, h_q, d)[at:at + s], K[b], V[b], P[b]))
+        at += s
+    # limits far above what is there
+    loose = B.Requests(req.token_start, req.context, _i(np.pad(table, ((0, 0), (0, 40)), constant_values=-1)), T + behind, max(S) + 5, max(n) + 2000)
+    got = _attend_shared(loose, B.SharedPrefixes(_i(group), _i(prefix), most + 100, max(prefix) + 3000), q, h_q, cache, fill=7.0).reshape(-1, h_q, d)
+    at = 0
+    for b, s in enumerate(S):
+        _close(got[at:at + s], *q4.attention(q.reshape(-1, h_q, d)[at:at + s], K[b], V[b], P[b]))
+        at += s
+
+
+@gpu
+def test_attention_shared_extremes():
+    """Pages that are missing, in the common part and behind it; a request that sees nothing; queries that are infinite or no numbers stay their own rows' matter; steps of 2 and more."""
+    rng = np.random.default_rng(22)
+    group, prefix, S, n, h_q, h_kv, d = [0, 3], [320], [1, 1, 1, 1], [400, 500, 330, 0], 4, 2, 64
+    k, v = _normal(rng, 400, h_kv, d), _normal(rng, 400, h_kv, d)
+    cache, table, K, V, P = _shared_batch(rng, group, prefix, S[:3], n[:3], h_kv, d)
+    table = np.pad(table, ((0, 1), (0, 0)), constant_values=-1)
+    table[:3, 2] = -1
+    table[1, 6] = 1 << 30
+    q = _normal(rng, 4, h_q * d)
+    req, shared = _requests(S, n, table), B.SharedPrefixes(_i(group), _i(prefix), 4, 320)
+    got = _attend_shared(req, shared, q, h_q, cache).reshape(-1, h_q, d)
+    for b in range(3):
+        there = np.ones(n[b], bool)
+        there[128:192] = False
+        if b == 1:
+            there[384:448] = False
+        _close(got[b:b + 1], *q4.attention(q.reshape(-1, h_q, d)[b:b + 1], K[b], V[b], P[b], there))
+    assert np.all(got[3] == 0)
+    bad = q.copy()
+    bad[0, :d] = np.nan
+    bad[2, d:2 * d] = np.inf
+    again = _attend_shared(req, shared, bad, h_q, cache).reshape(-1, h_q, d)
+    assert np.all(np.isnan(again[0, 0])) and np.all(np.isnan(again[2, 1]))
+    for b, h in ((0, 1), (0, 2), (0, 3), (1, 0), (1, 1), (1, 2), (1, 3), (2, 0), (2, 2), (2, 3)):
+        assert np.array_equal(again[b, h], got[b, h])
+    # values far apart: steps of 2 and more in some pages
+    S, n = [1, 1, 1], [400, 500, 330]
+    table, num = _pages(rng, n)
+    table[1, :5], table[2, :5] = table[0, :5], table[0, :5]
+    v = _normal(rng, sum(n), h_kv, d)
+    v[::7] *= np.float16(300)
+    k = _normal(rng, sum(n), h_kv, d)
+    for b, at in ((1, 400), (2, 900)):
+        k[at:at + 320], v[at:at + 320] = k[:320], v[:320]
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num, k, v)
+    got = _attend_shared(_requests(S, n, table), shared, q[:3], h_q, cache).reshape(-1, h_q, d)
+    for b in range(3):
+        _close(got[b:b + 1], *q4.attention(q.reshape(-1, h_q, d)[b:b + 1], K[b], V[b], P[b]))
+
+
+@gpu
+def test_attention_shared_arrays_that_break_the_rules_stay_inside():
+    rng = np.random.default_rng(23)
+    group, prefix, S, n, h_q, h_kv, d = [0, 3], [320], [1, 1, 1], [400, 500, 330], 4, 2, 64
+    cache, table, K, V, P = _shared_batch(rng, group, prefix, S, n, h_kv, d)
+    q = _normal(rng, 8, h_q * d)
+    for g, p in (([5, -3], [1 << 30]), ([0, 1 << 30], [-5]), ([2, 1], [320]), ([-9, 2], [2 ** 31 - 1])):
+        for start in ([0, 1, 2, 3], [0, 1 << 30, -4, 2], [3, 2, 1, 0]):
+            req = B.Requests(_i(start), _i([2 ** 31 - 1, -5, 330]), _i(table), 8, 2, 500)
+            out = torch.full((10, h_q * d), 9.0, dtype=torch.float16, device=DEV)
+            shared = B.SharedPrefixes(_i(g), _i(p), 3, 330)
+            ws = torch.zeros(B.qfc_attention_shared_q4_workspace_size(req, shared, h_q, cache) + 64, dtype=torch.uint8, device=DEV)
+            B.qfc_attention_shared_q4(_t(q), req, shared, h_q, cache, ws[:-64], out[:8])
+            assert bool((out[8:] == 9.0).all()) and not ws[-64:].any()
+
+
+# ---------------------------------------------------------------- bounds and selection
+def _bounds_of(K, n, h_kv, d):
+    pages = (n + 63) // 64
+    codes, steps = np.zeros((pages, h_kv, 2, d), np.int8), np.zeros((pages, h_kv), np.float32)
+    for p in range(pages):
+        for kv in range(h_kv):
+            codes[p, kv], steps[p, kv] = ref.bounds(K[64 * p:min(n, 64 * p + 64), kv])
+    return codes, steps
+
+
+@gpu
+@pytest.mark.parametrize("S,n,h_kv,d", [([1], [1], 1, 64), ([1, 1], [64, 65], 2, 128), ([3, 0, 1], [66, 40, 500], 3, 256), ([130, 1, 64], [130, 200, 128], 2, 64), ([66], [129], 1, 128), ([2], [65], 8, 128),
+                                        ([300, 7], [1000, 7], 4, 256)])
+def test_bound_pages(S, n, h_kv, d):
+    rng = np.random.default_rng(31)
+    table, num = _pages(rng, n)
+    k = _normal(rng, sum(n), h_kv, d)
+    k[0] = 0
+    k[-1] *= np.float16(100)
+    if sum(n) > 300:
+        k[100:200] *= np.float16(2.0 ** -12)
+    cache, K, _, _ = _filled(rng, n, h_kv, d, table, num, k)
+    bounds = B.PageBounds(cache)
+    bounds.codes.fill_(99), bounds.steps.fill_(-5.0)
+    B.qfc_bound_pages_q4(_requests(S, n, table), cache, bounds)
+    codes, steps = bounds.codes.cpu().numpy(), bounds.steps.cpu().numpy()
+    touched = set()
+    for b in range(len(S)):
+        want = _bounds_of(K[b], n[b], h_kv, d)
+        for p in range((n[b] - S[b]) // 64, (n[b] - 1) // 64 + 1) if S[b] else ():
+            page = table[b, p]
+            touched.add(int(page))
+            assert np.array_equal(codes[page], want[0][p]) and np.array_equal(steps[page], want[1][p]), (b, p)
+    for page in set(range(num)) - touched:
+        assert np.all(codes[page] == 99) and np.all(steps[page] == -5.0)
+
+
+SELECT = [  # S, n, h_q, h_kv, d, first, last, count
+    ([1], [1], 1, 1, 64, 0, 1, 1),
+    ([1], [640], 4, 1, 128, 1, 1, 4),
+    ([1, 1], [641, 100], 8, 2, 64, 0, 0, 3),
+    ([3, 1], [400, 1500], 2, 2, 256, 1, 2, 5),
+    ([1], [3000], 40, 2, 64, 2, 3, 10),      # 20 heads on one
+    ([70, 0, 2], [900, 5, 70], 3, 1, 128, 0, 1, 7),
+    ([1], [20000], 4, 4, 64, 1, 1, 100),
+    ([1], [40000], 2, 1, 64, 0, 1, 600),     # more pages than a workgroup of few threads takes
+    ([1, 1], [1000, 2000], 4, 2, 64, 5, 4, 9),  # nothing left to choose
+    ([2], [200], 4, 2, 128, 0, 1, 50),       # fewer pages than asked for
+]
+
+
+def _select(req, q, h_q, cache, bounds, first, last, count, T):
+    selected = torch.full((T, cache.h_kv, count), 12345, dtype=torch.int32, device=DEV)
+    B.qfc_select_pages_q4(_t(q), req, h_q, cache, bounds, first, last, selected, _space(B.qfc_select_pages_q4_workspace_size(req, h_q, cache)))
+    return selected
+
+
+@gpu
+@pytest.mark.parametrize("S,n,h_q,h_kv,d,first,last,count", SELECT)
+@pytest.mark.parametrize("alike", [False, True])
+def test_select_pages(S, n, h_q, h_kv, d, first, last, count, alike):
+    """alike: pages that repeat, so that many scores are equal."""
+    rng = np.random.default_rng(41)
+    table, num = _pages(rng, n)
+    k = _normal(rng, sum(n), h_kv, d)
+    if alike:
+        k = np.tile(_normal(rng, 192, h_kv, d), (sum(n) // 192 + 1, 1, 1))[:sum(n)]
+    cache, K, _, _ = _filled(rng, n, h_kv, d, table, num, k)
+    bounds = B.PageBounds(cache)
+    B.qfc_bound_pages_q4(_requests(n, n, table), cache, bounds)
+    if n[0] > 700:
+        table[0, 3] = -1  # an entry without a page
+    T = sum(S) + 2
+    q = _normal(rng, T, h_q * d)
+    q[0, :d] = 0
+    req = _requests(S, n, table, rows=T)
+    got = _select(req, q, h_q, cache, bounds, first, last, count, T).cpu().numpy()
+    # the same with scores in the workspace: limits above what fits the LDS
+    wide = np.full((len(n), 33000), -1, np.int32)
+    wide[:, :table.shape[1]] = table
+    far = B.Requests(req.token_start, req.context, _i(wide), T, max(S), 33000 * 64)
+    assert np.array_equal(_select(far, q, h_q, cache, bounds, first, last, count, T).cpu().numpy(), got)
+    at, g = 0, h_q // h_kv
+    for b, s in enumerate(S):
+        codes, steps = _bounds_of(K[b], n[b], h_kv, d)
+        there = table[b, :len(steps)] >= 0
+        for i in range(s):
+            sees = (n[b] - s + i) // 64 + 1
+            for kv in range(h_kv):
+                rows = q[at + i].reshape(h_q, d)[kv * g:(kv + 1) * g]
+                want = ref.select(ref.scores(rows, codes[:, kv], steps[:, kv], there), sees, first, last, count)
+                assert np.array_equal(got[at + i, kv], want), (b, i, kv)
+        at += s
+    assert np.all(got[at:] == 12345)
+
+
+@gpu
+def test_a_page_scores_at_least_what_its_keys_do():
+    """What the bounds are for: up to the rounding of the query (half a code of each of d components, against bounds of 127 steps) no key scores above its page."""
+    rng = np.random.default_rng(42)
+    n, h_kv, d = [1500], 2, 128
+    table, num = _pages(rng, n)
+    cache, K, _, _ = _filled(rng, n, h_kv, d, table, num)
+    codes, steps = _bounds_of(K[0], n[0], h_kv, d)
+    q = _normal(rng, 1, h_kv * d).reshape(h_kv, d)
+    for kv in range(h_kv):
+        score = ref.scores(q[kv:kv + 1], codes[:, kv], steps[:, kv], np.ones(len(steps), bool))
+        best = np.array([(K[0][64 * p:64 * p + 64, kv] @ q[kv].astype(np.float64)).max() for p in range(len(steps))])
+        slack = 0.5 * np.abs(q[kv].astype(np.float64)).max() / 127 * d * 127 * steps[:, kv]
+        assert np.all(best <= score + slack)
+
+
+# ---------------------------------------------------------------- attention over selected pages
+def _attend_selected(req, q, h_q, cache, selected, fill=0.0):
+    out = torch.full((q.shape[0], h_q * cache.d_head), fill, dtype=torch.float16, device=DEV)
+    n = B.qfc_attention_selected_q4_workspace_size(req, h_q, cache, selected.shape[2])
+    ws = torch.full((n + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    B.qfc_attention_selected_q4(_t(q), req, h_q, cache, selected, ws[:n], out)
+    torch.cuda.synchronize()
+    assert bool((ws[n:] == 0xFF).all())
+    return out.cpu().numpy().astype(np.float64)
+
+
+SOME = [  # S, n, h_q, h_kv, d, count
+    ([1], [1], 1, 1, 64, 1),
+    ([1], [640], 4, 1, 128, 3),
+    ([1, 1], [641, 100], 8, 2, 64, 5),
+    ([3, 1], [400, 1500], 2, 2, 256, 6),
+    ([1], [3000], 40, 2, 64, 17),
+    ([70, 0, 2], [900, 5, 70], 3, 1, 128, 7),
+    ([1], [9000], 32, 8, 128, 70),
+    ([1] * 40, [300 + 10 * i for i in range(40)], 8, 4, 256, 4),
+    ([130], [600], 4, 2, 64, 8),
+]
+
+
+@gpu
+@pytest.mark.parametrize("S,n,h_q,h_kv,d,count", SOME)
+def test_attention_selected(S, n, h_q, h_kv, d, count):
+    rng = np.random.default_rng(51)
+    table, num = _pages(rng, n)
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num)
+    T, behind, g = sum(S), 2, h_q // h_kv
+    q = _normal(rng, T + behind, h_q * d)
+    req = _requests(S, n, table, rows=T + behind)
+    selected = np.full((T + behind, h_kv, count), -1, np.int32)
+    at = 0
+    for b, s in enumerate(S):
+        for i in range(s):
+            sees = (n[b] - s + i) // 64 + 1
+            for kv in range(h_kv):
+                pick = rng.permutation(sees)[:rng.integers(0, min(sees, count) + 1)]
+                selected[at + i, kv, rng.permutation(count)[:len(pick)]] = pick  # any order, -1 in between
+                if rng.random() < 0.2 and len(pick) < count:
+                    selected[at + i, kv, np.flatnonzero(selected[at + i, kv] < 0)[0]] = rng.choice([sees + 1, 2 ** 31 - 1, -2 ** 31])  # pages that it does not see
+        at += s
+    got = _attend_selected(req, q, h_q, cache, _i(selected), fill=5.0)
+    assert np.all(got[T:] == 5.0)
+    got, at = got.reshape(-1, h_q, d), 0
+    for b, s in enumerate(S):
+        for i in range(s):
+            m = n[b] - s + i + 1
+            for kv in range(h_kv):
+                there = np.isin(np.arange(m) // 64, selected[at + i, kv])
+                heads = slice(kv * g, (kv + 1) * g)
+                rows = q[at + i].reshape(1, h_q, d)[:, heads]
+                _close(got[at + i:at + i + 1, heads], *q4.attention(rows, K[b][:m, kv:kv + 1], V[b][:m, kv:kv + 1], P[b][:m, kv:kv + 1], there))
+        at += s
+
+
+@gpu
+def test_a_page_listed_twice_counts_twice():
+    rng = np.random.default_rng(52)
+    n, h_q, h_kv, d = [400], 2, 1, 64
+    table, num = _pages(rng, n)
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num)
+    q = _normal(rng, 1, h_q * d)
+    got = _attend_selected(_requests([1], n, table), q, h_q, cache, _i([[[2, 0, 2, -1]]])).reshape(1, h_q, d)
+    rows = np.concatenate([np.arange(128, 192), np.arange(64), np.arange(128, 192)])
+    _close(got, *q4.attention(q.reshape(1, h_q, d), K[0][rows], V[0][rows], P[0][rows]))
+
+
+# ---------------------------------------------------------------- runs of them
+@gpu
+def test_a_server_that_picks_pages_step_by_step():
+    """Append, bound, select, attend, for prompts and then single tokens, pages taken as they are needed; with all pages selected the result is attention's over the cache."""
+    rng = np.random.default_rng(61)
+    h_q, h_kv, d, width, first, last, count = 8, 2, 64, 12, 1, 1, 5
+    S, n = np.array([200, 3, 330]), np.array([200, 3, 330])
+    cache = B.PagedCache(3 * width + 5, h_kv, d)
+    cache.pages.fill_(0xFF)
+    bounds, refs, table = B.PageBounds(cache), _i(np.zeros(cache.num_pages)), _i(np.full((3, width), -1))
+    space = _space(B.qfc_pages_workspace_size(cache, 3))
+    keys, values = [np.zeros((0, h_kv, d), np.float16) for _ in n], [np.zeros((0, h_kv, d), np.float16) for _ in n]
+    for step in range(6):
+        B.qfc_take_pages(cache, refs, table, _i(n), space)
+        T = int(S.sum())
+        qkv = _normal(rng, T, (h_q + 2 * h_kv) * d)
+        req = B.Requests(_i(np.concatenate([[0], np.cumsum(S)])), _i(n), table, T, int(S.max()), int(n.max()))
+        q = torch.empty((T, h_q * d), dtype=torch.float16, device=DEV)
+        B.qfc_append_q4(_t(qkv), req, h_q, None, None, cache, q)
+        B.qfc_bound_pages_q4(req, cache, bounds)
+        selected = _select(req, q.cpu().numpy(), h_q, cache, bounds, first, last, count, T)
+        out = _attend_selected(req, q.cpu().numpy(), h_q, cache, selected).reshape(T, h_q, d)
+        whole = _attend_selected(req, q.cpu().numpy(), h_q, cache, _select(req, q.cpu().numpy(), h_q, cache, bounds, 0, 1, width, T)).reshape(T, h_q, d)
+        x, at, g, picked = qkv.reshape(T, -1, d), 0, h_q // h_kv, selected.cpu().numpy()
+        for b in range(3):
+            keys[b] = np.concatenate([keys[b], x[at:at + S[b], h_q:h_q + h_kv]])
+            values[b] = np.concatenate([values[b], x[at:at + S[b], h_q + h_kv:]])
+            K, (V, P) = q4.q4_values(*q4.q4(keys[b]))[0], q4.q4_values(*q4.q4(values[b]))
+            rows = x[at:at + S[b], :h_q]
+            _close(whole[at:at + S[b]], *q4.attention(rows, K, V, P))
+            codes, steps = _bounds_of(K, n[b], h_kv, d)
+            for i in range(0, S[b], 1 if step else 37):
+                m = n[b] - S[b] + i + 1
+                for kv in range(h_kv):
+                    # (a page of a prompt is bounded with all its positions, later ones of the same prompt among them)
+                    want = ref.select(ref.scores(rows[i, kv * g:(kv + 1) * g], codes[:, kv], steps[:, kv], np.ones(len(steps), bool)), (m - 1) // 64 + 1, first, last, count)
+                    assert np.array_equal(picked[at + i, kv], want)
+                    there = np.isin(np.arange(m) // 64, want)
+                    _close(out[at + i:at + i + 1, kv * g:(kv + 1) * g], *q4.attention(rows[i:i + 1, kv * g:(kv + 1) * g], K[:m, kv:kv + 1], V[:m, kv:kv + 1], P[:m, kv:kv + 1], there))
+            at += S[b]
+        S = np.array([1, 1 + step % 2, 1])
+        n = n + S
+
+
+@gpu
+def test_a_search_behind_a_prompt_shares_its_pages():
+    """One prompt, forked into continuations that grow apart, attention behind the common pages; then the pool is compacted and the same call gives the same bits."""
+    rng = np.random.default_rng(62)
+    h_q, h_kv, d, width, n0, kids = 8, 2, 128, 8, 300, 6
+    cache = B.PagedCache(60, h_kv, d)
+    cache.pages.fill_(0xFF)
+    refs, root, space = _i(np.zeros(60)), _i(np.full((1, width), -1)), _space(B.qfc_pages_workspace_size(cache, kids))
+    holes = _i(np.full((1, 30), -1))
+    B.qfc_take_pages(cache, refs, holes, _i([30 * 64]), space)  # pages that are let go below
+    B.qfc_take_pages(cache, refs, root, _i([n0]), space)
+
+    def append(S, n, table):
+        T = sum(S)
+        qkv = _normal(rng, T, (h_q + 2 * h_kv) * d)
+        req = B.Requests(_i(np.concatenate([[0], np.cumsum(S)])), _i(n), table, T, max(S), max(n))
+        q = torch.empty((T, h_q * d), dtype=torch.float16, device=DEV)
+        B.qfc_append_q4(_t(qkv), req, h_q, None, None, cache, q)
+        return req, q, qkv.reshape(T, -1, d)
+
+    _, _, x = append([n0], [n0], root)
+    keys, values = [x[:, h_q:h_q + h_kv]] * kids, [x[:, h_q + h_kv:]] * kids
+    table, n = _i(np.zeros((kids, width))), [n0] * kids
+    B.qfc_fork_pages(cache, refs, root, _i([0] * kids), _i(n), table, space)
+    B.qfc_free_pages(cache, refs, root)
+    assert int(refs[30:34].min()) == kids and int(refs[34]) == 0  # four whole pages are shared, the fifth was copied
+    shared = B.SharedPrefixes(_i([0, kids]), _i([n0]), 3 * kids, n0)
+    for step in range(5):
+        S = [1 + (step * b) % 3 for b in range(kids)]
+        n = [a + b for a, b in zip(n, S)]
+        B.qfc_take_pages(cache, refs, table, _i(n), space)
+        req, q, x = append(S, n, table)
+        got, at = _attend_shared(req, shared, q.cpu().numpy(), h_q, cache).reshape(-1, h_q, d), 0
+        for b in range(kids):
+            keys[b], values[b] = np.concatenate([keys[b], x[at:at + S[b], h_q:h_q + h_kv]]), np.concatenate([values[b], x[at:at + S[b], h_q + h_kv:]])
+            K, (V, P) = q4.q4_values(*q4.q4(keys[b]))[0], q4.q4_values(*q4.q4(values[b]))
+            _close(got[at:at + S[b]], *q4.attention(x[at:at + S[b], :h_q], K, V, P))
+            at += S[b]
+    B.qfc_free_pages(cache, refs, holes)
+    before = table.clone()
+    used = _i([0])
+    B.qfc_compact_pages(cache, refs, table, space, used)
+    assert int(used) == int((refs > 0).sum()) and not torch.equal(before, table) and int(table.max()) < int(used)
+    assert np.array_equal(_attend_shared(req, shared, q.cpu().numpy(), h_q, cache).reshape(-1, h_q, d), got)
+
+
+@gpu
+def test_captured_steps_follow_the_arrays():
+    """Attention behind common pages, bounds, selection and attention over it in one graph; lengths, tables and groups change between replays."""
+    rng = np.random.default_rng(63)
+    h_q, h_kv, d, batch, width, count = 8, 2, 64, 4, 20, 4
+    lengths = [[700, 650, 1000, 64], [1200, 1, 300, 900], [80, 1279, 500, 640]]
+    cache = B.PagedCache(batch * width, h_kv, d)
+    table = np.arange(batch * width, dtype=np.int32).reshape(batch, width)
+    table[:2, :6] = table[0, :6]
+    every = [width * 64] * batch
+    k, v = _normal(rng, width * 64 * batch, h_kv, d), _normal(rng, width * 64 * batch, h_kv, d)
+    k[width * 64:width * 64 + 384], v[width * 64:width * 64 + 384] = k[:384], v[:384]
+    _, K, V, P = _filled(rng, every, h_kv, d, table, batch * width, k, v, cache=cache)
+    context, pages, start, group, prefix = _i(lengths[0]), _i(table), _i(range(batch + 1)), _i([0, 2]), _i([384])
+    req, shared, bounds = B.Requests(start, context, pages, batch, 1, width * 64), B.SharedPrefixes(group, prefix, batch, width * 64), B.PageBounds(cache)
+    B.qfc_bound_pages_q4(_requests(every, every, table), cache, bounds)
+    q = torch.empty((batch, h_q * d), dtype=torch.float16, device=DEV)
+    q.copy_(_t(_normal(rng, batch, h_q * d)))
+    outs = [torch.zeros_like(q) for _ in range(2)]
+    selected = torch.zeros((batch, h_kv, count), dtype=torch.int32, device=DEV)
+    ws = [_space(B.qfc_attention_shared_q4_workspace_size(req, shared, h_q, cache)), _space(B.qfc_select_pages_q4_workspace_size(req, h_q, cache)),
+          _space(B.qfc_attention_selected_q4_workspace_size(req, h_q, cache, count))]
+
+    def step():
+        B.qfc_attention_shared_q4(q, req, shared, h_q, cache, ws[0], outs[0])
+        B.qfc_bound_pages_q4(req, cache, bounds)
+        B.qfc_select_pages_q4(q, req, h_q, cache, bounds, 0, 1, selected, ws[1])
+        B.qfc_attention_selected_q4(q, req, h_q, cache, selected, ws[2], outs[1])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    torch.cuda.synchronize()
+    for n, (g, p) in zip(lengths * 2, [([0, 2], [384]), ([1, 2], [300]), ([0, 2], [64]), ([0, 0], [0]), ([0, 4], [0]), ([0, 2], [2000])]):
+        context.copy_(_i(n)), group.copy_(_i(g)), prefix.copy_(_i(p))
+        q.copy_(_t(_normal(rng, batch, h_q * d)))
+        for o in outs:
+            o.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [o.clone() for o in outs]
+        rows = q.cpu().numpy().reshape(batch, h_q, d)
+        if p[0] <= 384:
+            for b in range(batch):
+                _close(got[0][b:b + 1].cpu().numpy().astype(np.float64).reshape(1, h_q, d), *q4.attention(rows[b:b + 1], K[b][:n[b]], V[b][:n[b]], P[b][:n[b]]))
+        picked = selected.clone()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], outs[0]) and torch.equal(got[1], outs[1]) and torch.equal(picked, selected)
+
+
+@gpu
+def test_two_streams_with_workspaces_of_their_own():
+    rng = np.random.default_rng(64)
+    group, prefix, S, n, h_q, h_kv, d = [0, 20], [640], [1] * 20, [641 + 9 * i for i in range(20)], 8, 2, 128
+    cache, table, K, V, P = _shared_batch(rng, group, prefix, S, n, h_kv, d)
+    req, shared = _requests(S, n, table), B.SharedPrefixes(_i(group), _i(prefix), 20, 640)
+    qs = [_t(_normal(rng, 20, h_q * d)) for _ in range(2)]
+    picks = [_i(np.tile(np.arange(i, i + 6), (20, h_kv, 1))) for i in range(2)]
+    want = [(torch.empty_like(q), torch.empty_like(q)) for q in qs]
+    outs = [[(torch.empty_like(q), torch.empty_like(q)) for q in qs] for _ in range(5)]
+    sizes = B.qfc_attention_shared_q4_workspace_size(req, shared, h_q, cache), B.qfc_attention_selected_q4_workspace_size(req, h_q, cache, 6)
+    ws = [[_space(x) for x in sizes] for _ in range(2)]
+
+    def both(i, out):
+        B.qfc_attention_shared_q4(qs[i], req, shared, h_q, cache, ws[i][0], out[0])
+        B.qfc_attention_selected_q4(qs[i], req, h_q, cache, picks[i], ws[i][1], out[1])
+
+    for i in range(2):
+        both(i, want[i])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for out in outs:
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                both(i, out[i])
+    torch.cuda.synchronize()
+    for out in outs:
+        for i in range(2):
+            assert torch.equal(out[i][0], want[i][0]) and torch.equal(out[i][1], want[i][1])
