@@ -640,7 +640,7 @@ qfc_status_t qfc_attention_shared_q4(const void *q_f16, const qfc_requests_t *re
     if (p.prefix_blocks > INT32_MAX || p.blocks > INT32_MAX) return QFC_ERR_UNSUPPORTED;
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_attention_shared_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, shared->group_start, shared->positions, shared->groups,
-                                                 shared->max_group_tokens, shared->max_positions, p, workspace, out_f16, cus, static_cast<hipStream_t>(stream)));
+                                                 shared->max_group_tokens, shared->max_positions, p, workspace, out_f16, static_cast<hipStream_t>(stream)));
 }
 
 static qfc_status_t check_bounds(const qfc_page_bounds_t *b) {
@@ -698,10 +698,10 @@ qfc_status_t qfc_attention_selected_q4(const void *q_f16, const qfc_requests_t *
     if (!q_f16 || !workspace || !out_f16 || !selected) return QFC_ERR_INVALID_ARG;
     if (!aligned16(q_f16) || !aligned16(workspace) || !aligned16(out_f16) || !aligned(selected, 4)) return QFC_ERR_ALIGNMENT;
     const int cus = device_cus();
-    const AttnPartsPlan p = plan_attention_selected_q4(requests->tokens, h_q, cache->h_kv, cache->d_head, count, cus);
+    const SelectedPlan p = plan_attention_selected_q4(requests->tokens, h_q, cache->h_kv, cache->d_head, count, cus);
     if (workspace_bytes < p.bytes) return QFC_ERR_BUFFER_TOO_SMALL;
     if (cus < 1) return QFC_ERR_HIP;
-    return hip_status(launch_attention_selected_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, selected, count, p, workspace, out_f16, cus,
+    return hip_status(launch_attention_selected_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, selected, count, p, workspace, out_f16,
                                                    static_cast<hipStream_t>(stream)));
 }
 

@@ -14,12 +14,10 @@ struct PartsArgs {
     _Float16 *out;
     const char *pages;
     Requests req;
-    const int *selected;  // [tokens, h_kv, count], or null
-    int count;
     const int *group_start, *prefix;  // of groups with common pages
     int groups, group_tokens, longest;
     float *ws_o, *ws_ml;  // [slots][tokens * h_q][D] partial outputs, [..][2] (maximum, sum; 0: nothing was seen, no output)
-    int h_q, h_kv, g, head_blocks;
+    int h_q, h_kv, g;
     int prefix_parts, parts;  // slots: of common pages, and behind them of the others
     long prefix_items, items;  // of workgroups; items: all of them
     float scale;
@@ -68,136 +66,255 @@ __device__ __forceinline__ Group group_of(const PartsArgs &a, int i, int lane) {
     return Group{__builtin_amdgcn_readfirstlane(max(lead, 0)), __builtin_amdgcn_readfirstlane(lead < 0 ? 0 : least / kPage)};
 }
 
-// A workgroup per part: its four wavefronts have a quarter of the pages each and meet in LDS.
-template <int D, bool SELECTED>
-__global__ __launch_bounds__(256, kWgs) void attn_q4_parts_kernel(PartsArgs a) {
-    constexpr int STRIDE = D + 4;  // of a row of partial outputs in LDS (banks)
-    static_assert(16 * STRIDE * 4 <= 2 * Place<D>::PART, "a wavefront's partial outputs take its pages' places");
-    extern __shared__ float lds[];
-    __shared__ float sums[4][16][2];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long all_rows = (long)a.req.tokens * a.h_q;
-    const bool direct = a.prefix_parts + a.parts == 1;
-    Rows<D> rows(lds, wave, lane);
-    const int m = rows.m, r = rows.r;
-    for (long item = blockIdx.x; item < a.items; item += gridDim.x) {
-        // ---- which rows, which pages: from .. to - 1 of request b (of its list, where SELECTED)
-        int b, slot, token = 0, head = 0, lim, n, from, to;
-        bool real;
-        const int *list = nullptr;
-        const bool common = !SELECTED && item < a.prefix_items;
-        const long x = SELECTED || common ? item : item - a.prefix_items;
-        const int parts = common ? a.prefix_parts : a.parts, kv = (int)(x % a.h_kv), part = (int)(x / a.h_kv % parts);
-        const long block = x / a.h_kv / parts;
-        if constexpr (SELECTED) {
-            const int heads0 = (int)(block % a.head_blocks) * 16;
-            token = (int)(block / a.head_blocks);
-            b = __builtin_amdgcn_readfirstlane(request_of<1>(a.req, token, 0, lane));
-            if (b >= a.req.batch) return;  // (so are all later tokens)
-            const Span s = span_of(a.req, b);
-            if (token < s.first || token - s.first >= s.count) continue;
-            n = s.positions, lim = n - s.count + token - s.first + 1;
-            real = heads0 + m < a.g, head = kv * a.g + min(heads0 + m, a.g - 1);
-            const int per = (a.count + parts - 1) / parts;
-            from = min(part * per, a.count), to = min(from + per, a.count), slot = part;
-            list = a.selected + ((size_t)token * a.h_kv + kv) * a.count;
-        } else {
-            int first, row, rows_all, pages;
-            if (common) {
-                const Found f = find((int)block, a.groups, lane, [&](int i) __attribute__((always_inline)) { return (int)(((long)tokens_of_group(a, i) * a.g + 15) / 16); });
-                if (f.run < 0) {  // (on to the items behind the groups')
-                    item += (a.prefix_items - 1 - item) / gridDim.x * gridDim.x;
-                    continue;
-                }
-                const Group group = group_of(a, f.run, lane);
-                b = group.lead, pages = group.pages;
-                first = token_at(a, group_end(a, f.run)), rows_all = tokens_of_group(a, f.run) * a.g, row = f.place * 16 + m;
-                n = pages * kPage, lim = n, from = 0;
-            } else {
-                Found f = {(int)block, 0};
-                if (a.req.max_tokens * a.g > 16)
-                    f = find((int)block, a.req.batch, lane, [&](int i) __attribute__((always_inline)) { return (span_of(a.req, i).count * a.g + 15) / 16; });
-                if (f.run < 0 || f.run >= a.req.batch) return;
-                b = f.run;
-                const Span s = span_of(a.req, b);
-                first = s.first, rows_all = s.count * a.g, row = f.place * 16 + m;
-                n = s.positions, lim = n - s.count + row / a.g + 1;
-                // its group, and the pages that are done with that
-                int before = 0;
-                for (int c = 0; c <= a.groups; c += 64) before += __popcll(__ballot(c + lane <= a.groups && group_end(a, min(c + lane, a.groups)) <= b));
-                from = before > 0 && before <= a.groups ? group_of(a, before - 1, lane).pages : 0;
-                // (the last row's positions are the most)
-                const int sees = max(0, n - s.count + min(f.place * 16 + 15, rows_all - 1) / a.g + 1);
-                pages = (sees + kPage - 1) / kPage;
-            }
-            if (rows_all <= 0) continue;
-            real = row < rows_all, row = min(row, rows_all - 1);
-            token = first + row / a.g, head = kv * a.g + row % a.g;
-            const int per = max(4, (max(pages - from, 0) + parts - 1) / parts);
-            from = min(from + part * per, max(pages, from)), to = min(from + per, max(pages, from)), slot = part + (common ? 0 : a.prefix_parts);
-        }
-        const size_t at = (size_t)token * a.h_q + head, out_row = (size_t)slot * all_rows + at;
-        if (from >= to && !direct) {
-            if (wave == 0 && r == 0 && real) a.ws_ml[out_row * 2 + 1] = 0.0f;
-            continue;
-        }
-        // ---- this wavefront's quarter
-        const int share = (to - from + 3) / 4, begin = min(from + wave * share, to), count = __builtin_amdgcn_readfirstlane(min(begin + share, to) - begin);
-        int place = -1;  // of the page in its request, a page per lane
-        auto numbers = [&](int i) __attribute__((always_inline)) {
-            if constexpr (SELECTED) {
-                place = i + lane < count ? list[begin + i + lane] : -1;
-                return place >= 0 && place < (a.req.max_context + kPage - 1) / kPage ? page_of(a.req, b, place * kPage) : -1;
-            } else {
-                return i + lane < count ? page_of(a.req, b, (begin + i + lane) * kPage) : -1;
-            }
-        };
-        auto start_of = [&](int i) __attribute__((always_inline)) {
-            if constexpr (SELECTED) return __builtin_amdgcn_readlane(place, i & 63) * kPage;
-            return (begin + i) * kPage;
-        };
-        const int ahead = numbers(0);
-        rows.load(a.q + at * D, real, a.scale);
-        rows.walk(count, real ? lim : 0, n, a.pages, a.h_kv, kv, ahead, numbers, start_of);
-        // ---- the four meet
-        float *const mine = lds + wave * (2 * Place<D>::PART / 4) + m * STRIDE;
+// The four wavefronts of a workgroup have a quarter each of the same rows' pages and meet in LDS, in the places of their pages.
+template <int D>
+struct Four {
+    static constexpr int STRIDE = D + 4;  // of a row (banks)
+    static constexpr int WAVE = 2 * Place<D>::PART / 4;
+    static_assert(16 * (STRIDE + 2) <= WAVE, "a wavefront's partial outputs, maxima and sums take its pages' places");
+    float *const lds;  // (nothing beside it: with heads of 256 values two workgroups take a compute unit's LDS to the last byte)
+    __device__ __forceinline__ float *sums_of(int wave, int row) const { return lds + wave * WAVE + 16 * STRIDE + 2 * row; }
+    // Each thread gets 4 columns of row threadIdx.x / 16 from column 4 (threadIdx.x % 16) on, and every 64th behind them: put(row, column, output, 1 / sum), then put_sum(row, maximum, sum).
+    // What a lane knows of row m the threads of row threadIdx.x / 16 ask for: theirs(x).
+    template <class T>
+    __device__ static __forceinline__ T theirs(T x) {
+        return __shfl(x, (int)(threadIdx.x >> 4), 64);
+    }
+    template <class Put, class PutSum>
+    __device__ __forceinline__ void meet(const Rows<D> &rows, int wave, bool wanted, const Put &put, const PutSum &put_sum) const {
+        float *const mine = lds + wave * WAVE + rows.m * STRIDE;
         rows.columns([&](int d, const v4f &o) __attribute__((always_inline)) { *reinterpret_cast<v4f *>(mine + d) = o; });
         const float own_sum = rows.sum();
-        if (r == 0) sums[wave][m][0] = rows.run_max, sums[wave][m][1] = own_sum;
+        if (rows.r == 0) sums_of(wave, rows.m)[0] = rows.run_max, sums_of(wave, rows.m)[1] = own_sum;
         __syncthreads();
-        // thread: row threadIdx.x / 16, columns 4 (threadIdx.x % 16) and every 64th behind them.  (What a lane knows of row m the lanes of row threadIdx.x / 16 ask for.)
-        const int tr = threadIdx.x >> 4, from_lane = tr;
-        const size_t their_at = __shfl((unsigned long long)at, from_lane, 64);
-        const bool their_real = __shfl((int)real, from_lane, 64) != 0;
-        if (their_real) {
-            float f[4], top = sums[0][tr][0], l = 0.0f;
+        if (wanted) {
+            const int row = threadIdx.x >> 4;
+            float f[4], top = sums_of(0, row)[0], l = 0.0f;
 #pragma unroll
-            for (int w = 1; w < 4; ++w) top = fmaxf(top, sums[w][tr][0]);
+            for (int w = 1; w < 4; ++w) top = fmaxf(top, sums_of(w, row)[0]);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                f[w] = __builtin_amdgcn_exp2f(sums[w][tr][0] - top);
-                l = fmaf(f[w], sums[w][tr][1], l);
+                f[w] = __builtin_amdgcn_exp2f(sums_of(w, row)[0] - top);
+                l = fmaf(f[w], sums_of(w, row)[1], l);
             }
             const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-            const size_t to_row = (size_t)slot * all_rows + their_at;
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) {
                 const int d = 64 * c + 4 * (threadIdx.x & 15);
                 v4f o = {};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const v4f x4 = *reinterpret_cast<const v4f *>(lds + w * (2 * Place<D>::PART / 4) + tr * STRIDE + d);
+                    const v4f x4 = *reinterpret_cast<const v4f *>(lds + w * WAVE + row * STRIDE + d);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[i] = fmaf(f[w], x4[i], o[i]);
                 }
-                if (direct)
-                    *reinterpret_cast<h4 *>(a.out + their_at * D + d) = h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
-                else
-                    *reinterpret_cast<v4f *>(a.ws_o + to_row * D + d) = o;
+                put(d, o, inv);
             }
-            if (!direct && (threadIdx.x & 15) == 0) a.ws_ml[to_row * 2] = top, a.ws_ml[to_row * 2 + 1] = l;
+            if ((threadIdx.x & 15) == 0) put_sum(top, l);
         }
         __syncthreads();
+    }
+};
+__device__ __forceinline__ h4 rounded(const v4f &o, float by) { return h4{(_Float16)(o[0] * by), (_Float16)(o[1] * by), (_Float16)(o[2] * by), (_Float16)(o[3] * by)}; }
+
+// Sums over parts, eight on their way at a time: part i is at place(i), its maximum and sum at ml, its columns at o
+template <class Place>
+__device__ __forceinline__ v4f joined(const float *ml, const float *o_at, int stride, int parts, const Place &place, float &inv) {
+    float top = kNothingYet, l = 0.0f;
+    v4f o = {};
+    for (int s0 = 0; s0 < parts; s0 += 8) {
+        float ms[8], ls[8];
+        v4f os[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const size_t at = place(min(s0 + i, parts - 1));
+            ms[i] = ml[at * 2], ls[i] = ml[at * 2 + 1];
+            os[i] = *reinterpret_cast<const v4f *>(o_at + at * stride);
+        }
+        float new_top = top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (s0 + i >= parts) ls[i] = 0.0f;
+            new_top = ls[i] != 0.0f ? fmaxf(new_top, ms[i]) : new_top;
+        }
+        const float corr = __builtin_amdgcn_exp2f(top - new_top);
+        top = new_top, l *= corr;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= corr;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (ls[i] == 0.0f) continue;  // (nothing was seen: what stands there is not defined)
+            const float f = __builtin_amdgcn_exp2f(ms[i] - top);
+            l = fmaf(f, ls[i], l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, os[i][e], o[e]);
+        }
+    }
+    inv = l != 0.0f ? 1.0f / l : 0.0f;
+    return o;
+}
+
+// ---- selected pages.  Units of a token, a KV head and 16 of its query heads, one behind the other, each with the `count` places of its list; every workgroup has `share` places in a row, whatever
+// units they are of.  Of a unit that several have a part of, each leaves partial results: two at most per workgroup, of the unit that its share begins inside of (or with), and of the one
+// that it ends inside of.
+struct SelectedArgs {
+    const _Float16 *q;
+    _Float16 *out;
+    const char *pages;
+    Requests req;
+    const int *selected;  // [tokens, h_kv, count]
+    float *ws_o, *ws_ml;  // [workgroups][2][16][D], [..][2]
+    int h_q, h_kv, g, head_blocks, count;
+    long share, places;
+    float scale;
+};
+struct Unit {
+    long begin, end;
+    int token, kv, head0;
+    Span span;
+    int b;
+    bool real;  // the token is a request's
+};
+__device__ __forceinline__ Unit unit_of(const SelectedArgs &a, long place, int lane) {
+    Unit u;
+    const long unit = place / a.count, block = unit / a.h_kv;
+    u.begin = unit * a.count, u.end = u.begin + a.count;
+    u.kv = (int)(unit % a.h_kv), u.head0 = (int)(block % a.head_blocks) * 16, u.token = (int)(block / a.head_blocks);
+    u.b = __builtin_amdgcn_readfirstlane(request_of<1>(a.req, u.token, 0, lane));
+    u.real = u.b < a.req.batch;
+    if (u.real) {
+        u.span = span_of(a.req, u.b);
+        u.real = u.token >= u.span.first && u.token - u.span.first < u.span.count;
+    }
+    return u;
+}
+
+template <int D>
+__global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArgs a) {
+    extern __shared__ float lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Rows<D> rows(lds, wave, lane);
+    const Four<D> four = {lds};
+    const long from = blockIdx.x * a.share, stop = min(from + a.share, a.places);
+    for (long x = from; x < stop;) {
+        const Unit u = unit_of(a, x, lane);
+        const long last = min(stop, u.end);
+        const int p0 = (int)(x - u.begin), p1 = (int)(last - u.begin);
+        const bool whole = p0 == 0 && last == u.end;
+        x = last;
+        if (!u.real) continue;
+        const int n = u.span.positions, lim = n - u.span.count + u.token - u.span.first + 1;
+        const bool real = u.head0 + rows.m < a.g;
+        const int head = u.kv * a.g + min(u.head0 + rows.m, a.g - 1);
+        const size_t at = (size_t)u.token * a.h_q + head;
+        const int *const list = a.selected + ((size_t)u.token * a.h_kv + u.kv) * a.count;
+        const int begin = p0 + (int)((long)(p1 - p0) * wave / 4), count = __builtin_amdgcn_readfirstlane(p0 + (int)((long)(p1 - p0) * (wave + 1) / 4) - begin);
+        int place = -1;  // of the page in its request, a page per lane
+        auto numbers = [&](int i) __attribute__((always_inline)) {
+            place = i + lane < count ? list[begin + i + lane] : -1;
+            return place >= 0 && place < (a.req.max_context + kPage - 1) / kPage ? page_of(a.req, u.b, place * kPage) : -1;
+        };
+        const int ahead = numbers(0);
+        rows.load(a.q + at * D, real, a.scale);
+        rows.walk(count, real ? lim : 0, n, a.pages, a.h_kv, u.kv, ahead, numbers,
+                  [&](int i) __attribute__((always_inline)) { return (int)((uint32_t)__builtin_amdgcn_readlane(place, i & 63) * kPage); });
+        const size_t their_at = Four<D>::theirs((unsigned long long)at), part = ((size_t)blockIdx.x * 2 + (u.begin > from ? 1 : 0)) * 16 + (threadIdx.x >> 4);
+        four.meet(
+            rows, wave, Four<D>::theirs((int)real) != 0,
+            [&](int d, const v4f &o, float inv) __attribute__((always_inline)) {
+                if (whole)
+                    *reinterpret_cast<h4 *>(a.out + their_at * D + d) = rounded(o, inv);
+                else
+                    *reinterpret_cast<v4f *>(a.ws_o + part * D + d) = o;
+            },
+            [&](float top, float l) __attribute__((always_inline)) {
+                if (!whole) a.ws_ml[part * 2] = top, a.ws_ml[part * 2 + 1] = l;
+            });
+    }
+}
+
+// A workgroup for the unit that the share of workgroup blockIdx.x + 1 begins inside of, if that is the first to do so; D / 4 threads per row
+template <int D>
+__global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs a) {
+    const int lane = threadIdx.x & 63, d = 4 * (threadIdx.x % (D / 4));
+    const long x = ((long)blockIdx.x + 1) * a.share;
+    const Unit u = unit_of(a, x, lane);
+    if (u.begin >= x || x - u.begin > a.share || !u.real) return;
+    const long w0 = u.begin / a.share;
+    const int parts = (int)((u.end - 1) / a.share - w0) + 1;
+    for (int row = threadIdx.x / (D / 4); row < min(16, a.g - u.head0); row += 1024 / D) {
+        float inv;
+        const v4f o = joined(a.ws_ml, a.ws_o + d, D, parts,
+                             [&](int c) __attribute__((always_inline)) { return (size_t)((w0 + c) * 2 + (c == 0 && u.begin > w0 * a.share ? 1 : 0)) * 16 + row; }, inv);
+        *reinterpret_cast<h4 *>(a.out + ((size_t)u.token * a.h_q + u.kv * a.g + u.head0 + row) * D + d) = rounded(o, inv);
+    }
+}
+
+// ---- common pages.  A workgroup per part of the rows of a group or a request.
+template <int D>
+__global__ __launch_bounds__(256, kWgs) void attn_q4_parts_kernel(PartsArgs a) {
+    extern __shared__ float lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long all_rows = (long)a.req.tokens * a.h_q;
+    Rows<D> rows(lds, wave, lane);
+    const Four<D> four = {lds};
+    const int m = rows.m;
+    for (long item = blockIdx.x; item < a.items; item += gridDim.x) {
+        // ---- which rows, which pages: from .. to - 1 of request b
+        int b, lim, n, from, first, row, rows_all, pages;
+        const bool common = item < a.prefix_items;
+        const long x = common ? item : item - a.prefix_items;
+        const int parts = common ? a.prefix_parts : a.parts, kv = (int)(x % a.h_kv), part = (int)(x / a.h_kv % parts), block = (int)(x / a.h_kv / parts);
+        if (common) {
+            const Found f = find(block, a.groups, lane, [&](int i) __attribute__((always_inline)) { return (int)(((long)tokens_of_group(a, i) * a.g + 15) / 16); });
+            if (f.run < 0) {  // (on to the items behind the groups')
+                item += (a.prefix_items - 1 - item) / gridDim.x * gridDim.x;
+                continue;
+            }
+            const Group group = group_of(a, f.run, lane);
+            b = group.lead, pages = group.pages;
+            first = token_at(a, group_end(a, f.run)), rows_all = tokens_of_group(a, f.run) * a.g, row = f.place * 16 + m;
+            n = pages * kPage, lim = n, from = 0;
+        } else {
+            Found f = {block, 0};
+            if (a.req.max_tokens * a.g > 16)
+                f = find(block, a.req.batch, lane, [&](int i) __attribute__((always_inline)) { return (span_of(a.req, i).count * a.g + 15) / 16; });
+            if (f.run < 0 || f.run >= a.req.batch) return;
+            b = f.run;
+            const Span s = span_of(a.req, b);
+            first = s.first, rows_all = s.count * a.g, row = f.place * 16 + m;
+            n = s.positions, lim = n - s.count + row / a.g + 1;
+            // its group, and the pages that are done with that
+            int before = 0;
+            for (int c = 0; c <= a.groups; c += 64) before += __popcll(__ballot(c + lane <= a.groups && group_end(a, min(c + lane, a.groups)) <= b));
+            from = before > 0 && before <= a.groups ? group_of(a, before - 1, lane).pages : 0;
+            // (the last row's positions are the most)
+            const int sees = max(0, n - s.count + min(f.place * 16 + 15, rows_all - 1) / a.g + 1);
+            pages = (sees + kPage - 1) / kPage;
+        }
+        if (rows_all <= 0) continue;
+        const bool real = row < rows_all;
+        row = min(row, rows_all - 1);
+        const int token = first + row / a.g, head = kv * a.g + row % a.g, slot = part + (common ? 0 : a.prefix_parts);
+        const int per = max(4, (max(pages - from, 0) + parts - 1) / parts);
+        from = min(from + part * per, max(pages, from));
+        const int to = min(from + per, max(pages, from));
+        const size_t at = (size_t)token * a.h_q + head, out_row = (size_t)slot * all_rows + at;
+        if (from >= to) {
+            if (wave == 0 && rows.r == 0 && real) a.ws_ml[out_row * 2 + 1] = 0.0f;
+            continue;
+        }
+        // ---- this wavefront's quarter
+        const int share = (to - from + 3) / 4, begin = min(from + wave * share, to), count = __builtin_amdgcn_readfirstlane(min(begin + share, to) - begin);
+        auto numbers = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (begin + i + lane) * kPage) : -1; };
+        const int ahead = numbers(0);
+        rows.load(a.q + at * D, real, a.scale);
+        rows.walk(count, real ? lim : 0, n, a.pages, a.h_kv, kv, ahead, numbers, [&](int i) __attribute__((always_inline)) { return (begin + i) * kPage; });
+        const size_t to_row = Four<D>::theirs((unsigned long long)out_row);
+        four.meet(
+            rows, wave, Four<D>::theirs((int)real) != 0,
+            [&](int d, const v4f &o, float) __attribute__((always_inline)) { *reinterpret_cast<v4f *>(a.ws_o + to_row * D + d) = o; },
+            [&](float top, float l) __attribute__((always_inline)) { a.ws_ml[to_row * 2] = top, a.ws_ml[to_row * 2 + 1] = l; });
     }
 }
 
@@ -212,76 +329,41 @@ __global__ __launch_bounds__(256) void attn_q4_join_kernel(PartsArgs a) {
         const int token = (int)(row / a.h_q);
         if (token >= last) return;
         const int first = token >= group0 && token < group1 ? 0 : a.prefix_parts;
-        float top = kNothingYet, l = 0.0f;
-        v4f o = {};
-        for (int s0 = first; s0 < slots; s0 += 8) {
-            float ms[8], ls[8];
-            v4f os[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const size_t at = (size_t)min(s0 + i, slots - 1) * all_rows + row;
-                ms[i] = a.ws_ml[at * 2], ls[i] = a.ws_ml[at * 2 + 1];
-                os[i] = *reinterpret_cast<const v4f *>(a.ws_o + at * D + d);
-            }
-            float new_top = top;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (s0 + i >= slots) ls[i] = 0.0f;
-                new_top = ls[i] != 0.0f ? fmaxf(new_top, ms[i]) : new_top;
-            }
-            const float corr = __builtin_amdgcn_exp2f(top - new_top);
-            top = new_top, l *= corr;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] *= corr;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (ls[i] == 0.0f) continue;  // (nothing was seen: what stands there is not defined)
-                const float f = __builtin_amdgcn_exp2f(ms[i] - top);
-                l = fmaf(f, ls[i], l);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, os[i][e], o[e]);
-            }
-        }
-        const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-        *reinterpret_cast<h4 *>(a.out + row * D + d) = h4{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv), (_Float16)(o[2] * inv), (_Float16)(o[3] * inv)};
+        float inv;
+        const v4f o = joined(a.ws_ml, a.ws_o + d, D, slots - first, [&](int c) __attribute__((always_inline)) { return (size_t)(first + c) * all_rows + row; }, inv);
+        *reinterpret_cast<h4 *>(a.out + row * D + d) = rounded(o, inv);
     }
 }
 
-template <int D, bool SELECTED>
-hipError_t launch(const PartsArgs &a, int num_cus, hipStream_t st) {
+constexpr long kMostWgs = 1L << 22;  // (a launch has fewer than 2^32 threads)
+template <int D>
+hipError_t launch(const PartsArgs &a, hipStream_t st) {
     constexpr size_t lds = Place<D>::LDS;
-    if (const hipError_t e = allow_dynamic_lds<attn_q4_parts_kernel<D, SELECTED>>(lds); e != hipSuccess) return e;
-    const long most = 1L << 22;  // (a launch has fewer than 2^32 threads)
-    attn_q4_parts_kernel<D, SELECTED><<<(unsigned)(a.items < most ? a.items : most), 256, lds, st>>>(a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess || a.prefix_parts + a.parts == 1) return e;
+    if (const hipError_t e = allow_dynamic_lds<attn_q4_parts_kernel<D>>(lds); e != hipSuccess) return e;
+    attn_q4_parts_kernel<D><<<(unsigned)(a.items < kMostWgs ? a.items : kMostWgs), 256, lds, st>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const long joins = ((long)a.req.tokens * a.h_q + 1024 / D - 1) / (1024 / D);
-    attn_q4_join_kernel<D><<<(unsigned)(joins < most ? joins : most), 256, 0, st>>>(a);
+    attn_q4_join_kernel<D><<<(unsigned)(joins < kMostWgs ? joins : kMostWgs), 256, 0, st>>>(a);
     return hipGetLastError();
 }
-template <bool SELECTED>
-hipError_t launch(const PartsArgs &a, int d, int num_cus, hipStream_t st) {
+template <int D>
+hipError_t launch(const SelectedArgs &a, hipStream_t st) {
+    constexpr size_t lds = Place<D>::LDS;
+    if (const hipError_t e = allow_dynamic_lds<attn_q4_selected_kernel<D>>(lds); e != hipSuccess) return e;
+    const unsigned wgs = (unsigned)((a.places + a.share - 1) / a.share);
+    attn_q4_selected_kernel<D><<<wgs, 256, lds, st>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || wgs == 1 || a.share % a.count == 0) return e;  // (no unit is cut)
+    attn_q4_join_selected_kernel<D><<<wgs - 1, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <class Args>
+hipError_t launch(const Args &a, int d, hipStream_t st) {
     switch (d) {
-        case 64: return launch<64, SELECTED>(a, num_cus, st);
-        case 128: return launch<128, SELECTED>(a, num_cus, st);
-        case 256: return launch<256, SELECTED>(a, num_cus, st);
+        case 64: return launch<64>(a, st);
+        case 128: return launch<128>(a, st);
+        case 256: return launch<256>(a, st);
     }
     return hipErrorInvalidValue;
-}
-
-PartsArgs args_of(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const AttnPartsPlan &p, void *workspace, void *out) {
-    PartsArgs a = {};
-    a.q = static_cast<const _Float16 *>(q);
-    a.out = static_cast<_Float16 *>(out);
-    a.pages = static_cast<const char *>(pages);
-    a.req = req;
-    a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv, a.head_blocks = (a.g + 15) / 16;
-    a.prefix_parts = p.prefix_parts, a.parts = p.parts;
-    a.prefix_items = p.prefix_blocks * h_kv * p.prefix_parts;
-    a.items = a.prefix_items + p.blocks * h_kv * p.parts;
-    a.ws_o = static_cast<float *>(workspace);
-    a.ws_ml = a.ws_o + (size_t)(p.prefix_parts + p.parts) * req.tokens * h_q * d;
-    a.scale = 1.4426950408889634f / sqrtf((float)d);
-    return a;
 }
 
 constexpr int kMostParts = 16;
@@ -294,11 +376,17 @@ int parts_of(long blocks, int pages, int num_cus) {
 
 }  // namespace
 
-AttnPartsPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, int count, int num_cus) {
-    AttnPartsPlan p = {};
-    p.blocks = (long)tokens * ((h_q / h_kv + 15) / 16);
-    p.parts = parts_of(p.blocks * h_kv, count, num_cus);
-    p.bytes = 256 + (p.parts > 1 ? (size_t)p.parts * tokens * h_q * (d + 2) * sizeof(float) : 0);
+SelectedPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, int count, int num_cus) {
+    SelectedPlan p = {};
+    const long units = (long)tokens * h_kv * ((h_q / h_kv + 15) / 16), wgs = (long)kWgs * (num_cus > 0 ? num_cus : 1);
+    p.places = units * count;
+    p.share = (p.places + wgs - 1) / wgs;
+    if (p.share < 4) p.share = 4;  // (a page per wavefront)
+    // whole units, where that makes the largest share an eighth larger at most: nothing to join
+    const long whole = (p.share + count - 1) / count * count;
+    if (whole <= p.share + p.share / 8) p.share = whole;
+    p.wgs = (p.places + p.share - 1) / p.share;
+    p.bytes = 256 + (p.wgs > 1 && p.share % count != 0 ? (size_t)p.wgs * 2 * 16 * (d + 2) * sizeof(float) : 0);
     return p;
 }
 
@@ -314,18 +402,38 @@ AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv,
     return p;
 }
 
-hipError_t launch_attention_selected_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *selected, int count, const AttnPartsPlan &p, void *workspace,
-                                        void *out, int num_cus, hipStream_t st) {
-    PartsArgs a = args_of(q, req, h_q, h_kv, d, pages, p, workspace, out);
+hipError_t launch_attention_selected_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *selected, int count, const SelectedPlan &p, void *workspace,
+                                        void *out, hipStream_t st) {
+    SelectedArgs a = {};
+    a.q = static_cast<const _Float16 *>(q);
+    a.out = static_cast<_Float16 *>(out);
+    a.pages = static_cast<const char *>(pages);
+    a.req = req;
     a.selected = selected, a.count = count;
-    return launch<true>(a, d, num_cus, st);
+    a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv, a.head_blocks = (a.g + 15) / 16;
+    a.share = p.share, a.places = p.places;
+    a.ws_o = static_cast<float *>(workspace);
+    a.ws_ml = a.ws_o + (size_t)p.wgs * 2 * 16 * d;
+    a.scale = 1.4426950408889634f / sqrtf((float)d);
+    return launch(a, d, st);
 }
 
 hipError_t launch_attention_shared_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *group_start, const int *prefix, int groups, int group_tokens,
-                                      int longest, const AttnPartsPlan &p, void *workspace, void *out, int num_cus, hipStream_t st) {
-    PartsArgs a = args_of(q, req, h_q, h_kv, d, pages, p, workspace, out);
+                                      int longest, const AttnPartsPlan &p, void *workspace, void *out, hipStream_t st) {
+    PartsArgs a = {};
+    a.q = static_cast<const _Float16 *>(q);
+    a.out = static_cast<_Float16 *>(out);
+    a.pages = static_cast<const char *>(pages);
+    a.req = req;
     a.group_start = group_start, a.prefix = prefix, a.groups = groups, a.group_tokens = group_tokens, a.longest = longest;
-    return launch<false>(a, d, num_cus, st);
+    a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv;
+    a.prefix_parts = p.prefix_parts, a.parts = p.parts;
+    a.prefix_items = p.prefix_blocks * h_kv * p.prefix_parts;
+    a.items = a.prefix_items + p.blocks * h_kv * p.parts;
+    a.ws_o = static_cast<float *>(workspace);
+    a.ws_ml = a.ws_o + (size_t)(p.prefix_parts + p.parts) * req.tokens * h_q * d;
+    a.scale = 1.4426950408889634f / sqrtf((float)d);
+    return launch(a, d, st);
 }
 
 }  // namespace qfc

@@ -419,18 +419,22 @@ hipError_t launch_bound_pages_q4(const Requests &req, int h_kv, int d, const voi
 size_t select_workspace(int tokens, int h_kv, int max_context, int num_cus);
 hipError_t launch_select_pages_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const int8_t *codes, const float *steps, int first, int last, int count, void *workspace,
                                   int *selected, int num_cus, hipStream_t st);
-// Attention in parts that are joined: of selected pages, and of requests with common pages
+// Attention in parts that are joined: of requests with common pages, and of selected pages
 struct AttnPartsPlan {
     long prefix_blocks, blocks;  // of 16 query rows of a KV head: of groups (common pages), of requests
     int prefix_parts, parts;     // runs that their pages are cut into
     size_t bytes;                // of the workspace
 };
-AttnPartsPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, int count, int num_cus);
+struct SelectedPlan {
+    long places, share, wgs;  // pages of all lists, of a workgroup
+    size_t bytes;
+};
+SelectedPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, int count, int num_cus);
 AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv, int d, int max_tokens, int max_context, int groups, int group_tokens, int longest, int num_cus);
-hipError_t launch_attention_selected_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *selected, int count, const AttnPartsPlan &p, void *workspace,
-                                        void *out, int num_cus, hipStream_t st);
+hipError_t launch_attention_selected_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *selected, int count, const SelectedPlan &p, void *workspace,
+                                        void *out, hipStream_t st);
 hipError_t launch_attention_shared_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const void *pages, const int *group_start, const int *prefix, int groups, int group_tokens,
-                                      int longest, const AttnPartsPlan &p, void *workspace, void *out, int num_cus, hipStream_t st);
+                                      int longest, const AttnPartsPlan &p, void *workspace, void *out, hipStream_t st);
 struct AdapterPlan {
     int rows;           // M rounded up
     int parts, part_k;  // K in `parts` parts of `part_k`

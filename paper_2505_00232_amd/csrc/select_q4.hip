@@ -31,14 +31,17 @@ __device__ __forceinline__ float row_max(float x) {
 }
 __device__ __forceinline__ int clamped(float x) { return (int)fminf(fmaxf(x, -127.0f), 127.0f); }
 
-// A wavefront per page and head.  Lane (m, r) reads what it reads in attention: of the positions of its slots the octets 32 j + 8 r.
+// A workgroup per page and head, a wavefront of it for one group of 32 values (two of eight groups).  Lane (m, r) reads what it reads in attention: of the positions of its slots the octets
+// 32 j + 8 r.  Bound: latency, arrays, table, page one behind the other (a wavefront per page, with all groups, took TIMES).
 template <int D>
 __global__ __launch_bounds__(256) void bound_pages_kernel(BoundArgs a) {
     typedef PageLayout<D> L;
-    constexpr int G = L::G, W = L::W;
-    const int lane = threadIdx.x & 63, m = lane & 15, r = lane >> 4;
-    const long all = (long)a.req.batch * a.slots * a.h_kv, step = (long)gridDim.x * 4;
-    for (long i = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < all; i += step) {
+    constexpr int G = L::G, WAVES = G < 4 ? G : 4, J = G / WAVES;
+    __shared__ float tops[2][WAVES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, r = lane >> 4;
+    const long all = (long)a.req.batch * a.slots * a.h_kv;
+    int turn = 0;
+    for (long i = blockIdx.x; i < all; i += gridDim.x) {
         const int kv = (int)(i % a.h_kv), slot = (int)(i / a.h_kv % a.slots), b = (int)(i / a.h_kv / a.slots);
         const Span s = span_of(a.req, b);
         const int p0 = max(s.positions - s.count, 0) / kPage + slot;
@@ -46,56 +49,54 @@ __global__ __launch_bounds__(256) void bound_pages_kernel(BoundArgs a) {
         const int page = page_of(a.req, b, p0 * kPage), there = s.positions - p0 * kPage;
         if (page < 0) continue;
         const char *src = a.pages + ((size_t)page * a.h_kv + kv) * L::kBytes;
-        float hi[G][8], lo[G][8];  // (lo: negated)
-#pragma unroll
-        for (int j = 0; j < G; ++j)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) hi[j][e] = lo[j][e] = -INFINITY;
-        typedef uint32_t words __attribute__((ext_vector_type(W)));
+        // (everything is asked for before any of it is looked at)
+        uint32_t c[4][J];
+        _Float16 by[4][J], off[4][J];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const int p = 16 * (m >> 2) + 4 * t + (m & 3);
 #pragma unroll
-            for (int jj = 0; jj < G / W; ++jj) {
-                const words c = *reinterpret_cast<const words *>(src + L::kCodesK + ((t * (G / W) + jj) * 64 + lane) * (4 * W));
-#pragma unroll
-                for (int jw = 0; jw < W; ++jw) {
-                    const int j = jj * W + jw;
-                    const float by = (float)*reinterpret_cast<const _Float16 *>(src + L::step_k(p, j)), off = (float)*reinterpret_cast<const _Float16 *>(src + L::offset_k(p, j));
-                    if (p < there) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float x = fmaf((float)((c[jw] >> nibble(e)) & 15u) - 8.0f, by, off);
-                            hi[j][e] = fmaxf(hi[j][e], x), lo[j][e] = fmaxf(lo[j][e], -x);
-                        }
-                    }
-                }
+            for (int k = 0; k < J; ++k) {
+                const int j = wave + WAVES * k;
+                c[t][k] = *reinterpret_cast<const uint32_t *>(src + L::code_k(p, j, r));
+                by[t][k] = *reinterpret_cast<const _Float16 *>(src + L::step_k(p, j));
+                off[t][k] = *reinterpret_cast<const _Float16 *>(src + L::offset_k(p, j));
             }
         }
-        float most = 0.0f;
+        float hi[J][8], lo[J][8], most = 0.0f;  // (lo: negated)
 #pragma unroll
-        for (int j = 0; j < G; ++j)
+        for (int k = 0; k < J; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                hi[j][e] = row_max(hi[j][e]), lo[j][e] = row_max(lo[j][e]);
-                most = fmaxf(most, fmaxf(fabsf(hi[j][e]), fabsf(lo[j][e])));
+                hi[k][e] = lo[k][e] = -INFINITY;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const float x = fmaf((float)((c[t][k] >> nibble(e)) & 15u) - 8.0f, (float)by[t][k], (float)off[t][k]);
+                    const bool mine = 16 * (m >> 2) + 4 * t + (m & 3) < there;
+                    hi[k][e] = fmaxf(hi[k][e], mine ? x : -INFINITY), lo[k][e] = fmaxf(lo[k][e], mine ? -x : -INFINITY);
+                }
+                hi[k][e] = row_max(hi[k][e]), lo[k][e] = row_max(lo[k][e]);
+                most = fmaxf(most, fmaxf(fabsf(hi[k][e]), fabsf(lo[k][e])));
             }
         most = fmaxf(most, __shfl_xor(most, 16, 64));
         most = fmaxf(most, __shfl_xor(most, 32, 64));
+        turn ^= 1;  // (the next page's go beside these: one barrier is enough)
+        if (lane == 0) tops[turn][wave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) most = fmaxf(most, tops[turn][w]);
         const float f = most > 0.0f ? 127.0f / most : 0.0f;
         int8_t *dst = a.codes + ((size_t)page * a.h_kv + kv) * (2 * D);
 #pragma unroll
-        for (int j = 0; j < G; ++j) {  // lane m: octet m % G of the upper bounds (m < G) or the lower ones
-            if (m % 8 != j) continue;
-            u32x2 up = {0, 0}, down = {0, 0};
+        for (int k = 0; k < J; ++k) {  // lane m = 2 k: the upper bounds' octet, 2 k + 1: the lower ones'
+            if (m >> 1 != k) continue;
+            const bool upper = (m & 1) == 0;
+            u32x2 codes = {0, 0};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                up[e / 4] |= (uint32_t)(clamped(ceilf(hi[j][e] * f)) & 255) << (8 * (e % 4));
-                down[e / 4] |= (uint32_t)(clamped(floorf(-lo[j][e] * f)) & 255) << (8 * (e % 4));
-            }
-            *reinterpret_cast<u32x2 *>(dst + (m < 8 ? 0 : D) + 32 * j + 8 * r) = m < 8 ? up : down;
+            for (int e = 0; e < 8; ++e) codes[e / 4] |= (uint32_t)(clamped(upper ? ceilf(hi[k][e] * f) : floorf(-lo[k][e] * f)) & 255) << (8 * (e % 4));
+            *reinterpret_cast<u32x2 *>(dst + (upper ? 0 : D) + 32 * (wave + WAVES * k) + 8 * r) = codes;
         }
-        if (lane == 0) a.steps[(size_t)page * a.h_kv + kv] = most / 127.0f;
+        if (threadIdx.x == 0) a.steps[(size_t)page * a.h_kv + kv] = most / 127.0f;
     }
 }
 
@@ -105,9 +106,10 @@ struct SelectArgs {
     const int8_t *codes;
     const float *steps;
     int *selected;  // [tokens][h_kv][count]
-    float *scores;  // of a workgroup [most_pages], where they do not fit the LDS
+    float *scores;  // [items of a slice][most_pages], where scores and list are launches of their own
     int h_q, h_kv, g, first, last, count, most_pages;
-    long items;
+    long item0, items;  // tokens and heads of this launch
+    int pieces;         // workgroups of an item's scores
 };
 
 __device__ __forceinline__ uint32_t key_of(float x) {  // order of floats as one of whole numbers
@@ -115,15 +117,21 @@ __device__ __forceinline__ uint32_t key_of(float x) {  // order of floats as one
     return u ^ ((int)u < 0 ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// A workgroup per token and KV head: scores of all pages it sees, the one that is the last to be taken (a byte of it at a time, by how many scores begin so), and the list in ascending order.
-template <int D, bool IN_LDS>
+// Scores of all pages that a token sees, the score that is the last to be taken (a byte of it at a time, by how many scores begin so), and the list in ascending order: a workgroup per
+// token and KV head does all of it (kAll), or several of them the scores (kScores), and one the rest (kList).  Bound: latency, of the requests' arrays, the table, the bounds one behind the
+// other, and of some twenty barriers.
+enum { kAll, kScores, kList };
+template <int D, int PHASE, bool IN_LDS>
 __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
     constexpr int C = D / 64, AHEAD = 2;  // chunks of 64 components; groups of 16 pages on their way
     extern __shared__ float lds_scores[];
     __shared__ int counts[256], found[2], taken[16][2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, m = lane & 15, r = lane >> 4;
-    float *const scores = IN_LDS ? lds_scores : a.scores + (size_t)blockIdx.x * a.most_pages;
-    for (long item = blockIdx.x; item < a.items; item += gridDim.x) {
+    const int pieces = PHASE == kScores ? a.pieces : 1;
+    for (long work = blockIdx.x; work < a.items * pieces; work += gridDim.x) {
+        const long in_slice = work / pieces, item = a.item0 + in_slice;
+        float *const kept = PHASE == kAll ? nullptr : a.scores + (size_t)in_slice * a.most_pages;
+        float *const scores = IN_LDS ? lds_scores : kept;
         const int kv = (int)(item % a.h_kv), token = (int)(item / a.h_kv);
         const int b = __builtin_amdgcn_readfirstlane(request_of<1>(a.req, token, 0, lane));
         if (b >= a.req.batch) return;
@@ -132,12 +140,14 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
         const int pos = s.positions - s.count + token - s.first, sees = pos < 0 ? 0 : pos / kPage + 1;
         int *const out = a.selected + (size_t)item * a.count;
         if (sees <= a.count) {
-            for (int i = threadIdx.x; i < a.count; i += blockDim.x) out[i] = i < sees ? i : -1;
+            if (PHASE != kScores)
+                for (int i = threadIdx.x; i < a.count; i += blockDim.x) out[i] = i < sees ? i : -1;
             continue;
         }
         const int k = a.count - a.first - a.last, mid0 = a.first, mid1 = sees - a.last;
         if (k > 0) {
             // ---- scores of the pages in between, 16 heads at a time
+            if constexpr (PHASE != kList)
             for (int h0 = 0; h0 < a.g; h0 += 16) {
                 const _Float16 *q = a.q + ((size_t)token * a.h_q + kv * a.g + min(h0 + m, a.g - 1)) * D;
                 float x[C][16], top = 0.0f;
@@ -169,7 +179,7 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                 float of_row[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) of_row[i] = __shfl(by, 4 * r + i, 64);
-                for (int p0 = mid0 + wave * (16 * AHEAD); p0 < mid1; p0 += waves * (16 * AHEAD)) {
+                for (int p0 = mid0 + ((int)(work % pieces) * waves + wave) * (16 * AHEAD); p0 < mid1; p0 += pieces * waves * (16 * AHEAD)) {
                     int page[AHEAD];
                     float step[AHEAD];
                     i32x4 bound[AHEAD][2 * C];
@@ -201,6 +211,9 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                     }
                 }
             }
+            if constexpr (PHASE == kScores) continue;
+            if constexpr (PHASE == kList && IN_LDS)
+                for (int p = mid0 + (int)threadIdx.x; p < mid1; p += blockDim.x) scores[p] = kept[p];
             __syncthreads();
             // ---- the k-th of them
             uint32_t prefix = 0, mask = 0;
@@ -253,21 +266,43 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                 if (is_above || (is_level && level_here < left)) out[a.first + above_here + min(level_here, left)] = p;
             }
         }
+        if constexpr (PHASE == kScores) continue;
         for (int i = threadIdx.x; i < a.first + a.last; i += blockDim.x) out[i < a.first ? i : k + i] = i < a.first ? i : sees - (a.first + a.last) + i;
         __syncthreads();
     }
 }
 
-template <int D, bool IN_LDS>
-hipError_t launch_select(const SelectArgs &a, int threads, unsigned grid, hipStream_t st) {
-    const size_t lds = IN_LDS ? (size_t)a.most_pages * sizeof(float) : 0;
+int pages_below(int max_context) { return (max_context + kPage - 1) / kPage; }
+
+// Tokens and heads whose scores are kept in memory at a time
+constexpr int kSlice = 512;
+// One launch where scores fit the LDS and a workgroup has them at once, or workgroups fill the card; else scores and lists are launches of their own (one request at 131000
+// positions: TIMES).
+bool one_launch(long items, int pages, int num_cus) { return pages <= kSelectInLds && (pages <= 1024 || items >= num_cus); }
+
+template <int D, int PHASE, bool IN_LDS>
+hipError_t launch_phase(const SelectArgs &a, int threads, long wgs, hipStream_t st) {
     if constexpr (IN_LDS)
-        if (const hipError_t e = allow_dynamic_lds<select_pages_kernel<D, true>>((size_t)kSelectInLds * sizeof(float)); e != hipSuccess) return e;
-    select_pages_kernel<D, IN_LDS><<<grid, threads, lds, st>>>(a);
+        if (const hipError_t e = allow_dynamic_lds<select_pages_kernel<D, PHASE, true>>((size_t)kSelectInLds * sizeof(float)); e != hipSuccess) return e;
+    const long most = 1L << 20;
+    select_pages_kernel<D, PHASE, IN_LDS><<<(unsigned)(wgs < most ? wgs : most), threads, IN_LDS ? (size_t)a.most_pages * sizeof(float) : 0, st>>>(a);
     return hipGetLastError();
 }
 
-int pages_below(int max_context) { return (max_context + kPage - 1) / kPage; }
+template <int D>
+hipError_t launch_select(SelectArgs a, int num_cus, hipStream_t st) {
+    const int threads = a.most_pages <= 128 ? 256 : a.most_pages <= 256 ? 512 : 1024;  // (32 pages of a wavefront are on their way at once)
+    if (one_launch(a.items, a.most_pages, num_cus)) return launch_phase<D, kAll, true>(a, threads, a.items, st);
+    const long all = a.items;
+    for (; a.item0 < all; a.item0 += kSlice) {
+        a.items = all - a.item0 < kSlice ? all - a.item0 : kSlice;
+        a.pieces = (a.most_pages + 127) / 128;
+        if (const hipError_t e = launch_phase<D, kScores, false>(a, 256, a.items * a.pieces, st); e != hipSuccess) return e;
+        const hipError_t e = a.most_pages <= kSelectInLds ? launch_phase<D, kList, true>(a, 1024, a.items, st) : launch_phase<D, kList, false>(a, 1024, a.items, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 }  // namespace
 
@@ -277,10 +312,10 @@ hipError_t launch_bound_pages_q4(const Requests &req, int h_kv, int d, const voi
     a.req = req;
     a.codes = codes, a.steps = steps, a.h_kv = h_kv;
     a.slots = (req.max_tokens < req.max_context ? req.max_tokens : req.max_context) / kPage + 2;
-    const long wgs = ((long)req.batch * a.slots * h_kv + 3) / 4, most = 1L << 22;
+    const long wgs = (long)req.batch * a.slots * h_kv, most = 1L << 22;
     const unsigned grid = (unsigned)(wgs < most ? wgs : most);
     if (d == 64)
-        bound_pages_kernel<64><<<grid, 256, 0, st>>>(a);
+        bound_pages_kernel<64><<<grid, 128, 0, st>>>(a);
     else if (d == 128)
         bound_pages_kernel<128><<<grid, 256, 0, st>>>(a);
     else
@@ -290,26 +325,22 @@ hipError_t launch_bound_pages_q4(const Requests &req, int h_kv, int d, const voi
 
 size_t select_workspace(int tokens, int h_kv, int max_context, int num_cus) {
     const int pages = pages_below(max_context);
-    const long items = (long)tokens * h_kv, wgs = items < num_cus ? items : num_cus;
-    return 256 + (pages > kSelectInLds ? (size_t)wgs * pages * sizeof(float) : 0);
+    const long items = (long)tokens * h_kv, kept = items < kSlice ? items : kSlice;
+    return 256 + (one_launch(items, pages, num_cus) ? 0 : (size_t)kept * pages * sizeof(float));
 }
 
 hipError_t launch_select_pages_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const int8_t *codes, const float *steps, int first, int last, int count, void *workspace,
                                   int *selected, int num_cus, hipStream_t st) {
-    SelectArgs a;
+    SelectArgs a = {};
     a.q = static_cast<const _Float16 *>(q);
     a.req = req;
     a.codes = codes, a.steps = steps, a.selected = selected, a.scores = static_cast<float *>(workspace);
     a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv, a.first = first, a.last = last, a.count = count, a.most_pages = pages_below(req.max_context);
     a.items = (long)req.tokens * h_kv;
-    const bool in_lds = a.most_pages <= kSelectInLds;
-    const long most = in_lds ? 1L << 20 : num_cus;
-    const unsigned grid = (unsigned)(a.items < most ? a.items : most);
-    const int threads = a.most_pages > 512 ? 1024 : 256;
     switch (d) {
-        case 64: return in_lds ? launch_select<64, true>(a, threads, grid, st) : launch_select<64, false>(a, threads, grid, st);
-        case 128: return in_lds ? launch_select<128, true>(a, threads, grid, st) : launch_select<128, false>(a, threads, grid, st);
-        case 256: return in_lds ? launch_select<256, true>(a, threads, grid, st) : launch_select<256, false>(a, threads, grid, st);
+        case 64: return launch_select<64>(a, num_cus, st);
+        case 128: return launch_select<128>(a, num_cus, st);
+        case 256: return launch_select<256>(a, num_cus, st);
     }
     return hipErrorInvalidValue;
 }

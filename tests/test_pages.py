@@ -526,11 +526,12 @@ def test_select_pages(S, n, h_q, h_kv, d, first, last, count, alike):
     q[0, :d] = 0
     req = _requests(S, n, table, rows=T)
     got = _select(req, q, h_q, cache, bounds, first, last, count, T).cpu().numpy()
-    # the same with scores in the workspace: limits above what fits the LDS
-    wide = np.full((len(n), 33000), -1, np.int32)
-    wide[:, :table.shape[1]] = table
-    far = B.Requests(req.token_start, req.context, _i(wide), T, max(S), 33000 * 64)
-    assert np.array_equal(_select(far, q, h_q, cache, bounds, first, last, count, T).cpu().numpy(), got)
+    # the same with scores in the workspace: limits above what a workgroup has at once, and above what fits the LDS
+    for limit in (1500, 33000):
+        wide = np.full((len(n), limit), -1, np.int32)
+        wide[:, :table.shape[1]] = table
+        far = B.Requests(req.token_start, req.context, _i(wide), T, max(S), limit * 64)
+        assert np.array_equal(_select(far, q, h_q, cache, bounds, first, last, count, T).cpu().numpy(), got)
     at, g = 0, h_q // h_kv
     for b, s in enumerate(S):
         codes, steps = _bounds_of(K[b], n[b], h_kv, d)
