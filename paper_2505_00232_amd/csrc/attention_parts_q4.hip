@@ -180,12 +180,8 @@ __device__ __forceinline__ Unit unit_of(const SelectedArgs &a, long place, int l
     const long unit = place / a.count, block = unit / a.h_kv;
     u.begin = unit * a.count, u.end = u.begin + a.count;
     u.kv = (int)(unit % a.h_kv), u.head0 = (int)(block % a.head_blocks) * 16, u.token = (int)(block / a.head_blocks);
-    u.b = __builtin_amdgcn_readfirstlane(request_of<1>(a.req, u.token, 0, lane));
-    u.real = u.b < a.req.batch;
-    if (u.real) {
-        u.span = span_of(a.req, u.b);
-        u.real = u.token >= u.span.first && u.token - u.span.first < u.span.count;
-    }
+    u.b = __builtin_amdgcn_readfirstlane(request_of_token(a.req, u.token, lane, u.span));
+    u.real = u.b < a.req.batch && u.token >= u.span.first && u.token - u.span.first < u.span.count;
     return u;
 }
 

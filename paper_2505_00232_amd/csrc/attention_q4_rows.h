@@ -31,19 +31,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kFactor = 14.0f;  // log 2 of what P is multiplied with
 constexpr float kNothingYet = -1.0e25f;  // maximum of a row that has seen no position: below every score
 
-// Sums that end at the largest int.
-__device__ __forceinline__ int add(int x, int y) { return __builtin_elementwise_add_sat(x, y); }
-// sum over the lanes up to this one
-__device__ __forceinline__ int sum_upto(int x) {
-    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));  // row_shr 1, 2, 4, 8
-    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
-    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
-    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
-    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));  // row_bcast 15, 31
-    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
-    return x;
-}
-
 // Workgroups per compute unit.  More would fit the LDS with heads of 128 and 64 values and were slower: 32 requests of up to 8192 positions 47 us, with three 51; 16 requests of 3000
 // to 6000, heads of 64, 19.0, with three 21.7, with four 20.4.
 constexpr int kWgs = 2;

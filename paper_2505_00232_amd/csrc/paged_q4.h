@@ -63,6 +63,19 @@ __device__ __forceinline__ int page_of(const Requests &q, int b, int p) {
     const int page = q.table[(size_t)b * q.width + p / kPage];
     return page >= 0 && page < q.num_pages ? page : -1;
 }
+// Sums that end at the largest int.
+__device__ __forceinline__ int add(int x, int y) { return __builtin_elementwise_add_sat(x, y); }
+// sum over the lanes up to this one
+__device__ __forceinline__ int sum_upto(int x) {
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));  // row_shr 1, 2, 4, 8
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));  // row_bcast 15, 31
+    x = add(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
+    return x;
+}
+
 // Requests of the tokens of a wavefront, PER of them from `first` on: how many requests end at or before a token.  A lane looks at one request at a time.
 template <int PER>
 __device__ __forceinline__ int request_of(const Requests &q, int first, int mine, int lane) {
@@ -76,6 +89,21 @@ __device__ __forceinline__ int request_of(const Requests &q, int first, int mine
 #pragma unroll
     for (int i = 1; i < PER; ++i) b = mine == i ? count[i] : b;
     return b;
+}
+
+// Request of a token (batch: of none) and its span, the same in every lane.  What is known of 64 requests is asked for at once: no second look at memory for the one that it is.
+__device__ __forceinline__ int request_of_token(const Requests &q, int token, int lane, Span &s) {
+    for (int b0 = 0; b0 < q.batch; b0 += 64) {
+        const int b = b0 + lane, mine = min(b, q.batch - 1), end = q.start[mine + 1];
+        const Span own = span_of(q, mine);
+        const int before = (int)__popcll(__ballot(b < q.batch && end <= token));
+        if (before < min(64, q.batch - b0)) {
+            s = Span{__builtin_amdgcn_readlane(own.first, before), __builtin_amdgcn_readlane(own.count, before), __builtin_amdgcn_readlane(own.positions, before)};
+            return b0 + before;
+        }
+    }
+    s = Span{0, 0, 0};
+    return q.batch;
 }
 
 // Pages and how often tables name them, on the device

@@ -117,6 +117,54 @@ __device__ __forceinline__ uint32_t key_of(float x) {  // order of floats as one
     return u ^ ((int)u < 0 ? 0xFFFFFFFFu : 0x80000000u);
 }
 
+// The k largest of scores mid0 .. mid1 - 1 (64 R at most, more than k), of equal ones the first, ascending: by one wavefront, 64 at a time in its registers.  The k-th is looked for between the
+// least and the largest key by halving; as soon as k of them are not below the middle, those are the ones (some 12 steps for 500 scores, where a byte at a time by 16 wavefronts needs 4
+// passes of three barriers and many atomics on few words: 500 pages 12.5 us, so TIMES).
+template <int R>
+__device__ __forceinline__ void pick(const float *scores, int mid0, int mid1, int k, int lane, int *out) {
+    uint32_t key[R], lo = ~0u, hi = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        key[i] = key_of(scores[min(mid0 + 64 * i + lane, mid1 - 1)]);  // (the last again, for the lanes behind it: loads without branches between them)
+        lo = min(lo, key[i]), hi = max(hi, key[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) key[i] = mid0 + 64 * i + lane < mid1 ? key[i] : 0;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, off, 64)), hi = max(hi, (uint32_t)__shfl_xor((int)hi, off, 64));
+    lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
+    auto from = [&](uint32_t x) __attribute__((always_inline)) {  // how many are x and more
+        int n = 0;  // (of the lane first: a ballot's count per score, through the scalar unit, took three times as long)
+#pragma unroll
+        for (int i = 0; i < R; ++i) n += key[i] >= x ? 1 : 0;
+        return __builtin_amdgcn_readlane(sum_upto(n), 63);
+    };
+    int left = -1;
+    while (lo < hi) {
+        const uint32_t middle = lo + ((hi - lo) >> 1) + 1;
+        const int n = from(middle);
+        if (n == k) {
+            lo = middle - 1, left = 0;  // (all above this)
+            break;
+        }
+        if (n > k)
+            lo = middle;
+        else
+            hi = middle - 1;
+    }
+    if (left < 0) left = k - (lo == ~0u ? 0 : from(lo + 1));  // lo is the k-th: of those level with it
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int p = mid0 + 64 * i + lane;
+        const uint64_t lower = (1ull << lane) - 1, level = __ballot(p < mid1 && key[i] == lo), above = __ballot(p < mid1 && key[i] > lo);
+        const int level_before = (int)__popcll(level & lower), of_level = min((int)__popcll(level), left);
+        if ((above >> lane & 1) || ((level >> lane & 1) && level_before < left)) out[(int)__popcll(above & lower) + min(level_before, left)] = p;
+        out += (int)__popcll(above) + of_level;
+        left -= of_level;
+    }
+}
+constexpr int kPicked = 2048;  // scores that one wavefront picks from
+
 // Scores of all pages that a token sees, the score that is the last to be taken (a byte of it at a time, by how many scores begin so), and the list in ascending order: a workgroup per
 // token and KV head does all of it (kAll), or several of them the scores (kScores), and one the rest (kList).  Bound: latency, of the requests' arrays, the table, the bounds one behind the
 // other, and of some twenty barriers.
@@ -133,9 +181,9 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
         float *const kept = PHASE == kAll ? nullptr : a.scores + (size_t)in_slice * a.most_pages;
         float *const scores = IN_LDS ? lds_scores : kept;
         const int kv = (int)(item % a.h_kv), token = (int)(item / a.h_kv);
-        const int b = __builtin_amdgcn_readfirstlane(request_of<1>(a.req, token, 0, lane));
+        Span s;
+        const int b = __builtin_amdgcn_readfirstlane(request_of_token(a.req, token, lane, s));
         if (b >= a.req.batch) return;
-        const Span s = span_of(a.req, b);
         if (token < s.first || token - s.first >= s.count) continue;
         const int pos = s.positions - s.count + token - s.first, sees = pos < 0 ? 0 : pos / kPage + 1;
         int *const out = a.selected + (size_t)item * a.count;
@@ -212,6 +260,19 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                 }
             }
             if constexpr (PHASE == kScores) continue;
+            if (mid1 - mid0 <= kPicked) {
+                __syncthreads();
+                if (wave == 0) {
+                    const float *from = PHASE == kList ? kept : scores;
+                    const int n = mid1 - mid0;
+                    if (n <= 512)
+                        pick<8>(from, mid0, mid1, k, lane, out + a.first);
+                    else if (n <= 1024)
+                        pick<16>(from, mid0, mid1, k, lane, out + a.first);
+                    else
+                        pick<32>(from, mid0, mid1, k, lane, out + a.first);
+                }
+            } else {
             if constexpr (PHASE == kList && IN_LDS)
                 for (int p = mid0 + (int)threadIdx.x; p < mid1; p += blockDim.x) scores[p] = kept[p];
             __syncthreads();
@@ -264,6 +325,7 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                     above += t0, level += t1;
                 }
                 if (is_above || (is_level && level_here < left)) out[a.first + above_here + min(level_here, left)] = p;
+            }
             }
         }
         if constexpr (PHASE == kScores) continue;

@@ -494,7 +494,10 @@ SELECT = [  # S, n, h_q, h_kv, d, first, last, count
     ([1], [3000], 40, 2, 64, 2, 3, 10),      # 20 heads on one
     ([70, 0, 2], [900, 5, 70], 3, 1, 128, 0, 1, 7),
     ([1], [20000], 4, 4, 64, 1, 1, 100),
-    ([1], [40000], 2, 1, 64, 0, 1, 600),     # more pages than a workgroup of few threads takes
+    ([1], [64 * 1026], 4, 4, 64, 1, 1, 500),  # 1024 to choose from
+    ([2], [64 * 2049], 2, 1, 64, 0, 1, 7),   # 2047 and 2048
+    ([1], [64 * 2051], 2, 1, 64, 1, 1, 900),
+    ([1], [40000], 2, 1, 64, 0, 1, 600),
     ([1, 1], [1000, 2000], 4, 2, 64, 5, 4, 9),  # nothing left to choose
     ([2], [200], 4, 2, 128, 0, 1, 50),       # fewer pages than asked for
 ]
@@ -527,7 +530,7 @@ def test_select_pages(S, n, h_q, h_kv, d, first, last, count, alike):
     req = _requests(S, n, table, rows=T)
     got = _select(req, q, h_q, cache, bounds, first, last, count, T).cpu().numpy()
     # the same with scores in the workspace: limits above what a workgroup has at once, and above what fits the LDS
-    for limit in (1500, 33000):
+    for limit in (3000, 33000):
         wide = np.full((len(n), limit), -1, np.int32)
         wide[:, :table.shape[1]] = table
         far = B.Requests(req.token_start, req.context, _i(wide), T, max(S), limit * 64)
