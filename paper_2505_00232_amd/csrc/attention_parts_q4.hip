@@ -20,6 +20,7 @@ struct PartsArgs {
     int h_q, h_kv, g;
     int prefix_parts, parts;  // slots: of common pages, and behind them of the others
     long prefix_items, items;  // of workgroups; items: all of them
+    bool wide;
     float scale;
 };
 
@@ -246,6 +247,325 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
     }
 }
 
+// ---- common pages of many rows.  What attention_q4_rows.h does to a page for 16 query rows, most of its instructions, is to take its codes apart: 551 vector instructions of a page and 16 rows,
+// of which 192 for that.  Here the four wavefronts of a workgroup take a page's codes apart once, into LDS as binary16 whole numbers code - 8 (exact, as are the products with the queries), and
+// multiply them with 16 NB rows each; steps, offsets and P are taken into the sums in the same way and the same precision as there:
+//   q . k = sum_j step_j (q_j . (code_j - 8)) + sum_j offset_j sum q_j,   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
+// The common pages are in front of all rows' positions: nothing is masked.
+template <int D>
+struct Wide {
+    typedef PageLayout<D> L;
+    static constexpr int G = L::G, W = L::W, DT = D / 16, NB = D == 256 ? 1 : 2, ROWS = 64 * NB;
+    // LDS: K operands [4 tiles][G][64 lanes], V operands [G][low, high][2 halves of 16 positions][64 lanes], 16 bytes each; then the page's steps and offsets of keys, and of values
+    static constexpr int kV = 128 * D, kHeadK = 256 * D, kHeadV = 264 * D, kBytes = 272 * D;
+    static constexpr int kStepK = kHeadK, kOffsetK = kHeadK + 4 * D, kStepV = kHeadV, kOffsetV = kHeadV + 4 * D;
+    // A page on its way: what a thread has of it
+    static constexpr int kPiecesK = 4 * (G / W) * 64, kPiecesV = G * 64, PK = (kPiecesK + 255) / 256, PV = (kPiecesV + 255) / 256;
+    typedef uint32_t words __attribute__((ext_vector_type(W)));
+    words k[PK];
+    u32x4 v[PV], head;
+    __device__ __forceinline__ void fetch(const char *page) {
+#pragma unroll
+        for (int i = 0; i < PK; ++i) k[i] = *reinterpret_cast<const words *>(page + L::kCodesK + (256 * i + (int)threadIdx.x) * (4 * W));
+#pragma unroll
+        for (int i = 0; i < PV; ++i) v[i] = *reinterpret_cast<const u32x4 *>(page + L::kCodesV + min(256 * i + (int)threadIdx.x, kPiecesV - 1) * 16);
+        const int piece = min((int)threadIdx.x, D - 1);  // D / 2 pieces of 16 bytes of keys' steps and offsets, then of values'
+        head = *reinterpret_cast<const u32x4 *>(page + (piece < D / 2 ? L::kStepK + piece * 16 : L::kStepV + (piece - D / 2) * 16));
+    }
+    // two codes, 16 bits apart, as binary16 code - 8
+    __device__ static __forceinline__ uint32_t two(uint32_t w) {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        const h2 x = __builtin_bit_cast(h2, (w & 0x000F000Fu) | 0x64006400u);  // 1024 + code
+        return __builtin_bit_cast(uint32_t, x - h2{(_Float16)1032.0f, (_Float16)1032.0f});
+    }
+    __device__ __forceinline__ void put(char *lds) const {
+#pragma unroll
+        for (int i = 0; i < PK; ++i) {
+            const int piece = 256 * i + (int)threadIdx.x, lane = piece % 64, tile = piece / 64 / (G / W), j0 = piece / 64 % (G / W) * W;
+#pragma unroll
+            for (int w = 0; w < W; ++w) *reinterpret_cast<u32x4 *>(lds + ((tile * G + j0 + w) * 64 + lane) * 16) = u32x4{two(k[i][w]), two(k[i][w] >> 4), two(k[i][w] >> 8), two(k[i][w] >> 12)};
+        }
+#pragma unroll
+        for (int i = 0; i < PV; ++i) {
+            const int piece = 256 * i + (int)threadIdx.x, lane = piece % 64, j = piece / 64;
+            if (kPiecesV % 256 != 0 && piece >= kPiecesV) break;
+#pragma unroll
+            for (int high = 0; high < 2; ++high)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t a = v[i][2 * u] >> (4 * high), b = v[i][2 * u + 1] >> (4 * high);
+                    *reinterpret_cast<u32x4 *>(lds + kV + (((j * 2 + high) * 2 + u) * 64 + lane) * 16) = u32x4{two(a), two(a >> 8), two(b), two(b >> 8)};
+                }
+        }
+        if ((int)threadIdx.x < D) *reinterpret_cast<u32x4 *>(lds + kHeadK + threadIdx.x * 16) = head;
+    }
+};
+
+// The state of NB blocks of 16 rows, lane (m, r) as in Rows
+template <int D>
+struct WideRows {
+    typedef Wide<D> S;
+    static constexpr int G = S::G, DT = S::DT, NB = S::NB;
+    const int lane, m, r;
+    h8 qf[NB][G], sums[NB];
+    float to_score[NB], run_max[NB];
+    v4f acc[NB][DT], rest[NB];
+    int factor;  // log 2 of what P is multiplied with in acc (in rest: kFactor)
+    __device__ __forceinline__ WideRows(int l) : lane(l), m(l & 15), r(l >> 4), factor((int)kFactor) {}
+
+    __device__ __forceinline__ void load(int nb, const _Float16 *q, bool real, float scale) {
+        float top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            const h8 zero = {};
+            qf[nb][j] = real ? *reinterpret_cast<const h8 *>(q + 32 * j + 8 * r) : zero;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)qf[nb][j][e]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        // the largest to 2^9 .. 2^10: 32 of them add up to what binary16 holds, and what it loses of the smallest is 2^-34 of the largest
+        const int up = top > 0.0f ? 10 - __builtin_amdgcn_frexp_expf(top) : 0;
+        const float up2 = __builtin_amdgcn_ldexpf(1.0f, up);
+        to_score[nb] = __builtin_amdgcn_ldexpf(scale, -up);
+        sums[nb] = h8{};
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = (float)qf[nb][j][e] * up2;
+                s += x;
+                qf[nb][j][e] = (_Float16)x;
+            }
+            s += __shfl_xor(s, 16, 64);
+            s += __shfl_xor(s, 32, 64);
+            const _Float16 hi = (_Float16)s, lo = (_Float16)(s - (float)hi);
+            sums[nb][j] = r == 0 ? hi : r == 1 ? lo : (_Float16)0.0f;
+        }
+        run_max[nb] = kNothingYet;
+        rest[nb] = v4f{};
+#pragma unroll
+        for (int t = 0; t < DT; ++t) acc[nb][t] = v4f{};
+    }
+
+    typedef __attribute__((address_space(3))) const char *Lds;
+    template <class T>
+    __device__ static __forceinline__ T read(Lds at) {
+        return *reinterpret_cast<__attribute__((address_space(3))) const T *>(at);
+    }
+    // The operands of a lane are at constant distances from four addresses.  (Nothing says so to the compiler but that it does not know the four: it kept some hundred sums in registers otherwise, from
+    // page to page, and had to spill.)
+    Lds at16, at_r, at_m, at_rows, at_lane;
+    __device__ __forceinline__ void page(const char *lds) {
+        const Lds base = (Lds)lds;
+        at16 = base + 16 * lane, at_r = base + 32 * r, at_m = base + 2 * G * m, at_rows = base + min(m, G - 1) * (2 * kPage) + 32 * r, at_lane = base + 4 * lane;
+        asm volatile("" : "+v"(at16), "+v"(at_r), "+v"(at_m), "+v"(at_rows), "+v"(at_lane));
+        // ---- scores; lane (m, r), element 4 t + i: position 16 r + 4 t + i
+        float sc[NB][16];
+        {
+            v4f part[NB][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                typedef _Float16 offsets __attribute__((ext_vector_type(G)));
+                const offsets x = read<offsets>(at_m + S::kOffsetK + 32 * G * t);  // (whatever r: the sums of q are 0 behind the first two)
+                h8 off = {};
+#pragma unroll
+                for (int j = 0; j < G; ++j) off[j] = x[j];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) part[nb][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, sums[nb], v4f{}, 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                const h8 st[2] = {read<h8>(at_r + S::kStepK + j * kPage * 2), read<h8>(at_r + S::kStepK + j * kPage * 2 + 16)};
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const h8 op = read<h8>(at16 + (t * G + j) * 1024);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, qf[nb][j], v4f{}, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) part[nb][t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[nb][t][i]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[nb][e] = part[nb][e >> 2][e & 3];
+        }
+        // ---- P, 2^kFactor times as large
+        // (one branch for all blocks: behind a branch for the first, the compiler put off the sums of the second and kept every product that they are made of)
+        h8 pv[NB][2];
+        float most[NB];
+        bool more = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            most[nb] = fmaxf(sc[nb][0], sc[nb][1]);
+#pragma unroll
+            for (int e = 2; e < 16; e += 2) most[nb] = fmaxf(fmaxf(most[nb], sc[nb][e]), sc[nb][e + 1]);
+            most[nb] = fmaxf(most[nb], __shfl_xor(most[nb], 16, 64));
+            most[nb] = fmaxf(most[nb], __shfl_xor(most[nb], 32, 64)) * to_score[nb];
+            more = more || most[nb] > run_max[nb];
+        }
+        if (__any(more)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const float new_max = fmaxf(run_max[nb], most[nb]), corr = __builtin_amdgcn_exp2f(run_max[nb] - new_max);
+                run_max[nb] = new_max;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) acc[nb][t][i] *= corr;
+                    rest[nb][i] *= corr;
+                }
+            }
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const float from_max = kFactor - run_max[nb];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                sc[nb][e] = __builtin_amdgcn_exp2f(fmaf(sc[nb][e], to_score[nb], from_max));
+                pv[nb][e >> 3][e & 7] = (_Float16)sc[nb][e];
+            }
+        }
+        // ---- second product
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {  // rows 0 .. G - 1: offsets; row 15: ones; the others are not used
+            const u32x4 w = read<u32x4>(at_rows + S::kOffsetV + 16 * u);
+            const u32x4 rows = {m == 15 ? 0x3C003C00u : w.x, m == 15 ? 0x3C003C00u : w.y, m == 15 ? 0x3C003C00u : w.z, m == 15 ? 0x3C003C00u : w.w};
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) rest[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, rows), pv[nb][u], rest[nb], 0, 0, 0);
+        }
+        // Products of P and a step stay below 2^15: with steps of 2 and more the sums are of P 2^factor, from there on
+        uint32_t bits = 0;
+#pragma unroll
+        for (int j = 0; j < G; j += 2) bits |= read<uint32_t>(at_lane + S::kStepV + j * kPage * 2);  // (two groups' steps are 64 dwords)
+        if (__any((bits & 0x40004000u) != 0)) {
+            float most = 0.0f;
+#pragma unroll
+            for (int j = 0; j < G; ++j) most = fmaxf(most, (float)read<_Float16>(at_lane - 2 * lane + S::kStepV + j * kPage * 2));
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
+            const int to = min(factor, 15 - __builtin_amdgcn_frexp_expf(most));
+            const float by = __builtin_amdgcn_ldexpf(1.0f, to - factor);
+            factor = __builtin_amdgcn_readfirstlane(to);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[nb][t][i] *= by;
+        }
+        if (factor != (int)kFactor) {
+            const float by = __builtin_amdgcn_ldexpf(1.0f, factor - (int)kFactor);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[nb][e] *= by;
+        }
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            __builtin_amdgcn_sched_barrier(0);  // (a group after the other: registers)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const h8 step = read<h8>(at_r + S::kStepV + j * kPage * 2 + 16 * u), lo = read<h8>(at16 + S::kV + (4 * j + u) * 1024), hi = read<h8>(at16 + S::kV + (4 * j + 2 + u) * 1024);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    h8 p;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[nb][8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
+                    acc[nb][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, p, acc[nb][2 * j], 0, 0, 0);
+                    acc[nb][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, p, acc[nb][2 * j + 1], 0, 0, 0);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ float sum(int nb) const { return __shfl(rest[nb][3], 48 + m, 64); }
+    template <class Put>
+    __device__ __forceinline__ void columns(int nb, const Put &put) const {
+        const float back = __builtin_amdgcn_ldexpf(1.0f, (int)kFactor - factor);
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            const float off = __shfl(rest[nb][j & 3], (j >> 2) * 16 + m, 64);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                v4f o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = fmaf(acc[nb][2 * j + k][i], back, off);
+                put(32 * j + 16 * k + 4 * r, o);
+            }
+        }
+    }
+};
+
+// A workgroup per part of 64 NB rows of a group.  (A kernel of its own: beside the other path's state it had no registers for loads that are ahead of their use.)
+template <int D>
+__global__ __launch_bounds__(256, 2) void attn_q4_wide_kernel(PartsArgs a) {
+    typedef Wide<D> S;
+    constexpr int NB = S::NB;
+    extern __shared__ char wide_lds[];
+    char *const lds = wide_lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long x = blockIdx.x;
+    const int kv = (int)(x % a.h_kv), part = (int)(x / a.h_kv % a.prefix_parts), block = (int)(x / a.h_kv / a.prefix_parts);
+    const Found f = find(block, a.groups, lane, [&](int i) __attribute__((always_inline)) { return (int)(((long)tokens_of_group(a, i) * a.g + S::ROWS - 1) / S::ROWS); });
+    if (f.run < 0) return;
+    const Group group = group_of(a, f.run, lane);
+    const int first = token_at(a, group_end(a, f.run)), rows_all = tokens_of_group(a, f.run) * a.g;
+    const long all_rows = (long)a.req.tokens * a.h_q;
+    const int per = max(1, (group.pages + a.prefix_parts - 1) / a.prefix_parts), from = min(part * per, group.pages), to = min(from + per, group.pages);
+    WideRows<D> rows(lane);
+    size_t out_row[NB];
+    bool real[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int row = f.place * S::ROWS + (wave * NB + nb) * 16 + rows.m, held = min(row, rows_all - 1);
+        real[nb] = row < rows_all;
+        const size_t at = (size_t)(first + held / a.g) * a.h_q + kv * a.g + held % a.g;
+        out_row[nb] = (size_t)part * all_rows + at;
+        if (from < to) rows.load(nb, a.q + at * D, real[nb], a.scale);
+        if (from >= to && rows.r == 0 && real[nb]) a.ws_ml[out_row[nb] * 2 + 1] = 0.0f;
+    }
+    if (from >= to) return;
+    // the next page that there is, from place i on; a lane knows one of 64 places
+    int numbers = -1, known = from - 64;
+    auto following = [&](int &i) __attribute__((always_inline)) {
+        for (;; ++i) {
+            if (i >= to) return -1;
+            if (i >= known + 64) {
+                known = i;
+                numbers = i + lane < to ? page_of(a.req, group.lead, (i + lane) * kPage) : -1;
+            }
+            const int page = __builtin_amdgcn_readlane(numbers, i - known);
+            if (page >= 0) return page;
+        }
+    };
+    int i = from, page = following(i);
+    S raw;
+    auto fetch = [&](int of) __attribute__((always_inline)) { raw.fetch(a.pages + ((size_t)of * a.h_kv + kv) * PageLayout<D>::kBytes); };
+    if (page >= 0) fetch(page);
+    while (page >= 0) {
+        ++i;
+        const int next = following(i);
+        raw.put(lds);
+        __syncthreads();
+        if (next >= 0) fetch(next);
+        rows.page(lds);
+        __syncthreads();
+        page = next;
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const float l = rows.sum(nb);
+        if (!real[nb]) continue;
+        rows.columns(nb, [&](int d, const v4f &o) __attribute__((always_inline)) { *reinterpret_cast<v4f *>(a.ws_o + out_row[nb] * D + d) = o; });
+        if (rows.r == 0) a.ws_ml[out_row[nb] * 2] = rows.run_max[nb], a.ws_ml[out_row[nb] * 2 + 1] = l;
+    }
+}
+
 // ---- common pages.  A workgroup per part of the rows of a group or a request.
 template <int D>
 __global__ __launch_bounds__(256, kWgs) void attn_q4_parts_kernel(PartsArgs a) {
@@ -334,9 +654,17 @@ __global__ __launch_bounds__(256) void attn_q4_join_kernel(PartsArgs a) {
 constexpr long kMostWgs = 1L << 22;  // (a launch has fewer than 2^32 threads)
 template <int D>
 hipError_t launch(const PartsArgs &a, hipStream_t st) {
+    PartsArgs rest = a;
+    if (a.wide) {
+        constexpr size_t lds = Wide<D>::kBytes;
+        if (const hipError_t e = allow_dynamic_lds<attn_q4_wide_kernel<D>>(lds); e != hipSuccess) return e;
+        attn_q4_wide_kernel<D><<<(unsigned)a.prefix_items, 256, lds, st>>>(a);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        rest.items -= a.prefix_items, rest.prefix_items = 0;
+    }
     constexpr size_t lds = Place<D>::LDS;
     if (const hipError_t e = allow_dynamic_lds<attn_q4_parts_kernel<D>>(lds); e != hipSuccess) return e;
-    attn_q4_parts_kernel<D><<<(unsigned)(a.items < kMostWgs ? a.items : kMostWgs), 256, lds, st>>>(a);
+    attn_q4_parts_kernel<D><<<(unsigned)(rest.items < kMostWgs ? rest.items : kMostWgs), 256, lds, st>>>(rest);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const long joins = ((long)a.req.tokens * a.h_q + 1024 / D - 1) / (1024 / D);
     attn_q4_join_kernel<D><<<(unsigned)(joins < kMostWgs ? joins : kMostWgs), 256, 0, st>>>(a);
@@ -363,6 +691,7 @@ hipError_t launch(const Args &a, int d, hipStream_t st) {
 }
 
 constexpr int kMostParts = 16;
+constexpr int kWideFrom = 48;  // rows of a group and KV head from which on pages are taken apart for a workgroup
 // Workgroups that share a block's pages: as many as fill the card, each with a page per wavefront at least
 int parts_of(long blocks, int pages, int num_cus) {
     const long fill = ((long)kWgs * num_cus + blocks - 1) / (blocks > 0 ? blocks : 1), most = (pages + 3) / 4;
@@ -389,7 +718,9 @@ SelectedPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, in
 AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv, int d, int max_tokens, int max_context, int groups, int group_tokens, int longest, int num_cus) {
     AttnPartsPlan p = {};
     const int g = h_q / h_kv;
-    const long by_group = (long)groups * (((long)group_tokens * g + 15) / 16), by_token = ((long)tokens * g + 15) / 16 + groups;
+    p.wide = (long)group_tokens * g >= kWideFrom;
+    const int rows = !p.wide ? 16 : d == 256 ? Wide<256>::ROWS : Wide<128>::ROWS;
+    const long by_group = (long)groups * (((long)group_tokens * g + rows - 1) / rows), by_token = ((long)tokens * g + rows - 1) / rows + groups;
     p.prefix_blocks = by_group < by_token ? by_group : by_token;
     p.blocks = max_tokens * g <= 16 ? batch : ((long)tokens * g + 15) / 16 + batch;
     p.prefix_parts = parts_of(p.prefix_blocks * h_kv, (longest < max_context ? longest : max_context) / kPage, num_cus);
@@ -422,7 +753,7 @@ hipError_t launch_attention_shared_q4(const void *q, const Requests &req, int h_
     a.pages = static_cast<const char *>(pages);
     a.req = req;
     a.group_start = group_start, a.prefix = prefix, a.groups = groups, a.group_tokens = group_tokens, a.longest = longest;
-    a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv;
+    a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv, a.wide = p.wide;
     a.prefix_parts = p.prefix_parts, a.parts = p.parts;
     a.prefix_items = p.prefix_blocks * h_kv * p.prefix_parts;
     a.items = a.prefix_items + p.blocks * h_kv * p.parts;
