@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
 template <int D>
 struct Wide {
     typedef PageLayout<D> L;
-    static constexpr int G = L::G, W = L::W, DT = D / 16, NB = D == 256 ? 1 : 2, ROWS = 64 * NB;
+    static constexpr int G = L::G, W = L::W, DT = D / 16, NB = D == 256 ? 1 : 2, ROWS = 64 * NB, BUFFERS = D == 256 ? 1 : 2;
     // LDS: K operands [4 tiles][G][64 lanes], V operands [G][low, high][2 halves of 16 positions][64 lanes], 16 bytes each; then the page's steps and offsets of keys, and of values
     static constexpr int kV = 128 * D, kHeadK = 256 * D, kHeadV = 264 * D, kBytes = 272 * D;
     static constexpr int kStepK = kHeadK, kOffsetK = kHeadK + 4 * D, kStepV = kHeadV, kOffsetV = kHeadV + 4 * D;
@@ -275,7 +275,7 @@ struct Wide {
     // two codes, 16 bits apart, as binary16 code - 8
     __device__ static __forceinline__ uint32_t two(uint32_t w) {
         typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-        const h2 x = __builtin_bit_cast(h2, (w & 0x000F000Fu) | 0x64006400u);  // 1024 + code
+        const h2 x = __builtin_bit_cast(h2, __builtin_amdgcn_bitop3_b32(w, 0x000F000Fu, 0x64006400u, 0xEA));  // 1024 + code
         return __builtin_bit_cast(uint32_t, x - h2{(_Float16)1032.0f, (_Float16)1032.0f});
     }
     __device__ __forceinline__ void put(char *lds) const {
@@ -375,20 +375,29 @@ struct WideRows {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) part[nb][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(off, sums[nb], v4f{}, 0, 0, 0);
             }
+            // (operands of a group are asked for while the one before is worked on)
+            h8 op[2][4], st[2][2];
+            auto ask = [&](int j) __attribute__((always_inline)) {
+                st[j & 1][0] = read<h8>(at_r + S::kStepK + j * kPage * 2), st[j & 1][1] = read<h8>(at_r + S::kStepK + j * kPage * 2 + 16);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) op[j & 1][t] = read<h8>(at16 + (t * G + j) * 1024);
+            };
+            ask(0);
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 __builtin_amdgcn_sched_barrier(0);
-                const h8 st[2] = {read<h8>(at_r + S::kStepK + j * kPage * 2), read<h8>(at_r + S::kStepK + j * kPage * 2 + 16)};
+                if (j + 1 < G) ask(j + 1);
+                v4f x[NB][4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const h8 op = read<h8>(at16 + (t * G + j) * 1024);
+                for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) {
-                        const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, qf[nb][j], v4f{}, 0, 0, 0);
+                    for (int nb = 0; nb < NB; ++nb) x[nb][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op[j & 1][t], qf[nb][j], v4f{}, 0, 0, 0);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) part[nb][t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[nb][t][i]);
-                    }
-                }
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) part[nb][t][i] = fmaf((float)st[j & 1][t >> 1][4 * (t & 1) + i], x[nb][t][i], part[nb][t][i]);
             }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
@@ -405,9 +414,8 @@ struct WideRows {
             most[nb] = fmaxf(sc[nb][0], sc[nb][1]);
 #pragma unroll
             for (int e = 2; e < 16; e += 2) most[nb] = fmaxf(fmaxf(most[nb], sc[nb][e]), sc[nb][e + 1]);
-            most[nb] = fmaxf(most[nb], __shfl_xor(most[nb], 16, 64));
-            most[nb] = fmaxf(most[nb], __shfl_xor(most[nb], 32, 64)) * to_score[nb];
-            more = more || most[nb] > run_max[nb];
+            most[nb] = over_rows(most[nb]) * to_score[nb];
+            more = more || most[nb] > run_max[nb] + 3.0f;
         }
         if (__any(more)) {
 #pragma unroll
@@ -466,20 +474,24 @@ struct WideRows {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sc[nb][e] *= by;
         }
+        h8 step[2], lo[2], hi[2];
+        auto ask = [&](int k) __attribute__((always_inline)) {
+            const int j = k / 2, u = k % 2;
+            step[u] = read<h8>(at_r + S::kStepV + j * kPage * 2 + 16 * u), lo[u] = read<h8>(at16 + S::kV + (4 * j + u) * 1024), hi[u] = read<h8>(at16 + S::kV + (4 * j + 2 + u) * 1024);
+        };
+        ask(0);
 #pragma unroll
-        for (int j = 0; j < G; ++j) {
-            __builtin_amdgcn_sched_barrier(0);  // (a group after the other: registers)
+        for (int k = 0; k < 2 * G; ++k) {
+            const int j = k / 2, u = k % 2;
+            __builtin_amdgcn_sched_barrier(0);  // (one after the other: registers)
+            if (k + 1 < 2 * G) ask(k + 1);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const h8 step = read<h8>(at_r + S::kStepV + j * kPage * 2 + 16 * u), lo = read<h8>(at16 + S::kV + (4 * j + u) * 1024), hi = read<h8>(at16 + S::kV + (4 * j + 2 + u) * 1024);
+            for (int nb = 0; nb < NB; ++nb) {
+                h8 p;
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    h8 p;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[nb][8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
-                    acc[nb][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, p, acc[nb][2 * j], 0, 0, 0);
-                    acc[nb][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, p, acc[nb][2 * j + 1], 0, 0, 0);
-                }
+                for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[nb][8 * u + e], (float)step[u][e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
+                acc[nb][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[u], p, acc[nb][2 * j], 0, 0, 0);
+                acc[nb][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[u], p, acc[nb][2 * j + 1], 0, 0, 0);
             }
         }
     }
@@ -547,15 +559,36 @@ __global__ __launch_bounds__(256, 2) void attn_q4_wide_kernel(PartsArgs a) {
     S raw;
     auto fetch = [&](int of) __attribute__((always_inline)) { raw.fetch(a.pages + ((size_t)of * a.h_kv + kv) * PageLayout<D>::kBytes); };
     if (page >= 0) fetch(page);
-    while (page >= 0) {
-        ++i;
-        const int next = following(i);
-        raw.put(lds);
-        __syncthreads();
-        if (next >= 0) fetch(next);
-        rows.page(lds);
-        __syncthreads();
-        page = next;
+    if constexpr (S::BUFFERS == 2) {  // the next page is taken apart into the other place: one barrier per page
+        char *now = lds, *other = lds + S::kBytes;
+        if (page >= 0) {
+            raw.put(now);
+            ++i;
+            page = following(i);
+            if (page >= 0) fetch(page);
+            for (;;) {
+                __syncthreads();
+                rows.page(now);
+                if (page < 0) break;
+                raw.put(other);
+                ++i;
+                page = following(i);
+                if (page >= 0) fetch(page);
+                char *const x = now;
+                now = other, other = x;
+            }
+        }
+    } else {
+        while (page >= 0) {
+            ++i;
+            const int next = following(i);
+            raw.put(lds);
+            __syncthreads();
+            if (next >= 0) fetch(next);
+            rows.page(lds);
+            __syncthreads();
+            page = next;
+        }
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -568,7 +601,7 @@ __global__ __launch_bounds__(256, 2) void attn_q4_wide_kernel(PartsArgs a) {
 
 // ---- common pages.  A workgroup per part of the rows of a group or a request.
 template <int D>
-__global__ __launch_bounds__(256, kWgs) void attn_q4_parts_kernel(PartsArgs a) {
+__global__ __launch_bounds__(256, D <= 128 ? 3 : kWgs) void attn_q4_parts_kernel(PartsArgs a) {
     extern __shared__ float lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long all_rows = (long)a.req.tokens * a.h_q;
@@ -621,7 +654,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_parts_kernel(PartsArgs a) {
             continue;
         }
         // ---- this wavefront's quarter
-        const int share = (to - from + 3) / 4, begin = min(from + wave * share, to), count = __builtin_amdgcn_readfirstlane(min(begin + share, to) - begin);
+        const int begin = from + (to - from) * wave / 4, count = __builtin_amdgcn_readfirstlane(from + (to - from) * (wave + 1) / 4 - begin);
         auto numbers = [&](int i) __attribute__((always_inline)) { return i + lane < count ? page_of(a.req, b, (begin + i + lane) * kPage) : -1; };
         const int ahead = numbers(0);
         rows.load(a.q + at * D, real, a.scale);
@@ -656,7 +689,7 @@ template <int D>
 hipError_t launch(const PartsArgs &a, hipStream_t st) {
     PartsArgs rest = a;
     if (a.wide) {
-        constexpr size_t lds = Wide<D>::kBytes;
+        constexpr size_t lds = Wide<D>::kBytes * Wide<D>::BUFFERS;
         if (const hipError_t e = allow_dynamic_lds<attn_q4_wide_kernel<D>>(lds); e != hipSuccess) return e;
         attn_q4_wide_kernel<D><<<(unsigned)a.prefix_items, 256, lds, st>>>(a);
         if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -691,7 +724,7 @@ hipError_t launch(const Args &a, int d, hipStream_t st) {
 }
 
 constexpr int kMostParts = 16;
-constexpr int kWideFrom = 48;  // rows of a group and KV head from which on pages are taken apart for a workgroup
+constexpr int kWideFrom = 512;  // rows of a group and KV head from which on pages are taken apart for a workgroup
 // Workgroups that share a block's pages: as many as fill the card, each with a page per wavefront at least
 int parts_of(long blocks, int pages, int num_cus) {
     const long fill = ((long)kWgs * num_cus + blocks - 1) / (blocks > 0 ? blocks : 1), most = (pages + 3) / 4;
