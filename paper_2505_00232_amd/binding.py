@@ -594,18 +594,22 @@ def _table(t: torch.Tensor, what: str):
     """A matrix of page numbers: (rows, entries of a row)."""
     if not (isinstance(t, _Tensor) and t.dim() == 2):
         raise ValueError(f"{what}: a matrix is required")
-    batch, width = t.shape
-    _want(t, _i32, (batch, width), what)
-    return batch, width
+    shape = t.shape
+    _want(t, _i32, shape, what)
+    return shape
 
 
-def _numbers(t: torch.Tensor | None, count: int, what: str, *devices):
-    """int32 [count] (or None, for an argument that may be left out) on the current device, like everything else of the call: its address."""
-    if t is not None:
-        _want(t, _i32, (count,), what)
-        devices += (t.get_device(),)
-    _here(*devices)
-    return t.data_ptr() if t is not None else None
+def _numbers(count: int, *named, devices=()):
+    """int32 tensors of `count` numbers (name, tensor; None: left out), on the current device like everything else of the call."""
+    dev = _device() if _device is not None else torch.cuda.current_device()
+    for what, t in named:
+        if t is None and what in ("missing", "keep", "used") or isinstance(t, _Tensor) and t.dtype is _i32 and t.is_contiguous() and t.shape == (count,) and t.get_device() == dev:
+            continue
+        _look_again(t, _i32, (count,), what)
+        _here(t.get_device())
+    for d in devices:
+        if d != dev:
+            _here(d)
 
 
 def qfc_pages_workspace_size(cache: PagedCache, batch: int) -> int:
@@ -619,19 +623,19 @@ def qfc_copy_pages(source_cache: PagedCache, target_cache: PagedCache, source: t
     if not (isinstance(source, _Tensor) and source.dim() == 1):
         raise ValueError("source: a vector is required")
     count = source.shape[0]
-    s = _numbers(source, count, "source", source_cache.device)
-    t = _numbers(target, count, "target", target_cache.device)
-    _check(lib().qfc_copy_pages(source_cache.ref, target_cache.ref, s, t, count, _stream()), "qfc_copy_pages")
+    _numbers(count, ("source", source), ("target", target), devices=(source_cache.device, target_cache.device))
+    _check(lib().qfc_copy_pages(source_cache.ref, target_cache.ref, source.data_ptr(), target.data_ptr(), count, _stream()), "qfc_copy_pages")
 
 
 def qfc_take_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, positions: torch.Tensor, workspace: torch.Tensor, missing: torch.Tensor | None = None):
     """Free pages for the first positions[b] positions of each row that lack one."""
     batch, width = _table(page_table, "page_table")
     _want(workspace, _u8, None, "workspace")
-    r = _numbers(references, cache.num_pages, "references", cache.device, page_table.get_device(), workspace.get_device())
-    p = _numbers(positions, batch, "positions")
-    m = _numbers(missing, 1, "missing")
-    _check(lib().qfc_take_pages(cache.ref, r, page_table.data_ptr(), p, batch, width, m, workspace.data_ptr(), workspace.numel(), _stream()), "qfc_take_pages")
+    _numbers(cache.num_pages, ("references", references), devices=(cache.device, page_table.get_device(), workspace.get_device()))
+    _numbers(batch, ("positions", positions))
+    _numbers(1, ("missing", missing))
+    _check(lib().qfc_take_pages(cache.ref, references.data_ptr(), page_table.data_ptr(), positions.data_ptr(), batch, width, _ptr(missing), workspace.data_ptr(), workspace.numel(), _stream()),
+           "qfc_take_pages")
 
 
 def qfc_fork_pages(cache: PagedCache, references: torch.Tensor, from_table: torch.Tensor, parents: torch.Tensor, positions: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor,
@@ -640,28 +644,28 @@ def qfc_fork_pages(cache: PagedCache, references: torch.Tensor, from_table: torc
     from_batch, from_width = _table(from_table, "from_table")
     batch, width = _table(page_table, "page_table")
     _want(workspace, _u8, None, "workspace")
-    r = _numbers(references, cache.num_pages, "references", cache.device, from_table.get_device(), page_table.get_device(), workspace.get_device())
-    f, p = _numbers(parents, batch, "parents"), _numbers(positions, batch, "positions")
-    m = _numbers(missing, 1, "missing")
-    _check(lib().qfc_fork_pages(cache.ref, r, from_table.data_ptr(), from_batch, from_width, f, p, page_table.data_ptr(), batch, width, m, workspace.data_ptr(), workspace.numel(), _stream()),
-           "qfc_fork_pages")
+    _numbers(cache.num_pages, ("references", references), devices=(cache.device, from_table.get_device(), page_table.get_device(), workspace.get_device()))
+    _numbers(batch, ("parents", parents), ("positions", positions))
+    _numbers(1, ("missing", missing))
+    _check(lib().qfc_fork_pages(cache.ref, references.data_ptr(), from_table.data_ptr(), from_batch, from_width, parents.data_ptr(), positions.data_ptr(), page_table.data_ptr(), batch, width,
+                                _ptr(missing), workspace.data_ptr(), workspace.numel(), _stream()), "qfc_fork_pages")
 
 
 def qfc_free_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, keep: torch.Tensor | None = None):
     """Every row keeps the pages of its first keep[b] positions (None: of none) and lets the others go."""
     batch, width = _table(page_table, "page_table")
-    r = _numbers(references, cache.num_pages, "references", cache.device, page_table.get_device())
-    k = _numbers(keep, batch, "keep")
-    _check(lib().qfc_free_pages(cache.ref, r, page_table.data_ptr(), k, batch, width, _stream()), "qfc_free_pages")
+    _numbers(cache.num_pages, ("references", references), devices=(cache.device, page_table.get_device()))
+    _numbers(batch, ("keep", keep))
+    _check(lib().qfc_free_pages(cache.ref, references.data_ptr(), page_table.data_ptr(), _ptr(keep), batch, width, _stream()), "qfc_free_pages")
 
 
 def qfc_compact_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor, used: torch.Tensor | None = None):
     """The pages in use get the numbers from 0 on; page_table holds all rows that name pages of the cache."""
     batch, width = _table(page_table, "page_table")
     _want(workspace, _u8, None, "workspace")
-    r = _numbers(references, cache.num_pages, "references", cache.device, page_table.get_device(), workspace.get_device())
-    u = _numbers(used, 1, "used")
-    _check(lib().qfc_compact_pages(cache.ref, r, page_table.data_ptr(), batch, width, u, workspace.data_ptr(), workspace.numel(), _stream()), "qfc_compact_pages")
+    _numbers(cache.num_pages, ("references", references), devices=(cache.device, page_table.get_device(), workspace.get_device()))
+    _numbers(1, ("used", used))
+    _check(lib().qfc_compact_pages(cache.ref, references.data_ptr(), page_table.data_ptr(), batch, width, _ptr(used), workspace.data_ptr(), workspace.numel(), _stream()), "qfc_compact_pages")
 
 
 class SharedPrefixes:

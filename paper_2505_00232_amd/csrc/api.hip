@@ -833,6 +833,7 @@ void qfc_tune(int32_t key, int32_t value) {
     if (key == 13) t.attn_few = value;
     if (key == 14) t.attn_shares = value;
     if (key == 15) t.attn_q4_pages = value < 0 ? 0 : value;
+    if (key == 16) t.attn_wide_rows = value < 0 ? 0 : value;
     if (key == 12) t.attn_splits = value < 0 ? 0 : value > kAttnMaxSplits ? kAttnMaxSplits : value;
 }
 

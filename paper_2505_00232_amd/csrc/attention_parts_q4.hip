@@ -310,8 +310,10 @@ struct WideRows {
     h8 qf[NB][G], sums[NB];
     float to_score[NB], run_max[NB];
     v4f acc[NB][DT], rest[NB];
-    int factor;  // log 2 of what P is multiplied with in acc (in rest: kFactor)
-    __device__ __forceinline__ WideRows(int l) : lane(l), m(l & 15), r(l >> 4), factor((int)kFactor) {}
+    int factor;  // log 2 of what P is multiplied with in acc (in rest: kAt)
+    // The maximum may be kLag below a score (in units of log 2): what hardly moves it costs no pass over the sums.  P is then at most 2^(kAt + kLag) = 2^14.
+    static constexpr int kLag = 3, kAt = (int)kFactor - kLag;
+    __device__ __forceinline__ WideRows(int l) : lane(l), m(l & 15), r(l >> 4), factor(kAt) {}
 
     __device__ __forceinline__ void load(int nb, const _Float16 *q, bool real, float scale) {
         float top = 0.0f;
@@ -404,7 +406,7 @@ struct WideRows {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sc[nb][e] = part[nb][e >> 2][e & 3];
         }
-        // ---- P, 2^kFactor times as large
+        // ---- P, 2^kAt times as large
         // (one branch for all blocks: behind a branch for the first, the compiler put off the sums of the second and kept every product that they are made of)
         h8 pv[NB][2];
         float most[NB];
@@ -415,7 +417,7 @@ struct WideRows {
 #pragma unroll
             for (int e = 2; e < 16; e += 2) most[nb] = fmaxf(fmaxf(most[nb], sc[nb][e]), sc[nb][e + 1]);
             most[nb] = over_rows(most[nb]) * to_score[nb];
-            more = more || most[nb] > run_max[nb] + 3.0f;
+            more = more || most[nb] > run_max[nb] + (float)kLag;
         }
         if (__any(more)) {
 #pragma unroll
@@ -432,7 +434,7 @@ struct WideRows {
         }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const float from_max = kFactor - run_max[nb];
+            const float from_max = (float)kAt - run_max[nb];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 sc[nb][e] = __builtin_amdgcn_exp2f(fmaf(sc[nb][e], to_score[nb], from_max));
@@ -457,7 +459,7 @@ struct WideRows {
             for (int j = 0; j < G; ++j) most = fmaxf(most, (float)read<_Float16>(at_lane - 2 * lane + S::kStepV + j * kPage * 2));
 #pragma unroll
             for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
-            const int to = min(factor, 15 - __builtin_amdgcn_frexp_expf(most));
+            const int to = min(factor, 15 - kLag - __builtin_amdgcn_frexp_expf(most));
             const float by = __builtin_amdgcn_ldexpf(1.0f, to - factor);
             factor = __builtin_amdgcn_readfirstlane(to);
 #pragma unroll
@@ -467,8 +469,8 @@ struct WideRows {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[nb][t][i] *= by;
         }
-        if (factor != (int)kFactor) {
-            const float by = __builtin_amdgcn_ldexpf(1.0f, factor - (int)kFactor);
+        if (factor != kAt) {
+            const float by = __builtin_amdgcn_ldexpf(1.0f, factor - kAt);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -498,7 +500,7 @@ struct WideRows {
     __device__ __forceinline__ float sum(int nb) const { return __shfl(rest[nb][3], 48 + m, 64); }
     template <class Put>
     __device__ __forceinline__ void columns(int nb, const Put &put) const {
-        const float back = __builtin_amdgcn_ldexpf(1.0f, (int)kFactor - factor);
+        const float back = __builtin_amdgcn_ldexpf(1.0f, kAt - factor);
 #pragma unroll
         for (int j = 0; j < G; ++j) {
             const float off = __shfl(rest[nb][j & 3], (j >> 2) * 16 + m, 64);
@@ -595,7 +597,7 @@ __global__ __launch_bounds__(256, 2) void attn_q4_wide_kernel(PartsArgs a) {
         const float l = rows.sum(nb);
         if (!real[nb]) continue;
         rows.columns(nb, [&](int d, const v4f &o) __attribute__((always_inline)) { *reinterpret_cast<v4f *>(a.ws_o + out_row[nb] * D + d) = o; });
-        if (rows.r == 0) a.ws_ml[out_row[nb] * 2] = rows.run_max[nb], a.ws_ml[out_row[nb] * 2 + 1] = l;
+        if (rows.r == 0) a.ws_ml[out_row[nb] * 2] = rows.run_max[nb] + (float)WideRows<D>::kLag, a.ws_ml[out_row[nb] * 2 + 1] = l;  // (as of sums 2^kFactor times as large)
     }
 }
 
@@ -751,7 +753,8 @@ SelectedPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, in
 AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv, int d, int max_tokens, int max_context, int groups, int group_tokens, int longest, int num_cus) {
     AttnPartsPlan p = {};
     const int g = h_q / h_kv;
-    p.wide = (long)group_tokens * g >= kWideFrom;
+    const int forced = tuning().attn_wide_rows;
+    p.wide = (long)group_tokens * g >= (forced > 0 ? forced : kWideFrom);
     const int rows = !p.wide ? 16 : d == 256 ? Wide<256>::ROWS : Wide<128>::ROWS;
     const long by_group = (long)groups * (((long)group_tokens * g + rows - 1) / rows), by_token = ((long)tokens * g + rows - 1) / rows + groups;
     p.prefix_blocks = by_group < by_token ? by_group : by_token;

@@ -59,40 +59,43 @@ __device__ __forceinline__ Part part_of(const PagesArgs &a, int b) {
 
 // ---- first launch: free pages (workgroups up to chunks / 4), what rows lack (the others, a wavefront per row)
 enum { kTake = 0, kFork = 1, kCompact = 2 };
+__device__ __forceinline__ void count_chunk(const PagesArgs &a, int chunk, int lane) {
+    const long first = (long)chunk * kChunk;
+    int held[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) held[i] = a.references[min(first + 64 * i + lane, (long)a.num_pages - 1)];
+    uint64_t mine = 0;
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+        const uint64_t word = __ballot(held[i] <= 0 && first + 64 * i + lane < a.num_pages);
+        count += __popcll(word);
+        mine = lane == i ? word : mine;
+    }
+    if (lane < kWords) a.bits[(size_t)chunk * kWords + lane] = mine;
+    if (lane == 0) a.free_of[chunk] = count;
+}
+template <int KIND>
+__device__ __forceinline__ void count_row(const PagesArgs &a, int b, int lane) {
+    int lacks = 0;
+    if constexpr (KIND == kFork) {
+        lacks = part_of(a, b).page >= 0;
+    } else {
+        const int entries = pages_for(a.positions[b], a.width);
+        for (int e = lane; e < entries; e += 64) lacks += !is_page(a.table[(size_t)b * a.width + e], a.num_pages);
+        lacks = wave_sum(lacks);
+    }
+    if (lane == 0) a.need[b] = lacks;
+}
 template <int KIND>
 __global__ __launch_bounds__(256) void count_pages_kernel(PagesArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), counting = (a.chunks + 3) / 4;
     if ((int)blockIdx.x < counting) {
         const int chunk = (int)blockIdx.x * 4 + wave;
-        if (chunk >= a.chunks) return;
-        const long first = (long)chunk * kChunk;
-        int held[kWords];
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) held[i] = a.references[min(first + 64 * i + lane, (long)a.num_pages - 1)];
-        uint64_t mine = 0;
-        int count = 0;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) {
-            const uint64_t word = __ballot(held[i] <= 0 && first + 64 * i + lane < a.num_pages);
-            count += __popcll(word);
-            mine = lane == i ? word : mine;
-        }
-        if (lane < kWords) a.bits[(size_t)chunk * kWords + lane] = mine;
-        if (lane == 0) a.free_of[chunk] = count;
-        return;
-    }
-    if constexpr (KIND != kCompact) {
+        if (chunk < a.chunks) count_chunk(a, chunk, lane);
+    } else if constexpr (KIND != kCompact) {
         const int b = ((int)blockIdx.x - counting) * 4 + wave;
-        if (b >= a.batch) return;
-        int lacks = 0;
-        if constexpr (KIND == kFork) {
-            lacks = part_of(a, b).page >= 0;
-        } else {
-            const int entries = pages_for(a.positions[b], a.width);
-            for (int e = lane; e < entries; e += 64) lacks += !is_page(a.table[(size_t)b * a.width + e], a.num_pages);
-            lacks = wave_sum(lacks);
-        }
-        if (lane == 0) a.need[b] = lacks;
+        if (b < a.batch) count_row<KIND>(a, b, lane);
     }
 }
 
@@ -168,11 +171,8 @@ __device__ __forceinline__ void say_missing(const PagesArgs &a, int needed, int 
     if (lane == 0) *a.missing = max(needed - there, 0);
 }
 
-// A wavefront per row: pages for its entries that lack one.  Bound: latency (counts, chunk, bits, one after the other).
-__global__ __launch_bounds__(256) void take_pages_kernel(PagesArgs a) {
-    __shared__ int buffers[4][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = (int)blockIdx.x * 4 + wave;
-    if (b >= a.batch) return;
+// Pages for the entries of row b that lack one, by a wavefront
+__device__ __forceinline__ void take_row(const PagesArgs &a, int b, int lane, int *buffer) {
     const int need = a.need[b], before = sum_of(a.need, b, lane);
     if (b == a.batch - 1) say_missing(a, before + need, lane);
     if (need == 0) return;
@@ -184,12 +184,28 @@ __global__ __launch_bounds__(256) void take_pages_kernel(PagesArgs a) {
         const bool lacks = e < entries && !is_page(row[e], a.num_pages);
         const uint64_t all = __ballot(lacks);
         if (!all) continue;
-        const int page = __shfl(free_pages.next(__popcll(all), buffers[wave]), __popcll(all & ((1ull << lane) - 1)), 64);
+        const int page = __shfl(free_pages.next(__popcll(all), buffer), __popcll(all & ((1ull << lane) - 1)), 64);
         if (lacks) {
             row[e] = page;
             if (page >= 0) a.references[page] = 1;
         }
     }
+}
+// Bound: latency (counts, chunk, bits, one after the other)
+__global__ __launch_bounds__(256) void take_pages_kernel(PagesArgs a) {
+    __shared__ int buffers[4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = (int)blockIdx.x * 4 + wave;
+    if (b < a.batch) take_row(a, b, lane, buffers[wave]);
+}
+// Small pools and few rows: both steps in one launch, by one workgroup.  (A launch costs the host 2.7 us; with more rows the 16 wavefronts take longer than that one after the other.)
+constexpr int kSmallPool = 16 * kChunk, kFewRows = 64;
+__global__ __launch_bounds__(1024) void take_few_pages_kernel(PagesArgs a) {
+    __shared__ int buffers[16][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (wave < a.chunks) count_chunk(a, wave, lane);
+    for (int b = wave; b < a.batch; b += 16) count_row<kTake>(a, b, lane);
+    __syncthreads();  // (what the workgroup has written to memory is seen by all of it)
+    for (int b = wave; b < a.batch; b += 16) take_row(a, b, lane, buffers[wave]);
 }
 
 // Copies bytes [from, to) of a page, by the threads of a workgroup; both multiples of 16.  Four of a thread's loads on their way at once.
@@ -362,6 +378,10 @@ hipError_t launch_copy_pages(const void *from, int from_pages, void *to, int to_
 hipError_t launch_take_pages(const PagePool &pool, int *table, const int *positions, int batch, int width, int *missing, void *workspace, hipStream_t st) {
     PagesArgs a = args_of(pool, workspace, batch);
     a.table = table, a.positions = positions, a.width = width, a.missing = missing;
+    if (pool.num_pages <= kSmallPool && batch <= kFewRows) {
+        take_few_pages_kernel<<<1, 1024, 0, st>>>(a);
+        return hipGetLastError();
+    }
     count_pages_kernel<kTake><<<fours(a.chunks) + fours(batch), 256, 0, st>>>(a);
     take_pages_kernel<<<fours(batch), 256, 0, st>>>(a);
     return hipGetLastError();

@@ -141,6 +141,7 @@ struct Tuning {
     Tunable attn_few{-1};       // attention, blocks of 16 query rows: -1 automatic, 0 above 16 rows never, 1 always
     Tunable attn_splits{0};     // decode attention: workgroups per KV head (0: automatic)
     Tunable attn_q4_pages{0};   // attention over the 4-bit cache: pages a wavefront takes at least (0: automatic)
+    Tunable attn_wide_rows{0};  // rows of a group and KV head from which on its pages are taken apart for a workgroup (0 = automatic)
     Tunable gemv_half{-1};      // half-unit items of the decode kernel: -1 automatic, 0 never, 1 where possible
 };
 Tuning &tuning();

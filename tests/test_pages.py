@@ -365,9 +365,17 @@ SHARED = [  # group_start, positions, S, n, h_q, h_kv, d
 ]
 
 
+@pytest.fixture(params=["few", "many"])
+def rows_rule(request):
+    """Both paths for common pages, whatever the sizes."""
+    B.qfc_tune(16, 1 << 30 if request.param == "few" else 1)
+    yield request.param
+    B.qfc_tune(16, 0)
+
+
 @gpu
 @pytest.mark.parametrize("group,prefix,S,n,h_q,h_kv,d", SHARED)
-def test_attention_shared(group, prefix, S, n, h_q, h_kv, d):
+def test_attention_shared(group, prefix, S, n, h_q, h_kv, d, rows_rule):
     rng = np.random.default_rng(21)
     cache, table, K, V, P = _shared_batch(rng, group, prefix, S, n, h_kv, d)
     T, behind = sum(S), 3
@@ -392,7 +400,7 @@ def test_attention_shared(group, prefix, S, n, h_q, h_kv, d):
 
 
 @gpu
-def test_attention_shared_extremes():
+def test_attention_shared_extremes(rows_rule):
     """Pages that are missing, in the common part and behind it; a request that sees nothing; queries that are infinite or no numbers stay their own rows' matter; steps of 2 and more."""
     rng = np.random.default_rng(22)
     group, prefix, S, n, h_q, h_kv, d = [0, 3], [320], [1, 1, 1, 1], [400, 500, 330, 0], 4, 2, 64
@@ -434,7 +442,32 @@ def test_attention_shared_extremes():
 
 
 @gpu
-def test_attention_shared_arrays_that_break_the_rules_stay_inside():
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("rise", [0.3, 1.0, 2.0, 2.9, 3.1, -1.0])
+def test_attention_shared_maxima_that_move(d, rise, rows_rule):
+    """Scores that rise (or fall) from page to page by so many units of log 2, for some rows and not for others: what may lag behind the largest one does so by a bounded amount."""
+    rng = np.random.default_rng(24)
+    group, prefix, S, h_q, h_kv = [0, 5], [64 * 9], [1] * 5, 2, 1
+    n = [64 * 9 + 1 + 7 * i for i in range(5)]
+    table, num = _pages(rng, n)
+    k, v = _normal(rng, sum(n), h_kv, d) * np.float16(0.25), _normal(rng, sum(n), h_kv, d)
+    q = _normal(rng, 5, h_q * d)
+    q[:, ::d] = np.array([[0.0, 8.0], [8.0, -8.0], [4.0, 2.0], [8.0, 8.0], [-8.0, 1.0]], dtype=np.float16)
+    at = np.cumsum([0] + n[:-1])
+    for b in range(5):
+        k[at[b]:at[b] + n[b], 0, 0] = (np.arange(n[b]) // 64 * rise * np.log(2.0) * np.sqrt(d) / 8.0).astype(np.float16)
+        k[at[b]:at[b] + n[b], 0, 1:32] *= np.float16(0.1)
+    for b in range(1, 5):
+        table[b, :9] = table[0, :9]
+        k[at[b]:at[b] + 576], v[at[b]:at[b] + 576] = k[:576], v[:576]
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num, k, v)
+    got = _attend_shared(_requests(S, n, table), B.SharedPrefixes(_i(group), _i(prefix), 5, 576), q, h_q, cache).reshape(-1, h_q, d)
+    for b in range(5):
+        _close(got[b:b + 1], *q4.attention(q.reshape(-1, h_q, d)[b:b + 1], K[b], V[b], P[b]))
+
+
+@gpu
+def test_attention_shared_arrays_that_break_the_rules_stay_inside(rows_rule):
     rng = np.random.default_rng(23)
     group, prefix, S, n, h_q, h_kv, d = [0, 3], [320], [1, 1, 1], [400, 500, 330], 4, 2, 64
     cache, table, K, V, P = _shared_batch(rng, group, prefix, S, n, h_kv, d)
@@ -726,7 +759,7 @@ def test_a_search_behind_a_prompt_shares_its_pages():
 
 
 @gpu
-def test_captured_steps_follow_the_arrays():
+def test_captured_steps_follow_the_arrays(rows_rule):
     """Attention behind common pages, bounds, selection and attention over it in one graph; lengths, tables and groups change between replays."""
     rng = np.random.default_rng(63)
     h_q, h_kv, d, batch, width, count = 8, 2, 64, 4, 20, 4
@@ -781,7 +814,7 @@ def test_captured_steps_follow_the_arrays():
 
 
 @gpu
-def test_two_streams_with_workspaces_of_their_own():
+def test_two_streams_with_workspaces_of_their_own(rows_rule):
     rng = np.random.default_rng(64)
     group, prefix, S, n, h_q, h_kv, d = [0, 20], [640], [1] * 20, [641 + 9 * i for i in range(20)], 8, 2, 128
     cache, table, K, V, P = _shared_batch(rng, group, prefix, S, n, h_kv, d)
