@@ -48,9 +48,9 @@ struct Group {
     int lead, pages;  // the first one with tokens: its table's row is read
 };
 __device__ __forceinline__ int group_end(const PartsArgs &a, int i) { return min(max(a.group_start[i], 0), a.req.batch); }
-__device__ __forceinline__ int token_at(const PartsArgs &a, int b) { return min(max(a.req.start[b], 0), a.req.tokens); }
+__device__ __forceinline__ int token_at(const Requests &q, int b) { return min(max(q.start[b], 0), q.tokens); }
 __device__ __forceinline__ int tokens_of_group(const PartsArgs &a, int i) {
-    return min(max(token_at(a, group_end(a, i + 1)) - token_at(a, group_end(a, i)), 0), a.group_tokens);
+    return min(max(token_at(a.req, group_end(a, i + 1)) - token_at(a.req, group_end(a, i)), 0), a.group_tokens);
 }
 __device__ __forceinline__ Group group_of(const PartsArgs &a, int i, int lane) {
     const int first = group_end(a, i), end = group_end(a, i + 1);
@@ -172,17 +172,12 @@ struct SelectedArgs {
 struct Unit {
     long begin, end;
     int token, kv, head0;
-    Span span;
-    int b;
-    bool real;  // the token is a request's
 };
-__device__ __forceinline__ Unit unit_of(const SelectedArgs &a, long place, int lane) {
+__device__ __forceinline__ Unit unit_of(const SelectedArgs &a, long place) {
     Unit u;
     const long unit = place / a.count, block = unit / a.h_kv;
     u.begin = unit * a.count, u.end = u.begin + a.count;
     u.kv = (int)(unit % a.h_kv), u.head0 = (int)(block % a.head_blocks) * 16, u.token = (int)(block / a.head_blocks);
-    u.b = __builtin_amdgcn_readfirstlane(request_of_token(a.req, u.token, lane, u.span));
-    u.real = u.b < a.req.batch && u.token >= u.span.first && u.token - u.span.first < u.span.count;
     return u;
 }
 
@@ -194,24 +189,27 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArg
     const Four<D> four = {lds};
     const long from = blockIdx.x * a.share, stop = min(from + a.share, a.places);
     for (long x = from; x < stop;) {
-        const Unit u = unit_of(a, x, lane);
+        const Unit u = unit_of(a, x);
         const long last = min(stop, u.end);
         const int p0 = (int)(x - u.begin), p1 = (int)(last - u.begin);
         const bool whole = p0 == 0 && last == u.end;
         x = last;
-        if (!u.real) continue;
-        const int n = u.span.positions, lim = n - u.span.count + u.token - u.span.first + 1;
+        const int *const list = a.selected + ((size_t)u.token * a.h_kv + u.kv) * a.count;
+        const int begin = p0 + (int)((long)(p1 - p0) * wave / 4), count = __builtin_amdgcn_readfirstlane(p0 + (int)((long)(p1 - p0) * (wave + 1) / 4) - begin);
+        int place = lane < count ? list[begin + lane] : -1;  // of the page in its request, a page per lane; on its way before anything is known of the request
+        Span span;
+        const int b = __builtin_amdgcn_readfirstlane(request_of_token(a.req, u.token, lane, span));
+        if (b >= a.req.batch || u.token < span.first || u.token - span.first >= span.count) continue;
+        const int n = span.positions, lim = n - span.count + u.token - span.first + 1;
         const bool real = u.head0 + rows.m < a.g;
         const int head = u.kv * a.g + min(u.head0 + rows.m, a.g - 1);
         const size_t at = (size_t)u.token * a.h_q + head;
-        const int *const list = a.selected + ((size_t)u.token * a.h_kv + u.kv) * a.count;
-        const int begin = p0 + (int)((long)(p1 - p0) * wave / 4), count = __builtin_amdgcn_readfirstlane(p0 + (int)((long)(p1 - p0) * (wave + 1) / 4) - begin);
-        int place = -1;  // of the page in its request, a page per lane
+        auto page_at = [&](int of) __attribute__((always_inline)) { return of >= 0 && of < (a.req.max_context + kPage - 1) / kPage ? page_of(a.req, b, of * kPage) : -1; };
         auto numbers = [&](int i) __attribute__((always_inline)) {
             place = i + lane < count ? list[begin + i + lane] : -1;
-            return place >= 0 && place < (a.req.max_context + kPage - 1) / kPage ? page_of(a.req, u.b, place * kPage) : -1;
+            return page_at(place);
         };
-        const int ahead = numbers(0);
+        const int ahead = page_at(place);
         rows.load(a.q + at * D, real, a.scale);
         rows.walk(count, real ? lim : 0, n, a.pages, a.h_kv, u.kv, ahead, numbers,
                   [&](int i) __attribute__((always_inline)) { return (int)((uint32_t)__builtin_amdgcn_readlane(place, i & 63) * kPage); });
@@ -233,17 +231,17 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArg
 // A workgroup for the unit that the share of workgroup blockIdx.x + 1 begins inside of, if that is the first to do so; D / 4 threads per row
 template <int D>
 __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs a) {
-    const int lane = threadIdx.x & 63, d = 4 * (threadIdx.x % (D / 4));
+    const int d = 4 * (threadIdx.x % (D / 4)), from_token = token_at(a.req, 0), to_token = token_at(a.req, a.req.batch);
     const long x = ((long)blockIdx.x + 1) * a.share;
-    const Unit u = unit_of(a, x, lane);
-    if (u.begin >= x || x - u.begin > a.share || !u.real) return;
+    const Unit u = unit_of(a, x);
+    if (u.begin >= x || x - u.begin > a.share) return;
     const long w0 = u.begin / a.share;
     const int parts = (int)((u.end - 1) / a.share - w0) + 1;
     for (int row = threadIdx.x / (D / 4); row < min(16, a.g - u.head0); row += 1024 / D) {
         float inv;
         const v4f o = joined(a.ws_ml, a.ws_o + d, D, parts,
                              [&](int c) __attribute__((always_inline)) { return (size_t)((w0 + c) * 2 + (c == 0 && u.begin > w0 * a.share ? 1 : 0)) * 16 + row; }, inv);
-        *reinterpret_cast<h4 *>(a.out + ((size_t)u.token * a.h_q + u.kv * a.g + u.head0 + row) * D + d) = rounded(o, inv);
+        if (u.token >= from_token && u.token < to_token) *reinterpret_cast<h4 *>(a.out + ((size_t)u.token * a.h_q + u.kv * a.g + u.head0 + row) * D + d) = rounded(o, inv);
     }
 }
 
@@ -528,7 +526,7 @@ __global__ __launch_bounds__(256, 2) void attn_q4_wide_kernel(PartsArgs a) {
     const Found f = find(block, a.groups, lane, [&](int i) __attribute__((always_inline)) { return (int)(((long)tokens_of_group(a, i) * a.g + S::ROWS - 1) / S::ROWS); });
     if (f.run < 0) return;
     const Group group = group_of(a, f.run, lane);
-    const int first = token_at(a, group_end(a, f.run)), rows_all = tokens_of_group(a, f.run) * a.g;
+    const int first = token_at(a.req, group_end(a, f.run)), rows_all = tokens_of_group(a, f.run) * a.g;
     const long all_rows = (long)a.req.tokens * a.h_q;
     const int per = max(1, (group.pages + a.prefix_parts - 1) / a.prefix_parts), from = min(part * per, group.pages), to = min(from + per, group.pages);
     WideRows<D> rows(lane);
@@ -624,7 +622,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : kWgs) void attn_q4_parts_kernel
             }
             const Group group = group_of(a, f.run, lane);
             b = group.lead, pages = group.pages;
-            first = token_at(a, group_end(a, f.run)), rows_all = tokens_of_group(a, f.run) * a.g, row = f.place * 16 + m;
+            first = token_at(a.req, group_end(a, f.run)), rows_all = tokens_of_group(a, f.run) * a.g, row = f.place * 16 + m;
             n = pages * kPage, lim = n, from = 0;
         } else {
             Found f = {block, 0};
@@ -673,9 +671,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : kWgs) void attn_q4_parts_kernel
 template <int D>
 __global__ __launch_bounds__(256) void attn_q4_join_kernel(PartsArgs a) {
     const long all_rows = (long)a.req.tokens * a.h_q, step = (long)gridDim.x * (1024 / D);
-    const int d = 4 * (threadIdx.x % (D / 4)), last = token_at(a, a.req.batch), slots = a.prefix_parts + a.parts;
+    const int d = 4 * (threadIdx.x % (D / 4)), last = token_at(a.req, a.req.batch), slots = a.prefix_parts + a.parts;
     int group0 = 0, group1 = 0;  // tokens of groups
-    if (a.prefix_parts) group0 = token_at(a, group_end(a, 0)), group1 = token_at(a, group_end(a, a.groups));
+    if (a.prefix_parts) group0 = token_at(a.req, group_end(a, 0)), group1 = token_at(a.req, group_end(a, a.groups));
     for (long row = (long)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4); row < all_rows; row += step) {
         const int token = (int)(row / a.h_q);
         if (token >= last) return;

@@ -45,15 +45,6 @@ struct Place {
     static_assert(kWgs * LDS <= 160 * 1024 && COPIES <= 63, "LDS, and the 6-bit counter of outstanding copies");
 };
 
-// Largest over the lanes (m, r) of all r
-__device__ __forceinline__ float over_rows(float x) {
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    const float y = fmaxf(__uint_as_float(a.x), __uint_as_float(a.y));
-    const u32x2 b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-    return fmaxf(__uint_as_float(b.x), __uint_as_float(b.y));
-}
-
 // 16 query rows of a KV head, their sums over the pages walked so far, and the wavefront's places in LDS.  Lane (m, r) = (lane % 16, lane / 16) has row m.
 template <int D>
 struct Rows {

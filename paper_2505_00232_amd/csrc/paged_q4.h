@@ -76,6 +76,15 @@ __device__ __forceinline__ int sum_upto(int x) {
     return x;
 }
 
+// Largest over the lanes (m, r) of all r
+__device__ __forceinline__ float over_rows(float x) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    const float y = fmaxf(__uint_as_float(a.x), __uint_as_float(a.y));
+    const u32x2 b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+    return fmaxf(__uint_as_float(b.x), __uint_as_float(b.y));
+}
+
 // Requests of the tokens of a wavefront, PER of them from `first` on: how many requests end at or before a token.  A lane looks at one request at a time.
 template <int PER>
 __device__ __forceinline__ int request_of(const Requests &q, int first, int mine, int lane) {

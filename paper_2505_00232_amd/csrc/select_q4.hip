@@ -78,8 +78,7 @@ __global__ __launch_bounds__(256) void bound_pages_kernel(BoundArgs a) {
                 hi[k][e] = row_max(hi[k][e]), lo[k][e] = row_max(lo[k][e]);
                 most = fmaxf(most, fmaxf(fabsf(hi[k][e]), fabsf(lo[k][e])));
             }
-        most = fmaxf(most, __shfl_xor(most, 16, 64));
-        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        most = over_rows(most);
         turn ^= 1;  // (the next page's go beside these: one barrier is enough)
         if (lane == 0) tops[turn][wave] = most;
         __syncthreads();
@@ -117,50 +116,74 @@ __device__ __forceinline__ uint32_t key_of(float x) {  // order of floats as one
     return u ^ ((int)u < 0 ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// The k largest of scores mid0 .. mid1 - 1 (64 R at most, more than k), of equal ones the first, ascending: by one wavefront, 64 at a time in its registers.  The k-th is looked for between the
-// least and the largest key by halving; as soon as k of them are not below the middle, those are the ones (some 12 steps for 500 scores, where a byte at a time by 16 wavefronts needs 4
-// passes of three barriers and many atomics on few words: 500 pages 12.5 us, so TIMES).
+// Largest over the wavefront
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, false));  // row_ror 8, 4, 2, 1
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xF, 0xF, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xF, 0xF, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xF, 0xF, false));
+    const u32x2 y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(y.x, y.y);
+    const u32x2 z = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return __builtin_amdgcn_readfirstlane(max(z.x, z.y));
+}
+__device__ __forceinline__ int lower(uint64_t bits) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0)); }
+
+// The k largest of scores mid0 .. mid1 - 1 (64 R at most, more than k), of equal ones the first, ascending: by one wavefront, 64 at a time in its registers.  The range of the keys is cut into 64
+// bins, the bin of the k-th into 64 again and so on; as soon as a bin ends with the k-th, those down to it are the ones (mostly after two rounds.  500 scores: 1 us; by halving 3 us, and a byte
+// at a time by 16 wavefronts, with three barriers and many atomics on few words each, 5 us).
 template <int R>
-__device__ __forceinline__ void pick(const float *scores, int mid0, int mid1, int k, int lane, int *out) {
-    uint32_t key[R], lo = ~0u, hi = 0;
+__device__ __forceinline__ void pick(const float *scores, int mid0, int mid1, int k, int lane, int *bins, int *out) {
+    uint32_t key[R], least = 0, most = 0;  // (least: complemented)
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         key[i] = key_of(scores[min(mid0 + 64 * i + lane, mid1 - 1)]);  // (the last again, for the lanes behind it: loads without branches between them)
-        lo = min(lo, key[i]), hi = max(hi, key[i]);
+        least = max(least, ~key[i]), most = max(most, key[i]);
     }
+    uint32_t lo = ~wave_max(least);
+    const uint32_t range = wave_max(most) - lo;
+    int shift = range >= 64 ? 26 - __builtin_clz(range) : 0, above = 0, left = 0;  // (range >> shift is below 64)
+    for (;;) {
+        bins[lane] = 0;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
 #pragma unroll
-    for (int i = 0; i < R; ++i) key[i] = mid0 + 64 * i + lane < mid1 ? key[i] : 0;
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) lo = min(lo, (uint32_t)__shfl_xor((int)lo, off, 64)), hi = max(hi, (uint32_t)__shfl_xor((int)hi, off, 64));
-    lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
-    auto from = [&](uint32_t x) __attribute__((always_inline)) {  // how many are x and more
-        int n = 0;  // (of the lane first: a ballot's count per score, through the scalar unit, took three times as long)
-#pragma unroll
-        for (int i = 0; i < R; ++i) n += key[i] >= x ? 1 : 0;
-        return __builtin_amdgcn_readlane(sum_upto(n), 63);
-    };
-    int left = -1;
-    while (lo < hi) {
-        const uint32_t middle = lo + ((hi - lo) >> 1) + 1;
-        const int n = from(middle);
-        if (n == k) {
-            lo = middle - 1, left = 0;  // (all above this)
+        for (int i = 0; i < R; ++i) {
+            const uint32_t bin = (key[i] - lo) >> shift;
+            if (mid0 + 64 * i + lane < mid1 && key[i] >= lo && bin < 64) atomicAdd(bins + (63 - bin), 1);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        const int own = __hip_atomic_load(bins + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT), upto = above + sum_upto(own);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+        const int l = (int)__ffsll((unsigned long long)__ballot(upto >= k)) - 1;  // (the bins hold the k-th)
+        lo += (uint32_t)(63 - l) << shift;
+        const int to = __builtin_amdgcn_readlane(upto, l);
+        if (to == k) {
+            lo -= 1;  // (all above this)
             break;
         }
-        if (n > k)
-            lo = middle;
-        else
-            hi = middle - 1;
+        above = to - __builtin_amdgcn_readlane(own, l);
+        if (shift == 0) {
+            left = k - above;  // lo is the k-th: of those level with it
+            break;
+        }
+        shift = max(shift - 6, 0);
     }
-    if (left < 0) left = k - (lo == ~0u ? 0 : from(lo + 1));  // lo is the k-th: of those level with it
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         const int p = mid0 + 64 * i + lane;
-        const uint64_t lower = (1ull << lane) - 1, level = __ballot(p < mid1 && key[i] == lo), above = __ballot(p < mid1 && key[i] > lo);
-        const int level_before = (int)__popcll(level & lower), of_level = min((int)__popcll(level), left);
-        if ((above >> lane & 1) || ((level >> lane & 1) && level_before < left)) out[(int)__popcll(above & lower) + min(level_before, left)] = p;
-        out += (int)__popcll(above) + of_level;
-        left -= of_level;
+        const bool is_above = p < mid1 && key[i] > lo;
+        const uint64_t above_bits = __ballot(is_above);
+        if (left > 0) {
+            const bool is_level = p < mid1 && key[i] == lo;
+            const uint64_t level_bits = __ballot(is_level);
+            const int level_before = lower(level_bits), of_level = min((int)__popcll(level_bits), left);
+            if (is_above || (is_level && level_before < left)) out[lower(above_bits) + min(level_before, left)] = p;
+            out += (int)__popcll(above_bits) + of_level;
+            left -= of_level;
+        } else {
+            if (is_above) out[lower(above_bits)] = p;
+            out += (int)__popcll(above_bits);
+        }
     }
 }
 constexpr int kPicked = 2048;  // scores that one wavefront picks from
@@ -170,10 +193,12 @@ constexpr int kPicked = 2048;  // scores that one wavefront picks from
 // other, and of some twenty barriers.
 enum { kAll, kScores, kList };
 template <int D, int PHASE, bool IN_LDS>
-__global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
+__global__ __launch_bounds__(512) void select_pages_kernel(SelectArgs a) {
     constexpr int C = D / 64, AHEAD = 2;  // chunks of 64 components; groups of 16 pages on their way
     extern __shared__ float lds_scores[];
-    __shared__ int counts[256], found[2], taken[16][2];
+    __shared__ int counts[256], found[2], taken[8][2];
+    __shared__ float tops[C][16], steps_of[16];
+    __shared__ i32x4 codes[2][C][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, m = lane & 15, r = lane >> 4;
     const int pieces = PHASE == kScores ? a.pieces : 1;
     for (long work = blockIdx.x; work < a.items * pieces; work += gridDim.x) {
@@ -181,6 +206,13 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
         float *const kept = PHASE == kAll ? nullptr : a.scores + (size_t)in_slice * a.most_pages;
         float *const scores = IN_LDS ? lds_scores : kept;
         const int kv = (int)(item % a.h_kv), token = (int)(item / a.h_kv);
+        h8 asked[2] = {};
+        auto ask = [&](int h0) __attribute__((always_inline)) {
+            if (wave >= C) return;
+            const _Float16 *q = a.q + ((size_t)token * a.h_q + kv * a.g + min(h0 + m, a.g - 1)) * D + 64 * wave + 16 * r;
+            asked[0] = *reinterpret_cast<const h8 *>(q), asked[1] = *reinterpret_cast<const h8 *>(q + 8);
+        };
+        if constexpr (PHASE != kList) ask(0);  // (on their way before anything is known of the request)
         Span s;
         const int b = __builtin_amdgcn_readfirstlane(request_of_token(a.req, token, lane, s));
         if (b >= a.req.batch) return;
@@ -197,36 +229,38 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
             // ---- scores of the pages in between, 16 heads at a time
             if constexpr (PHASE != kList)
             for (int h0 = 0; h0 < a.g; h0 += 16) {
-                const _Float16 *q = a.q + ((size_t)token * a.h_q + kv * a.g + min(h0 + m, a.g - 1)) * D;
-                float x[C][16], top = 0.0f;
+                // wavefront c has the queries' components 64 c .. + 63; all get their codes from LDS (each for itself, the 16 of a workgroup were 3 us at it)
+                if (h0 > 0 || work != blockIdx.x) __syncthreads();  // (those before have been read)
+                if (h0 > 0) ask(h0);
+                float x[16], top = 0.0f;
+                if (wave < C) {
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+                    for (int e = 0; e < 16; ++e) x[e] = (float)asked[e / 8][e % 8], top = fmaxf(top, fabsf(x[e]));
+                    top = over_rows(top);
+                    if (r == 0) tops[wave][m] = top;
+                }
+                __syncthreads();
+                if (wave < C) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const h8 v = *reinterpret_cast<const h8 *>(q + 64 * c + 16 * r + 8 * u);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            x[c][8 * u + e] = (float)v[e];
-                            top = fmaxf(top, fabsf((float)v[e]));
-                        }
-                    }
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float f = top > 0.0f ? 127.0f / top : 0.0f, by = top / 127.0f;
-                i32x4 up[C], down[C];
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    up[c] = down[c] = i32x4{0, 0, 0, 0};
+                    for (int c = 0; c < C; ++c) top = fmaxf(top, tops[c][m]);
+                    const float f = top > 0.0f ? 127.0f / top : 0.0f;
+                    i32x4 up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int code = clamped(rintf(x[c][e] * f));
-                        up[c][e / 4] |= (max(code, 0) & 255) << (8 * (e % 4));
-                        down[c][e / 4] |= (min(code, 0) & 255) << (8 * (e % 4));
+                        const int code = clamped(rintf(x[e] * f));
+                        up[e / 4] |= (max(code, 0) & 255) << (8 * (e % 4));
+                        down[e / 4] |= (min(code, 0) & 255) << (8 * (e % 4));
                     }
+                    codes[0][wave][lane] = up, codes[1][wave][lane] = down;
+                    if (wave == 0 && r == 0) steps_of[m] = top / 127.0f;
                 }
+                __syncthreads();
+                i32x4 up[C], down[C];
                 float of_row[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) of_row[i] = __shfl(by, 4 * r + i, 64);
+                for (int c = 0; c < C; ++c) up[c] = codes[0][c][lane], down[c] = codes[1][c][lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) of_row[i] = steps_of[4 * r + i];
                 for (int p0 = mid0 + ((int)(work % pieces) * waves + wave) * (16 * AHEAD); p0 < mid1; p0 += pieces * waves * (16 * AHEAD)) {
                     int page[AHEAD];
                     float step[AHEAD];
@@ -241,6 +275,8 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                         step[u] = a.steps[at];
                     }
 #pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) asm volatile("" : "+v"(step[u]), "+v"(bound[u][0]));  // (asked for here, not in front of their use behind each other's waits)
+#pragma unroll
                     for (int u = 0; u < AHEAD; ++u) {
                         i32x4 sum = {0, 0, 0, 0};
 #pragma unroll
@@ -251,8 +287,7 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                         float most = (float)sum[0] * of_row[0];  // rows 4 r .. + 3, page m
 #pragma unroll
                         for (int i = 1; i < 4; ++i) most = fmaxf(most, (float)sum[i] * of_row[i]);
-                        most = fmaxf(most, __shfl_xor(most, 16, 64));
-                        most = fmaxf(most, __shfl_xor(most, 32, 64));
+                        most = over_rows(most);
                         most = page[u] < 0 ? -INFINITY : most * step[u];
                         const int p = p0 + 16 * u + m;
                         if (r == 0 && p < mid1) scores[p] = h0 == 0 ? most : fmaxf(scores[p], most);
@@ -265,12 +300,14 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                 if (wave == 0) {
                     const float *from = PHASE == kList ? kept : scores;
                     const int n = mid1 - mid0;
-                    if (n <= 512)
-                        pick<8>(from, mid0, mid1, k, lane, out + a.first);
+                    if (n <= 128)
+                        pick<2>(from, mid0, mid1, k, lane, counts, out + a.first);
+                    else if (n <= 512)
+                        pick<8>(from, mid0, mid1, k, lane, counts, out + a.first);
                     else if (n <= 1024)
-                        pick<16>(from, mid0, mid1, k, lane, out + a.first);
+                        pick<16>(from, mid0, mid1, k, lane, counts, out + a.first);
                     else
-                        pick<32>(from, mid0, mid1, k, lane, out + a.first);
+                        pick<32>(from, mid0, mid1, k, lane, counts, out + a.first);
                 }
             } else {
             if constexpr (PHASE == kList && IN_LDS)
@@ -353,14 +390,14 @@ hipError_t launch_phase(const SelectArgs &a, int threads, long wgs, hipStream_t 
 
 template <int D>
 hipError_t launch_select(SelectArgs a, int num_cus, hipStream_t st) {
-    const int threads = a.most_pages <= 128 ? 256 : a.most_pages <= 256 ? 512 : 1024;  // (32 pages of a wavefront are on their way at once)
+    const int threads = a.most_pages <= 128 ? 256 : 512;  // (32 pages of a wavefront are on their way at once)
     if (one_launch(a.items, a.most_pages, num_cus)) return launch_phase<D, kAll, true>(a, threads, a.items, st);
     const long all = a.items;
     for (; a.item0 < all; a.item0 += kSlice) {
         a.items = all - a.item0 < kSlice ? all - a.item0 : kSlice;
         a.pieces = (a.most_pages + 127) / 128;
         if (const hipError_t e = launch_phase<D, kScores, false>(a, 256, a.items * a.pieces, st); e != hipSuccess) return e;
-        const hipError_t e = a.most_pages <= kSelectInLds ? launch_phase<D, kList, true>(a, 1024, a.items, st) : launch_phase<D, kList, false>(a, 1024, a.items, st);
+        const hipError_t e = a.most_pages <= kSelectInLds ? launch_phase<D, kList, true>(a, 512, a.items, st) : launch_phase<D, kList, false>(a, 512, a.items, st);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
