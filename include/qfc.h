@@ -444,7 +444,7 @@ typedef struct qfc_shared {
 } qfc_shared_t;
 
 /* qfc_attention_q4 for requests of which groups have common pages: the same result up to roundings, with what is common read and multiplied once for all rows of a group (from the table
- * row of its first request with tokens).  Errors as qfc_attention_q4; QFC_ERR_INVALID_ARG for null pointers and sizes below 1 in `shared`. */
+ * row of its first request with tokens).  Errors as qfc_attention_q4; QFC_ERR_INVALID_ARG for null pointers and sizes below 1 in `shared`, QFC_ERR_UNSUPPORTED for groups * h_kv above 65535. */
 qfc_status_t qfc_attention_shared_q4_workspace_size(const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
 qfc_status_t qfc_attention_shared_q4(const void *q_f16, const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, void *workspace,
                                      size_t workspace_bytes, void *out_f16, void *stream);

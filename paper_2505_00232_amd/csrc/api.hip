@@ -609,8 +609,9 @@ qfc_status_t qfc_compact_pages(const qfc_q4_cache_t *cache, int32_t *references,
 }
 
 // ---- attention behind common pages, and over selected ones
-static qfc_status_t check_shared(const qfc_shared_t *s) {
-    return s && s->groups >= 1 && s->max_group_tokens >= 1 && s->max_positions >= 1 ? QFC_OK : QFC_ERR_INVALID_ARG;
+static qfc_status_t check_shared(const qfc_shared_t *s, const qfc_q4_cache_t *c) {
+    if (!s || s->groups < 1 || s->max_group_tokens < 1 || s->max_positions < 1) return QFC_ERR_INVALID_ARG;
+    return (long)s->groups * c->h_kv > 65535 ? QFC_ERR_UNSUPPORTED : QFC_OK;
 }
 
 static AttnPartsPlan shared_plan(const qfc_requests_t *r, const qfc_shared_t *s, int32_t h_q, const qfc_q4_cache_t *c, int cus) {
@@ -620,7 +621,7 @@ static AttnPartsPlan shared_plan(const qfc_requests_t *r, const qfc_shared_t *s,
 qfc_status_t qfc_attention_shared_q4_workspace_size(const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes) {
     if (!bytes) return QFC_ERR_INVALID_ARG;
     if (const qfc_status_t s = check_batch(requests, h_q, cache); s != QFC_OK) return s;
-    if (const qfc_status_t s = check_shared(shared); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_shared(shared, cache); s != QFC_OK) return s;
     *bytes = shared_plan(requests, shared, h_q, cache, device_cus()).bytes;
     return QFC_OK;
 }
@@ -628,7 +629,7 @@ qfc_status_t qfc_attention_shared_q4_workspace_size(const qfc_requests_t *reques
 qfc_status_t qfc_attention_shared_q4(const void *q_f16, const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, void *workspace,
                                      size_t workspace_bytes, void *out_f16, void *stream) {
     if (const qfc_status_t s = check_requests(requests, h_q, cache); s != QFC_OK) return s;
-    if (const qfc_status_t s = check_shared(shared); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_shared(shared, cache); s != QFC_OK) return s;
     if (!shared->group_start || !shared->positions) return QFC_ERR_INVALID_ARG;
     if (!aligned(shared->group_start, 4) || !aligned(shared->positions, 4)) return QFC_ERR_ALIGNMENT;
     if (requests->tokens == 0) return QFC_OK;

@@ -247,13 +247,14 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
 
 // ---- common pages of many rows.  What attention_q4_rows.h does to a page for 16 query rows, most of its instructions, is to take its codes apart: 551 vector instructions of a page and 16 rows,
 // of which 192 for that.  Here the four wavefronts of a workgroup take a page's codes apart once, into LDS as binary16 whole numbers code - 8 (exact, as are the products with the queries), and
-// multiply them with 16 NB rows each; steps, offsets and P are taken into the sums in the same way and the same precision as there:
+// multiply them with 32 rows each (310 instructions of a page and 16 rows); steps, offsets and P are taken into the sums in the same way and the same precision as there:
 //   q . k = sum_j step_j (q_j . (code_j - 8)) + sum_j offset_j sum q_j,   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
-// The common pages are in front of all rows' positions: nothing is masked.
+// The common pages are in front of all rows' positions: nothing is masked.  Bound: the LDS, 63 reads of a KiB of a page and wavefront at 64 bytes a cycle, beside vector instructions in 64 % of the
+// cycles (1024 rows of 8 heads of 128 values behind 20000 positions 150 us: 460 TFLOP/s).
 template <int D>
 struct Wide {
     typedef PageLayout<D> L;
-    static constexpr int G = L::G, W = L::W, DT = D / 16, NB = D == 256 ? 1 : 2, ROWS = 64 * NB, BUFFERS = D == 256 ? 1 : 2;
+    static constexpr int G = L::G, W = L::W, DT = D / 16, NB = 2, ROWS = 64 * NB;
     // LDS: K operands [4 tiles][G][64 lanes], V operands [G][low, high][2 halves of 16 positions][64 lanes], 16 bytes each; then the page's steps and offsets of keys, and of values
     static constexpr int kV = 128 * D, kHeadK = 256 * D, kHeadV = 264 * D, kBytes = 272 * D;
     static constexpr int kStepK = kHeadK, kOffsetK = kHeadK + 4 * D, kStepV = kHeadV, kOffsetV = kHeadV + 4 * D;
@@ -521,8 +522,7 @@ __global__ __launch_bounds__(256, 2) void attn_q4_wide_kernel(PartsArgs a) {
     extern __shared__ char wide_lds[];
     char *const lds = wide_lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long x = blockIdx.x;
-    const int kv = (int)(x % a.h_kv), part = (int)(x / a.h_kv % a.prefix_parts), block = (int)(x / a.h_kv / a.prefix_parts);
+    const int kv = (int)(blockIdx.x % a.h_kv), part = (int)(blockIdx.x / a.h_kv % a.prefix_parts), block = (int)(blockIdx.x / a.h_kv / a.prefix_parts);
     const Found f = find(block, a.groups, lane, [&](int i) __attribute__((always_inline)) { return (int)(((long)tokens_of_group(a, i) * a.g + S::ROWS - 1) / S::ROWS); });
     if (f.run < 0) return;
     const Group group = group_of(a, f.run, lane);
@@ -559,35 +559,23 @@ __global__ __launch_bounds__(256, 2) void attn_q4_wide_kernel(PartsArgs a) {
     S raw;
     auto fetch = [&](int of) __attribute__((always_inline)) { raw.fetch(a.pages + ((size_t)of * a.h_kv + kv) * PageLayout<D>::kBytes); };
     if (page >= 0) fetch(page);
-    if constexpr (S::BUFFERS == 2) {  // the next page is taken apart into the other place: one barrier per page
-        char *now = lds, *other = lds + S::kBytes;
-        if (page >= 0) {
-            raw.put(now);
+    // (the next page is taken apart into the other place: one barrier per page)
+    char *now = lds, *other = lds + S::kBytes;
+    if (page >= 0) {
+        raw.put(now);
+        ++i;
+        page = following(i);
+        if (page >= 0) fetch(page);
+        for (;;) {
+            __syncthreads();
+            rows.page(now);
+            if (page < 0) break;
+            raw.put(other);
             ++i;
             page = following(i);
             if (page >= 0) fetch(page);
-            for (;;) {
-                __syncthreads();
-                rows.page(now);
-                if (page < 0) break;
-                raw.put(other);
-                ++i;
-                page = following(i);
-                if (page >= 0) fetch(page);
-                char *const x = now;
-                now = other, other = x;
-            }
-        }
-    } else {
-        while (page >= 0) {
-            ++i;
-            const int next = following(i);
-            raw.put(lds);
-            __syncthreads();
-            if (next >= 0) fetch(next);
-            rows.page(lds);
-            __syncthreads();
-            page = next;
+            char *const x = now;
+            now = other, other = x;
         }
     }
 #pragma unroll
@@ -688,12 +676,14 @@ constexpr long kMostWgs = 1L << 22;  // (a launch has fewer than 2^32 threads)
 template <int D>
 hipError_t launch(const PartsArgs &a, hipStream_t st) {
     PartsArgs rest = a;
-    if (a.wide) {
-        constexpr size_t lds = Wide<D>::kBytes * Wide<D>::BUFFERS;
-        if (const hipError_t e = allow_dynamic_lds<attn_q4_wide_kernel<D>>(lds); e != hipSuccess) return e;
-        attn_q4_wide_kernel<D><<<(unsigned)a.prefix_items, 256, lds, st>>>(a);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        rest.items -= a.prefix_items, rest.prefix_items = 0;
+    if constexpr (D <= 128) {
+        if (a.wide) {
+            constexpr size_t lds = Wide<D>::kBytes * 2;
+            if (const hipError_t e = allow_dynamic_lds<attn_q4_wide_kernel<D>>(lds); e != hipSuccess) return e;
+            attn_q4_wide_kernel<D><<<(unsigned)a.prefix_items, 256, lds, st>>>(a);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+            rest.items -= a.prefix_items, rest.prefix_items = 0;
+        }
     }
     constexpr size_t lds = Place<D>::LDS;
     if (const hipError_t e = allow_dynamic_lds<attn_q4_parts_kernel<D>>(lds); e != hipSuccess) return e;
@@ -724,7 +714,9 @@ hipError_t launch(const Args &a, int d, hipStream_t st) {
 }
 
 constexpr int kMostParts = 16;
-constexpr int kWideFrom = 512;  // rows of a group and KV head from which on pages are taken apart for a workgroup
+// Rows and common pages of a group times heads and their size per compute unit from which on pages are taken apart for a workgroup.  Both ways' times, us, with 8 KV heads of 128 values: 512 rows
+// behind 6000 positions 50 and 63, behind 20000 116 and 107; 1024 rows 85 and 94, 219 and 186; with 4 heads of 64: 1024 rows behind 20000 75 and 79.
+constexpr long kWideFrom = 600000;
 // Workgroups that share a block's pages: as many as fill the card, each with a page per wavefront at least
 int parts_of(long blocks, int pages, int num_cus) {
     const long fill = ((long)kWgs * num_cus + blocks - 1) / (blocks > 0 ? blocks : 1), most = (pages + 3) / 4;
@@ -752,12 +744,13 @@ AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv,
     AttnPartsPlan p = {};
     const int g = h_q / h_kv;
     const int forced = tuning().attn_wide_rows;
-    p.wide = (long)group_tokens * g >= (forced > 0 ? forced : kWideFrom);
-    const int rows = !p.wide ? 16 : d == 256 ? Wide<256>::ROWS : Wide<128>::ROWS;
+    const long group_rows = (long)group_tokens * g, common = (longest < max_context ? longest : max_context) / kPage;
+    p.wide = d <= 128 && (forced > 0 ? group_rows >= forced : group_rows >= 2 * Wide<128>::ROWS && group_rows * common * h_kv * d >= kWideFrom * num_cus);
+    const int rows = p.wide ? Wide<128>::ROWS : 16;
     const long by_group = (long)groups * (((long)group_tokens * g + rows - 1) / rows), by_token = ((long)tokens * g + rows - 1) / rows + groups;
     p.prefix_blocks = by_group < by_token ? by_group : by_token;
     p.blocks = max_tokens * g <= 16 ? batch : ((long)tokens * g + 15) / 16 + batch;
-    p.prefix_parts = parts_of(p.prefix_blocks * h_kv, (longest < max_context ? longest : max_context) / kPage, num_cus);
+    p.prefix_parts = parts_of(p.prefix_blocks * h_kv, (int)common, num_cus);
     p.parts = parts_of(p.blocks * h_kv, (max_context + kPage - 1) / kPage, num_cus);
     p.bytes = 256 + (size_t)(p.prefix_parts + p.parts) * tokens * h_q * (d + 2) * sizeof(float);
     return p;

@@ -73,7 +73,7 @@ def test_attention_and_selection_refusals_before_any_launch():
         assert call(o=0x1001) == 4 and call(n=8) == 3
     for bad in (None, shared(None), shared(p=None), shared(n=0), shared(tokens=0), shared(longest=0)):
         assert common(sh=bad) == 1
-    assert common(sh=shared(odd)) == 4 and common(sh=shared(p=odd)) == 4 and common(o=0x1008) == 4
+    assert common(sh=shared(n=32768)) == 2 and common(sh=shared(odd)) == 4 and common(sh=shared(p=odd)) == 4 and common(o=0x1008) == 4
     for call in (bound, select):
         assert call(b=None) == 1 and call(b=bounds(None)) == 1 and call(b=bounds(t=None)) == 1 and call(b=bounds(0x1008)) == 4 and call(b=bounds(t=odd)) == 4
     assert select(first=-1) == 1 and select(last=-1) == 1 and select(count=0) == 1 and select(first=3, last=2) == 1 and select(first=2 ** 31 - 1, last=2 ** 31 - 1) == 1 and select(count=65537) == 2
