@@ -403,17 +403,29 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
  * one cache say nothing about another's.
  *   page_table    device, int32 [batch, table_width], changed by the call; an entry outside [0, num_pages) is no page
  *   missing       device, int32 [1], or null: how many entries got no page because none was free (they are -1, and attention does not see their positions)
+ *   bounds        host, or null: bounds of the keys of all pages (below), which belong to a page's number; they go where a page's contents go
  *   workspace     device scratch of qfc_pages_workspace_size bytes, 16-byte aligned, one call's at a time
  * Errors of all: QFC_ERR_INVALID_ARG (null pointers, sizes below 1), QFC_ERR_UNSUPPORTED (d_head other than 64, 128, 256; batch above 2^22; a page of 2^31 bytes and more),
  * QFC_ERR_ALIGNMENT (16 bytes for pages and workspace, 4 for int32 arrays), QFC_ERR_BUFFER_TOO_SMALL. */
+
+/* Bounds of the keys that a page holds for a KV head, for choosing pages without reading them: with hi_d and lo_d the largest and the smallest value of component d over the page's
+ * positions (rounded to 32 bits) and a the largest magnitude among them, step = a / 127, upper codes min(ceil(hi_d (127 / a)), 127), lower codes max(floor(lo_d (127 / a)), -127),
+ * every operation rounded to 32 bits; a = 0: zeros.  (Filled by qfc_bound_pages_q4; qfc_copy_pages, qfc_fork_pages and
+ * qfc_compact_pages take them along, where they are given.)
+ *   codes  device, int8 [num_pages, h_kv, 2, d_head] (upper, lower), 16-byte aligned;  steps  device, float [num_pages, h_kv] */
+typedef struct qfc_page_bounds {
+    int8_t *codes; /* device */
+    float *steps;  /* device */
+} qfc_page_bounds_t;
 
 /* Bytes of scratch that qfc_take_pages, qfc_fork_pages and qfc_compact_pages need for tables of `batch` rows (host pointers; of the cache the sizes are read). */
 qfc_status_t qfc_pages_workspace_size(const qfc_q4_cache_t *cache, int32_t batch, size_t *bytes);
 
 /* Pages source[i] of one cache to pages target[i] of another (or the same), i < count: all that they hold.  A pair with an index outside its cache copies nothing.  No page may be the
  * target of two pairs, nor of one where it is another's source.  The caches have the same h_kv and d_head, else QFC_ERR_INVALID_ARG.  source, target: device, int32 [count];
- * count 0: nothing to do. */
-qfc_status_t qfc_copy_pages(const qfc_q4_cache_t *from, const qfc_q4_cache_t *to, const int32_t *source, const int32_t *target, int32_t count, void *stream);
+ * count 0: nothing to do.  from_bounds and to_bounds: both or neither. */
+qfc_status_t qfc_copy_pages(const qfc_q4_cache_t *from, const qfc_q4_cache_t *to, const int32_t *source, const int32_t *target, int32_t count, const qfc_page_bounds_t *from_bounds,
+                            const qfc_page_bounds_t *to_bounds, void *stream);
 
 /* Every row b of the table gets pages for its first positions[b] positions: each of those entries that has none gets a free page, whose references become 1. */
 qfc_status_t qfc_take_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, const int32_t *positions, int32_t batch, int32_t table_width, int32_t *missing,
@@ -423,15 +435,16 @@ qfc_status_t qfc_take_pages(const qfc_q4_cache_t *cache, int32_t *references, in
  * shared, their references one more; a page that they fill in part is copied into a free one.  The row's other entries become -1: what it held before is not let go.  A parent outside
  * [0, from_batch): a row of -1.  parents, positions: device, int32 [batch].  The tables must not overlap. */
 qfc_status_t qfc_fork_pages(const qfc_q4_cache_t *cache, int32_t *references, const int32_t *from, int32_t from_batch, int32_t from_width, const int32_t *parents, const int32_t *positions,
-                            int32_t *page_table, int32_t batch, int32_t table_width, int32_t *missing, void *workspace, size_t workspace_bytes, void *stream);
+                            int32_t *page_table, int32_t batch, int32_t table_width, int32_t *missing, const qfc_page_bounds_t *bounds, void *workspace, size_t workspace_bytes,
+                            void *stream);
 
 /* Every row b keeps the pages of its first keep[b] positions (keep null: none) and lets the others go: their references are one less each, the entries become -1. */
 qfc_status_t qfc_free_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, const int32_t *keep, int32_t batch, int32_t table_width, void *stream);
 
 /* The pages in use get the numbers from 0 on: with U of them in use, the i-th of those with numbers from U on moves to the i-th free page below U, with its references and in all
  * entries of the table, which has to hold all rows that name pages of the cache.  used: device, int32 [1], or null: U. */
-qfc_status_t qfc_compact_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, int32_t batch, int32_t table_width, int32_t *used, void *workspace,
-                               size_t workspace_bytes, void *stream);
+qfc_status_t qfc_compact_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, int32_t batch, int32_t table_width, int32_t *used,
+                               const qfc_page_bounds_t *bounds, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Groups of consecutive requests whose first positions are the same pages: group i is requests group_start[i] .. group_start[i + 1] - 1, and the tables of its requests name the same
  * pages for their first positions[i] positions (counted in whole pages; where a request of the group has fewer in front of its new tokens, that many).  Requests outside
@@ -448,15 +461,6 @@ typedef struct qfc_shared {
 qfc_status_t qfc_attention_shared_q4_workspace_size(const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
 qfc_status_t qfc_attention_shared_q4(const void *q_f16, const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, void *workspace,
                                      size_t workspace_bytes, void *out_f16, void *stream);
-
-/* Bounds of the keys that a page holds for a KV head, for choosing pages without reading them: with hi_d and lo_d the largest and the smallest value of component d over the page's
- * positions (rounded to 32 bits) and a the largest magnitude among them, step = a / 127, upper codes min(ceil(hi_d (127 / a)), 127), lower codes max(floor(lo_d (127 / a)), -127),
- * every operation rounded to 32 bits; a = 0: zeros.
- *   codes  device, int8 [num_pages, h_kv, 2, d_head] (upper, lower), 16-byte aligned;  steps  device, float [num_pages, h_kv] */
-typedef struct qfc_page_bounds {
-    int8_t *codes; /* device */
-    float *steps;  /* device */
-} qfc_page_bounds_t;
 
 /* Bounds of all pages that the batch's new tokens are in, over the request's positions there: to be called behind qfc_append_q4 with the same requests.  Errors as qfc_append_q4's. */
 qfc_status_t qfc_bound_pages_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, const qfc_page_bounds_t *bounds, void *stream);

@@ -158,11 +158,11 @@ def lib() -> ctypes.CDLL:
         L.qfc_attention_q4.argtypes = [vp, req, i32, cache, vp, sz, vp, vp]
         shared, bounds = ctypes.POINTER(SharedDesc), ctypes.POINTER(BoundsDesc)
         L.qfc_pages_workspace_size.argtypes = [cache, i32, ctypes.POINTER(sz)]
-        L.qfc_copy_pages.argtypes = [cache, cache, vp, vp, i32, vp]
+        L.qfc_copy_pages.argtypes = [cache, cache, vp, vp, i32, bounds, bounds, vp]
         L.qfc_take_pages.argtypes = [cache, vp, vp, vp, i32, i32, vp, vp, sz, vp]
-        L.qfc_fork_pages.argtypes = [cache, vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]
+        L.qfc_fork_pages.argtypes = [cache, vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, bounds, vp, sz, vp]
         L.qfc_free_pages.argtypes = [cache, vp, vp, vp, i32, i32, vp]
-        L.qfc_compact_pages.argtypes = [cache, vp, vp, i32, i32, vp, vp, sz, vp]
+        L.qfc_compact_pages.argtypes = [cache, vp, vp, i32, i32, vp, bounds, vp, sz, vp]
         L.qfc_attention_shared_q4_workspace_size.argtypes = [req, shared, i32, cache, ctypes.POINTER(sz)]
         L.qfc_attention_shared_q4.argtypes = [vp, req, shared, i32, cache, vp, sz, vp, vp]
         L.qfc_bound_pages_q4.argtypes = [req, cache, bounds, vp]
@@ -612,19 +612,45 @@ def _numbers(count: int, *named, devices=()):
             _here(d)
 
 
+class PageBounds:
+    """Bounds of the keys of a cache's pages (qfc_page_bounds_t): codes int8 [num_pages, h_kv, 2, d_head] (upper, lower), steps float32 [num_pages, h_kv]."""
+
+    def __init__(self, cache: PagedCache):
+        self.codes = torch.zeros((cache.num_pages, cache.h_kv, 2, cache.d_head), dtype=_i8, device=cache.pages.device)
+        self.steps = torch.zeros((cache.num_pages, cache.h_kv), dtype=_f32, device=cache.pages.device)
+        self.shape, self.device = (cache.num_pages, cache.h_kv, cache.d_head), cache.device
+        self.desc = BoundsDesc(self.codes.data_ptr(), self.steps.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+    def _of(self, cache: PagedCache):
+        if self.shape != (cache.num_pages, cache.h_kv, cache.d_head):
+            raise ValueError(f"bounds: of a cache of {self.shape} pages, heads and values, not {(cache.num_pages, cache.h_kv, cache.d_head)}")
+
+
+def _moved(bounds: PageBounds | None, cache: PagedCache):
+    """Bounds that go where the cache's pages go (None: there are none)."""
+    if bounds is None:
+        return None
+    bounds._of(cache)
+    _here(bounds.device)
+    return bounds.ref
+
+
 def qfc_pages_workspace_size(cache: PagedCache, batch: int) -> int:
     out = ctypes.c_size_t(0)
     _check(lib().qfc_pages_workspace_size(cache.ref, batch, ctypes.byref(out)), "qfc_pages_workspace_size")
     return out.value
 
 
-def qfc_copy_pages(source_cache: PagedCache, target_cache: PagedCache, source: torch.Tensor, target: torch.Tensor):
-    """Pages source[i] of one cache to pages target[i] of another (or the same)."""
+def qfc_copy_pages(source_cache: PagedCache, target_cache: PagedCache, source: torch.Tensor, target: torch.Tensor, source_bounds: PageBounds | None = None,
+                   target_bounds: PageBounds | None = None):
+    """Pages source[i] of one cache to pages target[i] of another (or the same), and bounds of their keys with them."""
     if not (isinstance(source, _Tensor) and source.dim() == 1):
         raise ValueError("source: a vector is required")
     count = source.shape[0]
     _numbers(count, ("source", source), ("target", target), devices=(source_cache.device, target_cache.device))
-    _check(lib().qfc_copy_pages(source_cache.ref, target_cache.ref, source.data_ptr(), target.data_ptr(), count, _stream()), "qfc_copy_pages")
+    _check(lib().qfc_copy_pages(source_cache.ref, target_cache.ref, source.data_ptr(), target.data_ptr(), count, _moved(source_bounds, source_cache),
+                                _moved(target_bounds, target_cache), _stream()), "qfc_copy_pages")
 
 
 def qfc_take_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, positions: torch.Tensor, workspace: torch.Tensor, missing: torch.Tensor | None = None):
@@ -639,7 +665,7 @@ def qfc_take_pages(cache: PagedCache, references: torch.Tensor, page_table: torc
 
 
 def qfc_fork_pages(cache: PagedCache, references: torch.Tensor, from_table: torch.Tensor, parents: torch.Tensor, positions: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor,
-                   missing: torch.Tensor | None = None):
+                   missing: torch.Tensor | None = None, bounds: PageBounds | None = None):
     """Row b of page_table continues the first positions[b] positions of row parents[b] of from_table: whole pages are shared, the one in part filled is copied."""
     from_batch, from_width = _table(from_table, "from_table")
     batch, width = _table(page_table, "page_table")
@@ -648,7 +674,7 @@ def qfc_fork_pages(cache: PagedCache, references: torch.Tensor, from_table: torc
     _numbers(batch, ("parents", parents), ("positions", positions))
     _numbers(1, ("missing", missing))
     _check(lib().qfc_fork_pages(cache.ref, references.data_ptr(), from_table.data_ptr(), from_batch, from_width, parents.data_ptr(), positions.data_ptr(), page_table.data_ptr(), batch, width,
-                                _ptr(missing), workspace.data_ptr(), workspace.numel(), _stream()), "qfc_fork_pages")
+                                _ptr(missing), _moved(bounds, cache), workspace.data_ptr(), workspace.numel(), _stream()), "qfc_fork_pages")
 
 
 def qfc_free_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, keep: torch.Tensor | None = None):
@@ -659,13 +685,15 @@ def qfc_free_pages(cache: PagedCache, references: torch.Tensor, page_table: torc
     _check(lib().qfc_free_pages(cache.ref, references.data_ptr(), page_table.data_ptr(), _ptr(keep), batch, width, _stream()), "qfc_free_pages")
 
 
-def qfc_compact_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor, used: torch.Tensor | None = None):
+def qfc_compact_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor, used: torch.Tensor | None = None,
+                      bounds: PageBounds | None = None):
     """The pages in use get the numbers from 0 on; page_table holds all rows that name pages of the cache."""
     batch, width = _table(page_table, "page_table")
     _want(workspace, _u8, None, "workspace")
     _numbers(cache.num_pages, ("references", references), devices=(cache.device, page_table.get_device(), workspace.get_device()))
     _numbers(1, ("used", used))
-    _check(lib().qfc_compact_pages(cache.ref, references.data_ptr(), page_table.data_ptr(), batch, width, _ptr(used), workspace.data_ptr(), workspace.numel(), _stream()), "qfc_compact_pages")
+    _check(lib().qfc_compact_pages(cache.ref, references.data_ptr(), page_table.data_ptr(), batch, width, _ptr(used), _moved(bounds, cache), workspace.data_ptr(),
+                                   workspace.numel(), _stream()), "qfc_compact_pages")
 
 
 class SharedPrefixes:
@@ -699,21 +727,6 @@ def qfc_attention_shared_q4(q: torch.Tensor, requests: Requests, shared: SharedP
     _here(q.get_device(), out.get_device(), workspace.get_device(), cache.device, requests.device, shared.device)
     _check(lib().qfc_attention_shared_q4(q.data_ptr(), requests.ref, shared.ref, h_q, cache.ref, workspace.data_ptr(), workspace.numel(), out.data_ptr(), _stream()),
            "qfc_attention_shared_q4")
-
-
-class PageBounds:
-    """Bounds of the keys of a cache's pages (qfc_page_bounds_t): codes int8 [num_pages, h_kv, 2, d_head] (upper, lower), steps float32 [num_pages, h_kv]."""
-
-    def __init__(self, cache: PagedCache):
-        self.codes = torch.zeros((cache.num_pages, cache.h_kv, 2, cache.d_head), dtype=_i8, device=cache.pages.device)
-        self.steps = torch.zeros((cache.num_pages, cache.h_kv), dtype=_f32, device=cache.pages.device)
-        self.shape, self.device = (cache.num_pages, cache.h_kv, cache.d_head), cache.device
-        self.desc = BoundsDesc(self.codes.data_ptr(), self.steps.data_ptr())
-        self.ref = ctypes.byref(self.desc)
-
-    def _of(self, cache: PagedCache):
-        if self.shape != (cache.num_pages, cache.h_kv, cache.d_head):
-            raise ValueError(f"bounds: of a cache of {self.shape} pages, heads and values, not {(cache.num_pages, cache.h_kv, cache.d_head)}")
 
 
 def qfc_bound_pages_q4(requests: Requests, cache: PagedCache, bounds: PageBounds):

@@ -544,6 +544,17 @@ static qfc_status_t check_pool_work(const qfc_q4_cache_t *c, int32_t batch, cons
     return workspace_bytes < pages_workspace(c->num_pages, batch) ? QFC_ERR_BUFFER_TOO_SMALL : QFC_OK;
 }
 
+static qfc_status_t check_bounds(const qfc_page_bounds_t *b) {
+    if (!b || !b->codes || !b->steps) return QFC_ERR_INVALID_ARG;
+    return aligned16(b->codes) && aligned(b->steps, 4) ? QFC_OK : QFC_ERR_ALIGNMENT;
+}
+
+// Bounds that may be left out
+static qfc_status_t check_moved(const qfc_page_bounds_t *b) { return b ? check_bounds(b) : QFC_OK; }
+static PageBounds moved(const qfc_page_bounds_t *b, const qfc_q4_cache_t *c) {
+    return b ? PageBounds{b->codes, b->steps, c->h_kv, c->d_head} : PageBounds{};
+}
+
 static PagePool pool_of(const qfc_q4_cache_t *c, int32_t *references) { return PagePool{c->pages, references, c->num_pages, c->h_kv * 80 * c->d_head}; }
 
 qfc_status_t qfc_pages_workspace_size(const qfc_q4_cache_t *cache, int32_t batch, size_t *bytes) {
@@ -555,17 +566,21 @@ qfc_status_t qfc_pages_workspace_size(const qfc_q4_cache_t *cache, int32_t batch
     return QFC_OK;
 }
 
-qfc_status_t qfc_copy_pages(const qfc_q4_cache_t *from, const qfc_q4_cache_t *to, const int32_t *source, const int32_t *target, int32_t count, void *stream) {
+qfc_status_t qfc_copy_pages(const qfc_q4_cache_t *from, const qfc_q4_cache_t *to, const int32_t *source, const int32_t *target, int32_t count,
+                            const qfc_page_bounds_t *from_bounds, const qfc_page_bounds_t *to_bounds, void *stream) {
     if (const qfc_status_t s = check_q4_cache(from); s != QFC_OK) return s;
     if (const qfc_status_t s = check_q4_cache(to); s != QFC_OK) return s;
-    if (from->h_kv != to->h_kv || from->d_head != to->d_head || count < 0) return QFC_ERR_INVALID_ARG;
+    if (from->h_kv != to->h_kv || from->d_head != to->d_head || count < 0 || (from_bounds == nullptr) != (to_bounds == nullptr)) return QFC_ERR_INVALID_ARG;
+    if (const qfc_status_t s = check_moved(from_bounds); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_moved(to_bounds); s != QFC_OK) return s;
     if ((long)from->h_kv * 80 * from->d_head > INT32_MAX) return QFC_ERR_UNSUPPORTED;
     if (count == 0) return QFC_OK;
     if (!from->pages || !to->pages || !source || !target) return QFC_ERR_INVALID_ARG;
     if (!aligned16(from->pages) || !aligned16(to->pages) || !aligned(source, 4) || !aligned(target, 4)) return QFC_ERR_ALIGNMENT;
     const int cus = device_cus();
     if (cus < 1) return QFC_ERR_HIP;
-    return hip_status(launch_copy_pages(from->pages, from->num_pages, to->pages, to->num_pages, from->h_kv * 80 * from->d_head, source, target, count, cus, static_cast<hipStream_t>(stream)));
+    return hip_status(launch_copy_pages(from->pages, from->num_pages, to->pages, to->num_pages, from->h_kv * 80 * from->d_head, source, target, count,
+                                        moved(from_bounds, from), moved(to_bounds, to), cus, static_cast<hipStream_t>(stream)));
 }
 
 qfc_status_t qfc_take_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, const int32_t *positions, int32_t batch, int32_t table_width, int32_t *missing,
@@ -578,8 +593,10 @@ qfc_status_t qfc_take_pages(const qfc_q4_cache_t *cache, int32_t *references, in
 }
 
 qfc_status_t qfc_fork_pages(const qfc_q4_cache_t *cache, int32_t *references, const int32_t *from, int32_t from_batch, int32_t from_width, const int32_t *parents, const int32_t *positions,
-                            int32_t *page_table, int32_t batch, int32_t table_width, int32_t *missing, void *workspace, size_t workspace_bytes, void *stream) {
+                            int32_t *page_table, int32_t batch, int32_t table_width, int32_t *missing, const qfc_page_bounds_t *bounds, void *workspace, size_t workspace_bytes,
+                            void *stream) {
     if (const qfc_status_t s = check_pool(cache, references, page_table, batch, table_width); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_moved(bounds); s != QFC_OK) return s;
     if (!from || !parents || !positions || from_batch < 1 || from_width < 1) return QFC_ERR_INVALID_ARG;
     if (!aligned(from, 4) || !aligned(parents, 4) || !aligned(positions, 4)) return QFC_ERR_ALIGNMENT;
     const uintptr_t a = reinterpret_cast<uintptr_t>(from), b = reinterpret_cast<uintptr_t>(page_table);
@@ -587,8 +604,8 @@ qfc_status_t qfc_fork_pages(const qfc_q4_cache_t *cache, int32_t *references, co
     if (const qfc_status_t s = check_pool_work(cache, batch, missing, workspace, workspace_bytes); s != QFC_OK) return s;
     const int cus = device_cus();
     if (cus < 1) return QFC_ERR_HIP;
-    return hip_status(launch_fork_pages(pool_of(cache, references), from, from_batch, from_width, parents, positions, page_table, batch, table_width, missing, workspace, cus,
-                                        static_cast<hipStream_t>(stream)));
+    return hip_status(launch_fork_pages(pool_of(cache, references), from, from_batch, from_width, parents, positions, page_table, batch, table_width, missing,
+                                        moved(bounds, cache), workspace, cus,                                        static_cast<hipStream_t>(stream)));
 }
 
 qfc_status_t qfc_free_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, const int32_t *keep, int32_t batch, int32_t table_width, void *stream) {
@@ -599,13 +616,14 @@ qfc_status_t qfc_free_pages(const qfc_q4_cache_t *cache, int32_t *references, in
     return hip_status(launch_free_pages(references, cache->num_pages, page_table, keep, batch, table_width, cus, static_cast<hipStream_t>(stream)));
 }
 
-qfc_status_t qfc_compact_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, int32_t batch, int32_t table_width, int32_t *used, void *workspace,
-                               size_t workspace_bytes, void *stream) {
+qfc_status_t qfc_compact_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, int32_t batch, int32_t table_width, int32_t *used,
+                               const qfc_page_bounds_t *bounds, void *workspace, size_t workspace_bytes, void *stream) {
     if (const qfc_status_t s = check_pool(cache, references, page_table, batch, table_width); s != QFC_OK) return s;
+    if (const qfc_status_t s = check_moved(bounds); s != QFC_OK) return s;
     if (const qfc_status_t s = check_pool_work(cache, batch, used, workspace, workspace_bytes); s != QFC_OK) return s;
     const int cus = device_cus();
     if (cus < 1) return QFC_ERR_HIP;
-    return hip_status(launch_compact_pages(pool_of(cache, references), page_table, batch, table_width, used, workspace, cus, static_cast<hipStream_t>(stream)));
+    return hip_status(launch_compact_pages(pool_of(cache, references), page_table, batch, table_width, used, moved(bounds, cache), workspace, cus, static_cast<hipStream_t>(stream)));
 }
 
 // ---- attention behind common pages, and over selected ones
@@ -642,11 +660,6 @@ qfc_status_t qfc_attention_shared_q4(const void *q_f16, const qfc_requests_t *re
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_attention_shared_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, cache->pages, shared->group_start, shared->positions, shared->groups,
                                                  shared->max_group_tokens, shared->max_positions, p, workspace, out_f16, static_cast<hipStream_t>(stream)));
-}
-
-static qfc_status_t check_bounds(const qfc_page_bounds_t *b) {
-    if (!b || !b->codes || !b->steps) return QFC_ERR_INVALID_ARG;
-    return aligned16(b->codes) && aligned(b->steps, 4) ? QFC_OK : QFC_ERR_ALIGNMENT;
 }
 
 qfc_status_t qfc_bound_pages_q4(const qfc_requests_t *requests, const qfc_q4_cache_t *cache, const qfc_page_bounds_t *bounds, void *stream) {

@@ -115,6 +115,13 @@ __device__ __forceinline__ int request_of_token(const Requests &q, int token, in
     return q.batch;
 }
 
+// Bounds of pages' keys, on the device (qfc_page_bounds_t): codes [page][h_kv][2][d_head], steps [page][h_kv]
+struct PageBounds {
+    int8_t *codes;
+    float *steps;
+    int h_kv, d_head;
+};
+
 // Pages and how often tables name them, on the device
 struct PagePool {
     void *pages;

@@ -27,6 +27,7 @@ struct PagesArgs {
     int *free_of, *need;  // [chunks], [batch]
     int *source, *target, *before;  // compaction: moves, free pages before each chunk
     int chunks, slices;
+    PageBounds bounds;  // of the pages, moved with them (codes null: none)
 };
 
 __device__ __forceinline__ bool is_page(int page, int num_pages) { return page >= 0 && page < num_pages; }
@@ -219,6 +220,13 @@ __device__ __forceinline__ void copy_bytes(char *dst, const char *src, int from,
             if (at + 4096 * i < to) *reinterpret_cast<u32x4 *>(dst + at + 4096 * i) = x[i];
     }
 }
+// Bounds of a page's keys go where the page goes
+__device__ __forceinline__ void copy_bounds(const PageBounds &to, int target, const PageBounds &from, int source) {
+    if (!from.codes) return;
+    const size_t bytes = (size_t)from.h_kv * 2 * from.d_head;
+    for (size_t i = (size_t)threadIdx.x * 16; i < bytes; i += 4096) *reinterpret_cast<u32x4 *>(to.codes + target * bytes + i) = *reinterpret_cast<const u32x4 *>(from.codes + source * bytes + i);
+    for (int i = threadIdx.x; i < from.h_kv; i += 256) to.steps[(size_t)target * from.h_kv + i] = from.steps[(size_t)source * from.h_kv + i];
+}
 __device__ __forceinline__ int slice_at(const PagesArgs &a, int slice) { return (int)((long)a.page_bytes / 16 * slice / a.slices) * 16; }
 
 // Row b of the children: whole pages are its parent's, counted once more; the page in part filled is copied, a slice of it by each of the row's workgroups.
@@ -247,6 +255,7 @@ __global__ __launch_bounds__(256) void fork_pages_kernel(PagesArgs a) {
             a.table[(size_t)b * a.width + e] = e == part.entry ? fresh : page;
         }
         if (threadIdx.x == 0 && fresh >= 0) a.references[fresh] = 1;
+        if (fresh >= 0) copy_bounds(a.bounds, fresh, a.bounds, part.page);
     }
     if (fresh >= 0) copy_bytes(a.pages + (size_t)fresh * a.page_bytes, a.pages + (size_t)part.page * a.page_bytes, slice_at(a, slice), slice_at(a, slice + 1));
 }
@@ -264,11 +273,13 @@ __global__ __launch_bounds__(256) void free_pages_kernel(int *references, int nu
 }
 
 // Pairs of pages, a slice of one per workgroup, one after the other.  Bound: memory (3000 pages of 80 KiB 100 us: 4.9 TB/s).
-__global__ __launch_bounds__(256) void copy_pages_kernel(const char *from, int from_pages, char *to, int to_pages, const int *source, const int *target, int count, int page_bytes, int slices) {
+__global__ __launch_bounds__(256) void copy_pages_kernel(const char *from, int from_pages, char *to, int to_pages, const int *source, const int *target, int count, int page_bytes, int slices,
+                                                         PageBounds from_bounds, PageBounds to_bounds) {
     const long all = (long)count * slices;
     for (long i = blockIdx.x; i < all; i += gridDim.x) {
         const int pair = (int)(i / slices), slice = (int)(i % slices), s = source[pair], t = target[pair];
         if (!is_page(s, from_pages) || !is_page(t, to_pages)) continue;
+        if (slice == 0) copy_bounds(to_bounds, t, from_bounds, s);
         copy_bytes(to + (size_t)t * page_bytes, from + (size_t)s * page_bytes, (int)((long)page_bytes / 16 * slice / slices) * 16, (int)((long)page_bytes / 16 * (slice + 1) / slices) * 16);
     }
 }
@@ -318,6 +329,7 @@ __global__ __launch_bounds__(256) void move_pages_kernel(PagesArgs a, int movers
                 a.references[t] = a.references[s];
                 a.references[s] = 0;
             }
+            if (slice == 0) copy_bounds(a.bounds, t, a.bounds, s);
             copy_bytes(a.pages + (size_t)t * a.page_bytes, a.pages + (size_t)s * a.page_bytes, slice_at(a, slice), slice_at(a, slice + 1));
         }
         return;
@@ -368,10 +380,11 @@ size_t pages_workspace(int num_pages, int batch) {
     return 256 + chunks * kWords * 8 + chunks * 8 + (size_t)batch * 4 + 2 * ((size_t)num_pages / 2 + 1) * 4 + 6 * 16;
 }
 
-hipError_t launch_copy_pages(const void *from, int from_pages, void *to, int to_pages, int page_bytes, const int *source, const int *target, int count, int num_cus, hipStream_t st) {
+hipError_t launch_copy_pages(const void *from, int from_pages, void *to, int to_pages, int page_bytes, const int *source, const int *target, int count, const PageBounds &from_bounds, const PageBounds &to_bounds,
+                             int num_cus, hipStream_t st) {
     const int slices = slices_of(page_bytes, count, num_cus);
     const long all = (long)count * slices, most = 32L * num_cus;
-    copy_pages_kernel<<<(unsigned)(all < most ? all : most), 256, 0, st>>>(static_cast<const char *>(from), from_pages, static_cast<char *>(to), to_pages, source, target, count, page_bytes, slices);
+    copy_pages_kernel<<<(unsigned)(all < most ? all : most), 256, 0, st>>>(static_cast<const char *>(from), from_pages, static_cast<char *>(to), to_pages, source, target, count, page_bytes, slices, from_bounds, to_bounds);
     return hipGetLastError();
 }
 
@@ -388,8 +401,9 @@ hipError_t launch_take_pages(const PagePool &pool, int *table, const int *positi
 }
 
 hipError_t launch_fork_pages(const PagePool &pool, const int *from, int from_batch, int from_width, const int *parents, const int *positions, int *table, int batch, int width, int *missing,
-                             void *workspace, int num_cus, hipStream_t st) {
+                             const PageBounds &bounds, void *workspace, int num_cus, hipStream_t st) {
     PagesArgs a = args_of(pool, workspace, batch);
+    a.bounds = bounds;
     a.from = from, a.from_batch = from_batch, a.from_width = from_width, a.parents = parents;
     a.table = table, a.positions = positions, a.width = width, a.missing = missing;
     a.slices = slices_of(a.page_bytes, batch, num_cus);
@@ -405,8 +419,9 @@ hipError_t launch_free_pages(int *references, int num_pages, int *table, const i
     return hipGetLastError();
 }
 
-hipError_t launch_compact_pages(const PagePool &pool, int *table, int batch, int width, int *used, void *workspace, int num_cus, hipStream_t st) {
+hipError_t launch_compact_pages(const PagePool &pool, int *table, int batch, int width, int *used, const PageBounds &bounds, void *workspace, int num_cus, hipStream_t st) {
     PagesArgs a = args_of(pool, workspace, batch);
+    a.bounds = bounds;
     a.table = table, a.width = width;
     a.slices = slices_of(a.page_bytes, pool.num_pages / 4, num_cus);
     count_pages_kernel<kCompact><<<fours(a.chunks), 256, 0, st>>>(a);

@@ -407,13 +407,15 @@ hipError_t launch_attention_q4(const void *q, const Requests &req, int h_q, int 
                                hipStream_t st);
 // Pages that requests share (paged_q4.h: PagePool)
 struct PagePool;
+struct PageBounds;
 size_t pages_workspace(int num_pages, int batch);
-hipError_t launch_copy_pages(const void *from, int from_pages, void *to, int to_pages, int page_bytes, const int *source, const int *target, int count, int num_cus, hipStream_t st);
+hipError_t launch_copy_pages(const void *from, int from_pages, void *to, int to_pages, int page_bytes, const int *source, const int *target, int count, const PageBounds &from_bounds,
+                             const PageBounds &to_bounds, int num_cus, hipStream_t st);
 hipError_t launch_take_pages(const PagePool &pool, int *table, const int *positions, int batch, int width, int *missing, void *workspace, hipStream_t st);
 hipError_t launch_fork_pages(const PagePool &pool, const int *from, int from_batch, int from_width, const int *parents, const int *positions, int *table, int batch, int width, int *missing,
-                             void *workspace, int num_cus, hipStream_t st);
+                             const PageBounds &bounds, void *workspace, int num_cus, hipStream_t st);
 hipError_t launch_free_pages(int *references, int num_pages, int *table, const int *keep, int batch, int width, int num_cus, hipStream_t st);
-hipError_t launch_compact_pages(const PagePool &pool, int *table, int batch, int width, int *used, void *workspace, int num_cus, hipStream_t st);
+hipError_t launch_compact_pages(const PagePool &pool, int *table, int batch, int width, int *used, const PageBounds &bounds, void *workspace, int num_cus, hipStream_t st);
 // Bounds of pages' keys, pages selected by them
 constexpr int kSelectInLds = 32768;  // pages of a request whose scores fit the LDS
 hipError_t launch_bound_pages_q4(const Requests &req, int h_kv, int d, const void *pages, int8_t *codes, float *steps, hipStream_t st);

@@ -31,9 +31,9 @@ def test_page_refusals_before_any_launch():
     assert L.qfc_pages_workspace_size(cache(), 0, ctypes.byref(size)) == 1 and L.qfc_pages_workspace_size(cache(), 3, None) == 1 and L.qfc_pages_workspace_size(None, 3, ctypes.byref(size)) == 1
     assert L.qfc_pages_workspace_size(cache(d=96), 3, ctypes.byref(size)) == 2 and L.qfc_pages_workspace_size(cache(), (1 << 22) + 1, ctypes.byref(size)) == 2
     take = lambda c=cache(), r=A, t=A, p=A, b=2, w=3, m=A, ws=A, n=big: L.qfc_take_pages(c, r, t, p, b, w, m, ws, n, s)
-    fork = lambda c=cache(), r=A, f=far, fb=2, fw=3, pa=A, p=A, t=A, b=2, w=3, m=A, ws=A, n=big: L.qfc_fork_pages(c, r, f, fb, fw, pa, p, t, b, w, m, ws, n, s)
+    fork = lambda c=cache(), r=A, f=far, fb=2, fw=3, pa=A, p=A, t=A, b=2, w=3, m=A, ws=A, n=big, bd=None: L.qfc_fork_pages(c, r, f, fb, fw, pa, p, t, b, w, m, bd, ws, n, s)
     free = lambda c=cache(), r=A, t=A, k=A, b=2, w=3: L.qfc_free_pages(c, r, t, k, b, w, s)
-    compact = lambda c=cache(), r=A, t=A, b=2, w=3, m=A, ws=A, n=big: L.qfc_compact_pages(c, r, t, b, w, m, ws, n, s)
+    compact = lambda c=cache(), r=A, t=A, b=2, w=3, m=A, ws=A, n=big, bd=None: L.qfc_compact_pages(c, r, t, b, w, m, bd, ws, n, s)
     for call in (take, fork, free, compact):
         assert call(c=None) == 1 and call(c=cache(num=0)) == 1 and call(r=None) == 1 and call(t=None) == 1 and call(b=0) == 1 and call(w=0) == 1 and call(b=-1) == 1
         assert call(c=cache(d=80)) == 2 and call(b=(1 << 22) + 1) == 2 and call(c=cache(h=1 << 20)) == 2
@@ -45,7 +45,11 @@ def test_page_refusals_before_any_launch():
         assert fork(**{name: None}) == 1 and fork(**{name: odd}) == 4
     assert fork(fb=0) == 1 and fork(fw=0) == 1
     assert fork(f=A) == 1 and fork(f=A + 20) == 1 and fork(f=A - 20) == 1  # tables that overlap
-    copy = lambda f=cache(), t=cache(num=9), a=A, b=A, n=2: L.qfc_copy_pages(f, t, a, b, n, s)
+    copy = lambda f=cache(), t=cache(num=9), a=A, b=A, n=2, fb=None, tb=None: L.qfc_copy_pages(f, t, a, b, n, fb, tb, s)
+    bounds = lambda c=A, t=A: ctypes.byref(B.BoundsDesc(c, t))
+    for call in (fork, compact, lambda bd: copy(fb=bd, tb=bounds()), lambda bd: copy(fb=bounds(), tb=bd)):
+        assert call(bd=bounds(None)) == 1 and call(bd=bounds(t=None)) == 1 and call(bd=bounds(0x1008)) == 4 and call(bd=bounds(t=odd)) == 4
+    assert copy(fb=bounds()) == 1 and copy(tb=bounds()) == 1
     assert copy(f=None) == 1 and copy(t=None) == 1 and copy(t=cache(h=3)) == 1 and copy(t=cache(d=128)) == 1 and copy(n=-1) == 1 and copy(a=None) == 1 and copy(b=None) == 1
     assert copy(f=cache(None)) == 1 and copy(f=cache(0x1008)) == 4 and copy(a=odd) == 4 and copy(b=odd) == 4 and copy(f=cache(d=32), t=cache(d=32)) == 2
     assert copy(n=0) == 0 and copy(n=0, a=None, b=None) == 0  # nothing to do
@@ -119,6 +123,18 @@ def test_oracle_selection_by_hand():
 
 
 # ---------------------------------------------------------------- pages
+def _random_bounds(cache, seed):
+    """Bounds of no keys, and their copies on the host."""
+    b, rng = B.PageBounds(cache), np.random.default_rng(seed)
+    codes, steps = rng.integers(-128, 128, tuple(b.codes.shape), dtype=np.int8), rng.random(tuple(b.steps.shape), dtype=np.float32)
+    b.codes.copy_(torch.from_numpy(codes)), b.steps.copy_(torch.from_numpy(steps))
+    return b, codes, steps
+
+
+def _bounds_are(b, codes, steps):
+    assert np.array_equal(b.codes.cpu().numpy(), codes) and np.array_equal(b.steps.cpu().numpy(), steps)
+
+
 class Pool:
     """A cache with references and their copies on the host."""
 
@@ -177,9 +193,15 @@ def test_fork_pages(num, parents, children, from_width, width, share, h_kv, d):
     want = ref.fork(source, refs, of, positions, width, pool.pages)
     f, r, missing, (space, behind) = _i(source), _i(refs), _i([77]), pool.space(children)
     t = torch.full((children, width), 123456, dtype=torch.int32, device=DEV)
-    B.qfc_fork_pages(pool.cache, r, f, _i(of), _i(positions), t, space, missing)
+    bounds, codes, steps = _random_bounds(pool.cache, 1)
+    B.qfc_fork_pages(pool.cache, r, f, _i(of), _i(positions), t, space, missing, bounds)
     assert np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(r.cpu().numpy(), want[1]) and int(missing) == want[3]
     assert np.array_equal(pool.now(), want[2]) and np.array_equal(f.cpu().numpy(), source) and bool((behind == 0xAB).all())
+    for b in range(children):  # a copied page takes its bounds along
+        e = positions[b] // 64
+        if 0 <= of[b] < parents and positions[b] % 64 and e < min(width, from_width) and 0 <= source[of[b], e] < num and want[0][b, e] >= 0:
+            codes[want[0][b, e]], steps[want[0][b, e]] = codes[source[of[b], e]], steps[source[of[b], e]]
+    _bounds_are(bounds, codes, steps)
 
 
 @gpu
@@ -211,8 +233,12 @@ def test_compact_pages(num, batch, width, share, h_kv, d):
     refs = np.bincount(table[(table >= 0) & (table < num)], minlength=num).astype(np.int32)
     want = ref.compact(table, refs, pool.pages)
     t, r, count, (space, behind) = _i(table), _i(refs), _i([-1]), pool.space(batch)
-    B.qfc_compact_pages(pool.cache, r, t, space, count)
+    bounds, codes, steps = _random_bounds(pool.cache, 2)
+    B.qfc_compact_pages(pool.cache, r, t, space, count, bounds)
     n = want[3]
+    for a, b in zip(np.flatnonzero(refs[n:] > 0) + n, np.flatnonzero(refs[:n] <= 0)):
+        codes[b], steps[b] = codes[a], steps[a]
+    _bounds_are(bounds, codes, steps)
     assert int(count) == n and np.array_equal(t.cpu().numpy(), want[0]) and np.array_equal(r.cpu().numpy(), want[1]) and bool((behind == 0xAB).all())
     assert np.array_equal(pool.now(), want[2])
     assert bool((r[:n] > 0).all()) and not r[n:].any()
@@ -232,7 +258,12 @@ def test_copy_pages(count, h_kv, d):
     for x, y in zip(source, target):
         if 0 <= x < count + 7 and 0 <= y < count + 3:
             want[y] = a.pages[x]
-    B.qfc_copy_pages(a.cache, b.cache, _i(source), _i(target))
+    (fb, codes_a, steps_a), (tb, codes_b, steps_b) = _random_bounds(a.cache, 3), _random_bounds(b.cache, 4)
+    B.qfc_copy_pages(a.cache, b.cache, _i(source), _i(target), fb, tb)
+    for x, y in zip(source, target):
+        if 0 <= x < count + 7 and 0 <= y < count + 3:
+            codes_b[y], steps_b[y] = codes_a[x], steps_a[x]
+    _bounds_are(tb, codes_b, steps_b), _bounds_are(fb, codes_a, steps_a)
     assert np.array_equal(b.now(), want) and np.array_equal(a.now(), a.pages)
     one = a.now()
     B.qfc_copy_pages(a.cache, a.cache, _i([count + 6]), _i([0]))
