@@ -68,21 +68,24 @@ __device__ __forceinline__ Group group_of(const PartsArgs &a, int i, int lane) {
 }
 
 // The four wavefronts of a workgroup have a quarter each of the same rows' pages and meet in LDS, in the places of their pages.
-template <int D>
+template <int D, bool SPREAD = false>
 struct Four {
+    // A thread has columns of row threadIdx.x / 16: of all D from 4 (threadIdx.x % 16) on 4, and every 64th behind them; SPREAD: 2 of the row's group
+    static constexpr int PER = SPREAD ? 2 : 4;
+    typedef float cols __attribute__((ext_vector_type(PER)));
     static constexpr int STRIDE = D + 4;  // of a row (banks)
     static constexpr int WAVE = 2 * Place<D>::PART / 4;
     static_assert(16 * (STRIDE + 2) <= WAVE, "a wavefront's partial outputs, maxima and sums take its pages' places");
     float *const lds;  // (nothing beside it: with heads of 256 values two workgroups take a compute unit's LDS to the last byte)
     __device__ __forceinline__ float *sums_of(int wave, int row) const { return lds + wave * WAVE + 16 * STRIDE + 2 * row; }
-    // Each thread gets 4 columns of row threadIdx.x / 16 from column 4 (threadIdx.x % 16) on, and every 64th behind them: put(row, column, output, 1 / sum), then put_sum(row, maximum, sum).
+    // put(column, output, 1 / sum) for the thread's columns, then put_sum(maximum, sum).
     // What a lane knows of row m the threads of row threadIdx.x / 16 ask for: theirs(x).
     template <class T>
     __device__ static __forceinline__ T theirs(T x) {
         return __shfl(x, (int)(threadIdx.x >> 4), 64);
     }
     template <class Put, class PutSum>
-    __device__ __forceinline__ void meet(const Rows<D> &rows, int wave, bool wanted, const Put &put, const PutSum &put_sum) const {
+    __device__ __forceinline__ void meet(const Rows<D, SPREAD> &rows, int wave, bool wanted, const Put &put, const PutSum &put_sum) const {
         float *const mine = lds + wave * WAVE + rows.m * STRIDE;
         rows.columns([&](int d, const v4f &o) __attribute__((always_inline)) { *reinterpret_cast<v4f *>(mine + d) = o; });
         const float own_sum = rows.sum();
@@ -100,14 +103,14 @@ struct Four {
             }
             const float inv = l != 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-                const int d = 64 * c + 4 * (threadIdx.x & 15);
-                v4f o = {};
+            for (int c = 0; c < (SPREAD ? 1 : D / 64); ++c) {
+                const int d = SPREAD ? row / Rows<D, SPREAD>::ROWS * 32 + 2 * (threadIdx.x & 15) : 64 * c + 4 * (threadIdx.x & 15);
+                cols o = {};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const v4f x4 = *reinterpret_cast<const v4f *>(lds + w * WAVE + row * STRIDE + d);
+                    const cols x = *reinterpret_cast<const cols *>(lds + w * WAVE + row * STRIDE + d);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] = fmaf(f[w], x4[i], o[i]);
+                    for (int i = 0; i < PER; ++i) o[i] = fmaf(f[w], x[i], o[i]);
                 }
                 put(d, o, inv);
             }
@@ -117,6 +120,9 @@ struct Four {
     }
 };
 __device__ __forceinline__ h4 rounded(const v4f &o, float by) { return h4{(_Float16)(o[0] * by), (_Float16)(o[1] * by), (_Float16)(o[2] * by), (_Float16)(o[3] * by)}; }
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ h2 rounded(const v2f &o, float by) { return h2{(_Float16)(o[0] * by), (_Float16)(o[1] * by)}; }
 
 // Sums over parts, eight on their way at a time: part i is at place(i), its maximum and sum at ml, its columns at o
 template <class Place>
@@ -181,12 +187,13 @@ __device__ __forceinline__ Unit unit_of(const SelectedArgs &a, long place) {
     return u;
 }
 
-template <int D>
+template <int D, bool SPREAD>
 __global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArgs a) {
     extern __shared__ float lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    Rows<D> rows(lds, wave, lane);
-    const Four<D> four = {lds};
+    typedef Four<D, SPREAD> F;
+    Rows<D, SPREAD> rows(lds, wave, lane);
+    const F four = {lds};
     const long from = blockIdx.x * a.share, stop = min(from + a.share, a.places);
     for (long x = from; x < stop;) {
         const Unit u = unit_of(a, x);
@@ -201,8 +208,8 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArg
         const int b = __builtin_amdgcn_readfirstlane(request_of_token(a.req, u.token, lane, span));
         if (b >= a.req.batch || u.token < span.first || u.token - span.first >= span.count) continue;
         const int n = span.positions, lim = n - span.count + u.token - span.first + 1;
-        const bool real = u.head0 + rows.m < a.g;
-        const int head = u.kv * a.g + min(u.head0 + rows.m, a.g - 1);
+        const bool real = u.head0 + rows.row() < a.g;
+        const int head = u.kv * a.g + min(u.head0 + rows.row(), a.g - 1);
         const size_t at = (size_t)u.token * a.h_q + head;
         auto page_at = [&](int of) __attribute__((always_inline)) { return of >= 0 && of < (a.req.max_context + kPage - 1) / kPage ? page_of(a.req, b, of * kPage) : -1; };
         auto numbers = [&](int i) __attribute__((always_inline)) {
@@ -213,14 +220,14 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArg
         rows.load(a.q + at * D, real, a.scale);
         rows.walk(count, real ? lim : 0, n, a.pages, a.h_kv, u.kv, ahead, numbers,
                   [&](int i) __attribute__((always_inline)) { return (int)((uint32_t)__builtin_amdgcn_readlane(place, i & 63) * kPage); });
-        const size_t their_at = Four<D>::theirs((unsigned long long)at), part = ((size_t)blockIdx.x * 2 + (u.begin > from ? 1 : 0)) * 16 + (threadIdx.x >> 4);
+        const size_t their_at = F::theirs((unsigned long long)at), part = ((size_t)blockIdx.x * 2 + (u.begin > from ? 1 : 0)) * 16 + (threadIdx.x >> 4);
         four.meet(
-            rows, wave, Four<D>::theirs((int)real) != 0,
-            [&](int d, const v4f &o, float inv) __attribute__((always_inline)) {
+            rows, wave, F::theirs((int)real) != 0,
+            [&](int d, const typename F::cols &o, float inv) __attribute__((always_inline)) {
                 if (whole)
-                    *reinterpret_cast<h4 *>(a.out + their_at * D + d) = rounded(o, inv);
+                    *reinterpret_cast<decltype(rounded(o, inv)) *>(a.out + their_at * D + d) = rounded(o, inv);
                 else
-                    *reinterpret_cast<v4f *>(a.ws_o + part * D + d) = o;
+                    *reinterpret_cast<typename F::cols *>(a.ws_o + part * D + d) = o;
             },
             [&](float top, float l) __attribute__((always_inline)) {
                 if (!whole) a.ws_ml[part * 2] = top, a.ws_ml[part * 2 + 1] = l;
@@ -229,7 +236,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArg
 }
 
 // A workgroup for the unit that the share of workgroup blockIdx.x + 1 begins inside of, if that is the first to do so; D / 4 threads per row
-template <int D>
+template <int D, bool SPREAD>
 __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs a) {
     const int d = 4 * (threadIdx.x % (D / 4)), from_token = token_at(a.req, 0), to_token = token_at(a.req, a.req.batch);
     const long x = ((long)blockIdx.x + 1) * a.share;
@@ -238,9 +245,10 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
     const long w0 = u.begin / a.share;
     const int parts = (int)((u.end - 1) / a.share - w0) + 1;
     for (int row = threadIdx.x / (D / 4); row < min(16, a.g - u.head0); row += 1024 / D) {
+        const int held = SPREAD ? d / 32 * Rows<D, SPREAD>::ROWS + row : row;  // (the row of the parts that has these columns)
         float inv;
         const v4f o = joined(a.ws_ml, a.ws_o + d, D, parts,
-                             [&](int c) __attribute__((always_inline)) { return (size_t)((w0 + c) * 2 + (c == 0 && u.begin > w0 * a.share ? 1 : 0)) * 16 + row; }, inv);
+                             [&](int c) __attribute__((always_inline)) { return (size_t)((w0 + c) * 2 + (c == 0 && u.begin > w0 * a.share ? 1 : 0)) * 16 + held; }, inv);
         if (u.token >= from_token && u.token < to_token) *reinterpret_cast<h4 *>(a.out + ((size_t)u.token * a.h_q + u.kv * a.g + u.head0 + row) * D + d) = rounded(o, inv);
     }
 }
@@ -693,15 +701,19 @@ hipError_t launch(const PartsArgs &a, hipStream_t st) {
     attn_q4_join_kernel<D><<<(unsigned)(joins < kMostWgs ? joins : kMostWgs), 256, 0, st>>>(a);
     return hipGetLastError();
 }
+template <int D, bool SPREAD>
+hipError_t launch_selected(const SelectedArgs &a, hipStream_t st) {
+    constexpr size_t lds = Place<D>::LDS;
+    if (const hipError_t e = allow_dynamic_lds<attn_q4_selected_kernel<D, SPREAD>>(lds); e != hipSuccess) return e;
+    const unsigned wgs = (unsigned)((a.places + a.share - 1) / a.share);
+    attn_q4_selected_kernel<D, SPREAD><<<wgs, 256, lds, st>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || wgs == 1 || a.share % a.count == 0) return e;  // (no unit is cut)
+    attn_q4_join_selected_kernel<D, SPREAD><<<wgs - 1, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
 template <int D>
 hipError_t launch(const SelectedArgs &a, hipStream_t st) {
-    constexpr size_t lds = Place<D>::LDS;
-    if (const hipError_t e = allow_dynamic_lds<attn_q4_selected_kernel<D>>(lds); e != hipSuccess) return e;
-    const unsigned wgs = (unsigned)((a.places + a.share - 1) / a.share);
-    attn_q4_selected_kernel<D><<<wgs, 256, lds, st>>>(a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess || wgs == 1 || a.share % a.count == 0) return e;  // (no unit is cut)
-    attn_q4_join_selected_kernel<D><<<wgs - 1, 256, 0, st>>>(a);
-    return hipGetLastError();
+    return a.g <= Rows<D, true>::ROWS ? launch_selected<D, true>(a, st) : launch_selected<D, false>(a, st);
 }
 template <class Args>
 hipError_t launch(const Args &a, int d, hipStream_t st) {

@@ -46,11 +46,17 @@ struct Place {
 };
 
 // 16 query rows of a KV head, their sums over the pages walked so far, and the wavefront's places in LDS.  Lane (m, r) = (lane % 16, lane / 16) has row m.
-template <int D>
+//
+// SPREAD: 16 / G rows (a token's few heads), each G times, once for every group of 32 values: column m = (16 / G) a + b of the products is row b with group a's queries alone.  The products of all groups
+// then go into one sum, every lane multiplies with its own group's steps (a G-th of the multiplications and of the reads of steps), and the G columns of a row are added up; P times a step is
+// one product per position too, and of the second product's columns those of group a are good for the values of group a.  (A chunk of 157 tokens, 2 heads of 256 values on each of 4, 17 pages a token: 45 us, without 53; 32 tokens, 4 heads of 128 on
+// each of 8, 32 pages a token: 18.6 and 19.8.)
+template <int D, bool SPREAD = false>
 struct Rows {
     typedef PageLayout<D> L;
     typedef Place<D> R;
     static constexpr int G = L::G, DT = D / 16, W = L::W;
+    static constexpr int ROWS = SPREAD ? 16 / G : 16;
     const int lane, m, r;
     char *const keys, *const values;  // (the layout counts from the page's start)
     const uint32_t lds_at;
@@ -62,7 +68,11 @@ struct Rows {
         : lane(l), m(l & 15), r(l >> 4), keys(reinterpret_cast<char *>(lds) + wave * (2 * R::PART)), values(keys + R::PART - R::kHalf),
           lds_at(__builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)lds + wave * (2 * R::PART))) {}
 
-    // Row m of the queries is q (not read where it is not `real`); scale: of scores, times log2 e.  Lane (m, r) holds q[m][32 j + 8 r .. + 7], scaled by a power of two; no position has been seen
+    // Its row, and its group where SPREAD
+    __device__ __forceinline__ int row() const { return m % ROWS; }
+    __device__ __forceinline__ int group() const { return m / ROWS; }
+
+    // The lane's row of the queries is q (not read where it is not `real`); scale: of scores, times log2 e.  Lane (m, r) holds q[m][32 j + 8 r .. + 7], scaled by a power of two; no position has been seen
     __device__ __forceinline__ void load(const _Float16 *q, bool real, float scale) {
         float top = 0.0f;
 #pragma unroll
@@ -92,12 +102,27 @@ struct Rows {
             s += __shfl_xor(s, 32, 64);
             const _Float16 hi = (_Float16)(s * 0.0625f), lo = (_Float16)(s * 0.0625f - (float)hi);
             sums[j] = r == 0 ? hi : r == 1 ? lo : (_Float16)0.0f;
+            if constexpr (SPREAD) {
+                if (j != group()) qf[j] = h8{}, sums[j] = (_Float16)0.0f;
+            }
         }
 
         rest = v4f{};
 #pragma unroll
         for (int t = 0; t < DT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         run_max = kNothingYet;
+    }
+
+    __device__ __forceinline__ void step_k(int j, h8 (&st)[2]) const {
+        st[0] = *reinterpret_cast<const h8 *>(keys + L::kStepK + (j * kPage + 16 * r) * 2);
+        st[1] = *reinterpret_cast<const h8 *>(keys + L::kStepK + (j * kPage + 16 * r + 8) * 2);
+    }
+    // sum over the columns of a row, in each of them
+    __device__ static __forceinline__ float over_groups(float x) {
+        static_assert(G == 2 || G == 4 || G == 8, "columns 16 / G apart, 16 in a ring");
+        if constexpr (G >= 8) x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x122, 0xF, 0xF, true));  // row_ror 2, 4, 8
+        if constexpr (G >= 4) x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x124, 0xF, 0xF, true));
+        return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xF, 0xF, true));
     }
 
     // `count` pages of KV head kv, of which row m sees the positions below `lim` and anyone those below n.  numbers(i): page i + lane of them (-1: none), `ahead` = numbers(0);
@@ -143,6 +168,14 @@ struct Rows {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) part[t][i] *= 1.0f / 1048576.0f;
                 }
+                v4f all[4];
+                if constexpr (SPREAD) {
+                    v4f from = {};
+#pragma unroll
+                    for (int j = 0; j < G; ++j) from = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_k), qf[j], from, 0, 0, 0);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) all[t] = from;
+                }
 #pragma unroll
                 for (int jj = 0; jj < G / W; ++jj) {
                     typedef uint32_t words __attribute__((ext_vector_type(W)));
@@ -153,19 +186,31 @@ struct Rows {
                     for (int jw = 0; jw < W; ++jw) {
                         const int j = jj * W + jw;
                         const v4f zero = {};
-                        const v4f from = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_k), qf[j], zero, 0, 0, 0);
+                        v4f from = zero;
+                        if constexpr (!SPREAD) from = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, eight_k), qf[j], zero, 0, 0, 0);
                         h8 st[2];
-                        st[0] = *reinterpret_cast<const h8 *>(keys + L::kStepK + (j * kPage + 16 * r) * 2);
-                        st[1] = *reinterpret_cast<const h8 *>(keys + L::kStepK + (j * kPage + 16 * r + 8) * 2);
+                        if constexpr (!SPREAD) step_k(j, st);
 #pragma unroll
                         for (int t = 0; t < 4; ++t) {
                             const uint32_t w = c[t][jw];
                             const u32x4 op = {w & mask_lo, w & mask_hi, (w >> 8) & mask_lo, (w >> 8) & mask_hi};
-                            const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, op), qf[j], from, 0, 0, 0);
+                            if constexpr (SPREAD) {
+                                all[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, op), qf[j], all[t], 0, 0, 0);
+                            } else {
+                                const v4f x = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, op), qf[j], from, 0, 0, 0);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) part[t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[t][i]);
+                                for (int i = 0; i < 4; ++i) part[t][i] = fmaf((float)st[t >> 1][4 * (t & 1) + i], x[i], part[t][i]);
+                            }
                         }
                     }
+                }
+                if constexpr (SPREAD) {
+                    h8 st[2];
+                    step_k(group(), st);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) part[t][i] = over_groups(fmaf((float)st[t >> 1][4 * (t & 1) + i], all[t][i], part[t][i]));
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sc[e] = part[e >> 2][e & 3];
@@ -204,16 +249,29 @@ struct Rows {
             auto large = [&]() __attribute__((always_inline)) { return (steps >> 14 & 0x00010001u) * 0xFFFFu; };  // the bits of those
             bmax = over_rows(bmax) * to_score;  // (in units of log 2 from here on)
             auto product = [&](auto second, const float (&P)[16]) __attribute__((always_inline)) {
+                h8 own[2];
+                if constexpr (SPREAD) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const h8 step = step_of(group(), u);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) own[u][e] = (_Float16)fmaf(P[8 * u + e], (float)step[e], 0.0f);
+                    }
+                }
 #pragma unroll
                 for (int j = 0; j < G; ++j) {
                     if constexpr (decltype(second)::value) __builtin_amdgcn_sched_barrier(0);  // (a group after the other: registers)
                     const u32x4 c = *reinterpret_cast<const u32x4 *>(values + L::kCodesV + (j * 64 + lane) * 16);
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const h8 step = step_of(j, u);
                         h8 p;
+                        if constexpr (SPREAD) {
+                            p = own[u];
+                        } else {
+                            const h8 step = step_of(j, u);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(P[8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
+                            for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(P[8 * u + e], (float)step[e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
+                        }
                         const uint32_t c0 = c[2 * u], c1 = c[2 * u + 1];
                         const u32x4 lo = {c0 & mask_lo, (c0 >> 8) & mask_lo, c1 & mask_lo, (c1 >> 8) & mask_lo};
                         const u32x4 hi = {c0 & mask_hi, (c0 >> 8) & mask_hi, c1 & mask_hi, (c1 >> 8) & mask_hi};
@@ -239,11 +297,11 @@ struct Rows {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) P[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], to_score, kFactor - run_max));
 #pragma unroll
-                    for (int j = 0; j < G; ++j)
+                    for (int j = 0; j < (SPREAD ? 1 : G); ++j)
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
                             __builtin_amdgcn_sched_barrier(0);
-                            const h8 step = step_of(j, u);
+                            const h8 step = step_of(SPREAD ? group() : j, u);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) most = fmaxf(most, P[8 * u + e] * (float)step[e]);
                         }
@@ -299,6 +357,7 @@ struct Rows {
                 o[0][i] = fmaf(acc[2 * j][i], back, off);
                 o[1][i] = fmaf(acc[2 * j + 1][i], back * 0.0625f, off);
             }
+            if (SPREAD && j != group()) continue;  // (of the row's other columns)
 #pragma unroll
             for (int k = 0; k < 2; ++k) put(32 * j + 16 * k + 4 * r, o[k]);
         }
