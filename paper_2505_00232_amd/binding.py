@@ -2,7 +2,7 @@
 marshalling only.  PyTorch supplies device memory and the stream; every step of
 the path runs in the library's HIP kernels.  There is no fallback: if the
 library is missing or a call fails, an exception is raised.  (The two most frequent
-calls pass their arguments through the native module _marshal; where it
+calls, and those on tables of pages, pass their arguments through the native module _marshal; where it
 cannot be loaded they go through ctypes like the others.)"""
 from __future__ import annotations
 
@@ -116,10 +116,13 @@ def _load_marshal(L):
         built_for = getattr(_marshal, "built_for", "another version of this package")
         if built_for != _built_for():
             raise ImportError(f"built for {built_for}, this is {_built_for()}")
+        if not hasattr(_marshal, "bind_pages"):
+            raise ImportError("built for an earlier version of this package")
     except ImportError as e:
         warnings.warn(f"_marshal is not used, calls cost about 1 us more ({e}): run `python -m paper_2505_00232_amd.build`", RuntimeWarning, stacklevel=3)
         return None
     _marshal.bind(ctypes.cast(L.qfc_forward, ctypes.c_void_p).value, ctypes.cast(L.qfc_forward_fused, ctypes.c_void_p).value, _stream)
+    _marshal.bind_pages(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.qfc_take_pages, L.qfc_fork_pages, L.qfc_free_pages, L.qfc_compact_pages)))
     return _marshal
 
 
@@ -504,6 +507,7 @@ class PagedCache:
             raise ValueError(f"pages: {self.pages.numel()} bytes, {need} are needed")
         self.desc.pages = self.pages.data_ptr()
         self.ref, self.device = ctypes.byref(self.desc), self.pages.get_device()
+        self.address = ctypes.addressof(self.desc)
 
 
 class Requests:
@@ -620,7 +624,7 @@ class PageBounds:
         self.steps = torch.zeros((cache.num_pages, cache.h_kv), dtype=_f32, device=cache.pages.device)
         self.shape, self.device = (cache.num_pages, cache.h_kv, cache.d_head), cache.device
         self.desc = BoundsDesc(self.codes.data_ptr(), self.steps.data_ptr())
-        self.ref = ctypes.byref(self.desc)
+        self.ref, self.address = ctypes.byref(self.desc), ctypes.addressof(self.desc)
 
     def _of(self, cache: PagedCache):
         if self.shape != (cache.num_pages, cache.h_kv, cache.d_head):
@@ -642,6 +646,20 @@ def qfc_pages_workspace_size(cache: PagedCache, batch: int) -> int:
     return out.value
 
 
+def _native(call: str, cache: PagedCache, *arguments) -> bool:
+    """Whether _marshal has made the call: its arguments were in order, and so was its status."""
+    if _fast is None or _device is None or (status := getattr(_fast, call)(cache.address, cache.device, _device(), cache.num_pages, *arguments)) < 0:
+        return False
+    if status:
+        raise QfcError(status, "qfc_" + call)
+    return True
+
+
+def _moved_at(bounds: PageBounds | None, cache: PagedCache) -> int:
+    """Address of bounds that go where the cache's pages go (0: there are none)."""
+    return 0 if _moved(bounds, cache) is None else bounds.address
+
+
 def qfc_copy_pages(source_cache: PagedCache, target_cache: PagedCache, source: torch.Tensor, target: torch.Tensor, source_bounds: PageBounds | None = None,
                    target_bounds: PageBounds | None = None):
     """Pages source[i] of one cache to pages target[i] of another (or the same), and bounds of their keys with them."""
@@ -655,6 +673,8 @@ def qfc_copy_pages(source_cache: PagedCache, target_cache: PagedCache, source: t
 
 def qfc_take_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, positions: torch.Tensor, workspace: torch.Tensor, missing: torch.Tensor | None = None):
     """Free pages for the first positions[b] positions of each row that lack one."""
+    if _native("take_pages", cache, references, page_table, positions, workspace, missing):
+        return
     batch, width = _table(page_table, "page_table")
     _want(workspace, _u8, None, "workspace")
     _numbers(cache.num_pages, ("references", references), devices=(cache.device, page_table.get_device(), workspace.get_device()))
@@ -667,6 +687,8 @@ def qfc_take_pages(cache: PagedCache, references: torch.Tensor, page_table: torc
 def qfc_fork_pages(cache: PagedCache, references: torch.Tensor, from_table: torch.Tensor, parents: torch.Tensor, positions: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor,
                    missing: torch.Tensor | None = None, bounds: PageBounds | None = None):
     """Row b of page_table continues the first positions[b] positions of row parents[b] of from_table: whole pages are shared, the one in part filled is copied."""
+    if _native("fork_pages", cache, references, from_table, parents, positions, page_table, workspace, missing, _moved_at(bounds, cache)):
+        return
     from_batch, from_width = _table(from_table, "from_table")
     batch, width = _table(page_table, "page_table")
     _want(workspace, _u8, None, "workspace")
@@ -679,6 +701,8 @@ def qfc_fork_pages(cache: PagedCache, references: torch.Tensor, from_table: torc
 
 def qfc_free_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, keep: torch.Tensor | None = None):
     """Every row keeps the pages of its first keep[b] positions (None: of none) and lets the others go."""
+    if _native("free_pages", cache, references, page_table, keep):
+        return
     batch, width = _table(page_table, "page_table")
     _numbers(cache.num_pages, ("references", references), devices=(cache.device, page_table.get_device()))
     _numbers(batch, ("keep", keep))
@@ -688,6 +712,8 @@ def qfc_free_pages(cache: PagedCache, references: torch.Tensor, page_table: torc
 def qfc_compact_pages(cache: PagedCache, references: torch.Tensor, page_table: torch.Tensor, workspace: torch.Tensor, used: torch.Tensor | None = None,
                       bounds: PageBounds | None = None):
     """The pages in use get the numbers from 0 on; page_table holds all rows that name pages of the cache."""
+    if _native("compact_pages", cache, references, page_table, workspace, used, _moved_at(bounds, cache)):
+        return
     batch, width = _table(page_table, "page_table")
     _want(workspace, _u8, None, "workspace")
     _numbers(cache.num_pages, ("references", references), devices=(cache.device, page_table.get_device(), workspace.get_device()))

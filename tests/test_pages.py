@@ -158,6 +158,16 @@ def _counts(rng, num, share):
     return np.where(rng.random(num) < share, rng.integers(1, 4, num), 0).astype(np.int32)
 
 
+@pytest.fixture(params=["native", "ctypes"])
+def either_way(request, monkeypatch):
+    """Both ways of passing arguments."""
+    B.lib()
+    if request.param == "ctypes":
+        monkeypatch.setattr(B, "_fast", None)
+    elif B._fast is None:
+        pytest.skip("_marshal is not built")
+
+
 @gpu
 @pytest.mark.parametrize("num,batch,width,share", [(1, 1, 1, 0.0), (1, 2, 3, 1.0), (64, 3, 7, 0.5), (65, 1, 70, 0.1), (1023, 5, 130, 0.5), (1024, 4, 300, 0.9), (1025, 130, 9, 0.3), (5000, 37, 65, 0.7),
                                                    (70000, 11, 200, 0.99), (4096, 1, 5000, 0.0)])
@@ -273,7 +283,7 @@ def test_copy_pages(count, h_kv, d):
 
 
 @gpu
-def test_pages_of_a_search_step_by_step():
+def test_pages_of_a_search_step_by_step(either_way):
     """Forks, frees, new pages and compactions in turn, as a search over continuations makes them; the counts are those of the tables at every step."""
     rng = np.random.default_rng(9)
     num, batch, width = 400, 12, 20
@@ -304,6 +314,50 @@ def test_pages_of_a_search_step_by_step():
         assert np.array_equal(t.cpu().numpy(), table) and np.array_equal(r.cpu().numpy(), refs)
         assert np.array_equal(refs, np.bincount(table[table >= 0], minlength=num))
         assert np.array_equal(pool.now(), pages)
+
+
+@gpu
+def test_arguments_out_of_order_are_refused(either_way):
+    """Types, shapes, orders and devices that the C calls cannot see."""
+    pool = Pool(40)
+    space, _ = pool.space(3)
+    r, t, p, one = _i(np.zeros(40)), _i(np.full((3, 5), -1)), _i([70, 1, 0]), _i([0])
+    calls = {"take": lambda r=r, t=t, p=p, w=space, m=one: B.qfc_take_pages(pool.cache, r, t, p, w, m),
+             "fork": lambda r=r, t=t, p=p, w=space, m=one, f=_i(np.full((2, 5), -1)), of=_i([0, 1, 0]): B.qfc_fork_pages(pool.cache, r, f, of, p, t, w, m),
+             "free": lambda r=r, t=t, p=p: B.qfc_free_pages(pool.cache, r, t, p),
+             "compact": lambda r=r, t=t, w=space, m=one: B.qfc_compact_pages(pool.cache, r, t, w, m)}
+    bad_table = [t.long(), t.cpu(), t[0], t.t(), t.repeat(1, 2)[:, ::2], None]
+    bad_numbers = [p.long(), p.cpu(), p[:2], p.repeat(2)[::2], p[None], 5]
+    bad_pool = [r.long(), r.cpu(), r[:39], r.repeat(2)[::2], None]
+    for name, call in calls.items():
+        call()
+        for x in bad_table:
+            with pytest.raises(ValueError):
+                call(t=x)
+        for x in bad_pool:
+            with pytest.raises(ValueError):
+                call(r=x)
+        if name != "compact":
+            for x in bad_numbers:
+                with pytest.raises(ValueError):
+                    call(p=x)
+        if name != "free":
+            for x in (space.cpu(), space.float(), None):
+                with pytest.raises(ValueError):
+                    call(w=x)
+            for x in (one.long(), p, one.cpu()):
+                with pytest.raises(ValueError):
+                    call(m=x)
+            with pytest.raises(B.QfcError):
+                call(w=space[:16].clone())
+    for x in bad_table:
+        with pytest.raises(ValueError):
+            calls["fork"](f=x)
+    with pytest.raises(ValueError):
+        calls["take"](p=None)
+    other = B.PagedCache(41, 1, 64)
+    with pytest.raises(ValueError):
+        B.qfc_compact_pages(pool.cache, r, t, space, None, B.PageBounds(other))
 
 
 @gpu
