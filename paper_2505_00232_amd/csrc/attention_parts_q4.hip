@@ -54,17 +54,16 @@ __device__ __forceinline__ int tokens_of_group(const PartsArgs &a, int i) {
 }
 __device__ __forceinline__ Group group_of(const PartsArgs &a, int i, int lane) {
     const int first = group_end(a, i), end = group_end(a, i + 1);
-    int least = min(max(a.prefix[i], 0), a.longest), lead = -1;
-    for (int b0 = first; b0 < end; b0 += 64) {
-        const int b = b0 + lane;
-        const Span s = b < end ? span_of(a.req, b) : Span{0, 0, 0};
-        const uint64_t some = __ballot(s.count > 0);
-        if (lead < 0 && some) lead = b0 + __ffsll((unsigned long long)some) - 1;
-        if (s.count > 0) least = min(least, max(s.positions - s.count, 0));
+    int least = min(max(a.prefix[i], 0), a.longest), lead = INT32_MAX;
+#pragma unroll 4
+    for (int b0 = first; b0 < end; b0 += 64) {  // (no look at other lanes in here: several rounds' loads are on their way at once)
+        const int b = min(b0 + lane, end - 1);
+        const Span s = span_of(a.req, b);
+        if (s.count > 0) least = min(least, max(s.positions - s.count, 0)), lead = min(lead, b);
     }
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) least = min(least, __shfl_xor(least, off, 64));
-    return Group{__builtin_amdgcn_readfirstlane(max(lead, 0)), __builtin_amdgcn_readfirstlane(lead < 0 ? 0 : least / kPage)};
+    for (int off = 32; off > 0; off >>= 1) least = min(least, __shfl_xor(least, off, 64)), lead = min(lead, __shfl_xor(lead, off, 64));
+    return Group{__builtin_amdgcn_readfirstlane(lead == INT32_MAX ? 0 : lead), __builtin_amdgcn_readfirstlane(lead == INT32_MAX ? 0 : least / kPage)};
 }
 
 // The four wavefronts of a workgroup have a quarter each of the same rows' pages and meet in LDS, in the places of their pages.
