@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
 // multiply them with 32 rows each (310 instructions of a page and 16 rows); steps, offsets and P are taken into the sums in the same way and the same precision as there:
 //   q . k = sum_j step_j (q_j . (code_j - 8)) + sum_j offset_j sum q_j,   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
 // The common pages are in front of all rows' positions: nothing is masked.  Bound: the LDS, 63 reads of a KiB of a page and wavefront at 64 bytes a cycle, beside vector instructions in 64 % of the
-// cycles (1024 rows of 8 heads of 128 values behind 20000 positions 150 us: 460 TFLOP/s).
+// cycles (1024 rows of 8 heads of 128 values behind 20000 positions 167 us: 500 TFLOP/s).
 template <int D>
 struct Wide {
     typedef PageLayout<D> L;
