@@ -485,11 +485,11 @@ def test_attention_shared(group, prefix, S, n, h_q, h_kv, d, rows_rule):
 
 
 @gpu
-def test_attention_shared_extremes(rows_rule):
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_attention_shared_extremes(rows_rule, d):
     """Pages that are missing, in the common part and behind it; a request that sees nothing; queries that are infinite or no numbers stay their own rows' matter; steps of 2 and more."""
     rng = np.random.default_rng(22)
-    group, prefix, S, n, h_q, h_kv, d = [0, 3], [320], [1, 1, 1, 1], [400, 500, 330, 0], 4, 2, 64
-    k, v = _normal(rng, 400, h_kv, d), _normal(rng, 400, h_kv, d)
+    group, prefix, S, n, h_q, h_kv = [0, 3], [320], [1, 1, 1, 1], [400, 500, 330, 0], 4, 2
     cache, table, K, V, P = _shared_batch(rng, group, prefix, S[:3], n[:3], h_kv, d)
     table = np.pad(table, ((0, 1), (0, 0)), constant_values=-1)
     table[:3, 2] = -1
@@ -739,6 +739,43 @@ def test_attention_selected(S, n, h_q, h_kv, d, count):
                 rows = q[at + i].reshape(1, h_q, d)[:, heads]
                 _close(got[at + i:at + i + 1, heads], *q4.attention(rows, K[b][:m, kv:kv + 1], V[b][:m, kv:kv + 1], P[b][:m, kv:kv + 1], there))
         at += s
+
+
+@gpu
+@pytest.mark.parametrize("h_q,h_kv,d", [(2, 1, 64), (8, 1, 64), (9, 1, 64), (8, 2, 128), (5, 1, 128), (4, 2, 256), (3, 1, 256), (17, 1, 256)])
+@pytest.mark.parametrize("values", ["steps of 2 and more", "far from zero", "one of them large", "infinite and no queries"])
+def test_attention_selected_extremes(h_q, h_kv, d, values):
+    """On both sides of the number of heads that are spread over the groups of values."""
+    rng = np.random.default_rng(53)
+    S, n, g = [1, 2], [500, 700], h_q // h_kv
+    table, num = _pages(rng, n)
+    k, v, q = _normal(rng, sum(n), h_kv, d), _normal(rng, sum(n), h_kv, d), _normal(rng, 3, h_q * d)
+    if values == "steps of 2 and more":
+        v[::3] *= np.float16(300)
+        v[::7, :, 32:64] *= np.float16(20)
+    elif values == "far from zero":
+        v += np.float16(1000)
+        k += np.float16(20)
+    elif values == "one of them large":
+        v[:, :, 5] = 60000
+        k[40, :, :] = q.reshape(3, h_q, d)[0, 0]
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num, k, v)
+    picks = [np.arange(8), np.array([0, 3, 4, 6, 7, 8, 9, 10]), np.array([10, 2, 1, 0, 5, 6, 7, 8])]
+    selected = np.repeat(np.stack(picks)[:, None], h_kv, 1).astype(np.int32)
+    if values == "infinite and no queries":
+        want = _attend_selected(_requests(S, n, table), q, h_q, cache, _i(selected)).reshape(3, h_q, d)
+        bad = q.copy().reshape(3, h_q, d)
+        bad[0, 0, 3], bad[1, h_q - 1, d - 1] = np.nan, np.inf
+        got = _attend_selected(_requests(S, n, table), bad.reshape(3, -1), h_q, cache, _i(selected)).reshape(3, h_q, d)
+        assert np.all(np.isnan(got[0, 0])) and np.all(np.isnan(got[1, h_q - 1]))
+        keep = np.ones((3, h_q), bool)
+        keep[0, 0] = keep[1, h_q - 1] = False
+        assert np.array_equal(got[keep], want[keep])
+        return
+    got = _attend_selected(_requests(S, n, table), q, h_q, cache, _i(selected)).reshape(3, h_q, d)
+    for t, (b, m) in enumerate(((0, 500), (1, 699), (1, 700))):
+        there = np.isin(np.arange(m) // 64, picks[t])
+        _close(got[t:t + 1], *q4.attention(q.reshape(3, h_q, d)[t:t + 1], K[b][:m], V[b][:m], P[b][:m], there))
 
 
 @gpu
