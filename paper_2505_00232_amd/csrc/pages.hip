@@ -285,18 +285,14 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(const char *from, int f
 }
 
 // ---- compaction.  U pages are in use: the i-th of those with numbers from U on goes to the i-th free page below U.  A wavefront per chunk lists both.
-__global__ __launch_bounds__(256) void list_moves_kernel(PagesArgs a, int *used_out) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), chunk = (int)blockIdx.x * 4 + wave;
-    if (chunk >= a.chunks) return;
+__device__ __forceinline__ void list_chunk(const PagesArgs &a, int chunk, int lane, int *used_out) {
+    const uint64_t held = lane < kWords ? a.bits[(size_t)chunk * kWords + lane] : 0;  // lane w: word w
     int before = sum_of(a.free_of, chunk, lane);
     const int free_all = before + sum_of(a.free_of + chunk, a.chunks - chunk, lane), used = a.num_pages - free_all;
     // free pages below U, and with them the used ones: U lies in chunk cut
-    const int cut = used / kChunk;
-    int free_below = cut >= chunk ? before + sum_of(a.free_of + chunk, min(cut, a.chunks) - chunk, lane) : sum_of(a.free_of, cut, lane);
-    for (int w = 0; w < kWords && cut < a.chunks; ++w) {
-        const int left = used - cut * kChunk - 64 * w;
-        if (left > 0) free_below += __popcll(a.bits[(size_t)cut * kWords + w] & (left >= 64 ? ~0ull : (1ull << left) - 1));
-    }
+    const int cut = used / kChunk, left = used - cut * kChunk - 64 * lane;
+    const uint64_t at_cut = cut < a.chunks && lane < kWords && left > 0 ? a.bits[(size_t)cut * kWords + lane] & (left >= 64 ? ~0ull : (1ull << left) - 1) : 0;
+    const int free_below = (cut >= chunk ? before + sum_of(a.free_of + chunk, min(cut, a.chunks) - chunk, lane) : sum_of(a.free_of, cut, lane)) + wave_sum((int)__popcll(at_cut));
     if (lane == 0) {
         a.before[chunk] = before;
         if (chunk == 0) {
@@ -306,17 +302,29 @@ __global__ __launch_bounds__(256) void list_moves_kernel(PagesArgs a, int *used_
         }
     }
     const int used_below = used - free_below;
+#pragma unroll
     for (int w = 0; w < kWords; ++w) {
-        const uint64_t word = a.bits[(size_t)chunk * kWords + w];
+        const uint64_t word = __shfl((unsigned long long)held, w, 64);
         const long page = (long)chunk * kChunk + 64 * w + lane;
-        const int free_before = before + __popcll(word & ((1ull << lane) - 1));
+        const int free_before = before + (int)__popcll(word & ((1ull << lane) - 1));
         if (page < a.num_pages) {
             const bool is_free = word >> lane & 1;
             if (is_free && page < used) a.target[free_before] = (int)page;
             if (!is_free && page >= used) a.source[(int)page - free_before - used_below] = (int)page;
         }
-        before += __popcll(word);
+        before += (int)__popcll(word);
     }
+}
+__global__ __launch_bounds__(256) void list_moves_kernel(PagesArgs a, int *used_out) {
+    const int chunk = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (chunk < a.chunks) list_chunk(a, chunk, threadIdx.x & 63, used_out);
+}
+// Small pools: counted and listed in one launch, by one workgroup (5000 pages 5.6 us, two launches 2.4 and 5.2)
+__global__ __launch_bounds__(1024) void list_few_moves_kernel(PagesArgs a, int *used_out) {
+    const int chunk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (chunk < a.chunks) count_chunk(a, chunk, lane);
+    __syncthreads();  // (what the workgroup has written to memory is seen by all of it)
+    if (chunk < a.chunks) list_chunk(a, chunk, lane, used_out);
 }
 
 // Moves (a slice of a page per workgroup, one after the other) and tables (the other workgroups)
@@ -424,8 +432,12 @@ hipError_t launch_compact_pages(const PagePool &pool, int *table, int batch, int
     a.bounds = bounds;
     a.table = table, a.width = width;
     a.slices = slices_of(a.page_bytes, pool.num_pages / 4, num_cus);
-    count_pages_kernel<kCompact><<<fours(a.chunks), 256, 0, st>>>(a);
-    list_moves_kernel<<<fours(a.chunks), 256, 0, st>>>(a, used);
+    if (pool.num_pages <= kSmallPool) {
+        list_few_moves_kernel<<<1, 1024, 0, st>>>(a, used);
+    } else {
+        count_pages_kernel<kCompact><<<fours(a.chunks), 256, 0, st>>>(a);
+        list_moves_kernel<<<fours(a.chunks), 256, 0, st>>>(a, used);
+    }
     const long all = ((long)batch * width + 255) / 256, tables = all < 4L * num_cus ? all : 4L * num_cus;
     const long moves = (long)(pool.num_pages / 2 > 0 ? pool.num_pages / 2 : 1) * a.slices, movers = moves < 16L * num_cus ? moves : 16L * num_cus;
     move_pages_kernel<<<(unsigned)(movers + tables), 256, 0, st>>>(a, (int)movers);

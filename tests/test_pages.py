@@ -232,7 +232,8 @@ def test_free_pages(num, batch, width):
 
 @gpu
 @pytest.mark.parametrize("num,batch,width,share,h_kv,d", [(1, 1, 1, 0.0, 1, 64), (1, 1, 1, 1.0, 1, 64), (64, 3, 30, 0.5, 1, 64), (1024, 9, 200, 1.0, 1, 64), (1025, 9, 200, 0.5, 2, 64),
-                                                          (3001, 50, 40, 0.03, 1, 128), (2048, 3, 900, 0.5, 1, 256), (5000, 17, 300, 0.9, 3, 64)])
+                                                          (3001, 50, 40, 0.03, 1, 128), (2048, 3, 900, 0.5, 1, 256), (5000, 17, 300, 0.9, 3, 64),
+                                                          (16384, 30, 400, 0.5, 1, 64), (16385, 30, 400, 0.7, 1, 64), (40000, 5, 900, 0.05, 1, 64)])
 def test_compact_pages(num, batch, width, share, h_kv, d):
     rng = np.random.default_rng(num)
     pool = Pool(num, h_kv, d)
