@@ -405,7 +405,7 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
  *   missing       device, int32 [1], or null: how many entries got no page because none was free (they are -1, and attention does not see their positions)
  *   bounds        host, or null: bounds of the keys of all pages (below), which belong to a page's number; they go where a page's contents go
  *   workspace     device scratch of qfc_pages_workspace_size bytes, 16-byte aligned, one call's at a time
- * Errors of all: QFC_ERR_INVALID_ARG (null pointers, sizes below 1), QFC_ERR_UNSUPPORTED (d_head other than 64, 128, 256; batch above 2^22; a page of 2^31 bytes and more),
+ * Errors of all: QFC_ERR_INVALID_ARG (null pointers, sizes below 1), QFC_ERR_UNSUPPORTED (d_head other than 64, 128, 256; batch above 2^22; a table of 2^31 entries, a page of 2^31 bytes and more),
  * QFC_ERR_ALIGNMENT (16 bytes for pages and workspace, 4 for int32 arrays), QFC_ERR_BUFFER_TOO_SMALL. */
 
 /* Bounds of the keys that a page holds for a KV head, for choosing pages without reading them: with hi_d and lo_d the largest and the smallest value of component d over the page's

@@ -532,7 +532,7 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
 static qfc_status_t check_pool(const qfc_q4_cache_t *c, const int32_t *references, const int32_t *table, int32_t batch, int32_t width) {
     if (const qfc_status_t s = check_q4_cache(c); s != QFC_OK) return s;
     if (!references || !table || batch < 1 || width < 1) return QFC_ERR_INVALID_ARG;
-    if (batch > 1 << 22 || (long)c->h_kv * 80 * c->d_head > INT32_MAX) return QFC_ERR_UNSUPPORTED;
+    if (batch > 1 << 22 || (long)batch * width > INT32_MAX || (long)c->h_kv * 80 * c->d_head > INT32_MAX) return QFC_ERR_UNSUPPORTED;  // (entries without a page are counted in 32 bits)
     if (!aligned(references, 4) || !aligned(table, 4)) return QFC_ERR_ALIGNMENT;
     return QFC_OK;
 }
@@ -605,7 +605,7 @@ qfc_status_t qfc_fork_pages(const qfc_q4_cache_t *cache, int32_t *references, co
     const int cus = device_cus();
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_fork_pages(pool_of(cache, references), from, from_batch, from_width, parents, positions, page_table, batch, table_width, missing,
-                                        moved(bounds, cache), workspace, cus,                                        static_cast<hipStream_t>(stream)));
+                                        moved(bounds, cache), workspace, cus, static_cast<hipStream_t>(stream)));
 }
 
 qfc_status_t qfc_free_pages(const qfc_q4_cache_t *cache, int32_t *references, int32_t *page_table, const int32_t *keep, int32_t batch, int32_t table_width, void *stream) {

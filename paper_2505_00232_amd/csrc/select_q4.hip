@@ -346,7 +346,7 @@ __global__ __launch_bounds__(512) void select_pages_kernel(SelectArgs a) {
                 prefix |= (uint32_t)found[0] << shift, mask |= 255u << shift, left = found[1];
             }
             // ---- the list: above it, and of those level with it the first `left`
-            int above = 0, level = 0;  // before this round
+            int above = 0, level = 0;  // before this pass
             for (int base = mid0; base < mid1; base += blockDim.x) {
                 const int p = base + (int)threadIdx.x;
                 const uint32_t key = p < mid1 ? key_of(scores[p]) : 0;

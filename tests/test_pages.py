@@ -37,6 +37,7 @@ def test_page_refusals_before_any_launch():
     for call in (take, fork, free, compact):
         assert call(c=None) == 1 and call(c=cache(num=0)) == 1 and call(r=None) == 1 and call(t=None) == 1 and call(b=0) == 1 and call(w=0) == 1 and call(b=-1) == 1
         assert call(c=cache(d=80)) == 2 and call(b=(1 << 22) + 1) == 2 and call(c=cache(h=1 << 20)) == 2
+        assert call(b=1 << 22, w=512) == 2 and call(b=3, w=(1 << 31) - 1) == 2  # tables of 2^31 entries and more
         assert call(r=odd) == 4 and call(t=odd) == 4
     for call in (take, fork, compact):
         assert call(ws=None) == 1 and call(c=cache(None)) == 1 and call(n=8) == 3 and call(ws=0x1008) == 4 and call(m=odd) == 4 and call(c=cache(0x1008)) == 4
