@@ -141,15 +141,15 @@ __device__ __forceinline__ void pick(const float *scores, int mid0, int mid1, in
         least = max(least, ~key[i]), most = max(most, key[i]);
     }
     uint32_t lo = ~wave_max(least);
-    const uint32_t range = wave_max(most) - lo;
+    uint32_t range = wave_max(most) - lo;  // keys lo .. lo + range are in the bins, those above them are counted
     int shift = range >= 64 ? 26 - __builtin_clz(range) : 0, above = 0, left = 0;  // (range >> shift is below 64)
     for (;;) {
         bins[lane] = 0;
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const uint32_t bin = (key[i] - lo) >> shift;
-            if (mid0 + 64 * i + lane < mid1 && key[i] >= lo && bin < 64) atomicAdd(bins + (63 - bin), 1);
+            const uint32_t over = key[i] - lo;
+            if (mid0 + 64 * i + lane < mid1 && key[i] >= lo && over <= range) atomicAdd(bins + (63 - (over >> shift)), 1);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
         const int own = __hip_atomic_load(bins + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT), upto = above + sum_upto(own);
@@ -166,6 +166,7 @@ __device__ __forceinline__ void pick(const float *scores, int mid0, int mid1, in
             left = k - above;  // lo is the k-th: of those level with it
             break;
         }
+        range = (1u << shift) - 1;
         shift = max(shift - 6, 0);
     }
 #pragma unroll
@@ -186,17 +187,83 @@ __device__ __forceinline__ void pick(const float *scores, int mid0, int mid1, in
         }
     }
 }
-constexpr int kPicked = 2048;  // scores that one wavefront picks from
+constexpr int kPicked = 512;  // scores that one wavefront picks from
 
-// Scores of all pages that a token sees, the score that is the last to be taken (a byte of it at a time, by how many scores begin so), and the list in ascending order: a workgroup per
-// token and KV head does all of it (kAll), or several of them the scores (kScores), and one the rest (kList).  Bound: latency, of the requests' arrays, the table, the bounds one behind the
-// other, and of some twenty barriers.
+// The same by the wavefronts of a workgroup, each with a run of the scores (from .. to - 1 of mid0 .. mid1 - 1, in order), which it reads again in every round: at(p).  bins: 4 sets of 64, zeros;
+// places: two words per wavefront.  A round has one barrier: its bins are another set's than those that are read, and those that were read are zeroed.  (8 lists of 8000 scores, with the launch
+// that makes these, 20 us; a byte at a time, four rounds of three barriers and all scores counted at few words, 39.  2000 scores 1.4 us less than by one wavefront from 32 registers.)
+template <class At>
+__device__ __forceinline__ void pick_together(const At &at, int from, int to, int k, int lane, int wave, int waves, int *bins, int (*places)[2], int *out) {
+    uint32_t least = 0, most = 0;  // (least: complemented)
+#pragma unroll 4
+    for (int p = from + lane; p < to; p += 64) {
+        const uint32_t key = key_of(at(p));
+        least = max(least, ~key), most = max(most, key);
+    }
+    least = wave_max(least), most = wave_max(most);
+    if (lane == 0) places[wave][0] = (int)least, places[wave][1] = (int)most;
+    __syncthreads();
+    for (int w = 0; w < waves; ++w) least = max(least, (uint32_t)places[w][0]), most = max(most, (uint32_t)places[w][1]);
+    uint32_t lo = __builtin_amdgcn_readfirstlane(~least);
+    uint32_t range = __builtin_amdgcn_readfirstlane(most) - lo;
+    int shift = range >= 64 ? 26 - __builtin_clz(range) : 0, above = 0, left = 0;  // (range >> shift is below 64)
+    for (int set = 0;; set = (set + 1) & 3) {
+        int *const here = bins + 64 * set;
+#pragma unroll 4
+        for (int p = from + lane; p < to; p += 64) {
+            const uint32_t key = key_of(at(p)), over = key - lo;
+            if (key >= lo && over <= range) atomicAdd(here + (63 - (over >> shift)), 1);
+        }
+        __syncthreads();
+        const int own = here[lane], upto = above + sum_upto(own);
+        if (wave == 0) bins[64 * ((set + 3) & 3) + lane] = 0;  // (read in front of the barrier, used again behind two others)
+        const int l = (int)__ffsll((unsigned long long)__ballot(upto >= k)) - 1;  // (the bins hold the k-th)
+        lo += (uint32_t)(63 - l) << shift;
+        const int upto_l = __builtin_amdgcn_readlane(upto, l);
+        if (upto_l == k) {
+            lo -= 1;  // (all above this)
+            break;
+        }
+        above = upto_l - __builtin_amdgcn_readlane(own, l);
+        if (shift == 0) {
+            left = k - above;  // lo is the k-th: of those level with it
+            break;
+        }
+        range = (1u << shift) - 1;
+        shift = max(shift - 6, 0);
+    }
+    int mine = 0, level = 0;
+#pragma unroll 4
+    for (int p = from + lane; p < to; p += 64) {
+        const uint32_t key = key_of(at(p));
+        mine += key > lo, level += key == lo;
+    }
+    mine = __builtin_amdgcn_readlane(sum_upto(mine), 63), level = __builtin_amdgcn_readlane(sum_upto(level), 63);
+    if (lane == 0) places[wave][0] = mine, places[wave][1] = level;
+    __syncthreads();
+    int level_before = 0;
+    for (int w = 0; w < wave; ++w) out += places[w][0], level_before += places[w][1];
+    out += min(level_before, left), left = max(left - level_before, 0);
+    for (int p0 = from; p0 < to; p0 += 64) {
+        const int p = p0 + lane;
+        const uint32_t key = p < to ? key_of(at(p)) : 0;
+        const bool is_above = p < to && key > lo, is_level = p < to && key == lo;
+        const uint64_t above_bits = __ballot(is_above), level_bits = __ballot(is_level);
+        const int of_level = min((int)__popcll(level_bits), left), level_in_front = lower(level_bits);
+        if (is_above || (is_level && level_in_front < left)) out[lower(above_bits) + min(level_in_front, left)] = p;
+        out += (int)__popcll(above_bits) + of_level;
+        left -= of_level;
+    }
+}
+
+// Scores of all pages that a token sees, and the list of those to be taken in ascending order: a workgroup per token and KV head does all of it (kAll), or several of them the scores (kScores),
+// and one the rest (kList).  Bound: latency, of the requests' arrays, the table, the bounds one behind the other, and of the search's barriers.
 enum { kAll, kScores, kList };
 template <int D, int PHASE, bool IN_LDS>
 __global__ __launch_bounds__(512) void select_pages_kernel(SelectArgs a) {
     constexpr int C = D / 64, AHEAD = 2;  // chunks of 64 components; groups of 16 pages on their way
     extern __shared__ float lds_scores[];
-    __shared__ int counts[256], found[2], taken[8][2];
+    __shared__ int counts[256], taken[8][2];
     __shared__ float tops[C][16], steps_of[16];
     __shared__ i32x4 codes[2][C][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, m = lane & 15, r = lane >> 4;
@@ -302,67 +369,17 @@ __global__ __launch_bounds__(512) void select_pages_kernel(SelectArgs a) {
                     const int n = mid1 - mid0;
                     if (n <= 128)
                         pick<2>(from, mid0, mid1, k, lane, counts, out + a.first);
-                    else if (n <= 512)
-                        pick<8>(from, mid0, mid1, k, lane, counts, out + a.first);
-                    else if (n <= 1024)
-                        pick<16>(from, mid0, mid1, k, lane, counts, out + a.first);
                     else
-                        pick<32>(from, mid0, mid1, k, lane, counts, out + a.first);
+                        pick<8>(from, mid0, mid1, k, lane, counts, out + a.first);
                 }
             } else {
-            if constexpr (PHASE == kList && IN_LDS)
-                for (int p = mid0 + (int)threadIdx.x; p < mid1; p += blockDim.x) scores[p] = kept[p];
-            __syncthreads();
-            // ---- the k-th of them
-            uint32_t prefix = 0, mask = 0;
-            int left = k;
-            for (int shift = 24; shift >= 0; shift -= 8) {
+                const int run = ((mid1 - mid0 + waves - 1) / waves + 63) / 64 * 64, from = min(mid0 + wave * run, mid1), to = min(from + run, mid1);
+                if constexpr (PHASE == kList && IN_LDS)  // (a wavefront reads what it has written)
+#pragma unroll 4
+                    for (int p = from + lane; p < to; p += 64) scores[p] = kept[p];
                 for (int i = threadIdx.x; i < 256; i += blockDim.x) counts[i] = 0;
                 __syncthreads();
-                for (int p = mid0 + (int)threadIdx.x; p < mid1; p += blockDim.x) {
-                    const uint32_t key = key_of(scores[p]);
-                    if ((key & mask) == prefix) atomicAdd(counts + (key >> shift & 255u), 1);
-                }
-                __syncthreads();
-                if (wave == 0) {  // lane l: bytes 255 - 4 l and the three below
-                    int own[4], all = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) all += own[i] = counts[255 - 4 * lane - i];
-                    int upto = all;
-#pragma unroll
-                    for (int off = 1; off < 64; off <<= 1) {
-                        const int other = __shfl_up(upto, off, 64);
-                        upto += lane >= off ? other : 0;
-                    }
-                    if (upto >= left && upto - all < left) {
-                        int rest = left - (upto - all), byte = 255 - 4 * lane;
-#pragma unroll
-                        for (int i = 0; i < 3; ++i)
-                            if (rest > own[i] && byte == 255 - 4 * lane - i) rest -= own[i], --byte;
-                        found[0] = byte, found[1] = rest;
-                    }
-                }
-                __syncthreads();
-                prefix |= (uint32_t)found[0] << shift, mask |= 255u << shift, left = found[1];
-            }
-            // ---- the list: above it, and of those level with it the first `left`
-            int above = 0, level = 0;  // before this pass
-            for (int base = mid0; base < mid1; base += blockDim.x) {
-                const int p = base + (int)threadIdx.x;
-                const uint32_t key = p < mid1 ? key_of(scores[p]) : 0;
-                const bool is_above = p < mid1 && key > prefix, is_level = p < mid1 && key == prefix;
-                const uint64_t above_bits = __ballot(is_above), level_bits = __ballot(is_level), lower = (1ull << lane) - 1;
-                __syncthreads();  // (the round before has been read)
-                if (lane == 0) taken[wave][0] = __popcll(above_bits), taken[wave][1] = __popcll(level_bits);
-                __syncthreads();
-                int above_here = above + __popcll(above_bits & lower), level_here = level + __popcll(level_bits & lower);
-                for (int w = 0; w < waves; ++w) {
-                    const int t0 = taken[w][0], t1 = taken[w][1];
-                    if (w < wave) above_here += t0, level_here += t1;
-                    above += t0, level += t1;
-                }
-                if (is_above || (is_level && level_here < left)) out[a.first + above_here + min(level_here, left)] = p;
-            }
+                pick_together([&](int p) __attribute__((always_inline)) { return scores[p]; }, from, to, k, lane, wave, waves, counts, taken, out + a.first);
             }
         }
         if constexpr (PHASE == kScores) continue;

@@ -670,6 +670,36 @@ def test_select_pages(S, n, h_q, h_kv, d, first, last, count, alike):
 
 
 @gpu
+@pytest.mark.parametrize("pages,count", [(40, 7), (130, 11), (130, 99), (300, 50), (514, 3), (700, 33), (1030, 600), (2050, 77), (4000, 1234), (16400, 333), (33000, 2000)])
+def test_select_pages_whose_scores_are_close(pages, count):
+    """Scores that are neighbours among the numbers of 32 bits, or some of them far off: every step of the search for the last one's place decides."""
+    d, h = 64, 2
+    rng = np.random.default_rng(pages + count)
+    cache = B.PagedCache(pages, h, d)
+    b = B.PageBounds(cache)
+    codes = np.zeros((pages, h, 2, d), np.int8)
+    codes[:, :, 0, 0], codes[:, :, 1, 0] = 127, -127
+    i = np.stack([rng.permutation(pages), rng.integers(0, max(pages // 3, 2), pages)])
+    q = np.zeros((2, d), np.float16)
+    q[0, 0], q[1, 0] = 1, 1
+    table = rng.permutation(pages).astype(np.int32)[None]
+    n = pages * 64
+    req = _requests([1], [n], table)
+    for far in (0.0, 0.1, 0.9):
+        steps = (1.5 + i * 2.0 ** -23).astype(np.float32)
+        steps = np.where(rng.random((2, pages)) < far, rng.random((2, pages), dtype=np.float32) * np.float32(4), steps).T
+        b.codes.copy_(torch.from_numpy(codes)), b.steps.copy_(torch.from_numpy(np.ascontiguousarray(steps)))
+        for limit in sorted({pages, max(pages, 3000), 33000}):  # scores in the LDS, or in the workspace
+            wide = np.full((1, limit), -1, np.int32)
+            wide[:, :pages] = table
+            far_off = B.Requests(req.token_start, req.context, _i(wide), 1, 1, limit * 64)
+            got = _select(far_off, q.reshape(1, -1), 2, cache, b, 1, 1, count, 1).cpu().numpy()[0]
+            for kv in range(2):
+                score = ref.scores(q[kv:kv + 1], codes[table[0], kv], steps[table[0], kv], np.ones(pages, bool))
+                assert np.array_equal(got[kv], ref.select(score, pages, 1, 1, count)), (far, limit, kv)
+
+
+@gpu
 def test_a_page_scores_at_least_what_its_keys_do():
     """What the bounds are for: up to the rounding of the query (half a code of each of d components, against bounds of 127 steps) no key scores above its page."""
     rng = np.random.default_rng(42)
