@@ -5,6 +5,8 @@
 // No key k of the page has q . k above sum_d max(q_d, 0) hi_d + min(q_d, 0) lo_d.  With q in 8 bits too (s_h = max |q| / 127, codes rounded to the nearest) that sum is one of whole numbers
 // below 2^24, two runs of v_mfma_i32_16x16x64_i8 (the positive codes against the upper bounds, the negative ones against the lower), and exact in whatever order; a page's score for a
 // token and KV head is the most any of the head's queries could reach, step max_h s_h sum_h, each product rounded to 32 bits.
+#include <algorithm>
+
 #include "paged_q4.h"
 
 namespace qfc {
@@ -392,9 +394,10 @@ int pages_below(int max_context) { return (max_context + kPage - 1) / kPage; }
 
 // Tokens and heads whose scores are kept in memory at a time
 constexpr int kSlice = 512;
-// One launch where scores fit the LDS and a workgroup has them at once, or workgroups fill the card; else scores and lists are launches of their own (four requests of up to
-// 131000 positions: one launch 27 us, two 7 and 10).
-bool one_launch(long items, int pages, int num_cus) { return pages <= kSelectInLds && (pages <= 1024 || items >= num_cus); }
+// One launch where scores fit the LDS and a workgroup has them at once, or workgroups are as many as half the compute units; else scores and lists are launches of their own.  One and two, us, heads
+// of 128 values: 8 lists of 500 pages 10.1 and 9.1, 32 of 500 10.2 and 9.5, 128 of 500 10.7 and 11.2; 8 of 1000 15.4 and 10.2, 64 of 2000 29.1 and 19.3, 128 of 2000 29.3 and 26.4, 248 of 2000 31.6
+// and 40.4.
+bool one_launch(long items, int pages, int num_cus) { return pages <= kSelectInLds && (pages <= 512 || 2 * items > num_cus); }
 
 template <int D, int PHASE, bool IN_LDS>
 hipError_t launch_phase(const SelectArgs &a, int threads, long wgs, hipStream_t st) {
@@ -412,7 +415,8 @@ hipError_t launch_select(SelectArgs a, int num_cus, hipStream_t st) {
     const long all = a.items;
     for (; a.item0 < all; a.item0 += kSlice) {
         a.items = all - a.item0 < kSlice ? all - a.item0 : kSlice;
-        a.pieces = (a.most_pages + 127) / 128;
+        // 128 pages are on their way to the wavefronts of a workgroup at once; four workgroups per compute unit have them (as many as there are pieces: 4 requests of 16000 pages 54 us, so 48)
+        a.pieces = (int)std::min((a.most_pages + 127L) / 128, std::max(1L, (4L * num_cus + a.items - 1) / a.items));
         if (const hipError_t e = launch_phase<D, kScores, false>(a, 256, a.items * a.pieces, st); e != hipSuccess) return e;
         const hipError_t e = a.most_pages <= kSelectInLds ? launch_phase<D, kList, true>(a, 512, a.items, st) : launch_phase<D, kList, false>(a, 512, a.items, st);
         if (e != hipSuccess) return e;
