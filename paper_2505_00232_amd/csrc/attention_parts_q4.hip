@@ -66,10 +66,10 @@ __device__ __forceinline__ Group group_of(const PartsArgs &a, int i, int lane) {
     return Group{__builtin_amdgcn_readfirstlane(lead == INT32_MAX ? 0 : lead), __builtin_amdgcn_readfirstlane(lead == INT32_MAX ? 0 : least / kPage)};
 }
 
-// The four wavefronts of a workgroup have a quarter each of the same rows' pages and meet in LDS, in the places of their pages.
-template <int D, bool SPREAD = false>
-struct Four {
-    // A thread has columns of row threadIdx.x / 16: of all D from 4 (threadIdx.x % 16) on 4, and every 64th behind them; SPREAD: 2 of the row's group
+// The wavefronts of a workgroup have an equal share each of the same rows' pages and meet in LDS, in the places of their pages.
+template <int D, bool SPREAD = false, int WAVES = 4>
+struct Meeting {
+    // A thread (of the first 256) has columns of row threadIdx.x / 16: of all D from 4 (threadIdx.x % 16) on 4, and every 64th behind them; SPREAD: 2 of the row's group
     static constexpr int PER = SPREAD ? 2 : 4;
     typedef float cols __attribute__((ext_vector_type(PER)));
     static constexpr int STRIDE = D + 4;  // of a row (banks)
@@ -90,13 +90,13 @@ struct Four {
         const float own_sum = rows.sum();
         if (rows.r == 0) sums_of(wave, rows.m)[0] = rows.run_max, sums_of(wave, rows.m)[1] = own_sum;
         __syncthreads();
-        if (wanted) {
+        if (wanted && threadIdx.x < 256) {
             const int row = threadIdx.x >> 4;
-            float f[4], top = sums_of(0, row)[0], l = 0.0f;
+            float f[WAVES], top = sums_of(0, row)[0], l = 0.0f;
 #pragma unroll
-            for (int w = 1; w < 4; ++w) top = fmaxf(top, sums_of(w, row)[0]);
+            for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sums_of(w, row)[0]);
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 f[w] = __builtin_amdgcn_exp2f(sums_of(w, row)[0] - top);
                 l = fmaf(f[w], sums_of(w, row)[1], l);
             }
@@ -106,7 +106,7 @@ struct Four {
                 const int d = SPREAD ? row / Rows<D, SPREAD>::ROWS * 32 + 2 * (threadIdx.x & 15) : 64 * c + 4 * (threadIdx.x & 15);
                 cols o = {};
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
+                for (int w = 0; w < WAVES; ++w) {
                     const cols x = *reinterpret_cast<const cols *>(lds + w * WAVE + row * STRIDE + d);
 #pragma unroll
                     for (int i = 0; i < PER; ++i) o[i] = fmaf(f[w], x[i], o[i]);
@@ -170,7 +170,7 @@ struct SelectedArgs {
     Requests req;
     const int *selected;  // [tokens, h_kv, count]
     float *ws_o, *ws_ml;  // [workgroups][2][16][D], [..][2]
-    int h_q, h_kv, g, head_blocks, count;
+    int h_q, h_kv, g, head_blocks, count, waves;
     long share, places;
     float scale;
 };
@@ -186,11 +186,11 @@ __device__ __forceinline__ Unit unit_of(const SelectedArgs &a, long place) {
     return u;
 }
 
-template <int D, bool SPREAD>
-__global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArgs a) {
+template <int D, bool SPREAD, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, kWgs) void attn_q4_selected_kernel(SelectedArgs a) {
     extern __shared__ float lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    typedef Four<D, SPREAD> F;
+    typedef Meeting<D, SPREAD, WAVES> F;
     Rows<D, SPREAD> rows(lds, wave, lane);
     const F four = {lds};
     const long from = blockIdx.x * a.share, stop = min(from + a.share, a.places);
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256, kWgs) void attn_q4_selected_kernel(SelectedArg
         const bool whole = p0 == 0 && last == u.end;
         x = last;
         const int *const list = a.selected + ((size_t)u.token * a.h_kv + u.kv) * a.count;
-        const int begin = p0 + (int)((long)(p1 - p0) * wave / 4), count = __builtin_amdgcn_readfirstlane(p0 + (int)((long)(p1 - p0) * (wave + 1) / 4) - begin);
+        const int begin = p0 + (int)((long)(p1 - p0) * wave / WAVES), count = __builtin_amdgcn_readfirstlane(p0 + (int)((long)(p1 - p0) * (wave + 1) / WAVES) - begin);
         int place = lane < count ? list[begin + lane] : -1;  // of the page in its request, a page per lane; on its way before anything is known of the request
         Span span;
         const int b = __builtin_amdgcn_readfirstlane(request_of_token(a.req, u.token, lane, span));
@@ -601,7 +601,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : kWgs) void attn_q4_parts_kernel
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long all_rows = (long)a.req.tokens * a.h_q;
     Rows<D> rows(lds, wave, lane);
-    const Four<D> four = {lds};
+    const Meeting<D> four = {lds};
     const int m = rows.m;
     for (long item = blockIdx.x; item < a.items; item += gridDim.x) {
         // ---- which rows, which pages: from .. to - 1 of request b
@@ -654,9 +654,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 3 : kWgs) void attn_q4_parts_kernel
         const int ahead = numbers(0);
         rows.load(a.q + at * D, real, a.scale);
         rows.walk(count, real ? lim : 0, n, a.pages, a.h_kv, kv, ahead, numbers, [&](int i) __attribute__((always_inline)) { return (begin + i) * kPage; });
-        const size_t to_row = Four<D>::theirs((unsigned long long)out_row);
+        const size_t to_row = Meeting<D>::theirs((unsigned long long)out_row);
         four.meet(
-            rows, wave, Four<D>::theirs((int)real) != 0,
+            rows, wave, Meeting<D>::theirs((int)real) != 0,
             [&](int d, const v4f &o, float) __attribute__((always_inline)) { *reinterpret_cast<v4f *>(a.ws_o + to_row * D + d) = o; },
             [&](float top, float l) __attribute__((always_inline)) { a.ws_ml[to_row * 2] = top, a.ws_ml[to_row * 2 + 1] = l; });
     }
@@ -700,19 +700,20 @@ hipError_t launch(const PartsArgs &a, hipStream_t st) {
     attn_q4_join_kernel<D><<<(unsigned)(joins < kMostWgs ? joins : kMostWgs), 256, 0, st>>>(a);
     return hipGetLastError();
 }
-template <int D, bool SPREAD>
+template <int D, bool SPREAD, int WAVES>
 hipError_t launch_selected(const SelectedArgs &a, hipStream_t st) {
-    constexpr size_t lds = Place<D>::LDS;
-    if (const hipError_t e = allow_dynamic_lds<attn_q4_selected_kernel<D, SPREAD>>(lds); e != hipSuccess) return e;
+    constexpr size_t lds = Place<D>::LDS * WAVES / 4;
+    if (const hipError_t e = allow_dynamic_lds<attn_q4_selected_kernel<D, SPREAD, WAVES>>(lds); e != hipSuccess) return e;
     const unsigned wgs = (unsigned)((a.places + a.share - 1) / a.share);
-    attn_q4_selected_kernel<D, SPREAD><<<wgs, 256, lds, st>>>(a);
+    attn_q4_selected_kernel<D, SPREAD, WAVES><<<wgs, 64 * WAVES, lds, st>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || wgs == 1 || a.share % a.count == 0) return e;  // (no unit is cut)
     attn_q4_join_selected_kernel<D, SPREAD><<<wgs - 1, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 template <int D>
 hipError_t launch(const SelectedArgs &a, hipStream_t st) {
-    return a.g <= Rows<D, true>::ROWS ? launch_selected<D, true>(a, st) : launch_selected<D, false>(a, st);
+    if (a.waves == 8) return a.g <= Rows<D, true>::ROWS ? launch_selected<D, true, 8>(a, st) : launch_selected<D, false, 8>(a, st);
+    return a.g <= Rows<D, true>::ROWS ? launch_selected<D, true, 4>(a, st) : launch_selected<D, false, 4>(a, st);
 }
 template <class Args>
 hipError_t launch(const Args &a, int d, hipStream_t st) {
@@ -737,15 +738,25 @@ int parts_of(long blocks, int pages, int num_cus) {
 
 }  // namespace
 
+// Equal shares of all places for as many workgroups as the card has at once, a page per wavefront at least.  Whole units where that makes the largest share an eighth larger at most: nothing to
+// join.  Half as many workgroups of 8 wavefronts have whole units where 4 do not, or have a list of up to 8 pages at once.  (Heads of 128 values, 8 KV heads, us with and without workgroups of 8:
+// 30 requests of 32 pages 18.4 and 24.8, 32 of 32 19.4 and 22.6, 32 of 100 46.0 and 50.3; 1 of 8 7.7 and 9.0, but of 16 9.6 and 9.2 and of 32 13.9 and 9.4, if it were not cut.)
 SelectedPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, int count, int num_cus) {
     SelectedPlan p = {};
-    const long units = (long)tokens * h_kv * ((h_q / h_kv + 15) / 16), wgs = (long)kWgs * (num_cus > 0 ? num_cus : 1);
+    const long units = (long)tokens * h_kv * ((h_q / h_kv + 15) / 16), cus = num_cus > 0 ? num_cus : 1;
     p.places = units * count;
-    p.share = (p.places + wgs - 1) / wgs;
-    if (p.share < 4) p.share = 4;  // (a page per wavefront)
-    // whole units, where that makes the largest share an eighth larger at most: nothing to join
-    const long whole = (p.share + count - 1) / count * count;
-    if (whole <= p.share + p.share / 8) p.share = whole;
+    auto shares = [&](int waves, int least) {
+        const long wgs = kWgs * cus * 4 / waves, equal = (p.places + wgs - 1) / wgs;
+        p.waves = waves, p.share = equal < least ? least : equal;
+    };
+    auto whole = [&](int waves) {
+        shares(waves, count < waves ? count : waves);
+        const long units_only = (p.share + count - 1) / count * count;
+        const bool fits = units_only <= p.share + p.share / 8;
+        p.share = units_only;
+        return fits;
+    };
+    if (!whole(4) && !whole(8)) shares(4, 4);
     p.wgs = (p.places + p.share - 1) / p.share;
     p.bytes = 256 + (p.wgs > 1 && p.share % count != 0 ? (size_t)p.wgs * 2 * 16 * (d + 2) * sizeof(float) : 0);
     return p;
@@ -776,7 +787,7 @@ hipError_t launch_attention_selected_q4(const void *q, const Requests &req, int 
     a.req = req;
     a.selected = selected, a.count = count;
     a.h_q = h_q, a.h_kv = h_kv, a.g = h_q / h_kv, a.head_blocks = (a.g + 15) / 16;
-    a.share = p.share, a.places = p.places;
+    a.share = p.share, a.places = p.places, a.waves = p.waves;
     a.ws_o = static_cast<float *>(workspace);
     a.ws_ml = a.ws_o + (size_t)p.wgs * 2 * 16 * d;
     a.scale = 1.4426950408889634f / sqrtf((float)d);

@@ -431,6 +431,7 @@ struct AttnPartsPlan {
 };
 struct SelectedPlan {
     long places, share, wgs;  // pages of all lists, of a workgroup
+    int waves;                // of a workgroup
     size_t bytes;
 };
 SelectedPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, int count, int num_cus);

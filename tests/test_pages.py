@@ -736,6 +736,12 @@ SOME = [  # S, n, h_q, h_kv, d, count
     ([1], [9000], 32, 8, 128, 70),
     ([1] * 40, [300 + 10 * i for i in range(40)], 8, 4, 256, 4),
     ([130], [600], 4, 2, 64, 8),
+    ([1], [900], 32, 8, 128, 8),             # eight wavefronts, a page each
+    ([2], [700], 6, 2, 256, 5),
+    ([1] * 30, [1300 + i for i in range(30)], 32, 8, 64, 20),  # eight wavefronts, some pages each
+    ([1] * 62, [590 + i for i in range(62)], 32, 4, 128, 9),
+    ([1] * 62, [590 + i for i in range(62)], 8, 4, 256, 9),
+    ([100], [200], 7, 7, 64, 3),             # and three lists one after the other
 ]
 
 
