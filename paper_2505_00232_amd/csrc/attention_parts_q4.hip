@@ -254,7 +254,8 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
 
 // ---- common pages of many rows.  What attention_q4_rows.h does to a page for 16 query rows, most of its instructions, is to take its codes apart: 551 vector instructions of a page and 16 rows,
 // of which 192 for that.  Here the four wavefronts of a workgroup take a page's codes apart once, into LDS as binary16 whole numbers code - 8 (exact, as are the products with the queries), and
-// multiply them with 32 rows each (310 instructions of a page and 16 rows); steps, offsets and P are taken into the sums in the same way and the same precision as there:
+// multiply them with 32 rows each (310 instructions of a page and 16 rows); steps, offsets and P are taken into the sums in the same way and with the same precision as there, steps of 1 and
+// more (there: 2) in a turn of their own:
 //   q . k = sum_j step_j (q_j . (code_j - 8)) + sum_j offset_j sum q_j,   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
 // The common pages are in front of all rows' positions: nothing is masked.  Bound: the LDS, 63 reads of a KiB of a page and wavefront at 64 bytes a cycle, beside vector instructions in 64 % of the
 // cycles (1024 rows of 8 heads of 128 values behind 20000 positions 167 us: 500 TFLOP/s).
@@ -262,9 +263,10 @@ template <int D>
 struct Wide {
     typedef PageLayout<D> L;
     static constexpr int G = L::G, W = L::W, DT = D / 16, NB = 2, ROWS = 64 * NB;
-    // LDS: K operands [4 tiles][G][64 lanes], V operands [G][low, high][2 halves of 16 positions][64 lanes], 16 bytes each; then the page's steps and offsets of keys, and of values
-    static constexpr int kV = 128 * D, kHeadK = 256 * D, kHeadV = 264 * D, kBytes = 272 * D;
-    static constexpr int kStepK = kHeadK, kOffsetK = kHeadK + 4 * D, kStepV = kHeadV, kOffsetV = kHeadV + 4 * D;
+    // LDS: K operands [4 tiles][G][64 lanes], V operands [G][low, high][2 halves of 16 positions][64 lanes], 16 bytes each; then the page's steps and offsets of keys, and of values: steps below 1
+    // (zeros for the others), offsets, steps of 1 and more (zeros for the others)
+    static constexpr int kV = 128 * D, kHeadK = 256 * D, kHeadV = 264 * D, kBytes = 276 * D;
+    static constexpr int kStepK = kHeadK, kOffsetK = kHeadK + 4 * D, kStepV = kHeadV, kOffsetV = kHeadV + 4 * D, kLargeV = kHeadV + 8 * D;
     // A page on its way: what a thread has of it
     static constexpr int kPiecesK = 4 * (G / W) * 64, kPiecesV = G * 64, PK = (kPiecesK + 255) / 256, PV = (kPiecesV + 255) / 256;
     typedef uint32_t words __attribute__((ext_vector_type(W)));
@@ -303,7 +305,15 @@ struct Wide {
                     *reinterpret_cast<u32x4 *>(lds + kV + (((j * 2 + high) * 2 + u) * 64 + lane) * 16) = u32x4{two(a), two(a >> 8), two(b), two(b >> 8)};
                 }
         }
-        if ((int)threadIdx.x < D) *reinterpret_cast<u32x4 *>(lds + kHeadK + threadIdx.x * 16) = head;
+        const int piece = (int)threadIdx.x;
+        if (piece >= D) return;
+        u32x4 large = {};
+        if (piece >= D / 2 && piece < D / 2 + D / 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) large[i] = head[i] & (head[i] + 0x04000400u >> 14 & 0x00010001u) * 0xFFFFu;  // (exponents from 1.0's on)
+            *reinterpret_cast<u32x4 *>(lds + kLargeV + (piece - D / 2) * 16) = large;
+        }
+        *reinterpret_cast<u32x4 *>(lds + kHeadK + piece * 16) = head & ~large;
     }
 };
 
@@ -316,10 +326,11 @@ struct WideRows {
     h8 qf[NB][G], sums[NB];
     float to_score[NB], run_max[NB];
     v4f acc[NB][DT], rest[NB];
-    int factor;  // log 2 of what P is multiplied with in acc (in rest: kAt)
-    // The maximum may be kLag below a score (in units of log 2): what hardly moves it costs no pass over the sums.  P is then at most 2^(kAt + kLag) = 2^14.
-    static constexpr int kLag = 3, kAt = (int)kFactor - kLag;
-    __device__ __forceinline__ WideRows(int l) : lane(l), m(l & 15), r(l >> 4), factor(kAt) {}
+    // The maximum may be kLag below a score (in units of log 2): what hardly moves it costs no pass over the sums.  P is taken 2^kAt times as large, at most 2^15 then, and its products with
+    // steps below 1 are smaller: binary16 keeps as many bits of small ones as in attention_q4_rows.h.  (256 requests behind 20011 positions: a lag of 1 211 us; of 2, with P half as large, 209.)
+    static constexpr int kLag = 1, kAt = (int)kFactor;
+    static_assert(kAt + kLag <= 15, "P is rounded to binary16, which holds twice as much");
+    __device__ __forceinline__ WideRows(int l) : lane(l), m(l & 15), r(l >> 4) {}
 
     __device__ __forceinline__ void load(int nb, const _Float16 *q, bool real, float scale) {
         float top = 0.0f;
@@ -455,58 +466,71 @@ struct WideRows {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) rest[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, rows), pv[nb][u], rest[nb], 0, 0, 0);
         }
-        // Products of P and a step stay below 2^15: with steps of 2 and more the sums are of P 2^factor, from there on
+        // Steps below 1; those of 1 and more in a turn of their own behind it, with each row's P lowered until its largest product with one of them is below 2^15 (by powers of two: exact in P and in
+        // sums of 32 bits): what binary16 then loses is little against a product that is in the row's sums, and the small steps, in this page and the others, keep their bits.
+        auto product = [&](Lds steps) __attribute__((always_inline)) {
+            h8 step[2], lo[2], hi[2];
+            auto ask = [&](int k) __attribute__((always_inline)) {
+                const int j = k / 2, u = k % 2;
+                step[u] = read<h8>(steps + j * kPage * 2 + 16 * u), lo[u] = read<h8>(at16 + S::kV + (4 * j + u) * 1024), hi[u] = read<h8>(at16 + S::kV + (4 * j + 2 + u) * 1024);
+            };
+            ask(0);
+#pragma unroll
+            for (int k = 0; k < 2 * G; ++k) {
+                const int j = k / 2, u = k % 2;
+                __builtin_amdgcn_sched_barrier(0);  // (one after the other: registers)
+                if (k + 1 < 2 * G) ask(k + 1);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    h8 p;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[nb][8 * u + e], (float)step[u][e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
+                    acc[nb][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[u], p, acc[nb][2 * j], 0, 0, 0);
+                    acc[nb][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[u], p, acc[nb][2 * j + 1], 0, 0, 0);
+                }
+            }
+        };
+        product(at_r + S::kStepV);
         uint32_t bits = 0;
 #pragma unroll
-        for (int j = 0; j < G; j += 2) bits |= read<uint32_t>(at_lane + S::kStepV + j * kPage * 2);  // (two groups' steps are 64 dwords)
-        if (__any((bits & 0x40004000u) != 0)) {
-            float most = 0.0f;
+        for (int j = 0; j < G; j += 2) bits |= read<uint32_t>(at_lane + S::kLargeV + j * kPage * 2);  // (two groups' steps are 64 dwords)
+        if (__any(bits != 0)) {
+            float back[NB];
 #pragma unroll
-            for (int j = 0; j < G; ++j) most = fmaxf(most, (float)read<_Float16>(at_lane - 2 * lane + S::kStepV + j * kPage * 2));
+            for (int nb = 0; nb < NB; ++nb) {
+                float most = 0.0f;
 #pragma unroll
-            for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
-            const int to = min(factor, 15 - kLag - __builtin_amdgcn_frexp_expf(most));
-            const float by = __builtin_amdgcn_ldexpf(1.0f, to - factor);
-            factor = __builtin_amdgcn_readfirstlane(to);
+                for (int k = 0; k < 2 * G; ++k) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    const h8 step = read<h8>(at_r + S::kLargeV + k / 2 * kPage * 2 + 16 * (k % 2));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) most = fmaxf(most, sc[nb][8 * (k % 2) + e] * (float)step[e]);
+                }
+                most = over_rows(most);
+                const int down = most >= 32768.0f ? __builtin_amdgcn_frexp_expf(most) - 15 : 0;
+                const float by = __builtin_amdgcn_ldexpf(1.0f, -down);
+                back[nb] = __builtin_amdgcn_ldexpf(1.0f, down);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[nb][e] *= by;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[nb][t][i] *= by;
+            }
+            Lds again = at_r + S::kLargeV;
+            asm volatile("" : "+v"(again));  // (steps are read twice rather than kept)
+            product(again);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int t = 0; t < DT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[nb][t][i] *= by;
-        }
-        if (factor != kAt) {
-            const float by = __builtin_amdgcn_ldexpf(1.0f, factor - kAt);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sc[nb][e] *= by;
-        }
-        h8 step[2], lo[2], hi[2];
-        auto ask = [&](int k) __attribute__((always_inline)) {
-            const int j = k / 2, u = k % 2;
-            step[u] = read<h8>(at_r + S::kStepV + j * kPage * 2 + 16 * u), lo[u] = read<h8>(at16 + S::kV + (4 * j + u) * 1024), hi[u] = read<h8>(at16 + S::kV + (4 * j + 2 + u) * 1024);
-        };
-        ask(0);
-#pragma unroll
-        for (int k = 0; k < 2 * G; ++k) {
-            const int j = k / 2, u = k % 2;
-            __builtin_amdgcn_sched_barrier(0);  // (one after the other: registers)
-            if (k + 1 < 2 * G) ask(k + 1);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                h8 p;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = (_Float16)fmaf(sc[nb][8 * u + e], (float)step[u][e], 0.0f);  // (with the sum one instruction takes 32 and 16 bits)
-                acc[nb][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[u], p, acc[nb][2 * j], 0, 0, 0);
-                acc[nb][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[u], p, acc[nb][2 * j + 1], 0, 0, 0);
-            }
+                    for (int i = 0; i < 4; ++i) acc[nb][t][i] *= back[nb];
         }
     }
     __device__ __forceinline__ float sum(int nb) const { return __shfl(rest[nb][3], 48 + m, 64); }
     template <class Put>
     __device__ __forceinline__ void columns(int nb, const Put &put) const {
-        const float back = __builtin_amdgcn_ldexpf(1.0f, kAt - factor);
 #pragma unroll
         for (int j = 0; j < G; ++j) {
             const float off = __shfl(rest[nb][j & 3], (j >> 2) * 16 + m, 64);
@@ -514,7 +538,7 @@ struct WideRows {
             for (int k = 0; k < 2; ++k) {
                 v4f o;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = fmaf(acc[nb][2 * j + k][i], back, off);
+                for (int i = 0; i < 4; ++i) o[i] = acc[nb][2 * j + k][i] + off;
                 put(32 * j + 16 * k + 4 * r, o);
             }
         }
@@ -590,7 +614,7 @@ __global__ __launch_bounds__(256, 2) void attn_q4_wide_kernel(PartsArgs a) {
         const float l = rows.sum(nb);
         if (!real[nb]) continue;
         rows.columns(nb, [&](int d, const v4f &o) __attribute__((always_inline)) { *reinterpret_cast<v4f *>(a.ws_o + out_row[nb] * D + d) = o; });
-        if (rows.r == 0) a.ws_ml[out_row[nb] * 2] = rows.run_max[nb] + (float)WideRows<D>::kLag, a.ws_ml[out_row[nb] * 2 + 1] = l;  // (as of sums 2^kFactor times as large)
+        if (rows.r == 0) a.ws_ml[out_row[nb] * 2] = rows.run_max[nb], a.ws_ml[out_row[nb] * 2 + 1] = l;
     }
 }
 

@@ -553,6 +553,86 @@ def test_attention_shared_maxima_that_move(d, rise, rows_rule):
         _close(got[b:b + 1], *q4.attention(q.reshape(-1, h_q, d)[b:b + 1], K[b], V[b], P[b]))
 
 
+def _check_shared_alike(rng, S, n, d, k, v, q):
+    """Requests of n[b] positions, all but the last few of each in common pages that hold k, v (one KV head); q [tokens, heads, d]."""
+    whole = len(k) // 64
+    table, num = _pages(rng, n)
+    table[1:, :whole] = table[0, :whole]
+    own = lambda x, b: np.concatenate([x[:64 * whole], _normal(rng, n[b] - 64 * whole, 1, d) * np.float16(2.0 ** -10)])
+    cache, K, V, P = _filled(rng, n, 1, d, table, num, np.concatenate([own(k, b) for b in range(len(n))]), np.concatenate([own(v, b) for b in range(len(n))]))
+    got = _attend_shared(_requests(S, n, table), B.SharedPrefixes(_i([0, len(S)]), _i([len(k)]), sum(S), len(k)), q.reshape(sum(S), -1), q.shape[1], cache).reshape(q.shape)
+    at = 0
+    for b, s in enumerate(S):
+        _close(got[at:at + s], *q4.attention(q[at:at + s], K[b], V[b], P[b]))
+        at += s
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n,where,value,small,gap", [(1000, 100, 40, 0.05, 12), (1000, 100, 40, 0.005, 12), (8000, 100, 30.5, 0.01, 16), (8000, 70, 4000, 0.005, 12), (1000, 64, 60000, 0.01, 14),
+                                                     (1000, 950, 60000, 0.01, 14), (448, 0, 300, 0.02, 12), (1000, 100, 20, 0.005, 12)])
+def test_attention_shared_large_value_beside_small_ones(n, where, value, small, gap, d, rows_rule):
+    """One large value in one group of 32, groups of small ones beside it, and a position with nearly all of P whose values are next to nothing: the others make up the result.  (Products of P and
+    a step that are denormals of binary16 are off by 2^-25 of 2^14, times a code of 8: 2^-36 a position, either way, nothing against the bound's 2^-24.)"""
+    rng = np.random.default_rng(59)
+    base, k, v = _normal(rng, d), _normal(rng, n, 1, d), _normal(rng, n, 1, d)
+    k[5, 0] = base * np.float16(gap * np.sqrt(d) / np.sum(base.astype(np.float64) ** 2))
+    v[:, :, 32:] *= np.float16(small)
+    v[5] *= np.float16(1e-3)
+    v[where, 0, 3] = value
+    q = np.stack([base * np.float16(x) for x in (1.0, 0.9, 1.1, 1.0, 0.95, 1.05, 0.97, 1.02)]).reshape(4, 2, d)
+    _check_shared_alike(rng, [1, 2, 1], [n + 3, n + 70, n + 5], d, k, v, q)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("page", [0, 3, 8])
+@pytest.mark.parametrize("value,far", [(30000, 30), (60000, 24), (60000, 11), (35, 30)])
+def test_attention_shared_page_of_large_steps_that_hardly_counts(value, far, page, d, rows_rule):
+    """A page with steps of 2 and more and 2^-far of the largest P, and pages of small steps whose positions, all alike, have 2^-10 of it: their products with P round all the same way, once."""
+    rng = np.random.default_rng(60)
+    n = 640
+    unit = np.log(2.0) * np.sqrt(d) / 8.0  # of q . k, with 8 in the query
+    k, v = np.zeros((n, 1, d), np.float16), np.zeros((n, 1, d), np.float16)
+    k[64 * page:64 * page + 64, 0, 0] = -(far - 10) * unit
+    k[5 if page else 300, 0, 0] = 10 * unit
+    v[:, 0, :] = np.tile(np.linspace(-2.0 ** -5, 2.0 ** -5, 32).astype(np.float16), d // 32)
+    v[5 if page else 300] *= np.float16(2.0 ** -6)
+    v[64 * page:64 * page + 64, 0, 1::2] = value
+    q = np.zeros((3, 2, d), np.float16)
+    q[:, :, 0] = 8
+    _check_shared_alike(rng, [1, 1, 1], [n + 1, n + 2, n + 100], d, k, v, q)
+
+
+@gpu
+def test_attention_shared_by_its_own_rule():
+    """Sizes at which the rule, and not the tunable, takes the way of many rows: the same result, and large values beside small ones."""
+    rng = np.random.default_rng(61)
+    requests, h_q, h_kv, d, whole = 64, 32, 8, 128, 620
+    n = [64 * whole + 1 + 5 * b for b in range(requests)]
+    table = np.full((requests, whole + 6), -1, np.int32)
+    table[:, :whole] = rng.permutation(whole)
+    at = whole
+    for b, x in enumerate(n):
+        own = (x + 63) // 64 - whole
+        table[b, whole:whole + own] = np.arange(at, at + own)
+        at += own
+    cache = B.PagedCache(at, h_kv, d)
+    k, v = _normal(rng, at * 64, h_kv, d), _normal(rng, at * 64, h_kv, d)
+    v[:, :, 32:64] *= np.float16(0.005)
+    v[4000, :, 40] = 40
+    K, _ = q4.q4_values(*q4.q4(k))
+    V, P = q4.q4_values(*q4.q4(v))
+    every = _requests([at * 64], [at * 64], np.arange(at, dtype=np.int32)[None])
+    B.qfc_append_q4(_t(np.concatenate([k, k, v], 1).reshape(at * 64, -1)), every, h_kv, None, None, cache, torch.empty((at * 64, h_kv * d), dtype=torch.float16, device=DEV))
+    q = _normal(rng, requests, h_q * d)
+    req = _requests([1] * requests, n, table)
+    out = _attend_shared(req, B.SharedPrefixes(_i([0, requests]), _i([64 * whole]), requests, 64 * whole), q, h_q, cache).reshape(requests, h_q, d)
+    paged = lambda x, b: x.reshape(at, 64, h_kv, d)[table[b, :(n[b] + 63) // 64]].reshape(-1, h_kv, d)[:n[b]]
+    for b in (0, 31, 63):
+        _close(out[b:b + 1], *q4.attention(q.reshape(requests, h_q, d)[b:b + 1], paged(K, b), paged(V, b), paged(P, b)))
+
+
 @gpu
 def test_attention_shared_arrays_that_break_the_rules_stay_inside(rows_rule):
     rng = np.random.default_rng(23)
