@@ -209,15 +209,16 @@ __global__ __launch_bounds__(1024) void take_few_pages_kernel(PagesArgs a) {
     for (int b = wave; b < a.batch; b += 16) take_row(a, b, lane, buffers[wave]);
 }
 
-// Copies bytes [from, to) of a page, by the threads of a workgroup; both multiples of 16.  Four of a thread's loads on their way at once.
+// Copies bytes [from, to) of a page, by the threads of a workgroup; both multiples of 16.  Four of a thread's loads on their way at once.  (A page may end just below 2^31 bytes: what is added to places
+// in it passes 32 bits.)
 __device__ __forceinline__ void copy_bytes(char *dst, const char *src, int from, int to) {
-    for (int at = from + (int)threadIdx.x * 16; at < to; at += 4 * 4096) {
+    for (unsigned at = (unsigned)from + threadIdx.x * 16; at < (unsigned)to; at += 4 * 4096) {
         u32x4 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4 *>(src + min(at + 4096 * i, to - 16));
+        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4 *>(src + min(at + 4096 * i, (unsigned)to - 16));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (at + 4096 * i < to) *reinterpret_cast<u32x4 *>(dst + at + 4096 * i) = x[i];
+            if (at + 4096 * i < (unsigned)to) *reinterpret_cast<u32x4 *>(dst + at + 4096 * i) = x[i];
     }
 }
 // Bounds of a page's keys go where the page goes
@@ -377,7 +378,7 @@ PagesArgs args_of(const PagePool &pool, void *workspace, int batch) {
 unsigned fours(long x) { return (unsigned)((x + 3) / 4); }
 // Workgroups per page: 16 KiB each where pages are many, as many as fill the card where they are few
 int slices_of(int page_bytes, long pages, int num_cus) {
-    const long most = page_bytes / 4096 > 1 ? page_bytes / 4096 : 1, least = (page_bytes + 16383) / 16384, fill = (2L * num_cus + pages - 1) / (pages > 0 ? pages : 1);
+    const long most = page_bytes / 4096 > 1 ? page_bytes / 4096 : 1, least = (page_bytes + 16383L) / 16384, fill = (2L * num_cus + pages - 1) / (pages > 0 ? pages : 1);
     return (int)(fill < least ? least : fill > most ? most : fill);
 }
 

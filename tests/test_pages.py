@@ -402,6 +402,28 @@ def test_pages_captured_and_replayed():
         assert np.array_equal(kids.cpu().numpy(), table) and np.array_equal(r.cpu().numpy(), want) and np.array_equal(pool.now(), pages)
 
 
+@gpu
+def test_pages_of_almost_two_gibibytes():
+    """The largest page that is not refused: copied, forked and moved whole."""
+    h_kv, d = (2 ** 31 - 1) // (80 * 64), 64
+    cache = B.PagedCache(3, h_kv, d)
+    whole = cache.pages.view(3, -1)
+    assert whole.shape[1] > 2 ** 31 - 80 * 64
+    words = whole.view(torch.int32)
+    words[0] = torch.arange(words.shape[1], dtype=torch.int32, device=DEV) * 7 + 1
+    words[1:] = -1
+    B.qfc_copy_pages(cache, cache, _i([0]), _i([1]))
+    assert torch.equal(words[0], words[1]) and bool((words[2] == -1).all())
+    words[0] = -1
+    space = _space(B.qfc_pages_workspace_size(cache, 1))
+    r, table, child = _i([0, 1, 0]), _i([[1]]), _i([[7]])
+    B.qfc_compact_pages(cache, r, table, space)
+    assert torch.equal(words[0], words[1]) and bool((words[2] == -1).all()) and r.tolist() == [1, 0, 0] and table.tolist() == [[0]]
+    words[1] = -1
+    B.qfc_fork_pages(cache, r, table, _i([0]), _i([5]), child, space)
+    assert torch.equal(words[0], words[1]) and bool((words[2] == -1).all()) and r.tolist() == [1, 1, 0] and child.tolist() == [[1]]
+
+
 # ---------------------------------------------------------------- attention behind common pages
 def _attend_shared(req, shared, q, h_q, cache, fill=0.0):
     out = torch.full((q.shape[0], h_q * cache.d_head), fill, dtype=torch.float16, device=DEV)
