@@ -790,6 +790,7 @@ AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv,
     AttnPartsPlan p = {};
     const int g = h_q / h_kv;
     const int forced = tuning().attn_wide_rows;
+    group_tokens = group_tokens < tokens ? group_tokens : tokens;  // (a limit may be far above what the call holds)
     const long group_rows = (long)group_tokens * g, common = (longest < max_context ? longest : max_context) / kPage;
     p.wide = d <= 128 && (forced > 0 ? group_rows >= forced : group_rows >= 2 * Wide<128>::ROWS && group_rows * common * h_kv * d >= kWideFrom * num_cus);
     const int rows = p.wide ? Wide<128>::ROWS : 16;

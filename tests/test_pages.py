@@ -656,6 +656,20 @@ def test_attention_shared_by_its_own_rule():
 
 
 @gpu
+@pytest.mark.parametrize("most", [9, 300, 1 << 20, 2 ** 31 - 1])
+def test_attention_shared_limits_far_above_the_call_change_nothing(most):
+    """What a group may have is not what the call has: the same way is taken, and the same bits come out."""
+    rng = np.random.default_rng(62)
+    group, prefix, S, n, h_q, h_kv, d = [0, 8], [1300], [1] * 8, [1301 + 9 * i for i in range(8)], 8, 2, 128
+    cache, table, K, V, P = _shared_batch(rng, group, prefix, S, n, h_kv, d)
+    q, req = _normal(rng, 8, h_q * d), _requests(S, n, table)
+    want = _attend_shared(req, B.SharedPrefixes(_i(group), _i(prefix), 8, 1300), q, h_q, cache)
+    assert np.array_equal(_attend_shared(req, B.SharedPrefixes(_i(group), _i(prefix), most, 2 ** 31 - 1), q, h_q, cache), want)
+    for b in range(8):
+        _close(want.reshape(8, h_q, d)[b:b + 1], *q4.attention(q.reshape(8, h_q, d)[b:b + 1], K[b], V[b], P[b]))
+
+
+@gpu
 def test_attention_shared_arrays_that_break_the_rules_stay_inside(rows_rule):
     rng = np.random.default_rng(23)
     group, prefix, S, n, h_q, h_kv, d = [0, 3], [320], [1, 1, 1], [400, 500, 330], 4, 2, 64
