@@ -457,7 +457,8 @@ typedef struct qfc_shared {
 } qfc_shared_t;
 
 /* qfc_attention_q4 for requests of which groups have common pages: the same result up to roundings, with what is common read and multiplied once for all rows of a group (from the table
- * row of its first request with tokens).  Errors as qfc_attention_q4; QFC_ERR_INVALID_ARG for null pointers and sizes below 1 in `shared`, QFC_ERR_UNSUPPORTED for groups * h_kv above 65535. */
+ * row of its first request with tokens).  workspace: device scratch of at least the size's bytes, one call's at a time; a size is enough for every smaller call too (fewer tokens, limits no
+ * larger, fewer groups), so that a server needs that of its largest one.  Errors as qfc_attention_q4; QFC_ERR_INVALID_ARG for null pointers and sizes below 1 in `shared`, QFC_ERR_UNSUPPORTED for groups * h_kv above 65535. */
 qfc_status_t qfc_attention_shared_q4_workspace_size(const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
 qfc_status_t qfc_attention_shared_q4(const void *q_f16, const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, void *workspace,
                                      size_t workspace_bytes, void *out_f16, void *stream);
@@ -470,13 +471,14 @@ qfc_status_t qfc_bound_pages_q4(const qfc_requests_t *requests, const qfc_q4_cac
  *   per query head h: s_h = a / 127 with a = max |q|, codes c_d = clamp(rne(q_d (127 / a)), +-127) (a = 0: zeros), n_h = sum_d max(c_d, 0) upper_d + min(c_d, 0) lower_d;
  *   score = step max_h (s_h n_h), operations rounded to 32 bits; an entry of the table without a page comes behind all others.
  * selected: device, int32 [tokens, h_kv, count]: numbers of pages in the request (entries of its table's row), ascending, -1 behind them where the token sees fewer.
- * first, last >= 0, first + last <= count <= 65536; q finite.  workspace: as for qfc_attention_q4 (256 bytes for requests of up to 2^21 positions).  Errors as qfc_attention_q4. */
+ * first, last >= 0, first + last <= count <= 65536; q finite.  workspace: as for qfc_attention_shared_q4 (256 bytes for requests of up to 32768 positions, else four for each of their pages, new
+ * token and KV head, 512 tokens and heads at most).  Errors as qfc_attention_q4. */
 qfc_status_t qfc_select_pages_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
 qfc_status_t qfc_select_pages_q4(const void *q_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, const qfc_page_bounds_t *bounds, int32_t first, int32_t last,
                                  int32_t count, void *workspace, size_t workspace_bytes, int32_t *selected, void *stream);
 
 /* Attention of each new token and KV head over the pages that `selected` [tokens, h_kv, count] lists (numbers of pages in the request, in any order; outside the request's: none; twice:
- * counted twice), up to the token's own position; else as qfc_attention_q4.  1 <= count <= 65536. */
+ * counted twice), up to the token's own position; else as qfc_attention_q4.  1 <= count <= 65536.  workspace: as for qfc_attention_shared_q4 (smaller calls: also those of shorter lists). */
 qfc_status_t qfc_attention_selected_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, int32_t count, size_t *bytes);
 qfc_status_t qfc_attention_selected_q4(const void *q_f16, const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, const int32_t *selected, int32_t count,
                                        void *workspace, size_t workspace_bytes, void *out_f16, void *stream);

@@ -674,7 +674,7 @@ constexpr int kMostSelected = 1 << 16;
 qfc_status_t qfc_select_pages_q4_workspace_size(const qfc_requests_t *requests, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes) {
     if (!bytes) return QFC_ERR_INVALID_ARG;
     if (const qfc_status_t s = check_batch(requests, h_q, cache); s != QFC_OK) return s;
-    *bytes = select_workspace(requests->tokens, cache->h_kv, requests->max_context, device_cus());
+    *bytes = select_workspace(requests->tokens, cache->h_kv, requests->max_context);
     return QFC_OK;
 }
 
@@ -688,7 +688,7 @@ qfc_status_t qfc_select_pages_q4(const void *q_f16, const qfc_requests_t *reques
     if (!q_f16 || !workspace || !selected) return QFC_ERR_INVALID_ARG;
     if (!aligned16(q_f16) || !aligned16(workspace) || !aligned(selected, 4)) return QFC_ERR_ALIGNMENT;
     const int cus = device_cus();
-    if (workspace_bytes < select_workspace(requests->tokens, cache->h_kv, requests->max_context, cus)) return QFC_ERR_BUFFER_TOO_SMALL;
+    if (workspace_bytes < select_workspace(requests->tokens, cache->h_kv, requests->max_context)) return QFC_ERR_BUFFER_TOO_SMALL;
     if (cus < 1) return QFC_ERR_HIP;
     return hip_status(launch_select_pages_q4(q_f16, on_device(requests, cache), h_q, cache->h_kv, cache->d_head, bounds->codes, bounds->steps, first, last, count, workspace, selected, cus,
                                              static_cast<hipStream_t>(stream)));

@@ -750,6 +750,9 @@ hipError_t launch(const Args &a, int d, hipStream_t st) {
 }
 
 constexpr int kMostParts = 16;
+// Rows of partial results per compute unit, beside one part of all rows: with 256 compute units 16 parts of 273 tokens of 32 heads.  (Blocks that fill the card with their rows need 16 kWgs of them, or 128
+// kWgs where they are of 128 rows: more only where most of a call's rows are nobody's or in no group.)
+constexpr long kKeptRows = 256 * kWgs;
 // Rows and common pages of a group times heads and their size per compute unit from which on pages are taken apart for a workgroup.  Both ways' times, us, with 8 KV heads of 128 values: 512 rows
 // behind 6000 positions 50 and 63, behind 20000 116 and 107; 1024 rows 85 and 94, 219 and 186; with 4 heads of 64: 1024 rows behind 20000 75 and 79.
 constexpr long kWideFrom = 600000;
@@ -758,6 +761,11 @@ int parts_of(long blocks, int pages, int num_cus) {
     const long fill = ((long)kWgs * num_cus + blocks - 1) / (blocks > 0 ? blocks : 1), most = (pages + 3) / 4;
     const long parts = fill < most ? fill : most;
     return (int)(parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts);
+}
+// Most parts of `rows` rows, whose partial results are kept for every part; rows times this grow with `rows` and `pages`: a workspace for the largest call serves every smaller one
+long most_rows(long rows, long pages, int num_cus) {
+    const long parts = pages <= 4 ? 1 : (pages + 3) / 4 < kMostParts ? (pages + 3) / 4 : kMostParts, kept = kKeptRows * num_cus + rows;
+    return rows * parts < kept ? rows * parts : kept;
 }
 
 }  // namespace
@@ -782,7 +790,9 @@ SelectedPlan plan_attention_selected_q4(int tokens, int h_q, int h_kv, int d, in
     };
     if (!whole(4) && !whole(8)) shares(4, 4);
     p.wgs = (p.places + p.share - 1) / p.share;
-    p.bytes = 256 + (p.wgs > 1 && p.share % count != 0 ? (size_t)p.wgs * 2 * 16 * (d + 2) * sizeof(float) : 0);
+    // (what any call of as many places or fewer needs, where its units are cut)
+    const long most = kWgs * cus < (p.places + 3) / 4 ? kWgs * cus : (p.places + 3) / 4;
+    p.bytes = 256 + (most > 1 ? (size_t)most * 2 * 16 * (d + 2) * sizeof(float) : 0);
     return p;
 }
 
@@ -797,9 +807,11 @@ AttnPartsPlan plan_attention_shared_q4(int batch, int tokens, int h_q, int h_kv,
     const long by_group = (long)groups * (((long)group_tokens * g + rows - 1) / rows), by_token = ((long)tokens * g + rows - 1) / rows + groups;
     p.prefix_blocks = by_group < by_token ? by_group : by_token;
     p.blocks = max_tokens * g <= 16 ? batch : ((long)tokens * g + 15) / 16 + batch;
-    p.prefix_parts = parts_of(p.prefix_blocks * h_kv, (int)common, num_cus);
-    p.parts = parts_of(p.blocks * h_kv, (max_context + kPage - 1) / kPage, num_cus);
-    p.bytes = 256 + (size_t)(p.prefix_parts + p.parts) * tokens * h_q * (d + 2) * sizeof(float);
+    const long all_rows = (long)tokens * h_q, pages = (max_context + kPage - 1) / kPage, most_common = most_rows(all_rows, common, num_cus), most_own = most_rows(all_rows, pages, num_cus);
+    auto within = [&](int parts, long most) { return all_rows * parts > most ? (int)(most / all_rows) : parts; };
+    p.prefix_parts = within(parts_of(p.prefix_blocks * h_kv, (int)common, num_cus), most_common);
+    p.parts = within(parts_of(p.blocks * h_kv, (int)pages, num_cus), most_own);
+    p.bytes = 256 + (size_t)(most_common + most_own) * (d + 2) * sizeof(float);
     return p;
 }
 

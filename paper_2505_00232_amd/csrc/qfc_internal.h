@@ -419,7 +419,7 @@ hipError_t launch_compact_pages(const PagePool &pool, int *table, int batch, int
 // Bounds of pages' keys, pages selected by them
 constexpr int kSelectInLds = 32768;  // pages of a request whose scores fit the LDS
 hipError_t launch_bound_pages_q4(const Requests &req, int h_kv, int d, const void *pages, int8_t *codes, float *steps, hipStream_t st);
-size_t select_workspace(int tokens, int h_kv, int max_context, int num_cus);
+size_t select_workspace(int tokens, int h_kv, int max_context);
 hipError_t launch_select_pages_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const int8_t *codes, const float *steps, int first, int last, int count, void *workspace,
                                   int *selected, int num_cus, hipStream_t st);
 // Attention in parts that are joined: of requests with common pages, and of selected pages

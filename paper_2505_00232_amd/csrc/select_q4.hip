@@ -397,7 +397,8 @@ constexpr int kSlice = 512;
 // One launch where scores fit the LDS and a workgroup has them at once, or workgroups are as many as half the compute units; else scores and lists are launches of their own.  One and two, us, heads
 // of 128 values: 8 lists of 500 pages 10.1 and 9.1, 32 of 500 10.2 and 9.5, 128 of 500 10.7 and 11.2; 8 of 1000 15.4 and 10.2, 64 of 2000 29.1 and 19.3, 128 of 2000 29.3 and 26.4, 248 of 2000 31.6
 // and 40.4.
-bool one_launch(long items, int pages, int num_cus) { return pages <= kSelectInLds && (pages <= 512 || 2 * items > num_cus); }
+constexpr int kOneLaunch = 512;  // pages
+bool one_launch(long items, int pages, int num_cus) { return pages <= kSelectInLds && (pages <= kOneLaunch || 2 * items > num_cus); }
 
 template <int D, int PHASE, bool IN_LDS>
 hipError_t launch_phase(const SelectArgs &a, int threads, long wgs, hipStream_t st) {
@@ -443,10 +444,10 @@ hipError_t launch_bound_pages_q4(const Requests &req, int h_kv, int d, const voi
     return hipGetLastError();
 }
 
-size_t select_workspace(int tokens, int h_kv, int max_context, int num_cus) {
+size_t select_workspace(int tokens, int h_kv, int max_context) {
     const int pages = pages_below(max_context);
     const long items = (long)tokens * h_kv, kept = items < kSlice ? items : kSlice;
-    return 256 + (one_launch(items, pages, num_cus) ? 0 : (size_t)kept * pages * sizeof(float));
+    return 256 + (pages <= kOneLaunch ? 0 : (size_t)kept * pages * sizeof(float));  // (what any call of as many tokens and pages or fewer needs)
 }
 
 hipError_t launch_select_pages_q4(const void *q, const Requests &req, int h_q, int h_kv, int d, const int8_t *codes, const float *steps, int first, int last, int count, void *workspace,

@@ -101,6 +101,74 @@ def test_binding_refuses_host_tensors_and_other_shapes():
         B._table(torch.zeros((3, 2), dtype=torch.int32), "page_table")
 
 
+def _sizes(tokens, batch, most, longest, groups, group_tokens, common, h_q, h_kv, d, count):
+    """Workspaces of attention behind common pages, of selection, of attention over selected pages."""
+    L, out = B.lib(), []
+    req = ctypes.byref(B.RequestsDesc(None, None, None, batch, tokens, most, longest, (longest + 63) // 64))
+    cache = ctypes.byref(B.CacheDesc(None, 4, h_kv, d))
+    for f in (lambda p: L.qfc_attention_shared_q4_workspace_size(req, ctypes.byref(B.SharedDesc(None, None, groups, group_tokens, common)), h_q, cache, p),
+              lambda p: L.qfc_select_pages_q4_workspace_size(req, h_q, cache, p), lambda p: L.qfc_attention_selected_q4_workspace_size(req, h_q, cache, count, p)):
+        size = ctypes.c_size_t(0)
+        assert f(ctypes.byref(size)) == 0
+        out.append(size.value)
+    return np.array(out)
+
+
+def _check_sizes():
+    rng = np.random.default_rng(63)
+    some = lambda most: int(np.exp(rng.uniform(0, np.log(most))))
+    for _ in range(3000):
+        d, h_kv, g = int(rng.choice([64, 128, 256])), int(rng.choice([1, 2, 4, 8])), int(rng.choice([1, 2, 4, 8, 20]))
+        large = [some(2000), some(300), some(200), some(1 << 22), some(50), some(2000), some(1 << 22)]
+        small = [max(1, int(x * rng.choice([1.0, 0.99, 0.5, rng.random()]))) for x in large]
+        count = some(300)
+        less = max(1, int(count * rng.random()))
+        assert np.all(_sizes(*small, h_kv * g, h_kv, d, less) <= _sizes(*large, h_kv * g, h_kv, d, count)), (small, large, h_kv, g, d, less, count)
+
+
+def test_workspaces_of_large_calls_serve_small_ones():
+    _check_sizes()
+    sizes = lambda tokens, longest: _sizes(tokens, tokens, 1, longest, 1, tokens, longest, 32, 8, 128, 32)[1]
+    assert sizes(1, 32768) == 256 and sizes(1, 32769) == 256 + 8 * 513 * 4 and sizes(500, 1 << 20) == 256 + 512 * 16384 * 4
+
+
+@gpu
+def test_workspaces_of_large_calls_serve_small_ones_on_the_device(rows_rule):
+    """One workspace each, of the largest batch's size, for all smaller ones: around the numbers of tokens and pages at which calls are made in another way."""
+    _check_sizes()
+    rng = np.random.default_rng(64)
+    h_q, h_kv, d, pages, T, count = 16, 8, 64, 700, 40, 32
+    cache = B.PagedCache(pages, h_kv, d)
+    n = pages * 64
+    k, v = _normal(rng, n, h_kv, d), _normal(rng, n, h_kv, d)
+    table = rng.permutation(pages).astype(np.int32)[None]
+    whole = _requests([n], [n], table)
+    B.qfc_append_q4(_t(np.concatenate([k, k, v], 1).reshape(n, -1)), whole, h_kv, None, None, cache, torch.empty((n, h_kv * d), dtype=torch.float16, device=DEV))
+    bounds = B.PageBounds(cache)
+    B.qfc_bound_pages_q4(whole, cache, bounds)
+    q = _t(_normal(rng, T, h_q * d))
+
+    def call(tokens, longest, less, spaces):
+        req = _requests([1] * tokens, [longest - i for i in range(tokens)], np.repeat(table[:, :(longest + 63) // 64], tokens, 0))
+        shared = B.SharedPrefixes(_i([0, tokens]), _i([longest - tokens - 70]), tokens, longest)
+        selected = torch.full((tokens, h_kv, less), -7, dtype=torch.int32, device=DEV)
+        one, two = (torch.full((tokens, h_q * d), 3.0, dtype=torch.float16, device=DEV) for _ in range(2))
+        a, b, c = spaces or [_space(x) for x in (B.qfc_attention_shared_q4_workspace_size(req, shared, h_q, cache), B.qfc_select_pages_q4_workspace_size(req, h_q, cache),
+                                                 B.qfc_attention_selected_q4_workspace_size(req, h_q, cache, less))]
+        B.qfc_attention_shared_q4(q[:tokens], req, shared, h_q, cache, a, one)
+        B.qfc_select_pages_q4(q[:tokens], req, h_q, cache, bounds, 1, 1, selected, b)
+        B.qfc_attention_selected_q4(q[:tokens], req, h_q, cache, selected, c, two)
+        assert bool((selected >= 0).all()) and not bool((one == 3.0).all()) and not bool((two == 3.0).all())
+        return [one, selected, two], [a, b, c]
+
+    spaces = call(T, n, count, None)[1]
+    for tokens in (40, 33, 32, 31, 20, 17, 16, 15, 5, 2, 1):
+        for longest in (n, 513 * 64, 512 * 64, 3000):
+            for less in (count, count - 1, 9, 4):
+                for got, want in zip(call(tokens, longest, less, spaces)[0], call(tokens, longest, less, None)[0]):
+                    assert torch.equal(got, want), (tokens, longest, less)
+
+
 # ---------------------------------------------------------------- the oracle by hand
 def test_oracle_pages_by_hand():
     table, refs, missing = ref.take(np.array([[3, -1, -1], [7, 9, -1]]), np.array([0, 1, 0, 1, 0]), [130, 64])
