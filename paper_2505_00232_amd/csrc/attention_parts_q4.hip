@@ -186,6 +186,8 @@ __device__ __forceinline__ Unit unit_of(const SelectedArgs &a, long place) {
     return u;
 }
 
+constexpr float kNobodys = -1.0f;  // sum of the parts of a row that is left as it was
+
 template <int D, bool SPREAD, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, kWgs) void attn_q4_selected_kernel(SelectedArgs a) {
     extern __shared__ float lds[];
@@ -199,13 +201,17 @@ __global__ __launch_bounds__(64 * WAVES, kWgs) void attn_q4_selected_kernel(Sele
         const long last = min(stop, u.end);
         const int p0 = (int)(x - u.begin), p1 = (int)(last - u.begin);
         const bool whole = p0 == 0 && last == u.end;
+        const size_t part0 = ((size_t)blockIdx.x * 2 + (u.begin > from ? 1 : 0)) * 16;
         x = last;
         const int *const list = a.selected + ((size_t)u.token * a.h_kv + u.kv) * a.count;
         const int begin = p0 + (int)((long)(p1 - p0) * wave / WAVES), count = __builtin_amdgcn_readfirstlane(p0 + (int)((long)(p1 - p0) * (wave + 1) / WAVES) - begin);
         int place = lane < count ? list[begin + lane] : -1;  // of the page in its request, a page per lane; on its way before anything is known of the request
         Span span;
         const int b = __builtin_amdgcn_readfirstlane(request_of_token(a.req, u.token, lane, span));
-        if (b >= a.req.batch || u.token < span.first || u.token - span.first >= span.count) continue;
+        if (b >= a.req.batch || u.token < span.first || u.token - span.first >= span.count) {  // nobody's
+            if (!whole && threadIdx.x < 16) a.ws_ml[(part0 + threadIdx.x) * 2 + 1] = kNobodys;
+            continue;
+        }
         const int n = span.positions, lim = n - span.count + u.token - span.first + 1;
         const bool real = u.head0 + rows.row() < a.g;
         const int head = u.kv * a.g + min(u.head0 + rows.row(), a.g - 1);
@@ -219,7 +225,7 @@ __global__ __launch_bounds__(64 * WAVES, kWgs) void attn_q4_selected_kernel(Sele
         rows.load(a.q + at * D, real, a.scale);
         rows.walk(count, real ? lim : 0, n, a.pages, a.h_kv, u.kv, ahead, numbers,
                   [&](int i) __attribute__((always_inline)) { return (int)((uint32_t)__builtin_amdgcn_readlane(place, i & 63) * kPage); });
-        const size_t their_at = F::theirs((unsigned long long)at), part = ((size_t)blockIdx.x * 2 + (u.begin > from ? 1 : 0)) * 16 + (threadIdx.x >> 4);
+        const size_t their_at = F::theirs((unsigned long long)at), part = part0 + (threadIdx.x >> 4);
         four.meet(
             rows, wave, F::theirs((int)real) != 0,
             [&](int d, const typename F::cols &o, float inv) __attribute__((always_inline)) {
@@ -237,7 +243,7 @@ __global__ __launch_bounds__(64 * WAVES, kWgs) void attn_q4_selected_kernel(Sele
 // A workgroup for the unit that the share of workgroup blockIdx.x + 1 begins inside of, if that is the first to do so; D / 4 threads per row
 template <int D, bool SPREAD>
 __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs a) {
-    const int d = 4 * (threadIdx.x % (D / 4)), from_token = token_at(a.req, 0), to_token = token_at(a.req, a.req.batch);
+    const int d = 4 * (threadIdx.x % (D / 4));
     const long x = ((long)blockIdx.x + 1) * a.share;
     const Unit u = unit_of(a, x);
     if (u.begin >= x || x - u.begin > a.share) return;
@@ -246,9 +252,10 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
     for (int row = threadIdx.x / (D / 4); row < min(16, a.g - u.head0); row += 1024 / D) {
         const int held = SPREAD ? d / 32 * Rows<D, SPREAD>::ROWS + row : row;  // (the row of the parts that has these columns)
         float inv;
-        const v4f o = joined(a.ws_ml, a.ws_o + d, D, parts,
-                             [&](int c) __attribute__((always_inline)) { return (size_t)((w0 + c) * 2 + (c == 0 && u.begin > w0 * a.share ? 1 : 0)) * 16 + held; }, inv);
-        if (u.token >= from_token && u.token < to_token) *reinterpret_cast<h4 *>(a.out + ((size_t)u.token * a.h_q + u.kv * a.g + u.head0 + row) * D + d) = rounded(o, inv);
+        auto place = [&](int c) __attribute__((always_inline)) { return (size_t)((w0 + c) * 2 + (c == 0 && u.begin > w0 * a.share ? 1 : 0)) * 16 + held; };
+        const float first = a.ws_ml[place(0) * 2 + 1];
+        const v4f o = joined(a.ws_ml, a.ws_o + d, D, parts, place, inv);
+        if (first != kNobodys) *reinterpret_cast<h4 *>(a.out + ((size_t)u.token * a.h_q + u.kv * a.g + u.head0 + row) * D + d) = rounded(o, inv);
     }
 }
 

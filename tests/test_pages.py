@@ -1000,6 +1000,79 @@ def test_attention_selected_extremes(h_q, h_kv, d, values):
         _close(got[t:t + 1], *q4.attention(q.reshape(3, h_q, d)[t:t + 1], K[b][:m], V[b][:m], P[b][:m], there))
 
 
+BROKEN = [  # token_start, context
+    ([0, 1, 2, 3], [2 ** 31 - 1, -5, 330]), ([0, 1 << 30, -4, 2], [400, 500, 330]), ([3, 2, 1, 0], [400, 2 ** 31 - 1, 330]), ([0, 5, 5, 8], [400, 500, 330]), ([0, 8, 8, 8], [3, 2, 1]),
+    ([-9, 4, 9, 1 << 30], [-2 ** 31, 500, 500]), ([0, 3, 1, 8], [400, 500, 330]), ([6, 2 ** 31 - 1, 0, 7], [1, 500, 0]),
+]
+
+
+@gpu
+@pytest.mark.parametrize("start,context", BROKEN)
+@pytest.mark.parametrize("limit", [8, 600])  # pages: scores in one launch, in two
+def test_bounds_and_selection_with_arrays_that_break_the_rules_stay_inside(start, context, limit):
+    rng = np.random.default_rng(52)
+    n, h_q, h_kv, d, T, count = [400, 500, 330], 4, 2, 64, 8, 5
+    table, num = _pages(rng, n)
+    cache, _, _, _ = _filled(rng, n, h_kv, d, table, num)
+    table = np.pad(table, ((0, 0), (0, limit - table.shape[1])), constant_values=-1)
+    table[1, 3], table[0, 2] = 2 ** 31 - 1, num
+    for longest in (500, 64 * limit):
+        req = B.Requests(_i(start), _i(context), _i(table), T, 2, min(longest, 64 * limit))
+        b = B.PageBounds(cache)
+        codes, steps = torch.full((b.codes.numel() + 512,), 7, dtype=torch.int8, device=DEV), torch.full((b.steps.numel() + 64,), 2.0, device=DEV)
+        b.desc.codes, b.desc.steps = codes.data_ptr() + 256, steps.data_ptr() + 128
+        B.qfc_bound_pages_q4(req, cache, b)
+        lists = torch.full((T + 2, h_kv, count), 99, dtype=torch.int32, device=DEV)
+        size = B.qfc_select_pages_q4_workspace_size(req, h_q, cache)
+        ws = torch.full((size + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+        B.qfc_select_pages_q4(_t(_normal(rng, T, h_q * d)), req, h_q, cache, b, 1, 1, lists[1:-1], ws[:size])
+        assert bool((codes[:256] == 7).all()) and bool((codes[-256:] == 7).all()) and bool((steps[:32] == 2).all()) and bool((steps[-32:] == 2).all())
+        assert bool((lists[0] == 99).all()) and bool((lists[-1] == 99).all()) and bool((ws[size:] == 0xFF).all())
+        inside = lists[1:-1][lists[1:-1] != 99]
+        assert bool(((inside >= -1) & (inside < limit)).all())
+
+
+@gpu
+@pytest.mark.parametrize("start,context", BROKEN)
+@pytest.mark.parametrize("count", [4, 17])  # lists whole, lists cut
+def test_attention_selected_with_arrays_that_break_the_rules_stays_inside(start, context, count):
+    rng = np.random.default_rng(53)
+    n, h_q, h_kv, d, T = [400, 500, 330], 4, 2, 64, 8
+    table, num = _pages(rng, n)
+    cache, _, _, _ = _filled(rng, n, h_kv, d, table, num)
+    table[1, 3], table[0, 2] = 2 ** 31 - 1, num
+    selected = rng.integers(-3, 12, (T, h_kv, count)).astype(np.int32)
+    selected[:, :, 1], selected[:, :, 2] = 2 ** 31 - 1, -2 ** 31
+    req = B.Requests(_i(start), _i(context), _i(table), T, 2, 500)
+    size = B.qfc_attention_selected_q4_workspace_size(req, h_q, cache, count)
+    ws = torch.full((size + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    out = torch.full((T + 2, h_q * d), 9.0, dtype=torch.float16, device=DEV)
+    B.qfc_attention_selected_q4(_t(_normal(rng, T, h_q * d)), req, h_q, cache, _i(selected), ws[:size], out[1:-1])
+    assert bool((out[0] == 9.0).all()) and bool((out[-1] == 9.0).all()) and bool((ws[size:] == 0xFF).all())
+
+
+@gpu
+@pytest.mark.parametrize("h_q,h_kv,d", [(4, 2, 64), (40, 2, 128), (3, 1, 256)])
+@pytest.mark.parametrize("count", [4, 17])  # lists whole, lists cut
+def test_attention_selected_leaves_what_is_nobodys(h_q, h_kv, d, count):
+    """Tokens that no request has: in front of the first, behind the last, and those of a request that are more than any may have."""
+    rng = np.random.default_rng(54)
+    n = [400, 1500]
+    table, num = _pages(rng, n)
+    cache, K, V, P = _filled(rng, n, h_kv, d, table, num)
+    q = _normal(rng, 10, h_q * d)
+    selected = np.tile(np.arange(count, dtype=np.int32), (10, h_kv, 1))
+    req = B.Requests(_i([1, 3, 8]), _i(n), _i(table), 10, 2, 1500)
+    got = _attend_selected(req, q, h_q, cache, _i(selected), fill=9.0).reshape(10, h_q, d)
+    for t in range(10):
+        if t in (1, 2, 3, 4):
+            b, lim = (0, 399 + t - 1) if t < 3 else (1, 1499 + t - 3)
+            lim = min(lim, 64 * count)
+            _close(got[t:t + 1], *q4.attention(q.reshape(10, h_q, d)[t:t + 1], K[b][:lim], V[b][:lim], P[b][:lim]))
+        else:
+            assert np.all(got[t] == 9.0), t
+
+
 @gpu
 def test_a_page_listed_twice_counts_twice():
     rng = np.random.default_rng(52)
