@@ -1,9 +1,9 @@
 // The pages of a cache as things that requests take, share, let go and are moved between: references[page] table entries name a page, none: it is free.
 //
 // Free pages are given lowest first and to entries in order, so that the result is the same whatever the order in which wavefronts run: the i-th entry that lacks a page gets the i-th free
-// page.  A first launch writes the free pages as a bit each, their number in every 1024 (a chunk), and how many pages each row lacks; in the second one a wavefront per row adds
-// up the rows before its own, finds the chunk its first page is in, and takes bits one after the other.  The bits are a copy: what other wavefronts enter into references meanwhile
-// changes nothing here.
+// page.  A first launch writes the free pages as a bit each, their number in every 1024 (a chunk), and how many pages each row lacks; in the last one a wavefront per row adds
+// up what the rows before its own lack (many rows: sums of runs, from a launch between the two), finds the chunk its first page is in, and takes bits one after the other.  The bits are a copy: what
+// other wavefronts enter into references meanwhile changes nothing here.
 #include "paged_q4.h"
 
 namespace qfc {
@@ -12,6 +12,9 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 1024, kWords = kChunk / 64;
+// Rows from which on what they lack is added up in runs, by a launch of its own.  One entry per row, us with and without: take of 2048 rows 25.2 and 21.7, of 4096 28.4 and 30.0, of 131072 208 and
+// 1820 (without, every row reads those of all before it); fork of 4096 rows 44.6 and 42.5, of 8192 63.5 and 78.0, of 131072 687 and 6860.
+constexpr int kRun = 1024, kManyRows = 4096;
 
 struct PagesArgs {
     char *pages;
@@ -24,7 +27,7 @@ struct PagesArgs {
     int from_batch, from_width;
     int *missing;        // or null
     uint64_t *bits;      // of free pages
-    int *free_of, *need;  // [chunks], [batch]
+    int *free_of, *need, *need_of;  // [chunks], [batch], [batch / kRun]
     int *source, *target, *before;  // compaction: moves, free pages before each chunk
     int chunks, slices;
     PageBounds bounds;  // of the pages, moved with them (codes null: none)
@@ -98,6 +101,19 @@ __global__ __launch_bounds__(256) void count_pages_kernel(PagesArgs a) {
         const int b = ((int)blockIdx.x - counting) * 4 + wave;
         if (b < a.batch) count_row<KIND>(a, b, lane);
     }
+}
+
+// What the rows of each whole run lack
+__global__ __launch_bounds__(256) void sum_rows_kernel(PagesArgs a) {
+    const int lane = threadIdx.x & 63, run = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (run >= a.batch / kRun) return;
+    const int sum = sum_of(a.need + (size_t)run * kRun, kRun, lane);
+    if (lane == 0) a.need_of[run] = sum;
+}
+// What the rows before b lack
+__device__ __forceinline__ int lacking_before(const PagesArgs &a, int b, int lane) {
+    if (a.batch <= kManyRows) return sum_of(a.need, b, lane);
+    return sum_of(a.need_of, b / kRun, lane) + sum_of(a.need + b / kRun * kRun, b % kRun, lane);
 }
 
 // The free pages from the rank-th on, in ascending order, up to 64 at a time
@@ -174,7 +190,7 @@ __device__ __forceinline__ void say_missing(const PagesArgs &a, int needed, int 
 
 // Pages for the entries of row b that lack one, by a wavefront
 __device__ __forceinline__ void take_row(const PagesArgs &a, int b, int lane, int *buffer) {
-    const int need = a.need[b], before = sum_of(a.need, b, lane);
+    const int need = a.need[b], before = lacking_before(a, b, lane);
     if (b == a.batch - 1) say_missing(a, before + need, lane);
     if (need == 0) return;
     FreePages free_pages(a, lane, before);
@@ -238,7 +254,7 @@ __global__ __launch_bounds__(256) void fork_pages_kernel(PagesArgs a) {
     int fresh = -1;
     const bool last = b == a.batch - 1 && slice == 0 && wave == 0;
     if (part.page >= 0 || (last && a.missing)) {
-        const int before = sum_of(a.need, b, lane);
+        const int before = lacking_before(a, b, lane);
         if (last) say_missing(a, before + (part.page >= 0), lane);
         if (part.page >= 0) {
             FreePages free_pages(a, lane, before);
@@ -370,12 +386,16 @@ PagesArgs args_of(const PagePool &pool, void *workspace, int batch) {
     a.bits = reinterpret_cast<uint64_t *>(part((size_t)a.chunks * kWords * 8));
     a.free_of = reinterpret_cast<int *>(part((size_t)a.chunks * 4));
     a.need = reinterpret_cast<int *>(part((size_t)batch * 4));
+    a.need_of = reinterpret_cast<int *>(part((size_t)(batch / kRun) * 4));
     a.before = reinterpret_cast<int *>(part((size_t)(a.chunks + 2) * 4));
     a.source = reinterpret_cast<int *>(part((size_t)(pool.num_pages / 2 + 1) * 4));
     a.target = reinterpret_cast<int *>(part((size_t)(pool.num_pages / 2 + 1) * 4));
     return a;
 }
 unsigned fours(long x) { return (unsigned)((x + 3) / 4); }
+void sum_rows(const PagesArgs &a, hipStream_t st) {
+    if (a.batch > kManyRows) sum_rows_kernel<<<fours(a.batch / kRun), 256, 0, st>>>(a);
+}
 // Workgroups per page: 16 KiB each where pages are many, as many as fill the card where they are few
 int slices_of(int page_bytes, long pages, int num_cus) {
     const long most = page_bytes / 4096 > 1 ? page_bytes / 4096 : 1, least = (page_bytes + 16383L) / 16384, fill = (2L * num_cus + pages - 1) / (pages > 0 ? pages : 1);
@@ -386,7 +406,7 @@ int slices_of(int page_bytes, long pages, int num_cus) {
 
 size_t pages_workspace(int num_pages, int batch) {
     const size_t chunks = ((size_t)num_pages + kChunk - 1) / kChunk;
-    return 256 + chunks * kWords * 8 + chunks * 8 + (size_t)batch * 4 + 2 * ((size_t)num_pages / 2 + 1) * 4 + 6 * 16;
+    return 256 + chunks * kWords * 8 + chunks * 8 + (size_t)batch * 4 + (size_t)(batch / kRun) * 4 + 2 * ((size_t)num_pages / 2 + 1) * 4 + 7 * 16;
 }
 
 hipError_t launch_copy_pages(const void *from, int from_pages, void *to, int to_pages, int page_bytes, const int *source, const int *target, int count, const PageBounds &from_bounds, const PageBounds &to_bounds,
@@ -405,6 +425,7 @@ hipError_t launch_take_pages(const PagePool &pool, int *table, const int *positi
         return hipGetLastError();
     }
     count_pages_kernel<kTake><<<fours(a.chunks) + fours(batch), 256, 0, st>>>(a);
+    sum_rows(a, st);
     take_pages_kernel<<<fours(batch), 256, 0, st>>>(a);
     return hipGetLastError();
 }
@@ -418,6 +439,7 @@ hipError_t launch_fork_pages(const PagePool &pool, const int *from, int from_bat
     a.slices = slices_of(a.page_bytes, batch, num_cus);
     while ((long)batch * a.slices > 1L << 23) a.slices = (a.slices + 1) / 2;  // (a launch has fewer than 2^32 threads; batch is below 2^23)
     count_pages_kernel<kFork><<<fours(a.chunks) + fours(batch), 256, 0, st>>>(a);
+    sum_rows(a, st);
     fork_pages_kernel<<<(unsigned)batch * a.slices, 256, 0, st>>>(a);
     return hipGetLastError();
 }

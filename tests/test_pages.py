@@ -284,6 +284,15 @@ def test_fork_pages(num, parents, children, from_width, width, share, h_kv, d):
 
 
 @gpu
+@pytest.mark.parametrize("batch", [4096, 4097, 5119, 5120, 5121, 9001])
+def test_rows_by_the_thousand(batch):
+    """What many rows lack is added up in runs of 1024."""
+    test_take_pages(2 * batch, batch, 3, 0.3)
+    test_take_pages(batch // 2, batch, 1, 0.1)
+    test_fork_pages(batch + 500, 40, batch, 3, 4, 0.3, 1, 64)
+
+
+@gpu
 @pytest.mark.parametrize("num,batch,width", [(3, 1, 1), (100, 7, 33), (5000, 300, 100)])
 def test_free_pages(num, batch, width):
     rng = np.random.default_rng(num)
