@@ -261,17 +261,17 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
 
 // ---- common pages of many rows.  What attention_q4_rows.h does to a page for 16 query rows, most of its instructions, is to take its codes apart: 551 vector instructions of a page and 16 rows,
 // of which 192 for that.  Here the four wavefronts of a workgroup take a page's codes apart once, into LDS as binary16 whole numbers code - 8 (exact, as are the products with the queries), and
-// multiply them with 32 rows each (310 instructions of a page and 16 rows); steps, offsets and P are taken into the sums in the same way and with the same precision as there, steps of 1 and
-// more (there: 2) in a turn of their own:
+// multiply them with 32 rows each (335 instructions of a page and 16 rows); steps, offsets and P are taken into the sums in the same way and with the same precision as there, steps of 2 and
+// more in a turn of their own (where every page has some: 1024 rows behind 20011 positions 214 -> 355 us):
 //   q . k = sum_j step_j (q_j . (code_j - 8)) + sum_j offset_j sum q_j,   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
-// The common pages are in front of all rows' positions: nothing is masked.  Bound: the LDS, 63 reads of a KiB of a page and wavefront at 64 bytes a cycle, beside vector instructions in 64 % of the
-// cycles (1024 rows of 8 heads of 128 values behind 20000 positions 167 us: 500 TFLOP/s).
+// The common pages are in front of all rows' positions: nothing is masked.  Bound: the LDS, 63 reads of a KiB of a page and wavefront at 64 bytes a cycle, beside vector instructions in 71 % of the
+// cycles (1024 rows of 8 heads of 128 values behind 20000 positions 170 us: 490 TFLOP/s).
 template <int D>
 struct Wide {
     typedef PageLayout<D> L;
     static constexpr int G = L::G, W = L::W, DT = D / 16, NB = 2, ROWS = 64 * NB;
-    // LDS: K operands [4 tiles][G][64 lanes], V operands [G][low, high][2 halves of 16 positions][64 lanes], 16 bytes each; then the page's steps and offsets of keys, and of values: steps below 1
-    // (zeros for the others), offsets, steps of 1 and more (zeros for the others)
+    // LDS: K operands [4 tiles][G][64 lanes], V operands [G][low, high][2 halves of 16 positions][64 lanes], 16 bytes each; then the page's steps and offsets of keys, and of values: steps below 2
+    // (zeros for the others), offsets, steps of 2 and more (zeros for the others)
     static constexpr int kV = 128 * D, kHeadK = 256 * D, kHeadV = 264 * D, kBytes = 276 * D;
     static constexpr int kStepK = kHeadK, kOffsetK = kHeadK + 4 * D, kStepV = kHeadV, kOffsetV = kHeadV + 4 * D, kLargeV = kHeadV + 8 * D;
     // A page on its way: what a thread has of it
@@ -317,7 +317,7 @@ struct Wide {
         u32x4 large = {};
         if (piece >= D / 2 && piece < D / 2 + D / 4) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) large[i] = head[i] & (head[i] + 0x04000400u >> 14 & 0x00010001u) * 0xFFFFu;  // (exponents from 1.0's on)
+            for (int i = 0; i < 4; ++i) large[i] = head[i] & (head[i] >> 14 & 0x00010001u) * 0xFFFFu;  // (exponents from 2.0's on)
             *reinterpret_cast<u32x4 *>(lds + kLargeV + (piece - D / 2) * 16) = large;
         }
         *reinterpret_cast<u32x4 *>(lds + kHeadK + piece * 16) = head & ~large;
@@ -333,10 +333,11 @@ struct WideRows {
     h8 qf[NB][G], sums[NB];
     float to_score[NB], run_max[NB];
     v4f acc[NB][DT], rest[NB];
-    // The maximum may be kLag below a score (in units of log 2): what hardly moves it costs no pass over the sums.  P is taken 2^kAt times as large, at most 2^15 then, and its products with
-    // steps below 1 are smaller: binary16 keeps as many bits of small ones as in attention_q4_rows.h.  (256 requests behind 20011 positions: a lag of 1 211 us; of 2, with P half as large, 209.)
-    static constexpr int kLag = 1, kAt = (int)kFactor;
-    static_assert(kAt + kLag <= 15, "P is rounded to binary16, which holds twice as much");
+    // The maximum may be kLag below a score (in units of log 2): what hardly moves it costs no pass over the sums.  P is taken 2^kAt times as large, at most 2^14.5 then, and its products with
+    // steps below 2 are below 2^15.5: binary16 keeps as many bits of small ones as in attention_q4_rows.h.  (1024 rows behind 20011 positions 214 us with all that is behind them; with a lag of 2
+    // and P a quarter as large 209.)
+    static constexpr float kLag = 0.5f, kAt = kFactor;
+    static_assert(kAt + kLag + 1.0f <= 15.5f, "binary16 holds 2^16: a part of it is for what scores of thousands are rounded by");
     __device__ __forceinline__ WideRows(int l) : lane(l), m(l & 15), r(l >> 4) {}
 
     __device__ __forceinline__ void load(int nb, const _Float16 *q, bool real, float scale) {
@@ -441,7 +442,7 @@ struct WideRows {
 #pragma unroll
             for (int e = 2; e < 16; e += 2) most[nb] = fmaxf(fmaxf(most[nb], sc[nb][e]), sc[nb][e + 1]);
             most[nb] = over_rows(most[nb]) * to_score[nb];
-            more = more || most[nb] > run_max[nb] + (float)kLag;
+            more = more || most[nb] > run_max[nb] + kLag;
         }
         if (__any(more)) {
 #pragma unroll
@@ -458,7 +459,7 @@ struct WideRows {
         }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            const float from_max = (float)kAt - run_max[nb];
+            const float from_max = kAt - run_max[nb];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 sc[nb][e] = __builtin_amdgcn_exp2f(fmaf(sc[nb][e], to_score[nb], from_max));
@@ -473,7 +474,7 @@ struct WideRows {
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) rest[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, rows), pv[nb][u], rest[nb], 0, 0, 0);
         }
-        // Steps below 1; those of 1 and more in a turn of their own behind it, with each row's P lowered until its largest product with one of them is below 2^15 (by powers of two: exact in P and in
+        // Steps below 2; those of 2 and more in a turn of their own behind it, with each row's P lowered until its largest product with one of them is below 2^15 (by powers of two: exact in P and in
         // sums of 32 bits): what binary16 then loses is little against a product that is in the row's sums, and the small steps, in this page and the others, keep their bits.
         auto product = [&](Lds steps) __attribute__((always_inline)) {
             h8 step[2], lo[2], hi[2];
@@ -760,8 +761,9 @@ constexpr int kMostParts = 16;
 // Rows of partial results per compute unit, beside one part of all rows: with 256 compute units 16 parts of 273 tokens of 32 heads.  (Blocks that fill the card with their rows need 16 kWgs of them, or 128
 // kWgs where they are of 128 rows: more only where most of a call's rows are nobody's or in no group.)
 constexpr long kKeptRows = 256 * kWgs;
-// Rows and common pages of a group times heads and their size per compute unit from which on pages are taken apart for a workgroup.  Both ways' times, us, with 8 KV heads of 128 values: 512 rows
-// behind 6000 positions 50 and 63, behind 20000 116 and 107; 1024 rows 85 and 94, 219 and 186; with 4 heads of 64: 1024 rows behind 20000 75 and 79.
+// Rows and common pages of a group times heads and their size per compute unit from which on pages are taken apart for a workgroup.  Both ways' times, us, with 8 KV heads of 128 values: 256 rows
+// behind 40000 positions 108 and 117, 60000 163 and 159; 512 rows behind 6000 50 and 63, 16000 90 and 94, 20000 110 and 109, 26000 137 and 130; 1024 rows behind 6000 79 and 91, 20000 203 and 184; with
+// 4 heads of 64: 1024 rows behind 20000 72 and 79.  (640 and 768 rows make a few more workgroups than the card has at once, and are slower: behind 20000 146 and 170, 14000 111 and 151.)
 constexpr long kWideFrom = 600000;
 // Workgroups that share a block's pages: as many as fill the card, each with a page per wavefront at least
 int parts_of(long blocks, int pages, int num_cus) {
