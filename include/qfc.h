@@ -400,7 +400,7 @@ qfc_status_t qfc_attention_q4(const void *q_f16, const qfc_requests_t *requests,
  * references: device, int32 [num_pages] of a cache: how many table entries name a page; 0 (or less): the page is free.  A cache's first references are zeros; the calls below keep
  * them, as long as all tables of the cache are changed by them alone.  They run on the device, in order on the stream, and may be captured: nothing about pages has to be known to the
  * host.  Free pages are given lowest number first, to the entries in order (row by row), whatever the hardware's timing.  A page belongs to the cache it is in: references of
- * one cache say nothing about another's.
+ * one cache say nothing about another's.  (Caches of several layers behind one table: every call is made for each of them, on copies of the same table and references, which come out the same.)
  *   page_table    device, int32 [batch, table_width], changed by the call; an entry outside [0, num_pages) is no page
  *   missing       device, int32 [1], or null: how many entries got no page because none was free (they are -1, and attention does not see their positions)
  *   bounds        host, or null: bounds of the keys of all pages (below), which belong to a page's number; they go where a page's contents go
@@ -458,7 +458,8 @@ typedef struct qfc_shared {
 
 /* qfc_attention_q4 for requests of which groups have common pages: the same result up to roundings, with what is common read and multiplied once for all rows of a group (from the table
  * row of its first request with tokens).  workspace: device scratch of at least the size's bytes, one call's at a time; a size is enough for every smaller call too (fewer tokens, limits no
- * larger, fewer groups), so that a server needs that of its largest one.  Errors as qfc_attention_q4; QFC_ERR_INVALID_ARG for null pointers and sizes below 1 in `shared`, QFC_ERR_UNSUPPORTED for groups * h_kv above 65535. */
+ * larger, fewer groups), so that a server needs that of its largest one.  Errors as qfc_attention_q4; QFC_ERR_INVALID_ARG for null pointers and sizes
+ * below 1 in `shared`, QFC_ERR_UNSUPPORTED for groups * h_kv above 65535. */
 qfc_status_t qfc_attention_shared_q4_workspace_size(const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, size_t *bytes);
 qfc_status_t qfc_attention_shared_q4(const void *q_f16, const qfc_requests_t *requests, const qfc_shared_t *shared, int32_t h_q, const qfc_q4_cache_t *cache, void *workspace,
                                      size_t workspace_bytes, void *out_f16, void *stream);

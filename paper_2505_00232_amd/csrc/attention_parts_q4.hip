@@ -261,11 +261,11 @@ __global__ __launch_bounds__(256) void attn_q4_join_selected_kernel(SelectedArgs
 
 // ---- common pages of many rows.  What attention_q4_rows.h does to a page for 16 query rows, most of its instructions, is to take its codes apart: 551 vector instructions of a page and 16 rows,
 // of which 192 for that.  Here the four wavefronts of a workgroup take a page's codes apart once, into LDS as binary16 whole numbers code - 8 (exact, as are the products with the queries), and
-// multiply them with 32 rows each (335 instructions of a page and 16 rows); steps, offsets and P are taken into the sums in the same way and with the same precision as there, steps of 2 and
+// multiply them with 32 rows each (342 instructions of a page and 16 rows); steps, offsets and P are taken into the sums in the same way and with the same precision as there, steps of 2 and
 // more in a turn of their own (where every page has some: 1024 rows behind 20011 positions 214 -> 355 us):
 //   q . k = sum_j step_j (q_j . (code_j - 8)) + sum_j offset_j sum q_j,   out_d = sum_p (p step_j) (code - 8) + sum_p p offset_j
 // The common pages are in front of all rows' positions: nothing is masked.  Bound: the LDS, 63 reads of a KiB of a page and wavefront at 64 bytes a cycle, beside vector instructions in 71 % of the
-// cycles (1024 rows of 8 heads of 128 values behind 20000 positions 170 us: 490 TFLOP/s).
+// cycles (1024 rows of 8 heads of 128 values behind 20000 positions 173 us: 485 TFLOP/s).
 template <int D>
 struct Wide {
     typedef PageLayout<D> L;
@@ -762,8 +762,8 @@ constexpr int kMostParts = 16;
 // kWgs where they are of 128 rows: more only where most of a call's rows are nobody's or in no group.)
 constexpr long kKeptRows = 256 * kWgs;
 // Rows and common pages of a group times heads and their size per compute unit from which on pages are taken apart for a workgroup.  Both ways' times, us, with 8 KV heads of 128 values: 256 rows
-// behind 40000 positions 108 and 117, 60000 163 and 159; 512 rows behind 6000 50 and 63, 16000 90 and 94, 20000 110 and 109, 26000 137 and 130; 1024 rows behind 6000 79 and 91, 20000 203 and 184; with
-// 4 heads of 64: 1024 rows behind 20000 72 and 79.  (640 and 768 rows make a few more workgroups than the card has at once, and are slower: behind 20000 146 and 170, 14000 111 and 151.)
+// behind 40000 positions 108 and 117, 60000 163 and 160; 512 rows behind 6000 50 and 63, 16000 90 and 94, 22000 120 and 117, 26000 138 and 131; 1024 rows behind 6000 79 and 91, 20000 203 and 186; with
+// 4 heads of 64: 1024 rows behind 20000 72 and 79.  (640 and 768 rows make a few more workgroups than the card has at once, and are slower: behind 20000 147 and 171, 14000 114 and 152.)
 constexpr long kWideFrom = 600000;
 // Workgroups that share a block's pages: as many as fill the card, each with a page per wavefront at least
 int parts_of(long blocks, int pages, int num_cus) {

@@ -49,8 +49,8 @@ struct Place {
 //
 // SPREAD: 16 / G rows (a token's few heads), each G times, once for every group of 32 values: column m = (16 / G) a + b of the products is row b with group a's queries alone.  The products of all groups
 // then go into one sum, every lane multiplies with its own group's steps (a G-th of the multiplications and of the reads of steps), and the G columns of a row are added up; P times a step is
-// one product per position too, and of the second product's columns those of group a are good for the values of group a.  (A chunk of 157 tokens, 2 heads of 256 values on each of 4, 17 pages a token: 45 us, without 53; 32 tokens, 4 heads of 128 on
-// each of 8, 32 pages a token: 18.6 and 19.8.)
+// one product per position too, and of the second product's columns those of group a are good for the values of group a.  (Chunks of 150 and 24 tokens, 2 heads of
+// 256 values on each of 4, 17 pages a token: 45 us, without 53; 32 tokens, 4 heads of 128 on each of 8, 32 pages a token: 18.6 and 19.8.)
 template <int D, bool SPREAD = false>
 struct Rows {
     typedef PageLayout<D> L;

@@ -426,7 +426,7 @@ hipError_t launch_select_pages_q4(const void *q, const Requests &req, int h_q, i
 struct AttnPartsPlan {
     long prefix_blocks, blocks;  // of 16 query rows of a KV head: of groups (common pages), of requests
     int prefix_parts, parts;     // runs that their pages are cut into
-    bool wide;                   // groups of many rows: blocks of 64 or 128
+    bool wide;                   // groups of many rows: blocks of 128
     size_t bytes;                // of the workspace
 };
 struct SelectedPlan {
