@@ -480,6 +480,35 @@ def test_pages_captured_and_replayed():
 
 
 @gpu
+def test_layers_behind_one_table():
+    """Caches of several layers, of heads of their own: the calls on copies of one table and its references give one table, and every cache holds what it names."""
+    rng = np.random.default_rng(65)
+    num, batch, width, kids = 900, 12, 9, 40
+    order = rng.permutation(num)[:batch * 5].reshape(batch, 5)
+    table = np.full((batch, width), -1, np.int32)
+    table[:, :5] = order
+    refs = np.bincount(order.ravel(), minlength=num).astype(np.int32)
+    parents, positions = rng.integers(0, batch, kids).astype(np.int32), rng.integers(1, 320, kids).astype(np.int32)
+    came_out = []
+    for h_kv, d in ((1, 64), (2, 128), (1, 256)):
+        pool = Pool(num, h_kv, d, np.random.default_rng(h_kv * d))
+        t, r, child, used = _i(table), _i(refs), _i(np.full((kids, width), -1)), _i([0])
+        space = pool.space(kids)[0]
+        B.qfc_fork_pages(pool.cache, r, t, _i(parents), _i(positions), child, space)
+        B.qfc_free_pages(pool.cache, r, t)
+        B.qfc_take_pages(pool.cache, r, child, _i(positions + 70), space)
+        B.qfc_compact_pages(pool.cache, r, child, space, used)
+        kid, want, pages, _ = ref.fork(table, refs, parents, positions, width, pool.pages)
+        _, want = ref.free(table, want)
+        kid, want, _ = ref.take(kid, want, positions + 70)
+        kid, want, pages, count = ref.compact(kid, want, pages)
+        assert np.array_equal(pool.now(), pages) and int(used) == count
+        came_out.append((child.cpu().numpy(), r.cpu().numpy()))
+        assert np.array_equal(came_out[-1][0], kid) and np.array_equal(came_out[-1][1], want)
+    assert all(np.array_equal(a, b) for x in came_out[1:] for a, b in zip(came_out[0], x))
+
+
+@gpu
 def test_pages_of_almost_two_gibibytes():
     """The largest page that is not refused: copied, forked and moved whole."""
     h_kv, d = (2 ** 31 - 1) // (80 * 64), 64
